@@ -267,6 +267,152 @@ mosa_status mosa_check_status(const mosa_shape *shape, void *workspace, void *st
 mosa_status mosa_route_noalloc(const mosa_shape *shape, const void *X, const void *W_r,
                                int32_t *I, float *r_sel, void *stream);
 
+/* ---- Window heads: operators beside the MoSA heads -----------------------
+ * Local heads as a language model trains and serves them: queries and keys
+ * normalised per head and turned by their positions, attention within a
+ * sliding window with a few first tokens that stay visible (sinks), and the
+ * single-token form of both over a ring cache.  These calls take strided
+ * tensors and groups of query heads that share a key / value head, so the
+ * q | k | v rows of one projection can be passed as they are.
+ *
+ * Conventions shared by these calls (where they differ from the layer's):
+ *   - A tensor is a device pointer and the strides, in elements, of its
+ *     sequences (b), tokens (t) and heads (h); the hp values of one head are
+ *     contiguous.  Strides are >= 0; where a size is 1 its stride is ignored.
+ *     Inputs may overlap (stride 0 repeats a row); outputs may not, neither
+ *     within themselves nor with inputs.
+ *   - q, o (and their gradients) have H heads, k and v Hkv; query head h uses key /
+ *     value head h / (H / Hkv).
+ *   - Storage dtype as in mosa_dtype for every tensor but lse, dgamma_*, lens
+ *     and positions.  Sums, softmax statistics and norms are held in fp32;
+ *     outputs are rounded to the storage dtype once.
+ *   - Tensors start at a multiple of their element size.  Where pointers are
+ *     multiples of 16 bytes and strides of 16 bytes' worth of elements, the fast kernels
+ *     run (bf16: tensor cores); elsewhere slower ones that compute the same.
+ *   - Sizes: hp in {16, 32, 64, 128} as for the layer; B, H <= 65535; fewer than
+ *     2^30 tokens (else MOSA_ERR_UNSUPPORTED).  The attention needs H % Hkv == 0
+ *     (else MOSA_ERR_INVALID_ARG); the norm takes any H and Hkv.
+ *   - Nothing is captured into graphs by these calls, so they can be captured by
+ *     the caller (after one call outside the capture, which loads the kernels).
+ *   - MOSA_FORCE_SIMT=1 runs the CUDA-core kernels only, as for the layer. */
+typedef struct {
+    int64_t b, t, h;
+} mosa_strides;
+
+/* Norm and rotation of queries and keys (Sec. 2.2, positional encodings, with
+ * the RMS norm of queries and keys before it): for each head x of each token at
+ * position t
+ *     n = x / sqrt(mean(x^2) + eps) * gamma,      y = R(t) n
+ * where R(t) turns pair p of the first `rotary` dimensions by
+ * t * theta^(-2p / rotary): pair (2p, 2p+1), or with halves = 1
+ * (p, p + rotary/2).  The layer's own rotation is rotary = hp/2, theta = 10000,
+ * halves = 0.  Sizes: rotary even and 0 <= rotary <= hp (0: no rotation); with halves = 1
+ * rotary is 8 or a multiple of 16 (else MOSA_ERR_UNSUPPORTED); eps >= 0; theta >= 1. */
+typedef struct {
+    int32_t B, T, H, Hkv, hp;
+    int32_t dtype;
+    int32_t rotary, halves;
+    float theta, eps;
+    mosa_strides q, k;    /* inputs */
+    mosa_strides yq, yk;  /* outputs; in the backward their gradients */
+    mosa_strides dq, dk;  /* backward only: gradients of the inputs */
+} mosa_qk_shape;
+
+/* Forward.  q [B,T,H,hp], k [B,T,Hkv,hp]; gamma_q, gamma_k [hp] in the storage
+ * dtype, or NULL for ones; positions [B,T] int32, or NULL for 0..T-1 (any
+ * value; the angle is exact in 64-bit fixed point); yq, yk outputs, which may
+ * be q and k themselves (same pointer and strides).  Keys may be written
+ * straight into a cache through yk's strides.  Needs no workspace. */
+mosa_status mosa_qk_norm_rope(const mosa_qk_shape *shape, const void *q, const void *k,
+                              const void *gamma_q, const void *gamma_k,
+                              const int32_t *positions, void *yq, void *yk, void *stream);
+
+/* Workspace of the backward (256-byte aligned); 0 if the shape is invalid. */
+size_t mosa_qk_norm_rope_workspace_bytes(const mosa_qk_shape *shape);
+
+/* Backward: from the inputs and the gradients dyq, dyk of the outputs, dq and
+ * dk (which may be dyq and dyk themselves) and, where not NULL, dgamma_q, dgamma_k [hp] fp32 (sums
+ * over all tokens and heads, in a fixed order: the same bits every time). */
+mosa_status mosa_qk_norm_rope_backward(const mosa_qk_shape *shape, const void *q, const void *k,
+                                       const void *gamma_q, const void *gamma_k,
+                                       const int32_t *positions, const void *dyq,
+                                       const void *dyk, void *dq, void *dk, float *dgamma_q,
+                                       float *dgamma_k, void *workspace, size_t workspace_bytes,
+                                       void *stream);
+
+/* Sliding-window attention with sinks.  Queries are the last Tq of Tk tokens:
+ * query i stands at position p = Tk - Tq + i and sees token t iff
+ *     t <= p  and  (p - t < window  or  t < sinks)  and  p, t < lens[b]
+ * (window = 0: no limit, as for the hybrid layer's dense heads).
+ *     S = scale q k^T,  P = softmax over the visible tokens,  O = P v
+ * scale = 0 stands for 1/sqrt(hp).  A query that sees nothing (p >= lens[b])
+ * gets O = 0, lse = -inf and no gradient.  What a masked place holds, NaN and
+ * infinities among them, reaches no output that does not see it; a visible
+ * NaN or infinity makes the results that it reaches NaN or infinite.
+ * 0 <= window; 0 <= sinks; 1 <= Tq <= Tk. */
+typedef struct {
+    int32_t B, Tq, Tk, H, Hkv, hp;
+    int32_t dtype;
+    int32_t window, sinks;
+    float scale;
+    mosa_strides q, k, v, o;        /* forward */
+    mosa_strides go, dq, dk, dv;    /* backward only: of dO and the gradients */
+} mosa_window_shape;
+
+/* Workspace of a forward or backward (256-byte aligned); 0 if the shape is invalid or
+ * unsupported.  Nothing in it is kept between calls but the status word in its
+ * first 4 bytes: zero those once, before the workspace's first call. */
+size_t mosa_window_workspace_bytes(const mosa_window_shape *shape);
+
+/* Forward: q [B,Tq,H,hp], k and v [B,Tk,Hkv,hp], lens [B] int32 or NULL (all
+ * Tk; values outside 0..Tk count as the nearer end); outputs O [B,Tq,H,hp] in
+ * the storage dtype and lse [B,H,Tq] fp32, the log-sum-exp of each query's
+ * visible scores, which the backward needs (NULL if not wanted). */
+mosa_status mosa_window_forward(const mosa_window_shape *shape, const void *q, const void *k,
+                                const void *v, const int32_t *lens, void *O, float *lse,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* Backward: from the forward's inputs and outputs and dO, the gradients dq, dk
+ * and dv in the storage dtype, dk and dv summed over the query heads that share them.
+ * Sums run in a fixed order: the same bits every time. */
+mosa_status mosa_window_backward(const mosa_window_shape *shape, const void *q, const void *k,
+                                 const void *v, const int32_t *lens, const void *O,
+                                 const float *lse, const void *dO, void *dq, void *dk, void *dv,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* Waits for `stream`, then reads and clears the status word of a window call's
+ * workspace: MOSA_OK or MOSA_ERR_DEVICE_TIMEOUT. */
+mosa_status mosa_window_check_status(void *workspace, void *stream);
+
+/* One decoding step over a ring cache.  Sequence b has lens[b] tokens, the new
+ * one included (position lens[b] - 1); its token t < sinks is kept in slot t,
+ * the others in slot sinks + (t - sinks) % (C - sinks), so C slots hold the
+ * sinks and the last C - sinks tokens whatever the length.  The step
+ *   1. with norm = 1 normalises the new token's q and k per head (gamma_q, gamma_k
+ *      as in mosa_qk_norm_rope), and turns them to its position (rotary > 0),
+ *   2. writes k (rounded to the storage dtype) and v into its slot,
+ *   3. attends over the visible tokens as mosa_window_forward does.
+ * A window larger than C - sinks is limited to what the cache holds (0: all of it).  lens[b] <= 0: the sequence is skipped, its
+ * cache unchanged and its output 0.
+ *   q, o [B,H,hp], k, v [B,Hkv,hp] (strides b and h; t ignored); K_cache, V_cache
+ *   [B,C,Hkv,hp] by strides, slots not yet written may hold anything; C > sinks. */
+typedef struct {
+    int32_t B, C, H, Hkv, hp;
+    int32_t dtype;
+    int32_t window, sinks;
+    int32_t norm, rotary, halves;
+    float scale, theta, eps;
+    mosa_strides q, k, v, o;
+    mosa_strides kc, vc;
+} mosa_decode_shape;
+
+size_t mosa_window_decode_workspace_bytes(const mosa_decode_shape *shape);
+
+mosa_status mosa_window_decode(const mosa_decode_shape *shape, const void *q, const void *k,
+                               const void *v, const void *gamma_q, const void *gamma_k,
+                               const int32_t *lens, void *K_cache, void *V_cache, void *O,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- Measurement support (not part of the layer) ----------------------
  * Stages: 0 router, 1 select, 2 qkv, 3 attn_fwd, 4 out, 5 out_bwd,
  * 6 attn_bwd, 7 in_bwd, 8 w_bwd, 9 dwo (dW_o), 10 fwd_unit (F3-F5 fused,

@@ -17,8 +17,16 @@ __all__ = ["mosa_forward", "mosa_forward_with_indices", "mosa_backward", "mosa_t
            "mosa_hybrid_workspace_bytes", "alloc_hybrid_workspace", "mosa_hybrid_forward",
            "mosa_hybrid_backward"]
 
+#: The window heads' calls (``_window``).
+_WINDOW = ["mosa_qk_norm_rope", "mosa_qk_norm_rope_backward", "mosa_window_forward",
+           "mosa_window_backward", "mosa_window_check_status", "mosa_window_decode"]
+__all__ += _WINDOW
+
 
 def __getattr__(name):
+    if name in _WINDOW:
+        from . import _window
+        return getattr(_window, name)
     if name in __all__:
         from . import _binding
         return getattr(_binding, name)

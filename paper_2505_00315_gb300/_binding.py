@@ -31,7 +31,10 @@ EXPORTED = ("mosa_status_string", "mosa_workspace_bytes", "mosa_forward",
             "mosa_stage_name", "mosa_stage_engine", "mosa_route_noalloc", "mosa_adaptive_k",
             "mosa_hybrid_workspace_bytes", "mosa_hybrid_forward", "mosa_hybrid_backward",
             "mosa_profile_spans", "mosa_profile_timeline", "mosa_profile_timeline_read",
-            "mosa_profile_spans_copy")
+            "mosa_profile_spans_copy", "mosa_qk_norm_rope", "mosa_qk_norm_rope_workspace_bytes",
+            "mosa_qk_norm_rope_backward", "mosa_window_workspace_bytes", "mosa_window_forward",
+            "mosa_window_backward", "mosa_window_check_status",
+            "mosa_window_decode_workspace_bytes", "mosa_window_decode")
 
 
 class MosaShape(ctypes.Structure):
@@ -128,6 +131,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         L.mosa_hybrid_forward.restype = ctypes.c_int
         L.mosa_hybrid_backward.argtypes = [hp_] + [vp] * 10 + [vp, vp, vp] + [vp] * 10 + [vp, sz, vp]
         L.mosa_hybrid_backward.restype = ctypes.c_int
+        from . import _window
+        _window.declare(L)
         _lib = L
         return L
 

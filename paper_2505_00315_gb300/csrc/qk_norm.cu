@@ -1,0 +1,253 @@
+// Norm and rotation of queries and keys, one pass over each (Sec. 2.2, positional
+// encodings, after an RMS norm per head):
+//     r = 1/sqrt(mean(x^2) + eps),  n = r x gamma,  y = R(t) n
+// and backward, with g = R(t)^T dy (the rotation's transpose turns back),
+//     dgamma = sum g r x,  u = g gamma,  dx = r (u - r x mean(u r x)).
+// Memory bound: x and y move once, forward; x, dy and dx backward (r is computed
+// again from x, which is read anyway).  A head's hp values lie on hp/8 lanes, eight a
+// lane (16 bytes of bf16), so the mean is a few shuffles and nothing is staged; a
+// block takes some tokens with all their heads and computes each token's sines
+// and cosines once for all of them, in shared memory.
+#include <cmath>
+
+#include "head_rows.cuh"
+#include "launch.h"
+#include "profile.h"
+#include "window.h"
+
+namespace mosa {
+namespace win {
+
+Turns make_turns(int rotary, double theta) {
+    Turns t{};
+    const double two_pi = 6.283185307179586476925286766559;
+    for (int p = 0; p < rotary / 2 && p < 64; ++p) {
+        const double turns = std::pow(theta, -2.0 * p / rotary) / two_pi;   // <= 0.16
+        t.phi[p] = (uint64_t)(turns * 18446744073709551616.0);
+    }
+    return t;
+}
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTokens = 4;   // tokens of one block's step
+constexpr int kBatch = 4;       // heads whose loads a lane keeps in flight
+
+struct NormArgs {
+    Norm n;
+    const void *q, *k, *gq, *gk, *dyq, *dyk;
+    void *oq, *ok;          // forward: y; backward: dx
+    const int32_t *pos;
+    float *partial;         // backward: [blocks][2][hp] partial sums of dgamma
+    int tokens;             // of one step: 1 .. kMaxTokens
+};
+
+// Sines and cosines of `tokens` tokens from token0 (of B*T) on.
+__device__ __forceinline__ void fill_angles(float2 (*cs)[64], const NormArgs &p, const Turns &tab,
+                                            long long token0, int tokens) {
+    const int pairs = p.n.rotary >> 1;
+    for (int e = threadIdx.x; e < tokens * pairs; e += kThreads) {
+        const int i = e / pairs, a = e - i * pairs;
+        const long long tok = token0 + i;
+        const int t = p.pos != nullptr ? p.pos[tok] : (int)(tok % p.n.T);
+        cs[i][a] = angle_of(tab.phi[a], t);
+    }
+}
+
+// Where head hh of token tok lies: heads 0 .. H-1 are queries, the rest keys.
+struct Place {
+    bool key;
+    long long b, t;
+    int h;
+};
+__device__ __forceinline__ Place place(const Norm &n, long long tok, int hh) {
+    Place w;
+    w.key = hh >= n.H;
+    w.h = w.key ? hh - n.H : hh;
+    w.b = tok / n.T;
+    w.t = tok - w.b * n.T;
+    return w;
+}
+
+template <class T, bool VEC, bool kBackward>
+__global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_constant__ NormArgs p,
+                                                                const __grid_constant__ Turns tab) {
+    __shared__ float2 cs[kMaxTokens][64];
+    extern __shared__ float red[];   // backward: [groups][2][hp]
+    const Norm &n = p.n;
+    const int lanes = n.hp >> 3, groups = kThreads / lanes, lane = threadIdx.x & 31;
+    const int grp = threadIdx.x / lanes, c = (threadIdx.x % lanes) * 8;
+    const int HH = n.H + n.Hkv;
+    const long long N = (long long)n.B * n.T;
+    float gq[8], gk[8], aq[8], ak[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 1.f, aq[e] = ak[e] = 0.f;
+    if (p.gq != nullptr) load8<T, false>((const T *)p.gq + c, gq);
+    if (p.gk != nullptr) load8<T, false>((const T *)p.gk + c, gk);
+    for (long long tok0 = (long long)blockIdx.x * p.tokens; tok0 < N;
+         tok0 += (long long)gridDim.x * p.tokens) {
+        const int tokens = (int)min((long long)p.tokens, N - tok0);
+        __syncthreads();   // the last step's angles have been read
+        fill_angles(cs, p, tab, tok0, tokens);
+        __syncthreads();
+        const int items = tokens * HH;
+        for (int it0 = 0; it0 < items; it0 += kBatch * groups) {
+            float x[kBatch][8], g[kBackward ? kBatch : 1][8];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int it = it0 + u * groups + grp;
+                if (it < items) {
+                    const Place w = place(n, tok0 + it / HH, it % HH);
+                    load8<T, VEC>(w.key ? (const T *)p.k + n.k.at(w.b, w.t, w.h) + c
+                                        : (const T *)p.q + n.q.at(w.b, w.t, w.h) + c,
+                                  x[u]);
+                    if (kBackward)
+                        load8<T, VEC>(w.key ? (const T *)p.dyk + n.yk.at(w.b, w.t, w.h) + c
+                                            : (const T *)p.dyq + n.yq.at(w.b, w.t, w.h) + c,
+                                      g[kBackward ? u : 0]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[u][e] = g[kBackward ? u : 0][e] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int it = it0 + u * groups + grp;
+                const bool on = it < items;
+                const int i = on ? it / HH : 0;
+                const Place w = place(n, tok0 + i, on ? it % HH : 0);
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = fmaf(x[u][e], x[u][e], ss);
+                const float r = rsqrtf(group_sum(ss, lanes) / (float)n.hp + n.eps);
+                if (!kBackward) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[u][e] *= r * (w.key ? gk[e] : gq[e]);
+                    turn8(x[u], c, n.rotary, n.halves, cs[i], 1.f, lane);
+                    if (on)
+                        store8<T, VEC>(w.key ? (T *)p.ok + n.yk.at(w.b, w.t, w.h) + c
+                                             : (T *)p.oq + n.yq.at(w.b, w.t, w.h) + c,
+                                       x[u]);
+                } else {
+                    float (&gu)[8] = g[kBackward ? u : 0];
+                    turn8(gu, c, n.rotary, n.halves, cs[i], -1.f, lane);
+                    float dot = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float xn = x[u][e] * r, d = gu[e] * xn;
+                        if (w.key) ak[e] += on ? d : 0.f;
+                        else aq[e] += on ? d : 0.f;
+                        gu[e] *= w.key ? gk[e] : gq[e];
+                        dot = fmaf(gu[e], xn, dot);
+                        x[u][e] = xn;
+                    }
+                    dot = group_sum(dot, lanes) / (float)n.hp;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) gu[e] = r * (gu[e] - x[u][e] * dot);
+                    if (on)
+                        store8<T, VEC>(w.key ? (T *)p.ok + n.dk.at(w.b, w.t, w.h) + c
+                                             : (T *)p.oq + n.dq.at(w.b, w.t, w.h) + c,
+                                       gu);
+                }
+            }
+        }
+    }
+    if (kBackward && p.partial != nullptr) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            red[(grp * 2 + 0) * n.hp + c + e] = aq[e];
+            red[(grp * 2 + 1) * n.hp + c + e] = ak[e];
+        }
+        __syncthreads();
+        for (int o = threadIdx.x; o < 2 * n.hp; o += kThreads) {
+            float sum = 0.f;
+            for (int u = 0; u < groups; ++u) sum += red[u * 2 * n.hp + o];
+            p.partial[(long long)blockIdx.x * 2 * n.hp + o] = sum;
+        }
+    }
+}
+
+// dgamma = the blocks' partial sums: 32 columns a block, 32 runs of rows each,
+// added up in a fixed order.
+__global__ void __launch_bounds__(1024) qk_dgamma_kernel(const float *partial, int blocks, int hp,
+                                                         float *dgq, float *dgk) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float red[32][33];
+    const int cc = threadIdx.x & 31, run = threadIdx.x >> 5;
+    const int col = blockIdx.x * 32 + cc;
+    float sum = 0.f;
+    for (int r = run; r < blocks; r += 32) sum += partial[(long long)r * 2 * hp + col];
+    red[run][cc] = sum;
+    __syncthreads();
+    if (run == 0) {
+        float t = 0.f;
+        for (int u = 0; u < 32; ++u) t += red[u][cc];
+        float *out = col < hp ? dgq : dgk;
+        if (out != nullptr) out[col < hp ? col : col - hp] = t;
+    }
+}
+
+constexpr int kMaxBlocks = 152 * 4;   // of the backward: each keeps its dgamma to the end
+
+int step_tokens(const Norm &n) {
+    // several tokens a step only where every SM still gets work: with few, one token a
+    // block starts and ends sooner
+    const long long N = (long long)n.B * n.T;
+    return N >= 4LL * kMaxTokens * 152 ? kMaxTokens : 1;
+}
+
+int bwd_blocks(const Norm &n) {
+    const long long N = (long long)n.B * n.T, t = step_tokens(n), steps = (N + t - 1) / t;
+    return (int)(steps < kMaxBlocks ? steps : kMaxBlocks);
+}
+
+template <bool kBackward>
+cudaError_t launch(const NormArgs &p, bool vec, unsigned blocks, cudaStream_t s) {
+    const Turns tab = make_turns(p.n.rotary, p.n.theta);
+    const int smem = kBackward ? kThreads / (p.n.hp / 8) * 2 * p.n.hp * 4 : 0;   // 16 KB
+    auto go = [&](auto kernel) {
+        kernel<<<blocks, kThreads, smem, s>>>(p, tab);
+        note_launches(1);
+        return cudaGetLastError();
+    };
+    if (p.n.bf16)
+        return vec ? go(qk_norm_rope_kernel<bf16, true, kBackward>)
+                   : go(qk_norm_rope_kernel<bf16, false, kBackward>);
+    return vec ? go(qk_norm_rope_kernel<float, true, kBackward>)
+               : go(qk_norm_rope_kernel<float, false, kBackward>);
+}
+
+}  // namespace
+
+size_t norm_workspace(const Norm &n) { return (size_t)bwd_blocks(n) * 2 * n.hp * sizeof(float); }
+
+cudaError_t launch_norm(const Norm &n, const void *q, const void *k, const void *gq, const void *gk,
+                        const int32_t *pos, void *yq, void *yk, cudaStream_t s) {
+    NormArgs p{n, q, k, gq, gk, nullptr, nullptr, yq, yk, pos, nullptr, step_tokens(n)};
+    const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) && rows16(yq, n.yq, n.bf16) &&
+                     rows16(yk, n.yk, n.bf16);
+    const long long N = (long long)n.B * n.T;
+    return launch<false>(p, vec, (unsigned)((N + p.tokens - 1) / p.tokens), s);
+}
+
+cudaError_t launch_norm_bwd(const Norm &n, const void *q, const void *k, const void *gq,
+                            const void *gk, const int32_t *pos, const void *dyq, const void *dyk,
+                            void *dq, void *dk, float *dgq, float *dgk, void *ws, cudaStream_t s) {
+    const bool sums = dgq != nullptr || dgk != nullptr;
+    NormArgs p{n, q, k, gq, gk, dyq, dyk, dq, dk, pos, sums ? (float *)ws : nullptr, step_tokens(n)};
+    const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) &&
+                     rows16(dyq, n.yq, n.bf16) && rows16(dyk, n.yk, n.bf16) &&
+                     rows16(dq, n.dq, n.bf16) && rows16(dk, n.dk, n.bf16);
+    const int blocks = bwd_blocks(n);
+    cudaError_t e = launch<true>(p, vec, (unsigned)blocks, s);
+    if (e != cudaSuccess || !sums) return e;
+    e = launch_pdl(qk_dgamma_kernel, dim3(2 * n.hp / 32), dim3(1024), 0, s, (const float *)p.partial,
+                   blocks, n.hp, dgq, dgk);
+    note_launches(1);
+    return e;
+}
+
+}  // namespace win
+}  // namespace mosa

@@ -1,0 +1,509 @@
+// Window attention on CUDA cores: fp32 storage, and any strides or alignment
+// that the tensor-core kernels do not take.
+//
+// For a query at position p over its visible tokens t (window_tiles.cuh)
+//     S = scale q k_t,  P = softmax(S),  O = sum P v,  lse = log sum exp S
+// and backward, with D = sum(dO o O) and P recomputed from lse,
+//     dP = dO v,  dS = P (dP - D),  dq = scale sum dS k,
+//     dk = scale sum dS q,  dv = sum P dO      (over queries and the heads of a group).
+// One CTA of 256 threads per 64-row tile: 64 x 64 scores a step, four by four a
+// thread, operands as fp32 in shared memory, the softmax's running maximum and
+// sum in registers.  The backward takes one kernel by key tiles (dk, dv) and one by
+// query tiles (dq), so that every sum runs in one thread in a fixed order.
+#include "launch.h"
+#include "profile.h"
+#include "window_tiles.cuh"
+
+namespace mosa {
+namespace win {
+namespace {
+
+constexpr int kT = 64;         // rows of a tile, queries and keys
+constexpr int kThreads = 256;
+constexpr int kPS = kT + 4;    // stride of a tile of scores
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+template <class T>
+struct Ptrs {
+    const T *q, *k, *v, *dO;
+    T *o, *dq, *dk, *dv;
+    const int32_t *lens;
+    float *lse;
+    const float *lse_in, *delta;
+    bool vec;   // rows of every input start at a multiple of 16 bytes
+};
+
+// Rows t0 .. t0+63 of one head into dst [64][HD + 4]; rows outside [lo, hi) are zeros.
+template <int HD, class T>
+__device__ __forceinline__ void load_tile(float *dst, const T *src, long long st, int t0, int lo,
+                                          int hi, bool vec) {
+    constexpr int E = 16 / sizeof(T), U = HD / E;
+    for (int e = threadIdx.x; e < kT * U; e += kThreads) {
+        const int r = e / U, u = e % U, t = t0 + r;
+        float *d = dst + r * (HD + 4) + u * E;
+        if (t < lo || t >= hi) {
+#pragma unroll
+            for (int x = 0; x < E; ++x) d[x] = 0.f;
+            continue;
+        }
+        const T *s = src + (long long)t * st + u * E;
+        if (vec) {
+            alignas(16) T w[E];
+            *reinterpret_cast<uint4 *>(w) = *reinterpret_cast<const uint4 *>(s);
+#pragma unroll
+            for (int x = 0; x < E; ++x) d[x] = to_f32(w[x]);
+        } else {
+#pragma unroll
+            for (int x = 0; x < E; ++x) d[x] = to_f32(s[x]);
+        }
+    }
+}
+
+// acc[i][j] = <row ty*4+i of A, row tx+16j of B> over HD columns.
+template <int HD>
+__device__ __forceinline__ void dot_tiles(const float *A, const float *B, int ty, int tx,
+                                          float (&acc)[4][4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < HD; d += 4) {
+        float4 a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            a[i] = *reinterpret_cast<const float4 *>(A + (ty * 4 + i) * (HD + 4) + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            b[j] = *reinterpret_cast<const float4 *>(B + (tx + 16 * j) * (HD + 4) + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                acc[i][j] = fmaf(a[i].x, b[j].x, acc[i][j]);
+                acc[i][j] = fmaf(a[i].y, b[j].y, acc[i][j]);
+                acc[i][j] = fmaf(a[i].z, b[j].z, acc[i][j]);
+                acc[i][j] = fmaf(a[i].w, b[j].w, acc[i][j]);
+            }
+    }
+}
+
+// The HD/16 columns of thread tx: runs of up to four, 16 runs side by side.
+template <int HD>
+__device__ __forceinline__ int col_of(int tx, int c) {
+    constexpr int CW = HD / 16;
+    return CW <= 4 ? tx * CW + c : (c >> 2) * 64 + tx * 4 + (c & 3);
+}
+
+// acc[i][c] += sum_j W[ty*4+i][j] X[j][col_of(c)].  With `skip` a weight of zero adds
+// nothing whatever X holds (masked places may hold NaN).
+template <int HD, bool kRowsFirst>
+__device__ __forceinline__ void add_weighted(const float *W, const float *X, int ty, int tx,
+                                             bool skip, float (&acc)[4][HD / 16]) {
+    constexpr int CW = HD / 16;
+#pragma unroll 2
+    for (int j = 0; j < kT; j += 4) {
+        float w[4][4];   // [row][step]
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 t = *reinterpret_cast<const float4 *>(
+                kRowsFirst ? W + (ty * 4 + i) * kPS + j : W + (j + i) * kPS + ty * 4);
+            if (kRowsFirst) {
+                w[i][0] = t.x; w[i][1] = t.y; w[i][2] = t.z; w[i][3] = t.w;
+            } else {
+                w[0][i] = t.x; w[1][i] = t.y; w[2][i] = t.z; w[3][i] = t.w;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            float x[CW];
+#pragma unroll
+            for (int c = 0; c < CW; ++c) x[c] = X[(j + u) * (HD + 4) + col_of<HD>(tx, c)];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (!skip || w[i][u] != 0.f) {
+#pragma unroll
+                    for (int c = 0; c < CW; ++c) acc[i][c] = fmaf(w[i][u], x[c], acc[i][c]);
+                }
+        }
+    }
+}
+
+template <int HD, class T>
+__device__ __forceinline__ void store_row(T *dst, int tx, const float (&v)[HD / 16], float f) {
+#pragma unroll
+    for (int c = 0; c < HD / 16; ++c) dst[col_of<HD>(tx, c)] = from_f32<T>(v[c] * f);
+}
+
+__device__ __forceinline__ float max16(float x) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return x;
+}
+__device__ __forceinline__ float sum16(float x) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+template <int HD>
+constexpr int tile_floats() { return kT * (HD + 4); }
+
+template <int HD, class T>
+__global__ void __launch_bounds__(kThreads) window_fwd_simt_kernel(Attn a, Ptrs<T> p) {
+    extern __shared__ float sm[];
+    float *sQ = sm, *sK = sQ + tile_floats<HD>(), *sV = sK + tile_floats<HD>(),
+          *sP = sV + tile_floats<HD>();
+    const int h = blockIdx.y, b = blockIdx.z, hk = h / a.G();
+    const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kT, off = a.Tk - a.Tq;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int len = seq_len(p.lens, b, a.Tk);
+    const int pf = off + i0, pl = min(off + min(i0 + kT, a.Tq), len) - 1;
+    float acc[4][HD / 16], m[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < HD / 16; ++c) acc[i][c] = 0.f;
+    }
+    if (pl >= pf) {
+        load_tile<HD>(sQ, p.q + a.q.at(b, 0, h), a.q.t, i0, 0, pl - off + 1, p.vec);
+        const KeyBlocks<kT> kb(pf, pl, a.window, a.sinks);
+        const float sl2 = a.scale * kLog2e;
+        for (int j = 0; j < kb.count(); ++j) {
+            const int ks = kb.start(j);
+            __syncthreads();
+            load_tile<HD>(sK, p.k + a.k.at(b, 0, hk), a.k.t, ks, 0, len, p.vec);
+            load_tile<HD>(sV, p.v + a.v.at(b, 0, hk), a.v.t, ks, 0, len, p.vec);
+            __syncthreads();
+            float s[4][4];
+            dot_tiles<HD>(sQ, sK, ty, tx, s);
+            const bool whole = kb.whole(j, pf, pl, a.window) && pl - pf == kT - 1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int pos = pf + ty * 4 + i;
+                float mb = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (!whole && !(pos <= pl && kb.sees(j, ks, tx + 16 * c, pos, a.window, a.sinks)))
+                        s[i][c] = -INFINITY;
+                    else
+                        s[i][c] *= sl2;
+                    mb = fmaxf(mb, s[i][c]);
+                }
+                // (fmax drops a NaN; the exponentials keep it)
+                const float mn = fmaxf(m[i], max16(mb));
+                const float base = mn == -INFINITY ? 0.f : mn;
+                const float corr = exp2f(m[i] - base);
+                float sum = 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const float e = exp2f(s[i][c] - base);
+                    sum += e;
+                    sP[(ty * 4 + i) * kPS + tx + 16 * c] = e;
+                }
+                l[i] = l[i] * corr + sum16(sum);
+                m[i] = mn;
+#pragma unroll
+                for (int c = 0; c < HD / 16; ++c) acc[i][c] *= corr;
+            }
+            __syncwarp();   // a row of sP is written and read by the 16 lanes of one half warp
+            add_weighted<HD, true>(sP, sV, ty, tx, !whole, acc);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i0 + ty * 4 + i;
+        if (r >= a.Tq) continue;
+        store_row<HD>(p.o + a.o.at(b, r, h), tx, acc[i], l[i] == 0.f ? 0.f : 1.f / l[i]);
+        if (p.lse != nullptr && tx == 0)
+            p.lse[((long long)b * a.H + h) * a.Tq + r] =
+                l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
+    }
+}
+
+// P (into sP, [query][key]) and dS (into sS) of one pair of tiles: queries at
+// positions pq .. pq+63 (rows past `last` see nothing), keys ks .. ks+63.
+template <int HD, class Sees>
+__device__ __forceinline__ void grad_scores(const float *sQ, const float *sG, const float *sK,
+                                            const float *sV, const float *sL, const float *sD,
+                                            float sl2, bool whole, Sees sees, float *sP, float *sS,
+                                            int ty, int tx, int pq, int window, int sinks) {
+    float s[4][4], dp[4][4];
+    dot_tiles<HD>(sQ, sK, ty, tx, s);
+    dot_tiles<HD>(sG, sV, ty, tx, dp);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = ty * 4 + i;
+        const float lse2 = sL[r], D = sD[r];
+        const bool one = sees_one(pq + r, window, sinks);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const bool on = whole || sees(r, tx + 16 * c);
+            const float e = on ? exp2f(fmaf(s[i][c], sl2, -lse2)) : 0.f;
+            if (sP != nullptr) sP[r * kPS + tx + 16 * c] = e;
+            sS[r * kPS + tx + 16 * c] = on && !one ? e * (dp[i][c] - D) : 0.f;
+        }
+    }
+}
+
+// lse (in log2 units) and D of the queries i0 .. i0+63; rows outside [0, n) see nothing.
+template <class T>
+__device__ __forceinline__ void load_rows(float *sL, float *sD, const Ptrs<T> &p, long long row0,
+                                          int i0, int n) {
+    if (threadIdx.x < kT) {
+        const int i = i0 + threadIdx.x;
+        const bool ok = i >= 0 && i < n;
+        sL[threadIdx.x] = ok ? p.lse_in[row0 + i] * kLog2e : 0.f;
+        sD[threadIdx.x] = ok ? p.delta[row0 + i] : 0.f;
+    }
+}
+
+// dq of one 64-query tile.
+template <int HD, class T>
+__global__ void __launch_bounds__(kThreads) window_dq_simt_kernel(Attn a, Ptrs<T> p) {
+    extern __shared__ float sm[];
+    float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
+          *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sL = sS + kT * kPS,
+          *sD = sL + kT;
+    const int h = blockIdx.y, b = blockIdx.z, hk = h / a.G();
+    const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kT, off = a.Tk - a.Tq;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int len = seq_len(p.lens, b, a.Tk);
+    const int pf = off + i0, pl = min(off + min(i0 + kT, a.Tq), len) - 1;
+    float acc[4][HD / 16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < HD / 16; ++c) acc[i][c] = 0.f;
+    if (pl >= pf) {
+        const long long row0 = ((long long)b * a.H + h) * a.Tq;
+        load_tile<HD>(sQ, p.q + a.q.at(b, 0, h), a.q.t, i0, 0, pl - off + 1, p.vec);
+        load_tile<HD>(sG, p.dO + a.go.at(b, 0, h), a.go.t, i0, 0, pl - off + 1, p.vec);
+        load_rows(sL, sD, p, row0, i0, pl - off + 1);
+        const KeyBlocks<kT> kb(pf, pl, a.window, a.sinks);
+        for (int j = 0; j < kb.count(); ++j) {
+            const int ks = kb.start(j);
+            __syncthreads();
+            load_tile<HD>(sK, p.k + a.k.at(b, 0, hk), a.k.t, ks, 0, len, p.vec);
+            load_tile<HD>(sV, p.v + a.v.at(b, 0, hk), a.v.t, ks, 0, len, p.vec);
+            __syncthreads();
+            const bool whole = kb.whole(j, pf, pl, a.window) && pl - pf == kT - 1;
+            grad_scores<HD>(
+                sQ, sG, sK, sV, sL, sD, a.scale * kLog2e, whole,
+                [&](int r, int c) {
+                    return pf + r <= pl && kb.sees(j, ks, c, pf + r, a.window, a.sinks);
+                },
+                (float *)nullptr, sS, ty, tx, pf, a.window, a.sinks);
+            __syncwarp();
+            add_weighted<HD, true>(sS, sK, ty, tx, !whole, acc);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i0 + ty * 4 + i;
+        if (r < a.Tq) store_row<HD>(p.dq + a.dq.at(b, r, h), tx, acc[i], a.scale);
+    }
+}
+
+// dk and dv of one 64-key tile, over the queries that see it and the group's heads.
+template <int HD, class T>
+__global__ void __launch_bounds__(kThreads) window_dkv_simt_kernel(Attn a, Ptrs<T> p) {
+    extern __shared__ float sm[];
+    float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
+          *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sP = sS + kT * kPS,
+          *sL = sP + kT * kPS, *sD = sL + kT;
+    const int hk = blockIdx.y, b = blockIdx.z, G = a.G();
+    const int k0 = (int)blockIdx.x * kT, off = a.Tk - a.Tq;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int len = seq_len(p.lens, b, a.Tk);
+    float dk[4][HD / 16], dv[4][HD / 16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < HD / 16; ++c) dk[i][c] = dv[i][c] = 0.f;
+    // positions first .. last see some key of the tile
+    const int first = max(k0, off);
+    const int last = (k0 < a.sinks || a.window >= a.Tk) ? len - 1
+                                                        : min(k0 + kT - 1 + a.window - 1, len - 1);
+    if (k0 < len && first <= last) {
+        load_tile<HD>(sK, p.k + a.k.at(b, 0, hk), a.k.t, k0, 0, len, p.vec);
+        load_tile<HD>(sV, p.v + a.v.at(b, 0, hk), a.v.t, k0, 0, len, p.vec);
+        for (int g = 0; g < G; ++g) {
+            const int h = hk * G + g;
+            const long long row0 = ((long long)b * a.H + h) * a.Tq;
+            for (int pq = first; pq <= last; pq += kT) {
+                const int i0 = pq - off, n = min(a.Tq, len - off);
+                __syncthreads();
+                load_tile<HD>(sQ, p.q + a.q.at(b, 0, h), a.q.t, i0, 0, n, p.vec);
+                load_tile<HD>(sG, p.dO + a.go.at(b, 0, h), a.go.t, i0, 0, n, p.vec);
+                load_rows(sL, sD, p, row0, i0, n);
+                __syncthreads();
+                const bool whole = pq >= k0 + kT - 1 && pq + kT - 1 - k0 < a.window &&
+                                   pq + kT - 1 < len && k0 + kT <= len;
+                grad_scores<HD>(
+                    sQ, sG, sK, sV, sL, sD, a.scale * kLog2e, whole,
+                    [&](int r, int c) {
+                        const int pos = pq + r, t = k0 + c;
+                        return pos < len && t <= pos && (pos - t < a.window || t < a.sinks);
+                    },
+                    sP, sS, ty, tx, pq, a.window, a.sinks);
+                __syncthreads();
+                add_weighted<HD, false>(sP, sG, ty, tx, !whole, dv);
+                add_weighted<HD, false>(sS, sQ, ty, tx, !whole, dk);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = k0 + ty * 4 + i;
+        if (t >= a.Tk) continue;
+        store_row<HD>(p.dk + a.dk.at(b, t, hk), tx, dk[i], a.scale);
+        store_row<HD>(p.dv + a.dv.at(b, t, hk), tx, dv[i], 1.f);
+    }
+}
+
+// One thread per 8 values of a row: hp/8 lanes a row.
+template <class T>
+__global__ void __launch_bounds__(256) window_delta_kernel(Attn a, const T *O, const T *dO,
+                                                           float *delta, bool vec) {
+    const int lanes = a.hp / 8;
+    const long long g = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long rows = (long long)a.B * a.Tq * a.H;
+    const long long row = g / lanes;
+    const int c = (int)(g % lanes) * 8;
+    float sum = 0.f;
+    int b = 0, h = 0, t = 0;
+    if (row < rows) {
+        h = (int)(row % a.H);
+        t = (int)(row / a.H % a.Tq);
+        b = (int)(row / a.H / a.Tq);
+        const T *x = O + a.o.at(b, t, h) + c, *y = dO + a.go.at(b, t, h) + c;
+        alignas(16) T u[8], w[8];
+        if (vec) {
+#pragma unroll
+            for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i) {
+                reinterpret_cast<uint4 *>(u)[i] = reinterpret_cast<const uint4 *>(x)[i];
+                reinterpret_cast<uint4 *>(w)[i] = reinterpret_cast<const uint4 *>(y)[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = x[i], w[i] = y[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fmaf(to_f32(u[i]), to_f32(w[i]), sum);
+    }
+    for (int o = lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (row < rows && c == 0) delta[((long long)b * a.H + h) * a.Tq + t] = sum;
+}
+
+template <int HD>
+constexpr int fwd_smem() { return 4 * (3 * tile_floats<HD>() + kT * kPS); }
+template <int HD>
+constexpr int dq_smem() { return 4 * (4 * tile_floats<HD>() + kT * kPS + 2 * kT); }
+template <int HD>
+constexpr int dkv_smem() { return 4 * (4 * tile_floats<HD>() + 2 * kT * kPS + 2 * kT); }
+
+template <class Kernel, class T>
+cudaError_t go(Kernel kernel, dim3 grid, int smem, const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
+    cudaError_t e = allow_smem((const void *)kernel, smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<grid, kThreads, smem, s>>>(a, p);
+    note_launches(1);
+    return cudaGetLastError();
+}
+
+template <class T>
+cudaError_t fwd(const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
+    const dim3 grid((a.Tq + kT - 1) / kT, a.H, a.B);
+    switch (a.hp) {
+        case 16: return go(window_fwd_simt_kernel<16, T>, grid, fwd_smem<16>(), a, p, s);
+        case 32: return go(window_fwd_simt_kernel<32, T>, grid, fwd_smem<32>(), a, p, s);
+        case 64: return go(window_fwd_simt_kernel<64, T>, grid, fwd_smem<64>(), a, p, s);
+        default: return go(window_fwd_simt_kernel<128, T>, grid, fwd_smem<128>(), a, p, s);
+    }
+}
+
+template <int HD, class T>
+cudaError_t bwd_hd(const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
+    const dim3 gk((a.Tk + kT - 1) / kT, a.Hkv, a.B), gq((a.Tq + kT - 1) / kT, a.H, a.B);
+    cudaError_t e = go(window_dkv_simt_kernel<HD, T>, gk, dkv_smem<HD>(), a, p, s);
+    return e != cudaSuccess ? e : go(window_dq_simt_kernel<HD, T>, gq, dq_smem<HD>(), a, p, s);
+}
+
+template <class T>
+cudaError_t bwd(const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
+    switch (a.hp) {
+        case 16: return bwd_hd<16>(a, p, s);
+        case 32: return bwd_hd<32>(a, p, s);
+        case 64: return bwd_hd<64>(a, p, s);
+        default: return bwd_hd<128>(a, p, s);
+    }
+}
+
+template <class T>
+Ptrs<T> ptrs(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens) {
+    Ptrs<T> p{};
+    p.q = (const T *)q;
+    p.k = (const T *)k;
+    p.v = (const T *)v;
+    p.lens = lens;
+    p.vec = rows16(q, a.q, a.bf16) && rows16(k, a.k, a.bf16) && rows16(v, a.v, a.bf16);
+    return p;
+}
+
+template <class T>
+cudaError_t fwd_of(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
+                   void *O, float *lse, cudaStream_t s) {
+    Ptrs<T> p = ptrs<T>(a, q, k, v, lens);
+    p.o = (T *)O;
+    p.lse = lse;
+    return fwd<T>(a, p, s);
+}
+
+template <class T>
+cudaError_t bwd_of(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
+                   const float *lse, const void *dO, const float *delta, void *dq, void *dk,
+                   void *dv, cudaStream_t s) {
+    Ptrs<T> p = ptrs<T>(a, q, k, v, lens);
+    p.vec = p.vec && rows16(dO, a.go, a.bf16);
+    p.dO = (const T *)dO;
+    p.lse_in = lse;
+    p.delta = delta;
+    p.dq = (T *)dq;
+    p.dk = (T *)dk;
+    p.dv = (T *)dv;
+    return bwd<T>(a, p, s);
+}
+
+}  // namespace
+
+cudaError_t simt_window_fwd(const Attn &a, const void *q, const void *k, const void *v,
+                            const int32_t *lens, void *O, float *lse, cudaStream_t s) {
+    return a.bf16 ? fwd_of<bf16>(a, q, k, v, lens, O, lse, s)
+                  : fwd_of<float>(a, q, k, v, lens, O, lse, s);
+}
+
+cudaError_t simt_window_bwd(const Attn &a, const void *q, const void *k, const void *v,
+                            const int32_t *lens, const float *lse, const void *dO,
+                            const float *delta, void *dq, void *dk, void *dv, cudaStream_t s) {
+    return a.bf16 ? bwd_of<bf16>(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, s)
+                  : bwd_of<float>(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, s);
+}
+
+cudaError_t window_delta(const Attn &a, const void *O, const void *dO, float *delta,
+                         cudaStream_t s) {
+    const long long n = (long long)a.B * a.Tq * a.H * (a.hp / 8);
+    const bool vec = rows16(O, a.o, a.bf16) && rows16(dO, a.go, a.bf16);
+    const dim3 grid((unsigned)((n + 255) / 256));
+    if (a.bf16)
+        window_delta_kernel<bf16><<<grid, 256, 0, s>>>(a, (const bf16 *)O, (const bf16 *)dO, delta, vec);
+    else
+        window_delta_kernel<float><<<grid, 256, 0, s>>>(a, (const float *)O, (const float *)dO, delta, vec);
+    note_launches(1);
+    return cudaGetLastError();
+}
+
+}  // namespace win
+}  // namespace mosa
