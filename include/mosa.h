@@ -360,19 +360,20 @@ typedef struct {
 } mosa_window_shape;
 
 /* Workspace of a forward or backward (256-byte aligned); 0 if the shape is invalid or
- * unsupported.  Nothing in it is kept between calls but the status word in its
- * first 4 bytes: zero those once, before the workspace's first call. */
+ * unsupported.  It carries the status word in its first 4 bytes (zero those once,
+ * before the workspace's first call) and, from a bf16 forward with lse to the backward
+ * that follows, what the rounding of O cut off: pass the same buffer to both. */
 size_t mosa_window_workspace_bytes(const mosa_window_shape *shape);
 
 /* Forward: q [B,Tq,H,hp], k and v [B,Tk,Hkv,hp], lens [B] int32 or NULL (all
  * Tk; values outside 0..Tk count as the nearer end); outputs O [B,Tq,H,hp] in
  * the storage dtype and lse [B,H,Tq] fp32, the log-sum-exp of each query's
- * visible scores, which the backward needs (NULL if not wanted). */
+ * visible scores, which the backward needs (NULL where none follows). */
 mosa_status mosa_window_forward(const mosa_window_shape *shape, const void *q, const void *k,
                                 const void *v, const int32_t *lens, void *O, float *lse,
                                 void *workspace, size_t workspace_bytes, void *stream);
 
-/* Backward: from the forward's inputs and outputs and dO, the gradients dq, dk
+/* Backward: from the forward's inputs, outputs and workspace and dO, the gradients dq, dk
  * and dv in the storage dtype, dk and dv summed over the query heads that share them.
  * Sums run in a fixed order: the same bits every time. */
 mosa_status mosa_window_backward(const mosa_window_shape *shape, const void *q, const void *k,

@@ -210,23 +210,25 @@ def _window(q, k, v, window, sinks, lens):
 
 
 def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: float = 0.0,
-                        workspace=None, out=None, stream=None):
+                        workspace=None, out=None, stream=None, want_lse: bool = True):
     """Attention of q [B,Tq,H,hp], the last Tq of Tk tokens, over k and v [B,Tk,Hkv,hp]:
     each token sees those up to itself that are among the last ``window`` (0: all) or the
     first ``sinks``, below its sequence's length (lens [B] int32, Tk by default).
-    scale = 0 is 1/sqrt(hp).  Returns (O, lse, workspace): O like q, lse [B,H,Tq] fp32.
-    ``out`` may hold "O" and "lse"."""
+    scale = 0 is 1/sqrt(hp).  Returns (O, lse, workspace): O like q, lse [B,H,Tq] fp32, or
+    None without ``want_lse`` (where no backward follows).  ``out`` may hold "O" and "lse"."""
     sizes, n = _window(q, k, v, window, sinks, lens)
     B, Tq, Tk, H = sizes[:4]
     f32 = _b._torch_mod.float32
-    O, lse = _new(q, out, "O"), _new(q, out, "lse", (B, H, Tq), f32)
+    O = _new(q, out, "O")
+    lse = _new(q, out, "lse", (B, H, Tq), f32) if want_lse else None
     _b._want("lse", lse, (B, H, Tq))
     s, ref = _window_shape(sizes, scale, _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k.shape),
                            _heads(O, "O", q.shape))
     L = _b.load()
     workspace = _space(L.mosa_window_workspace_bytes, ref, "mosa_window_forward", workspace, q.device)
     rc = L.mosa_window_forward(ref, _at(q, "q"), _at(k, "k"), _at(v, "v"), n,
-                               _at(O, "O", q.dtype), _b._dev(lse, "lse", f32),
+                               _at(O, "O", q.dtype),
+                               None if lse is None else _b._dev(lse, "lse", f32),
                                _b._dev(workspace, "workspace"), workspace.numel(),
                                _b._stream(stream))
     if rc:
@@ -236,8 +238,9 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
 
 def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int = 0, lens=None,
                          scale: float = 0.0, out=None, stream=None):
-    """Gradients of mosa_window_forward: a dict with dq, dk and dv like q, k and v, dk and dv
-    summed over the query heads that share them.  ``out`` may hold any of them."""
+    """Gradients of mosa_window_forward, given its outputs and its workspace: a dict with dq, dk
+    and dv like q, k and v, dk and dv summed over the query heads that share them.  ``out`` may
+    hold any of them."""
     sizes, n = _window(q, k, v, window, sinks, lens)
     B, Tq, Tk, H = sizes[:4]
     _b._same(q, ("O", O), ("dO", dO))

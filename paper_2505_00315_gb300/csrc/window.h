@@ -24,6 +24,8 @@ struct Attn {
     float scale;
     Str q, k, v, o, go, dq, dk, dv;
     __host__ __device__ int G() const { return H / Hkv; }
+    // of a packed tensor [B, Tq, H, hp]
+    __host__ __device__ Str packed() const { return Str{(long long)Tq * H * hp, (long long)H * hp, hp}; }
 };
 
 // Fixed-point turns per position of each rotated pair (see rope_turn).
@@ -65,14 +67,27 @@ cudaError_t launch_norm_bwd(const Norm &n, const void *q, const void *k, const v
                             void *dq, void *dk, float *dgq, float *dgk, void *ws, cudaStream_t s);
 
 // Attention on CUDA cores, any strides and alignment (window_simt.cu).  delta:
-// [B,H,Tq] fp32 scratch.
+// [B,H,Tq] fp32 scratch.  rest (bf16 storage, or null): [B,Tq,H,hp], what O lost when it was
+// rounded, as bf16, so that the backward's D = sum(dO o O) is not off by O's rounding: dP - D cancels
+// where a query's weight lies on one token, as on a sink.
 cudaError_t simt_window_fwd(const Attn &a, const void *q, const void *k, const void *v,
-                            const int32_t *lens, void *O, float *lse, cudaStream_t s);
+                            const int32_t *lens, void *O, float *lse, bf16 *rest, cudaStream_t s);
 cudaError_t simt_window_bwd(const Attn &a, const void *q, const void *k, const void *v,
                             const int32_t *lens, const float *lse, const void *dO,
                             const float *delta, void *dq, void *dk, void *dv, cudaStream_t s);
-// delta[b,h,i] = sum over the head of dO o O, in fp32.
-cudaError_t window_delta(const Attn &a, const void *O, const void *dO, float *delta, cudaStream_t s);
+// delta[b,h,i] = sum over the head of dO o (O + rest), in fp32.
+cudaError_t window_delta(const Attn &a, const void *O, const bf16 *rest, const void *dO, float *delta,
+                         cudaStream_t s);
+
+// The same on the tensor cores (bf16, window_tc_*.cu); false, and nothing launched, where
+// the tensors' places or strides do not suit.
+bool tc_window_fwd(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
+                   void *O, float *lse, bf16 *rest, uint32_t *status, cudaStream_t s, cudaError_t *err);
+bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
+                   const float *lse, const void *dO, const float *delta, void *dq, void *dk, void *dv,
+                   float *partial, uint32_t *status, cudaStream_t s, cudaError_t *err);
+// Bytes of its `partial`.
+size_t tc_window_bwd_bytes(const Attn &a);
 
 size_t decode_workspace(const Decode &d);
 cudaError_t launch_decode(const Decode &d, const void *q, const void *k, const void *v,

@@ -142,8 +142,20 @@ mosa_status check_space(const void *ws, size_t bytes, size_t need) {
 
 mosa_status of(cudaError_t e) { return e == cudaSuccess ? MOSA_OK : MOSA_ERR_CUDA; }
 
-// The status word, then the backward's D [B,H,Tq].
-size_t window_bytes(const Attn &a) { return 256 + (size_t)a.B * a.H * a.Tq * sizeof(float); }
+// MOSA_FORCE_SIMT=1 keeps these calls, as the layer's, on the CUDA cores.
+bool tensor_cores() { return use_split(); }
+
+// The status word, then the backward's D [B,H,Tq], what the forward's O lost by its rounding
+// (bf16 storage) and the backward's partial sums of sink rows.
+size_t rest_at(const Attn &a) {
+    return 256 + ((size_t)a.B * a.H * a.Tq * sizeof(float) + 255) / 256 * 256;
+}
+size_t partial_at(const Attn &a) {
+    return rest_at(a) + (a.bf16 ? ((size_t)a.B * a.H * a.Tq * a.hp * 2 + 255) / 256 * 256 : 0);
+}
+size_t window_bytes(const Attn &a) {
+    return partial_at(a) + (a.bf16 ? tc_window_bwd_bytes(a) : 0);
+}
 
 }  // namespace
 }  // namespace win
@@ -203,7 +215,12 @@ mosa_status mosa_window_forward(const mosa_window_shape *shape, const void *q, c
     if ((st = check_ptrs(shape->dtype, {q, k, v, O})) != MOSA_OK) return st;
     if (!aligned(lens, MOSA_F32) || !aligned(lse, MOSA_F32)) return MOSA_ERR_INVALID_ARG;
     if ((st = check_space(workspace, workspace_bytes, window_bytes(a))) != MOSA_OK) return st;
-    return of(simt_window_fwd(a, q, k, v, lens, O, lse, (cudaStream_t)stream));
+    cudaStream_t cs = (cudaStream_t)stream;
+    cudaError_t e = cudaSuccess;
+    bf16 *rest = lse != nullptr && a.bf16 ? (bf16 *)((char *)workspace + rest_at(a)) : nullptr;
+    if (tensor_cores() && tc_window_fwd(a, q, k, v, lens, O, lse, rest, (uint32_t *)workspace, cs, &e))
+        return of(e);
+    return of(simt_window_fwd(a, q, k, v, lens, O, lse, rest, cs));
 }
 
 mosa_status mosa_window_backward(const mosa_window_shape *shape, const void *q, const void *k,
@@ -219,9 +236,14 @@ mosa_status mosa_window_backward(const mosa_window_shape *shape, const void *q, 
     if ((st = check_space(workspace, workspace_bytes, window_bytes(a))) != MOSA_OK) return st;
     float *delta = reinterpret_cast<float *>(static_cast<char *>(workspace) + 256);
     cudaStream_t s = (cudaStream_t)stream;
-    cudaError_t e = window_delta(a, O, dO, delta, s);
-    if (e == cudaSuccess) e = simt_window_bwd(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, s);
-    return of(e);
+    cudaError_t e = window_delta(a, O, a.bf16 ? (const bf16 *)((const char *)workspace + rest_at(a)) : nullptr, dO,
+                                 delta, s);
+    if (e != cudaSuccess) return MOSA_ERR_CUDA;
+    float *partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + partial_at(a));
+    if (tensor_cores() && tc_window_bwd(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, partial,
+                                        (uint32_t *)workspace, s, &e))
+        return of(e);
+    return of(simt_window_bwd(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, s));
 }
 
 mosa_status mosa_window_check_status(void *workspace, void *stream) {

@@ -29,6 +29,7 @@ struct Ptrs {
     T *o, *dq, *dk, *dv;
     const int32_t *lens;
     float *lse;
+    bf16 *rest;
     const float *lse_in, *delta;
     bool vec;   // rows of every input start at a multiple of 16 bytes
 };
@@ -216,7 +217,16 @@ __global__ void __launch_bounds__(kThreads) window_fwd_simt_kernel(Attn a, Ptrs<
     for (int i = 0; i < 4; ++i) {
         const int r = i0 + ty * 4 + i;
         if (r >= a.Tq) continue;
-        store_row<HD>(p.o + a.o.at(b, r, h), tx, acc[i], l[i] == 0.f ? 0.f : 1.f / l[i]);
+        const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+        store_row<HD>(p.o + a.o.at(b, r, h), tx, acc[i], inv);
+        if (p.rest != nullptr) {
+#pragma unroll
+            for (int c = 0; c < HD / 16; ++c) {
+                const float o = acc[i][c] * inv;
+                p.rest[a.packed().at(b, r, h) + col_of<HD>(tx, c)] =
+                    from_f32<bf16>(o - to_f32(from_f32<T>(o)));
+            }
+        }
         if (p.lse != nullptr && tx == 0)
             p.lse[((long long)b * a.H + h) * a.Tq + r] =
                 l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
@@ -367,7 +377,7 @@ __global__ void __launch_bounds__(kThreads) window_dkv_simt_kernel(Attn a, Ptrs<
 // One thread per 8 values of a row: hp/8 lanes a row.
 template <class T>
 __global__ void __launch_bounds__(256) window_delta_kernel(Attn a, const T *O, const T *dO,
-                                                           float *delta, bool vec) {
+                                                           const bf16 *rest, float *delta, bool vec) {
     const int lanes = a.hp / 8;
     const long long g = (long long)blockIdx.x * 256 + threadIdx.x;
     const long long rows = (long long)a.B * a.Tq * a.H;
@@ -391,8 +401,17 @@ __global__ void __launch_bounds__(256) window_delta_kernel(Attn a, const T *O, c
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[i] = x[i], w[i] = y[i];
         }
+        float o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(to_f32(u[i]), to_f32(w[i]), sum);
+        for (int i = 0; i < 8; ++i) o[i] = to_f32(u[i]);
+        if (rest != nullptr) {
+            alignas(16) bf16 e[8];
+            *reinterpret_cast<uint4 *>(e) = *reinterpret_cast<const uint4 *>(rest + a.packed().at(b, t, h) + c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] += to_f32(e[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fmaf(o[i], to_f32(w[i]), sum);
     }
     for (int o = lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (row < rows && c == 0) delta[((long long)b * a.H + h) * a.Tq + t] = sum;
@@ -455,10 +474,11 @@ Ptrs<T> ptrs(const Attn &a, const void *q, const void *k, const void *v, const i
 
 template <class T>
 cudaError_t fwd_of(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
-                   void *O, float *lse, cudaStream_t s) {
+                   void *O, float *lse, bf16 *rest, cudaStream_t s) {
     Ptrs<T> p = ptrs<T>(a, q, k, v, lens);
     p.o = (T *)O;
     p.lse = lse;
+    p.rest = rest;
     return fwd<T>(a, p, s);
 }
 
@@ -480,9 +500,9 @@ cudaError_t bwd_of(const Attn &a, const void *q, const void *k, const void *v, c
 }  // namespace
 
 cudaError_t simt_window_fwd(const Attn &a, const void *q, const void *k, const void *v,
-                            const int32_t *lens, void *O, float *lse, cudaStream_t s) {
-    return a.bf16 ? fwd_of<bf16>(a, q, k, v, lens, O, lse, s)
-                  : fwd_of<float>(a, q, k, v, lens, O, lse, s);
+                            const int32_t *lens, void *O, float *lse, bf16 *rest, cudaStream_t s) {
+    return a.bf16 ? fwd_of<bf16>(a, q, k, v, lens, O, lse, rest, s)
+                  : fwd_of<float>(a, q, k, v, lens, O, lse, nullptr, s);
 }
 
 cudaError_t simt_window_bwd(const Attn &a, const void *q, const void *k, const void *v,
@@ -492,15 +512,17 @@ cudaError_t simt_window_bwd(const Attn &a, const void *q, const void *k, const v
                   : bwd_of<float>(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, s);
 }
 
-cudaError_t window_delta(const Attn &a, const void *O, const void *dO, float *delta,
+cudaError_t window_delta(const Attn &a, const void *O, const bf16 *rest, const void *dO, float *delta,
                          cudaStream_t s) {
     const long long n = (long long)a.B * a.Tq * a.H * (a.hp / 8);
     const bool vec = rows16(O, a.o, a.bf16) && rows16(dO, a.go, a.bf16);
     const dim3 grid((unsigned)((n + 255) / 256));
     if (a.bf16)
-        window_delta_kernel<bf16><<<grid, 256, 0, s>>>(a, (const bf16 *)O, (const bf16 *)dO, delta, vec);
+        window_delta_kernel<bf16><<<grid, 256, 0, s>>>(a, (const bf16 *)O, (const bf16 *)dO, rest, delta,
+                                                        vec);
     else
-        window_delta_kernel<float><<<grid, 256, 0, s>>>(a, (const float *)O, (const float *)dO, delta, vec);
+        window_delta_kernel<float><<<grid, 256, 0, s>>>(a, (const float *)O, (const float *)dO, nullptr,
+                                                         delta, vec);
     note_launches(1);
     return cudaGetLastError();
 }

@@ -1,0 +1,778 @@
+// Sliding-window attention with sinks on the tensor cores, backward (bf16).
+//
+// P is computed again from the forward's lse; with D = sum(dO o O) per query
+//     S = Q K^T,  P = exp(scale S - lse),  dP = dO V^T,  dS = P (dP - D)
+//     dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
+// in two kernels, so that every sum runs in one accumulator in a fixed order:
+//   dK, dV  one CTA per (128-key tile, key / value head, sequence) over the 128-query blocks
+//           of the group's heads that see it.  Scores are taken transposed
+//           (S^T = K Q^T), so that P^T and dS^T, bf16 in TMEM in the place of the
+//           scores, are the A operands of dV and dK with no pass through shared memory.
+//   dQ      one CTA per (128-query tile, head, sequence) over the key blocks it meets.
+// One kernel with five products instead of the seven here would have to add dQ up
+// from several CTAs: 64 KB of fp32 reductions per pair of tiles against 2560
+// cycles of MMAs (hp = 128), in an order that changes from run to run, and a pass to zero
+// and one to round it.
+// Keys that are sinks are seen by every later query: those queries beyond the
+// tile's window go to CTAs of their own, some blocks each, whose fp32 sums for the
+// sink rows a last small kernel adds up in order (else the first tile's CTA would
+// outlast the others by Tk / window).
+//
+// Warps 0-7 compute (two per TMEM lane quadrant, each half of the columns), warp 8
+// loads by TMA, warp 9 issues the MMAs, warp 10 (dK, dV) brings lse and D.  While MMAs
+// of one block run, the workers turn the other scores: the queue of MMAs is
+//   dK, dV:  dV_i S_i+1 | dK_i dP_i+1        dQ:  dQ_j dP_j+1 S_j+2
+// so that one pair of products always covers one half of the elementwise work.
+//
+// Where a pair of tiles is seen in part, the masked places have P = dS = 0; a NaN or
+// infinity in an operand row that meets them would still make a NaN of them.  dK, dV:
+// query rows whose lse or D is not finite are zeroed in shared memory (their P is NaN where it
+// is seen).  dQ: a CTA whose results are not all finite runs a second time with such rows of
+// K zeroed (a query that sees one has lse NaN).
+#include "launch.h"
+#include "profile.h"
+#include "window_tc.cuh"
+
+namespace mosa {
+namespace win {
+namespace {
+
+constexpr int kTile = 128;
+constexpr int kBlk = 128 * 64 * 2;      // 128 rows of 64 columns
+constexpr int kWorkers = 256;
+
+struct BwdArgs {
+    Map q, k, v, go, dq, dk, dv;
+    const int32_t *lens;
+    const float *lse, *delta;           // [B, H, Tq]
+    bf16 *dQ, *dK, *dV;
+    Str sdq, sdk, sdv;
+    float *partial;                     // [B, Hkv, slots, sinks, 2, hp] fp32: dk, dv of the sink rows
+    uint32_t *status;
+    int Tq, Tk, H, Hkv, G, hp, window, sinks;
+    int tiles, extra, chunk;            // key tiles; CTAs per sink tile beside it; their blocks
+    float scale, scale_log2;
+};
+
+// v[0 .. 31] * f of row r (zeros unless `on`) as bf16, into the 16-byte units u0 .. u0+3 of its
+// 128 bytes in a staged block.
+__device__ __forceinline__ void stage_bf16_32(uint8_t *blk, int r, int u0, const uint32_t (&v)[32],
+                                              float f, bool on) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = on ? pack_bf16x2(__uint_as_float(v[8 * u + 2 * e]) * f,
+                                    __uint_as_float(v[8 * u + 2 * e + 1]) * f) : 0u;
+        *reinterpret_cast<uint4 *>(blk + xoff128(r, u0 + u)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// ------------------------------------------------------------------ dK, dV
+
+template <int HD>
+struct KvSm {
+    static constexpr int NB = HD / 64;
+    uint8_t k[NB][kBlk], v[NB][kBlk];
+    uint8_t q[3][NB][kBlk], go[2][NB][kBlk];
+    float lse[2][kTile], delta[2][kTile];      // of a block's queries (lse in log2 units)
+    uint64_t kv_full, q_full[3], q_empty[3], g_full[2], g_empty[2], st_full[2], st_empty[2];
+    uint64_t s_full, dp_full, p_ready, ds_ready, done, drained;
+    uint32_t odd[2][4];                        // queries of the block with lse or D not finite
+    uint32_t tmem;
+    int abort;
+};
+
+constexpr int kKvThreads = 352;
+
+template <int HD>
+__global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __grid_constant__ BwdArgs p) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    using Sm = KvSm<HD>;
+    constexpr int NB = Sm::NB;
+    Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = blockIdx.z, hk = blockIdx.y, off = p.Tk - p.Tq;
+    const int len = seq_len(p.lens, b, p.Tk);
+    // the sink tiles' extra work first, then the key tiles
+    const int sink_tiles = (p.sinks + kTile - 1) / kTile, extras = sink_tiles * p.extra;
+    const bool is_extra = (int)blockIdx.x < extras;
+    const int part = is_extra ? 1 + (int)blockIdx.x % p.extra : 0;
+    const int tile = is_extra ? (int)blockIdx.x / p.extra : (int)blockIdx.x - extras;
+    const int k0 = tile * kTile;
+    const bool has_sinks = k0 < p.sinks && p.extra > 0;   // rows below p.sinks go to `partial`
+    int first = max(k0, off), last = min(k0 + kTile - 1 + p.window - 1, len - 1);
+    if (k0 < p.sinks && p.extra == 0) last = len - 1;
+    if (is_extra) {
+        first = max(k0 + kTile - 1 + p.window, off) + (part - 1) * p.chunk * kTile;
+        last = min(first + p.chunk * kTile, len) - 1;
+    }
+    const int blocks = first <= last && k0 < len ? (last - first) / kTile + 1 : 0;
+    const int n = blocks * p.G;            // (head of the group, block) pairs, heads outermost
+    float *sink_sums = p.partial + (((long long)b * p.Hkv + hk) * (p.extra + 1) + part) * p.sinks * 2 * p.hp;
+
+    if (n == 0) {   // no query sees the tile: zeros
+        const int units = p.hp / 8;
+        if (has_sinks)
+            for (int e = threadIdx.x; e < min(kTile, p.sinks - k0) * 2 * p.hp; e += kKvThreads)
+                sink_sums[(long long)k0 * 2 * p.hp + e] = 0.f;
+        if (!is_extra)
+            for (int e = threadIdx.x; e < min(kTile, p.Tk - k0) * units; e += kKvThreads) {
+                const int t = k0 + e / units;
+                if (has_sinks && t < p.sinks) continue;
+                *reinterpret_cast<uint4 *>(p.dK + p.sdk.at(b, t, hk) + e % units * 8) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(p.dV + p.sdv.at(b, t, hk) + e % units * 8) = make_uint4(0, 0, 0, 0);
+            }
+        return;
+    }
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&sm.kv_full), 1);
+        for (int s = 0; s < 3; ++s) {
+            mbar_init(smem_u32(&sm.q_full[s]), 1);
+            mbar_init(smem_u32(&sm.q_empty[s]), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(smem_u32(&sm.g_full[s]), 1);
+            mbar_init(smem_u32(&sm.g_empty[s]), 1);
+            mbar_init(smem_u32(&sm.st_full[s]), 32);
+            mbar_init(smem_u32(&sm.st_empty[s]), kWorkers);
+        }
+        mbar_init(smem_u32(&sm.s_full), 1);
+        mbar_init(smem_u32(&sm.dp_full), 1);
+        mbar_init(smem_u32(&sm.p_ready), kWorkers);
+        mbar_init(smem_u32(&sm.ds_ready), kWorkers);
+        mbar_init(smem_u32(&sm.done), 1);
+        mbar_init(smem_u32(&sm.drained), 1);
+        sm.abort = 0;
+        fence_barrier_init();
+    }
+    if (warp == 8) {
+        tmem_alloc(smem_u32(&sm.tmem), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tS = sm.tmem, tG = tS + 128, tdV = tS + 256, tdK = tS + 384;
+    auto wait = [&](uint64_t &bar, uint32_t parity) {
+        return wait_or_abort(bar, parity, &sm.abort, p.status);
+    };
+
+    if (warp == 8) {
+        if (lane == 0) {
+            const uint32_t kvb = smem_u32(&sm.kv_full);
+            mbar_expect_tx(kvb, 2 * NB * kBlk);
+            for (int c = 0; c < NB; ++c) {
+                load_box(smem_u32(sm.k[c]), p.k, kvb, 64 * c, k0, hk, b);
+                load_box(smem_u32(sm.v[c]), p.v, kvb, 64 * c, k0, hk, b);
+            }
+            int nq = 0, ng = 0;
+            for (int i = 0; i < n; ++i) {
+                const int h = hk * p.G + i / blocks, i0 = first - off + kTile * (i % blocks);
+                if (!wait(sm.q_empty[i % 3], ((i / 3) & 1) ^ 1)) break;
+                mbar_expect_tx(smem_u32(&sm.q_full[i % 3]), NB * kBlk);
+                for (int c = 0; c < NB; ++c)
+                    load_box(smem_u32(sm.q[i % 3][c]), p.q, smem_u32(&sm.q_full[i % 3]), 64 * c, i0, h, b);
+                nq = i + 1;
+                if (!wait(sm.g_empty[i & 1], ((i >> 1) & 1) ^ 1)) break;
+                mbar_expect_tx(smem_u32(&sm.g_full[i & 1]), NB * kBlk);
+                for (int c = 0; c < NB; ++c)
+                    load_box(smem_u32(sm.go[i & 1][c]), p.go, smem_u32(&sm.g_full[i & 1]), 64 * c, i0, h, b);
+                ng = i + 1;
+            }
+            drain_phase(kvb, 0);
+            for (int t = max(0, nq - 3); t < nq; ++t) drain_phase(smem_u32(&sm.q_full[t % 3]), (t / 3) & 1);
+            for (int t = max(0, ng - 2); t < ng; ++t) drain_phase(smem_u32(&sm.g_full[t & 1]), (t >> 1) & 1);
+        }
+    } else if (warp == 9) {
+        if (elect_one()) {
+            constexpr uint32_t idS = idesc_bf16(128, 128, false, false);
+            constexpr uint32_t idG = idesc_bf16(128, HD, false, true);
+            bool ok = wait(sm.kv_full, 0);
+            // D = A B^T over HD columns, both K-major tiles
+            auto scores = [&](uint32_t d, uint8_t (*A)[kBlk], uint8_t (*B)[kBlk]) {
+#pragma unroll
+                for (int c = 0; c < NB; ++c)
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+                        mma_bf16(d, smem_desc_sw128(smem_u32(A[c]) + kk * 32, 16, 1024),
+                                 smem_desc_sw128(smem_u32(B[c]) + kk * 32, 16, 1024), idS,
+                                 (c > 0 || kk > 0) ? 1u : 0u);
+            };
+            // D += W X: W bf16 in TMEM (128 x 128; columns 64.. lie 64 TMEM columns on), X rows
+            // in shared memory
+            auto add = [&](uint32_t d, uint32_t w, uint8_t (*X)[kBlk], bool more) {
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                    mma_bf16_ts(d, w + 64 * (kk >> 2) + 8 * (kk & 3),
+                                smem_desc_sw128(smem_u32(X[0]) + kk * 2048, kBlk, 1024), idG,
+                                (more || kk > 0) ? 1u : 0u);
+            };
+            auto s_of = [&](int i) {
+                ok = ok && wait(sm.q_full[i % 3], (i / 3) & 1);
+                if (!ok) return;
+                tc_fence_after();
+                scores(tS, sm.k, sm.q[i % 3]);
+                mma_commit(smem_u32(&sm.s_full));
+            };
+            auto dp_of = [&](int i) {
+                ok = ok && wait(sm.g_full[i & 1], (i >> 1) & 1);
+                if (!ok) return;
+                tc_fence_after();
+                scores(tG, sm.v, sm.go[i & 1]);
+                mma_commit(smem_u32(&sm.dp_full));
+            };
+            s_of(0);
+            dp_of(0);
+            for (int i = 0; i < n && ok; ++i) {
+                ok = wait(sm.p_ready, i & 1);
+                if (!ok) break;
+                tc_fence_after();
+                add(tdV, tS, sm.go[i & 1], i > 0);
+                mma_commit(smem_u32(&sm.g_empty[i & 1]));
+                if (i + 1 < n) s_of(i + 1);
+                ok = ok && wait(sm.ds_ready, i & 1);
+                if (!ok) break;
+                tc_fence_after();
+                add(tdK, tG, sm.q[i % 3], i > 0);
+                mma_commit(smem_u32(&sm.q_empty[i % 3]));
+                if (i + 1 < n) dp_of(i + 1);
+            }
+            mma_commit(smem_u32(&sm.done));
+            if (!ok) {
+                mma_commit(smem_u32(&sm.s_full));
+                mma_commit(smem_u32(&sm.dp_full));
+            }
+            drain_mmas(smem_u32(&sm.drained));
+        }
+    } else if (warp == 10) {
+        for (int i = 0; i < n; ++i) {
+            const int u = i & 1;
+            if (!__all_sync(0xffffffffu, wait(sm.st_empty[u], ((i >> 1) & 1) ^ 1))) break;
+            const int pq = first + kTile * (i % blocks);
+            const long long row = ((long long)b * p.H + hk * p.G + i / blocks) * p.Tq + pq - off;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int c = 32 * x + lane;
+                const bool on = pq + c < len;   // (len <= Tk)
+                float L = on ? p.lse[row + c] * kLog2e : 0.f, D = on ? p.delta[row + c] : 0.f;
+                const bool odd = !(fabsf(L) < INFINITY) || !(fabsf(D) < INFINITY);
+                if (odd) L = NAN;
+                sm.lse[u][c] = L;
+                sm.delta[u][c] = D;
+                // rows past the length are hidden from every key, whatever they hold (past Tk
+                // they were read as zeros)
+                const uint32_t w = __ballot_sync(0xffffffffu, on ? odd : pq + c < p.Tk);
+                if (lane == 0) sm.odd[u][x] = w;
+            }
+            mbar_arrive(smem_u32(&sm.st_full[u]));
+        }
+    } else {
+        const int ch = warp >> 2, r = (warp & 3) * 32 + lane, t = k0 + r;
+        const uint32_t at = ((uint32_t)((warp & 3) * 32) << 16) + 64 * ch;
+        bool ok = true;
+        for (int i = 0; i < n; ++i) {
+            const int u = i & 1, pq = first + kTile * (i % blocks);
+            const bool whole = pq >= k0 + kTile - 1 && pq + kTile - 1 - k0 < p.window &&
+                               pq + kTile - 1 <= last;
+            // columns lo .. hi of this half are seen
+            int lo = 0, hi = 63;
+            if (!whole) {
+                lo = t - pq - 64 * ch;
+                hi = min(last, t < p.sinks ? last : t + p.window - 1) - pq - 64 * ch;
+            }
+            ok = wait(sm.s_full, i & 1) && ok;
+            ok = wait(sm.st_full[u], (i >> 1) & 1) && ok;
+            tc_fence_after();
+            uint32_t raw[2][32];
+            tmem_ld32_async(tS + at, raw[0]);
+            tmem_ld32_async(tS + at + 32, raw[1]);
+            tmem_ready(raw[0]);
+            tmem_ready(raw[1]);
+            float P[64];
+            const float *L = sm.lse[u] + 64 * ch, *D = sm.delta[u] + 64 * ch;
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                const float4 l4 = *reinterpret_cast<const float4 *>(L + c);
+                const float l[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    P[c + e] = exp2_fast(fmaf(__uint_as_float(raw[(c + e) >> 5][(c + e) & 31]),
+                                              p.scale_log2, -l[e]));
+            }
+            if (!whole) {
+#pragma unroll
+                for (int c = 0; c < 64; ++c)
+                    if (c < lo || c > hi) P[c] = 0.f;
+                if ((sm.odd[u][0] | sm.odd[u][1] | sm.odd[u][2] | sm.odd[u][3]) != 0) {
+                    // zero those queries' rows, once S and dP have been taken from them
+                    ok = wait(sm.dp_full, i & 1) && ok;
+                    const int row = threadIdx.x & 127;
+                    if (((sm.odd[u][row >> 5] >> (row & 31)) & 1u) != 0) {
+                        uint8_t *x = threadIdx.x < 128 ? sm.q[i % 3][0] : sm.go[i & 1][0];
+#pragma unroll 1
+                        for (int e = 0; e < 8 * NB; ++e)
+                            *reinterpret_cast<uint4 *>(x + (e >> 3) * kBlk + row * 128 + (e & 7) * 16) =
+                                make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async();
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(P[32 * x + 2 * e], P[32 * x + 2 * e + 1]);
+                tmem_st16_async(tS + at + 16 * x, w);
+            }
+            tmem_stored();
+            tc_fence_before();
+            mbar_arrive(smem_u32(&sm.p_ready));
+
+            ok = wait(sm.dp_full, i & 1) && ok;
+            tc_fence_after();
+            tmem_ld32_async(tG + at, raw[0]);
+            tmem_ld32_async(tG + at + 32, raw[1]);
+            tmem_ready(raw[0]);
+            tmem_ready(raw[1]);
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                const float4 d4 = *reinterpret_cast<const float4 *>(D + c);
+                const float d[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    P[c + e] *= __uint_as_float(raw[(c + e) >> 5][(c + e) & 31]) - d[e];
+            }
+            if (!whole) {
+                // (again: dP may be NaN where P is 0; and a query that sees one token only has
+                // no gradient)
+                const bool none = p.window == 1 && p.sinks == 0;
+#pragma unroll
+                for (int c = 0; c < 64; ++c)
+                    if (c < lo || c > hi || none || pq + 64 * ch + c == 0) P[c] = 0.f;
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(P[32 * x + 2 * e], P[32 * x + 2 * e + 1]);
+                tmem_st16_async(tG + at + 16 * x, w);
+            }
+            tmem_stored();
+            tc_fence_before();
+            mbar_arrive(smem_u32(&sm.ds_ready));
+            mbar_arrive(smem_u32(&sm.st_empty[u]));
+        }
+        ok = wait(sm.done, 0) && ok;
+        tc_fence_after();
+        named_barrier(1, kWorkers);
+        if (*(volatile int *)&sm.abort == 0) {
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+            // this thread's half of the row's columns, 32 at a time
+#pragma unroll
+            for (int x = 0; x < HD / 64; ++x) {
+                const int c = ch * (HD / 2) + 32 * x;
+                uint32_t dv[32], dk[32];
+                tmem_ld32_async(tdV + lanes + c, dv);
+                tmem_ld32_async(tdK + lanes + c, dk);
+                tmem_ready(dv);
+                tmem_ready(dk);
+                if (!has_sinks) {
+                    stage_bf16_32(sm.v[c >> 6], r, (c & 63) >> 3, dv, 1.f, true);
+                    stage_bf16_32(sm.k[c >> 6], r, (c & 63) >> 3, dk, p.scale, true);
+                } else if (t < p.Tk && c < p.hp && (t < p.sinks || !is_extra)) {
+                    // columns in units of 8 (hp = 16 ends inside these 32)
+                    const int end = min(32, p.hp - c);
+#pragma unroll
+                    for (int u = 0; u < 32; u += 8) {
+                        if (u >= end) break;
+                        if (t < p.sinks) {
+                            float *o = sink_sums + (long long)t * 2 * p.hp + c + u;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                o[e] = __uint_as_float(dk[u + e]) * p.scale;
+                                o[p.hp + e] = __uint_as_float(dv[u + e]);
+                            }
+                        } else {
+                            uint32_t wk[4], wv[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                wk[e] = pack_bf16x2(__uint_as_float(dk[u + 2 * e]) * p.scale,
+                                                    __uint_as_float(dk[u + 2 * e + 1]) * p.scale);
+                                wv[e] = pack_bf16x2(__uint_as_float(dv[u + 2 * e]),
+                                                    __uint_as_float(dv[u + 2 * e + 1]));
+                            }
+                            *reinterpret_cast<uint4 *>(p.dK + p.sdk.at(b, t, hk) + c + u) =
+                                make_uint4(wk[0], wk[1], wk[2], wk[3]);
+                            *reinterpret_cast<uint4 *>(p.dV + p.sdv.at(b, t, hk) + c + u) =
+                                make_uint4(wv[0], wv[1], wv[2], wv[3]);
+                        }
+                    }
+                }
+            }
+            if (!has_sinks) {
+                fence_proxy_async();
+                named_barrier(1, kWorkers);
+                if (threadIdx.x == 0) {
+                    for (int c = 0; c < NB; ++c) {
+                        store_box(p.dv, smem_u32(sm.v[c]), 64 * c, k0, hk, b);
+                        store_box(p.dk, smem_u32(sm.k[c]), 64 * c, k0, hk, b);
+                    }
+                    bulk_commit();
+                    bulk_wait_read0();
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 8) tmem_dealloc(sm.tmem, 512);
+}
+
+// dk and dv of the sink rows: the tile's own sum and the extra CTAs', in order.
+__global__ void __launch_bounds__(256) window_sink_rows_kernel(const __grid_constant__ BwdArgs p) {
+    const int b = blockIdx.z, hk = blockIdx.y, t = blockIdx.x;
+    for (int e = threadIdx.x; e < 2 * p.hp; e += blockDim.x) {
+        const float *s = p.partial + (((long long)b * p.Hkv + hk) * (p.extra + 1) * p.sinks + t) * 2 * p.hp + e;
+        float sum = 0.f;
+        for (int x = 0; x <= p.extra; ++x) sum += s[(long long)x * p.sinks * 2 * p.hp];
+        if (e < p.hp) p.dK[p.sdk.at(b, t, hk) + e] = from_f32<bf16>(sum);
+        else p.dV[p.sdv.at(b, t, hk) + e - p.hp] = from_f32<bf16>(sum);
+    }
+}
+
+// ---------------------------------------------------------------------- dQ
+
+template <int HD>
+struct QSm {
+    static constexpr int NB = HD / 64;
+    uint8_t q[NB][kBlk], go[NB][kBlk];
+    uint8_t k[3][NB][kBlk], v[2][NB][kBlk];
+    uint64_t q_full, k_full[3], k_empty[3], v_full[2], v_empty[2];
+    uint64_t s_full[2], dp_full, ds_ready, done, drained;
+    uint32_t tmem;
+    int abort, redo;
+};
+
+constexpr int kQThreads = 320;
+
+template <int HD>
+__global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid_constant__ BwdArgs p) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    using Sm = QSm<HD>;
+    constexpr int NB = Sm::NB;
+    Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = blockIdx.z, h = blockIdx.y, hk = h / p.G, off = p.Tk - p.Tq;
+    const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kTile;
+    const int len = seq_len(p.lens, b, p.Tk);
+    const int pf = off + i0, pl = min(off + min(i0 + kTile, p.Tq), len) - 1;
+    if (pl < pf) {
+        const int rows = min(kTile, p.Tq - i0), units = p.hp / 8;
+        for (int e = threadIdx.x; e < rows * units; e += kQThreads)
+            *reinterpret_cast<uint4 *>(p.dQ + p.sdq.at(b, i0 + e / units, h) + e % units * 8) =
+                make_uint4(0, 0, 0, 0);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&sm.q_full), 1);
+        for (int s = 0; s < 3; ++s) {
+            mbar_init(smem_u32(&sm.k_full[s]), 1);
+            mbar_init(smem_u32(&sm.k_empty[s]), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(smem_u32(&sm.v_full[s]), 1);
+            mbar_init(smem_u32(&sm.v_empty[s]), 1);
+            mbar_init(smem_u32(&sm.s_full[s]), 1);
+        }
+        mbar_init(smem_u32(&sm.dp_full), 1);
+        mbar_init(smem_u32(&sm.ds_ready), kWorkers);
+        mbar_init(smem_u32(&sm.done), 1);
+        mbar_init(smem_u32(&sm.drained), 1);
+        sm.abort = sm.redo = 0;
+        fence_barrier_init();
+    }
+    if (warp == 8) {
+        tmem_alloc(smem_u32(&sm.tmem), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tS = sm.tmem, tG = tS + 256, tdQ = tS + 384;   // S buffers at tS, tS + 128
+    const KeyBlocks<kTile> kb(pf, pl, p.window, p.sinks);
+    const int n = kb.count();
+    auto wait = [&](uint64_t &bar, uint32_t parity) {
+        return wait_or_abort(bar, parity, &sm.abort, p.status);
+    };
+    bool ok = true;
+    // Key blocks of both passes are numbered on: block j of pass 1 is number n + j, and its S
+    // lies in buffer number & 1.
+    for (int pass = 0; pass < 2; ++pass) {
+        const int g0 = pass * n;
+        if (warp == 8) {
+            if (lane == 0) {
+                if (pass == 0) {
+                    mbar_expect_tx(smem_u32(&sm.q_full), 2 * NB * kBlk);
+                    for (int c = 0; c < NB; ++c) {
+                        load_box(smem_u32(sm.q[c]), p.q, smem_u32(&sm.q_full), 64 * c, i0, h, b);
+                        load_box(smem_u32(sm.go[c]), p.go, smem_u32(&sm.q_full), 64 * c, i0, h, b);
+                    }
+                }
+                int nk = g0, nv = g0;
+                for (int j = 0; j < n && ok; ++j) {
+                    const int g = g0 + j, ks = kb.start(j);
+                    ok = wait(sm.k_empty[g % 3], ((g / 3) & 1) ^ 1);
+                    if (!ok) break;
+                    mbar_expect_tx(smem_u32(&sm.k_full[g % 3]), NB * kBlk);
+                    for (int c = 0; c < NB; ++c)
+                        load_box(smem_u32(sm.k[g % 3][c]), p.k, smem_u32(&sm.k_full[g % 3]), 64 * c, ks, hk, b);
+                    nk = g + 1;
+                    ok = wait(sm.v_empty[g & 1], ((g >> 1) & 1) ^ 1);
+                    if (!ok) break;
+                    mbar_expect_tx(smem_u32(&sm.v_full[g & 1]), NB * kBlk);
+                    for (int c = 0; c < NB; ++c)
+                        load_box(smem_u32(sm.v[g & 1][c]), p.v, smem_u32(&sm.v_full[g & 1]), 64 * c, ks, hk, b);
+                    nv = g + 1;
+                }
+                drain_phase(smem_u32(&sm.q_full), 0);
+                for (int t = max(0, nk - 3); t < nk; ++t) drain_phase(smem_u32(&sm.k_full[t % 3]), (t / 3) & 1);
+                for (int t = max(0, nv - 2); t < nv; ++t) drain_phase(smem_u32(&sm.v_full[t & 1]), (t >> 1) & 1);
+            }
+            __syncwarp();
+        } else if (warp == 9) {
+            if (elect_one()) {
+                constexpr uint32_t idS = idesc_bf16(128, 128, false, false);
+                constexpr uint32_t idG = idesc_bf16(128, HD, false, true);
+                ok = ok && wait(sm.q_full, 0);
+                auto scores = [&](uint32_t d, uint8_t (*A)[kBlk], uint8_t (*B)[kBlk]) {
+#pragma unroll
+                    for (int c = 0; c < NB; ++c)
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            mma_bf16(d, smem_desc_sw128(smem_u32(A[c]) + kk * 32, 16, 1024),
+                                     smem_desc_sw128(smem_u32(B[c]) + kk * 32, 16, 1024), idS,
+                                     (c > 0 || kk > 0) ? 1u : 0u);
+                };
+                auto s_of = [&](int g) {
+                    ok = ok && wait(sm.k_full[g % 3], (g / 3) & 1);
+                    if (!ok) return;
+                    tc_fence_after();
+                    scores(tS + 128 * (g & 1), sm.q, sm.k[g % 3]);
+                    mma_commit(smem_u32(&sm.s_full[g & 1]));
+                };
+                auto dp_of = [&](int g) {
+                    ok = ok && wait(sm.v_full[g & 1], (g >> 1) & 1);
+                    if (!ok) return;
+                    tc_fence_after();
+                    scores(tG, sm.go, sm.v[g & 1]);
+                    mma_commit(smem_u32(&sm.dp_full));
+                    mma_commit(smem_u32(&sm.v_empty[g & 1]));
+                };
+                s_of(g0);
+                dp_of(g0);
+                if (n > 1) s_of(g0 + 1);
+                for (int j = 0; j < n && ok; ++j) {
+                    const int g = g0 + j;
+                    ok = wait(sm.ds_ready, g & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)   // dQ += dS K_j
+                        mma_bf16_ts(tdQ, tS + 128 * (g & 1) + 64 * (kk >> 2) + 8 * (kk & 3),
+                                    smem_desc_sw128(smem_u32(sm.k[g % 3][0]) + kk * 2048, kBlk, 1024), idG,
+                                    (j > 0 || kk > 0) ? 1u : 0u);
+                    mma_commit(smem_u32(&sm.k_empty[g % 3]));
+                    if (j + 1 < n) dp_of(g + 1);
+                    if (j + 2 < n) s_of(g + 2);
+                }
+                mma_commit(smem_u32(&sm.done));
+                if (!ok) {
+                    mma_commit(smem_u32(&sm.s_full[0]));
+                    mma_commit(smem_u32(&sm.s_full[1]));
+                    mma_commit(smem_u32(&sm.dp_full));
+                }
+            }
+            __syncwarp();
+        } else {
+            const int ch = warp >> 2, r = (warp & 3) * 32 + lane, pos = pf + r;
+            const bool valid = pos <= pl;
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, at = lanes + 64 * ch;
+            const long long row = ((long long)b * p.H + h) * p.Tq + i0 + r;
+            // a query that sees one token only has no gradient: P = 0
+            const float L = !valid ? 0.f : sees_one(pos, p.window, p.sinks) ? INFINITY : p.lse[row] * kLog2e;
+            const float D = valid ? p.delta[row] : 0.f;
+            for (int j = 0; j < n; ++j) {
+                const int g = g0 + j, ks = kb.start(j);
+                const uint32_t tSj = tS + 128 * (g & 1) + at;
+                const bool whole = kb.whole(j, pf, pl, p.window);
+                ok = wait(sm.s_full[g & 1], (g >> 1) & 1) && ok;
+                tc_fence_after();
+                uint32_t raw[2][32];
+                tmem_ld32_async(tSj, raw[0]);
+                tmem_ld32_async(tSj + 32, raw[1]);
+                tmem_ready(raw[0]);
+                tmem_ready(raw[1]);
+                float P[64];
+#pragma unroll
+                for (int c = 0; c < 64; ++c)
+                    P[c] = exp2_fast(fmaf(__uint_as_float(raw[c >> 5][c & 31]), p.scale_log2, -L));
+                ok = wait(sm.dp_full, g & 1) && ok;
+                tc_fence_after();
+                tmem_ld32_async(tG + at, raw[0]);
+                tmem_ld32_async(tG + at + 32, raw[1]);
+                tmem_ready(raw[0]);
+                tmem_ready(raw[1]);
+#pragma unroll
+                for (int c = 0; c < 64; ++c) P[c] *= __uint_as_float(raw[c >> 5][c & 31]) - D;
+                if (!whole) {
+                    int first = 0, last = kTile - 1, sink = 0;
+                    const int low = max(-ks, 0) - 64 * ch;
+                    if (!kb.is_far(j)) {
+                        first = max(pos - p.window + 1, 0) - ks;
+                        last = min(pos - ks, kTile - 1);
+                        sink = min(p.sinks - ks, last + 1);
+                    } else {
+                        last = kb.slim - ks - 1;
+                    }
+                    first -= 64 * ch;
+                    last -= 64 * ch;
+                    sink -= 64 * ch;
+#pragma unroll
+                    for (int c = 0; c < 64; ++c)
+                        if (!(c <= last && c >= low && (c >= first || c < sink))) P[c] = 0.f;
+                    if (pass == 1) {
+                        if (ch == 0) {
+                            uint8_t *blk[NB];
+                            for (int c = 0; c < NB; ++c) blk[c] = sm.k[g % 3][c];
+                            clean_row<NB>(blk, r);
+                        }
+                        fence_proxy_async();
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(P[32 * x + 2 * e], P[32 * x + 2 * e + 1]);
+                    tmem_st16_async(tSj + 16 * x, w);
+                }
+                tmem_stored();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&sm.ds_ready));
+            }
+            ok = wait(sm.done, pass) && ok;
+            tc_fence_after();
+            uint32_t raw[HD / 64][32];
+#pragma unroll
+            for (int x = 0; x < HD / 64; ++x) tmem_ld32_async(tdQ + lanes + ch * (HD / 2) + 32 * x, raw[x]);
+#pragma unroll
+            for (int x = 0; x < HD / 64; ++x) tmem_ready(raw[x]);
+            float odd = 0.f;
+#pragma unroll
+            for (int x = 0; x < HD / 64; ++x)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) odd = fmaf(__uint_as_float(raw[x][e]), 0.f, odd);
+            if (pass == 0 && valid && !(odd == 0.f)) sm.redo = 1;
+            named_barrier(1, kWorkers);
+            if (*(volatile int *)&sm.abort == 0 && (pass == 1 || *(volatile int *)&sm.redo == 0)) {
+#pragma unroll
+                for (int x = 0; x < HD / 64; ++x) {
+                    const int c = ch * (HD / 2) + 32 * x;
+                    stage_bf16_32(sm.q[c >> 6], r, (c & 63) >> 3, raw[x], p.scale, valid);
+                }
+                fence_proxy_async();
+                named_barrier(1, kWorkers);
+                if (threadIdx.x == 0) {
+                    for (int c = 0; c < NB; ++c) store_box(p.dq, smem_u32(sm.q[c]), 64 * c, i0, h, b);
+                    bulk_commit();
+                    bulk_wait_read0();
+                }
+            }
+        }
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        if (*(volatile int *)&sm.redo == 0 || *(volatile int *)&sm.abort != 0) break;
+    }
+    if (warp == 9 && elect_one()) drain_mmas(smem_u32(&sm.drained));
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(sm.tmem, 512);
+}
+
+// Extra CTAs per sink tile, and the query blocks of each: as many as a tile without
+// sinks has, so that all CTAs take about as long.
+void split_sinks(const Attn &a, int *extra, int *chunk) {
+    *chunk = (a.window + kTile - 2) / kTile + 1;
+    const long long beyond = (long long)a.Tk - (kTile - 1 + (long long)a.window);
+    *extra = a.sinks > 0 && beyond > 0
+                 ? (int)((beyond + (long long)*chunk * kTile - 1) / ((long long)*chunk * kTile)) : 0;
+}
+
+template <int HD>
+cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
+    constexpr int kv = (int)sizeof(KvSm<HD>), qb = (int)sizeof(QSm<HD>);
+    static_assert(kv <= 227 * 1024 && qb <= 227 * 1024, "shared memory");
+    cudaError_t e = allow_smem((const void *)window_dkv_tc_kernel<HD>, kv);
+    if (e == cudaSuccess) e = allow_smem((const void *)window_dq_tc_kernel<HD>, qb);
+    if (e != cudaSuccess) return e;
+    const int sink_tiles = (p.sinks + kTile - 1) / kTile;
+    window_dkv_tc_kernel<HD><<<dim3(p.tiles + sink_tiles * p.extra, p.Hkv, B), kKvThreads, kv, s>>>(p);
+    window_dq_tc_kernel<HD><<<dim3((p.Tq + kTile - 1) / kTile, p.H, B), kQThreads, qb, s>>>(p);
+    note_launches(2);
+    if (p.extra > 0) {
+        window_sink_rows_kernel<<<dim3(p.sinks, p.Hkv, B), 256, 0, s>>>(p);
+        note_launches(1);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t tc_window_bwd_bytes(const Attn &a) {
+    int extra, chunk;
+    split_sinks(a, &extra, &chunk);
+    return extra == 0 ? 0 : (size_t)a.B * a.Hkv * (extra + 1) * a.sinks * 2 * a.hp * sizeof(float);
+}
+
+bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
+                   const float *lse, const void *dO, const float *delta, void *dq, void *dk, void *dv,
+                   float *partial, uint32_t *status, cudaStream_t s, cudaError_t *err) {
+    if (!a.bf16) return false;
+    BwdArgs p;
+    if (!make_map(&p.q, q, a.q, a.B, a.Tq, a.H, a.hp) || !make_map(&p.k, k, a.k, a.B, a.Tk, a.Hkv, a.hp) ||
+        !make_map(&p.v, v, a.v, a.B, a.Tk, a.Hkv, a.hp) || !make_map(&p.go, dO, a.go, a.B, a.Tq, a.H, a.hp) ||
+        !make_map(&p.dq, dq, a.dq, a.B, a.Tq, a.H, a.hp) || !make_map(&p.dk, dk, a.dk, a.B, a.Tk, a.Hkv, a.hp) ||
+        !make_map(&p.dv, dv, a.dv, a.B, a.Tk, a.Hkv, a.hp))
+        return false;
+    p.lens = lens;
+    p.lse = lse;
+    p.delta = delta;
+    p.dQ = (bf16 *)dq;
+    p.dK = (bf16 *)dk;
+    p.dV = (bf16 *)dv;
+    p.sdq = a.dq;
+    p.sdk = a.dk;
+    p.sdv = a.dv;
+    p.partial = partial;
+    p.status = status;
+    p.Tq = a.Tq;
+    p.Tk = a.Tk;
+    p.H = a.H;
+    p.Hkv = a.Hkv;
+    p.G = a.G();
+    p.hp = a.hp;
+    p.window = a.window;
+    p.sinks = a.sinks;
+    p.tiles = (a.Tk + kTile - 1) / kTile;
+    split_sinks(a, &p.extra, &p.chunk);
+    p.scale = a.scale;
+    p.scale_log2 = a.scale * kLog2e;
+    *err = a.hp <= 64 ? launch<64>(p, a.B, s) : launch<128>(p, a.B, s);
+    return true;
+}
+
+}  // namespace win
+}  // namespace mosa

@@ -14,10 +14,13 @@ __device__ __forceinline__ int seq_len(const int32_t *lens, int b, int Tk) {
     return lens == nullptr ? Tk : min(max(lens[b], 0), Tk);
 }
 
-// Key blocks of NK tokens for the queries at positions pf .. pl (pf <= pl < len).
-// Blocks 0 .. near-1 walk down from the last query's own position (block 0 holds it),
-// so that window + tile tokens take as few blocks as can be wherever the tile
-// starts; blocks near .. near+far-1 hold the sinks below them, from token 0 up.
+// Key blocks of NK tokens for the queries at positions pf .. pl (pf <= pl < len), in the
+// order of their tokens: blocks 0 .. far-1 hold the sinks below the window, from token 0 up,
+// the others lead up to the last query's own position, the end of the last block, so
+// that window + tile tokens take as few blocks as can be wherever the tile starts.
+// Sinks come first because weight often lies on them: a softmax whose running
+// maximum starts there seldom has to be rescaled, and their weights are powers of two then,
+// which a rounding to bf16 leaves as they are.
 template <int NK>
 struct KeyBlocks {
     int top, near, far, slim;   // slim: sinks [0, slim) are left to the far blocks
@@ -29,19 +32,20 @@ struct KeyBlocks {
         far = (slim + NK - 1) / NK;
     }
     __device__ __forceinline__ int count() const { return near + far; }
+    __device__ __forceinline__ bool is_far(int j) const { return j < far; }
     __device__ __forceinline__ int start(int j) const {
-        return j < near ? top - NK * (j + 1) : NK * (j - near);
+        return is_far(j) ? NK * j : top - NK * (far + near - j);
     }
     // Every query pf .. pl sees every key of block j.
     __device__ __forceinline__ bool whole(int j, int pf, int pl, int window) const {
         const int ks = start(j);
-        if (j >= near) return ks + NK <= slim;
+        if (is_far(j)) return ks + NK <= slim;
         return ks >= 0 && ks + NK - 1 <= pf && pl - ks < window;
     }
     // Whether position p (in pf .. pl) sees column c of block j, which starts at ks.
     __device__ __forceinline__ bool sees(int j, int ks, int c, int p, int window, int sinks) const {
         const int t = ks + c;
-        if (j >= near) return t < slim;
+        if (is_far(j)) return t < slim;
         return t >= 0 && t <= p && (p - t < window || t < sinks);
     }
 };

@@ -363,3 +363,17 @@ def test_decode_in_a_cache_past_32_bits():
     S = torch.einsum("bhd,bthd->bht", q.double(), small[0][:, -50:].double()) / math.sqrt(hp)
     want = torch.einsum("bht,bthd->bhd", torch.softmax(S, -1), small[1][:, -50:].double())
     assert rel(O, want) < 4e-3
+
+
+@pytest.mark.parametrize("hp", [64, 128])
+@pytest.mark.parametrize("force", ["0", "1"])
+def test_gradients_where_the_weight_lies_on_one_token(hp, force, monkeypatch):
+    """A strong sink: dP - D cancels there, so D must not carry O's rounding (with it these
+    gradients are off by 2e-2 and more).  The scores' gradients are rounded once, 2^-9 of each."""
+    monkeypatch.setenv("MOSA_FORCE_SIMT", force)
+    q, k, v, dO = inputs(2, 300, 300, 4, 2, hp, "bf16", seed=31, layout="plain")
+    u = torch.randn(hp, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda")
+    q += (0.7 * u).to(q.dtype)
+    k[:, :1] += (0.7 * u).to(k.dtype)
+    want = ref.attention(q, k, v, 24, 1, dO=dO)
+    check(run(q, k, v, dO, 24, 1), want, torch.bfloat16)
