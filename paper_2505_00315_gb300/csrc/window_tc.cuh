@@ -50,15 +50,61 @@ __device__ __forceinline__ void store_box(const Map &m, uint32_t src, int c, int
         : "memory");
 }
 
-// Waits for a phase; gives up (false) at once when the CTA is giving up, and after the
-// usual limit, which sets the status.
+// Waits for a phase; gives up (false) when the CTA is giving up, and after the usual
+// limit, which sets the status.
 __device__ __forceinline__ bool wait_or_abort(uint64_t &bar, uint32_t parity, int *abort,
                                               uint32_t *status) {
-    if (*(volatile int *)abort) return false;
-    if (mbar_wait(smem_u32(&bar), parity)) return true;
-    atomicOr(status, kStatusTimeout);
-    *(volatile int *)abort = 1;
-    return false;
+    const uint32_t at = smem_u32(&bar);
+    if (mbar_try_wait(at, parity)) return true;
+    const unsigned long long t0 = globaltimer();
+    while (!mbar_try_wait(at, parity)) {
+        if (*(volatile int *)abort) return false;
+        if (globaltimer() - t0 > kWaitLimitNs) {
+            atomicOr(status, kStatusTimeout);
+            *(volatile int *)abort = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
+// Products of whole tiles, issued by one thread.  Operand tiles are NB 64-column blocks of 128
+// rows, kBlk bytes apart; their descriptors differ by constants from the first, so that a
+// product costs the issuing thread a few instructions and not the dozen of a descriptor made
+// anew (8 products then take longer to issue than to run).
+constexpr int kBlk = 128 * 64 * 2;
+
+// D = A B^T over 64 NB columns, both K-major.
+template <int NB>
+__device__ __forceinline__ void mma_scores(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
+#pragma unroll
+    for (int c = 0; c < NB; ++c)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+            mma_bf16(d, a + (uint32_t)(c * (kBlk >> 4) + 2 * kk), b + (uint32_t)(c * (kBlk >> 4) + 2 * kk),
+                     idesc, (c > 0 || kk > 0) ? 1u : 0u);
+}
+// D (+)= W X: W bf16 in TMEM, 128 columns of 16 bits, 2^lg of them every 2^lg TMEM columns (a
+// worker's columns start where its scores did); X 128 rows read MN-major.
+template <int lg>
+__device__ __forceinline__ void mma_weights(uint32_t d, uint32_t w, uint64_t x, uint32_t idesc, bool more) {
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+        mma_bf16_ts(d, w + ((16 * kk) >> lg << lg) + (((16 * kk) & ((1 << lg) - 1)) >> 1), x + 128u * kk,
+                    idesc, (more || kk > 0) ? 1u : 0u);
+}
+__device__ __forceinline__ uint64_t k_major(const void *tile) {
+    return smem_desc_sw128(smem_u32(tile), 16, 1024);
+}
+__device__ __forceinline__ uint64_t mn_major(const void *tile) {
+    return smem_desc_sw128(smem_u32(tile), kBlk, 1024);
+}
+
+// One arrival for the whole warp, after what its lanes did before (an arrival of every lane goes
+// through the barrier's word one by one).
+__device__ __forceinline__ void warp_arrive(uint64_t &bar, int lane) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&bar));
 }
 
 // 32 columns of this thread's TMEM lane, without waiting: the values may be used only
@@ -101,6 +147,44 @@ __device__ __forceinline__ void tmem_stored() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long &>(d))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)),
+          "l"(reinterpret_cast<unsigned long long &>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long &>(d))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long &>(d))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return d;
+}
+
+// Bits lo .. hi of 32 (any of them may lie outside).
+__device__ __forceinline__ uint32_t bits(int lo, int hi) {
+    const uint32_t a = lo <= 0 ? ~0u : lo > 31 ? 0u : ~0u << lo;
+    return hi < 0 ? 0u : hi >= 31 ? a : a & ((2u << hi) - 1u);
+}
+// Which of the 32 columns from c0 on of key block j (start ks) position pos sees, as bits.
+__device__ __forceinline__ uint32_t seen_bits(const KeyBlocks<128> &kb, int j, int ks, int c0, int pos,
+                                              int window, int sinks) {
+    if (kb.is_far(j)) return bits(0, kb.slim - ks - 1 - c0);
+    const int low = max(-ks, 0) - c0, last = pos - ks - c0;
+    return bits(max(max(pos - window + 1, 0) - ks - c0, low), last) |
+           bits(low, min(sinks - ks - 1 - c0, last));
+}
+
 // Two values as a bf16x2 word, rounded to nearest even, a in the low half.
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
     uint32_t w;
@@ -113,24 +197,19 @@ __device__ __forceinline__ bool odd_bf16x2(uint32_t w) {
     return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }
 
-// Zeroes row r of a tile of NB 64-column blocks (128-byte rows, 16 KB apart) where it
-// holds a NaN or an infinity; says whether it did.
+// Zeroes row r of a tile of NB blocks where it holds a NaN or an infinity; says whether it did.
 template <int NB>
-__device__ __forceinline__ bool clean_row(uint8_t *(&blk)[NB], int r) {
+__device__ __forceinline__ bool clean_row(uint8_t *tile, int r) {
     bool odd = false;
 #pragma unroll 1
-    for (int n = 0; n < NB; ++n)
-#pragma unroll 1
-        for (int u = 0; u < 8; ++u) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(blk[n] + r * 128 + u * 16);
-            odd = odd || odd_bf16x2(w.x) || odd_bf16x2(w.y) || odd_bf16x2(w.z) || odd_bf16x2(w.w);
-        }
+    for (int u = 0; u < 8 * NB; ++u) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(tile + (u >> 3) * kBlk + r * 128 + (u & 7) * 16);
+        odd = odd || odd_bf16x2(w.x) || odd_bf16x2(w.y) || odd_bf16x2(w.z) || odd_bf16x2(w.w);
+    }
     if (odd)
 #pragma unroll 1
-        for (int n = 0; n < NB; ++n)
-#pragma unroll 1
-            for (int u = 0; u < 8; ++u)
-                *reinterpret_cast<uint4 *>(blk[n] + r * 128 + u * 16) = make_uint4(0, 0, 0, 0);
+        for (int u = 0; u < 8 * NB; ++u)
+            *reinterpret_cast<uint4 *>(tile + (u >> 3) * kBlk + r * 128 + (u & 7) * 16) = make_uint4(0, 0, 0, 0);
     return odd;
 }
 

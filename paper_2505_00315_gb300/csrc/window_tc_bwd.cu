@@ -38,8 +38,7 @@ namespace win {
 namespace {
 
 constexpr int kTile = 128;
-constexpr int kBlk = 128 * 64 * 2;      // 128 rows of 64 columns
-constexpr int kWorkers = 256;
+constexpr int kWorkers = 256, kWarps = 8;
 
 struct BwdArgs {
     Map q, k, v, go, dq, dk, dv;
@@ -135,13 +134,13 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(&sm.g_full[s]), 1);
             mbar_init(smem_u32(&sm.g_empty[s]), 1);
-            mbar_init(smem_u32(&sm.st_full[s]), 32);
-            mbar_init(smem_u32(&sm.st_empty[s]), kWorkers);
+            mbar_init(smem_u32(&sm.st_full[s]), 1);
+            mbar_init(smem_u32(&sm.st_empty[s]), kWarps);
         }
         mbar_init(smem_u32(&sm.s_full), 1);
         mbar_init(smem_u32(&sm.dp_full), 1);
-        mbar_init(smem_u32(&sm.p_ready), kWorkers);
-        mbar_init(smem_u32(&sm.ds_ready), kWorkers);
+        mbar_init(smem_u32(&sm.p_ready), kWarps);
+        mbar_init(smem_u32(&sm.ds_ready), kWarps);
         mbar_init(smem_u32(&sm.done), 1);
         mbar_init(smem_u32(&sm.drained), 1);
         sm.abort = 0;
@@ -190,37 +189,19 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
             constexpr uint32_t idS = idesc_bf16(128, 128, false, false);
             constexpr uint32_t idG = idesc_bf16(128, HD, false, true);
             bool ok = wait(sm.kv_full, 0);
-            // D = A B^T over HD columns, both K-major tiles
-            auto scores = [&](uint32_t d, uint8_t (*A)[kBlk], uint8_t (*B)[kBlk]) {
-#pragma unroll
-                for (int c = 0; c < NB; ++c)
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        mma_bf16(d, smem_desc_sw128(smem_u32(A[c]) + kk * 32, 16, 1024),
-                                 smem_desc_sw128(smem_u32(B[c]) + kk * 32, 16, 1024), idS,
-                                 (c > 0 || kk > 0) ? 1u : 0u);
-            };
-            // D += W X: W bf16 in TMEM (128 x 128; columns 64.. lie 64 TMEM columns on), X rows
-            // in shared memory
-            auto add = [&](uint32_t d, uint32_t w, uint8_t (*X)[kBlk], bool more) {
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    mma_bf16_ts(d, w + 64 * (kk >> 2) + 8 * (kk & 3),
-                                smem_desc_sw128(smem_u32(X[0]) + kk * 2048, kBlk, 1024), idG,
-                                (more || kk > 0) ? 1u : 0u);
-            };
+            const uint64_t dk = k_major(sm.k), dv = k_major(sm.v);
             auto s_of = [&](int i) {
                 ok = ok && wait(sm.q_full[i % 3], (i / 3) & 1);
                 if (!ok) return;
                 tc_fence_after();
-                scores(tS, sm.k, sm.q[i % 3]);
+                mma_scores<NB>(tS, dk, k_major(sm.q[i % 3]), idS);
                 mma_commit(smem_u32(&sm.s_full));
             };
             auto dp_of = [&](int i) {
                 ok = ok && wait(sm.g_full[i & 1], (i >> 1) & 1);
                 if (!ok) return;
                 tc_fence_after();
-                scores(tG, sm.v, sm.go[i & 1]);
+                mma_scores<NB>(tG, dv, k_major(sm.go[i & 1]), idS);
                 mma_commit(smem_u32(&sm.dp_full));
             };
             s_of(0);
@@ -229,13 +210,13 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                 ok = wait(sm.p_ready, i & 1);
                 if (!ok) break;
                 tc_fence_after();
-                add(tdV, tS, sm.go[i & 1], i > 0);
+                mma_weights<6>(tdV, tS, mn_major(sm.go[i & 1]), idG, i > 0);
                 mma_commit(smem_u32(&sm.g_empty[i & 1]));
                 if (i + 1 < n) s_of(i + 1);
                 ok = ok && wait(sm.ds_ready, i & 1);
                 if (!ok) break;
                 tc_fence_after();
-                add(tdK, tG, sm.q[i % 3], i > 0);
+                mma_weights<6>(tdK, tG, mn_major(sm.q[i % 3]), idG, i > 0);
                 mma_commit(smem_u32(&sm.q_empty[i % 3]));
                 if (i + 1 < n) dp_of(i + 1);
             }
@@ -266,7 +247,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                 const uint32_t w = __ballot_sync(0xffffffffu, on ? odd : pq + c < p.Tk);
                 if (lane == 0) sm.odd[u][x] = w;
             }
-            mbar_arrive(smem_u32(&sm.st_full[u]));
+            warp_arrive(sm.st_full[u], lane);
         }
     } else {
         const int ch = warp >> 2, r = (warp & 3) * 32 + lane, t = k0 + r;
@@ -328,7 +309,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
             }
             tmem_stored();
             tc_fence_before();
-            mbar_arrive(smem_u32(&sm.p_ready));
+            warp_arrive(sm.p_ready, lane);
 
             ok = wait(sm.dp_full, i & 1) && ok;
             tc_fence_after();
@@ -361,8 +342,8 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
             }
             tmem_stored();
             tc_fence_before();
-            mbar_arrive(smem_u32(&sm.ds_ready));
-            mbar_arrive(smem_u32(&sm.st_empty[u]));
+            warp_arrive(sm.ds_ready, lane);
+            warp_arrive(sm.st_empty[u], lane);
         }
         ok = wait(sm.done, 0) && ok;
         tc_fence_after();
@@ -488,7 +469,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
             mbar_init(smem_u32(&sm.s_full[s]), 1);
         }
         mbar_init(smem_u32(&sm.dp_full), 1);
-        mbar_init(smem_u32(&sm.ds_ready), kWorkers);
+        mbar_init(smem_u32(&sm.ds_ready), kWarps);
         mbar_init(smem_u32(&sm.done), 1);
         mbar_init(smem_u32(&sm.drained), 1);
         sm.abort = sm.redo = 0;
@@ -547,27 +528,19 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 constexpr uint32_t idS = idesc_bf16(128, 128, false, false);
                 constexpr uint32_t idG = idesc_bf16(128, HD, false, true);
                 ok = ok && wait(sm.q_full, 0);
-                auto scores = [&](uint32_t d, uint8_t (*A)[kBlk], uint8_t (*B)[kBlk]) {
-#pragma unroll
-                    for (int c = 0; c < NB; ++c)
-#pragma unroll
-                        for (int kk = 0; kk < 4; ++kk)
-                            mma_bf16(d, smem_desc_sw128(smem_u32(A[c]) + kk * 32, 16, 1024),
-                                     smem_desc_sw128(smem_u32(B[c]) + kk * 32, 16, 1024), idS,
-                                     (c > 0 || kk > 0) ? 1u : 0u);
-                };
+                const uint64_t dq = k_major(sm.q), dg = k_major(sm.go);
                 auto s_of = [&](int g) {
                     ok = ok && wait(sm.k_full[g % 3], (g / 3) & 1);
                     if (!ok) return;
                     tc_fence_after();
-                    scores(tS + 128 * (g & 1), sm.q, sm.k[g % 3]);
+                    mma_scores<NB>(tS + 128 * (g & 1), dq, k_major(sm.k[g % 3]), idS);
                     mma_commit(smem_u32(&sm.s_full[g & 1]));
                 };
                 auto dp_of = [&](int g) {
                     ok = ok && wait(sm.v_full[g & 1], (g >> 1) & 1);
                     if (!ok) return;
                     tc_fence_after();
-                    scores(tG, sm.go, sm.v[g & 1]);
+                    mma_scores<NB>(tG, dg, k_major(sm.v[g & 1]), idS);
                     mma_commit(smem_u32(&sm.dp_full));
                     mma_commit(smem_u32(&sm.v_empty[g & 1]));
                 };
@@ -579,11 +552,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                     ok = wait(sm.ds_ready, g & 1);
                     if (!ok) break;
                     tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)   // dQ += dS K_j
-                        mma_bf16_ts(tdQ, tS + 128 * (g & 1) + 64 * (kk >> 2) + 8 * (kk & 3),
-                                    smem_desc_sw128(smem_u32(sm.k[g % 3][0]) + kk * 2048, kBlk, 1024), idG,
-                                    (j > 0 || kk > 0) ? 1u : 0u);
+                    mma_weights<6>(tdQ, tS + 128 * (g & 1), mn_major(sm.k[g % 3]), idG, j > 0);   // dQ += dS K_j
                     mma_commit(smem_u32(&sm.k_empty[g % 3]));
                     if (j + 1 < n) dp_of(g + 1);
                     if (j + 2 < n) s_of(g + 2);
@@ -644,11 +613,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                     for (int c = 0; c < 64; ++c)
                         if (!(c <= last && c >= low && (c >= first || c < sink))) P[c] = 0.f;
                     if (pass == 1) {
-                        if (ch == 0) {
-                            uint8_t *blk[NB];
-                            for (int c = 0; c < NB; ++c) blk[c] = sm.k[g % 3][c];
-                            clean_row<NB>(blk, r);
-                        }
+                        if (ch == 0) clean_row<NB>(sm.k[g % 3][0], r);
                         fence_proxy_async();
                     }
                 }
@@ -661,7 +626,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 }
                 tmem_stored();
                 tc_fence_before();
-                mbar_arrive(smem_u32(&sm.ds_ready));
+                warp_arrive(sm.ds_ready, lane);
             }
             ok = wait(sm.done, pass) && ok;
             tc_fence_after();
