@@ -18,8 +18,8 @@
 // sink rows a last small kernel adds up in order (else the first tile's CTA would
 // outlast the others by Tk / window).
 //
-// Warps 0-7 compute (two per TMEM lane quadrant, each half of the columns), warp 8
-// loads by TMA, warp 9 issues the MMAs, warp 10 (dK, dV) brings lse and D.  While MMAs
+// Sixteen warps compute (four per TMEM lane quadrant, each a quarter of the columns), one
+// loads by TMA, one issues the MMAs, one more (dK, dV) brings lse and D.  While MMAs
 // of one block run, the workers turn the other scores: the queue of MMAs is
 //   dK, dV:  dV_i S_i+1 | dK_i dP_i+1        dQ:  dQ_j dP_j+1 S_j+2
 // so that one pair of products always covers one half of the elementwise work.
@@ -38,7 +38,8 @@ namespace win {
 namespace {
 
 constexpr int kTile = 128;
-constexpr int kWorkers = 256, kWarps = 8;
+constexpr int kWarps = 16, kWorkers = 32 * kWarps;   // the workers'
+constexpr int kCols = 128 / (kWarps / 4);            // score columns of one worker thread
 
 struct BwdArgs {
     Map q, k, v, go, dq, dk, dv;
@@ -53,19 +54,28 @@ struct BwdArgs {
     float scale, scale_log2;
 };
 
-// v[0 .. 31] * f of row r (zeros unless `on`) as bf16, into the 16-byte units u0 .. u0+3 of its
+// v[0 .. 15] * f of row r (zeros unless `on`) as bf16, into the 16-byte units u0 and u0+1 of its
 // 128 bytes in a staged block.
-__device__ __forceinline__ void stage_bf16_32(uint8_t *blk, int r, int u0, const uint32_t (&v)[32],
-                                              float f, bool on) {
+__device__ __forceinline__ void stage_bf16_16(uint8_t *blk, int r, int u0, const float (&v)[16], float f,
+                                              bool on) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < 2; ++u) {
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            w[e] = on ? pack_bf16x2(__uint_as_float(v[8 * u + 2 * e]) * f,
-                                    __uint_as_float(v[8 * u + 2 * e + 1]) * f) : 0u;
+            w[e] = on ? pack_bf16x2(v[8 * u + 2 * e] * f, v[8 * u + 2 * e + 1] * f) : 0u;
         *reinterpret_cast<uint4 *>(blk + xoff128(r, u0 + u)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
+}
+
+// 32 values as bf16 into the 16 TMEM columns at taddr.
+__device__ __forceinline__ void put_weights(uint32_t taddr, const float (&v)[32]) {
+    uint32_t w[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+    tmem_st16_async(taddr, w);
+    tmem_stored();
+    tc_fence_before();
 }
 
 // ------------------------------------------------------------------ dK, dV
@@ -83,7 +93,7 @@ struct KvSm {
     int abort;
 };
 
-constexpr int kKvThreads = 352;
+constexpr int kKvThreads = kWorkers + 96;
 
 template <int HD>
 __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __grid_constant__ BwdArgs p) {
@@ -146,7 +156,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
         sm.abort = 0;
         fence_barrier_init();
     }
-    if (warp == 8) {
+    if (warp == kWarps) {
         tmem_alloc(smem_u32(&sm.tmem), 512);
         tmem_relinquish();
     }
@@ -158,7 +168,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
         return wait_or_abort(bar, parity, &sm.abort, p.status);
     };
 
-    if (warp == 8) {
+    if (warp == kWarps) {
         if (lane == 0) {
             const uint32_t kvb = smem_u32(&sm.kv_full);
             mbar_expect_tx(kvb, 2 * NB * kBlk);
@@ -184,7 +194,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
             for (int t = max(0, nq - 3); t < nq; ++t) drain_phase(smem_u32(&sm.q_full[t % 3]), (t / 3) & 1);
             for (int t = max(0, ng - 2); t < ng; ++t) drain_phase(smem_u32(&sm.g_full[t & 1]), (t >> 1) & 1);
         }
-    } else if (warp == 9) {
+    } else if (warp == kWarps + 1) {
         if (elect_one()) {
             constexpr uint32_t idS = idesc_bf16(128, 128, false, false);
             constexpr uint32_t idG = idesc_bf16(128, HD, false, true);
@@ -210,13 +220,13 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                 ok = wait(sm.p_ready, i & 1);
                 if (!ok) break;
                 tc_fence_after();
-                mma_weights<6>(tdV, tS, mn_major(sm.go[i & 1]), idG, i > 0);
+                mma_weights<5>(tdV, tS, mn_major(sm.go[i & 1]), idG, i > 0);
                 mma_commit(smem_u32(&sm.g_empty[i & 1]));
                 if (i + 1 < n) s_of(i + 1);
                 ok = ok && wait(sm.ds_ready, i & 1);
                 if (!ok) break;
                 tc_fence_after();
-                mma_weights<6>(tdK, tG, mn_major(sm.q[i % 3]), idG, i > 0);
+                mma_weights<5>(tdK, tG, mn_major(sm.q[i % 3]), idG, i > 0);
                 mma_commit(smem_u32(&sm.q_empty[i % 3]));
                 if (i + 1 < n) dp_of(i + 1);
             }
@@ -227,7 +237,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
             }
             drain_mmas(smem_u32(&sm.drained));
         }
-    } else if (warp == 10) {
+    } else if (warp == kWarps + 2) {
         for (int i = 0; i < n; ++i) {
             const int u = i & 1;
             if (!__all_sync(0xffffffffu, wait(sm.st_empty[u], ((i >> 1) & 1) ^ 1))) break;
@@ -250,47 +260,46 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
             warp_arrive(sm.st_full[u], lane);
         }
     } else {
-        const int ch = warp >> 2, r = (warp & 3) * 32 + lane, t = k0 + r;
-        const uint32_t at = ((uint32_t)((warp & 3) * 32) << 16) + 64 * ch;
+        const int c0 = kCols * (warp >> 2), r = (warp & 3) * 32 + lane, t = k0 + r;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, at = lanes + c0;
+        const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             const int u = i & 1, pq = first + kTile * (i % blocks);
             const bool whole = pq >= k0 + kTile - 1 && pq + kTile - 1 - k0 < p.window &&
                                pq + kTile - 1 <= last;
-            // columns lo .. hi of this half are seen
-            int lo = 0, hi = 63;
-            if (!whole) {
-                lo = t - pq - 64 * ch;
-                hi = min(last, t < p.sinks ? last : t + p.window - 1) - pq - 64 * ch;
-            }
-            ok = wait(sm.s_full, i & 1) && ok;
+            uint32_t seen = ~0u;   // which of this thread's queries see its key
+            if (!whole)
+                seen = bits(t - pq - c0, min(last, t < p.sinks ? last : t + p.window - 1) - pq - c0);
+            const float *L = sm.lse[u] + c0, *D = sm.delta[u] + c0;
             ok = wait(sm.st_full[u], (i >> 1) & 1) && ok;
+            ok = wait(sm.s_full, i & 1) && ok;
             tc_fence_after();
-            uint32_t raw[2][32];
-            tmem_ld32_async(tS + at, raw[0]);
-            tmem_ld32_async(tS + at + 32, raw[1]);
-            tmem_ready(raw[0]);
-            tmem_ready(raw[1]);
-            float P[64];
-            const float *L = sm.lse[u] + 64 * ch, *D = sm.delta[u] + 64 * ch;
+            uint32_t raw[32];
+            tmem_ld32_async(tS + at, raw);
+            tmem_ready(raw);
+            float P[32];
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
+            for (int c = 0; c < 32; c += 4) {
                 const float4 l4 = *reinterpret_cast<const float4 *>(L + c);
-                const float l[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    P[c + e] = exp2_fast(fmaf(__uint_as_float(raw[(c + e) >> 5][(c + e) & 31]),
-                                              p.scale_log2, -l[e]));
+                const float2 x = fma2(make_float2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2,
+                                      make_float2(-l4.x, -l4.y));
+                const float2 y = fma2(make_float2(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])),
+                                      sl2, make_float2(-l4.z, -l4.w));
+                P[c] = exp2_fast(x.x);
+                P[c + 1] = exp2_fast(x.y);
+                P[c + 2] = exp2_fast(y.x);
+                P[c + 3] = exp2_fast(y.y);
             }
             if (!whole) {
 #pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (c < lo || c > hi) P[c] = 0.f;
+                for (int c = 0; c < 32; ++c)
+                    if (((seen >> c) & 1u) == 0) P[c] = 0.f;
                 if ((sm.odd[u][0] | sm.odd[u][1] | sm.odd[u][2] | sm.odd[u][3]) != 0) {
                     // zero those queries' rows, once S and dP have been taken from them
                     ok = wait(sm.dp_full, i & 1) && ok;
                     const int row = threadIdx.x & 127;
-                    if (((sm.odd[u][row >> 5] >> (row & 31)) & 1u) != 0) {
+                    if (threadIdx.x < 256 && ((sm.odd[u][row >> 5] >> (row & 31)) & 1u) != 0) {
                         uint8_t *x = threadIdx.x < 128 ? sm.q[i % 3][0] : sm.go[i & 1][0];
 #pragma unroll 1
                         for (int e = 0; e < 8 * NB; ++e)
@@ -300,89 +309,70 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                     fence_proxy_async();
                 }
             }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                uint32_t w[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(P[32 * x + 2 * e], P[32 * x + 2 * e + 1]);
-                tmem_st16_async(tS + at + 16 * x, w);
-            }
-            tmem_stored();
-            tc_fence_before();
+            put_weights(tS + at, P);
             warp_arrive(sm.p_ready, lane);
 
             ok = wait(sm.dp_full, i & 1) && ok;
             tc_fence_after();
-            tmem_ld32_async(tG + at, raw[0]);
-            tmem_ld32_async(tG + at + 32, raw[1]);
-            tmem_ready(raw[0]);
-            tmem_ready(raw[1]);
+            tmem_ld32_async(tG + at, raw);
+            tmem_ready(raw);
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
+            for (int c = 0; c < 32; c += 4) {
                 const float4 d4 = *reinterpret_cast<const float4 *>(D + c);
-                const float d[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    P[c + e] *= __uint_as_float(raw[(c + e) >> 5][(c + e) & 31]) - d[e];
+                const float2 x = mul2(make_float2(P[c], P[c + 1]),
+                                      add2(make_float2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])),
+                                           make_float2(-d4.x, -d4.y)));
+                const float2 y = mul2(make_float2(P[c + 2], P[c + 3]),
+                                      add2(make_float2(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])),
+                                           make_float2(-d4.z, -d4.w)));
+                P[c] = x.x;
+                P[c + 1] = x.y;
+                P[c + 2] = y.x;
+                P[c + 3] = y.y;
             }
             if (!whole) {
                 // (again: dP may be NaN where P is 0; and a query that sees one token only has
                 // no gradient)
-                const bool none = p.window == 1 && p.sinks == 0;
+                if (p.window == 1 && p.sinks == 0) seen = 0;
+                if (pq == 0 && c0 == 0) seen &= ~1u;
 #pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (c < lo || c > hi || none || pq + 64 * ch + c == 0) P[c] = 0.f;
+                for (int c = 0; c < 32; ++c)
+                    if (((seen >> c) & 1u) == 0) P[c] = 0.f;
             }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                uint32_t w[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(P[32 * x + 2 * e], P[32 * x + 2 * e + 1]);
-                tmem_st16_async(tG + at + 16 * x, w);
-            }
-            tmem_stored();
-            tc_fence_before();
+            put_weights(tG + at, P);
             warp_arrive(sm.ds_ready, lane);
-            warp_arrive(sm.st_empty[u], lane);
+            if (lane == 0) mbar_arrive(smem_u32(&sm.st_empty[u]));
         }
         ok = wait(sm.done, 0) && ok;
         tc_fence_after();
         named_barrier(1, kWorkers);
         if (*(volatile int *)&sm.abort == 0) {
-            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-            // this thread's half of the row's columns, 32 at a time
+            // this thread's quarter of the row's columns, 16 at a time
 #pragma unroll
             for (int x = 0; x < HD / 64; ++x) {
-                const int c = ch * (HD / 2) + 32 * x;
-                uint32_t dv[32], dk[32];
-                tmem_ld32_async(tdV + lanes + c, dv);
-                tmem_ld32_async(tdK + lanes + c, dk);
-                tmem_ready(dv);
-                tmem_ready(dk);
+                const int c = (warp >> 2) * (HD / 4) + 16 * x;
+                float dv[16], dk[16];
+                tmem_ld16(tdV + lanes + c, dv);
+                tmem_ld16(tdK + lanes + c, dk);
                 if (!has_sinks) {
-                    stage_bf16_32(sm.v[c >> 6], r, (c & 63) >> 3, dv, 1.f, true);
-                    stage_bf16_32(sm.k[c >> 6], r, (c & 63) >> 3, dk, p.scale, true);
+                    stage_bf16_16(sm.v[c >> 6], r, (c & 63) >> 3, dv, 1.f, true);
+                    stage_bf16_16(sm.k[c >> 6], r, (c & 63) >> 3, dk, p.scale, true);
                 } else if (t < p.Tk && c < p.hp && (t < p.sinks || !is_extra)) {
-                    // columns in units of 8 (hp = 16 ends inside these 32)
-                    const int end = min(32, p.hp - c);
+                    if (t < p.sinks) {
+                        float *o = sink_sums + (long long)t * 2 * p.hp + c;
 #pragma unroll
-                    for (int u = 0; u < 32; u += 8) {
-                        if (u >= end) break;
-                        if (t < p.sinks) {
-                            float *o = sink_sums + (long long)t * 2 * p.hp + c + u;
+                        for (int e = 0; e < 16; ++e) {
+                            o[e] = dk[e] * p.scale;
+                            o[p.hp + e] = dv[e];
+                        }
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                o[e] = __uint_as_float(dk[u + e]) * p.scale;
-                                o[p.hp + e] = __uint_as_float(dv[u + e]);
-                            }
-                        } else {
+                        for (int u = 0; u < 16; u += 8) {
                             uint32_t wk[4], wv[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                wk[e] = pack_bf16x2(__uint_as_float(dk[u + 2 * e]) * p.scale,
-                                                    __uint_as_float(dk[u + 2 * e + 1]) * p.scale);
-                                wv[e] = pack_bf16x2(__uint_as_float(dv[u + 2 * e]),
-                                                    __uint_as_float(dv[u + 2 * e + 1]));
+                                wk[e] = pack_bf16x2(dk[u + 2 * e] * p.scale, dk[u + 2 * e + 1] * p.scale);
+                                wv[e] = pack_bf16x2(dv[u + 2 * e], dv[u + 2 * e + 1]);
                             }
                             *reinterpret_cast<uint4 *>(p.dK + p.sdk.at(b, t, hk) + c + u) =
                                 make_uint4(wk[0], wk[1], wk[2], wk[3]);
@@ -409,7 +399,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 8) tmem_dealloc(sm.tmem, 512);
+    if (warp == kWarps) tmem_dealloc(sm.tmem, 512);
 }
 
 // dk and dv of the sink rows: the tile's own sum and the extra CTAs', in order.
@@ -437,7 +427,7 @@ struct QSm {
     int abort, redo;
 };
 
-constexpr int kQThreads = 320;
+constexpr int kQThreads = kWorkers + 64;
 
 template <int HD>
 __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid_constant__ BwdArgs p) {
@@ -475,7 +465,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
         sm.abort = sm.redo = 0;
         fence_barrier_init();
     }
-    if (warp == 8) {
+    if (warp == kWarps) {
         tmem_alloc(smem_u32(&sm.tmem), 512);
         tmem_relinquish();
     }
@@ -493,7 +483,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
     // lies in buffer number & 1.
     for (int pass = 0; pass < 2; ++pass) {
         const int g0 = pass * n;
-        if (warp == 8) {
+        if (warp == kWarps) {
             if (lane == 0) {
                 if (pass == 0) {
                     mbar_expect_tx(smem_u32(&sm.q_full), 2 * NB * kBlk);
@@ -523,7 +513,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 for (int t = max(0, nv - 2); t < nv; ++t) drain_phase(smem_u32(&sm.v_full[t & 1]), (t >> 1) & 1);
             }
             __syncwarp();
-        } else if (warp == 9) {
+        } else if (warp == kWarps + 1) {
             if (elect_one()) {
                 constexpr uint32_t idS = idesc_bf16(128, 128, false, false);
                 constexpr uint32_t idG = idesc_bf16(128, HD, false, true);
@@ -552,7 +542,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                     ok = wait(sm.ds_ready, g & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    mma_weights<6>(tdQ, tS + 128 * (g & 1), mn_major(sm.k[g % 3]), idG, j > 0);   // dQ += dS K_j
+                    mma_weights<5>(tdQ, tS + 128 * (g & 1), mn_major(sm.k[g % 3]), idG, j > 0);   // dQ += dS K_j
                     mma_commit(smem_u32(&sm.k_empty[g % 3]));
                     if (j + 1 < n) dp_of(g + 1);
                     if (j + 2 < n) s_of(g + 2);
@@ -566,87 +556,73 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
             }
             __syncwarp();
         } else {
-            const int ch = warp >> 2, r = (warp & 3) * 32 + lane, pos = pf + r;
+            const int c0 = kCols * (warp >> 2), r = (warp & 3) * 32 + lane, pos = pf + r;
             const bool valid = pos <= pl;
-            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, at = lanes + 64 * ch;
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
             const long long row = ((long long)b * p.H + h) * p.Tq + i0 + r;
             // a query that sees one token only has no gradient: P = 0
             const float L = !valid ? 0.f : sees_one(pos, p.window, p.sinks) ? INFINITY : p.lse[row] * kLog2e;
             const float D = valid ? p.delta[row] : 0.f;
+            const float2 sl2 = make_float2(p.scale_log2, p.scale_log2), nL = make_float2(-L, -L),
+                         nD = make_float2(-D, -D);
             for (int j = 0; j < n; ++j) {
-                const int g = g0 + j, ks = kb.start(j);
-                const uint32_t tSj = tS + 128 * (g & 1) + at;
+                const int g = g0 + j;
+                const uint32_t tSj = tS + 128 * (g & 1) + lanes + c0;
                 const bool whole = kb.whole(j, pf, pl, p.window);
                 ok = wait(sm.s_full[g & 1], (g >> 1) & 1) && ok;
                 tc_fence_after();
-                uint32_t raw[2][32];
-                tmem_ld32_async(tSj, raw[0]);
-                tmem_ld32_async(tSj + 32, raw[1]);
-                tmem_ready(raw[0]);
-                tmem_ready(raw[1]);
-                float P[64];
+                uint32_t raw[32];
+                tmem_ld32_async(tSj, raw);
+                tmem_ready(raw);
+                float P[32];
 #pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    P[c] = exp2_fast(fmaf(__uint_as_float(raw[c >> 5][c & 31]), p.scale_log2, -L));
+                for (int c = 0; c < 32; c += 2) {
+                    const float2 x = fma2(make_float2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])),
+                                          sl2, nL);
+                    P[c] = exp2_fast(x.x);
+                    P[c + 1] = exp2_fast(x.y);
+                }
                 ok = wait(sm.dp_full, g & 1) && ok;
                 tc_fence_after();
-                tmem_ld32_async(tG + at, raw[0]);
-                tmem_ld32_async(tG + at + 32, raw[1]);
-                tmem_ready(raw[0]);
-                tmem_ready(raw[1]);
+                tmem_ld32_async(tG + lanes + c0, raw);
+                tmem_ready(raw);
 #pragma unroll
-                for (int c = 0; c < 64; ++c) P[c] *= __uint_as_float(raw[c >> 5][c & 31]) - D;
+                for (int c = 0; c < 32; c += 2) {
+                    const float2 x = mul2(make_float2(P[c], P[c + 1]),
+                                          add2(make_float2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), nD));
+                    P[c] = x.x;
+                    P[c + 1] = x.y;
+                }
                 if (!whole) {
-                    int first = 0, last = kTile - 1, sink = 0;
-                    const int low = max(-ks, 0) - 64 * ch;
-                    if (!kb.is_far(j)) {
-                        first = max(pos - p.window + 1, 0) - ks;
-                        last = min(pos - ks, kTile - 1);
-                        sink = min(p.sinks - ks, last + 1);
-                    } else {
-                        last = kb.slim - ks - 1;
-                    }
-                    first -= 64 * ch;
-                    last -= 64 * ch;
-                    sink -= 64 * ch;
+                    const uint32_t seen = seen_bits(kb, j, kb.start(j), c0, pos, p.window, p.sinks);
 #pragma unroll
-                    for (int c = 0; c < 64; ++c)
-                        if (!(c <= last && c >= low && (c >= first || c < sink))) P[c] = 0.f;
+                    for (int c = 0; c < 32; ++c)
+                        if (((seen >> c) & 1u) == 0) P[c] = 0.f;
                     if (pass == 1) {
-                        if (ch == 0) clean_row<NB>(sm.k[g % 3][0], r);
+                        if (c0 == 0) clean_row<NB>(sm.k[g % 3][0], r);
                         fence_proxy_async();
                     }
                 }
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(P[32 * x + 2 * e], P[32 * x + 2 * e + 1]);
-                    tmem_st16_async(tSj + 16 * x, w);
-                }
-                tmem_stored();
-                tc_fence_before();
+                put_weights(tSj, P);
                 warp_arrive(sm.ds_ready, lane);
             }
             ok = wait(sm.done, pass) && ok;
             tc_fence_after();
-            uint32_t raw[HD / 64][32];
-#pragma unroll
-            for (int x = 0; x < HD / 64; ++x) tmem_ld32_async(tdQ + lanes + ch * (HD / 2) + 32 * x, raw[x]);
-#pragma unroll
-            for (int x = 0; x < HD / 64; ++x) tmem_ready(raw[x]);
+            float dq[HD / 64][16];   // this thread's quarter of the columns
             float odd = 0.f;
 #pragma unroll
-            for (int x = 0; x < HD / 64; ++x)
+            for (int x = 0; x < HD / 64; ++x) {
+                tmem_ld16(tdQ + lanes + (warp >> 2) * (HD / 4) + 16 * x, dq[x]);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) odd = fmaf(__uint_as_float(raw[x][e]), 0.f, odd);
+                for (int e = 0; e < 16; ++e) odd = fmaf(dq[x][e], 0.f, odd);
+            }
             if (pass == 0 && valid && !(odd == 0.f)) sm.redo = 1;
             named_barrier(1, kWorkers);
             if (*(volatile int *)&sm.abort == 0 && (pass == 1 || *(volatile int *)&sm.redo == 0)) {
 #pragma unroll
                 for (int x = 0; x < HD / 64; ++x) {
-                    const int c = ch * (HD / 2) + 32 * x;
-                    stage_bf16_32(sm.q[c >> 6], r, (c & 63) >> 3, raw[x], p.scale, valid);
+                    const int c = (warp >> 2) * (HD / 4) + 16 * x;
+                    stage_bf16_16(sm.q[c >> 6], r, (c & 63) >> 3, dq[x], p.scale, valid);
                 }
                 fence_proxy_async();
                 named_barrier(1, kWorkers);
@@ -662,9 +638,9 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
         tc_fence_after();
         if (*(volatile int *)&sm.redo == 0 || *(volatile int *)&sm.abort != 0) break;
     }
-    if (warp == 9 && elect_one()) drain_mmas(smem_u32(&sm.drained));
+    if (warp == kWarps + 1 && elect_one()) drain_mmas(smem_u32(&sm.drained));
     __syncthreads();
-    if (warp == 8) tmem_dealloc(sm.tmem, 512);
+    if (warp == kWarps) tmem_dealloc(sm.tmem, 512);
 }
 
 // Extra CTAs per sink tile, and the query blocks of each: as many as a tile without
