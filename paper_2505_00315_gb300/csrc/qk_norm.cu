@@ -31,8 +31,8 @@ Turns make_turns(int rotary, double theta) {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTokens = 4;   // tokens of one block's step
-constexpr int kBatch = 4;       // heads whose loads a lane keeps in flight
+constexpr int kBatch = 4;       // tokens of one item: loads that a lane keeps in flight
+constexpr int kMaxTokens = 8;   // tokens of one block's step
 
 struct NormArgs {
     Norm n;
@@ -40,121 +40,112 @@ struct NormArgs {
     void *oq, *ok;          // forward: y; backward: dx
     const int32_t *pos;
     float *partial;         // backward: [blocks][2][hp] partial sums of dgamma
-    int tokens;             // of one step: 1 .. kMaxTokens
+    int step, batch;        // tokens of a step, and of an item
 };
 
-// Sines and cosines of `tokens` tokens from token0 (of B*T) on.
-__device__ __forceinline__ void fill_angles(float2 (*cs)[64], const NormArgs &p, const Turns &tab,
-                                            long long token0, int tokens) {
-    const int pairs = p.n.rotary >> 1;
-    for (int e = threadIdx.x; e < tokens * pairs; e += kThreads) {
-        const int i = e / pairs, a = e - i * pairs;
-        const long long tok = token0 + i;
-        const int t = p.pos != nullptr ? p.pos[tok] : (int)(tok % p.n.T);
-        cs[i][a] = angle_of(tab.phi[a], t);
+struct StepTokens {
+    float2 cs[kMaxTokens][64];          // cosines and sines
+    int b[kMaxTokens], t[kMaxTokens];   // sequence and token
+};
+
+// The queries' (KEY: keys') part of one step: items of `batch` tokens of one head, one a
+// lane group.  acc: backward, this lane's sums of g r x.
+template <class T, bool VEC, bool kBackward, bool KEY>
+__device__ __forceinline__ void norm_step(const NormArgs &p, const StepTokens &st, int tokens,
+                                          const float (&gamma)[8], float (&acc)[8]) {
+    const Norm &n = p.n;
+    const int lanes = n.hp >> 3, groups = kThreads / lanes, lane = threadIdx.x & 31;
+    const int grp = threadIdx.x / lanes, c = (threadIdx.x % lanes) * 8;
+    const int heads = KEY ? n.Hkv : n.H;
+    const T *in = static_cast<const T *>(KEY ? p.k : p.q) + c;
+    const T *dy = static_cast<const T *>(KEY ? p.dyk : p.dyq) + c;
+    T *out = static_cast<T *>(KEY ? p.ok : p.oq) + c;
+    const Str &si = KEY ? n.k : n.q, &sy = KEY ? n.yk : n.yq, &sd = KEY ? n.dk : n.dq;
+    const float inv_hp = 1.f / (float)n.hp;
+    const int items = (tokens + p.batch - 1) / p.batch * heads;
+    for (int it0 = 0; it0 < items; it0 += groups) {   // (all lanes together: the sums are shuffles)
+        const int it = it0 + grp, bat = it / heads, h = it - bat * heads;
+        const int i0 = bat * p.batch, count = it < items ? min(p.batch, tokens - i0) : 0;
+        float x[kBatch][8], g[kBackward ? kBatch : 1][8];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (u < count) {
+                load8<T, VEC>(in + si.at(st.b[i0 + u], st.t[i0 + u], h), x[u]);
+                if (kBackward) load8<T, VEC>(dy + sy.at(st.b[i0 + u], st.t[i0 + u], h), g[kBackward ? u : 0]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[u][e] = g[kBackward ? u : 0][e] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (u >= p.batch) break;
+            const float2 *cs = st.cs[u < count ? i0 + u : 0];
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fmaf(x[u][e], x[u][e], ss);
+            const float r = rsqrtf(fmaf(group_sum(ss, lanes), inv_hp, n.eps));
+            if (!kBackward) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[u][e] *= r * gamma[e];
+                turn8(x[u], c, n.rotary, n.halves, cs, 1.f, lane);
+                if (u < count) store8<T, VEC>(out + sy.at(st.b[i0 + u], st.t[i0 + u], h), x[u]);
+            } else {
+                float (&gu)[8] = g[kBackward ? u : 0];
+                turn8(gu, c, n.rotary, n.halves, cs, -1.f, lane);
+                float dot = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[u][e] *= r;
+                    acc[e] = fmaf(gu[e], x[u][e], acc[e]);   // (rows past the end hold zeros)
+                    gu[e] *= gamma[e];
+                    dot = fmaf(gu[e], x[u][e], dot);
+                }
+                dot = group_sum(dot, lanes) * inv_hp;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) gu[e] = r * fmaf(-x[u][e], dot, gu[e]);
+                if (u < count) store8<T, VEC>(out + sd.at(st.b[i0 + u], st.t[i0 + u], h), gu);
+            }
+        }
     }
-}
-
-// Where head hh of token tok lies: heads 0 .. H-1 are queries, the rest keys.
-struct Place {
-    bool key;
-    long long b, t;
-    int h;
-};
-__device__ __forceinline__ Place place(const Norm &n, long long tok, int hh) {
-    Place w;
-    w.key = hh >= n.H;
-    w.h = w.key ? hh - n.H : hh;
-    w.b = tok / n.T;
-    w.t = tok - w.b * n.T;
-    return w;
 }
 
 template <class T, bool VEC, bool kBackward>
 __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_constant__ NormArgs p,
                                                                 const __grid_constant__ Turns tab) {
-    __shared__ float2 cs[kMaxTokens][64];
+    __shared__ StepTokens st;
     extern __shared__ float red[];   // backward: [groups][2][hp]
     const Norm &n = p.n;
-    const int lanes = n.hp >> 3, groups = kThreads / lanes, lane = threadIdx.x & 31;
+    const int lanes = n.hp >> 3, groups = kThreads / lanes;
     const int grp = threadIdx.x / lanes, c = (threadIdx.x % lanes) * 8;
-    const int HH = n.H + n.Hkv;
     const long long N = (long long)n.B * n.T;
     float gq[8], gk[8], aq[8], ak[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 1.f, aq[e] = ak[e] = 0.f;
     if (p.gq != nullptr) load8<T, false>((const T *)p.gq + c, gq);
     if (p.gk != nullptr) load8<T, false>((const T *)p.gk + c, gk);
-    for (long long tok0 = (long long)blockIdx.x * p.tokens; tok0 < N;
-         tok0 += (long long)gridDim.x * p.tokens) {
-        const int tokens = (int)min((long long)p.tokens, N - tok0);
-        __syncthreads();   // the last step's angles have been read
-        fill_angles(cs, p, tab, tok0, tokens);
-        __syncthreads();
-        const int items = tokens * HH;
-        for (int it0 = 0; it0 < items; it0 += kBatch * groups) {
-            float x[kBatch][8], g[kBackward ? kBatch : 1][8];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int it = it0 + u * groups + grp;
-                if (it < items) {
-                    const Place w = place(n, tok0 + it / HH, it % HH);
-                    load8<T, VEC>(w.key ? (const T *)p.k + n.k.at(w.b, w.t, w.h) + c
-                                        : (const T *)p.q + n.q.at(w.b, w.t, w.h) + c,
-                                  x[u]);
-                    if (kBackward)
-                        load8<T, VEC>(w.key ? (const T *)p.dyk + n.yk.at(w.b, w.t, w.h) + c
-                                            : (const T *)p.dyq + n.yq.at(w.b, w.t, w.h) + c,
-                                      g[kBackward ? u : 0]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[u][e] = g[kBackward ? u : 0][e] = 0.f;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int it = it0 + u * groups + grp;
-                const bool on = it < items;
-                const int i = on ? it / HH : 0;
-                const Place w = place(n, tok0 + i, on ? it % HH : 0);
-                float ss = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fmaf(x[u][e], x[u][e], ss);
-                const float r = rsqrtf(group_sum(ss, lanes) / (float)n.hp + n.eps);
-                if (!kBackward) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[u][e] *= r * (w.key ? gk[e] : gq[e]);
-                    turn8(x[u], c, n.rotary, n.halves, cs[i], 1.f, lane);
-                    if (on)
-                        store8<T, VEC>(w.key ? (T *)p.ok + n.yk.at(w.b, w.t, w.h) + c
-                                             : (T *)p.oq + n.yq.at(w.b, w.t, w.h) + c,
-                                       x[u]);
-                } else {
-                    float (&gu)[8] = g[kBackward ? u : 0];
-                    turn8(gu, c, n.rotary, n.halves, cs[i], -1.f, lane);
-                    float dot = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float xn = x[u][e] * r, d = gu[e] * xn;
-                        if (w.key) ak[e] += on ? d : 0.f;
-                        else aq[e] += on ? d : 0.f;
-                        gu[e] *= w.key ? gk[e] : gq[e];
-                        dot = fmaf(gu[e], xn, dot);
-                        x[u][e] = xn;
-                    }
-                    dot = group_sum(dot, lanes) / (float)n.hp;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) gu[e] = r * (gu[e] - x[u][e] * dot);
-                    if (on)
-                        store8<T, VEC>(w.key ? (T *)p.ok + n.dk.at(w.b, w.t, w.h) + c
-                                             : (T *)p.oq + n.dq.at(w.b, w.t, w.h) + c,
-                                       gu);
-                }
-            }
+    const int pairs = n.rotary >> 1;
+    for (long long tok0 = (long long)blockIdx.x * p.step; tok0 < N; tok0 += (long long)gridDim.x * p.step) {
+        const int tokens = (int)min((long long)p.step, N - tok0);
+        const int b0 = (int)(tok0 / n.T), t0 = (int)(tok0 - (long long)b0 * n.T);
+        __syncthreads();   // the last step's tokens are done with
+        if (threadIdx.x < tokens) {
+            int b = b0, t = t0 + threadIdx.x;
+            while (t >= n.T) t -= n.T, ++b;
+            st.b[threadIdx.x] = b;
+            st.t[threadIdx.x] = t;
         }
+        for (int e = threadIdx.x; e < tokens * pairs; e += kThreads) {
+            const int i = e / pairs, a = e - i * pairs;
+            int t = t0 + i;
+            while (t >= n.T) t -= n.T;
+            st.cs[i][a] = angle_of(tab.phi[a], p.pos != nullptr ? p.pos[tok0 + i] : t);
+        }
+        __syncthreads();
+        norm_step<T, VEC, kBackward, false>(p, st, tokens, gq, aq);
+        norm_step<T, VEC, kBackward, true>(p, st, tokens, gk, ak);
     }
     if (kBackward && p.partial != nullptr) {
-        __syncthreads();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             red[(grp * 2 + 0) * n.hp + c + e] = aq[e];
@@ -189,17 +180,14 @@ __global__ void __launch_bounds__(1024) qk_dgamma_kernel(const float *partial, i
     }
 }
 
-constexpr int kMaxBlocks = 152 * 4;   // of the backward: each keeps its dgamma to the end
+constexpr int kMaxBlocks = 152 * 2;   // of the backward: each keeps its dgamma to the end
 
-int step_tokens(const Norm &n) {
-    // several tokens a step only where every SM still gets work: with few, one token a
-    // block starts and ends sooner
-    const long long N = (long long)n.B * n.T;
-    return N >= 4LL * kMaxTokens * 152 ? kMaxTokens : 1;
-}
+// Several tokens a step, and an item, only where every SM still gets some: with few, one token a
+// block starts and ends sooner.
+bool many(const Norm &n) { return (long long)n.B * n.T >= 2LL * kMaxTokens * 152; }
 
 int bwd_blocks(const Norm &n) {
-    const long long N = (long long)n.B * n.T, t = step_tokens(n), steps = (N + t - 1) / t;
+    const long long N = (long long)n.B * n.T, t = many(n) ? kMaxTokens : 1, steps = (N + t - 1) / t;
     return (int)(steps < kMaxBlocks ? steps : kMaxBlocks);
 }
 
@@ -225,18 +213,20 @@ size_t norm_workspace(const Norm &n) { return (size_t)bwd_blocks(n) * 2 * n.hp *
 
 cudaError_t launch_norm(const Norm &n, const void *q, const void *k, const void *gq, const void *gk,
                         const int32_t *pos, void *yq, void *yk, cudaStream_t s) {
-    NormArgs p{n, q, k, gq, gk, nullptr, nullptr, yq, yk, pos, nullptr, step_tokens(n)};
+    NormArgs p{n, q, k, gq, gk, nullptr, nullptr, yq, yk, pos, nullptr, many(n) ? kMaxTokens : 1,
+               many(n) ? kBatch : 1};
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) && rows16(yq, n.yq, n.bf16) &&
                      rows16(yk, n.yk, n.bf16);
     const long long N = (long long)n.B * n.T;
-    return launch<false>(p, vec, (unsigned)((N + p.tokens - 1) / p.tokens), s);
+    return launch<false>(p, vec, (unsigned)((N + p.step - 1) / p.step), s);
 }
 
 cudaError_t launch_norm_bwd(const Norm &n, const void *q, const void *k, const void *gq,
                             const void *gk, const int32_t *pos, const void *dyq, const void *dyk,
                             void *dq, void *dk, float *dgq, float *dgk, void *ws, cudaStream_t s) {
     const bool sums = dgq != nullptr || dgk != nullptr;
-    NormArgs p{n, q, k, gq, gk, dyq, dyk, dq, dk, pos, sums ? (float *)ws : nullptr, step_tokens(n)};
+    NormArgs p{n, q, k, gq, gk, dyq, dyk, dq, dk, pos, sums ? (float *)ws : nullptr,
+               many(n) ? kMaxTokens : 1, many(n) ? kBatch : 1};
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) &&
                      rows16(dyq, n.yq, n.bf16) && rows16(dyk, n.yk, n.bf16) &&
                      rows16(dq, n.dq, n.bf16) && rows16(dk, n.dk, n.bf16);

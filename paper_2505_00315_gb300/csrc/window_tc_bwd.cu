@@ -21,8 +21,8 @@
 // Sixteen warps compute (four per TMEM lane quadrant, each a quarter of the columns), one
 // loads by TMA, one issues the MMAs, one more (dK, dV) brings lse and D.  While MMAs
 // of one block run, the workers turn the other scores: the queue of MMAs is
-//   dK, dV:  dV_i S_i+1 | dK_i dP_i+1        dQ:  dQ_j dP_j+1 S_j+2
-// so that one pair of products always covers one half of the elementwise work.
+//   dK, dV:  dV_i S_i+1 | dK_i dP_i+1        dQ:  dP_j+1 dQ_j S_j+2
+// so that products always cover the elementwise work of the next scores.
 //
 // Where a pair of tiles is seen in part, the masked places have P = dS = 0; a NaN or
 // infinity in an operand row that meets them would still make a NaN of them.  dK, dV:
@@ -541,10 +541,11 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                     const int g = g0 + j;
                     ok = wait(sm.ds_ready, g & 1);
                     if (!ok) break;
+                    if (j + 1 < n) dp_of(g + 1);   // first: the workers' next step waits for it
+                    if (!ok) break;
                     tc_fence_after();
                     mma_weights<5>(tdQ, tS + 128 * (g & 1), mn_major(sm.k[g % 3]), idG, j > 0);   // dQ += dS K_j
                     mma_commit(smem_u32(&sm.k_empty[g % 3]));
-                    if (j + 1 < n) dp_of(g + 1);
                     if (j + 2 < n) s_of(g + 2);
                 }
                 mma_commit(smem_u32(&sm.done));
