@@ -306,8 +306,8 @@ typedef struct {
  * where R(t) turns pair p of the first `rotary` dimensions by
  * t * theta^(-2p / rotary): pair (2p, 2p+1), or with halves = 1
  * (p, p + rotary/2).  The layer's own rotation is rotary = hp/2, theta = 10000,
- * halves = 0.  Sizes: rotary even and 0 <= rotary <= hp (0: no rotation); with halves = 1
- * rotary is 8 or a multiple of 16 (else MOSA_ERR_UNSUPPORTED); eps >= 0; theta >= 1. */
+ * halves = 0.  Sizes: rotary even and 0 <= rotary <= hp (0: no rotation), with halves = 1
+ * a multiple of 8 (else MOSA_ERR_UNSUPPORTED); eps >= 0; theta >= 1. */
 typedef struct {
     int32_t B, T, H, Hkv, hp;
     int32_t dtype;

@@ -7,73 +7,101 @@
 namespace mosa {
 namespace win {
 
+// The values of lane li of a row: lo .. lo+3 and hi .. hi+3, so that both values of each
+// rotated pair lie on one lane: neighbours, or with halves the same places of the
+// two halves of the rotated dimensions (whose number is a multiple of 8 then).
+struct Part {
+    int lo, hi;
+    __device__ __forceinline__ Part(int li, int rotary, int halves) {
+        const bool split = halves && 8 * li < rotary;
+        lo = split ? 4 * li : 8 * li;
+        hi = split ? 4 * li + (rotary >> 1) : 8 * li + 4;
+    }
+};
+
+// Four consecutive values, in one access where VEC.
 template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
-    if (VEC) {
-        alignas(16) T w[8];
+__device__ __forceinline__ void load4(const T *p, float *v) {
+    if (!VEC) {
 #pragma unroll
-        for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i)
-            reinterpret_cast<uint4 *>(w)[i] = reinterpret_cast<const uint4 *>(p)[i];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f32(w[i]);
+        for (int i = 0; i < 4; ++i) v[i] = to_f32(p[i]);
+    } else if constexpr (sizeof(T) == 4) {
+        const float4 w = *reinterpret_cast<const float4 *>(p);
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f32(p[i]);
+        const uint2 w = *reinterpret_cast<const uint2 *>(p);
+        v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
     }
 }
 
+// Two bf16 values of a word, rounded to nearest even (the first in the low half).
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
+    uint32_t w;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    return w;
+}
+
 template <class T, bool VEC>
-__device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
-    if (VEC) {
-        alignas(16) T w[8];
+__device__ __forceinline__ void store4(T *p, const float *v) {
+    if (!VEC) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = from_f32<T>(v[i]);
-#pragma unroll
-        for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i)
-            reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(w)[i];
+        for (int i = 0; i < 4; ++i) p[i] = from_f32<T>(v[i]);
+    } else if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = from_f32<T>(v[i]);
+        *reinterpret_cast<uint2 *>(p) = make_uint2(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]));
     }
 }
 
-// Turns the head whose values c .. c+7 this lane holds by the angles of cs (dir =
-// -1: back).  Every lane of the warp takes part.
-__device__ __forceinline__ void turn8(float (&v)[8], int c, int rotary, int halves,
-                                      const float2 *cs, float dir, int lane) {
-    if (!halves) {
-#pragma unroll
-        for (int e = 0; e < 8; e += 2)
-            if (c + e < rotary) {
-                const float2 a = cs[(c + e) >> 1];
-                const float x0 = v[e], x1 = v[e + 1], sn = a.y * dir;
-                v[e] = x0 * a.x - x1 * sn;
-                v[e + 1] = x0 * sn + x1 * a.x;
-            }
+// A lane's eight values of the row at p: one access of 16 bytes of bf16 where they are neighbours.
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T *p, const Part &at, float (&v)[8]) {
+    if (VEC && sizeof(T) == 2 && at.hi == at.lo + 4) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(p + at.lo);
+        v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+        v[4] = __uint_as_float(w.z << 16); v[5] = __uint_as_float(w.z & 0xFFFF0000u);
+        v[6] = __uint_as_float(w.w << 16); v[7] = __uint_as_float(w.w & 0xFFFF0000u);
         return;
     }
-    const int half = rotary >> 1;
-    if (half == 4) {   // both partners on this lane
-        if (c == 0) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 a = cs[e];
-                const float x0 = v[e], x1 = v[e + 4], sn = a.y * dir;
-                v[e] = x0 * a.x - x1 * sn;
-                v[e + 4] = x0 * sn + x1 * a.x;
-            }
-        }
+    load4<T, VEC>(p + at.lo, v);
+    load4<T, VEC>(p + at.hi, v + 4);
+}
+
+template <class T, bool VEC>
+__device__ __forceinline__ void store8(T *p, const Part &at, const float (&v)[8]) {
+    if (VEC && sizeof(T) == 2 && at.hi == at.lo + 4) {
+        *reinterpret_cast<uint4 *>(p + at.lo) = make_uint4(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]),
+                                                           two_bf16(v[4], v[5]), two_bf16(v[6], v[7]));
         return;
     }
-    const bool low = c < half, turned = c < rotary;
-    const int other = turned ? (low ? lane + (half >> 3) : lane - (half >> 3)) : lane;
+    store4<T, VEC>(p + at.lo, v);
+    store4<T, VEC>(p + at.hi, v + 4);
+}
+
+// Turns lane li's eight values by the angles of cs (dir = -1: back).
+__device__ __forceinline__ void turn8(float (&v)[8], int li, int rotary, int halves, const float2 *cs,
+                                      float dir) {
+    if (8 * li >= rotary) return;
+    const float4 a = reinterpret_cast<const float4 *>(cs)[2 * li];
+    const float4 b = reinterpret_cast<const float4 *>(cs)[2 * li + 1];
+    const float co[4] = {a.x, a.z, b.x, b.z}, sn[4] = {a.y * dir, a.w * dir, b.y * dir, b.w * dir};
+    if (halves) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float x = __shfl_sync(0xffffffffu, v[e], other);
-        if (turned) {
-            const float2 a = cs[(low ? c : c - half) + e];
-            v[e] = fmaf(low ? -x : x, a.y * dir, v[e] * a.x);
+        for (int e = 0; e < 4; ++e) {
+            const float x0 = v[e], x1 = v[e + 4];
+            v[e] = x0 * co[e] - x1 * sn[e];
+            v[e + 4] = x0 * sn[e] + x1 * co[e];
         }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (8 * li + 2 * e < rotary) {
+                const float x0 = v[2 * e], x1 = v[2 * e + 1];
+                v[2 * e] = x0 * co[e] - x1 * sn[e];
+                v[2 * e + 1] = x0 * sn[e] + x1 * co[e];
+            }
     }
 }
 

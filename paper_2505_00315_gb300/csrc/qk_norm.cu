@@ -43,35 +43,37 @@ struct NormArgs {
     int step, batch;        // tokens of a step, and of an item
 };
 
+// What a block keeps of a step's tokens: cosines and sines, and where each token's rows start in
+// the input, the output (backward: its gradient) and the input's gradient.
 struct StepTokens {
-    float2 cs[kMaxTokens][64];          // cosines and sines
-    int b[kMaxTokens], t[kMaxTokens];   // sequence and token
+    alignas(16) float2 cs[kMaxTokens][64];
+    long long in[2][kMaxTokens], y[2][kMaxTokens], d[2][kMaxTokens];   // [queries, keys]
 };
 
 // The queries' (KEY: keys') part of one step: items of `batch` tokens of one head, one a
-// lane group.  acc: backward, this lane's sums of g r x.
-template <class T, bool VEC, bool kBackward, bool KEY>
+// lane group (LG lanes).  acc: backward, this lane's sums of g r x.
+template <class T, bool VEC, bool kBackward, int LG, bool KEY>
 __device__ __forceinline__ void norm_step(const NormArgs &p, const StepTokens &st, int tokens,
-                                          const float (&gamma)[8], float (&acc)[8]) {
+                                          const Part &at, const float (&gamma)[8], float (&acc)[8]) {
+    constexpr int groups = kThreads / LG;
     const Norm &n = p.n;
-    const int lanes = n.hp >> 3, groups = kThreads / lanes, lane = threadIdx.x & 31;
-    const int grp = threadIdx.x / lanes, c = (threadIdx.x % lanes) * 8;
+    const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
     const int heads = KEY ? n.Hkv : n.H;
-    const T *in = static_cast<const T *>(KEY ? p.k : p.q) + c;
-    const T *dy = static_cast<const T *>(KEY ? p.dyk : p.dyq) + c;
-    T *out = static_cast<T *>(KEY ? p.ok : p.oq) + c;
-    const Str &si = KEY ? n.k : n.q, &sy = KEY ? n.yk : n.yq, &sd = KEY ? n.dk : n.dq;
-    const float inv_hp = 1.f / (float)n.hp;
+    const long long hi = KEY ? n.k.h : n.q.h, hy = KEY ? n.yk.h : n.yq.h, hd = KEY ? n.dk.h : n.dq.h;
     const int items = (tokens + p.batch - 1) / p.batch * heads;
     for (int it0 = 0; it0 < items; it0 += groups) {   // (all lanes together: the sums are shuffles)
         const int it = it0 + grp, bat = it / heads, h = it - bat * heads;
         const int i0 = bat * p.batch, count = it < items ? min(p.batch, tokens - i0) : 0;
+        const T *in = static_cast<const T *>(KEY ? p.k : p.q) + h * hi;
+        const T *dy = static_cast<const T *>(KEY ? p.dyk : p.dyq) + h * hy;
+        T *out = static_cast<T *>(KEY ? p.ok : p.oq) + h * (kBackward ? hd : hy);
+        const long long *to = kBackward ? st.d[KEY] : st.y[KEY];
         float x[kBatch][8], g[kBackward ? kBatch : 1][8];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             if (u < count) {
-                load8<T, VEC>(in + si.at(st.b[i0 + u], st.t[i0 + u], h), x[u]);
-                if (kBackward) load8<T, VEC>(dy + sy.at(st.b[i0 + u], st.t[i0 + u], h), g[kBackward ? u : 0]);
+                load8<T, VEC>(in + st.in[KEY][i0 + u], at, x[u]);
+                if (kBackward) load8<T, VEC>(dy + st.y[KEY][i0 + u], at, g[kBackward ? u : 0]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[u][e] = g[kBackward ? u : 0][e] = 0.f;
@@ -84,15 +86,15 @@ __device__ __forceinline__ void norm_step(const NormArgs &p, const StepTokens &s
             float ss = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss = fmaf(x[u][e], x[u][e], ss);
-            const float r = rsqrtf(fmaf(group_sum(ss, lanes), inv_hp, n.eps));
+            const float r = rsqrtf(fmaf(group_sum(ss, LG), 1.f / (8 * LG), n.eps));
             if (!kBackward) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[u][e] *= r * gamma[e];
-                turn8(x[u], c, n.rotary, n.halves, cs, 1.f, lane);
-                if (u < count) store8<T, VEC>(out + sy.at(st.b[i0 + u], st.t[i0 + u], h), x[u]);
+                turn8(x[u], li, n.rotary, n.halves, cs, 1.f);
+                if (u < count) store8<T, VEC>(out + to[i0 + u], at, x[u]);
             } else {
                 float (&gu)[8] = g[kBackward ? u : 0];
-                turn8(gu, c, n.rotary, n.halves, cs, -1.f, lane);
+                turn8(gu, li, n.rotary, n.halves, cs, -1.f);
                 float dot = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -101,29 +103,30 @@ __device__ __forceinline__ void norm_step(const NormArgs &p, const StepTokens &s
                     gu[e] *= gamma[e];
                     dot = fmaf(gu[e], x[u][e], dot);
                 }
-                dot = group_sum(dot, lanes) * inv_hp;
+                dot = group_sum(dot, LG) * (1.f / (8 * LG));
 #pragma unroll
                 for (int e = 0; e < 8; ++e) gu[e] = r * fmaf(-x[u][e], dot, gu[e]);
-                if (u < count) store8<T, VEC>(out + sd.at(st.b[i0 + u], st.t[i0 + u], h), gu);
+                if (u < count) store8<T, VEC>(out + to[i0 + u], at, gu);
             }
         }
     }
 }
 
-template <class T, bool VEC, bool kBackward>
+template <class T, bool VEC, bool kBackward, int LG>
 __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_constant__ NormArgs p,
                                                                 const __grid_constant__ Turns tab) {
+    constexpr int groups = kThreads / LG, hp = 8 * LG;
     __shared__ StepTokens st;
     extern __shared__ float red[];   // backward: [groups][2][hp]
     const Norm &n = p.n;
-    const int lanes = n.hp >> 3, groups = kThreads / lanes;
-    const int grp = threadIdx.x / lanes, c = (threadIdx.x % lanes) * 8;
+    const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
+    const Part at(li, n.rotary, n.halves);
     const long long N = (long long)n.B * n.T;
     float gq[8], gk[8], aq[8], ak[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 1.f, aq[e] = ak[e] = 0.f;
-    if (p.gq != nullptr) load8<T, false>((const T *)p.gq + c, gq);
-    if (p.gk != nullptr) load8<T, false>((const T *)p.gk + c, gk);
+    if (p.gq != nullptr) load8<T, false>((const T *)p.gq, at, gq);
+    if (p.gk != nullptr) load8<T, false>((const T *)p.gk, at, gk);
     const int pairs = n.rotary >> 1;
     for (long long tok0 = (long long)blockIdx.x * p.step; tok0 < N; tok0 += (long long)gridDim.x * p.step) {
         const int tokens = (int)min((long long)p.step, N - tok0);
@@ -132,8 +135,12 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_con
         if (threadIdx.x < tokens) {
             int b = b0, t = t0 + threadIdx.x;
             while (t >= n.T) t -= n.T, ++b;
-            st.b[threadIdx.x] = b;
-            st.t[threadIdx.x] = t;
+            st.in[0][threadIdx.x] = n.q.at(b, t, 0);
+            st.in[1][threadIdx.x] = n.k.at(b, t, 0);
+            st.y[0][threadIdx.x] = n.yq.at(b, t, 0);
+            st.y[1][threadIdx.x] = n.yk.at(b, t, 0);
+            st.d[0][threadIdx.x] = n.dq.at(b, t, 0);
+            st.d[1][threadIdx.x] = n.dk.at(b, t, 0);
         }
         for (int e = threadIdx.x; e < tokens * pairs; e += kThreads) {
             const int i = e / pairs, a = e - i * pairs;
@@ -142,20 +149,21 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_con
             st.cs[i][a] = angle_of(tab.phi[a], p.pos != nullptr ? p.pos[tok0 + i] : t);
         }
         __syncthreads();
-        norm_step<T, VEC, kBackward, false>(p, st, tokens, gq, aq);
-        norm_step<T, VEC, kBackward, true>(p, st, tokens, gk, ak);
+        norm_step<T, VEC, kBackward, LG, false>(p, st, tokens, at, gq, aq);
+        norm_step<T, VEC, kBackward, LG, true>(p, st, tokens, at, gk, ak);
     }
     if (kBackward && p.partial != nullptr) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            red[(grp * 2 + 0) * n.hp + c + e] = aq[e];
-            red[(grp * 2 + 1) * n.hp + c + e] = ak[e];
+            const int c = e < 4 ? at.lo + e : at.hi + e - 4;
+            red[(grp * 2 + 0) * hp + c] = aq[e];
+            red[(grp * 2 + 1) * hp + c] = ak[e];
         }
         __syncthreads();
-        for (int o = threadIdx.x; o < 2 * n.hp; o += kThreads) {
+        for (int o = threadIdx.x; o < 2 * hp; o += kThreads) {
             float sum = 0.f;
-            for (int u = 0; u < groups; ++u) sum += red[u * 2 * n.hp + o];
-            p.partial[(long long)blockIdx.x * 2 * n.hp + o] = sum;
+            for (int u = 0; u < groups; ++u) sum += red[u * 2 * hp + o];
+            p.partial[(long long)blockIdx.x * 2 * hp + o] = sum;
         }
     }
 }
@@ -191,20 +199,25 @@ int bwd_blocks(const Norm &n) {
     return (int)(steps < kMaxBlocks ? steps : kMaxBlocks);
 }
 
-template <bool kBackward>
-cudaError_t launch(const NormArgs &p, bool vec, unsigned blocks, cudaStream_t s) {
+template <bool kBackward, class T, bool VEC>
+cudaError_t launch_of(const NormArgs &p, unsigned blocks, cudaStream_t s) {
     const Turns tab = make_turns(p.n.rotary, p.n.theta);
     const int smem = kBackward ? kThreads / (p.n.hp / 8) * 2 * p.n.hp * 4 : 0;   // 16 KB
-    auto go = [&](auto kernel) {
-        kernel<<<blocks, kThreads, smem, s>>>(p, tab);
-        note_launches(1);
-        return cudaGetLastError();
-    };
+    switch (p.n.hp) {
+        case 16: qk_norm_rope_kernel<T, VEC, kBackward, 2><<<blocks, kThreads, smem, s>>>(p, tab); break;
+        case 32: qk_norm_rope_kernel<T, VEC, kBackward, 4><<<blocks, kThreads, smem, s>>>(p, tab); break;
+        case 64: qk_norm_rope_kernel<T, VEC, kBackward, 8><<<blocks, kThreads, smem, s>>>(p, tab); break;
+        default: qk_norm_rope_kernel<T, VEC, kBackward, 16><<<blocks, kThreads, smem, s>>>(p, tab); break;
+    }
+    note_launches(1);
+    return cudaGetLastError();
+}
+
+template <bool kBackward>
+cudaError_t launch(const NormArgs &p, bool vec, unsigned blocks, cudaStream_t s) {
     if (p.n.bf16)
-        return vec ? go(qk_norm_rope_kernel<bf16, true, kBackward>)
-                   : go(qk_norm_rope_kernel<bf16, false, kBackward>);
-    return vec ? go(qk_norm_rope_kernel<float, true, kBackward>)
-               : go(qk_norm_rope_kernel<float, false, kBackward>);
+        return vec ? launch_of<kBackward, bf16, true>(p, blocks, s) : launch_of<kBackward, bf16, false>(p, blocks, s);
+    return vec ? launch_of<kBackward, float, true>(p, blocks, s) : launch_of<kBackward, float, false>(p, blocks, s);
 }
 
 }  // namespace

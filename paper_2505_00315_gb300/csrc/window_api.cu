@@ -47,7 +47,7 @@ mosa_status check_rotation(int rotary, int halves, int hp, float theta, float ep
     if (halves != 0 && halves != 1) return MOSA_ERR_INVALID_ARG;
     if (!(theta >= 1.f) || std::isinf(theta) || !(eps >= 0.f) || std::isinf(eps))
         return MOSA_ERR_INVALID_ARG;
-    if (halves && rotary != 0 && rotary != 8 && rotary % 16 != 0) return MOSA_ERR_UNSUPPORTED;
+    if (halves && rotary % 8 != 0) return MOSA_ERR_UNSUPPORTED;
     return MOSA_OK;
 }
 

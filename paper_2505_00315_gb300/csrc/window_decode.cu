@@ -3,12 +3,19 @@
 // where a sequence's slots are split over several CTAs a second one that joins
 // their partial softmaxes.
 //
-// For each query head, over the visible tokens u and the new one,
+// For each query head, over the visible tokens u (the new one last)
 //     s_u = scale q . k_u,  m = max s,  l = sum exp(s - m),  O = sum exp(s - m) v_u / l
-// in one pass: running m, l and O, joined over lanes, warps and splits by
+// in one pass: running m, l and O, joined over warps and splits by
 //     (m, l, O) + (m', l', O') = (M, l e^(m-M) + l' e^(m'-M), O e^(m-M) + O' e^(m'-M)).
-// Bound by the cache's bytes, each read once: hp/8 lanes hold a row, eight values a
-// lane, and up to eight query heads of a group meet a row while it is in registers.
+// Bound by the cache's bytes, each read once for up to eight query heads of a group.
+//   bf16   warp-wide matrix products (m16n8k16) take 16 tokens a step, with rows of K and V
+//          loaded straight into fragments, 16 bytes a lane: a product's order of summation
+//          is free, so a lane's eight neighbouring values may be any eight of it.  The 16
+//          rows of the other operand are the eight heads twice, what bf16 holds of q (and of the weights)
+//          and what its rounding leaves, so that nothing but the cache itself is rounded.
+//          tcgen05 would want 128 rows and its operands in shared memory; the products are
+//          a tenth of the time that the bytes take.
+//   fp32, hp = 16, unaligned rows   CUDA cores: hp/8 lanes hold a row, eight values a lane.
 #include "head_rows.cuh"
 #include "launch.h"
 #include "profile.h"
@@ -18,9 +25,6 @@ namespace mosa {
 namespace win {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kKeys = 4;        // rows a lane group takes at once
 constexpr int kMaxSplits = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -38,77 +42,131 @@ __device__ __forceinline__ float merge_scale(float m, float M) {
     return m == -INFINITY ? 0.f : exp2f(m - M);
 }
 
-template <class T, bool VEC, int HD, int GT>
-__global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_constant__ DecodeArgs p,
-                                                                 const __grid_constant__ Turns tab) {
-    constexpr int LK = HD / 8, kRows = 32 / LK;          // lanes a row, rows a warp
-    const Decode &d = p.d;
-    const int G = d.H / d.Hkv;
-    const int split = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
-    const int hk = blockIdx.y, b = blockIdx.z;
-    const int g0 = chunk * GT, heads = min(GT, G - g0);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int grp = threadIdx.x / LK, c = (threadIdx.x % LK) * 8;
-    __shared__ float2 cs[64];
-    __shared__ __align__(16) float sq[GT][HD];
-    __shared__ __align__(16) float sk[HD];
-    __shared__ float sm_m[kWarps][GT], sm_l[kWarps][GT];
-    __shared__ __align__(16) float sm_o[kWarps][GT][HD];
+// The tokens of one split of one sequence: numbers lo .. hi-1 of its visible tokens, of which the
+// first nS are sinks (in their slots) and the others, up to the new one, follow one another
+// in the ring from slot s0 on.
+struct Seen {
+    int lo, hi, nS, s0, C, ring;
+    __device__ __forceinline__ int slot(int u) const {
+        const int s = u < nS ? u : s0 + (u - nS);
+        return s >= C ? s - ring : s;   // (a window is no longer than the ring)
+    }
+};
 
-    const int len = p.lens[b], at = len - 1;
+// What every CTA does first: the query heads g0 .. g0+heads-1 of the group, normalised, turned
+// and scaled (log2 units) into sq, and in the CTAs whose split holds the new token the
+// token's rows into the caches.  False where the sequence is skipped.
+template <class T, int HD, int GT, int THREADS>
+__device__ __forceinline__ bool decode_prologue(const DecodeArgs &p, const Turns &tab, int split,
+                                                int hk, int b, int g0, int heads, float (*sq)[HD],
+                                                Seen *seen) {
+    constexpr int LG = HD / 8;
+    __shared__ __align__(16) float2 cs[64];
+    const Decode &d = p.d;
+    const int G = d.H / d.Hkv, len = p.lens[b], at = len - 1;
     if (len <= 0) {   // skipped: the output is zero, the cache stays
         if (split == 0)
-            for (int e = threadIdx.x; e < heads * HD; e += kThreads)
+            for (int e = threadIdx.x; e < heads * HD; e += THREADS)
                 static_cast<T *>(p.o)[d.o.at(b, 0, hk * G + g0 + e / HD) + e % HD] = from_f32<T>(0.f);
-        return;
+        return false;
     }
-    for (int e = threadIdx.x; e < d.rotary / 2; e += kThreads) cs[e] = angle_of(tab.phi[e], at);
+    const int ring = d.C - d.sinks, nS = min(d.sinks, len);
+    const int wlo = max(d.sinks, at - d.window + 1), n = nS + max(at + 1 - wlo, 0);
+    const int per = (n + p.splits - 1) / p.splits;
+    *seen = Seen{min(split * per, n), min((split + 1) * per, n), nS,
+                 at >= wlo ? d.sinks + (wlo - d.sinks) % ring : 0, d.C, ring};
+    const bool newest = seen->lo < n && seen->hi == n;   // this split holds the new token
+    for (int e = threadIdx.x; e < d.rotary / 2; e += THREADS) cs[e] = angle_of(tab.phi[e], at);
     __syncthreads();
-    // the new token's q heads, and in the first split its k
-    for (int u0 = 0; u0 < GT + 1; u0 += kThreads / LK) {
+    const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
+    const Part part(li, d.rotary, d.halves);
+    for (int u0 = 0; u0 < GT + 1; u0 += THREADS / LG) {   // (all lanes together: the sums are shuffles)
         const int u = u0 + grp;
-        const bool key = u == GT, on = u < heads || (key && split == 0);
+        const bool key = u == GT, on = u < heads || (key && newest);
         float x[8], gm[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.f, gm[e] = 1.f;
         if (on) {
-            load8<T, false>((key ? (const T *)p.k + d.k.at(b, 0, hk)
-                                 : (const T *)p.q + d.q.at(b, 0, hk * G + g0 + u)) + c, x);
+            load8<T, false>(key ? (const T *)p.k + d.k.at(b, 0, hk)
+                                : (const T *)p.q + d.q.at(b, 0, hk * G + g0 + u), part, x);
             const T *gamma = (const T *)(key ? p.gk : p.gq);
-            if (d.norm && gamma != nullptr) load8<T, false>(gamma + c, gm);
+            if (d.norm && gamma != nullptr) load8<T, false>(gamma, part, gm);
         }
         if (d.norm) {
             float ss = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-            const float r = rsqrtf(group_sum(ss, LK) / (float)HD + d.eps);
+            const float r = rsqrtf(fmaf(group_sum(ss, LG), 1.f / HD, d.eps));
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= r * gm[e];
         }
-        turn8(x, c, d.rotary, d.halves, cs, 1.f, lane);
-        if (on) {
-            float *dst = key ? sk + c : sq[u < GT ? u : 0] + c;
+        turn8(x, li, d.rotary, d.halves, cs, 1.f);
+        if (on && key) {
+            const int slot = seen->slot(n - 1);
+            store8<T, false>((T *)p.kc + d.kc.at(b, slot, hk), part, x);
+            const T *v = (const T *)p.v + d.v.at(b, 0, hk);
+            T *o = (T *)p.vc + d.vc.at(b, slot, hk);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dst[e] = key ? to_f32(from_f32<T>(x[e])) : x[e];
+            for (int e = 0; e < 8; ++e) o[8 * li + e] = v[8 * li + e];
+        } else if (u < GT) {
+            const float f = d.scale * kLog2e;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sq[u][e < 4 ? part.lo + e : part.hi + e - 4] = x[e] * f;
         }
     }
     __syncthreads();
-    const int ring = d.C - d.sinks;
-    if (split == 0 && chunk == 0 && threadIdx.x < HD) {   // append
-        const int slot = at < d.sinks ? at : d.sinks + (at - d.sinks) % ring;
-        const int e = threadIdx.x;
-        static_cast<T *>(p.kc)[d.kc.at(b, slot, hk) + e] = from_f32<T>(sk[e]);
-        static_cast<T *>(p.vc)[d.vc.at(b, slot, hk) + e] = static_cast<const T *>(p.v)[d.v.at(b, 0, hk) + e];
-    }
-    // the older tokens it sees: sinks 0 .. nS-1, then wlo .. at-1, which may wrap in the ring once
-    const int nS = min(d.sinks, at), wlo = max(d.sinks, at - d.window + 1);
-    const int nW = max(at - wlo, 0), n = nS + nW;
-    const int s0 = nW > 0 ? d.sinks + (wlo - d.sinks) % ring : 0;
-    const int per = (n + p.splits - 1) / p.splits;
-    const int lo = min(split * per, n), hi = min(lo + per, n);
-    const T *Kb = (const T *)p.kc + d.kc.at(b, 0, hk) + c, *Vb = (const T *)p.vc + d.vc.at(b, 0, hk) + c;
-    const float sl2 = d.scale * kLog2e;
+    return true;
+}
 
+// The warps' partial softmaxes (m, l and O of each head in shared memory) joined and written.
+template <class T, int HD, int GT, int WARPS>
+__device__ __forceinline__ void decode_epilogue(const DecodeArgs &p, int split, int hk, int b, int g0,
+                                                int heads, const float (*sm_m)[GT],
+                                                const float (*sm_l)[GT], const float (*sm_o)[GT][HD]) {
+    const Decode &d = p.d;
+    __syncthreads();
+    for (int e = threadIdx.x; e < heads * HD; e += WARPS * 32) {
+        const int g = e / HD, x = e % HD, h = hk * (d.H / d.Hkv) + g0 + g;
+        float M = -INFINITY, L = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) M = fmaxf(M, sm_m[w][g]);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = merge_scale(sm_m[w][g], M);
+            L += sm_l[w][g] * f;
+            o += sm_o[w][g][x] * f;
+        }
+        if (p.splits == 1) {
+            static_cast<T *>(p.o)[d.o.at(b, 0, h) + x] = from_f32<T>(o / L);
+        } else {
+            const long long row = ((long long)b * d.H + h) * p.splits + split;
+            p.po[row * HD + x] = o;
+            if (x == 0) p.pml[row] = make_float2(M, L);
+        }
+    }
+}
+
+// ------------------------------------------------------------- CUDA cores
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kKeys = 4;        // rows a lane group takes at once
+
+template <class T, bool VEC, int HD, int GT>
+__global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_constant__ DecodeArgs p,
+                                                                 const __grid_constant__ Turns tab) {
+    constexpr int LK = HD / 8, kRows = 32 / LK;          // lanes a row, rows a warp
+    const Decode &d = p.d;
+    const int split = blockIdx.x / p.chunks, g0 = blockIdx.x % p.chunks * GT;
+    const int hk = blockIdx.y, b = blockIdx.z, heads = min(GT, d.H / d.Hkv - g0);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (threadIdx.x % LK) * 8;
+    __shared__ __align__(16) float sq[GT][HD];
+    __shared__ float sm_m[kWarps][GT], sm_l[kWarps][GT];
+    __shared__ __align__(16) float sm_o[kWarps][GT][HD];
+    Seen seen;
+    if (!decode_prologue<T, HD, GT, kThreads>(p, tab, split, hk, b, g0, heads, sq, &seen)) return;
+    const Part part(threadIdx.x % LK, 0, 0);
+    const T *Kb = (const T *)p.kc + d.kc.at(b, 0, hk), *Vb = (const T *)p.vc + d.vc.at(b, 0, hk);
     float q[GT][8], acc[GT][8], m[GT], l[GT];
 #pragma unroll
     for (int g = 0; g < GT; ++g) {
@@ -116,40 +174,20 @@ __global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_co
         l[g] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            q[g][e] = g < heads ? sq[g][c + e] * sl2 : 0.f;
+            q[g][e] = g < heads ? sq[g][c + e] : 0.f;
             acc[g][e] = 0.f;
         }
     }
-    if (split == 0 && grp == 0) {   // the new token itself
-        float v[8];
-        load8<T, false>((const T *)p.v + d.v.at(b, 0, hk) + c, v);
-#pragma unroll
-        for (int g = 0; g < GT; ++g) {
-            float s = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s = fmaf(q[g][e], sk[c + e], s);
-#pragma unroll
-            for (int o = LK / 2; o > 0; o >>= 1)
-                s += __shfl_xor_sync((LK == 32 ? 0xffffffffu : (1u << LK) - 1u), s, o);
-            m[g] = s;
-            l[g] = 1.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[g][e] = v[e];
-        }
-    }
-    __syncwarp();
-    for (int u0 = lo + warp * kRows * kKeys; u0 < hi; u0 += kWarps * kRows * kKeys) {
+    for (int u0 = seen.lo + warp * kRows * kKeys; u0 < seen.hi; u0 += kWarps * kRows * kKeys) {
         float kx[kKeys][8], vx[kKeys][8];
         bool on[kKeys];
 #pragma unroll
         for (int j = 0; j < kKeys; ++j) {
-            const int u = u0 + j * kRows + lane / LK;
-            on[j] = u < hi;
-            int slot = u < nS ? u : s0 + (u - nS);
-            if (slot >= d.C) slot -= ring;
+            const int u = u0 + j * kRows + lane / LK, slot = seen.slot(u);
+            on[j] = u < seen.hi;
             if (on[j]) {
-                load8<T, VEC>(Kb + (long long)slot * d.kc.t, kx[j]);
-                load8<T, VEC>(Vb + (long long)slot * d.vc.t, vx[j]);
+                load8<T, VEC>(Kb + (long long)slot * d.kc.t, part, kx[j]);
+                load8<T, VEC>(Vb + (long long)slot * d.vc.t, part, vx[j]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) kx[j][e] = vx[j][e] = 0.f;
@@ -183,7 +221,7 @@ __global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_co
             }
         }
     }
-    // join the rows of a warp, then the warps
+    // join the rows of a warp
 #pragma unroll
     for (int g = 0; g < GT; ++g) {
 #pragma unroll
@@ -202,26 +240,150 @@ __global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_co
             if (lane == 0) sm_m[warp][g] = m[g], sm_l[warp][g] = l[g];
         }
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < heads * HD; e += kThreads) {
-        const int g = e / HD, x = e % HD, h = hk * G + g0 + g;
-        float M = -INFINITY, L = 0.f, o = 0.f;
+    decode_epilogue<T, HD, GT, kWarps>(p, split, hk, b, g0, heads, sm_m, sm_l, sm_o);
+}
+
+// ------------------------------------------------------- matrix products
+
+constexpr int kMmaWarps = 4, kMmaHeads = 8, kMmaTokens = 16;
+
+// D += A B: A 16 x 16, B 16 x 8, bf16; D fp32.
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+        "{%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Two values as bf16 (hi) and what their rounding left, as bf16 (lo).
+__device__ __forceinline__ void halves_of(float a, float b, uint32_t &hi, uint32_t &lo) {
+    hi = two_bf16(a, b);
+    lo = two_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xFFFF0000u));
+}
+
+// Lane (g, t) = (lane / 4, lane % 4).  Scores of 8 tokens: A = the heads' q (rows g: hi, g + 8: lo),
+// B = the tokens' rows of K, token g on lane (g, .), whose 16-byte pieces t, t + 4, .. serve two
+// 16-wide steps each.  O: A = the weights (hi and lo rows again) of 16 tokens, in the places where
+// the scores' results lie; B = V, tokens 2t, 2t+1, 8+2t, 9+2t on lane (g, t), its piece g (and g + 8) of
+// the row: value j of a piece is column g of output tile j.
+template <int HD>
+__global__ void __launch_bounds__(kMmaWarps * 32) window_decode_mma_kernel(
+    const __grid_constant__ DecodeArgs p, const __grid_constant__ Turns tab) {
+    constexpr int kPieces = HD / 32;                 // 16-byte pieces of K a lane
+    constexpr int VP = HD >= 64 ? HD / 64 : 1;       // pieces of V a lane, of
+    constexpr int VE = HD >= 64 ? 8 : HD / 8;        // so many values
+    const Decode &d = p.d;
+    const int split = blockIdx.x / p.chunks, g0 = blockIdx.x % p.chunks * kMmaHeads;
+    const int hk = blockIdx.y, b = blockIdx.z, heads = min(kMmaHeads, d.H / d.Hkv - g0);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    __shared__ __align__(16) float sq[kMmaHeads][HD];
+    __shared__ float sm_m[kMmaWarps][kMmaHeads], sm_l[kMmaWarps][kMmaHeads];
+    __shared__ __align__(16) float sm_o[kMmaWarps][kMmaHeads][HD];
+    Seen seen;
+    if (!decode_prologue<bf16, HD, kMmaHeads, kMmaWarps * 32>(p, tab, split, hk, b, g0, heads, sq, &seen))
+        return;
+    uint32_t qa[kPieces][2][4];
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm_m[w][g]);
+    for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float f = merge_scale(sm_m[w][g], M);
-            L += sm_l[w][g] * f;
-            o += sm_o[w][g][x] * f;
+        for (int s = 0; s < 2; ++s) {
+            const float *x = &sq[g][8 * (t + 4 * i) + 4 * s];
+            halves_of(x[0], x[1], qa[i][s][0], qa[i][s][1]);
+            halves_of(x[2], x[3], qa[i][s][2], qa[i][s][3]);
         }
-        if (p.splits == 1) {
-            static_cast<T *>(p.o)[d.o.at(b, 0, h) + x] = from_f32<T>(o / L);
-        } else {
-            const long long row = ((long long)b * d.H + h) * p.splits + split;
-            p.po[row * HD + x] = o;
-            if (x == 0) p.pml[row] = make_float2(M, L);
+    const bf16 *Kb = (const bf16 *)p.kc + d.kc.at(b, 0, hk) + 8 * t;
+    const bf16 *Vb = (const bf16 *)p.vc + d.vc.at(b, 0, hk) + VE * g;
+    float acc[VP * VE][4], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int j = 0; j < VP * VE; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
+    for (int u0 = seen.lo + warp * kMmaTokens; u0 < seen.hi; u0 += kMmaWarps * kMmaTokens) {
+        uint4 kx[2][kPieces];
+        uint32_t vx[4][VP][VE / 2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int u = u0 + 8 * r + g;
+            const bf16 *row = Kb + (long long)seen.slot(u) * d.kc.t;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                kx[r][i] = u < seen.hi ? *reinterpret_cast<const uint4 *>(row + 32 * i) : make_uint4(0, 0, 0, 0);
         }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int u = u0 + 8 * (r >> 1) + 2 * t + (r & 1);
+            const bf16 *row = Vb + (long long)seen.slot(u) * d.vc.t;
+#pragma unroll
+            for (int i = 0; i < VP; ++i) {
+                if constexpr (VE == 8) {
+                    const uint4 w = u < seen.hi ? *reinterpret_cast<const uint4 *>(row + 64 * i) : make_uint4(0, 0, 0, 0);
+                    vx[r][i][0] = w.x; vx[r][i][1] = w.y; vx[r][i][2] = w.z; vx[r][i][3] = w.w;
+                } else {
+                    const uint2 w = u < seen.hi ? *reinterpret_cast<const uint2 *>(row) : make_uint2(0, 0);
+                    vx[r][i][0] = w.x; vx[r][i][1] = w.y;
+                }
+            }
+        }
+        float s[2][4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[r][e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                mma16816(s[r], qa[i][0], kx[r][i].x, kx[r][i].y);
+                mma16816(s[r], qa[i][1], kx[r][i].z, kx[r][i].w);
+            }
+        }
+        // this lane: head g, tokens 8 r + 2 t + e; hi and lo rows added up
+        float w[4], mx = m;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            w[x] = s[x >> 1][x & 1] + s[x >> 1][2 + (x & 1)];
+            if (u0 + 8 * (x >> 1) + 2 * t + (x & 1) >= seen.hi) w[x] = -INFINITY;
+            mx = fmaxf(mx, w[x]);
+        }
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const float base = mx == -INFINITY ? 0.f : mx;
+        if (__any_sync(0xffffffffu, mx > m)) {
+            const float corr = exp2f(m - base);
+            l *= corr;
+#pragma unroll
+            for (int j = 0; j < VP * VE; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][e] *= corr;
+            m = mx;
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            w[x] = exp2f(w[x] - base);
+            l += w[x];
+        }
+        uint32_t pa[4];
+        halves_of(w[0], w[1], pa[0], pa[1]);
+        halves_of(w[2], w[3], pa[2], pa[3]);
+#pragma unroll
+        for (int i = 0; i < VP; ++i)
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+                const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
+                mma16816(acc[i * VE + j], pa, __byte_perm(vx[0][i][j >> 1], vx[1][i][j >> 1], sel),
+                         __byte_perm(vx[2][i][j >> 1], vx[3][i][j >> 1], sel));
+            }
     }
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    if (t == 0) sm_m[warp][g] = m, sm_l[warp][g] = l;
+#pragma unroll
+    for (int i = 0; i < VP; ++i)
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)   // output columns 2t, 2t+1 of the tile are pieces 2t, 2t+1
+                sm_o[warp][g][64 * i + VE * (2 * t + e) + j] = acc[i * VE + j][e] + acc[i * VE + j][2 + e];
+    decode_epilogue<bf16, HD, kMmaHeads, kMmaWarps>(p, split, hk, b, g0, heads, sm_m, sm_l, sm_o);
 }
 
 // O of one head: the splits' partial softmaxes joined.
@@ -243,35 +405,46 @@ __global__ void __launch_bounds__(128) decode_join_kernel(const __grid_constant_
     static_cast<T *>(p.o)[d.o.at(b, 0, h) + x] = from_f32<T>(o / L);
 }
 
-int heads_of(const Decode &d) {   // query heads a CTA takes
+// Whether the step runs on matrix products (the workspace does not depend on it).
+bool use_mma(const Decode &d, const void *Kc, const void *Vc) {
+    return d.bf16 && d.hp >= 32 && rows16(Kc, d.kc, true) && rows16(Vc, d.vc, true);
+}
+
+int heads_of(const Decode &d, bool mma) {   // query heads a CTA takes
     const int G = d.H / d.Hkv;
-    return G == 1 ? 1 : G == 2 ? 2 : G <= 4 ? 4 : 8;
+    return mma ? kMmaHeads : G == 1 ? 1 : G == 2 ? 2 : G <= 4 ? 4 : 8;
 }
 
 int splits_of(const Decode &d) {
-    const int G = d.H / d.Hkv, GT = heads_of(d), chunks = (G + GT - 1) / GT;
+    const int G = d.H / d.Hkv, chunks = (G + kMmaHeads - 1) / kMmaHeads;
     const long long ctas = (long long)d.B * d.Hkv * chunks;
     const long long seen = (long long)d.sinks + d.window;
-    const long long want = (2 * 152 + ctas - 1) / ctas, most = (seen + 127) / 128;
+    const long long want = (4 * 152 + ctas - 1) / ctas, most = (seen + 127) / 128;
     long long s = want < most ? want : most;
     return (int)(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s);
+}
+
+cudaError_t join(const DecodeArgs &p, cudaStream_t s) {
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess || p.splits == 1) return e;
+    const dim3 grid(p.d.H, p.d.B);
+    e = p.d.bf16 ? launch_pdl(decode_join_kernel<bf16>, grid, dim3(p.d.hp), 0, s, p)
+                 : launch_pdl(decode_join_kernel<float>, grid, dim3(p.d.hp), 0, s, p);
+    note_launches(1);
+    return e;
 }
 
 template <class T, bool VEC, int HD>
 cudaError_t launch_hd(const DecodeArgs &p, const Turns &tab, cudaStream_t s) {
     const dim3 grid(p.splits * p.chunks, p.d.Hkv, p.d.B);
-    switch (heads_of(p.d)) {
+    switch (heads_of(p.d, false)) {
         case 1: window_decode_kernel<T, VEC, HD, 1><<<grid, kThreads, 0, s>>>(p, tab); break;
         case 2: window_decode_kernel<T, VEC, HD, 2><<<grid, kThreads, 0, s>>>(p, tab); break;
         case 4: window_decode_kernel<T, VEC, HD, 4><<<grid, kThreads, 0, s>>>(p, tab); break;
         default: window_decode_kernel<T, VEC, HD, 8><<<grid, kThreads, 0, s>>>(p, tab); break;
     }
     note_launches(1);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || p.splits == 1) return e;
-    e = launch_pdl(decode_join_kernel<T>, dim3(p.d.H, p.d.B), dim3(HD), 0, s, p);
-    note_launches(1);
-    return e;
+    return join(p, s);
 }
 
 template <class T, bool VEC>
@@ -282,6 +455,17 @@ cudaError_t launch_of(const DecodeArgs &p, const Turns &tab, cudaStream_t s) {
         case 64: return launch_hd<T, VEC, 64>(p, tab, s);
         default: return launch_hd<T, VEC, 128>(p, tab, s);
     }
+}
+
+cudaError_t launch_mma(const DecodeArgs &p, const Turns &tab, cudaStream_t s) {
+    const dim3 grid(p.splits * p.chunks, p.d.Hkv, p.d.B);
+    switch (p.d.hp) {
+        case 32: window_decode_mma_kernel<32><<<grid, kMmaWarps * 32, 0, s>>>(p, tab); break;
+        case 64: window_decode_mma_kernel<64><<<grid, kMmaWarps * 32, 0, s>>>(p, tab); break;
+        default: window_decode_mma_kernel<128><<<grid, kMmaWarps * 32, 0, s>>>(p, tab); break;
+    }
+    note_launches(1);
+    return join(p, s);
 }
 
 size_t partial_bytes(const Decode &d, int splits) {
@@ -298,10 +482,12 @@ size_t decode_workspace(const Decode &d) {
 cudaError_t launch_decode(const Decode &d, const void *q, const void *k, const void *v,
                           const void *gq, const void *gk, const int32_t *lens, void *Kc, void *Vc,
                           void *O, void *ws, cudaStream_t s) {
-    const int splits = splits_of(d), GT = heads_of(d), G = d.H / d.Hkv;
+    const bool mma = use_split() && use_mma(d, Kc, Vc);
+    const int splits = splits_of(d), GT = heads_of(d, mma), G = d.H / d.Hkv;
     DecodeArgs p{d, q, k, v, gq, gk, Kc, Vc, O, lens, splits, (G + GT - 1) / GT, (float *)ws,
                  (float2 *)((char *)ws + partial_bytes(d, splits))};
     const Turns tab = make_turns(d.rotary, d.theta);
+    if (mma) return launch_mma(p, tab, s);
     const bool vec = rows16(Kc, d.kc, d.bf16) && rows16(Vc, d.vc, d.bf16);
     if (d.bf16) return vec ? launch_of<bf16, true>(p, tab, s) : launch_of<bf16, false>(p, tab, s);
     return vec ? launch_of<float, true>(p, tab, s) : launch_of<float, false>(p, tab, s);

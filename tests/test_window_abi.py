@@ -75,7 +75,7 @@ S = W.MosaStrides
 @pytest.mark.parametrize("kw,code", [
     (dict(B=0), INV), (dict(T=0), INV), (dict(H=-1), INV), (dict(dtype=5), INV), (dict(hp=48), UNS),
     (dict(rotary=3), INV), (dict(rotary=66), INV), (dict(rotary=-2), INV), (dict(halves=2), INV),
-    (dict(halves=1, rotary=24), UNS), (dict(theta=0.5), INV), (dict(theta=float("inf")), INV),
+    (dict(halves=1, rotary=20), UNS), (dict(theta=0.5), INV), (dict(theta=float("inf")), INV),
     (dict(eps=-1.0), INV), (dict(eps=float("nan")), INV), (dict(B=70000), UNS), (dict(T=1 << 30), UNS),
     (dict(B=60000, T=60000), UNS), (dict(s_q=S(-1, 64, 64)), INV), (dict(s_yq=S(0, 256, 64)), INV),
     (dict(s_yk=S(1280, 32, 64)), INV), (dict(s_q=S(1 << 61, 64, 64)), INV),
@@ -149,7 +149,7 @@ def test_attention_refuses_pointers_and_workspaces():
 @pytest.mark.parametrize("kw,code", [
     (dict(B=-1), INV), (dict(C=4), INV), (dict(C=0, sinks=0), INV), (dict(window=-2), INV),
     (dict(sinks=-1), INV), (dict(norm=2), INV), (dict(rotary=65), INV), (dict(H=5), INV),
-    (dict(halves=1, rotary=40), UNS), (dict(C=1 << 30), UNS), (dict(hp=8), UNS),
+    (dict(halves=1, rotary=36), UNS), (dict(C=1 << 30), UNS), (dict(hp=8), UNS),
     (dict(scale=-1.0), INV), (dict(s_kc=S(0, 128, 64)), INV), (dict(s_vc=S(2560, 128, 0)), INV),
 ])
 def test_decode_refuses(kw, code):
