@@ -80,6 +80,59 @@ __device__ __forceinline__ void store8(T *p, const Part &at, const float (&v)[8]
     store4<T, VEC>(p + at.hi, v + 4);
 }
 
+// A lane's eight values as they lie in memory, to be kept in flight (VEC rows).
+template <class T>
+struct Raw8 {
+    uint4 w[sizeof(T) / 2];
+};
+template <class T, bool VEC>
+__device__ __forceinline__ void load_raw(const T *p, const Part &at, Raw8<T> &r) {
+    if constexpr (!VEC) {
+        T v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[i < 4 ? at.lo + i : at.hi + i - 4];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                r.w[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                    __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+        } else {
+            uint32_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                u[i] = (uint32_t)__bfloat16_as_ushort(v[2 * i]) | (uint32_t)__bfloat16_as_ushort(v[2 * i + 1]) << 16;
+            r.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+    } else if constexpr (sizeof(T) == 4) {
+        r.w[0] = *reinterpret_cast<const uint4 *>(p + at.lo);
+        r.w[1] = *reinterpret_cast<const uint4 *>(p + at.hi);
+    } else if (at.hi == at.lo + 4) {
+        r.w[0] = *reinterpret_cast<const uint4 *>(p + at.lo);
+    } else {
+        const uint2 a = *reinterpret_cast<const uint2 *>(p + at.lo), b = *reinterpret_cast<const uint2 *>(p + at.hi);
+        r.w[0] = make_uint4(a.x, a.y, b.x, b.y);
+    }
+}
+template <class T>
+__device__ __forceinline__ void unpack(const Raw8<T> &r, float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            v[4 * i] = __uint_as_float(r.w[i].x);
+            v[4 * i + 1] = __uint_as_float(r.w[i].y);
+            v[4 * i + 2] = __uint_as_float(r.w[i].z);
+            v[4 * i + 3] = __uint_as_float(r.w[i].w);
+        }
+    } else {
+        const uint32_t u[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(u[i] << 16);
+            v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+        }
+    }
+}
+
 // Turns lane li's eight values by the angles of cs (dir = -1: back).
 __device__ __forceinline__ void turn8(float (&v)[8], int li, int rotary, int halves, const float2 *cs,
                                       float dir) {

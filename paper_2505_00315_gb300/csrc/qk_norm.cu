@@ -31,7 +31,8 @@ Turns make_turns(int rotary, double theta) {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 4;       // tokens of one item: loads that a lane keeps in flight
+// Tokens of one item: 64 bytes of loads that a lane keeps in flight while it works on the last.
+constexpr int batch_of(int esize, bool backward) { return (esize == 2 ? 4 : 2) / (backward ? 2 : 1); }
 constexpr int kMaxTokens = 8;   // tokens of one block's step
 
 struct NormArgs {
@@ -50,83 +51,26 @@ struct StepTokens {
     long long in[2][kMaxTokens], y[2][kMaxTokens], d[2][kMaxTokens];   // [queries, keys]
 };
 
-// The queries' (KEY: keys') part of one step: items of `batch` tokens of one head, one a
-// lane group (LG lanes).  acc: backward, this lane's sums of g r x.
-template <class T, bool VEC, bool kBackward, int LG, bool KEY>
-__device__ __forceinline__ void norm_step(const NormArgs &p, const StepTokens &st, int tokens,
-                                          const Part &at, const float (&gamma)[8], float (&acc)[8]) {
-    constexpr int groups = kThreads / LG;
-    const Norm &n = p.n;
-    const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
-    const int heads = KEY ? n.Hkv : n.H;
-    const long long hi = KEY ? n.k.h : n.q.h, hy = KEY ? n.yk.h : n.yq.h, hd = KEY ? n.dk.h : n.dq.h;
-    const int items = (tokens + p.batch - 1) / p.batch * heads;
-    for (int it0 = 0; it0 < items; it0 += groups) {   // (all lanes together: the sums are shuffles)
-        const int it = it0 + grp, bat = it / heads, h = it - bat * heads;
-        const int i0 = bat * p.batch, count = it < items ? min(p.batch, tokens - i0) : 0;
-        const T *in = static_cast<const T *>(KEY ? p.k : p.q) + h * hi;
-        const T *dy = static_cast<const T *>(KEY ? p.dyk : p.dyq) + h * hy;
-        T *out = static_cast<T *>(KEY ? p.ok : p.oq) + h * (kBackward ? hd : hy);
-        const long long *to = kBackward ? st.d[KEY] : st.y[KEY];
-        float x[kBatch][8], g[kBackward ? kBatch : 1][8];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            if (u < count) {
-                load8<T, VEC>(in + st.in[KEY][i0 + u], at, x[u]);
-                if (kBackward) load8<T, VEC>(dy + st.y[KEY][i0 + u], at, g[kBackward ? u : 0]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[u][e] = g[kBackward ? u : 0][e] = 0.f;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            if (u >= p.batch) break;
-            const float2 *cs = st.cs[u < count ? i0 + u : 0];
-            float ss = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fmaf(x[u][e], x[u][e], ss);
-            const float r = rsqrtf(fmaf(group_sum(ss, LG), 1.f / (8 * LG), n.eps));
-            if (!kBackward) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[u][e] *= r * gamma[e];
-                turn8(x[u], li, n.rotary, n.halves, cs, 1.f);
-                if (u < count) store8<T, VEC>(out + to[i0 + u], at, x[u]);
-            } else {
-                float (&gu)[8] = g[kBackward ? u : 0];
-                turn8(gu, li, n.rotary, n.halves, cs, -1.f);
-                float dot = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[u][e] *= r;
-                    acc[e] = fmaf(gu[e], x[u][e], acc[e]);   // (rows past the end hold zeros)
-                    gu[e] *= gamma[e];
-                    dot = fmaf(gu[e], x[u][e], dot);
-                }
-                dot = group_sum(dot, LG) * (1.f / (8 * LG));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) gu[e] = r * fmaf(-x[u][e], dot, gu[e]);
-                if (u < count) store8<T, VEC>(out + to[i0 + u], at, gu);
-            }
-        }
-    }
-}
-
 template <class T, bool VEC, bool kBackward, int LG>
-__global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_constant__ NormArgs p,
+__global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kernel(const __grid_constant__ NormArgs p,
                                                                 const __grid_constant__ Turns tab) {
     constexpr int groups = kThreads / LG, hp = 8 * LG;
+    constexpr int kBatch = batch_of(sizeof(T), kBackward);
     __shared__ StepTokens st;
+    __shared__ float gamma[2][hp];
     extern __shared__ float red[];   // backward: [groups][2][hp]
     const Norm &n = p.n;
     const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
     const Part at(li, n.rotary, n.halves);
     const long long N = (long long)n.B * n.T;
-    float gq[8], gk[8], aq[8], ak[8];
+    for (int e = threadIdx.x; e < 2 * hp; e += kThreads) {
+        const T *g = static_cast<const T *>(e < hp ? p.gq : p.gk);
+        gamma[e / hp][e % hp] = g == nullptr ? 1.f : to_f32(g[e % hp]);
+    }
+    float acc[2][8];   // backward: this lane's sums of g r x, of queries and keys
 #pragma unroll
-    for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 1.f, aq[e] = ak[e] = 0.f;
-    if (p.gq != nullptr) load8<T, false>((const T *)p.gq, at, gq);
-    if (p.gk != nullptr) load8<T, false>((const T *)p.gk, at, gk);
+    for (int e = 0; e < 8; ++e) acc[0][e] = acc[1][e] = 0.f;
+    const int HH = n.H + n.Hkv;   // heads 0 .. H-1 are queries, the others keys
     const int pairs = n.rotary >> 1;
     for (long long tok0 = (long long)blockIdx.x * p.step; tok0 < N; tok0 += (long long)gridDim.x * p.step) {
         const int tokens = (int)min((long long)p.step, N - tok0);
@@ -142,6 +86,74 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_con
             st.d[0][threadIdx.x] = n.dq.at(b, t, 0);
             st.d[1][threadIdx.x] = n.dk.at(b, t, 0);
         }
+        __syncthreads();
+        // items of `batch` tokens of one head, one a lane group; the next item's loads are under way
+        // while one is worked on
+        const int items = (tokens + p.batch - 1) / p.batch * HH;
+        Raw8<T> x[2][kBatch], dy[2][kBackward ? kBatch : 1];
+        struct Item {
+            int key, h, i0, count;
+        };
+        auto item = [&](int it) {
+            const int bat = it / HH, hh = it - bat * HH, i0 = bat * p.batch;
+            const int key = hh >= n.H;
+            return Item{key, key ? hh - n.H : hh, i0, it < items ? min(p.batch, tokens - i0) : 0};
+        };
+        auto load = [&](const Item &w, Raw8<T> (&xr)[kBatch], Raw8<T> (&yr)[kBackward ? kBatch : 1]) {
+            const T *in = static_cast<const T *>(w.key ? p.k : p.q) + w.h * (w.key ? n.k.h : n.q.h);
+            const T *gr = static_cast<const T *>(w.key ? p.dyk : p.dyq) + w.h * (w.key ? n.yk.h : n.yq.h);
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if (u < w.count) {
+                    load_raw<T, VEC>(in + st.in[w.key][w.i0 + u], at, xr[u]);
+                    if (kBackward) load_raw<T, VEC>(gr + st.y[w.key][w.i0 + u], at, yr[kBackward ? u : 0]);
+                }
+            }
+        };
+        auto work = [&](const Item &w, Raw8<T> (&xr)[kBatch], Raw8<T> (&yr)[kBackward ? kBatch : 1]) {
+            T *out = static_cast<T *>(w.key ? p.ok : p.oq) +
+                     w.h * (kBackward ? (w.key ? n.dk.h : n.dq.h) : (w.key ? n.yk.h : n.yq.h));
+            const float4 ga = *reinterpret_cast<const float4 *>(&gamma[w.key][at.lo]);
+            const float4 gb = *reinterpret_cast<const float4 *>(&gamma[w.key][at.hi]);
+            const float gm[8] = {ga.x, ga.y, ga.z, ga.w, gb.x, gb.y, gb.z, gb.w};
+            const float isq = w.key ? 0.f : 1.f, isk = w.key ? 1.f : 0.f;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if (u >= p.batch) break;
+                const bool on = u < w.count;
+                const float2 *cs = st.cs[on ? w.i0 + u : 0];
+                float v[8], ss = 0.f;
+                unpack<T>(xr[u], v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], ss);
+                const float r = rsqrtf(fmaf(group_sum(ss, LG), 1.f / hp, n.eps));
+                if (!kBackward) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= r * gm[e];
+                    turn8(v, li, n.rotary, n.halves, cs, 1.f);
+                    if (on) store8<T, VEC>(out + st.y[w.key][w.i0 + u], at, v);
+                } else {
+                    float g[8], dot = 0.f;
+                    unpack<T>(yr[kBackward ? u : 0], g);
+                    turn8(g, li, n.rotary, n.halves, cs, -1.f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] *= r;
+                        const float d = on ? g[e] * v[e] : 0.f;
+                        acc[0][e] = fmaf(d, isq, acc[0][e]);
+                        acc[1][e] = fmaf(d, isk, acc[1][e]);
+                        g[e] *= gm[e];
+                        dot = fmaf(g[e], v[e], dot);
+                    }
+                    dot = group_sum(dot, LG) * (1.f / hp);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) g[e] = r * fmaf(-v[e], dot, g[e]);
+                    if (on) store8<T, VEC>(out + st.d[w.key][w.i0 + u], at, g);
+                }
+            }
+        };
+        Item cur = item(grp);
+        load(cur, x[0], dy[0]);
         for (int e = threadIdx.x; e < tokens * pairs; e += kThreads) {
             const int i = e / pairs, a = e - i * pairs;
             int t = t0 + i;
@@ -149,15 +161,22 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const __grid_con
             st.cs[i][a] = angle_of(tab.phi[a], p.pos != nullptr ? p.pos[tok0 + i] : t);
         }
         __syncthreads();
-        norm_step<T, VEC, kBackward, LG, false>(p, st, tokens, at, gq, aq);
-        norm_step<T, VEC, kBackward, LG, true>(p, st, tokens, at, gk, ak);
+        for (int it0 = 0; it0 < items; it0 += 2 * groups) {   // (all lanes together: the sums are shuffles)
+            Item next = item(it0 + groups + grp);
+            load(next, x[1], dy[1]);
+            work(cur, x[0], dy[0]);
+            if (it0 + groups >= items) break;
+            cur = item(it0 + 2 * groups + grp);
+            load(cur, x[0], dy[0]);
+            work(next, x[1], dy[1]);
+        }
     }
     if (kBackward && p.partial != nullptr) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int c = e < 4 ? at.lo + e : at.hi + e - 4;
-            red[(grp * 2 + 0) * hp + c] = aq[e];
-            red[(grp * 2 + 1) * hp + c] = ak[e];
+            red[(grp * 2 + 0) * hp + c] = acc[0][e];
+            red[(grp * 2 + 1) * hp + c] = acc[1][e];
         }
         __syncthreads();
         for (int o = threadIdx.x; o < 2 * hp; o += kThreads) {
@@ -227,7 +246,7 @@ size_t norm_workspace(const Norm &n) { return (size_t)bwd_blocks(n) * 2 * n.hp *
 cudaError_t launch_norm(const Norm &n, const void *q, const void *k, const void *gq, const void *gk,
                         const int32_t *pos, void *yq, void *yk, cudaStream_t s) {
     NormArgs p{n, q, k, gq, gk, nullptr, nullptr, yq, yk, pos, nullptr, many(n) ? kMaxTokens : 1,
-               many(n) ? kBatch : 1};
+               many(n) ? batch_of(n.bf16 ? 2 : 4, false) : 1};
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) && rows16(yq, n.yq, n.bf16) &&
                      rows16(yk, n.yk, n.bf16);
     const long long N = (long long)n.B * n.T;
@@ -239,7 +258,7 @@ cudaError_t launch_norm_bwd(const Norm &n, const void *q, const void *k, const v
                             void *dq, void *dk, float *dgq, float *dgk, void *ws, cudaStream_t s) {
     const bool sums = dgq != nullptr || dgk != nullptr;
     NormArgs p{n, q, k, gq, gk, dyq, dyk, dq, dk, pos, sums ? (float *)ws : nullptr,
-               many(n) ? kMaxTokens : 1, many(n) ? kBatch : 1};
+               many(n) ? kMaxTokens : 1, many(n) ? batch_of(n.bf16 ? 2 : 4, true) : 1};
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) &&
                      rows16(dyq, n.yq, n.bf16) && rows16(dyk, n.yk, n.bf16) &&
                      rows16(dq, n.dq, n.bf16) && rows16(dk, n.dk, n.bf16);
