@@ -24,10 +24,9 @@ __all__ += _WINDOW
 
 
 def __getattr__(name):
-    if name in _WINDOW:
-        from . import _window
-        return getattr(_window, name)
     if name in __all__:
-        from . import _binding
-        return getattr(_binding, name)
+        from . import _binding, _window
+        value = getattr(_window if name in _WINDOW else _binding, name)
+        globals()[name] = value   # found at once the next time
+        return value
     raise AttributeError(name)

@@ -5,7 +5,6 @@ with any strides whose last is 1."""
 from __future__ import annotations
 
 import ctypes
-import functools
 
 from . import _binding as _b
 
@@ -57,46 +56,77 @@ def declare(L) -> None:
         f.argtypes, f.restype = args, res
 
 
-def _at(t, name, dtype=None) -> int:
-    """The device address of a strided tensor, checked."""
-    if not isinstance(t, _b._torch_mod.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
+# A call's host time is mostly this marshalling, so what depends on shapes, strides and types alone
+# (the checks and the library's struct) is done once for each set of them and kept as a plan; a
+# later call looks it up (1 us) and passes addresses (mosa_window_forward 20.6 -> 12.5 us).
+_plans: dict = {}
+
+
+def _plan(key, make):
+    plan = _plans.get(key)
+    if plan is None:
+        plan = make()
+        if len(_plans) >= 512:
+            _plans.clear()
+        _plans[key] = plan
+    return plan
+
+
+def _of(*tensors):
+    """Shapes, strides and types of the tensors (None for None), as a key."""
+    key = []
+    for t in tensors:
+        if t is None:
+            key.append(None)
+        else:
+            key += (t.shape, t.stride(), t.dtype)
+    return tuple(key)
+
+
+def _key(*tensors):
+    try:
+        return _of(*tensors)
+    except AttributeError:
+        raise TypeError("every tensor argument must be a torch.Tensor") from None
+
+
+def _at(t, name) -> int:
+    """The device address of a tensor whose shape, strides and type a plan has checked."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor (libmosa runs on the GPU only)")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     return t.data_ptr()
 
 
-def _heads(t, name, like=None):
-    """Strides of a tensor whose last dimension is contiguous, its shape ``like``'s."""
+def _heads(t, name, like=None, dtype=None):
+    """Strides (but the last, 1) of a tensor of heads, its shape ``like`` and type checked."""
     if like is not None and t.shape != like:
         raise ValueError(f"{name} must have shape {tuple(like)}, got {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must have the storage dtype {dtype}, got {t.dtype}")
     s = t.stride()
     if s[-1] != 1 and t.shape[-1] != 1:
         raise ValueError(f"{name}: the values of a head must be contiguous")
-    return s[:-1]
+    return MosaStrides(*s[:-1])
 
 
-def _new(t, out, name, shape=None, dtype=None):
-    """out[name], or a new contiguous tensor of t's shape and dtype."""
-    o = out.get(name) if out else None
-    if o is None:
-        torch = _b._torch_mod
-        o = torch.empty(t.shape if shape is None else shape, dtype=dtype or t.dtype, device=t.device)
-    return o
+def _packed(shape):
+    """Strides of a new contiguous tensor of that shape."""
+    return MosaStrides(shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3])
 
 
-def _space(fn, ref, name, workspace, device):
-    """The workspace's address and size, a new one where none is given."""
-    if workspace is None:
-        n = int(fn(ref))
-        if n == 0:
-            raise _b.MosaError(_b.MOSA_ERR_INVALID_ARG, name)
-        torch = _b._torch_mod
-        # zeroed: the status word of a window call's workspace is read before any call clears it
-        workspace = torch.zeros(n, dtype=torch.uint8, device=device)
-    return workspace
+def _out(t, name, like, dtype):
+    """Strides of a result: a given tensor's, or those of the one to be made."""
+    return _packed(like) if t is None else _heads(t, name, like, dtype)
+
+
+def _vector(t, name, shape, dtype):
+    """A contiguous tensor of exactly that shape and type, or None."""
+    if t is not None:
+        _b._want(name, t, shape)
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
 
 
 def _rank(t, name, n):
@@ -104,34 +134,43 @@ def _rank(t, name, n):
         raise ValueError(f"{name} must have {n} dimensions, got {tuple(t.shape)}")
 
 
+def _space(workspace, need, name, device):
+    """The given workspace, or a new one."""
+    if workspace is not None:
+        _b._dev(workspace, "workspace", _b._torch_mod.uint8)
+        return workspace
+    if need == 0:
+        raise _b.MosaError(_b.MOSA_ERR_INVALID_ARG, name)
+    # zeroed: the status word of a window call's workspace is read before any call clears it
+    return _b._torch_mod.zeros(need, dtype=_b._torch_mod.uint8, device=device)
+
+
 # ------------------------------------------------------ norm and rotation
 
-@functools.lru_cache(maxsize=512)
-def _qk_shape(sizes, theta, eps, *strides):
-    s = MosaQkShape(*sizes, theta, eps, *[MosaStrides(*x) for x in strides])
-    return s, ctypes.byref(s)
-
-
-def _qk(q, k, gamma_q, gamma_k, positions, rotary, halves):
-    torch = _b._torch()
+def _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps, halves, yq, yk, dq=None, dk=None,
+             dgamma_q=None, dgamma_k=None, backward=False):
+    torch = _b._torch_mod
     _rank(q, "q", 4)
     _rank(k, "k", 4)
     B, T, H, hp = q.shape
     Hkv = k.shape[2]
     if k.shape != (B, T, Hkv, hp):
         raise ValueError(f"k must be [B, T, Hkv, hp] with q's B, T and hp, got {tuple(k.shape)}")
-    _b._same(q, ("k", k))
-    ptrs = [None, None, None]
-    for i, (n, g) in enumerate((("gamma_q", gamma_q), ("gamma_k", gamma_k))):
-        if g is not None:
-            _b._want(n, g, (hp,))
-            ptrs[i] = _b._dev(g, n, q.dtype)
-    if positions is not None:
-        _b._want("positions", positions, (B, T))
-        ptrs[2] = _b._dev(positions, "positions", torch.int32)
-    sizes = (B, T, H, Hkv, hp, _b._dtype_code(q), hp // 2 if rotary is None else int(rotary),
-             1 if halves else 0)
-    return sizes, ptrs
+    dt = q.dtype
+    _vector(gamma_q, "gamma_q", (hp,), dt)
+    _vector(gamma_k, "gamma_k", (hp,), dt)
+    _vector(positions, "positions", (B, T), torch.int32)
+    _vector(dgamma_q, "dgamma_q", (hp,), torch.float32)
+    _vector(dgamma_k, "dgamma_k", (hp,), torch.float32)
+    y = ("dyq", "dyk") if backward else ("out q", "out k")
+    s = MosaQkShape(B, T, H, Hkv, hp, _b._dtype_code(q), hp // 2 if rotary is None else int(rotary),
+                    1 if halves else 0, theta, eps, _heads(q, "q"), _heads(k, "k", None, dt),
+                    _out(yq, y[0], q.shape, dt), _out(yk, y[1], k.shape, dt))
+    need = 0
+    if backward:
+        s.dq, s.dk = _out(dq, "dq", q.shape, dt), _out(dk, "dk", k.shape, dt)
+        need = int(_b.load().mosa_qk_norm_rope_workspace_bytes(ctypes.byref(s)))
+    return ctypes.byref(s), need, s
 
 
 def mosa_qk_norm_rope(q, k, gamma_q=None, gamma_k=None, positions=None, rotary=None,
@@ -142,14 +181,20 @@ def mosa_qk_norm_rope(q, k, gamma_q=None, gamma_k=None, positions=None, rotary=N
     ``rotary`` dimensions (hp/2 by default) by t * theta^(-2p/rotary), neighbours or, with
     ``halves``, (p, p + rotary/2).  Returns (yq, yk); ``out`` may hold "q" and "k" to write
     to, q and k themselves among them."""
-    sizes, (gq, gk, pos) = _qk(q, k, gamma_q, gamma_k, positions, rotary, halves)
-    yq, yk = _new(q, out, "q"), _new(k, out, "k")
-    sq, sk = _heads(q, "q"), _heads(k, "k")
-    s, ref = _qk_shape(sizes, theta, eps, sq, sk, _heads(yq, "out q", q.shape),
-                       _heads(yk, "out k", k.shape), (), ())
-    dt = q.dtype
-    rc = _b.load().mosa_qk_norm_rope(ref, _at(q, "q"), _at(k, "k"), gq, gk, pos,
-                                     _at(yq, "out q", dt), _at(yk, "out k", dt), _b._stream(stream))
+    torch = _b._torch()
+    yq, yk = (out.get("q"), out.get("k")) if out else (None, None)
+    key = ("norm", rotary, theta, eps, halves) + _key(q, k, gamma_q, gamma_k, positions, yq, yk)
+    ref = _plan(key, lambda: _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps, halves,
+                                      yq, yk))[0]
+    if yq is None:
+        yq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if yk is None:
+        yk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    rc = _b.load().mosa_qk_norm_rope(
+        ref, _at(q, "q"), _at(k, "k"), None if gamma_q is None else _at(gamma_q, "gamma_q"),
+        None if gamma_k is None else _at(gamma_k, "gamma_k"),
+        None if positions is None else _at(positions, "positions"), _at(yq, "out q"),
+        _at(yk, "out k"), _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_qk_norm_rope")
     return yq, yk
@@ -161,52 +206,57 @@ def mosa_qk_norm_rope_backward(q, k, gamma_q, gamma_k, dyq, dyk, positions=None,
     """Gradients of mosa_qk_norm_rope from its inputs and the gradients of its outputs.
     Returns ({"dq", "dk", "dgamma_q", "dgamma_k"}, workspace); dgamma_* are fp32 [hp].
     ``out`` may hold any of them ("dq" and "dk" may be dyq and dyk)."""
-    sizes, (gq, gk, pos) = _qk(q, k, gamma_q, gamma_k, positions, rotary, halves)
-    _b._same(q, ("dyq", dyq), ("dyk", dyk))
-    f32 = _b._torch_mod.float32
-    g = {"dq": _new(q, out, "dq"), "dk": _new(k, out, "dk")}
-    for n in ("dgamma_q", "dgamma_k"):
-        g[n] = _new(q, out, n, (q.shape[3],), f32)
-        _b._want(n, g[n], (q.shape[3],))
-    s, ref = _qk_shape(sizes, theta, eps, _heads(q, "q"), _heads(k, "k"),
-                       _heads(dyq, "dyq", q.shape), _heads(dyk, "dyk", k.shape),
-                       _heads(g["dq"], "dq", q.shape), _heads(g["dk"], "dk", k.shape))
-    L = _b.load()
-    workspace = _space(L.mosa_qk_norm_rope_workspace_bytes, ref, "mosa_qk_norm_rope_backward",
-                       workspace, q.device)
-    dt = q.dtype
-    rc = L.mosa_qk_norm_rope_backward(
-        ref, _at(q, "q"), _at(k, "k"), gq, gk, pos, _at(dyq, "dyq"), _at(dyk, "dyk"),
-        _at(g["dq"], "dq", dt), _at(g["dk"], "dk", dt), _b._dev(g["dgamma_q"], "dgamma_q", f32),
-        _b._dev(g["dgamma_k"], "dgamma_k", f32), _b._dev(workspace, "workspace"),
-        workspace.numel(), _b._stream(stream))
+    torch = _b._torch()
+    o = out or {}
+    dq, dk, dgq, dgk = (o.get(n) for n in ("dq", "dk", "dgamma_q", "dgamma_k"))
+    if dyq is None or dyk is None:
+        raise TypeError("dyq and dyk must be torch.Tensors")
+    key = ("norm_backward", rotary, theta, eps, halves) + _key(q, k, gamma_q, gamma_k, positions, dyq,
+                                                               dyk, dq, dk, dgq, dgk)
+    ref, need, _ = _plan(key, lambda: _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps,
+                                               halves, dyq, dyk, dq, dk, dgq, dgk, True))
+    dev, f32 = q.device, torch.float32
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=k.dtype, device=dev)
+    if dgq is None:
+        dgq = torch.empty(q.shape[3], dtype=f32, device=dev)
+    if dgk is None:
+        dgk = torch.empty(q.shape[3], dtype=f32, device=dev)
+    workspace = _space(workspace, need, "mosa_qk_norm_rope_backward", dev)
+    rc = _b.load().mosa_qk_norm_rope_backward(
+        ref, _at(q, "q"), _at(k, "k"), None if gamma_q is None else _at(gamma_q, "gamma_q"),
+        None if gamma_k is None else _at(gamma_k, "gamma_k"),
+        None if positions is None else _at(positions, "positions"), _at(dyq, "dyq"), _at(dyk, "dyk"),
+        _at(dq, "dq"), _at(dk, "dk"), _at(dgq, "dgamma_q"), _at(dgk, "dgamma_k"),
+        workspace.data_ptr(), workspace.numel(), _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_qk_norm_rope_backward")
-    return g, workspace
+    return {"dq": dq, "dk": dk, "dgamma_q": dgq, "dgamma_k": dgk}, workspace
 
 
 # --------------------------------------------------------- window attention
 
-@functools.lru_cache(maxsize=512)
-def _window_shape(sizes, scale, *strides):
-    s = MosaWindowShape(*sizes, scale, *[MosaStrides(*x) for x in strides])
-    return s, ctypes.byref(s)
-
-
-def _window(q, k, v, window, sinks, lens):
-    torch = _b._torch()
+def _window_plan(q, k, v, O, lse, lens, window, sinks, scale, dO=None, dq=None, dk=None, dv=None):
+    torch = _b._torch_mod
     _rank(q, "q", 4)
     _rank(k, "k", 4)
     B, Tq, H, hp = q.shape
     Tk, Hkv = k.shape[1], k.shape[2]
     if k.shape != (B, Tk, Hkv, hp):
         raise ValueError(f"k must be [B, Tk, Hkv, hp] with q's B and hp, got {tuple(k.shape)}")
-    _b._same(q, ("k", k), ("v", v))
-    n = None
-    if lens is not None:
-        _b._want("lens", lens, (B,))
-        n = _b._dev(lens, "lens", torch.int32)
-    return (B, Tq, Tk, H, Hkv, hp, _b._dtype_code(q), int(window), int(sinks)), n
+    dt = q.dtype
+    _vector(lens, "lens", (B,), torch.int32)
+    _vector(lse, "lse", (B, H, Tq), torch.float32)
+    s = MosaWindowShape(B, Tq, Tk, H, Hkv, hp, _b._dtype_code(q), int(window), int(sinks), scale,
+                        _heads(q, "q"), _heads(k, "k", None, dt), _heads(v, "v", k.shape, dt),
+                        _out(O, "O", q.shape, dt))
+    if dO is not None:
+        s.go = _heads(dO, "dO", q.shape, dt)
+        s.dq, s.dk, s.dv = (_out(dq, "dq", q.shape, dt), _out(dk, "dk", k.shape, dt),
+                            _out(dv, "dv", k.shape, dt))
+    return ctypes.byref(s), int(_b.load().mosa_window_workspace_bytes(ctypes.byref(s))), s
 
 
 def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: float = 0.0,
@@ -216,24 +266,23 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
     first ``sinks``, below its sequence's length (lens [B] int32, Tk by default).
     scale = 0 is 1/sqrt(hp).  Returns (O, lse, workspace): O like q, lse [B,H,Tq] fp32, or
     None without ``want_lse`` (where no backward follows).  ``out`` may hold "O" and "lse"."""
-    sizes, n = _window(q, k, v, window, sinks, lens)
-    B, Tq, Tk, H = sizes[:4]
-    f32 = _b._torch_mod.float32
-    O = _new(q, out, "O")
-    lse = _new(q, out, "lse", (B, H, Tq), f32) if want_lse else None
-    _b._want("lse", lse, (B, H, Tq))
-    s, ref = _window_shape(sizes, scale, _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k.shape),
-                           _heads(O, "O", q.shape))
-    L = _b.load()
-    workspace = _space(L.mosa_window_workspace_bytes, ref, "mosa_window_forward", workspace, q.device)
-    rc = L.mosa_window_forward(ref, _at(q, "q"), _at(k, "k"), _at(v, "v"), n,
-                               _at(O, "O", q.dtype),
-                               None if lse is None else _b._dev(lse, "lse", f32),
-                               _b._dev(workspace, "workspace"), workspace.numel(),
-                               _b._stream(stream))
+    torch = _b._torch()
+    O, lse = (out.get("O"), out.get("lse")) if out else (None, None)
+    key = ("window", window, sinks, scale) + _key(q, k, v, O, lse, lens)
+    ref, need, _ = _plan(key, lambda: _window_plan(q, k, v, O, lse, lens, window, sinks, scale))
+    dev = q.device
+    if O is None:
+        O = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if lse is None and want_lse:
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=dev)
+    workspace = _space(workspace, need, "mosa_window_forward", dev)
+    rc = _b.load().mosa_window_forward(
+        ref, _at(q, "q"), _at(k, "k"), _at(v, "v"), None if lens is None else _at(lens, "lens"),
+        _at(O, "O"), _at(lse, "lse") if want_lse else None, workspace.data_ptr(), workspace.numel(),
+        _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_window_forward")
-    return O, lse, workspace
+    return O, lse if want_lse else None, workspace
 
 
 def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int = 0, lens=None,
@@ -241,24 +290,29 @@ def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int
     """Gradients of mosa_window_forward, given its outputs and its workspace: a dict with dq, dk
     and dv like q, k and v, dk and dv summed over the query heads that share them.  ``out`` may
     hold any of them."""
-    sizes, n = _window(q, k, v, window, sinks, lens)
-    B, Tq, Tk, H = sizes[:4]
-    _b._same(q, ("O", O), ("dO", dO))
-    f32 = _b._torch_mod.float32
-    _b._want("lse", lse, (B, H, Tq))
-    g = {"dq": _new(q, out, "dq"), "dk": _new(k, out, "dk"), "dv": _new(v, out, "dv")}
-    s, ref = _window_shape(sizes, scale, _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k.shape),
-                           _heads(O, "O", q.shape), _heads(dO, "dO", q.shape),
-                           _heads(g["dq"], "dq", q.shape), _heads(g["dk"], "dk", k.shape),
-                           _heads(g["dv"], "dv", k.shape))
-    dt = q.dtype
+    torch = _b._torch()
+    o = out or {}
+    dq, dk, dv = o.get("dq"), o.get("dk"), o.get("dv")
+    if O is None or lse is None or dO is None or workspace is None:
+        raise TypeError("O, lse, dO and workspace must be torch.Tensors")
+    key = ("window_backward", window, sinks, scale) + _key(q, k, v, O, lse, lens, dO, dq, dk, dv)
+    ref = _plan(key, lambda: _window_plan(q, k, v, O, lse, lens, window, sinks, scale, dO, dq, dk,
+                                          dv))[0]
+    dev = q.device
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=k.dtype, device=dev)
+    if dv is None:
+        dv = torch.empty(k.shape, dtype=k.dtype, device=dev)
+    _space(workspace, 0, "mosa_window_backward", dev)
     rc = _b.load().mosa_window_backward(
-        ref, _at(q, "q"), _at(k, "k"), _at(v, "v"), n, _at(O, "O"), _b._dev(lse, "lse", f32),
-        _at(dO, "dO"), _at(g["dq"], "dq", dt), _at(g["dk"], "dk", dt), _at(g["dv"], "dv", dt),
-        _b._dev(workspace, "workspace"), workspace.numel(), _b._stream(stream))
+        ref, _at(q, "q"), _at(k, "k"), _at(v, "v"), None if lens is None else _at(lens, "lens"),
+        _at(O, "O"), _at(lse, "lse"), _at(dO, "dO"), _at(dq, "dq"), _at(dk, "dk"), _at(dv, "dv"),
+        workspace.data_ptr(), workspace.numel(), _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_window_backward")
-    return g
+    return {"dq": dq, "dk": dk, "dv": dv}
 
 
 def mosa_window_check_status(workspace, stream=None) -> int:
@@ -270,16 +324,34 @@ def mosa_window_check_status(workspace, stream=None) -> int:
 
 # ------------------------------------------------------------------- decode
 
-@functools.lru_cache(maxsize=512)
-def _decode_shape(sizes, scale, theta, eps, *strides):
-    s = MosaDecodeShape(*sizes, scale, theta, eps, *[MosaStrides(*x) for x in strides])
-    return s, ctypes.byref(s)
+def _bh(t, name, like, dtype):
+    """Strides (b, -, h) of a tensor [B, heads, hp]."""
+    if t is None:
+        return MosaStrides(like[1] * like[2], 0, like[2])
+    if t.shape != like:
+        raise ValueError(f"{name} must have shape {tuple(like)}, got {tuple(t.shape)}")
+    s = _heads(t[:, None], name, None, dtype)
+    return MosaStrides(s.b, 0, s.h)
 
 
-def _bh(t, name, like):
-    """Strides (b, 0, h) of a tensor [B, heads, hp]."""
-    s = _heads(t, name, like)
-    return s[0], 0, s[1]
+def _decode_plan(q, k, v, Kc, Vc, lens, O, gamma_q, gamma_k, window, sinks, norm, rotary, theta, eps,
+                 halves, scale):
+    for name, t, n in (("q", q, 3), ("k", k, 3), ("K_cache", Kc, 4)):
+        _rank(t, name, n)
+    B, H, hp = q.shape
+    Hkv, C = k.shape[1], Kc.shape[1]
+    kv, cache, dt = (B, Hkv, hp), (B, C, Hkv, hp), q.dtype
+    _b._want("lens", lens, (B,))
+    _vector(gamma_q, "gamma_q", (hp,), dt)
+    _vector(gamma_k, "gamma_k", (hp,), dt)
+    strides = (_bh(q, "q", q.shape, dt), _bh(k, "k", kv, dt), _bh(v, "v", kv, dt),
+               _bh(O, "O", q.shape, dt), _heads(Kc, "K_cache", cache, dt),
+               _heads(Vc, "V_cache", cache, dt))
+    _vector(lens, "lens", (B,), _b._torch_mod.int32)
+    s = MosaDecodeShape(B, C, H, Hkv, hp, _b._dtype_code(q), int(window), int(sinks),
+                        1 if norm else 0, hp // 2 if rotary is None else int(rotary),
+                        1 if halves else 0, scale, theta, eps, *strides)
+    return ctypes.byref(s), int(_b.load().mosa_window_decode_workspace_bytes(ctypes.byref(s))), s
 
 
 def mosa_window_decode(q, k, v, K_cache, V_cache, lens, window: int, sinks: int = 0, gamma_q=None,
@@ -292,31 +364,23 @@ def mosa_window_decode(q, k, v, K_cache, V_cache, lens, window: int, sinks: int 
     (t - sinks) % (C - sinks)), and q attends over the visible tokens.  lens [B] int32 counts
     the new token; 0 skips a sequence.  Returns (O [B,H,hp], workspace)."""
     torch = _b._torch()
-    for name, t, n in (("q", q, 3), ("k", k, 3), ("K_cache", K_cache, 4)):
-        _rank(t, name, n)
-    B, H, hp = q.shape
-    Hkv, C = k.shape[1], K_cache.shape[1]
-    kv, cache, dt = (B, Hkv, hp), (B, C, Hkv, hp), q.dtype
-    _b._want("lens", lens, (B,))
-    ptrs = [None, None]
-    for i, (n, g) in enumerate((("gamma_q", gamma_q), ("gamma_k", gamma_k))):
-        if g is not None:
-            _b._want(n, g, (hp,))
-            ptrs[i] = _b._dev(g, n, dt)
-    O = _new(q, out, "O")
-    s, ref = _decode_shape(
-        (B, C, H, Hkv, hp, _b._dtype_code(q), int(window), int(sinks), 1 if norm else 0,
-         hp // 2 if rotary is None else int(rotary), 1 if halves else 0), scale, theta, eps,
-        _bh(q, "q", q.shape), _bh(k, "k", kv), _bh(v, "v", kv), _bh(O, "O", q.shape),
-        _heads(K_cache, "K_cache", cache), _heads(V_cache, "V_cache", cache))
-    L = _b.load()
-    workspace = _space(L.mosa_window_decode_workspace_bytes, ref, "mosa_window_decode", workspace,
-                       q.device)
-    rc = L.mosa_window_decode(ref, _at(q, "q"), _at(k, "k", dt), _at(v, "v", dt), *ptrs,
-                              _b._dev(lens, "lens", torch.int32), _at(K_cache, "K_cache", dt),
-                              _at(V_cache, "V_cache", dt), _at(O, "O", dt),
-                              _b._dev(workspace, "workspace"), workspace.numel(),
-                              _b._stream(stream))
+    O = out.get("O") if out else None
+    if lens is None:
+        raise TypeError("lens must be a torch.Tensor")
+    key = (("decode", window, sinks, norm, rotary, theta, eps, halves, scale)
+           + _key(q, k, v, K_cache, V_cache, lens, O, gamma_q, gamma_k))
+    ref, need, _ = _plan(key, lambda: _decode_plan(q, k, v, K_cache, V_cache, lens, O, gamma_q, gamma_k,
+                                                   window, sinks, norm, rotary, theta, eps, halves,
+                                                   scale))
+    if O is None:
+        O = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    workspace = _space(workspace, need, "mosa_window_decode", q.device)
+    rc = _b.load().mosa_window_decode(
+        ref, _at(q, "q"), _at(k, "k"), _at(v, "v"),
+        None if gamma_q is None else _at(gamma_q, "gamma_q"),
+        None if gamma_k is None else _at(gamma_k, "gamma_k"), _at(lens, "lens"),
+        _at(K_cache, "K_cache"), _at(V_cache, "V_cache"), _at(O, "O"), workspace.data_ptr(),
+        workspace.numel(), _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_window_decode")
     return O, workspace
