@@ -51,6 +51,8 @@ struct Decode {
     Str q, k, v, o, kc, vc;
 };
 
+constexpr int kTcTile = 128;   // queries and keys of a tile on the tensor cores
+
 // True when every row of the tensor starts at a multiple of 16 bytes.
 inline bool rows16(const void *p, const Str &s, bool bf16) {
     const long long per = bf16 ? 8 : 4;
@@ -74,7 +76,12 @@ cudaError_t simt_window_fwd(const Attn &a, const void *q, const void *k, const v
                             const int32_t *lens, void *O, float *lse, bf16 *rest, cudaStream_t s);
 cudaError_t simt_window_bwd(const Attn &a, const void *q, const void *k, const void *v,
                             const int32_t *lens, const float *lse, const void *dO,
-                            const float *delta, void *dq, void *dk, void *dv, cudaStream_t s);
+                            const float *delta, void *dq, void *dk, void *dv, float *partial,
+                            cudaStream_t s);
+// Bytes of the backward's `partial`, and dk and dv of the sink rows from it (window_tiles.cuh).
+size_t window_bwd_bytes(const Attn &a);
+cudaError_t add_sink_rows(const Attn &a, const float *partial, int extra, void *dk, void *dv,
+                          cudaStream_t s);
 // delta[b,h,i] = sum over the head of dO o (O + rest), in fp32.
 cudaError_t window_delta(const Attn &a, const void *O, const bf16 *rest, const void *dO, float *delta,
                          cudaStream_t s);
@@ -86,8 +93,6 @@ bool tc_window_fwd(const Attn &a, const void *q, const void *k, const void *v, c
 bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
                    const float *lse, const void *dO, const float *delta, void *dq, void *dk, void *dv,
                    float *partial, uint32_t *status, cudaStream_t s, cudaError_t *err);
-// Bytes of its `partial`.
-size_t tc_window_bwd_bytes(const Attn &a);
 
 size_t decode_workspace(const Decode &d);
 cudaError_t launch_decode(const Decode &d, const void *q, const void *k, const void *v,

@@ -154,7 +154,7 @@ size_t partial_at(const Attn &a) {
     return rest_at(a) + (a.bf16 ? ((size_t)a.B * a.H * a.Tq * a.hp * 2 + 255) / 256 * 256 : 0);
 }
 size_t window_bytes(const Attn &a) {
-    return partial_at(a) + (a.bf16 ? tc_window_bwd_bytes(a) : 0);
+    return partial_at(a) + window_bwd_bytes(a);
 }
 
 }  // namespace
@@ -243,7 +243,7 @@ mosa_status mosa_window_backward(const mosa_window_shape *shape, const void *q, 
     if (tensor_cores() && tc_window_bwd(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, partial,
                                         (uint32_t *)workspace, s, &e))
         return of(e);
-    return of(simt_window_bwd(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, s));
+    return of(simt_window_bwd(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, partial, s));
 }
 
 mosa_status mosa_window_check_status(void *workspace, void *stream) {

@@ -10,6 +10,8 @@
 // thread, operands as fp32 in shared memory, the softmax's running maximum and
 // sum in registers.  The backward takes one kernel by key tiles (dk, dv) and one by
 // query tiles (dq), so that every sum runs in one thread in a fixed order.
+#include <algorithm>
+
 #include "launch.h"
 #include "profile.h"
 #include "window_tiles.cuh"
@@ -27,6 +29,8 @@ template <class T>
 struct Ptrs {
     const T *q, *k, *v, *dO;
     T *o, *dq, *dk, *dv;
+    float *partial;
+    SinkSplit sinks;
     const int32_t *lens;
     float *lse;
     bf16 *rest;
@@ -118,8 +122,19 @@ __device__ __forceinline__ void add_weighted(const float *W, const float *X, int
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             float x[CW];
+            const float *row = X + (j + u) * (HD + 4);
+            if constexpr (CW >= 4) {
 #pragma unroll
-            for (int c = 0; c < CW; ++c) x[c] = X[(j + u) * (HD + 4) + col_of<HD>(tx, c)];
+                for (int c = 0; c < CW; c += 4) {
+                    const float4 t = *reinterpret_cast<const float4 *>(row + (c >> 2) * 64 + tx * 4);
+                    x[c] = t.x; x[c + 1] = t.y; x[c + 2] = t.z; x[c + 3] = t.w;
+                }
+            } else if constexpr (CW == 2) {
+                const float2 t = *reinterpret_cast<const float2 *>(row + tx * 2);
+                x[0] = t.x; x[1] = t.y;
+            } else {
+                x[0] = row[tx];
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (!skip || w[i][u] != 0.f) {
@@ -317,46 +332,44 @@ __global__ void __launch_bounds__(kThreads) window_dq_simt_kernel(Attn a, Ptrs<T
     }
 }
 
-// dk and dv of one 64-key tile, over the queries that see it and the group's heads.
+// dk and dv of one 64-key tile, over the queries that see it and the group's heads; the sinks'
+// far queries in CTAs of their own (SinkSplit).
 template <int HD, class T>
 __global__ void __launch_bounds__(kThreads) window_dkv_simt_kernel(Attn a, Ptrs<T> p) {
     extern __shared__ float sm[];
     float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
           *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sP = sS + kT * kPS,
           *sL = sP + kT * kPS, *sD = sL + kT;
-    const int hk = blockIdx.y, b = blockIdx.z, G = a.G();
-    const int k0 = (int)blockIdx.x * kT, off = a.Tk - a.Tq;
+    const int hk = blockIdx.y, b = blockIdx.z, G = a.G(), off = a.Tk - a.Tq;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int len = seq_len(p.lens, b, a.Tk);
+    const KeyTile<kT> kt(blockIdx.x, a, p.sinks, len);
+    const int k0 = kt.k0;
     float dk[4][HD / 16], dv[4][HD / 16];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int c = 0; c < HD / 16; ++c) dk[i][c] = dv[i][c] = 0.f;
-    // positions first .. last see some key of the tile
-    const int first = max(k0, off);
-    const int last = (k0 < a.sinks || a.window >= a.Tk) ? len - 1
-                                                        : min(k0 + kT - 1 + a.window - 1, len - 1);
-    if (k0 < len && first <= last) {
+    if (k0 < len && kt.first <= kt.last) {
         load_tile<HD>(sK, p.k + a.k.at(b, 0, hk), a.k.t, k0, 0, len, p.vec);
         load_tile<HD>(sV, p.v + a.v.at(b, 0, hk), a.v.t, k0, 0, len, p.vec);
         for (int g = 0; g < G; ++g) {
             const int h = hk * G + g;
             const long long row0 = ((long long)b * a.H + h) * a.Tq;
-            for (int pq = first; pq <= last; pq += kT) {
-                const int i0 = pq - off, n = min(a.Tq, len - off);
+            for (int pq = kt.first; pq <= kt.last; pq += kT) {
+                const int i0 = pq - off, n = kt.last + 1 - off;
                 __syncthreads();
                 load_tile<HD>(sQ, p.q + a.q.at(b, 0, h), a.q.t, i0, 0, n, p.vec);
                 load_tile<HD>(sG, p.dO + a.go.at(b, 0, h), a.go.t, i0, 0, n, p.vec);
                 load_rows(sL, sD, p, row0, i0, n);
                 __syncthreads();
                 const bool whole = pq >= k0 + kT - 1 && pq + kT - 1 - k0 < a.window &&
-                                   pq + kT - 1 < len && k0 + kT <= len;
+                                   pq + kT - 1 <= kt.last && k0 + kT <= len;
                 grad_scores<HD>(
                     sQ, sG, sK, sV, sL, sD, a.scale * kLog2e, whole,
                     [&](int r, int c) {
                         const int pos = pq + r, t = k0 + c;
-                        return pos < len && t <= pos && (pos - t < a.window || t < a.sinks);
+                        return pos <= kt.last && t <= pos && (pos - t < a.window || t < a.sinks);
                     },
                     sP, sS, ty, tx, pq, a.window, a.sinks);
                 __syncthreads();
@@ -365,12 +378,36 @@ __global__ void __launch_bounds__(kThreads) window_dkv_simt_kernel(Attn a, Ptrs<
             }
         }
     }
+    float *sums = p.partial + kt.partial_at(b, hk, a);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int t = k0 + ty * 4 + i;
         if (t >= a.Tk) continue;
-        store_row<HD>(p.dk + a.dk.at(b, t, hk), tx, dk[i], a.scale);
-        store_row<HD>(p.dv + a.dv.at(b, t, hk), tx, dv[i], 1.f);
+        if (kt.has_sinks && t < a.sinks) {
+#pragma unroll
+            for (int c = 0; c < HD / 16; ++c) {
+                sums[(long long)t * 2 * HD + col_of<HD>(tx, c)] = dk[i][c] * a.scale;
+                sums[(long long)t * 2 * HD + HD + col_of<HD>(tx, c)] = dv[i][c];
+            }
+        } else if (kt.part == 0) {
+            store_row<HD>(p.dk + a.dk.at(b, t, hk), tx, dk[i], a.scale);
+            store_row<HD>(p.dv + a.dv.at(b, t, hk), tx, dv[i], 1.f);
+        }
+    }
+}
+
+// dk and dv of the sink rows: the tile's own sum and the other CTAs', in order.
+template <class T>
+__global__ void __launch_bounds__(256) window_sink_rows_kernel(Attn a, const float *partial, int extra,
+                                                               T *dk, T *dv) {
+    const int b = blockIdx.z, hk = blockIdx.y, t = blockIdx.x;
+    const long long slot = (long long)a.sinks * 2 * a.hp;
+    for (int e = threadIdx.x; e < 2 * a.hp; e += blockDim.x) {
+        const float *s = partial + ((long long)b * a.Hkv + hk) * (extra + 1) * slot + (long long)t * 2 * a.hp + e;
+        float sum = 0.f;
+        for (int x = 0; x <= extra; ++x) sum += s[x * slot];
+        if (e < a.hp) dk[a.dk.at(b, t, hk) + e] = from_f32<T>(sum);
+        else dv[a.dv.at(b, t, hk) + e - a.hp] = from_f32<T>(sum);
     }
 }
 
@@ -446,9 +483,10 @@ cudaError_t fwd(const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
 
 template <int HD, class T>
 cudaError_t bwd_hd(const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
-    const dim3 gk((a.Tk + kT - 1) / kT, a.Hkv, a.B), gq((a.Tq + kT - 1) / kT, a.H, a.B);
+    const dim3 gk(p.sinks.ctas(a, kT), a.Hkv, a.B), gq((a.Tq + kT - 1) / kT, a.H, a.B);
     cudaError_t e = go(window_dkv_simt_kernel<HD, T>, gk, dkv_smem<HD>(), a, p, s);
-    return e != cudaSuccess ? e : go(window_dq_simt_kernel<HD, T>, gq, dq_smem<HD>(), a, p, s);
+    if (e == cudaSuccess) e = go(window_dq_simt_kernel<HD, T>, gq, dq_smem<HD>(), a, p, s);
+    return e != cudaSuccess ? e : add_sink_rows(a, p.partial, p.sinks.extra, p.dk, p.dv, s);
 }
 
 template <class T>
@@ -485,8 +523,10 @@ cudaError_t fwd_of(const Attn &a, const void *q, const void *k, const void *v, c
 template <class T>
 cudaError_t bwd_of(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
                    const float *lse, const void *dO, const float *delta, void *dq, void *dk,
-                   void *dv, cudaStream_t s) {
+                   void *dv, float *partial, cudaStream_t s) {
     Ptrs<T> p = ptrs<T>(a, q, k, v, lens);
+    p.partial = partial;
+    p.sinks = SinkSplit(a, kT);
     p.vec = p.vec && rows16(dO, a.go, a.bf16);
     p.dO = (const T *)dO;
     p.lse_in = lse;
@@ -507,9 +547,26 @@ cudaError_t simt_window_fwd(const Attn &a, const void *q, const void *k, const v
 
 cudaError_t simt_window_bwd(const Attn &a, const void *q, const void *k, const void *v,
                             const int32_t *lens, const float *lse, const void *dO,
-                            const float *delta, void *dq, void *dk, void *dv, cudaStream_t s) {
-    return a.bf16 ? bwd_of<bf16>(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, s)
-                  : bwd_of<float>(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, s);
+                            const float *delta, void *dq, void *dk, void *dv, float *partial,
+                            cudaStream_t s) {
+    return a.bf16 ? bwd_of<bf16>(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, partial, s)
+                  : bwd_of<float>(a, q, k, v, lens, lse, dO, delta, dq, dk, dv, partial, s);
+}
+
+cudaError_t add_sink_rows(const Attn &a, const float *partial, int extra, void *dk, void *dv,
+                          cudaStream_t s) {
+    if (extra == 0) return cudaSuccess;
+    const dim3 grid(a.sinks, a.Hkv, a.B);
+    if (a.bf16) window_sink_rows_kernel<bf16><<<grid, 256, 0, s>>>(a, partial, extra, (bf16 *)dk, (bf16 *)dv);
+    else window_sink_rows_kernel<float><<<grid, 256, 0, s>>>(a, partial, extra, (float *)dk, (float *)dv);
+    note_launches(1);
+    return cudaGetLastError();
+}
+
+// The larger of both kernels' tiles: which one runs hangs on the tensors' places.
+size_t window_bwd_bytes(const Attn &a) {
+    const size_t x = SinkSplit(a, kT).bytes(a);
+    return a.bf16 ? std::max(x, SinkSplit(a, kTcTile).bytes(a)) : x;
 }
 
 cudaError_t window_delta(const Attn &a, const void *O, const bf16 *rest, const void *dO, float *delta,

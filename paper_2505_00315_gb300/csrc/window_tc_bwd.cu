@@ -37,7 +37,7 @@ namespace mosa {
 namespace win {
 namespace {
 
-constexpr int kTile = 128;
+constexpr int kTile = kTcTile;
 constexpr int kWarps = 16, kWorkers = 32 * kWarps;   // the workers'
 constexpr int kCols = 128 / (kWarps / 4);            // score columns of one worker thread
 
@@ -49,8 +49,9 @@ struct BwdArgs {
     Str sdq, sdk, sdv;
     float *partial;                     // [B, Hkv, slots, sinks, 2, hp] fp32: dk, dv of the sink rows
     uint32_t *status;
+    Attn a;
+    SinkSplit split;
     int Tq, Tk, H, Hkv, G, hp, window, sinks;
-    int tiles, extra, chunk;            // key tiles; CTAs per sink tile beside it; their blocks
     float scale, scale_log2;
 };
 
@@ -104,22 +105,12 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int b = blockIdx.z, hk = blockIdx.y, off = p.Tk - p.Tq;
     const int len = seq_len(p.lens, b, p.Tk);
-    // the sink tiles' extra work first, then the key tiles
-    const int sink_tiles = (p.sinks + kTile - 1) / kTile, extras = sink_tiles * p.extra;
-    const bool is_extra = (int)blockIdx.x < extras;
-    const int part = is_extra ? 1 + (int)blockIdx.x % p.extra : 0;
-    const int tile = is_extra ? (int)blockIdx.x / p.extra : (int)blockIdx.x - extras;
-    const int k0 = tile * kTile;
-    const bool has_sinks = k0 < p.sinks && p.extra > 0;   // rows below p.sinks go to `partial`
-    int first = max(k0, off), last = min(k0 + kTile - 1 + p.window - 1, len - 1);
-    if (k0 < p.sinks && p.extra == 0) last = len - 1;
-    if (is_extra) {
-        first = max(k0 + kTile - 1 + p.window, off) + (part - 1) * p.chunk * kTile;
-        last = min(first + p.chunk * kTile, len) - 1;
-    }
+    const KeyTile<kTile> kt(blockIdx.x, p.a, p.split, len);
+    const int k0 = kt.k0, first = kt.first, last = kt.last;
+    const bool is_extra = kt.part > 0, has_sinks = kt.has_sinks;
     const int blocks = first <= last && k0 < len ? (last - first) / kTile + 1 : 0;
     const int n = blocks * p.G;            // (head of the group, block) pairs, heads outermost
-    float *sink_sums = p.partial + (((long long)b * p.Hkv + hk) * (p.extra + 1) + part) * p.sinks * 2 * p.hp;
+    float *sink_sums = p.partial + kt.partial_at(b, hk, p.a);
 
     if (n == 0) {   // no query sees the tile: zeros
         const int units = p.hp / 8;
@@ -402,18 +393,6 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
     if (warp == kWarps) tmem_dealloc(sm.tmem, 512);
 }
 
-// dk and dv of the sink rows: the tile's own sum and the extra CTAs', in order.
-__global__ void __launch_bounds__(256) window_sink_rows_kernel(const __grid_constant__ BwdArgs p) {
-    const int b = blockIdx.z, hk = blockIdx.y, t = blockIdx.x;
-    for (int e = threadIdx.x; e < 2 * p.hp; e += blockDim.x) {
-        const float *s = p.partial + (((long long)b * p.Hkv + hk) * (p.extra + 1) * p.sinks + t) * 2 * p.hp + e;
-        float sum = 0.f;
-        for (int x = 0; x <= p.extra; ++x) sum += s[(long long)x * p.sinks * 2 * p.hp];
-        if (e < p.hp) p.dK[p.sdk.at(b, t, hk) + e] = from_f32<bf16>(sum);
-        else p.dV[p.sdv.at(b, t, hk) + e - p.hp] = from_f32<bf16>(sum);
-    }
-}
-
 // ---------------------------------------------------------------------- dQ
 
 template <int HD>
@@ -644,15 +623,6 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
     if (warp == kWarps) tmem_dealloc(sm.tmem, 512);
 }
 
-// Extra CTAs per sink tile, and the query blocks of each: as many as a tile without
-// sinks has, so that all CTAs take about as long.
-void split_sinks(const Attn &a, int *extra, int *chunk) {
-    *chunk = (a.window + kTile - 2) / kTile + 1;
-    const long long beyond = (long long)a.Tk - (kTile - 1 + (long long)a.window);
-    *extra = a.sinks > 0 && beyond > 0
-                 ? (int)((beyond + (long long)*chunk * kTile - 1) / ((long long)*chunk * kTile)) : 0;
-}
-
 template <int HD>
 cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     constexpr int kv = (int)sizeof(KvSm<HD>), qb = (int)sizeof(QSm<HD>);
@@ -660,24 +630,14 @@ cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     cudaError_t e = allow_smem((const void *)window_dkv_tc_kernel<HD>, kv);
     if (e == cudaSuccess) e = allow_smem((const void *)window_dq_tc_kernel<HD>, qb);
     if (e != cudaSuccess) return e;
-    const int sink_tiles = (p.sinks + kTile - 1) / kTile;
-    window_dkv_tc_kernel<HD><<<dim3(p.tiles + sink_tiles * p.extra, p.Hkv, B), kKvThreads, kv, s>>>(p);
+    window_dkv_tc_kernel<HD><<<dim3(p.split.ctas(p.a, kTile), p.Hkv, B), kKvThreads, kv, s>>>(p);
     window_dq_tc_kernel<HD><<<dim3((p.Tq + kTile - 1) / kTile, p.H, B), kQThreads, qb, s>>>(p);
     note_launches(2);
-    if (p.extra > 0) {
-        window_sink_rows_kernel<<<dim3(p.sinks, p.Hkv, B), 256, 0, s>>>(p);
-        note_launches(1);
-    }
-    return cudaGetLastError();
+    e = cudaGetLastError();
+    return e != cudaSuccess ? e : add_sink_rows(p.a, p.partial, p.split.extra, p.dK, p.dV, s);
 }
 
 }  // namespace
-
-size_t tc_window_bwd_bytes(const Attn &a) {
-    int extra, chunk;
-    split_sinks(a, &extra, &chunk);
-    return extra == 0 ? 0 : (size_t)a.B * a.Hkv * (extra + 1) * a.sinks * 2 * a.hp * sizeof(float);
-}
 
 bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, const int32_t *lens,
                    const float *lse, const void *dO, const float *delta, void *dq, void *dk, void *dv,
@@ -708,8 +668,8 @@ bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, c
     p.hp = a.hp;
     p.window = a.window;
     p.sinks = a.sinks;
-    p.tiles = (a.Tk + kTile - 1) / kTile;
-    split_sinks(a, &p.extra, &p.chunk);
+    p.a = a;
+    p.split = SinkSplit(a, kTile);
     p.scale = a.scale;
     p.scale_log2 = a.scale * kLog2e;
     *err = a.hp <= 64 ? launch<64>(p, a.B, s) : launch<128>(p, a.B, s);

@@ -50,6 +50,51 @@ struct KeyBlocks {
     }
 };
 
+// dk and dv are summed by one CTA per key tile, over the queries that see it: window + tile of them,
+// but for sinks all later ones, Tk / window times as many.  Those beyond a sink tile's window go
+// to `extra` CTAs of their own, `chunk` tiles of queries each (as many as other tiles have), which
+// leave fp32 sums of the sink rows; add_sink_rows adds them up in order.
+struct SinkSplit {
+    int extra = 0, chunk = 1;
+    SinkSplit() = default;
+    SinkSplit(const Attn &a, int tile) {
+        chunk = (a.window + tile - 2) / tile + 1;
+        const long long beyond = (long long)a.Tk - (tile - 1 + (long long)a.window), per = (long long)chunk * tile;
+        extra = a.sinks > 0 && beyond > 0 ? (int)((beyond + per - 1) / per) : 0;
+    }
+    __host__ __device__ int extras(const Attn &a, int tile) const { return (a.sinks + tile - 1) / tile * extra; }
+    // CTAs of one key head of one sequence: the extra ones first.
+    int ctas(const Attn &a, int tile) const { return extras(a, tile) + (a.Tk + tile - 1) / tile; }
+    size_t bytes(const Attn &a) const {
+        return extra == 0 ? 0 : (size_t)a.B * a.Hkv * (extra + 1) * a.sinks * 2 * a.hp * sizeof(float);
+    }
+};
+
+// One of those CTAs: its key tile from k0 on and its query positions first .. last.
+template <int N>
+struct KeyTile {
+    int k0, part, first, last, extra;
+    bool has_sinks;   // rows below the number of sinks go to the partial sums
+    __device__ __forceinline__ KeyTile(int x, const Attn &a, const SinkSplit &sp, int len) {
+        const int extras = sp.extras(a, N), off = a.Tk - a.Tq;
+        extra = sp.extra;
+        part = x < extras ? 1 + x % extra : 0;
+        k0 = (x < extras ? x / extra : x - extras) * N;
+        has_sinks = k0 < a.sinks && extra > 0;
+        if (part == 0) {
+            first = max(k0, off);
+            last = k0 < a.sinks && extra == 0 ? len - 1 : min(k0 + N - 1 + a.window - 1, len - 1);
+        } else {
+            first = max(k0 + N - 1 + a.window, off) + (part - 1) * sp.chunk * N;
+            last = min(first + sp.chunk * N, len) - 1;
+        }
+    }
+    // Where this CTA's sums start in the partial sums [B, Hkv, extra + 1, sinks, 2, hp].
+    __device__ __forceinline__ long long partial_at(int b, int hk, const Attn &a) const {
+        return (((long long)b * a.Hkv + hk) * (extra + 1) + part) * a.sinks * 2 * a.hp;
+    }
+};
+
 // A query that sees one token only has P = 1: its scores have no gradient.  Set to
 // exactly zero there, where rounding would leave a remainder of dP - D.
 __device__ __forceinline__ bool sees_one(int p, int window, int sinks) {
