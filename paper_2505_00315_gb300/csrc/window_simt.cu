@@ -72,7 +72,7 @@ __device__ __forceinline__ void dot_tiles(const float *A, const float *B, int ty
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-#pragma unroll 4
+#pragma unroll 2
     for (int d = 0; d < HD; d += 4) {
         float4 a[4], b[4];
 #pragma unroll
@@ -166,7 +166,7 @@ template <int HD>
 constexpr int tile_floats() { return kT * (HD + 4); }
 
 template <int HD, class T>
-__global__ void __launch_bounds__(kThreads) window_fwd_simt_kernel(Attn a, Ptrs<T> p) {
+__global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Ptrs<T> p) {
     extern __shared__ float sm[];
     float *sQ = sm, *sK = sQ + tile_floats<HD>(), *sV = sK + tile_floats<HD>(),
           *sP = sV + tile_floats<HD>();
@@ -287,7 +287,7 @@ __device__ __forceinline__ void load_rows(float *sL, float *sD, const Ptrs<T> &p
 
 // dq of one 64-query tile.
 template <int HD, class T>
-__global__ void __launch_bounds__(kThreads) window_dq_simt_kernel(Attn a, Ptrs<T> p) {
+__global__ void __launch_bounds__(kThreads, HD <= 64 ? 2 : 1) window_dq_simt_kernel(Attn a, Ptrs<T> p) {
     extern __shared__ float sm[];
     float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
           *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sL = sS + kT * kPS,
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kThreads) window_dq_simt_kernel(Attn a, Ptrs<T
 // dk and dv of one 64-key tile, over the queries that see it and the group's heads; the sinks'
 // far queries in CTAs of their own (SinkSplit).
 template <int HD, class T>
-__global__ void __launch_bounds__(kThreads) window_dkv_simt_kernel(Attn a, Ptrs<T> p) {
+__global__ void __launch_bounds__(kThreads, HD <= 64 ? 2 : 1) window_dkv_simt_kernel(Attn a, Ptrs<T> p) {
     extern __shared__ float sm[];
     float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
           *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sP = sS + kT * kPS,
