@@ -26,7 +26,7 @@ namespace mosa {
 namespace win {
 namespace {
 
-constexpr int kThreads = 320, kWorkers = 256;
+constexpr int kWarps = 16, kWorkers = 32 * kWarps, kThreads = kWorkers + 64;
 constexpr int kQ = 128, kN = 128;             // queries and keys of a tile
 constexpr float kRescaleLog2 = 8.f;
 
@@ -48,7 +48,7 @@ struct FwdSm {
     uint8_t q[NB][kBlk];
     uint8_t kv[NS][NB][kBlk];    // K_0, V_0, K_1, V_1, ..
     uint64_t q_full, kv_full[NS], kv_empty[NS], s_full, p_ready, o_done, drained;
-    float part[2][2][kQ];        // [parity][half]: block maxima, final sums
+    float part[2][4][kQ];        // [parity][quarter]: block maxima, final sums
     uint32_t tmem;
     uint32_t odd[4];             // second pass: keys of the block whose V row was zeroed
     int abort, redo;
@@ -82,13 +82,13 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
             mbar_init(smem_u32(&sm.kv_empty[s]), 1);
         }
         mbar_init(smem_u32(&sm.s_full), 1);
-        mbar_init(smem_u32(&sm.p_ready), 8);
+        mbar_init(smem_u32(&sm.p_ready), kWarps);
         mbar_init(smem_u32(&sm.o_done), 1);
         mbar_init(smem_u32(&sm.drained), 1);
         sm.abort = sm.redo = 0;
         fence_barrier_init();
     }
-    if (warp == 8) {
+    if (warp == kWarps) {
         tmem_alloc(smem_u32(&sm.tmem), 256);
         tmem_relinquish();
     }
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
     int item = 0, phase = 0;   // K/V tiles and key blocks of both passes so far
     bool ok = true;
     for (int pass = 0; pass < 2; ++pass) {
-        if (warp == 8) {
+        if (warp == kWarps) {
             if (lane == 0) {
                 if (pass == 0) {
                     mbar_expect_tx(smem_u32(&sm.q_full), NB * kBlk);
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     drain_phase(smem_u32(&sm.kv_full[t % NS]), (t / NS) & 1);
             }
             __syncwarp();
-        } else if (warp == 9) {
+        } else if (warp == kWarps + 1) {
             if (elect_one()) {
                 constexpr uint32_t idS = idesc_bf16(128, kN, false, false);
                 constexpr uint32_t idO = idesc_bf16(128, HD, false, true);
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     ok = wait_or_abort(sm.p_ready, phase & 1, &sm.abort, p.status);
                     const int s = next();
                     if (s < 0) break;
-                    mma_weights<6>(tO, tS, mn_major(sm.kv[s]), idO, j > 0);   // O += P V_j
+                    mma_weights<5>(tO, tS, mn_major(sm.kv[s]), idO, j > 0);   // O += P V_j
                     mma_commit(smem_u32(&sm.kv_empty[s]));
                     // (the next scores overwrite P: MMAs run in the order of issue)
                     if (j + 1 < n) scores();
@@ -162,92 +162,81 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
             }
             __syncwarp();
         } else {
-            const int ch = warp >> 2, q = warp & 3, r = q * 32 + lane, pos = pf + r;
-            const uint32_t lanes = (uint32_t)(q * 32) << 16, tmy = tS + lanes + 64 * ch;
+            const int cq = warp >> 2, q = warp & 3, r = q * 32 + lane, pos = pf + r;
+            const uint32_t lanes = (uint32_t)(q * 32) << 16, tmy = tS + lanes + 32 * cq;
             const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < n; ++j, ++phase) {
+                const bool whole = kb.whole(j, pf, pl, p.window);
+                uint32_t seen = ~0u;
+                if (!whole) seen = seen_bits(kb, j, kb.start(j), 32 * cq, pos, p.window, p.sinks);
                 ok = wait_or_abort(sm.s_full, phase & 1, &sm.abort, p.status) && ok;
                 tc_fence_after();
-                uint32_t raw[2][32];
-                tmem_ld32_async(tmy, raw[0]);
-                tmem_ld32_async(tmy + 32, raw[1]);
-                const bool whole = kb.whole(j, pf, pl, p.window);
-                uint32_t seen[2] = {~0u, ~0u};
-                if (!whole) {
-                    const int ks = kb.start(j);
-                    seen[0] = seen_bits(kb, j, ks, 64 * ch, pos, p.window, p.sinks);
-                    seen[1] = seen_bits(kb, j, ks, 64 * ch + 32, pos, p.window, p.sinks);
-                }
-                tmem_ready(raw[0]);
-                tmem_ready(raw[1]);
-                float s[64];
+                uint32_t raw[32];
+                tmem_ld32_async(tmy, raw);
+                tmem_ready(raw);
+                float s[32];
 #pragma unroll
-                for (int c = 0; c < 64; ++c) s[c] = __uint_as_float(raw[c >> 5][c & 31]);
+                for (int c = 0; c < 32; ++c) s[c] = __uint_as_float(raw[c]);
                 if (!whole) {
 #pragma unroll
-                    for (int c = 0; c < 64; ++c)
-                        if (((seen[c >> 5] >> (c & 31)) & 1u) == 0) s[c] = -INFINITY;
+                    for (int c = 0; c < 32; ++c)
+                        if (((seen >> c) & 1u) == 0) s[c] = -INFINITY;
                 }
                 float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                for (int c = 4; c < 64; c += 8) {
+                for (int c = 4; c < 32; c += 8) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        mx[e] = fmaxf(fmaxf(mx[e], s[c + e]), c + 4 + e < 64 ? s[c + 4 + e] : s[c + e]);
+                        mx[e] = fmaxf(fmaxf(mx[e], s[c + e]), c + 4 + e < 32 ? s[c + 4 + e] : s[c + e]);
                 }
-                float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+                float (*part)[kQ] = sm.part[phase & 1];
                 // (the buffer of this parity was last read before the last block's barrier)
-                sm.part[phase & 1][ch][r] = mb;
-                named_barrier(1 + q, 64);
-                mb = fmaxf(mb, sm.part[phase & 1][ch ^ 1][r]);
-                const bool grow = mb > m + kRescaleLog2;   // the same in both threads of the row
+                part[cq][r] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                named_barrier(1 + q, 128);
+                const float mb = fmaxf(fmaxf(part[0][r], part[1][r]), fmaxf(part[2][r], part[3][r])) * p.scale_log2;
+                const bool grow = mb > m + kRescaleLog2;   // the same in all four threads of the row
                 const float m_new = grow ? mb : m;
                 const float corr = grow ? exp2_fast(m - m_new) : 1.f;   // 0 on a row's first block
                 const float base = m_new == -INFINITY ? 0.f : m_new;
                 const float2 neg = make_float2(-base, -base);
-                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int c = 0; c < 64; c += 2) {
+                for (int c = 0; c < 32; c += 2) {
                     const float2 x = fma2(make_float2(s[c], s[c + 1]), sl2, neg);
                     s[c] = exp2_fast(x.x);
                     s[c + 1] = exp2_fast(x.y);
-                    sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], make_float2(s[c], s[c + 1]));
+                    sum = add2(sum, make_float2(s[c], s[c + 1]));
                 }
-                l = l * corr + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+                l = l * corr + (sum.x + sum.y);
                 m = m_new;
-                if (j > 0 && __any_sync(0xffffffffu, grow)) {
-                    // (S_j was issued after P_{j-1} V_{j-1}, so O is complete)
-#pragma unroll
-                    for (int c = 0; c < HD / 2; c += 16) {
-                        float o[16];
-                        uint32_t w[16];
-                        tmem_ld16(tO + lanes + ch * (HD / 2) + c, o);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * corr);
-                        tmem_st16_async(tO + lanes + ch * (HD / 2) + c, w);
-                    }
-                }
                 if (pass == 1 && !whole) {
                     // V rows with NaN or infinities: zeroed, and NaN for the rows that see them
                     const int t = item + 2 * j + 1;
                     ok = wait_or_abort(sm.kv_full[t % NS], (t / NS) & 1, &sm.abort, p.status) && ok;
-                    if (ch == 0) {
+                    if (cq == 0) {
                         const uint32_t odd = __ballot_sync(0xffffffffu, clean_row<NB>(sm.kv[t % NS][0], r));
                         if (lane == 0) sm.odd[q] = odd;
                         fence_proxy_async();
                     }
                     named_barrier(5, kWorkers);
-                    if (((sm.odd[2 * ch] & seen[0]) | (sm.odd[2 * ch + 1] & seen[1])) != 0)
-                        s[0] = NAN;   // times the row of that key, whatever it holds
+                    if ((sm.odd[cq] & seen) != 0) s[0] = NAN;   // times the row of that key, whatever it holds
                     named_barrier(5, kWorkers);
                 }
+                uint32_t w[16];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    uint32_t w[16];
+                for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
+                tmem_st16_async(tmy, w);
+                if (j > 0 && __any_sync(0xffffffffu, grow)) {
+                    // (S_j was issued after P_{j-1} V_{j-1}, so O is complete)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(s[32 * u + 2 * e], s[32 * u + 2 * e + 1]);
-                    tmem_st16_async(tmy + 16 * u, w);
+                    for (int c = 0; c < HD / 4; c += 16) {
+                        float o[16];
+                        tmem_ld16(tO + lanes + cq * (HD / 4) + c, o);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * corr);
+                        tmem_st16_async(tO + lanes + cq * (HD / 4) + c, w);
+                    }
                 }
                 tmem_stored();
                 tc_fence_before();
@@ -256,45 +245,42 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
             item += 2 * n;
             ok = wait_or_abort(sm.o_done, pass, &sm.abort, p.status) && ok;
             tc_fence_after();
-            uint32_t raw[HD / 64][32];   // this thread's half of the columns
-#pragma unroll
-            for (int u = 0; u < HD / 64; ++u)
-                tmem_ld32_async(tO + lanes + ch * (HD / 2) + 32 * u, raw[u]);
-#pragma unroll
-            for (int u = 0; u < HD / 64; ++u) tmem_ready(raw[u]);
-            const bool valid = pos <= pl;
+            float o[HD / 64][16];   // this thread's quarter of the columns
             float odd = 0.f;
+            const bool valid = pos <= pl;
 #pragma unroll
-            for (int u = 0; u < HD / 64; ++u)
+            for (int u = 0; u < HD / 64; ++u) {
+                tmem_ld16(tO + lanes + cq * (HD / 4) + 16 * u, o[u]);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) odd = fmaf(__uint_as_float(raw[u][e]), 0.f, odd);
+                for (int e = 0; e < 16; ++e) odd = fmaf(o[u][e], 0.f, odd);
+            }
             if (pass == 0 && valid && !(odd == 0.f)) sm.redo = 1;
-            sm.part[phase & 1][ch][r] = l;
+            float (*part)[kQ] = sm.part[phase & 1];
+            part[cq][r] = l;
             named_barrier(5, kWorkers);
-            l += sm.part[phase & 1][ch ^ 1][r];
+            l = (part[0][r] + part[1][r]) + (part[2][r] + part[3][r]);
             const bool live = *(volatile int *)&sm.abort == 0;
             if (live && (pass == 1 || *(volatile int *)&sm.redo == 0)) {
                 const float inv = valid ? 1.f / l : 0.f;
 #pragma unroll
-                for (int u = 0; u < HD / 16; ++u) {
+                for (int u = 0; u < HD / 32; ++u) {
                     uint32_t w[4], y[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int c = 8 * u + 2 * e;
-                        const float x0 = __uint_as_float(raw[c >> 5][c & 31]) * inv;
-                        const float x1 = __uint_as_float(raw[c >> 5][(c & 31) + 1]) * inv;
+                        const int c = 8 * (u & 1) + 2 * e;
+                        const float x0 = o[u >> 1][c] * inv, x1 = o[u >> 1][c + 1] * inv;
                         w[e] = valid ? pack_bf16x2(x0, x1) : 0u;
                         y[e] = valid ? pack_bf16x2(x0 - __uint_as_float(w[e] << 16),
                                                    x1 - __uint_as_float(w[e] & 0xFFFF0000u)) : 0u;
                     }
-                    const int unit = ch * (HD / 16) + u;
+                    const int unit = cq * (HD / 32) + u;
                     *reinterpret_cast<uint4 *>(sm.q[unit >> 3] + xoff128(r, unit & 7)) =
                         make_uint4(w[0], w[1], w[2], w[3]);
                     if (p.keep_rest)
                         *reinterpret_cast<uint4 *>(sm.kv[0][unit >> 3] + xoff128(r, unit & 7)) =
                             make_uint4(y[0], y[1], y[2], y[3]);
                 }
-                if (lse != nullptr && ch == 0 && i0 + r < p.Tq)
+                if (lse != nullptr && cq == 0 && i0 + r < p.Tq)
                     lse[i0 + r] = valid ? (m + log2f(l)) * kLn2 : -INFINITY;
                 fence_proxy_async();
                 named_barrier(5, kWorkers);
@@ -313,9 +299,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
         tc_fence_after();
         if (*(volatile int *)&sm.redo == 0 || *(volatile int *)&sm.abort != 0) break;
     }
-    if (warp == 9 && elect_one()) drain_mmas(smem_u32(&sm.drained));
+    if (warp == kWarps + 1 && elect_one()) drain_mmas(smem_u32(&sm.drained));
     __syncthreads();
-    if (warp == 8) tmem_dealloc(sm.tmem, 256);
+    if (warp == kWarps) tmem_dealloc(sm.tmem, 256);
 }
 
 template <int HD>
