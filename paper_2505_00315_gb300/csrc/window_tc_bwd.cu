@@ -266,16 +266,15 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
             ok = wait(sm.st_full[u], (i >> 1) & 1) && ok;
             ok = wait(sm.s_full, i & 1) && ok;
             tc_fence_after();
-            uint32_t raw[32];
-            tmem_ld32_async(tS + at, raw);
-            tmem_ready(raw);
+            float raw[32];
+            tmem_get32(tS + at, raw);
             float P[32];
 #pragma unroll
             for (int c = 0; c < 32; c += 4) {
                 const float4 l4 = *reinterpret_cast<const float4 *>(L + c);
-                const float2 x = fma2(make_float2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2,
+                const float2 x = fma2(make_float2(raw[c], raw[c + 1]), sl2,
                                       make_float2(-l4.x, -l4.y));
-                const float2 y = fma2(make_float2(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])),
+                const float2 y = fma2(make_float2(raw[c + 2], raw[c + 3]),
                                       sl2, make_float2(-l4.z, -l4.w));
                 P[c] = exp2_fast(x.x);
                 P[c + 1] = exp2_fast(x.y);
@@ -305,16 +304,15 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
 
             ok = wait(sm.dp_full, i & 1) && ok;
             tc_fence_after();
-            tmem_ld32_async(tG + at, raw);
-            tmem_ready(raw);
+            tmem_get32(tG + at, raw);
 #pragma unroll
             for (int c = 0; c < 32; c += 4) {
                 const float4 d4 = *reinterpret_cast<const float4 *>(D + c);
                 const float2 x = mul2(make_float2(P[c], P[c + 1]),
-                                      add2(make_float2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])),
+                                      add2(make_float2(raw[c], raw[c + 1]),
                                            make_float2(-d4.x, -d4.y)));
                 const float2 y = mul2(make_float2(P[c + 2], P[c + 3]),
-                                      add2(make_float2(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])),
+                                      add2(make_float2(raw[c + 2], raw[c + 3]),
                                            make_float2(-d4.z, -d4.w)));
                 P[c] = x.x;
                 P[c + 1] = x.y;
@@ -551,25 +549,23 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 const bool whole = kb.whole(j, pf, pl, p.window);
                 ok = wait(sm.s_full[g & 1], (g >> 1) & 1) && ok;
                 tc_fence_after();
-                uint32_t raw[32];
-                tmem_ld32_async(tSj, raw);
-                tmem_ready(raw);
+                float raw[32];
+                tmem_get32(tSj, raw);
                 float P[32];
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
-                    const float2 x = fma2(make_float2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])),
+                    const float2 x = fma2(make_float2(raw[c], raw[c + 1]),
                                           sl2, nL);
                     P[c] = exp2_fast(x.x);
                     P[c + 1] = exp2_fast(x.y);
                 }
                 ok = wait(sm.dp_full, g & 1) && ok;
                 tc_fence_after();
-                tmem_ld32_async(tG + lanes + c0, raw);
-                tmem_ready(raw);
+                tmem_get32(tG + lanes + c0, raw);
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
                     const float2 x = mul2(make_float2(P[c], P[c + 1]),
-                                          add2(make_float2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), nD));
+                                          add2(make_float2(raw[c], raw[c + 1]), nD));
                     P[c] = x.x;
                     P[c + 1] = x.y;
                 }

@@ -172,29 +172,24 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                 if (!whole) seen = seen_bits(kb, j, kb.start(j), 32 * cq, pos, p.window, p.sinks);
                 ok = wait_or_abort(sm.s_full, phase & 1, &sm.abort, p.status) && ok;
                 tc_fence_after();
-                uint32_t raw[32];
-                tmem_ld32_async(tmy, raw);
-                tmem_ready(raw);
                 float s[32];
-#pragma unroll
-                for (int c = 0; c < 32; ++c) s[c] = __uint_as_float(raw[c]);
+                tmem_get32(tmy, s);
                 if (!whole) {
 #pragma unroll
                     for (int c = 0; c < 32; ++c)
                         if (((seen >> c) & 1u) == 0) s[c] = -INFINITY;
                 }
-                float mx[4] = {s[0], s[1], s[2], s[3]};
+                float mx[2] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3])};
 #pragma unroll
-                for (int c = 4; c < 32; c += 8) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        mx[e] = fmaxf(fmaxf(mx[e], s[c + e]), c + 4 + e < 32 ? s[c + 4 + e] : s[c + e]);
+                for (int c = 4; c < 32; c += 4) {
+                    mx[0] = max3(mx[0], s[c], s[c + 1]);
+                    mx[1] = max3(mx[1], s[c + 2], s[c + 3]);
                 }
                 float (*part)[kQ] = sm.part[phase & 1];
                 // (the buffer of this parity was last read before the last block's barrier)
-                part[cq][r] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                part[cq][r] = fmaxf(mx[0], mx[1]);
                 named_barrier(1 + q, 128);
-                const float mb = fmaxf(fmaxf(part[0][r], part[1][r]), fmaxf(part[2][r], part[3][r])) * p.scale_log2;
+                const float mb = fmaxf(max3(part[0][r], part[1][r], part[2][r]), part[3][r]) * p.scale_log2;
                 const bool grow = mb > m + kRescaleLog2;   // the same in all four threads of the row
                 const float m_new = grow ? mb : m;
                 const float corr = grow ? exp2_fast(m - m_new) : 1.f;   // 0 on a row's first block
@@ -206,7 +201,8 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     const float2 x = fma2(make_float2(s[c], s[c + 1]), sl2, neg);
                     s[c] = exp2_fast(x.x);
                     s[c + 1] = exp2_fast(x.y);
-                    sum = add2(sum, make_float2(s[c], s[c + 1]));
+                    sum.x += s[c];
+                    sum.y += s[c + 1];
                 }
                 l = l * corr + (sum.x + sum.y);
                 m = m_new;
