@@ -10,10 +10,12 @@
 // range at the same relative precision.  P is rounded to bf16, the type of the V it
 // meets (8 bits, as the output has); l sums the unrounded values.
 //
-// Warps 0-7 compute (two per TMEM lane quadrant, each half of the keys: two threads a row),
-// warp 8 loads by TMA, warp 9 issues the MMAs.  Two CTAs share an SM (256 of 512 TMEM columns, half
-// the shared memory each): while one's softmax runs the other's MMAs do, so a CTA's own
-// chain S -> P -> O may be plain.
+// Sixteen warps compute (four per TMEM lane quadrant, each a quarter of the keys: four threads a
+// row), one loads by TMA, one issues the MMAs.  Two CTAs share an SM (256 of 512 TMEM columns, half
+// the shared memory each): while one's softmax runs the other's MMAs do.  With hp = 128, S and
+// O fill a CTA's columns and P takes the place of S, so its chain is S -> P -> O -> S.
+// With hp <= 64 P has columns of its own, and the next scores are computed as soon as
+// the warps have read the last ones.
 //
 // A masked key has P = 0, but 0 times a NaN or infinity of its V row is NaN: a CTA whose
 // results are not all finite runs its blocks a second time with such V rows zeroed in
@@ -46,19 +48,42 @@ template <int HD>
 struct FwdSm {
     static constexpr int NB = HD / 64, NS = HD == 128 ? 2 : 4;
     uint8_t q[NB][kBlk];
-    uint8_t kv[NS][NB][kBlk];    // K_0, V_0, K_1, V_1, ..
-    uint64_t q_full, kv_full[NS], kv_empty[NS], s_full, p_ready, o_done, drained;
+    uint8_t kv[NS][NB][kBlk];    // the tiles of K and V in the order of kv_tile
+    uint64_t q_full, kv_full[NS], kv_empty[NS], s_full, s_free, p_ready, pv_done, o_done, drained;
     float part[2][4][kQ];        // [parity][quarter]: block maxima, final sums
     uint32_t tmem;
     uint32_t odd[4];             // second pass: keys of the block whose V row was zeroed
     int abort, redo;
 };
 
+// The K and V tiles of n blocks in the order in which the MMAs take them: K_0 V_0 K_1 V_1 .., or
+// where the next scores come early K_0 K_1 V_0 K_2 V_1 ..  Tile x is V's or K's of block j;
+// V's of block j is tile v_tile.
+template <bool kEarly>
+__device__ __forceinline__ bool kv_tile(int x, int n, int &j) {
+    if (!kEarly || x == 0 || x == 2 * n - 1) {
+        j = x >> 1;
+        return (x & 1) != 0;
+    }
+    j = x >> 1;   // x = 2j - 1: K_j; x = 2j + 2: V_j
+    if ((x & 1) != 0) {
+        ++j;
+        return false;
+    }
+    --j;
+    return true;
+}
+template <bool kEarly>
+__device__ __forceinline__ int v_tile(int j, int n) {
+    return !kEarly || j == n - 1 ? 2 * j + 1 : 2 * j + 2;
+}
+
 template <int HD>
 __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid_constant__ FwdArgs p) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using Sm = FwdSm<HD>;
     constexpr int NB = Sm::NB, NS = Sm::NS;
+    constexpr bool kEarly = HD == 64;
     Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int b = blockIdx.z, h = blockIdx.y, hk = h / p.G;
@@ -82,7 +107,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
             mbar_init(smem_u32(&sm.kv_empty[s]), 1);
         }
         mbar_init(smem_u32(&sm.s_full), 1);
+        mbar_init(smem_u32(&sm.s_free), kWarps);
         mbar_init(smem_u32(&sm.p_ready), kWarps);
+        mbar_init(smem_u32(&sm.pv_done), 1);
         mbar_init(smem_u32(&sm.o_done), 1);
         mbar_init(smem_u32(&sm.drained), 1);
         sm.abort = sm.redo = 0;
@@ -95,7 +122,8 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tS = sm.tmem, tO = tS + 128;   // (P: the first half of each half of S)
+    // P: columns of its own, or the first half of each quarter of S
+    const uint32_t tS = sm.tmem, tO = tS + 128, tP = kEarly ? tS + 192 : tS;
     const KeyBlocks<kN> kb(pf, pl, p.window, p.sinks);
     const int n = kb.count();
 
@@ -110,14 +138,15 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                         load_box(smem_u32(sm.q[c]), p.q, smem_u32(&sm.q_full), 64 * c, i0, h, b);
                 }
                 for (int x = 0; x < 2 * n && ok; ++x) {
+                    int j;
+                    const bool is_v = kv_tile<kEarly>(x, n, j);
                     const int s = item % NS;
                     ok = wait_or_abort(sm.kv_empty[s], ((item / NS) & 1) ^ 1, &sm.abort, p.status);
                     if (!ok) break;
                     const uint32_t bar = smem_u32(&sm.kv_full[s]);
                     mbar_expect_tx(bar, NB * kBlk);
                     for (int c = 0; c < NB; ++c)
-                        load_box(smem_u32(sm.kv[s][c]), (x & 1) == 0 ? p.k : p.v, bar, 64 * c,
-                                 kb.start(x >> 1), hk, b);
+                        load_box(smem_u32(sm.kv[s][c]), is_v ? p.v : p.k, bar, 64 * c, kb.start(j), hk, b);
                     ++item;
                 }
                 // what was loaded has landed
@@ -149,16 +178,24 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                 };
                 scores();
                 for (int j = 0; j < n && ok; ++j, ++phase) {
-                    ok = wait_or_abort(sm.p_ready, phase & 1, &sm.abort, p.status);
+                    if (kEarly && j + 1 < n) {
+                        ok = wait_or_abort(sm.s_free, phase & 1, &sm.abort, p.status);
+                        scores();
+                    }
+                    ok = ok && wait_or_abort(sm.p_ready, phase & 1, &sm.abort, p.status);
                     const int s = next();
                     if (s < 0) break;
-                    mma_weights<5>(tO, tS, mn_major(sm.kv[s]), idO, j > 0);   // O += P V_j
+                    mma_weights<kEarly ? 7 : 5>(tO, tP, mn_major(sm.kv[s]), idO, j > 0);   // O += P V_j
                     mma_commit(smem_u32(&sm.kv_empty[s]));
-                    // (the next scores overwrite P: MMAs run in the order of issue)
-                    if (j + 1 < n) scores();
+                    if (kEarly) mma_commit(smem_u32(&sm.pv_done));
+                    // (else the next scores overwrite P: MMAs run in the order of issue)
+                    else if (j + 1 < n) scores();
                 }
                 mma_commit(smem_u32(&sm.o_done));
-                if (!ok) mma_commit(smem_u32(&sm.s_full));
+                if (!ok) {
+                    mma_commit(smem_u32(&sm.s_full));
+                    mma_commit(smem_u32(&sm.pv_done));
+                }
             }
             __syncwarp();
         } else {
@@ -174,6 +211,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                 tc_fence_after();
                 float s[32];
                 tmem_get32(tmy, s);
+                if (kEarly) {   // S_{j+1} may be written
+                    tc_fence_before();
+                    warp_arrive(sm.s_free, lane);
+                }
                 if (!whole) {
 #pragma unroll
                     for (int c = 0; c < 32; ++c)
@@ -208,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                 m = m_new;
                 if (pass == 1 && !whole) {
                     // V rows with NaN or infinities: zeroed, and NaN for the rows that see them
-                    const int t = item + 2 * j + 1;
+                    const int t = item + v_tile<kEarly>(j, n);
                     ok = wait_or_abort(sm.kv_full[t % NS], (t / NS) & 1, &sm.abort, p.status) && ok;
                     if (cq == 0) {
                         const uint32_t odd = __ballot_sync(0xffffffffu, clean_row<NB>(sm.kv[t % NS][0], r));
@@ -222,9 +263,13 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
-                tmem_st16_async(tmy, w);
+                if (kEarly && j > 0) {   // P and O may be written: P_{j-1} V_{j-1} is done
+                    ok = wait_or_abort(sm.pv_done, (phase & 1) ^ 1, &sm.abort, p.status) && ok;
+                    tc_fence_after();
+                }
+                tmem_st16_async(kEarly ? tP + lanes + 16 * cq : tmy, w);
                 if (j > 0 && __any_sync(0xffffffffu, grow)) {
-                    // (S_j was issued after P_{j-1} V_{j-1}, so O is complete)
+                    // (not early: S_j was issued after P_{j-1} V_{j-1})
 #pragma unroll
                     for (int c = 0; c < HD / 4; c += 16) {
                         float o[16];
