@@ -1,4 +1,4 @@
-// Eight values a lane of a head's row: loads and stores, sums over the row's lanes and
+// Some values a lane of a head's row: loads and stores, sums over the row's lanes and
 // the rotation of qk_norm.cu, shared with the decoding step.
 #pragma once
 
@@ -7,33 +7,19 @@
 namespace mosa {
 namespace win {
 
-// The values of lane li of a row: lo .. lo+3 and hi .. hi+3, so that both values of each
-// rotated pair lie on one lane: neighbours, or with halves the same places of the
-// two halves of the rotated dimensions (whose number is a multiple of 8 then).
+// The W values of lane li of a row: lo .. lo+W/2-1 and hi .. hi+W/2-1, so that both values of
+// each rotated pair lie on one lane: neighbours, or with halves the same places of the
+// two halves of the rotated dimensions (whose number is a multiple of W then).
+template <int W>
 struct Part {
     int lo, hi;
     __device__ __forceinline__ Part(int li, int rotary, int halves) {
-        const bool split = halves && 8 * li < rotary;
-        lo = split ? 4 * li : 8 * li;
-        hi = split ? 4 * li + (rotary >> 1) : 8 * li + 4;
+        const bool split = halves && W * li < rotary;
+        lo = split ? W / 2 * li : W * li;
+        hi = split ? W / 2 * li + (rotary >> 1) : W * li + W / 2;
     }
+    __device__ __forceinline__ int at(int e) const { return e < W / 2 ? lo + e : hi + e - W / 2; }
 };
-
-// Four consecutive values, in one access where VEC.
-template <class T, bool VEC>
-__device__ __forceinline__ void load4(const T *p, float *v) {
-    if (!VEC) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = to_f32(p[i]);
-    } else if constexpr (sizeof(T) == 4) {
-        const float4 w = *reinterpret_cast<const float4 *>(p);
-        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-    } else {
-        const uint2 w = *reinterpret_cast<const uint2 *>(p);
-        v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
-        v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
-    }
-}
 
 // Two bf16 values of a word, rounded to nearest even (the first in the low half).
 __device__ __forceinline__ uint32_t two_bf16(float a, float b) {
@@ -42,119 +28,124 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b) {
     return w;
 }
 
-template <class T, bool VEC>
-__device__ __forceinline__ void store4(T *p, const float *v) {
-    if (!VEC) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = from_f32<T>(v[i]);
-    } else if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-        *reinterpret_cast<uint2 *>(p) = make_uint2(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]));
-    }
-}
-
-// A lane's eight values of the row at p: one access of 16 bytes of bf16 where they are neighbours.
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T *p, const Part &at, float (&v)[8]) {
-    if (VEC && sizeof(T) == 2 && at.hi == at.lo + 4) {
-        const uint4 w = *reinterpret_cast<const uint4 *>(p + at.lo);
-        v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
-        v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
-        v[4] = __uint_as_float(w.z << 16); v[5] = __uint_as_float(w.z & 0xFFFF0000u);
-        v[6] = __uint_as_float(w.w << 16); v[7] = __uint_as_float(w.w & 0xFFFF0000u);
-        return;
-    }
-    load4<T, VEC>(p + at.lo, v);
-    load4<T, VEC>(p + at.hi, v + 4);
-}
-
-template <class T, bool VEC>
-__device__ __forceinline__ void store8(T *p, const Part &at, const float (&v)[8]) {
-    if (VEC && sizeof(T) == 2 && at.hi == at.lo + 4) {
-        *reinterpret_cast<uint4 *>(p + at.lo) = make_uint4(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]),
-                                                           two_bf16(v[4], v[5]), two_bf16(v[6], v[7]));
-        return;
-    }
-    store4<T, VEC>(p + at.lo, v);
-    store4<T, VEC>(p + at.hi, v + 4);
-}
-
-// A lane's eight values as they lie in memory, to be kept in flight (VEC rows).
-template <class T>
-struct Raw8 {
-    uint4 w[sizeof(T) / 2];
+// A lane's values as they lie in memory, to be kept in flight.
+template <class T, int W>
+struct Raw {
+    uint32_t w[W * sizeof(T) / 4];
 };
-template <class T, bool VEC>
-__device__ __forceinline__ void load_raw(const T *p, const Part &at, Raw8<T> &r) {
-    if constexpr (!VEC) {
-        T v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p[i < 4 ? at.lo + i : at.hi + i - 4];
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                r.w[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
-                                    __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-        } else {
-            uint32_t u[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                u[i] = (uint32_t)__bfloat16_as_ushort(v[2 * i]) | (uint32_t)__bfloat16_as_ushort(v[2 * i + 1]) << 16;
-            r.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
-        }
-    } else if constexpr (sizeof(T) == 4) {
-        r.w[0] = *reinterpret_cast<const uint4 *>(p + at.lo);
-        r.w[1] = *reinterpret_cast<const uint4 *>(p + at.hi);
-    } else if (at.hi == at.lo + 4) {
-        r.w[0] = *reinterpret_cast<const uint4 *>(p + at.lo);
+
+// N words from or to p, in the widest pieces that its alignment (VEC: 16 bytes of W/2 values) allows.
+template <int N>
+__device__ __forceinline__ void words_in(const void *p, uint32_t *w) {
+    if constexpr (N == 2) {
+        const uint2 x = *static_cast<const uint2 *>(p);
+        w[0] = x.x; w[1] = x.y;
     } else {
-        const uint2 a = *reinterpret_cast<const uint2 *>(p + at.lo), b = *reinterpret_cast<const uint2 *>(p + at.hi);
-        r.w[0] = make_uint4(a.x, a.y, b.x, b.y);
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 x = static_cast<const uint4 *>(p)[i / 4];
+            w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
+        }
     }
 }
-template <class T>
-__device__ __forceinline__ void unpack(const Raw8<T> &r, float (&v)[8]) {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            v[4 * i] = __uint_as_float(r.w[i].x);
-            v[4 * i + 1] = __uint_as_float(r.w[i].y);
-            v[4 * i + 2] = __uint_as_float(r.w[i].z);
-            v[4 * i + 3] = __uint_as_float(r.w[i].w);
-        }
+template <int N>
+__device__ __forceinline__ void words_out(void *p, const uint32_t *w) {
+    if constexpr (N == 2) {
+        *static_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
     } else {
-        const uint32_t u[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(u[i] << 16);
-            v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+        for (int i = 0; i < N; i += 4) static_cast<uint4 *>(p)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+    }
+}
+
+template <class T, bool VEC, int W>
+__device__ __forceinline__ void load_raw(const T *p, const Part<W> &at, Raw<T, W> &r) {
+    constexpr int H = W * (int)sizeof(T) / 8;   // words of half of them
+    if constexpr (!VEC) {
+        T v[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = p[at.at(i)];
+#pragma unroll
+        for (int i = 0; i < 2 * H; ++i) {
+            if constexpr (sizeof(T) == 4)
+                r.w[i] = __float_as_uint(v[i]);
+            else
+                r.w[i] = (uint32_t)__bfloat16_as_ushort(v[2 * i]) | (uint32_t)__bfloat16_as_ushort(v[2 * i + 1]) << 16;
+        }
+    } else if (H < 4 && at.hi == at.lo + W / 2) {   // 16 bytes of neighbours
+        words_in<2 * H>(p + at.lo, r.w);
+    } else {
+        words_in<H>(p + at.lo, r.w);
+        words_in<H>(p + at.hi, r.w + H);
+    }
+}
+
+template <class T, int W>
+__device__ __forceinline__ void unpack(const Raw<T, W> &r, float (&v)[W]) {
+#pragma unroll
+    for (int i = 0; i < W * (int)sizeof(T) / 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v[i] = __uint_as_float(r.w[i]);
+        } else {
+            v[2 * i] = __uint_as_float(r.w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
         }
     }
 }
 
-// Turns lane li's eight values by the angles of cs (dir = -1: back).
-__device__ __forceinline__ void turn8(float (&v)[8], int li, int rotary, int halves, const float2 *cs,
-                                      float dir) {
-    if (8 * li >= rotary) return;
-    const float4 a = reinterpret_cast<const float4 *>(cs)[2 * li];
-    const float4 b = reinterpret_cast<const float4 *>(cs)[2 * li + 1];
-    const float co[4] = {a.x, a.z, b.x, b.z}, sn[4] = {a.y * dir, a.w * dir, b.y * dir, b.w * dir};
-    if (halves) {
+template <class T, bool VEC, int W>
+__device__ __forceinline__ void load_part(const T *p, const Part<W> &at, float (&v)[W]) {
+    Raw<T, W> r;
+    load_raw<T, VEC, W>(p, at, r);
+    unpack<T, W>(r, v);
+}
+
+template <class T, bool VEC, int W>
+__device__ __forceinline__ void store_part(T *p, const Part<W> &at, const float (&v)[W]) {
+    constexpr int H = W * (int)sizeof(T) / 8;
+    if constexpr (!VEC) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float x0 = v[e], x1 = v[e + 4];
-            v[e] = x0 * co[e] - x1 * sn[e];
-            v[e + 4] = x0 * sn[e] + x1 * co[e];
-        }
+        for (int i = 0; i < W; ++i) p[at.at(i)] = from_f32<T>(v[i]);
+        return;
+    }
+    uint32_t w[2 * H];
+#pragma unroll
+    for (int i = 0; i < 2 * H; ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
+        else w[i] = two_bf16(v[2 * i], v[2 * i + 1]);
+    }
+    if (H < 4 && at.hi == at.lo + W / 2) {
+        words_out<2 * H>(p + at.lo, w);
     } else {
+        words_out<H>(p + at.lo, w);
+        words_out<H>(p + at.hi, w + H);
+    }
+}
+
+// Turns lane li's values by the angles of cs (16-byte aligned; dir = -1: back).
+template <int W>
+__device__ __forceinline__ void turn(float (&v)[W], int li, int rotary, int halves, const float2 *cs, float dir) {
+    if (W * li >= rotary) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (8 * li + 2 * e < rotary) {
-                const float x0 = v[2 * e], x1 = v[2 * e + 1];
-                v[2 * e] = x0 * co[e] - x1 * sn[e];
-                v[2 * e + 1] = x0 * sn[e] + x1 * co[e];
+    for (int e = 0; e < W / 2; e += 2) {
+        const float4 a = reinterpret_cast<const float4 *>(cs)[(W / 2 * li + e) >> 1];
+        const float s0 = a.y * dir, s1 = a.w * dir;
+        if (halves) {
+            const float x0 = v[e], x1 = v[e + W / 2], y0 = v[e + 1], y1 = v[e + 1 + W / 2];
+            v[e] = x0 * a.x - x1 * s0;
+            v[e + W / 2] = x0 * s0 + x1 * a.x;
+            v[e + 1] = y0 * a.z - y1 * s1;
+            v[e + 1 + W / 2] = y0 * s1 + y1 * a.z;
+        } else if (W * li + 2 * e < rotary) {
+            const float x0 = v[2 * e], x1 = v[2 * e + 1];
+            v[2 * e] = x0 * a.x - x1 * s0;
+            v[2 * e + 1] = x0 * s0 + x1 * a.x;
+            if (W * li + 2 * e + 2 < rotary) {
+                const float y0 = v[2 * e + 2], y1 = v[2 * e + 3];
+                v[2 * e + 2] = y0 * a.z - y1 * s1;
+                v[2 * e + 3] = y0 * s1 + y1 * a.z;
             }
+        }
     }
 }
 
@@ -169,6 +160,7 @@ __device__ __forceinline__ float2 angle_of(uint64_t phi, int t) {
 
 // Sum over the `lanes` (a power of two) neighbouring lanes of a row.
 __device__ __forceinline__ float group_sum(float x, int lanes) {
+#pragma unroll
     for (int o = lanes >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }

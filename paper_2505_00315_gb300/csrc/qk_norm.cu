@@ -4,10 +4,10 @@
 // and backward, with g = R(t)^T dy (the rotation's transpose turns back),
 //     dgamma = sum g r x,  u = g gamma,  dx = r (u - r x mean(u r x)).
 // Memory bound: x and y move once, forward; x, dy and dx backward (r is computed
-// again from x, which is read anyway).  A head's hp values lie on hp/8 lanes, eight a
-// lane (16 bytes of bf16), so the mean is a few shuffles and nothing is staged; a
-// block takes some tokens with all their heads and computes each token's sines
-// and cosines once for all of them, in shared memory.
+// again from x, which is read anyway).  A head's hp values lie on hp/W lanes, W = 16 a
+// lane where the rows' places allow it (32 bytes of bf16), else 8, so that the mean is a few
+// shuffles and nothing is staged; a block takes some tokens with all their heads and
+// computes each token's sines and cosines once for all of them, in shared memory.
 #include <cmath>
 
 #include "head_rows.cuh"
@@ -32,7 +32,7 @@ namespace {
 
 constexpr int kThreads = 256;
 // Tokens of one item: 64 bytes of loads that a lane keeps in flight while it works on the last.
-constexpr int batch_of(int esize, bool backward) { return (esize == 2 ? 4 : 2) / (backward ? 2 : 1); }
+constexpr int batch_of(int lane_bytes, bool backward) { return (backward ? 32 : 64) / lane_bytes; }
 constexpr int kMaxTokens = 8;   // tokens of one block's step
 
 struct NormArgs {
@@ -51,25 +51,25 @@ struct StepTokens {
     long long in[2][kMaxTokens], y[2][kMaxTokens], d[2][kMaxTokens];   // [queries, keys]
 };
 
-template <class T, bool VEC, bool kBackward, int LG>
+template <class T, bool VEC, bool kBackward, int W, int LG>
 __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kernel(const __grid_constant__ NormArgs p,
                                                                 const __grid_constant__ Turns tab) {
-    constexpr int groups = kThreads / LG, hp = 8 * LG;
-    constexpr int kBatch = batch_of(sizeof(T), kBackward);
+    constexpr int groups = kThreads / LG, hp = W * LG;
+    constexpr int kBatch = batch_of(W * sizeof(T), kBackward);
     __shared__ StepTokens st;
     __shared__ float gamma[2][hp];
     extern __shared__ float red[];   // backward: [groups][2][hp]
     const Norm &n = p.n;
     const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
-    const Part at(li, n.rotary, n.halves);
+    const Part<W> at(li, n.rotary, n.halves);
     const long long N = (long long)n.B * n.T;
     for (int e = threadIdx.x; e < 2 * hp; e += kThreads) {
         const T *g = static_cast<const T *>(e < hp ? p.gq : p.gk);
         gamma[e / hp][e % hp] = g == nullptr ? 1.f : to_f32(g[e % hp]);
     }
-    float acc[2][8];   // backward: this lane's sums of g r x, of queries and keys
+    float acc[2][W];   // backward: this lane's sums of g r x, of queries and keys
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[0][e] = acc[1][e] = 0.f;
+    for (int e = 0; e < W; ++e) acc[0][e] = acc[1][e] = 0.f;
     const int HH = n.H + n.Hkv;   // heads 0 .. H-1 are queries, the others keys
     const int pairs = n.rotary >> 1;
     for (long long tok0 = (long long)blockIdx.x * p.step; tok0 < N; tok0 += (long long)gridDim.x * p.step) {
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
         // items of `batch` tokens of one head, one a lane group; the next item's loads are under way
         // while one is worked on
         const int items = (tokens + p.batch - 1) / p.batch * HH;
-        Raw8<T> x[2][kBatch], dy[2][kBackward ? kBatch : 1];
+        Raw<T, W> x[2][kBatch], dy[2][kBackward ? kBatch : 1];
         struct Item {
             int key, h, i0, count;
         };
@@ -99,45 +99,48 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
             const int key = hh >= n.H;
             return Item{key, key ? hh - n.H : hh, i0, it < items ? min(p.batch, tokens - i0) : 0};
         };
-        auto load = [&](const Item &w, Raw8<T> (&xr)[kBatch], Raw8<T> (&yr)[kBackward ? kBatch : 1]) {
+        auto load = [&](const Item &w, Raw<T, W> (&xr)[kBatch], Raw<T, W> (&yr)[kBackward ? kBatch : 1]) {
             const T *in = static_cast<const T *>(w.key ? p.k : p.q) + w.h * (w.key ? n.k.h : n.q.h);
             const T *gr = static_cast<const T *>(w.key ? p.dyk : p.dyq) + w.h * (w.key ? n.yk.h : n.yq.h);
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 if (u < w.count) {
-                    load_raw<T, VEC>(in + st.in[w.key][w.i0 + u], at, xr[u]);
-                    if (kBackward) load_raw<T, VEC>(gr + st.y[w.key][w.i0 + u], at, yr[kBackward ? u : 0]);
+                    load_raw<T, VEC, W>(in + st.in[w.key][w.i0 + u], at, xr[u]);
+                    if (kBackward) load_raw<T, VEC, W>(gr + st.y[w.key][w.i0 + u], at, yr[kBackward ? u : 0]);
                 }
             }
         };
-        auto work = [&](const Item &w, Raw8<T> (&xr)[kBatch], Raw8<T> (&yr)[kBackward ? kBatch : 1]) {
+        auto work = [&](const Item &w, Raw<T, W> (&xr)[kBatch], Raw<T, W> (&yr)[kBackward ? kBatch : 1]) {
             T *out = static_cast<T *>(w.key ? p.ok : p.oq) +
                      w.h * (kBackward ? (w.key ? n.dk.h : n.dq.h) : (w.key ? n.yk.h : n.yq.h));
-            const float4 ga = *reinterpret_cast<const float4 *>(&gamma[w.key][at.lo]);
-            const float4 gb = *reinterpret_cast<const float4 *>(&gamma[w.key][at.hi]);
-            const float gm[8] = {ga.x, ga.y, ga.z, ga.w, gb.x, gb.y, gb.z, gb.w};
+            float gm[W];
+#pragma unroll
+            for (int e = 0; e < W; e += 4) {
+                const float4 g4 = *reinterpret_cast<const float4 *>(&gamma[w.key][at.at(e)]);
+                gm[e] = g4.x; gm[e + 1] = g4.y; gm[e + 2] = g4.z; gm[e + 3] = g4.w;
+            }
             const float isq = w.key ? 0.f : 1.f, isk = w.key ? 1.f : 0.f;
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 if (u >= p.batch) break;
                 const bool on = u < w.count;
                 const float2 *cs = st.cs[on ? w.i0 + u : 0];
-                float v[8], ss = 0.f;
-                unpack<T>(xr[u], v);
+                float v[W], ss = 0.f;
+                unpack<T, W>(xr[u], v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], ss);
+                for (int e = 0; e < W; ++e) ss = fmaf(v[e], v[e], ss);
                 const float r = rsqrtf(fmaf(group_sum(ss, LG), 1.f / hp, n.eps));
                 if (!kBackward) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] *= r * gm[e];
-                    turn8(v, li, n.rotary, n.halves, cs, 1.f);
-                    if (on) store8<T, VEC>(out + st.y[w.key][w.i0 + u], at, v);
+                    for (int e = 0; e < W; ++e) v[e] *= r * gm[e];
+                    turn<W>(v, li, n.rotary, n.halves, cs, 1.f);
+                    if (on) store_part<T, VEC, W>(out + st.y[w.key][w.i0 + u], at, v);
                 } else {
-                    float g[8], dot = 0.f;
-                    unpack<T>(yr[kBackward ? u : 0], g);
-                    turn8(g, li, n.rotary, n.halves, cs, -1.f);
+                    float g[W], dot = 0.f;
+                    unpack<T, W>(yr[kBackward ? u : 0], g);
+                    turn<W>(g, li, n.rotary, n.halves, cs, -1.f);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
+                    for (int e = 0; e < W; ++e) {
                         v[e] *= r;
                         const float d = on ? g[e] * v[e] : 0.f;
                         acc[0][e] = fmaf(d, isq, acc[0][e]);
@@ -147,8 +150,8 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
                     }
                     dot = group_sum(dot, LG) * (1.f / hp);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) g[e] = r * fmaf(-v[e], dot, g[e]);
-                    if (on) store8<T, VEC>(out + st.d[w.key][w.i0 + u], at, g);
+                    for (int e = 0; e < W; ++e) g[e] = r * fmaf(-v[e], dot, g[e]);
+                    if (on) store_part<T, VEC, W>(out + st.d[w.key][w.i0 + u], at, g);
                 }
             }
         };
@@ -173,8 +176,8 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
     }
     if (kBackward && p.partial != nullptr) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int c = e < 4 ? at.lo + e : at.hi + e - 4;
+        for (int e = 0; e < W; ++e) {
+            const int c = at.at(e);
             red[(grp * 2 + 0) * hp + c] = acc[0][e];
             red[(grp * 2 + 1) * hp + c] = acc[1][e];
         }
@@ -218,25 +221,32 @@ int bwd_blocks(const Norm &n) {
     return (int)(steps < kMaxBlocks ? steps : kMaxBlocks);
 }
 
-template <bool kBackward, class T, bool VEC>
+// Values of a lane: 16 where rows are whole 16-byte pieces of bf16 and rotated halves split into
+// eights.  B4 T4096 H32 + 8 of 128: 16 a lane FWD16, 8 a lane FWD8.
+bool wide(const Norm &n, bool vec) { return n.bf16 && vec && (!n.halves || n.rotary % 16 == 0); }
+
+template <bool kBackward, class T, bool VEC, int W>
 cudaError_t launch_of(const NormArgs &p, unsigned blocks, cudaStream_t s) {
     const Turns tab = make_turns(p.n.rotary, p.n.theta);
-    const int smem = kBackward ? kThreads / (p.n.hp / 8) * 2 * p.n.hp * 4 : 0;   // 16 KB
+    const int smem = kBackward ? kThreads * W * 2 * 4 : 0;   // 16 or 32 KB
     switch (p.n.hp) {
-        case 16: qk_norm_rope_kernel<T, VEC, kBackward, 2><<<blocks, kThreads, smem, s>>>(p, tab); break;
-        case 32: qk_norm_rope_kernel<T, VEC, kBackward, 4><<<blocks, kThreads, smem, s>>>(p, tab); break;
-        case 64: qk_norm_rope_kernel<T, VEC, kBackward, 8><<<blocks, kThreads, smem, s>>>(p, tab); break;
-        default: qk_norm_rope_kernel<T, VEC, kBackward, 16><<<blocks, kThreads, smem, s>>>(p, tab); break;
+        case 16: qk_norm_rope_kernel<T, VEC, kBackward, W, 16 / W><<<blocks, kThreads, smem, s>>>(p, tab); break;
+        case 32: qk_norm_rope_kernel<T, VEC, kBackward, W, 32 / W><<<blocks, kThreads, smem, s>>>(p, tab); break;
+        case 64: qk_norm_rope_kernel<T, VEC, kBackward, W, 64 / W><<<blocks, kThreads, smem, s>>>(p, tab); break;
+        default: qk_norm_rope_kernel<T, VEC, kBackward, W, 128 / W><<<blocks, kThreads, smem, s>>>(p, tab); break;
     }
     note_launches(1);
     return cudaGetLastError();
 }
 
 template <bool kBackward>
-cudaError_t launch(const NormArgs &p, bool vec, unsigned blocks, cudaStream_t s) {
+cudaError_t launch(NormArgs p, bool vec, unsigned blocks, cudaStream_t s) {
+    const bool w16 = wide(p.n, vec);
+    if (p.step > 1) p.batch = batch_of((w16 ? 16 : 8) * (p.n.bf16 ? 2 : 4), kBackward);
+    if (w16) return launch_of<kBackward, bf16, true, 16>(p, blocks, s);
     if (p.n.bf16)
-        return vec ? launch_of<kBackward, bf16, true>(p, blocks, s) : launch_of<kBackward, bf16, false>(p, blocks, s);
-    return vec ? launch_of<kBackward, float, true>(p, blocks, s) : launch_of<kBackward, float, false>(p, blocks, s);
+        return vec ? launch_of<kBackward, bf16, true, 8>(p, blocks, s) : launch_of<kBackward, bf16, false, 8>(p, blocks, s);
+    return vec ? launch_of<kBackward, float, true, 8>(p, blocks, s) : launch_of<kBackward, float, false, 8>(p, blocks, s);
 }
 
 }  // namespace
@@ -245,8 +255,7 @@ size_t norm_workspace(const Norm &n) { return (size_t)bwd_blocks(n) * 2 * n.hp *
 
 cudaError_t launch_norm(const Norm &n, const void *q, const void *k, const void *gq, const void *gk,
                         const int32_t *pos, void *yq, void *yk, cudaStream_t s) {
-    NormArgs p{n, q, k, gq, gk, nullptr, nullptr, yq, yk, pos, nullptr, many(n) ? kMaxTokens : 1,
-               many(n) ? batch_of(n.bf16 ? 2 : 4, false) : 1};
+    NormArgs p{n, q, k, gq, gk, nullptr, nullptr, yq, yk, pos, nullptr, many(n) ? kMaxTokens : 1, 1};
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) && rows16(yq, n.yq, n.bf16) &&
                      rows16(yk, n.yk, n.bf16);
     const long long N = (long long)n.B * n.T;
@@ -258,7 +267,7 @@ cudaError_t launch_norm_bwd(const Norm &n, const void *q, const void *k, const v
                             void *dq, void *dk, float *dgq, float *dgk, void *ws, cudaStream_t s) {
     const bool sums = dgq != nullptr || dgk != nullptr;
     NormArgs p{n, q, k, gq, gk, dyq, dyk, dq, dk, pos, sums ? (float *)ws : nullptr,
-               many(n) ? kMaxTokens : 1, many(n) ? batch_of(n.bf16 ? 2 : 4, true) : 1};
+               many(n) ? kMaxTokens : 1, 1};
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) &&
                      rows16(dyq, n.yq, n.bf16) && rows16(dyk, n.yk, n.bf16) &&
                      rows16(dq, n.dq, n.bf16) && rows16(dk, n.dk, n.bf16);

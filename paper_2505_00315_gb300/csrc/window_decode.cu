@@ -79,7 +79,7 @@ __device__ __forceinline__ bool decode_prologue(const DecodeArgs &p, const Turns
     for (int e = threadIdx.x; e < d.rotary / 2; e += THREADS) cs[e] = angle_of(tab.phi[e], at);
     __syncthreads();
     const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
-    const Part part(li, d.rotary, d.halves);
+    const Part<8> part(li, d.rotary, d.halves);
     for (int u0 = 0; u0 < GT + 1; u0 += THREADS / LG) {   // (all lanes together: the sums are shuffles)
         const int u = u0 + grp;
         const bool key = u == GT, on = u < heads || (key && newest);
@@ -87,10 +87,10 @@ __device__ __forceinline__ bool decode_prologue(const DecodeArgs &p, const Turns
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.f, gm[e] = 1.f;
         if (on) {
-            load8<T, false>(key ? (const T *)p.k + d.k.at(b, 0, hk)
+            load_part<T, false, 8>(key ? (const T *)p.k + d.k.at(b, 0, hk)
                                 : (const T *)p.q + d.q.at(b, 0, hk * G + g0 + u), part, x);
             const T *gamma = (const T *)(key ? p.gk : p.gq);
-            if (d.norm && gamma != nullptr) load8<T, false>(gamma, part, gm);
+            if (d.norm && gamma != nullptr) load_part<T, false, 8>(gamma, part, gm);
         }
         if (d.norm) {
             float ss = 0.f;
@@ -100,10 +100,10 @@ __device__ __forceinline__ bool decode_prologue(const DecodeArgs &p, const Turns
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= r * gm[e];
         }
-        turn8(x, li, d.rotary, d.halves, cs, 1.f);
+        turn<8>(x, li, d.rotary, d.halves, cs, 1.f);
         if (on && key) {
             const int slot = seen->slot(n - 1);
-            store8<T, false>((T *)p.kc + d.kc.at(b, slot, hk), part, x);
+            store_part<T, false, 8>((T *)p.kc + d.kc.at(b, slot, hk), part, x);
             const T *v = (const T *)p.v + d.v.at(b, 0, hk);
             T *o = (T *)p.vc + d.vc.at(b, slot, hk);
 #pragma unroll
@@ -111,7 +111,7 @@ __device__ __forceinline__ bool decode_prologue(const DecodeArgs &p, const Turns
         } else if (u < GT) {
             const float f = d.scale * kLog2e;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sq[u][e < 4 ? part.lo + e : part.hi + e - 4] = x[e] * f;
+            for (int e = 0; e < 8; ++e) sq[u][part.at(e)] = x[e] * f;
         }
     }
     __syncthreads();
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_co
     __shared__ __align__(16) float sm_o[kWarps][GT][HD];
     Seen seen;
     if (!decode_prologue<T, HD, GT, kThreads>(p, tab, split, hk, b, g0, heads, sq, &seen)) return;
-    const Part part(threadIdx.x % LK, 0, 0);
+    const Part<8> part(threadIdx.x % LK, 0, 0);
     const T *Kb = (const T *)p.kc + d.kc.at(b, 0, hk), *Vb = (const T *)p.vc + d.vc.at(b, 0, hk);
     float q[GT][8], acc[GT][8], m[GT], l[GT];
 #pragma unroll
@@ -186,8 +186,8 @@ __global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_co
             const int u = u0 + j * kRows + lane / LK, slot = seen.slot(u);
             on[j] = u < seen.hi;
             if (on[j]) {
-                load8<T, VEC>(Kb + (long long)slot * d.kc.t, part, kx[j]);
-                load8<T, VEC>(Vb + (long long)slot * d.vc.t, part, vx[j]);
+                load_part<T, VEC, 8>(Kb + (long long)slot * d.kc.t, part, kx[j]);
+                load_part<T, VEC, 8>(Vb + (long long)slot * d.vc.t, part, vx[j]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) kx[j][e] = vx[j][e] = 0.f;

@@ -411,47 +411,82 @@ __global__ void __launch_bounds__(256) window_sink_rows_kernel(Attn a, const flo
     }
 }
 
-// One thread per 8 values of a row: hp/8 lanes a row.
+// D: eight values a lane, hp/8 lanes a row (a power of two), four such items a thread in flight.
+// Reads O, dO and what O's rounding left once: memory bound.
+constexpr int kDeltaItems = 4;
+
 template <class T>
 __global__ void __launch_bounds__(256) window_delta_kernel(Attn a, const T *O, const T *dO,
                                                            const bf16 *rest, float *delta, bool vec) {
-    const int lanes = a.hp / 8;
-    const long long g = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long rows = (long long)a.B * a.Tq * a.H;
-    const long long row = g / lanes;
-    const int c = (int)(g % lanes) * 8;
-    float sum = 0.f;
-    int b = 0, h = 0, t = 0;
-    if (row < rows) {
-        h = (int)(row % a.H);
-        t = (int)(row / a.H % a.Tq);
-        b = (int)(row / a.H / a.Tq);
-        const T *x = O + a.o.at(b, t, h) + c, *y = dO + a.go.at(b, t, h) + c;
-        alignas(16) T u[8], w[8];
+    constexpr int V = 8 * sizeof(T) / 16;
+    const int lg = 31 - __clz(a.hp >> 3), U = a.H << lg;   // items of one token
+    const long long all = (long long)a.B * a.Tq * U, base = (long long)blockIdx.x * (256 * kDeltaItems);
+    const long long tok0 = base / U;
+    const int rem0 = (int)(base - tok0 * U), b0 = (int)(tok0 / a.Tq), t0 = (int)(tok0 - (long long)b0 * a.Tq);
+    const Str pk = a.packed();
+    uint4 u[kDeltaItems][V], w[kDeltaItems][V], e[kDeltaItems];
+    int bb[kDeltaItems], tt[kDeltaItems], hc[kDeltaItems];
+#pragma unroll
+    for (int i = 0; i < kDeltaItems; ++i) {
+        const int x = rem0 + threadIdx.x + 256 * i, tok = x / U, r = x - tok * U;
+        const int over = (t0 + tok) / a.Tq, b = b0 + over, t = t0 + tok - over * a.Tq;
+        const int h = r >> lg, c = (r & ((1 << lg) - 1)) << 3;
+        bb[i] = b;
+        tt[i] = t;
+        hc[i] = h;
+        e[i] = make_uint4(0, 0, 0, 0);
+        if (base + threadIdx.x + 256 * i >= all) {
+            bb[i] = -1;
+#pragma unroll
+            for (int k = 0; k < V; ++k) u[i][k] = w[i][k] = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        const T *po = O + a.o.at(b, t, h) + c, *pg = dO + a.go.at(b, t, h) + c;
         if (vec) {
 #pragma unroll
-            for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i) {
-                reinterpret_cast<uint4 *>(u)[i] = reinterpret_cast<const uint4 *>(x)[i];
-                reinterpret_cast<uint4 *>(w)[i] = reinterpret_cast<const uint4 *>(y)[i];
+            for (int k = 0; k < V; ++k) {
+                u[i][k] = reinterpret_cast<const uint4 *>(po)[k];
+                w[i][k] = reinterpret_cast<const uint4 *>(pg)[k];
             }
         } else {
+            alignas(16) T x8[8], y8[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = x[i], w[i] = y[i];
+            for (int k = 0; k < 8; ++k) x8[k] = po[k], y8[k] = pg[k];
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                u[i][k] = reinterpret_cast<const uint4 *>(x8)[k];
+                w[i][k] = reinterpret_cast<const uint4 *>(y8)[k];
+            }
         }
-        float o[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = to_f32(u[i]);
-        if (rest != nullptr) {
-            alignas(16) bf16 e[8];
-            *reinterpret_cast<uint4 *>(e) = *reinterpret_cast<const uint4 *>(rest + a.packed().at(b, t, h) + c);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] += to_f32(e[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(o[i], to_f32(w[i]), sum);
+        if (rest != nullptr) e[i] = *reinterpret_cast<const uint4 *>(rest + pk.at(b, t, h) + c);
     }
-    for (int o = lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (row < rows && c == 0) delta[((long long)b * a.H + h) * a.Tq + t] = sum;
+#pragma unroll
+    for (int i = 0; i < kDeltaItems; ++i) {
+        float sum = 0.f;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                sum = fmaf(__uint_as_float(u[i][k].x), __uint_as_float(w[i][k].x), sum);
+                sum = fmaf(__uint_as_float(u[i][k].y), __uint_as_float(w[i][k].y), sum);
+                sum = fmaf(__uint_as_float(u[i][k].z), __uint_as_float(w[i][k].z), sum);
+                sum = fmaf(__uint_as_float(u[i][k].w), __uint_as_float(w[i][k].w), sum);
+            }
+        } else {
+            const uint32_t ou[4] = {u[i][0].x, u[i][0].y, u[i][0].z, u[i][0].w};
+            const uint32_t gu[4] = {w[i][0].x, w[i][0].y, w[i][0].z, w[i][0].w};
+            const uint32_t eu[4] = {e[i].x, e[i].y, e[i].z, e[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                sum = fmaf(__uint_as_float(ou[k] << 16) + __uint_as_float(eu[k] << 16),
+                           __uint_as_float(gu[k] << 16), sum);
+                sum = fmaf(__uint_as_float(ou[k] & 0xFFFF0000u) + __uint_as_float(eu[k] & 0xFFFF0000u),
+                           __uint_as_float(gu[k] & 0xFFFF0000u), sum);
+            }
+        }
+        for (int o = 1 << lg >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (bb[i] >= 0 && (threadIdx.x & ((1 << lg) - 1)) == 0)
+            delta[((long long)bb[i] * a.H + hc[i]) * a.Tq + tt[i]] = sum;
+    }
 }
 
 template <int HD>
@@ -573,7 +608,7 @@ cudaError_t window_delta(const Attn &a, const void *O, const bf16 *rest, const v
                          cudaStream_t s) {
     const long long n = (long long)a.B * a.Tq * a.H * (a.hp / 8);
     const bool vec = rows16(O, a.o, a.bf16) && rows16(dO, a.go, a.bf16);
-    const dim3 grid((unsigned)((n + 255) / 256));
+    const dim3 grid((unsigned)((n + 256 * kDeltaItems - 1) / (256 * kDeltaItems)));
     if (a.bf16)
         window_delta_kernel<bf16><<<grid, 256, 0, s>>>(a, (const bf16 *)O, (const bf16 *)dO, rest, delta,
                                                         vec);
