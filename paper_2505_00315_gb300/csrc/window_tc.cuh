@@ -172,6 +172,19 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
     const uint32_t a = lo <= 0 ? ~0u : lo > 31 ? 0u : ~0u << lo;
     return hi < 0 ? 0u : hi >= 31 ? a : a & ((2u << hi) - 1u);
 }
+// The blocks that all of the queries pf .. pl see whole are far blocks 0 .. far_whole-1 and near blocks
+// lo .. hi-1.
+struct WholeBlocks {
+    int far_whole, lo, hi;
+    __device__ __forceinline__ WholeBlocks(const KeyBlocks<128> &kb, int pf, int pl, int window) {
+        far_whole = kb.slim / 128;
+        lo = kb.far;
+        while (lo < kb.count() && !kb.whole(lo, pf, pl, window)) ++lo;
+        hi = kb.count();
+        while (hi > lo && !kb.whole(hi - 1, pf, pl, window)) --hi;
+    }
+    __device__ __forceinline__ bool has(int j) const { return j < far_whole || (j >= lo && j < hi); }
+};
 // Which of the 32 columns from c0 on of key block j (start ks) position pos sees, as bits.
 __device__ __forceinline__ uint32_t seen_bits(const KeyBlocks<128> &kb, int j, int ks, int c0, int pos,
                                               int window, int sinks) {

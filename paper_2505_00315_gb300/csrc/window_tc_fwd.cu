@@ -202,12 +202,15 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
             const int cq = warp >> 2, q = warp & 3, r = q * 32 + lane, pos = pf + r;
             const uint32_t lanes = (uint32_t)(q * 32) << 16, tmy = tS + lanes + 32 * cq;
             const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
-            float m = -INFINITY, l = 0.f;
+            const WholeBlocks wb(kb, pf, pl, p.window);
+            float *const part0 = &sm.part[0][0][r];
+            float m = -1e38f, l = 0.f;   // (m: below every score, and finite)
+#pragma unroll 1
             for (int j = 0; j < n; ++j, ++phase) {
-                const bool whole = kb.whole(j, pf, pl, p.window);
+                const bool whole = wb.has(j);
                 uint32_t seen = ~0u;
                 if (!whole) seen = seen_bits(kb, j, kb.start(j), 32 * cq, pos, p.window, p.sinks);
-                ok = wait_or_abort(sm.s_full, phase & 1, &sm.abort, p.status) && ok;
+                wait_or_abort(sm.s_full, phase & 1, &sm.abort, p.status);
                 tc_fence_after();
                 float s[32];
                 tmem_get32(tmy, s);
@@ -226,16 +229,15 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     mx[0] = max3(mx[0], s[c], s[c + 1]);
                     mx[1] = max3(mx[1], s[c + 2], s[c + 3]);
                 }
-                float (*part)[kQ] = sm.part[phase & 1];
                 // (the buffer of this parity was last read before the last block's barrier)
-                part[cq][r] = fmaxf(mx[0], mx[1]);
+                float *const part = part0 + (phase & 1) * (4 * kQ);
+                part[cq * kQ] = fmaxf(mx[0], mx[1]);
                 named_barrier(1 + q, 128);
-                const float mb = fmaxf(max3(part[0][r], part[1][r], part[2][r]), part[3][r]) * p.scale_log2;
+                const float mb = fmaxf(max3(part[0], part[kQ], part[2 * kQ]), part[3 * kQ]) * p.scale_log2;
                 const bool grow = mb > m + kRescaleLog2;   // the same in all four threads of the row
-                const float m_new = grow ? mb : m;
-                const float corr = grow ? exp2_fast(m - m_new) : 1.f;   // 0 on a row's first block
-                const float base = m_new == -INFINITY ? 0.f : m_new;
-                const float2 neg = make_float2(-base, -base);
+                const float corr = grow ? exp2_fast(m - mb) : 1.f;   // 0 on a row's first block
+                if (grow) m = mb;
+                const float2 neg = make_float2(-m, -m);
                 float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
@@ -246,11 +248,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     sum.y += s[c + 1];
                 }
                 l = l * corr + (sum.x + sum.y);
-                m = m_new;
-                if (pass == 1 && !whole) {
+                if (!whole && pass == 1) {
                     // V rows with NaN or infinities: zeroed, and NaN for the rows that see them
                     const int t = item + v_tile<kEarly>(j, n);
-                    ok = wait_or_abort(sm.kv_full[t % NS], (t / NS) & 1, &sm.abort, p.status) && ok;
+                    wait_or_abort(sm.kv_full[t % NS], (t / NS) & 1, &sm.abort, p.status);
                     if (cq == 0) {
                         const uint32_t odd = __ballot_sync(0xffffffffu, clean_row<NB>(sm.kv[t % NS][0], r));
                         if (lane == 0) sm.odd[q] = odd;
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
 #pragma unroll
                 for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
                 if (kEarly && j > 0) {   // P and O may be written: P_{j-1} V_{j-1} is done
-                    ok = wait_or_abort(sm.pv_done, (phase & 1) ^ 1, &sm.abort, p.status) && ok;
+                    wait_or_abort(sm.pv_done, (phase & 1) ^ 1, &sm.abort, p.status);
                     tc_fence_after();
                 }
                 tmem_st16_async(kEarly ? tP + lanes + 16 * cq : tmy, w);
@@ -284,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                 warp_arrive(sm.p_ready, lane);
             }
             item += 2 * n;
-            ok = wait_or_abort(sm.o_done, pass, &sm.abort, p.status) && ok;
+            wait_or_abort(sm.o_done, pass, &sm.abort, p.status);
             tc_fence_after();
             float o[HD / 64][16];   // this thread's quarter of the columns
             float odd = 0.f;
