@@ -29,6 +29,8 @@
 // query rows whose lse or D is not finite are zeroed in shared memory (their P is NaN where it
 // is seen).  dQ: a CTA whose results are not all finite runs a second time with such rows of
 // K zeroed (a query that sees one has lse NaN).
+#include <algorithm>
+
 #include "launch.h"
 #include "profile.h"
 #include "window_tc.cuh"
@@ -42,7 +44,7 @@ constexpr int kWarps = 16, kWorkers = 32 * kWarps;   // the workers'
 constexpr int kCols = 128 / (kWarps / 4);            // score columns of one worker thread
 
 struct BwdArgs {
-    Map q, k, v, go, dq, dk, dv;
+    Map q, k, v, go, dk, dv;
     const int32_t *lens;
     const float *lse, *delta;           // [B, H, Tq]
     bf16 *dQ, *dK, *dV;
@@ -393,39 +395,50 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
 
 // ---------------------------------------------------------------------- dQ
 
+// CTAs stay for several tiles (one CTA an SM), so that a tile's loads and first scores run beside the
+// end of the tile before: Q and dO are free once the last dP is done, and dQ is read out while the
+// next scores are computed.
+constexpr int kMaxTiles = 64;   // of one CTA
+
 template <int HD>
 struct QSm {
     static constexpr int NB = HD / 64;
     uint8_t q[NB][kBlk], go[NB][kBlk];
     uint8_t k[3][NB][kBlk], v[2][NB][kBlk];
-    uint64_t q_full, k_full[3], k_empty[3], v_full[2], v_empty[2];
-    uint64_t s_full[2], dp_full, ds_ready, done, drained;
+    uint64_t q_full, q_empty, k_full[3], k_empty[3], v_full[2], v_empty[2];
+    uint64_t s_full[2], dp_full, ds_ready, dq_full, dq_empty, drained;
     uint32_t tmem;
     int abort, redo;
+    uint8_t again[kMaxTiles];   // tiles whose results are not all finite
 };
 
 constexpr int kQThreads = kWorkers + 64;
 
+// The x-th query tile of all, heaviest of a head first.
+struct QueryTile {
+    int b, h, i0, pf, pl;
+    __device__ __forceinline__ QueryTile(const BwdArgs &p, long long x, int tiles) {
+        const long long rest = x / tiles;
+        i0 = (tiles - 1 - (int)(x - rest * tiles)) * kTile;
+        b = (int)(rest / p.H);
+        h = (int)(rest - (long long)b * p.H);
+        pf = p.Tk - p.Tq + i0;
+        pl = min(p.Tk - p.Tq + min(i0 + kTile, p.Tq), seq_len(p.lens, b, p.Tk)) - 1;
+    }
+    __device__ __forceinline__ bool empty() const { return pl < pf; }
+};
+
 template <int HD>
-__global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid_constant__ BwdArgs p) {
+__global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid_constant__ BwdArgs p,
+                                                                    long long all, int tiles) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using Sm = QSm<HD>;
     constexpr int NB = Sm::NB;
     Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = blockIdx.z, h = blockIdx.y, hk = h / p.G, off = p.Tk - p.Tq;
-    const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kTile;
-    const int len = seq_len(p.lens, b, p.Tk);
-    const int pf = off + i0, pl = min(off + min(i0 + kTile, p.Tq), len) - 1;
-    if (pl < pf) {
-        const int rows = min(kTile, p.Tq - i0), units = p.hp / 8;
-        for (int e = threadIdx.x; e < rows * units; e += kQThreads)
-            *reinterpret_cast<uint4 *>(p.dQ + p.sdq.at(b, i0 + e / units, h) + e % units * 8) =
-                make_uint4(0, 0, 0, 0);
-        return;
-    }
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&sm.q_full), 1);
+        mbar_init(smem_u32(&sm.q_empty), 1);
         for (int s = 0; s < 3; ++s) {
             mbar_init(smem_u32(&sm.k_full[s]), 1);
             mbar_init(smem_u32(&sm.k_empty[s]), 1);
@@ -437,9 +450,11 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
         }
         mbar_init(smem_u32(&sm.dp_full), 1);
         mbar_init(smem_u32(&sm.ds_ready), kWarps);
-        mbar_init(smem_u32(&sm.done), 1);
+        mbar_init(smem_u32(&sm.dq_full), 1);
+        mbar_init(smem_u32(&sm.dq_empty), kWarps);
         mbar_init(smem_u32(&sm.drained), 1);
         sm.abort = sm.redo = 0;
+        for (int x = 0; x < kMaxTiles; ++x) sm.again[x] = 0;
         fence_barrier_init();
     }
     if (warp == kWarps) {
@@ -450,42 +465,48 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
     __syncthreads();
     tc_fence_after();
     const uint32_t tS = sm.tmem, tG = tS + 256, tdQ = tS + 384;   // S buffers at tS, tS + 128
-    const KeyBlocks<kTile> kb(pf, pl, p.window, p.sinks);
-    const int n = kb.count();
     auto wait = [&](uint64_t &bar, uint32_t parity) {
         return wait_or_abort(bar, parity, &sm.abort, p.status);
     };
+    // Tiles and key blocks of both passes are numbered on (it, g); the S of block g lies in buffer
+    // g & 1.  The second pass takes the tiles marked in `again`.
     bool ok = true;
-    // Key blocks of both passes are numbered on: block j of pass 1 is number n + j, and its S
-    // lies in buffer number & 1.
+    int it = 0, g = 0;
     for (int pass = 0; pass < 2; ++pass) {
-        const int g0 = pass * n;
         if (warp == kWarps) {
             if (lane == 0) {
-                if (pass == 0) {
+                int nq = it, nk = g, nv = g;
+                for (int t = 0; ok; ++t) {
+                    const long long x = blockIdx.x + (long long)t * gridDim.x;
+                    if (x >= all) break;
+                    if (pass == 1 && sm.again[t] == 0) continue;
+                    const QueryTile w(p, x, tiles);
+                    if (w.empty()) continue;
+                    const KeyBlocks<kTile> kb(w.pf, w.pl, p.window, p.sinks);
+                    const int hk = w.h / p.G;
+                    if (!(ok = wait(sm.q_empty, (it & 1) ^ 1))) break;
                     mbar_expect_tx(smem_u32(&sm.q_full), 2 * NB * kBlk);
                     for (int c = 0; c < NB; ++c) {
-                        load_box(smem_u32(sm.q[c]), p.q, smem_u32(&sm.q_full), 64 * c, i0, h, b);
-                        load_box(smem_u32(sm.go[c]), p.go, smem_u32(&sm.q_full), 64 * c, i0, h, b);
+                        load_box(smem_u32(sm.q[c]), p.q, smem_u32(&sm.q_full), 64 * c, w.i0, w.h, w.b);
+                        load_box(smem_u32(sm.go[c]), p.go, smem_u32(&sm.q_full), 64 * c, w.i0, w.h, w.b);
+                    }
+                    nq = ++it;
+                    for (int j = 0; j < kb.count(); ++j, ++g) {
+                        const int ks = kb.start(j);
+                        if (!(ok = wait(sm.k_empty[g % 3], ((g / 3) & 1) ^ 1))) break;
+                        mbar_expect_tx(smem_u32(&sm.k_full[g % 3]), NB * kBlk);
+                        for (int c = 0; c < NB; ++c)
+                            load_box(smem_u32(sm.k[g % 3][c]), p.k, smem_u32(&sm.k_full[g % 3]), 64 * c, ks, hk, w.b);
+                        nk = g + 1;
+                        if (!(ok = wait(sm.v_empty[g & 1], ((g >> 1) & 1) ^ 1))) break;
+                        mbar_expect_tx(smem_u32(&sm.v_full[g & 1]), NB * kBlk);
+                        for (int c = 0; c < NB; ++c)
+                            load_box(smem_u32(sm.v[g & 1][c]), p.v, smem_u32(&sm.v_full[g & 1]), 64 * c, ks, hk, w.b);
+                        nv = g + 1;
                     }
                 }
-                int nk = g0, nv = g0;
-                for (int j = 0; j < n && ok; ++j) {
-                    const int g = g0 + j, ks = kb.start(j);
-                    ok = wait(sm.k_empty[g % 3], ((g / 3) & 1) ^ 1);
-                    if (!ok) break;
-                    mbar_expect_tx(smem_u32(&sm.k_full[g % 3]), NB * kBlk);
-                    for (int c = 0; c < NB; ++c)
-                        load_box(smem_u32(sm.k[g % 3][c]), p.k, smem_u32(&sm.k_full[g % 3]), 64 * c, ks, hk, b);
-                    nk = g + 1;
-                    ok = wait(sm.v_empty[g & 1], ((g >> 1) & 1) ^ 1);
-                    if (!ok) break;
-                    mbar_expect_tx(smem_u32(&sm.v_full[g & 1]), NB * kBlk);
-                    for (int c = 0; c < NB; ++c)
-                        load_box(smem_u32(sm.v[g & 1][c]), p.v, smem_u32(&sm.v_full[g & 1]), 64 * c, ks, hk, b);
-                    nv = g + 1;
-                }
-                drain_phase(smem_u32(&sm.q_full), 0);
+                // what was loaded has landed
+                if (nq > 0) drain_phase(smem_u32(&sm.q_full), (nq - 1) & 1);
                 for (int t = max(0, nk - 3); t < nk; ++t) drain_phase(smem_u32(&sm.k_full[t % 3]), (t / 3) & 1);
                 for (int t = max(0, nv - 2); t < nv; ++t) drain_phase(smem_u32(&sm.v_full[t & 1]), (t >> 1) & 1);
             }
@@ -494,7 +515,6 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
             if (elect_one()) {
                 constexpr uint32_t idS = idesc_bf16(128, 128, false, false);
                 constexpr uint32_t idG = idesc_bf16(128, HD, false, true);
-                ok = ok && wait(sm.q_full, 0);
                 const uint64_t dq = k_major(sm.q), dg = k_major(sm.go);
                 auto s_of = [&](int g) {
                     ok = ok && wait(sm.k_full[g % 3], (g / 3) & 1);
@@ -503,29 +523,41 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                     mma_scores<NB>(tS + 128 * (g & 1), dq, k_major(sm.k[g % 3]), idS);
                     mma_commit(smem_u32(&sm.s_full[g & 1]));
                 };
-                auto dp_of = [&](int g) {
+                auto dp_of = [&](int g, bool last) {
                     ok = ok && wait(sm.v_full[g & 1], (g >> 1) & 1);
                     if (!ok) return;
                     tc_fence_after();
                     mma_scores<NB>(tG, dg, k_major(sm.v[g & 1]), idS);
                     mma_commit(smem_u32(&sm.dp_full));
                     mma_commit(smem_u32(&sm.v_empty[g & 1]));
+                    if (last) mma_commit(smem_u32(&sm.q_empty));   // (the last scores came before)
                 };
-                s_of(g0);
-                dp_of(g0);
-                if (n > 1) s_of(g0 + 1);
-                for (int j = 0; j < n && ok; ++j) {
-                    const int g = g0 + j;
-                    ok = wait(sm.ds_ready, g & 1);
-                    if (!ok) break;
-                    if (j + 1 < n) dp_of(g + 1);   // first: the workers' next step waits for it
-                    if (!ok) break;
-                    tc_fence_after();
-                    mma_weights<5>(tdQ, tS + 128 * (g & 1), mn_major(sm.k[g % 3]), idG, j > 0);   // dQ += dS K_j
-                    mma_commit(smem_u32(&sm.k_empty[g % 3]));
-                    if (j + 2 < n) s_of(g + 2);
+                for (int t = 0; ok; ++t) {
+                    const long long x = blockIdx.x + (long long)t * gridDim.x;
+                    if (x >= all) break;
+                    if (pass == 1 && sm.again[t] == 0) continue;
+                    const QueryTile w(p, x, tiles);
+                    if (w.empty()) continue;
+                    const int n = KeyBlocks<kTile>(w.pf, w.pl, p.window, p.sinks).count();
+                    ok = wait(sm.q_full, it & 1);
+                    s_of(g);
+                    // (the last tile's dP has been read: its last dS was waited for)
+                    dp_of(g, n == 1);
+                    if (n > 1) s_of(g + 1);
+                    for (int j = 0; j < n && ok; ++j, ++g) {
+                        ok = wait(sm.ds_ready, g & 1);
+                        if (!ok) break;
+                        if (j + 1 < n) dp_of(g + 1, j + 2 == n);   // first: the workers' next step waits for it
+                        if (j == 0) ok = ok && wait(sm.dq_empty, (it & 1) ^ 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        mma_weights<5>(tdQ, tS + 128 * (g & 1), mn_major(sm.k[g % 3]), idG, j > 0);   // dQ += dS K_j
+                        mma_commit(smem_u32(&sm.k_empty[g % 3]));
+                        if (j + 2 < n) s_of(g + 2);
+                    }
+                    mma_commit(smem_u32(&sm.dq_full));
+                    ++it;
                 }
-                mma_commit(smem_u32(&sm.done));
                 if (!ok) {
                     mma_commit(smem_u32(&sm.s_full[0]));
                     mma_commit(smem_u32(&sm.s_full[1]));
@@ -534,78 +566,94 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
             }
             __syncwarp();
         } else {
-            const int c0 = kCols * (warp >> 2), r = (warp & 3) * 32 + lane, pos = pf + r;
-            const bool valid = pos <= pl;
+            const int c0 = kCols * (warp >> 2), r = (warp & 3) * 32 + lane;
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-            const long long row = ((long long)b * p.H + h) * p.Tq + i0 + r;
-            // a query that sees one token only has no gradient: P = 0
-            const float L = !valid ? 0.f : sees_one(pos, p.window, p.sinks) ? INFINITY : p.lse[row] * kLog2e;
-            const float D = valid ? p.delta[row] : 0.f;
-            const float2 sl2 = make_float2(p.scale_log2, p.scale_log2), nL = make_float2(-L, -L),
-                         nD = make_float2(-D, -D);
-            for (int j = 0; j < n; ++j) {
-                const int g = g0 + j;
-                const uint32_t tSj = tS + 128 * (g & 1) + lanes + c0;
-                const bool whole = kb.whole(j, pf, pl, p.window);
-                ok = wait(sm.s_full[g & 1], (g >> 1) & 1) && ok;
-                tc_fence_after();
-                float raw[32];
-                tmem_get32(tSj, raw);
-                float P[32];
+            const int d0 = (warp >> 2) * (HD / 4);   // this thread's quarter of the columns of dQ
+            const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
+            for (int t = 0;; ++t) {
+                const long long x = blockIdx.x + (long long)t * gridDim.x;
+                if (x >= all || *(volatile int *)&sm.abort != 0) break;
+                if (pass == 1 && sm.again[t] == 0) continue;
+                const QueryTile w(p, x, tiles);
+                const int pos = w.pf + r;
+                const bool valid = pos <= w.pl;
+                bf16 *out = p.dQ + p.sdq.at(w.b, w.i0 + r, w.h) + d0;
+                if (w.empty()) {
+                    if (w.i0 + r < p.Tq)
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    const float2 x = fma2(make_float2(raw[c], raw[c + 1]),
-                                          sl2, nL);
-                    P[c] = exp2_fast(x.x);
-                    P[c + 1] = exp2_fast(x.y);
+                        for (int c = 0; c < HD / 4; c += 8)
+                            if (d0 + c < p.hp) *reinterpret_cast<uint4 *>(out + c) = make_uint4(0, 0, 0, 0);
+                    continue;
                 }
-                ok = wait(sm.dp_full, g & 1) && ok;
-                tc_fence_after();
-                tmem_get32(tG + lanes + c0, raw);
+                const KeyBlocks<kTile> kb(w.pf, w.pl, p.window, p.sinks);
+                const WholeBlocks wb(kb, w.pf, w.pl, p.window);
+                const int n = kb.count();
+                const long long row = ((long long)w.b * p.H + w.h) * p.Tq + w.i0 + r;
+                // a query that sees one token only has no gradient: P = 0
+                const float L = !valid ? 0.f : sees_one(pos, p.window, p.sinks) ? INFINITY : p.lse[row] * kLog2e;
+                const float D = valid ? p.delta[row] : 0.f;
+                const float2 nL = make_float2(-L, -L), nD = make_float2(-D, -D);
+#pragma unroll 1
+                for (int j = 0; j < n; ++j, ++g) {
+                    const uint32_t tSj = tS + 128 * (g & 1) + lanes + c0;
+                    const bool whole = wb.has(j);
+                    wait(sm.s_full[g & 1], (g >> 1) & 1);
+                    tc_fence_after();
+                    float raw[32];
+                    tmem_get32(tSj, raw);
+                    float P[32];
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    const float2 x = mul2(make_float2(P[c], P[c + 1]),
-                                          add2(make_float2(raw[c], raw[c + 1]), nD));
-                    P[c] = x.x;
-                    P[c + 1] = x.y;
-                }
-                if (!whole) {
-                    const uint32_t seen = seen_bits(kb, j, kb.start(j), c0, pos, p.window, p.sinks);
-#pragma unroll
-                    for (int c = 0; c < 32; ++c)
-                        if (((seen >> c) & 1u) == 0) P[c] = 0.f;
-                    if (pass == 1) {
-                        if (c0 == 0) clean_row<NB>(sm.k[g % 3][0], r);
-                        fence_proxy_async();
+                    for (int c = 0; c < 32; c += 2) {
+                        const float2 y = fma2(make_float2(raw[c], raw[c + 1]), sl2, nL);
+                        P[c] = exp2_fast(y.x);
+                        P[c + 1] = exp2_fast(y.y);
                     }
+                    wait(sm.dp_full, g & 1);
+                    tc_fence_after();
+                    tmem_get32(tG + lanes + c0, raw);
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        const float2 y = mul2(make_float2(P[c], P[c + 1]), add2(make_float2(raw[c], raw[c + 1]), nD));
+                        P[c] = y.x;
+                        P[c + 1] = y.y;
+                    }
+                    if (!whole) {
+                        const uint32_t seen = seen_bits(kb, j, kb.start(j), c0, pos, p.window, p.sinks);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (((seen >> c) & 1u) == 0) P[c] = 0.f;
+                        if (pass == 1) {
+                            if (c0 == 0) clean_row<NB>(sm.k[g % 3][0], r);
+                            fence_proxy_async();
+                        }
+                    }
+                    put_weights(tSj, P);
+                    warp_arrive(sm.ds_ready, lane);
                 }
-                put_weights(tSj, P);
-                warp_arrive(sm.ds_ready, lane);
-            }
-            ok = wait(sm.done, pass) && ok;
-            tc_fence_after();
-            float dq[HD / 64][16];   // this thread's quarter of the columns
-            float odd = 0.f;
+                wait(sm.dq_full, it & 1);
+                ++it;
+                tc_fence_after();
+                float dq[HD / 64][16];
+                float odd = 0.f;
 #pragma unroll
-            for (int x = 0; x < HD / 64; ++x) {
-                tmem_ld16(tdQ + lanes + (warp >> 2) * (HD / 4) + 16 * x, dq[x]);
+                for (int c = 0; c < HD / 64; ++c) tmem_ld16(tdQ + lanes + d0 + 16 * c, dq[c]);
+                tc_fence_before();
+                warp_arrive(sm.dq_empty, lane);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) odd = fmaf(dq[x][e], 0.f, odd);
-            }
-            if (pass == 0 && valid && !(odd == 0.f)) sm.redo = 1;
-            named_barrier(1, kWorkers);
-            if (*(volatile int *)&sm.abort == 0 && (pass == 1 || *(volatile int *)&sm.redo == 0)) {
+                for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
-                for (int x = 0; x < HD / 64; ++x) {
-                    const int c = (warp >> 2) * (HD / 4) + 16 * x;
-                    stage_bf16_16(sm.q[c >> 6], r, (c & 63) >> 3, dq[x], p.scale, valid);
-                }
-                fence_proxy_async();
-                named_barrier(1, kWorkers);
-                if (threadIdx.x == 0) {
-                    for (int c = 0; c < NB; ++c) store_box(p.dq, smem_u32(sm.q[c]), 64 * c, i0, h, b);
-                    bulk_commit();
-                    bulk_wait_read0();
+                    for (int e = 0; e < 16; ++e) odd = fmaf(dq[c][e], 0.f, odd);
+                if (pass == 0 && valid && !(odd == 0.f)) sm.again[t] = 1, sm.redo = 1;
+                if (w.i0 + r < p.Tq && *(volatile int *)&sm.abort == 0) {
+#pragma unroll
+                    for (int c = 0; c < HD / 4; c += 8) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            o[e] = valid ? pack_bf16x2(dq[c >> 4][(c & 8) + 2 * e] * p.scale,
+                                                       dq[c >> 4][(c & 8) + 2 * e + 1] * p.scale) : 0u;
+                        if (d0 + c < p.hp) *reinterpret_cast<uint4 *>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
+                    }
                 }
             }
         }
@@ -627,7 +675,10 @@ cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     if (e == cudaSuccess) e = allow_smem((const void *)window_dq_tc_kernel<HD>, qb);
     if (e != cudaSuccess) return e;
     window_dkv_tc_kernel<HD><<<dim3(p.split.ctas(p.a, kTile), p.Hkv, B), kKvThreads, kv, s>>>(p);
-    window_dq_tc_kernel<HD><<<dim3((p.Tq + kTile - 1) / kTile, p.H, B), kQThreads, qb, s>>>(p);
+    const int tiles = (p.Tq + kTile - 1) / kTile;
+    const long long all = (long long)tiles * p.H * B;
+    const long long ctas = std::max(std::min(all, 152LL), (all + kMaxTiles - 1) / kMaxTiles);
+    window_dq_tc_kernel<HD><<<(unsigned)ctas, kQThreads, qb, s>>>(p, all, tiles);
     note_launches(2);
     e = cudaGetLastError();
     return e != cudaSuccess ? e : add_sink_rows(p.a, p.partial, p.split.extra, p.dK, p.dV, s);
@@ -642,7 +693,7 @@ bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, c
     BwdArgs p;
     if (!make_map(&p.q, q, a.q, a.B, a.Tq, a.H, a.hp) || !make_map(&p.k, k, a.k, a.B, a.Tk, a.Hkv, a.hp) ||
         !make_map(&p.v, v, a.v, a.B, a.Tk, a.Hkv, a.hp) || !make_map(&p.go, dO, a.go, a.B, a.Tq, a.H, a.hp) ||
-        !make_map(&p.dq, dq, a.dq, a.B, a.Tq, a.H, a.hp) || !make_map(&p.dk, dk, a.dk, a.B, a.Tk, a.Hkv, a.hp) ||
+        !rows16(dq, a.dq, true) || !make_map(&p.dk, dk, a.dk, a.B, a.Tk, a.Hkv, a.hp) ||
         !make_map(&p.dv, dv, a.dv, a.B, a.Tk, a.Hkv, a.hp))
         return false;
     p.lens = lens;
