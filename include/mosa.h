@@ -349,7 +349,7 @@ mosa_status mosa_qk_norm_rope_backward(const mosa_qk_shape *shape, const void *q
  * gets O = 0, lse = -inf and no gradient.  What a masked place holds, NaN and
  * infinities among them, reaches no output that does not see it; a visible
  * NaN or infinity makes the results that it reaches NaN or infinite.
- * 0 <= window; 0 <= sinks; 1 <= Tq <= Tk. */
+ * 0 <= window; 0 <= sinks; 1 <= Tq <= Tk; B*H*Tq < 2^31. */
 typedef struct {
     int32_t B, Tq, Tk, H, Hkv, hp;
     int32_t dtype;

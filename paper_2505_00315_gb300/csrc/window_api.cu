@@ -80,7 +80,7 @@ mosa_status check_window(const mosa_window_shape *s, bool backward, Attn *a) {
     if (st != MOSA_OK) return st;
     if (s->Tq <= 0 || s->Tq > s->Tk || s->window < 0 || s->sinks < 0) return MOSA_ERR_INVALID_ARG;
     if (!(s->scale >= 0.f) || std::isinf(s->scale)) return MOSA_ERR_INVALID_ARG;
-    if (s->Tk >= kMaxTokens || (long long)s->B * s->H * s->Tq >= (1LL << 35)) return MOSA_ERR_UNSUPPORTED;
+    if (s->Tk >= kMaxTokens || (long long)s->B * s->H * s->Tq >= (1LL << 31)) return MOSA_ERR_UNSUPPORTED;
     *a = Attn{};
     a->B = s->B;
     a->Tq = s->Tq;

@@ -185,6 +185,15 @@ struct WholeBlocks {
     }
     __device__ __forceinline__ bool has(int j) const { return j < far_whole || (j >= lo && j < hi); }
 };
+// Zeroes (or `hidden`) the values whose bit of `seen` is not set; warps whose lanes see all of
+// theirs, as most of a partly seen block's do, pass by.
+__device__ __forceinline__ void hide(float (&v)[32], uint32_t seen, float hidden) {
+    if (__all_sync(0xffffffffu, seen == ~0u)) return;
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+        if (((seen >> c) & 1u) == 0) v[c] = hidden;
+}
+
 // Which of the 32 columns from c0 on of key block j (start ks) position pos sees, as bits.
 __device__ __forceinline__ uint32_t seen_bits(const KeyBlocks<128> &kb, int j, int ks, int c0, int pos,
                                               int window, int sinks) {

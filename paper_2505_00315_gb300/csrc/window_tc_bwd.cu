@@ -284,9 +284,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                 P[c + 3] = exp2_fast(y.y);
             }
             if (!whole) {
-#pragma unroll
-                for (int c = 0; c < 32; ++c)
-                    if (((seen >> c) & 1u) == 0) P[c] = 0.f;
+                hide(P, seen, 0.f);
                 if ((sm.odd[u][0] | sm.odd[u][1] | sm.odd[u][2] | sm.odd[u][3]) != 0) {
                     // zero those queries' rows, once S and dP have been taken from them
                     ok = wait(sm.dp_full, i & 1) && ok;
@@ -326,9 +324,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                 // no gradient)
                 if (p.window == 1 && p.sinks == 0) seen = 0;
                 if (pq == 0 && c0 == 0) seen &= ~1u;
-#pragma unroll
-                for (int c = 0; c < 32; ++c)
-                    if (((seen >> c) & 1u) == 0) P[c] = 0.f;
+                hide(P, seen, 0.f);
             }
             put_weights(tG + at, P);
             warp_arrive(sm.ds_ready, lane);
@@ -417,11 +413,11 @@ constexpr int kQThreads = kWorkers + 64;
 // The x-th query tile of all, heaviest of a head first.
 struct QueryTile {
     int b, h, i0, pf, pl;
-    __device__ __forceinline__ QueryTile(const BwdArgs &p, long long x, int tiles) {
-        const long long rest = x / tiles;
+    __device__ __forceinline__ QueryTile(const BwdArgs &p, uint32_t x, int tiles) {
+        const uint32_t rest = x / (uint32_t)tiles;
         i0 = (tiles - 1 - (int)(x - rest * tiles)) * kTile;
-        b = (int)(rest / p.H);
-        h = (int)(rest - (long long)b * p.H);
+        b = (int)(rest / (uint32_t)p.H);
+        h = (int)(rest - (uint32_t)(b * p.H));
         pf = p.Tk - p.Tq + i0;
         pl = min(p.Tk - p.Tq + min(i0 + kTile, p.Tq), seq_len(p.lens, b, p.Tk)) - 1;
     }
@@ -430,7 +426,7 @@ struct QueryTile {
 
 template <int HD>
 __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid_constant__ BwdArgs p,
-                                                                    long long all, int tiles) {
+                                                                    uint32_t all, int tiles) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using Sm = QSm<HD>;
     constexpr int NB = Sm::NB;
@@ -477,7 +473,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
             if (lane == 0) {
                 int nq = it, nk = g, nv = g;
                 for (int t = 0; ok; ++t) {
-                    const long long x = blockIdx.x + (long long)t * gridDim.x;
+                    const uint32_t x = blockIdx.x + (uint32_t)t * gridDim.x;
                     if (x >= all) break;
                     if (pass == 1 && sm.again[t] == 0) continue;
                     const QueryTile w(p, x, tiles);
@@ -533,7 +529,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                     if (last) mma_commit(smem_u32(&sm.q_empty));   // (the last scores came before)
                 };
                 for (int t = 0; ok; ++t) {
-                    const long long x = blockIdx.x + (long long)t * gridDim.x;
+                    const uint32_t x = blockIdx.x + (uint32_t)t * gridDim.x;
                     if (x >= all) break;
                     if (pass == 1 && sm.again[t] == 0) continue;
                     const QueryTile w(p, x, tiles);
@@ -570,33 +566,55 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
             const int d0 = (warp >> 2) * (HD / 4);   // this thread's quarter of the columns of dQ
             const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
-            for (int t = 0;; ++t) {
-                const long long x = blockIdx.x + (long long)t * gridDim.x;
-                if (x >= all || *(volatile int *)&sm.abort != 0) break;
-                if (pass == 1 && sm.again[t] == 0) continue;
-                const QueryTile w(p, x, tiles);
-                const int pos = w.pf + r;
+            // This thread's row of a tile; the next tile's is fetched while the last dQ is summed.
+            struct Row {
+                QueryTile w;
+                float L, D;
+            };
+            auto row_of = [&](uint32_t x) {
+                Row y{QueryTile(p, x, tiles), 0.f, 0.f};
+                const int pos = y.w.pf + r;
+                if (pos <= y.w.pl) {
+                    const long long row = ((long long)y.w.b * p.H + y.w.h) * p.Tq + y.w.i0 + r;
+                    y.L = p.lse[row] * kLog2e;
+                    y.D = p.delta[row];
+                    // a query that sees one token only has no gradient: P = 0
+                    if (sees_one(pos, p.window, p.sinks)) y.L = INFINITY;
+                }
+                return y;
+            };
+            auto next_of = [&](int t) {   // the next tile of this pass from t on
+                while (pass == 1 && blockIdx.x + (uint32_t)t * gridDim.x < all && sm.again[t] == 0) ++t;
+                return t;
+            };
+            int t = next_of(0);
+            uint32_t x = blockIdx.x + (uint32_t)t * gridDim.x;
+            Row row = row_of(min(x, all - 1));
+            while (x < all && *(volatile int *)&sm.abort == 0) {
+                const QueryTile w = row.w;
+                const int pos = w.pf + r, tile_no = t;
                 const bool valid = pos <= w.pl;
+                const float2 nL = make_float2(-row.L, -row.L), nD = make_float2(-row.D, -row.D);
                 bf16 *out = p.dQ + p.sdq.at(w.b, w.i0 + r, w.h) + d0;
+                t = next_of(t + 1);
+                x = blockIdx.x + (uint32_t)t * gridDim.x;
                 if (w.empty()) {
                     if (w.i0 + r < p.Tq)
 #pragma unroll
                         for (int c = 0; c < HD / 4; c += 8)
                             if (d0 + c < p.hp) *reinterpret_cast<uint4 *>(out + c) = make_uint4(0, 0, 0, 0);
+                    row = row_of(min(x, all - 1));
                     continue;
                 }
                 const KeyBlocks<kTile> kb(w.pf, w.pl, p.window, p.sinks);
                 const WholeBlocks wb(kb, w.pf, w.pl, p.window);
                 const int n = kb.count();
-                const long long row = ((long long)w.b * p.H + w.h) * p.Tq + w.i0 + r;
-                // a query that sees one token only has no gradient: P = 0
-                const float L = !valid ? 0.f : sees_one(pos, p.window, p.sinks) ? INFINITY : p.lse[row] * kLog2e;
-                const float D = valid ? p.delta[row] : 0.f;
-                const float2 nL = make_float2(-L, -L), nD = make_float2(-D, -D);
 #pragma unroll 1
                 for (int j = 0; j < n; ++j, ++g) {
                     const uint32_t tSj = tS + 128 * (g & 1) + lanes + c0;
                     const bool whole = wb.has(j);
+                    uint32_t seen = ~0u;
+                    if (!whole) seen = seen_bits(kb, j, kb.start(j), c0, pos, p.window, p.sinks);
                     wait(sm.s_full[g & 1], (g >> 1) & 1);
                     tc_fence_after();
                     float raw[32];
@@ -618,10 +636,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                         P[c + 1] = y.y;
                     }
                     if (!whole) {
-                        const uint32_t seen = seen_bits(kb, j, kb.start(j), c0, pos, p.window, p.sinks);
-#pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (((seen >> c) & 1u) == 0) P[c] = 0.f;
+                        hide(P, seen, 0.f);
                         if (pass == 1) {
                             if (c0 == 0) clean_row<NB>(sm.k[g % 3][0], r);
                             fence_proxy_async();
@@ -630,6 +645,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                     put_weights(tSj, P);
                     warp_arrive(sm.ds_ready, lane);
                 }
+                row = row_of(min(x, all - 1));
                 wait(sm.dq_full, it & 1);
                 ++it;
                 tc_fence_after();
@@ -643,7 +659,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) odd = fmaf(dq[c][e], 0.f, odd);
-                if (pass == 0 && valid && !(odd == 0.f)) sm.again[t] = 1, sm.redo = 1;
+                if (pass == 0 && valid && !(odd == 0.f)) sm.again[tile_no] = 1, sm.redo = 1;
                 if (w.i0 + r < p.Tq && *(volatile int *)&sm.abort == 0) {
 #pragma unroll
                     for (int c = 0; c < HD / 4; c += 8) {
@@ -678,7 +694,7 @@ cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     const int tiles = (p.Tq + kTile - 1) / kTile;
     const long long all = (long long)tiles * p.H * B;
     const long long ctas = std::max(std::min(all, 152LL), (all + kMaxTiles - 1) / kMaxTiles);
-    window_dq_tc_kernel<HD><<<(unsigned)ctas, kQThreads, qb, s>>>(p, all, tiles);
+    window_dq_tc_kernel<HD><<<(unsigned)ctas, kQThreads, qb, s>>>(p, (uint32_t)all, tiles);
     note_launches(2);
     e = cudaGetLastError();
     return e != cudaSuccess ? e : add_sink_rows(p.a, p.partial, p.split.extra, p.dK, p.dV, s);

@@ -218,11 +218,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     tc_fence_before();
                     warp_arrive(sm.s_free, lane);
                 }
-                if (!whole) {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c)
-                        if (((seen >> c) & 1u) == 0) s[c] = -INFINITY;
-                }
+                if (!whole) hide(s, seen, -INFINITY);
                 float mx[2] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3])};
 #pragma unroll
                 for (int c = 4; c < 32; c += 4) {
