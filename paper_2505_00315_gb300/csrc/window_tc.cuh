@@ -210,6 +210,18 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
     return w;
 }
 
+// 32 bytes in one store (a whole sector), or two of 16.
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8], bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]),
+                     "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        static_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        static_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
 // Whether a bf16x2 word holds a NaN or an infinity.
 __device__ __forceinline__ bool odd_bf16x2(uint32_t w) {
     return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;

@@ -49,6 +49,7 @@ struct BwdArgs {
     const float *lse, *delta;           // [B, H, Tq]
     bf16 *dQ, *dK, *dV;
     Str sdq, sdk, sdv;
+    int wide_dq;                        // rows of dQ start at a multiple of 32 bytes
     float *partial;                     // [B, Hkv, slots, sinks, 2, hp] fp32: dk, dv of the sink rows
     uint32_t *status;
     Attn a;
@@ -662,13 +663,12 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 if (pass == 0 && valid && !(odd == 0.f)) sm.again[tile_no] = 1, sm.redo = 1;
                 if (w.i0 + r < p.Tq && *(volatile int *)&sm.abort == 0) {
 #pragma unroll
-                    for (int c = 0; c < HD / 4; c += 8) {
-                        uint32_t o[4];
+                    for (int c = 0; c < HD / 64; ++c) {
+                        uint32_t o[8];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            o[e] = valid ? pack_bf16x2(dq[c >> 4][(c & 8) + 2 * e] * p.scale,
-                                                       dq[c >> 4][(c & 8) + 2 * e + 1] * p.scale) : 0u;
-                        if (d0 + c < p.hp) *reinterpret_cast<uint4 *>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
+                        for (int e = 0; e < 8; ++e)
+                            o[e] = valid ? pack_bf16x2(dq[c][2 * e] * p.scale, dq[c][2 * e + 1] * p.scale) : 0u;
+                        if (d0 + 16 * c < p.hp) store32(out + 16 * c, o, p.wide_dq);
                     }
                 }
             }
@@ -719,6 +719,7 @@ bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, c
     p.dK = (bf16 *)dk;
     p.dV = (bf16 *)dv;
     p.sdq = a.dq;
+    p.wide_dq = (reinterpret_cast<uintptr_t>(dq) & 31) == 0 && ((a.dq.b | a.dq.t | a.dq.h) & 15) == 0;
     p.sdk = a.dk;
     p.sdv = a.dv;
     p.partial = partial;
