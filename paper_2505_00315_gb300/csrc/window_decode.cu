@@ -268,7 +268,7 @@ __device__ __forceinline__ void halves_of(float a, float b, uint32_t &hi, uint32
 // the scores' results lie; B = V, tokens 2t, 2t+1, 8+2t, 9+2t on lane (g, t), its piece g (and g + 8) of
 // the row: value j of a piece is column g of output tile j.
 template <int HD>
-__global__ void __launch_bounds__(kMmaWarps * 32) window_decode_mma_kernel(
+__global__ void __launch_bounds__(kMmaWarps * 32, 3) window_decode_mma_kernel(
     const __grid_constant__ DecodeArgs p, const __grid_constant__ Turns tab) {
     constexpr int kPieces = HD / 32;                 // 16-byte pieces of K a lane
     constexpr int VP = HD >= 64 ? HD / 64 : 1;       // pieces of V a lane, of
@@ -280,18 +280,23 @@ __global__ void __launch_bounds__(kMmaWarps * 32) window_decode_mma_kernel(
     __shared__ __align__(16) float sq[kMmaHeads][HD];
     __shared__ float sm_m[kMmaWarps][kMmaHeads], sm_l[kMmaWarps][kMmaHeads];
     __shared__ __align__(16) float sm_o[kMmaWarps][kMmaHeads][HD];
+    __shared__ uint4 sm_q[2 * kPieces][32];
     Seen seen;
     if (!decode_prologue<bf16, HD, kMmaHeads, kMmaWarps * 32>(p, tab, split, hk, b, g0, heads, sq, &seen))
         return;
-    uint32_t qa[kPieces][2][4];
+    // the heads' operand, the same for every warp: in shared memory, where registers would cost a third of
+    // the warps in flight
+    if (warp == 0) {
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const float *x = &sq[g][8 * (t + 4 * i) + 4 * s];
-            halves_of(x[0], x[1], qa[i][s][0], qa[i][s][1]);
-            halves_of(x[2], x[3], qa[i][s][2], qa[i][s][3]);
+        for (int i = 0; i < 2 * kPieces; ++i) {
+            const float *x = &sq[g][8 * (t + 4 * (i >> 1)) + 4 * (i & 1)];
+            uint4 w;
+            halves_of(x[0], x[1], w.x, w.y);
+            halves_of(x[2], x[3], w.z, w.w);
+            sm_q[i][lane] = w;
         }
+    }
+    __syncthreads();
     const bf16 *Kb = (const bf16 *)p.kc + d.kc.at(b, 0, hk) + 8 * t;
     const bf16 *Vb = (const bf16 *)p.vc + d.vc.at(b, 0, hk) + VE * g;
     float acc[VP * VE][4], m = -INFINITY, l = 0.f;
@@ -299,9 +304,9 @@ __global__ void __launch_bounds__(kMmaWarps * 32) window_decode_mma_kernel(
     for (int j = 0; j < VP * VE; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
-    for (int u0 = seen.lo + warp * kMmaTokens; u0 < seen.hi; u0 += kMmaWarps * kMmaTokens) {
-        uint4 kx[2][kPieces];
-        uint32_t vx[4][VP][VE / 2];
+    uint4 kx[2][kPieces];
+    uint32_t vx[4][VP][VE / 2];
+    auto load_k = [&](int u0) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const int u = u0 + 8 * r + g;
@@ -310,6 +315,8 @@ __global__ void __launch_bounds__(kMmaWarps * 32) window_decode_mma_kernel(
             for (int i = 0; i < kPieces; ++i)
                 kx[r][i] = u < seen.hi ? *reinterpret_cast<const uint4 *>(row + 32 * i) : make_uint4(0, 0, 0, 0);
         }
+    };
+    auto load_v = [&](int u0) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int u = u0 + 8 * (r >> 1) + 2 * t + (r & 1);
@@ -325,17 +332,26 @@ __global__ void __launch_bounds__(kMmaWarps * 32) window_decode_mma_kernel(
                 }
             }
         }
+    };
+    // loads are always under way: the next tokens' K from the last use of these tokens' on, V from
+    // the step's beginning
+    load_k(seen.lo + warp * kMmaTokens);
+    for (int u0 = seen.lo + warp * kMmaTokens; u0 < seen.hi; u0 += kMmaWarps * kMmaTokens) {
+        load_v(u0);
         float s[2][4];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int e = 0; e < 4; ++e) s[0][e] = s[1][e] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[r][e] = 0.f;
+        for (int i = 0; i < kPieces; ++i) {
+            const uint4 x = sm_q[2 * i][lane], y = sm_q[2 * i + 1][lane];
+            const uint32_t qx[4] = {x.x, x.y, x.z, x.w}, qy[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                mma16816(s[r], qa[i][0], kx[r][i].x, kx[r][i].y);
-                mma16816(s[r], qa[i][1], kx[r][i].z, kx[r][i].w);
+            for (int r = 0; r < 2; ++r) {
+                mma16816(s[r], qx, kx[r][i].x, kx[r][i].y);
+                mma16816(s[r], qy, kx[r][i].z, kx[r][i].w);
             }
         }
+        load_k(u0 + kMmaWarps * kMmaTokens);
         // this lane: head g, tokens 8 r + 2 t + e; hi and lo rows added up
         float w[4], mx = m;
 #pragma unroll
