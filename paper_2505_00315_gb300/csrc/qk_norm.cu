@@ -56,6 +56,7 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
                                                                 const __grid_constant__ Turns tab) {
     constexpr int groups = kThreads / LG, hp = W * LG;
     constexpr int kBatch = batch_of(W * sizeof(T), kBackward);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ StepTokens st;
     __shared__ float gamma[2][hp];
     extern __shared__ float red[];   // backward: [groups][2][hp]
@@ -229,14 +230,14 @@ template <bool kBackward, class T, bool VEC, int W>
 cudaError_t launch_of(const NormArgs &p, unsigned blocks, cudaStream_t s) {
     const Turns tab = make_turns(p.n.rotary, p.n.theta);
     const int smem = kBackward ? kThreads * W * 2 * 4 : 0;   // 16 or 32 KB
-    switch (p.n.hp) {
-        case 16: qk_norm_rope_kernel<T, VEC, kBackward, W, 16 / W><<<blocks, kThreads, smem, s>>>(p, tab); break;
-        case 32: qk_norm_rope_kernel<T, VEC, kBackward, W, 32 / W><<<blocks, kThreads, smem, s>>>(p, tab); break;
-        case 64: qk_norm_rope_kernel<T, VEC, kBackward, W, 64 / W><<<blocks, kThreads, smem, s>>>(p, tab); break;
-        default: qk_norm_rope_kernel<T, VEC, kBackward, W, 128 / W><<<blocks, kThreads, smem, s>>>(p, tab); break;
-    }
+    auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(blocks), dim3(kThreads), smem, s, p, tab); };
     note_launches(1);
-    return cudaGetLastError();
+    switch (p.n.hp) {
+        case 16: return go(qk_norm_rope_kernel<T, VEC, kBackward, W, 16 / W>);
+        case 32: return go(qk_norm_rope_kernel<T, VEC, kBackward, W, 32 / W>);
+        case 64: return go(qk_norm_rope_kernel<T, VEC, kBackward, W, 64 / W>);
+        default: return go(qk_norm_rope_kernel<T, VEC, kBackward, W, 128 / W>);
+    }
 }
 
 template <bool kBackward>

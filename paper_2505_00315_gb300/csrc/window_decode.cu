@@ -61,6 +61,7 @@ __device__ __forceinline__ bool decode_prologue(const DecodeArgs &p, const Turns
                                                 int hk, int b, int g0, int heads, float (*sq)[HD],
                                                 Seen *seen) {
     constexpr int LG = HD / 8;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ __align__(16) float2 cs[64];
     const Decode &d = p.d;
     const int G = d.H / d.Hkv, len = p.lens[b], at = len - 1;
@@ -441,10 +442,9 @@ int splits_of(const Decode &d) {
 }
 
 cudaError_t join(const DecodeArgs &p, cudaStream_t s) {
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || p.splits == 1) return e;
+    if (p.splits == 1) return cudaSuccess;
     const dim3 grid(p.d.H, p.d.B);
-    e = p.d.bf16 ? launch_pdl(decode_join_kernel<bf16>, grid, dim3(p.d.hp), 0, s, p)
+    const cudaError_t e = p.d.bf16 ? launch_pdl(decode_join_kernel<bf16>, grid, dim3(p.d.hp), 0, s, p)
                  : launch_pdl(decode_join_kernel<float>, grid, dim3(p.d.hp), 0, s, p);
     note_launches(1);
     return e;
@@ -453,14 +453,15 @@ cudaError_t join(const DecodeArgs &p, cudaStream_t s) {
 template <class T, bool VEC, int HD>
 cudaError_t launch_hd(const DecodeArgs &p, const Turns &tab, cudaStream_t s) {
     const dim3 grid(p.splits * p.chunks, p.d.Hkv, p.d.B);
+    cudaError_t e;
     switch (heads_of(p.d, false)) {
-        case 1: window_decode_kernel<T, VEC, HD, 1><<<grid, kThreads, 0, s>>>(p, tab); break;
-        case 2: window_decode_kernel<T, VEC, HD, 2><<<grid, kThreads, 0, s>>>(p, tab); break;
-        case 4: window_decode_kernel<T, VEC, HD, 4><<<grid, kThreads, 0, s>>>(p, tab); break;
-        default: window_decode_kernel<T, VEC, HD, 8><<<grid, kThreads, 0, s>>>(p, tab); break;
+        case 1: e = launch_pdl(window_decode_kernel<T, VEC, HD, 1>, grid, dim3(kThreads), 0, s, p, tab); break;
+        case 2: e = launch_pdl(window_decode_kernel<T, VEC, HD, 2>, grid, dim3(kThreads), 0, s, p, tab); break;
+        case 4: e = launch_pdl(window_decode_kernel<T, VEC, HD, 4>, grid, dim3(kThreads), 0, s, p, tab); break;
+        default: e = launch_pdl(window_decode_kernel<T, VEC, HD, 8>, grid, dim3(kThreads), 0, s, p, tab); break;
     }
     note_launches(1);
-    return join(p, s);
+    return e != cudaSuccess ? e : join(p, s);
 }
 
 template <class T, bool VEC>
@@ -475,13 +476,14 @@ cudaError_t launch_of(const DecodeArgs &p, const Turns &tab, cudaStream_t s) {
 
 cudaError_t launch_mma(const DecodeArgs &p, const Turns &tab, cudaStream_t s) {
     const dim3 grid(p.splits * p.chunks, p.d.Hkv, p.d.B);
+    cudaError_t e;
     switch (p.d.hp) {
-        case 32: window_decode_mma_kernel<32><<<grid, kMmaWarps * 32, 0, s>>>(p, tab); break;
-        case 64: window_decode_mma_kernel<64><<<grid, kMmaWarps * 32, 0, s>>>(p, tab); break;
-        default: window_decode_mma_kernel<128><<<grid, kMmaWarps * 32, 0, s>>>(p, tab); break;
+        case 32: e = launch_pdl(window_decode_mma_kernel<32>, grid, dim3(kMmaWarps * 32), 0, s, p, tab); break;
+        case 64: e = launch_pdl(window_decode_mma_kernel<64>, grid, dim3(kMmaWarps * 32), 0, s, p, tab); break;
+        default: e = launch_pdl(window_decode_mma_kernel<128>, grid, dim3(kMmaWarps * 32), 0, s, p, tab); break;
     }
     note_launches(1);
-    return join(p, s);
+    return e != cudaSuccess ? e : join(p, s);
 }
 
 size_t partial_bytes(const Decode &d, int splits) {

@@ -400,6 +400,7 @@ __global__ void __launch_bounds__(kThreads, HD <= 64 ? 2 : 1) window_dkv_simt_ke
 template <class T>
 __global__ void __launch_bounds__(256) window_sink_rows_kernel(Attn a, const float *partial, int extra,
                                                                T *dk, T *dv) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int b = blockIdx.z, hk = blockIdx.y, t = blockIdx.x;
     const long long slot = (long long)a.sinks * 2 * a.hp;
     for (int e = threadIdx.x; e < 2 * a.hp; e += blockDim.x) {
@@ -418,6 +419,7 @@ constexpr int kDeltaItems = 4;
 template <class T>
 __global__ void __launch_bounds__(256) window_delta_kernel(Attn a, const T *O, const T *dO,
                                                            const bf16 *rest, float *delta, bool vec) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int V = 8 * sizeof(T) / 16;
     const int lg = 31 - __clz(a.hp >> 3), U = a.H << lg;   // items of one token
     const long long all = (long long)a.B * a.Tq * U, base = (long long)blockIdx.x * (256 * kDeltaItems);
@@ -592,10 +594,11 @@ cudaError_t add_sink_rows(const Attn &a, const float *partial, int extra, void *
                           cudaStream_t s) {
     if (extra == 0) return cudaSuccess;
     const dim3 grid(a.sinks, a.Hkv, a.B);
-    if (a.bf16) window_sink_rows_kernel<bf16><<<grid, 256, 0, s>>>(a, partial, extra, (bf16 *)dk, (bf16 *)dv);
-    else window_sink_rows_kernel<float><<<grid, 256, 0, s>>>(a, partial, extra, (float *)dk, (float *)dv);
+    const cudaError_t e =
+        a.bf16 ? launch_pdl(window_sink_rows_kernel<bf16>, grid, dim3(256), 0, s, a, partial, extra, (bf16 *)dk, (bf16 *)dv)
+               : launch_pdl(window_sink_rows_kernel<float>, grid, dim3(256), 0, s, a, partial, extra, (float *)dk, (float *)dv);
     note_launches(1);
-    return cudaGetLastError();
+    return e;
 }
 
 // The larger of both kernels' tiles: which one runs hangs on the tensors' places.
@@ -609,14 +612,12 @@ cudaError_t window_delta(const Attn &a, const void *O, const bf16 *rest, const v
     const long long n = (long long)a.B * a.Tq * a.H * (a.hp / 8);
     const bool vec = rows16(O, a.o, a.bf16) && rows16(dO, a.go, a.bf16);
     const dim3 grid((unsigned)((n + 256 * kDeltaItems - 1) / (256 * kDeltaItems)));
-    if (a.bf16)
-        window_delta_kernel<bf16><<<grid, 256, 0, s>>>(a, (const bf16 *)O, (const bf16 *)dO, rest, delta,
-                                                        vec);
-    else
-        window_delta_kernel<float><<<grid, 256, 0, s>>>(a, (const float *)O, (const float *)dO, nullptr,
-                                                         delta, vec);
+    const cudaError_t e =
+        a.bf16 ? launch_pdl(window_delta_kernel<bf16>, grid, dim3(256), 0, s, a, (const bf16 *)O, (const bf16 *)dO, rest, delta, vec)
+               : launch_pdl(window_delta_kernel<float>, grid, dim3(256), 0, s, a, (const float *)O, (const float *)dO,
+                            (const bf16 *)nullptr, delta, vec);
     note_launches(1);
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace win

@@ -8,7 +8,7 @@
 //           of the group's heads that see it.  Scores are taken transposed
 //           (S^T = K Q^T), so that P^T and dS^T, bf16 in TMEM in the place of the
 //           scores, are the A operands of dV and dK with no pass through shared memory.
-//   dQ      one CTA per (128-query tile, head, sequence) over the key blocks it meets.
+//   dQ      one CTA an SM, for some (128-query tile, head, sequence) each, over the key blocks they meet.
 // One kernel with five products instead of the seven here would have to add dQ up
 // from several CTAs: 64 KB of fp32 reductions per pair of tiles against 2560
 // cycles of MMAs (hp = 128), in an order that changes from run to run, and a pass to zero
@@ -127,6 +127,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                 *reinterpret_cast<uint4 *>(p.dK + p.sdk.at(b, t, hk) + e % units * 8) = make_uint4(0, 0, 0, 0);
                 *reinterpret_cast<uint4 *>(p.dV + p.sdv.at(b, t, hk) + e % units * 8) = make_uint4(0, 0, 0, 0);
             }
+        pdl_wait();
         return;
     }
     if (threadIdx.x == 0) {
@@ -388,6 +389,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
     __syncthreads();
     tc_fence_after();
     if (warp == kWarps) tmem_dealloc(sm.tmem, 512);
+    pdl_wait();   // this kernel ends after the dQ kernel that it started beside
 }
 
 // ---------------------------------------------------------------------- dQ
@@ -433,6 +435,8 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
     constexpr int NB = Sm::NB;
     Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_wait();      // D, and all that came before it
+    pdl_trigger();   // the dK, dV kernel may take the SMs that this one leaves
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&sm.q_full), 1);
         mbar_init(smem_u32(&sm.q_empty), 1);
@@ -690,14 +694,17 @@ cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     cudaError_t e = allow_smem((const void *)window_dkv_tc_kernel<HD>, kv);
     if (e == cudaSuccess) e = allow_smem((const void *)window_dq_tc_kernel<HD>, qb);
     if (e != cudaSuccess) return e;
-    window_dkv_tc_kernel<HD><<<dim3(p.split.ctas(p.a, kTile), p.Hkv, B), kKvThreads, kv, s>>>(p);
+    // dQ first, whose CTAs all end at about the same time; then dK, dV, whose many CTAs fill the SMs
+    // as they come free (it waits for D through the dQ kernel, and for that one's end at its own).
     const int tiles = (p.Tq + kTile - 1) / kTile;
     const long long all = (long long)tiles * p.H * B;
     const long long ctas = std::max(std::min(all, 152LL), (all + kMaxTiles - 1) / kMaxTiles);
-    window_dq_tc_kernel<HD><<<(unsigned)ctas, kQThreads, qb, s>>>(p, (uint32_t)all, tiles);
+    e = launch_pdl(window_dq_tc_kernel<HD>, dim3((unsigned)ctas), dim3(kQThreads), qb, s, p, (uint32_t)all, tiles);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(window_dkv_tc_kernel<HD>, dim3(p.split.ctas(p.a, kTile), p.Hkv, B), dim3(kKvThreads), kv, s, p);
+    if (e != cudaSuccess) return e;
     note_launches(2);
-    e = cudaGetLastError();
-    return e != cudaSuccess ? e : add_sink_rows(p.a, p.partial, p.split.extra, p.dK, p.dV, s);
+    return add_sink_rows(p.a, p.partial, p.split.extra, p.dK, p.dV, s);
 }
 
 }  // namespace

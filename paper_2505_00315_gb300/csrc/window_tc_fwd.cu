@@ -86,6 +86,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
     constexpr bool kEarly = HD == 64;
     Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_wait();
     const int b = blockIdx.z, h = blockIdx.y, hk = h / p.G;
     const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kQ, off = p.Tk - p.Tq;
     const int len = seq_len(p.lens, b, p.Tk);
@@ -349,9 +350,9 @@ cudaError_t launch(const FwdArgs &p, dim3 grid, cudaStream_t s) {
     auto kernel = window_fwd_tc_kernel<HD>;
     cudaError_t e = allow_smem((const void *)kernel, bytes);
     if (e != cudaSuccess) return e;
-    kernel<<<grid, kThreads, bytes, s>>>(p);
+    e = launch_pdl(kernel, grid, dim3(kThreads), bytes, s, p);
     note_launches(1);
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace
