@@ -122,13 +122,21 @@ __device__ __forceinline__ void store_part(T *p, const Part<W> &at, const float 
     }
 }
 
-// Turns lane li's values by the angles of cs (16-byte aligned; dir = -1: back).
-template <int W>
+// Where the (cos, sin) of pair a of a row on LG lanes lies: two pairs of a lane together, the lanes
+// side by side, so that 16-byte reads of neighbouring lanes meet no bank twice.
+template <int W, int LG>
+__device__ __forceinline__ int angle_at(int a) {
+    const int li = a / (W / 2), e = a % (W / 2);
+    return 2 * ((e >> 1) * LG + li) + (e & 1);
+}
+
+// Turns lane li's values by the angles of cs (laid out by angle_at, 16-byte aligned; dir = -1: back).
+template <int W, int LG>
 __device__ __forceinline__ void turn(float (&v)[W], int li, int rotary, int halves, const float2 *cs, float dir) {
     if (W * li >= rotary) return;
 #pragma unroll
     for (int e = 0; e < W / 2; e += 2) {
-        const float4 a = reinterpret_cast<const float4 *>(cs)[(W / 2 * li + e) >> 1];
+        const float4 a = reinterpret_cast<const float4 *>(cs)[(e >> 1) * LG + li];
         const float s0 = a.y * dir, s1 = a.w * dir;
         if (halves) {
             const float x0 = v[e], x1 = v[e + W / 2], y0 = v[e + 1], y1 = v[e + 1 + W / 2];

@@ -134,12 +134,12 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
                 if (!kBackward) {
 #pragma unroll
                     for (int e = 0; e < W; ++e) v[e] *= r * gm[e];
-                    turn<W>(v, li, n.rotary, n.halves, cs, 1.f);
+                    turn<W, LG>(v, li, n.rotary, n.halves, cs, 1.f);
                     if (on) store_part<T, VEC, W>(out + st.y[w.key][w.i0 + u], at, v);
                 } else {
                     float g[W], dot = 0.f;
                     unpack<T, W>(yr[kBackward ? u : 0], g);
-                    turn<W>(g, li, n.rotary, n.halves, cs, -1.f);
+                    turn<W, LG>(g, li, n.rotary, n.halves, cs, -1.f);
 #pragma unroll
                     for (int e = 0; e < W; ++e) {
                         v[e] *= r;
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
             const int i = e / pairs, a = e - i * pairs;
             int t = t0 + i;
             while (t >= n.T) t -= n.T;
-            st.cs[i][a] = angle_of(tab.phi[a], p.pos != nullptr ? p.pos[tok0 + i] : t);
+            st.cs[i][angle_at<W, LG>(a)] = angle_of(tab.phi[a], p.pos != nullptr ? p.pos[tok0 + i] : t);
         }
         __syncthreads();
         for (int it0 = 0; it0 < items; it0 += 2 * groups) {   // (all lanes together: the sums are shuffles)

@@ -77,7 +77,7 @@ __device__ __forceinline__ bool decode_prologue(const DecodeArgs &p, const Turns
     *seen = Seen{min(split * per, n), min((split + 1) * per, n), nS,
                  at >= wlo ? d.sinks + (wlo - d.sinks) % ring : 0, d.C, ring};
     const bool newest = seen->lo < n && seen->hi == n;   // this split holds the new token
-    for (int e = threadIdx.x; e < d.rotary / 2; e += THREADS) cs[e] = angle_of(tab.phi[e], at);
+    for (int e = threadIdx.x; e < d.rotary / 2; e += THREADS) cs[angle_at<8, LG>(e)] = angle_of(tab.phi[e], at);
     __syncthreads();
     const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
     const Part<8> part(li, d.rotary, d.halves);
@@ -101,7 +101,7 @@ __device__ __forceinline__ bool decode_prologue(const DecodeArgs &p, const Turns
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= r * gm[e];
         }
-        turn<8>(x, li, d.rotary, d.halves, cs, 1.f);
+        turn<8, LG>(x, li, d.rotary, d.halves, cs, 1.f);
         if (on && key) {
             const int slot = seen->slot(n - 1);
             store_part<T, false, 8>((T *)p.kc + d.kc.at(b, slot, hk), part, x);
