@@ -57,8 +57,9 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
     constexpr int groups = kThreads / LG, hp = W * LG;
     constexpr int kBatch = batch_of(W * sizeof(T), kBackward);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    __shared__ StepTokens st;
-    __shared__ float gamma[2][hp];
+    // Three steps' tokens: the next ones are filled in while a slower warp may still be at the last.
+    __shared__ StepTokens buf[3];
+    __shared__ __align__(16) float gamma[2][hp];
     extern __shared__ float red[];   // backward: [groups][2][hp]
     const Norm &n = p.n;
     const int grp = threadIdx.x / LG, li = threadIdx.x % LG;
@@ -73,13 +74,16 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
     for (int e = 0; e < W; ++e) acc[0][e] = acc[1][e] = 0.f;
     const int HH = n.H + n.Hkv;   // heads 0 .. H-1 are queries, the others keys
     const int pairs = n.rotary >> 1;
-    for (long long tok0 = (long long)blockIdx.x * p.step; tok0 < N; tok0 += (long long)gridDim.x * p.step) {
+    struct Step {
+        const StepTokens *st;
+        int tokens, items;
+    };
+    // Fills in the step of tokens from tok0 on.
+    auto fill = [&](StepTokens &st, long long tok0) {
         const int tokens = (int)min((long long)p.step, N - tok0);
         const int b0 = (int)(tok0 / n.T), t0 = (int)(tok0 - (long long)b0 * n.T);
-        __syncthreads();   // the last step's tokens are done with
         if (threadIdx.x < tokens) {
-            int b = b0, t = t0 + threadIdx.x;
-            while (t >= n.T) t -= n.T, ++b;
+            const int over = (t0 + (int)threadIdx.x) / n.T, b = b0 + over, t = t0 + threadIdx.x - over * n.T;
             st.in[0][threadIdx.x] = n.q.at(b, t, 0);
             st.in[1][threadIdx.x] = n.k.at(b, t, 0);
             st.y[0][threadIdx.x] = n.yq.at(b, t, 0);
@@ -87,93 +91,110 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
             st.d[0][threadIdx.x] = n.dq.at(b, t, 0);
             st.d[1][threadIdx.x] = n.dk.at(b, t, 0);
         }
-        __syncthreads();
-        // items of `batch` tokens of one head, one a lane group; the next item's loads are under way
-        // while one is worked on
-        const int items = (tokens + p.batch - 1) / p.batch * HH;
-        Raw<T, W> x[2][kBatch], dy[2][kBackward ? kBatch : 1];
-        struct Item {
-            int key, h, i0, count;
-        };
-        auto item = [&](int it) {
-            const int bat = it / HH, hh = it - bat * HH, i0 = bat * p.batch;
-            const int key = hh >= n.H;
-            return Item{key, key ? hh - n.H : hh, i0, it < items ? min(p.batch, tokens - i0) : 0};
-        };
-        auto load = [&](const Item &w, Raw<T, W> (&xr)[kBatch], Raw<T, W> (&yr)[kBackward ? kBatch : 1]) {
-            const T *in = static_cast<const T *>(w.key ? p.k : p.q) + w.h * (w.key ? n.k.h : n.q.h);
-            const T *gr = static_cast<const T *>(w.key ? p.dyk : p.dyq) + w.h * (w.key ? n.yk.h : n.yq.h);
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                if (u < w.count) {
-                    load_raw<T, VEC, W>(in + st.in[w.key][w.i0 + u], at, xr[u]);
-                    if (kBackward) load_raw<T, VEC, W>(gr + st.y[w.key][w.i0 + u], at, yr[kBackward ? u : 0]);
-                }
-            }
-        };
-        auto work = [&](const Item &w, Raw<T, W> (&xr)[kBatch], Raw<T, W> (&yr)[kBackward ? kBatch : 1]) {
-            T *out = static_cast<T *>(w.key ? p.ok : p.oq) +
-                     w.h * (kBackward ? (w.key ? n.dk.h : n.dq.h) : (w.key ? n.yk.h : n.yq.h));
-            float gm[W];
-#pragma unroll
-            for (int e = 0; e < W; e += 4) {
-                const float4 g4 = *reinterpret_cast<const float4 *>(&gamma[w.key][at.at(e)]);
-                gm[e] = g4.x; gm[e + 1] = g4.y; gm[e + 2] = g4.z; gm[e + 3] = g4.w;
-            }
-            const float isq = w.key ? 0.f : 1.f, isk = w.key ? 1.f : 0.f;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                if (u >= p.batch) break;
-                const bool on = u < w.count;
-                const float2 *cs = st.cs[on ? w.i0 + u : 0];
-                float v[W], ss = 0.f;
-                unpack<T, W>(xr[u], v);
-#pragma unroll
-                for (int e = 0; e < W; ++e) ss = fmaf(v[e], v[e], ss);
-                const float r = rsqrtf(fmaf(group_sum(ss, LG), 1.f / hp, n.eps));
-                if (!kBackward) {
-#pragma unroll
-                    for (int e = 0; e < W; ++e) v[e] *= r * gm[e];
-                    turn<W, LG>(v, li, n.rotary, n.halves, cs, 1.f);
-                    if (on) store_part<T, VEC, W>(out + st.y[w.key][w.i0 + u], at, v);
-                } else {
-                    float g[W], dot = 0.f;
-                    unpack<T, W>(yr[kBackward ? u : 0], g);
-                    turn<W, LG>(g, li, n.rotary, n.halves, cs, -1.f);
-#pragma unroll
-                    for (int e = 0; e < W; ++e) {
-                        v[e] *= r;
-                        const float d = on ? g[e] * v[e] : 0.f;
-                        acc[0][e] = fmaf(d, isq, acc[0][e]);
-                        acc[1][e] = fmaf(d, isk, acc[1][e]);
-                        g[e] *= gm[e];
-                        dot = fmaf(g[e], v[e], dot);
-                    }
-                    dot = group_sum(dot, LG) * (1.f / hp);
-#pragma unroll
-                    for (int e = 0; e < W; ++e) g[e] = r * fmaf(-v[e], dot, g[e]);
-                    if (on) store_part<T, VEC, W>(out + st.d[w.key][w.i0 + u], at, g);
-                }
-            }
-        };
-        Item cur = item(grp);
-        load(cur, x[0], dy[0]);
         for (int e = threadIdx.x; e < tokens * pairs; e += kThreads) {
             const int i = e / pairs, a = e - i * pairs;
-            int t = t0 + i;
-            while (t >= n.T) t -= n.T;
-            st.cs[i][angle_at<W, LG>(a)] = angle_of(tab.phi[a], p.pos != nullptr ? p.pos[tok0 + i] : t);
+            const int t = p.pos != nullptr ? p.pos[tok0 + i] : (t0 + i) % n.T;
+            st.cs[i][angle_at<W, LG>(a)] = angle_of(tab.phi[a], t);
         }
+        return Step{&st, tokens, (tokens + p.batch - 1) / p.batch * HH};
+    };
+    // An item: `batch` tokens of one head, on one lane group.
+    struct Item {
+        const StepTokens *st;
+        int key, h, i0, count;
+    };
+    auto item = [&](const Step &s, int it) {
+        const int bat = it / HH, hh = it - bat * HH, i0 = bat * p.batch;
+        const int key = hh >= n.H;
+        return Item{s.st, key, key ? hh - n.H : hh, i0, it < s.items ? min(p.batch, s.tokens - i0) : 0};
+    };
+    auto load = [&](const Item &w, Raw<T, W> (&xr)[kBatch], Raw<T, W> (&yr)[kBackward ? kBatch : 1]) {
+        const T *in = static_cast<const T *>(w.key ? p.k : p.q) + w.h * (w.key ? n.k.h : n.q.h);
+        const T *gr = static_cast<const T *>(w.key ? p.dyk : p.dyq) + w.h * (w.key ? n.yk.h : n.yq.h);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (u < w.count) {
+                load_raw<T, VEC, W>(in + w.st->in[w.key][w.i0 + u], at, xr[u]);
+                if (kBackward) load_raw<T, VEC, W>(gr + w.st->y[w.key][w.i0 + u], at, yr[kBackward ? u : 0]);
+            }
+        }
+    };
+    auto work = [&](const Item &w, Raw<T, W> (&xr)[kBatch], Raw<T, W> (&yr)[kBackward ? kBatch : 1]) {
+        T *out = static_cast<T *>(w.key ? p.ok : p.oq) +
+                 w.h * (kBackward ? (w.key ? n.dk.h : n.dq.h) : (w.key ? n.yk.h : n.yq.h));
+        float gm[W];
+#pragma unroll
+        for (int e = 0; e < W; e += 4) {
+            const float4 g4 = *reinterpret_cast<const float4 *>(&gamma[w.key][at.at(e)]);
+            gm[e] = g4.x; gm[e + 1] = g4.y; gm[e + 2] = g4.z; gm[e + 3] = g4.w;
+        }
+        const float isq = w.key ? 0.f : 1.f, isk = w.key ? 1.f : 0.f;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (u >= p.batch) break;
+            const bool on = u < w.count;
+            const float2 *cs = w.st->cs[on ? w.i0 + u : 0];
+            float v[W], ss = 0.f;
+            unpack<T, W>(xr[u], v);
+#pragma unroll
+            for (int e = 0; e < W; ++e) ss = fmaf(v[e], v[e], ss);
+            const float r = rsqrtf(fmaf(group_sum(ss, LG), 1.f / hp, n.eps));
+            if (!kBackward) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) v[e] *= r * gm[e];
+                turn<W, LG>(v, li, n.rotary, n.halves, cs, 1.f);
+                if (on) store_part<T, VEC, W>(out + w.st->y[w.key][w.i0 + u], at, v);
+            } else {
+                float g[W], dot = 0.f;
+                unpack<T, W>(yr[kBackward ? u : 0], g);
+                turn<W, LG>(g, li, n.rotary, n.halves, cs, -1.f);
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    v[e] *= r;
+                    const float d = on ? g[e] * v[e] : 0.f;
+                    acc[0][e] = fmaf(d, isq, acc[0][e]);
+                    acc[1][e] = fmaf(d, isk, acc[1][e]);
+                    g[e] *= gm[e];
+                    dot = fmaf(g[e], v[e], dot);
+                }
+                dot = group_sum(dot, LG) * (1.f / hp);
+#pragma unroll
+                for (int e = 0; e < W; ++e) g[e] = r * fmaf(-v[e], dot, g[e]);
+                if (on) store_part<T, VEC, W>(out + w.st->d[w.key][w.i0 + u], at, g);
+            }
+        }
+    };
+    // The next item's loads are under way while one is worked on, across steps too.
+    const long long stride = (long long)gridDim.x * p.step;
+    long long tok0 = (long long)blockIdx.x * p.step;   // (below N: no block is without a step)
+    Step cur_step = fill(buf[0], tok0);
+    __syncthreads();
+    Raw<T, W> x[kBatch], dy[kBackward ? kBatch : 1];
+    Item cur = item(cur_step, grp);
+    load(cur, x, dy);
+    for (int no = 1;; no = no == 2 ? 0 : no + 1) {
+        tok0 += stride;
+        const bool more = tok0 < N;
+        Step next_step{};
+        if (more) next_step = fill(buf[no], tok0);
         __syncthreads();
-        for (int it0 = 0; it0 < items; it0 += 2 * groups) {   // (all lanes together: the sums are shuffles)
-            Item next = item(it0 + groups + grp);
-            load(next, x[1], dy[1]);
-            work(cur, x[0], dy[0]);
-            if (it0 + groups >= items) break;
-            cur = item(it0 + 2 * groups + grp);
-            load(cur, x[0], dy[0]);
-            work(next, x[1], dy[1]);
+        for (int it0 = 0; it0 < cur_step.items; it0 += groups) {   // (all lanes together: the sums are shuffles)
+            const bool last = it0 + groups >= cur_step.items;
+            Item next{cur.st, 0, 0, 0, 0};
+            if (!last) next = item(cur_step, it0 + groups + grp);
+            else if (more) next = item(next_step, grp);
+            Raw<T, W> nx[kBatch], ndy[kBackward ? kBatch : 1];
+            load(next, nx, ndy);
+            work(cur, x, dy);
+            cur = next;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                x[u] = nx[u];
+                if (kBackward) dy[kBackward ? u : 0] = ndy[kBackward ? u : 0];
+            }
         }
+        if (!more) break;
+        cur_step = next_step;
     }
     if (kBackward && p.partial != nullptr) {
 #pragma unroll
@@ -211,7 +232,9 @@ __global__ void __launch_bounds__(1024) qk_dgamma_kernel(const float *partial, i
     }
 }
 
-constexpr int kMaxBlocks = 152 * 2;   // of the backward: each keeps its dgamma to the end
+// A block stays for several steps: three blocks an SM, two in the backward, whose blocks also keep their dgamma
+// to the end.
+constexpr int kMaxBlocks = 152 * 2, kMaxForwardBlocks = 152 * 3;
 
 // Several tokens a step, and an item, only where every SM still gets some: with few, one token a
 // block starts and ends sooner.
@@ -260,7 +283,8 @@ cudaError_t launch_norm(const Norm &n, const void *q, const void *k, const void 
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) && rows16(yq, n.yq, n.bf16) &&
                      rows16(yk, n.yk, n.bf16);
     const long long N = (long long)n.B * n.T;
-    return launch<false>(p, vec, (unsigned)((N + p.step - 1) / p.step), s);
+    const long long steps = (N + p.step - 1) / p.step;
+    return launch<false>(p, vec, (unsigned)(steps < kMaxForwardBlocks ? steps : kMaxForwardBlocks), s);
 }
 
 cudaError_t launch_norm_bwd(const Norm &n, const void *q, const void *k, const void *gq,
