@@ -5,6 +5,8 @@
 // t < sinks, both below the sequence's length.
 #pragma once
 
+#include <algorithm>
+
 #include "window.h"
 
 namespace mosa {
@@ -52,15 +54,19 @@ struct KeyBlocks {
 
 // dk and dv are summed by one CTA per key tile, over the queries that see it: window + tile of them,
 // but for sinks all later ones, Tk / window times as many.  Those beyond a sink tile's window go
-// to `extra` CTAs of their own, `chunk` tiles of queries each (as many as other tiles have), which
-// leave fp32 sums of the sink rows; add_sink_rows adds them up in order.
+// to `extra` CTAs of their own, `chunk` tiles of queries each (as many as other tiles have, and more
+// where that would take over kMostExtra CTAs), which leave fp32 sums of the sink rows;
+// add_sink_rows adds them up in order.  With over kMostSinks sinks their tiles are many and
+// fill the GPU by themselves: nothing is split, so that the sums' room stays small.
 struct SinkSplit {
+    static constexpr int kMostExtra = 64, kMostSinks = 512;
     int extra = 0, chunk = 1;
     SinkSplit() = default;
     SinkSplit(const Attn &a, int tile) {
-        chunk = (a.window + tile - 2) / tile + 1;
-        const long long beyond = (long long)a.Tk - (tile - 1 + (long long)a.window), per = (long long)chunk * tile;
-        extra = a.sinks > 0 && beyond > 0 ? (int)((beyond + per - 1) / per) : 0;
+        const long long beyond = ((long long)a.Tk - (tile - 1 + (long long)a.window) + tile - 1) / tile;   // tiles
+        if (a.sinks <= 0 || a.sinks > kMostSinks || beyond <= 0) return;
+        chunk = std::max((a.window + tile - 2) / tile + 1, (int)((beyond + kMostExtra - 1) / kMostExtra));
+        extra = (int)((beyond + chunk - 1) / chunk);
     }
     __host__ __device__ int extras(const Attn &a, int tile) const { return (a.sinks + tile - 1) / tile * extra; }
     // CTAs of one key head of one sequence: the extra ones first.
