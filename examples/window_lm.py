@@ -170,7 +170,7 @@ def main(steps=150, n_mosa=0, seed=0, T=160, period=24, vocab=64, quiet=False):
         opt.zero_grad()
         loss.backward()
         opt.step()
-        losses.append(float(loss))
+        losses.append(float(loss.detach()))
         if not quiet and (i % 25 == 0 or i == steps - 1):
             print(f"step {i:4d}  loss {losses[-1]:.4f}")
     if n_mosa:

@@ -82,6 +82,21 @@ __device__ __forceinline__ void put_weights(uint32_t taddr, const float (&v)[32]
     tc_fence_before();
 }
 
+// The same in two parts: what bf16 holds of them, and 16 columns on what their rounding leaves.
+__device__ __forceinline__ void put_weights_split(uint32_t taddr, const float (&v)[32]) {
+    uint32_t w[16], y[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+        y[e] = pack_bf16x2(v[2 * e] - __uint_as_float(w[e] << 16),
+                           v[2 * e + 1] - __uint_as_float(w[e] & 0xFFFF0000u));
+    }
+    tmem_st16_async(taddr, w);
+    tmem_st16_async(taddr + 16, y);
+    tmem_stored();
+    tc_fence_before();
+}
+
 // ------------------------------------------------------------------ dK, dV
 
 template <int HD>
@@ -552,7 +567,9 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                         if (j == 0) ok = ok && wait(sm.dq_empty, (it & 1) ^ 1);
                         if (!ok) break;
                         tc_fence_after();
-                        mma_weights<5>(tdQ, tS + 128 * (g & 1), mn_major(sm.k[g % 3]), idG, j > 0);   // dQ += dS K_j
+                        const uint64_t dk = mn_major(sm.k[g % 3]);   // dQ += dS K_j
+                        mma_weights<5>(tdQ, tS + 128 * (g & 1), dk, idG, j > 0);
+                        mma_weights<5>(tdQ, tS + 128 * (g & 1) + 16, dk, idG, true);
                         mma_commit(smem_u32(&sm.k_empty[g % 3]));
                         if (j + 2 < n) s_of(g + 2);
                     }
@@ -647,7 +664,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                             fence_proxy_async();
                         }
                     }
-                    put_weights(tSj, P);
+                    put_weights_split(tSj, P);
                     warp_arrive(sm.ds_ready, lane);
                 }
                 row = row_of(min(x, all - 1));

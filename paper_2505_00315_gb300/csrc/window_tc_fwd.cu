@@ -78,7 +78,11 @@ __device__ __forceinline__ int v_tile(int j, int n) {
     return !kEarly || j == n - 1 ? 2 * j + 1 : 2 * j + 2;
 }
 
-template <int HD>
+// kSplit (Tk <= 128: every tile meets one block): P's rounding is given back by a second product with
+// what it left, in columns of S that nothing uses any more.  Short texts have few and large
+// weights, whose rounding would show in the backward's D; their time is latency, and
+// stays the same.  (In the kernel for longer ones the branch alone, never taken, cost a fifth.)
+template <int HD, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid_constant__ FwdArgs p) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using Sm = FwdSm<HD>;
@@ -186,7 +190,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     ok = ok && wait_or_abort(sm.p_ready, phase & 1, &sm.abort, p.status);
                     const int s = next();
                     if (s < 0) break;
-                    mma_weights<kEarly ? 7 : 5>(tO, tP, mn_major(sm.kv[s]), idO, j > 0);   // O += P V_j
+                    const uint64_t dv = mn_major(sm.kv[s]);
+                    mma_weights<kEarly ? 7 : 5>(tO, tP, dv, idO, j > 0);   // O += P V_j
+                    if (kSplit) mma_weights<5>(tO, tS + 16, dv, idO, true);
                     mma_commit(smem_u32(&sm.kv_empty[s]));
                     if (kEarly) mma_commit(smem_u32(&sm.pv_done));
                     // (else the next scores overwrite P: MMAs run in the order of issue)
@@ -266,6 +272,13 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     tc_fence_after();
                 }
                 tmem_st16_async(kEarly ? tP + lanes + 16 * cq : tmy, w);
+                if (kSplit) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        w[e] = pack_bf16x2(s[2 * e] - __uint_as_float(w[e] << 16),
+                                           s[2 * e + 1] - __uint_as_float(w[e] & 0xFFFF0000u));
+                    tmem_st16_async(tmy + 16, w);
+                }
                 if (j > 0 && __any_sync(0xffffffffu, grow)) {
                     // (not early: S_j was issued after P_{j-1} V_{j-1})
 #pragma unroll
@@ -343,11 +356,11 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
     if (warp == kWarps) tmem_dealloc(sm.tmem, 256);
 }
 
-template <int HD>
+template <int HD, bool kSplit>
 cudaError_t launch(const FwdArgs &p, dim3 grid, cudaStream_t s) {
     constexpr int bytes = (int)sizeof(FwdSm<HD>);
     static_assert(bytes <= 115712, "two CTAs an SM");
-    auto kernel = window_fwd_tc_kernel<HD>;
+    auto kernel = window_fwd_tc_kernel<HD, kSplit>;
     cudaError_t e = allow_smem((const void *)kernel, bytes);
     if (e != cudaSuccess) return e;
     e = launch_pdl(kernel, grid, dim3(kThreads), bytes, s, p);
@@ -381,7 +394,9 @@ bool tc_window_fwd(const Attn &a, const void *q, const void *k, const void *v, c
     p.sinks = a.sinks;
     p.scale_log2 = a.scale * kLog2e;
     const dim3 grid((a.Tq + kQ - 1) / kQ, a.H, a.B);
-    *err = a.hp <= 64 ? launch<64>(p, grid, s) : launch<128>(p, grid, s);
+    const bool split = a.Tk <= kN;
+    *err = a.hp <= 64 ? (split ? launch<64, true>(p, grid, s) : launch<64, false>(p, grid, s))
+                      : (split ? launch<128, true>(p, grid, s) : launch<128, false>(p, grid, s));
     return true;
 }
 
