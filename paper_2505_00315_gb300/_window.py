@@ -5,6 +5,7 @@ with any strides whose last is 1."""
 from __future__ import annotations
 
 import ctypes
+import operator
 
 from . import _binding as _b
 
@@ -58,43 +59,32 @@ def declare(L) -> None:
 
 # A call's host time is mostly this marshalling, so what depends on shapes, strides and types alone
 # (the checks and the library's struct) is done once for each set of them and kept as a plan; a
-# later call looks it up (1 us) and passes addresses (mosa_window_forward 20.6 -> 12.5 us).
+# later call builds the key, looks it up and passes addresses, with as few Python calls as that takes
+# (mosa_window_forward with its results' allocation 20.6 -> 15.1 us).
 _plans: dict = {}
 
 
-def _plan(key, make):
-    plan = _plans.get(key)
-    if plan is None:
-        plan = make()
-        if len(_plans) >= 512:
-            _plans.clear()
-        _plans[key] = plan
+def _keep(key, plan):
+    if len(_plans) >= 512:
+        _plans.clear()
+    _plans[key] = plan
     return plan
 
 
-def _of(*tensors):
-    """Shapes, strides and types of the tensors (None for None), as a key."""
-    key = []
-    for t in tensors:
-        if t is None:
-            key.append(None)
-        else:
-            key += (t.shape, t.stride(), t.dtype)
-    return tuple(key)
+def _sig(t):
+    """Shape, strides and type of an optional tensor, as part of a key."""
+    return None if t is None else (t.shape, t.stride(), t.dtype)
 
 
-def _key(*tensors):
-    try:
-        return _of(*tensors)
-    except AttributeError:
-        raise TypeError("every tensor argument must be a torch.Tensor") from None
-
-
-def _at(t, name) -> int:
-    """The device address of a tensor whose shape, strides and type a plan has checked."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor (libmosa runs on the GPU only)")
-    return t.data_ptr()
+def _bad(*named):
+    """Says which argument is not a tensor on the GPU."""
+    for name, t in named:
+        if t is not None and not isinstance(t, _b._torch().Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+    for name, t in named:
+        if t is not None and not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor (libmosa runs on the GPU only)")
+    raise TypeError("a tensor argument is missing")
 
 
 def _heads(t, name, like=None, dtype=None):
@@ -119,6 +109,12 @@ def _out(t, name, like, dtype):
     return _packed(like) if t is None else _heads(t, name, like, dtype)
 
 
+def _new(t):
+    """A new contiguous tensor like t (empty_like takes 0.5 us less than empty)."""
+    torch = _b._torch_mod
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _vector(t, name, shape, dtype):
     """A contiguous tensor of exactly that shape and type, or None."""
     if t is not None:
@@ -134,10 +130,19 @@ def _rank(t, name, n):
         raise ValueError(f"{name} must have {n} dimensions, got {tuple(t.shape)}")
 
 
+def _int(x, name):
+    """A Python or NumPy integer that the library's 32-bit field holds."""
+    x = operator.index(x)
+    if not -2**31 <= x < 2**31:
+        raise ValueError(f"{name} does not fit 32 bits: {x}")
+    return x
+
+
 def _space(workspace, need, name, device):
     """The given workspace, or a new one."""
     if workspace is not None:
-        _b._dev(workspace, "workspace", _b._torch_mod.uint8)
+        if not (workspace.is_cuda and workspace.dtype is _b._torch_mod.uint8 and workspace.is_contiguous()):
+            _b._dev(workspace, "workspace", _b._torch_mod.uint8)   # says what is wrong
         return workspace
     if need == 0:
         raise _b.MosaError(_b.MOSA_ERR_INVALID_ARG, name)
@@ -163,9 +168,10 @@ def _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps, halves, yq, 
     _vector(dgamma_q, "dgamma_q", (hp,), torch.float32)
     _vector(dgamma_k, "dgamma_k", (hp,), torch.float32)
     y = ("dyq", "dyk") if backward else ("out q", "out k")
-    s = MosaQkShape(B, T, H, Hkv, hp, _b._dtype_code(q), hp // 2 if rotary is None else int(rotary),
-                    1 if halves else 0, theta, eps, _heads(q, "q"), _heads(k, "k", None, dt),
-                    _out(yq, y[0], q.shape, dt), _out(yk, y[1], k.shape, dt))
+    s = MosaQkShape(B, T, H, Hkv, hp, _b._dtype_code(q),
+                    hp // 2 if rotary is None else _int(rotary, "rotary"), 1 if halves else 0, theta,
+                    eps, _heads(q, "q"), _heads(k, "k", None, dt), _out(yq, y[0], q.shape, dt),
+                    _out(yk, y[1], k.shape, dt))
     need = 0
     if backward:
         s.dq, s.dk = _out(dq, "dq", q.shape, dt), _out(dk, "dk", k.shape, dt)
@@ -183,18 +189,28 @@ def mosa_qk_norm_rope(q, k, gamma_q=None, gamma_k=None, positions=None, rotary=N
     to, q and k themselves among them."""
     torch = _b._torch()
     yq, yk = (out.get("q"), out.get("k")) if out else (None, None)
-    key = ("norm", rotary, theta, eps, halves) + _key(q, k, gamma_q, gamma_k, positions, yq, yk)
-    ref = _plan(key, lambda: _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps, halves,
-                                      yq, yk))[0]
+    try:
+        key = (1, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, rotary, theta, eps, halves,
+               _sig(gamma_q), _sig(gamma_k), _sig(positions), _sig(yq), _sig(yk))
+    except AttributeError:
+        _bad(("q", q), ("k", k), ("gamma_q", gamma_q), ("gamma_k", gamma_k), ("positions", positions),
+             ("out q", yq), ("out k", yk))
+    plan = _plans.get(key) or _keep(key, _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps,
+                                                  halves, yq, yk))
     if yq is None:
-        yq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        yq = _new(q)
     if yk is None:
-        yk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        yk = _new(k)
+    if not (q.is_cuda and k.is_cuda and yq.is_cuda and yk.is_cuda
+            and (gamma_q is None or gamma_q.is_cuda) and (gamma_k is None or gamma_k.is_cuda)
+            and (positions is None or positions.is_cuda)):
+        _bad(("q", q), ("k", k), ("gamma_q", gamma_q), ("gamma_k", gamma_k), ("positions", positions),
+             ("out q", yq), ("out k", yk))
     rc = _b.load().mosa_qk_norm_rope(
-        ref, _at(q, "q"), _at(k, "k"), None if gamma_q is None else _at(gamma_q, "gamma_q"),
-        None if gamma_k is None else _at(gamma_k, "gamma_k"),
-        None if positions is None else _at(positions, "positions"), _at(yq, "out q"),
-        _at(yk, "out k"), _b._stream(stream))
+        plan[0], q.data_ptr(), k.data_ptr(), None if gamma_q is None else gamma_q.data_ptr(),
+        None if gamma_k is None else gamma_k.data_ptr(),
+        None if positions is None else positions.data_ptr(), yq.data_ptr(), yk.data_ptr(),
+        _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_qk_norm_rope")
     return yq, yk
@@ -207,30 +223,38 @@ def mosa_qk_norm_rope_backward(q, k, gamma_q, gamma_k, dyq, dyk, positions=None,
     Returns ({"dq", "dk", "dgamma_q", "dgamma_k"}, workspace); dgamma_* are fp32 [hp].
     ``out`` may hold any of them ("dq" and "dk" may be dyq and dyk)."""
     torch = _b._torch()
-    o = out or {}
-    dq, dk, dgq, dgk = (o.get(n) for n in ("dq", "dk", "dgamma_q", "dgamma_k"))
-    if dyq is None or dyk is None:
-        raise TypeError("dyq and dyk must be torch.Tensors")
-    key = ("norm_backward", rotary, theta, eps, halves) + _key(q, k, gamma_q, gamma_k, positions, dyq,
-                                                               dyk, dq, dk, dgq, dgk)
-    ref, need, _ = _plan(key, lambda: _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps,
-                                               halves, dyq, dyk, dq, dk, dgq, dgk, True))
+    dq, dk, dgq, dgk = ((out.get("dq"), out.get("dk"), out.get("dgamma_q"), out.get("dgamma_k"))
+                        if out else (None, None, None, None))
+    try:
+        key = (2, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, rotary, theta, eps, halves,
+               _sig(gamma_q), _sig(gamma_k), _sig(positions), dyq.shape, dyq.stride(), dyq.dtype,
+               dyk.shape, dyk.stride(), dyk.dtype, out and (_sig(dq), _sig(dk), _sig(dgq), _sig(dgk)))
+    except AttributeError:
+        _bad(("q", q), ("k", k), ("gamma_q", gamma_q), ("gamma_k", gamma_k), ("dyq", dyq), ("dyk", dyk),
+             ("positions", positions), ("dq", dq), ("dk", dk), ("dgamma_q", dgq), ("dgamma_k", dgk))
+    plan = _plans.get(key) or _keep(key, _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps,
+                                                  halves, dyq, dyk, dq, dk, dgq, dgk, True))
     dev, f32 = q.device, torch.float32
     if dq is None:
-        dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        dq = _new(q)
     if dk is None:
-        dk = torch.empty(k.shape, dtype=k.dtype, device=dev)
+        dk = _new(k)
     if dgq is None:
         dgq = torch.empty(q.shape[3], dtype=f32, device=dev)
     if dgk is None:
         dgk = torch.empty(q.shape[3], dtype=f32, device=dev)
-    workspace = _space(workspace, need, "mosa_qk_norm_rope_backward", dev)
+    if not (q.is_cuda and k.is_cuda and dyq.is_cuda and dyk.is_cuda and dq.is_cuda and dk.is_cuda
+            and dgq.is_cuda and dgk.is_cuda and (gamma_q is None or gamma_q.is_cuda)
+            and (gamma_k is None or gamma_k.is_cuda) and (positions is None or positions.is_cuda)):
+        _bad(("q", q), ("k", k), ("gamma_q", gamma_q), ("gamma_k", gamma_k), ("dyq", dyq), ("dyk", dyk),
+             ("positions", positions), ("dq", dq), ("dk", dk), ("dgamma_q", dgq), ("dgamma_k", dgk))
+    workspace = _space(workspace, plan[1], "mosa_qk_norm_rope_backward", dev)
     rc = _b.load().mosa_qk_norm_rope_backward(
-        ref, _at(q, "q"), _at(k, "k"), None if gamma_q is None else _at(gamma_q, "gamma_q"),
-        None if gamma_k is None else _at(gamma_k, "gamma_k"),
-        None if positions is None else _at(positions, "positions"), _at(dyq, "dyq"), _at(dyk, "dyk"),
-        _at(dq, "dq"), _at(dk, "dk"), _at(dgq, "dgamma_q"), _at(dgk, "dgamma_k"),
-        workspace.data_ptr(), workspace.numel(), _b._stream(stream))
+        plan[0], q.data_ptr(), k.data_ptr(), None if gamma_q is None else gamma_q.data_ptr(),
+        None if gamma_k is None else gamma_k.data_ptr(),
+        None if positions is None else positions.data_ptr(), dyq.data_ptr(), dyk.data_ptr(),
+        dq.data_ptr(), dk.data_ptr(), dgq.data_ptr(), dgk.data_ptr(), workspace.data_ptr(),
+        workspace.numel(), _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_qk_norm_rope_backward")
     return {"dq": dq, "dk": dk, "dgamma_q": dgq, "dgamma_k": dgk}, workspace
@@ -249,9 +273,9 @@ def _window_plan(q, k, v, O, lse, lens, window, sinks, scale, dO=None, dq=None, 
     dt = q.dtype
     _vector(lens, "lens", (B,), torch.int32)
     _vector(lse, "lse", (B, H, Tq), torch.float32)
-    s = MosaWindowShape(B, Tq, Tk, H, Hkv, hp, _b._dtype_code(q), int(window), int(sinks), scale,
-                        _heads(q, "q"), _heads(k, "k", None, dt), _heads(v, "v", k.shape, dt),
-                        _out(O, "O", q.shape, dt))
+    s = MosaWindowShape(B, Tq, Tk, H, Hkv, hp, _b._dtype_code(q), _int(window, "window"),
+                        _int(sinks, "sinks"), scale, _heads(q, "q"), _heads(k, "k", None, dt),
+                        _heads(v, "v", k.shape, dt), _out(O, "O", q.shape, dt))
     if dO is not None:
         s.go = _heads(dO, "dO", q.shape, dt)
         s.dq, s.dk, s.dv = (_out(dq, "dq", q.shape, dt), _out(dk, "dk", k.shape, dt),
@@ -268,21 +292,31 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
     None without ``want_lse`` (where no backward follows).  ``out`` may hold "O" and "lse"."""
     torch = _b._torch()
     O, lse = (out.get("O"), out.get("lse")) if out else (None, None)
-    key = ("window", window, sinks, scale) + _key(q, k, v, O, lse, lens)
-    ref, need, _ = _plan(key, lambda: _window_plan(q, k, v, O, lse, lens, window, sinks, scale))
+    try:
+        qs = q.shape
+        key = (3, qs, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+               window, sinks, scale, _sig(lens), out and (_sig(O), _sig(lse)))
+    except AttributeError:
+        _bad(("q", q), ("k", k), ("v", v), ("lens", lens), ("O", O), ("lse", lse))
+    plan = _plans.get(key) or _keep(key, _window_plan(q, k, v, O, lse, lens, window, sinks, scale))
     dev = q.device
     if O is None:
-        O = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    if lse is None and want_lse:
-        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=dev)
-    workspace = _space(workspace, need, "mosa_window_forward", dev)
+        O = _new(q)
+    if not want_lse:
+        lse = None
+    elif lse is None:
+        lse = torch.empty((qs[0], qs[2], qs[1]), dtype=torch.float32, device=dev)
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and O.is_cuda and (lse is None or lse.is_cuda)
+            and (lens is None or lens.is_cuda)):
+        _bad(("q", q), ("k", k), ("v", v), ("lens", lens), ("O", O), ("lse", lse))
+    workspace = _space(workspace, plan[1], "mosa_window_forward", dev)
     rc = _b.load().mosa_window_forward(
-        ref, _at(q, "q"), _at(k, "k"), _at(v, "v"), None if lens is None else _at(lens, "lens"),
-        _at(O, "O"), _at(lse, "lse") if want_lse else None, workspace.data_ptr(), workspace.numel(),
-        _b._stream(stream))
+        plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lens is None else lens.data_ptr(),
+        O.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+        workspace.numel(), _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_window_forward")
-    return O, lse if want_lse else None, workspace
+    return O, lse, workspace
 
 
 def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int = 0, lens=None,
@@ -291,24 +325,33 @@ def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int
     and dv like q, k and v, dk and dv summed over the query heads that share them.  ``out`` may
     hold any of them."""
     torch = _b._torch()
-    o = out or {}
-    dq, dk, dv = o.get("dq"), o.get("dk"), o.get("dv")
-    if O is None or lse is None or dO is None or workspace is None:
-        raise TypeError("O, lse, dO and workspace must be torch.Tensors")
-    key = ("window_backward", window, sinks, scale) + _key(q, k, v, O, lse, lens, dO, dq, dk, dv)
-    ref = _plan(key, lambda: _window_plan(q, k, v, O, lse, lens, window, sinks, scale, dO, dq, dk,
-                                          dv))[0]
+    dq, dk, dv = (out.get("dq"), out.get("dk"), out.get("dv")) if out else (None, None, None)
+    try:
+        key = (4, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+               O.shape, O.stride(), O.dtype, lse.shape, lse.stride(), lse.dtype, dO.shape, dO.stride(),
+               dO.dtype, window, sinks, scale, _sig(lens), out and (_sig(dq), _sig(dk), _sig(dv)))
+    except AttributeError:
+        _bad(("q", q), ("k", k), ("v", v), ("O", O), ("lse", lse), ("dO", dO), ("lens", lens), ("dq", dq),
+             ("dk", dk), ("dv", dv))
+    plan = _plans.get(key) or _keep(key, _window_plan(q, k, v, O, lse, lens, window, sinks, scale, dO, dq,
+                                                      dk, dv))
     dev = q.device
     if dq is None:
-        dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        dq = _new(q)
     if dk is None:
-        dk = torch.empty(k.shape, dtype=k.dtype, device=dev)
+        dk = _new(k)
     if dv is None:
-        dv = torch.empty(k.shape, dtype=k.dtype, device=dev)
+        dv = _new(k)
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and O.is_cuda and lse.is_cuda and dO.is_cuda
+            and dq.is_cuda and dk.is_cuda and dv.is_cuda and (lens is None or lens.is_cuda)):
+        _bad(("q", q), ("k", k), ("v", v), ("O", O), ("lse", lse), ("dO", dO), ("lens", lens), ("dq", dq),
+             ("dk", dk), ("dv", dv))
+    if workspace is None:
+        raise TypeError("workspace must be the forward's")
     _space(workspace, 0, "mosa_window_backward", dev)
     rc = _b.load().mosa_window_backward(
-        ref, _at(q, "q"), _at(k, "k"), _at(v, "v"), None if lens is None else _at(lens, "lens"),
-        _at(O, "O"), _at(lse, "lse"), _at(dO, "dO"), _at(dq, "dq"), _at(dk, "dk"), _at(dv, "dv"),
+        plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lens is None else lens.data_ptr(),
+        O.data_ptr(), lse.data_ptr(), dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
         workspace.data_ptr(), workspace.numel(), _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_window_backward")
@@ -348,8 +391,8 @@ def _decode_plan(q, k, v, Kc, Vc, lens, O, gamma_q, gamma_k, window, sinks, norm
                _bh(O, "O", q.shape, dt), _heads(Kc, "K_cache", cache, dt),
                _heads(Vc, "V_cache", cache, dt))
     _vector(lens, "lens", (B,), _b._torch_mod.int32)
-    s = MosaDecodeShape(B, C, H, Hkv, hp, _b._dtype_code(q), int(window), int(sinks),
-                        1 if norm else 0, hp // 2 if rotary is None else int(rotary),
+    s = MosaDecodeShape(B, C, H, Hkv, hp, _b._dtype_code(q), _int(window, "window"), _int(sinks, "sinks"),
+                        1 if norm else 0, hp // 2 if rotary is None else _int(rotary, "rotary"),
                         1 if halves else 0, scale, theta, eps, *strides)
     return ctypes.byref(s), int(_b.load().mosa_window_decode_workspace_bytes(ctypes.byref(s))), s
 
@@ -365,22 +408,30 @@ def mosa_window_decode(q, k, v, K_cache, V_cache, lens, window: int, sinks: int 
     the new token; 0 skips a sequence.  Returns (O [B,H,hp], workspace)."""
     torch = _b._torch()
     O = out.get("O") if out else None
-    if lens is None:
-        raise TypeError("lens must be a torch.Tensor")
-    key = (("decode", window, sinks, norm, rotary, theta, eps, halves, scale)
-           + _key(q, k, v, K_cache, V_cache, lens, O, gamma_q, gamma_k))
-    ref, need, _ = _plan(key, lambda: _decode_plan(q, k, v, K_cache, V_cache, lens, O, gamma_q, gamma_k,
-                                                   window, sinks, norm, rotary, theta, eps, halves,
-                                                   scale))
+    try:
+        key = (5, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+               K_cache.shape, K_cache.stride(), K_cache.dtype, V_cache.shape, V_cache.stride(),
+               V_cache.dtype, lens.shape, lens.stride(), lens.dtype, _sig(O), _sig(gamma_q),
+               _sig(gamma_k), window, sinks, norm, rotary, theta, eps, halves, scale)
+    except AttributeError:
+        _bad(("q", q), ("k", k), ("v", v), ("K_cache", K_cache), ("V_cache", V_cache), ("lens", lens),
+             ("O", O), ("gamma_q", gamma_q), ("gamma_k", gamma_k))
+    plan = _plans.get(key) or _keep(key, _decode_plan(q, k, v, K_cache, V_cache, lens, O, gamma_q, gamma_k,
+                                                      window, sinks, norm, rotary, theta, eps, halves,
+                                                      scale))
     if O is None:
-        O = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    workspace = _space(workspace, need, "mosa_window_decode", q.device)
+        O = _new(q)
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and K_cache.is_cuda and V_cache.is_cuda and lens.is_cuda
+            and O.is_cuda and (gamma_q is None or gamma_q.is_cuda)
+            and (gamma_k is None or gamma_k.is_cuda)):
+        _bad(("q", q), ("k", k), ("v", v), ("K_cache", K_cache), ("V_cache", V_cache), ("lens", lens),
+             ("O", O), ("gamma_q", gamma_q), ("gamma_k", gamma_k))
+    workspace = _space(workspace, plan[1], "mosa_window_decode", q.device)
     rc = _b.load().mosa_window_decode(
-        ref, _at(q, "q"), _at(k, "k"), _at(v, "v"),
-        None if gamma_q is None else _at(gamma_q, "gamma_q"),
-        None if gamma_k is None else _at(gamma_k, "gamma_k"), _at(lens, "lens"),
-        _at(K_cache, "K_cache"), _at(V_cache, "V_cache"), _at(O, "O"), workspace.data_ptr(),
-        workspace.numel(), _b._stream(stream))
+        plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        None if gamma_q is None else gamma_q.data_ptr(),
+        None if gamma_k is None else gamma_k.data_ptr(), lens.data_ptr(), K_cache.data_ptr(),
+        V_cache.data_ptr(), O.data_ptr(), workspace.data_ptr(), workspace.numel(), _b._stream(stream))
     if rc:
         _b._check(rc, "mosa_window_decode")
     return O, workspace

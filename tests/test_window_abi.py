@@ -187,6 +187,10 @@ def test_binding_refuses():
         W.mosa_window_forward(q, k, k, 4, lens=torch.zeros(3, dtype=torch.int32))
     with pytest.raises(ValueError, match="O must have shape"):
         W.mosa_window_forward(q, k, k, 4, out={"O": k})
+    with pytest.raises(TypeError):
+        W.mosa_window_forward(q, k, k, 4.5)
+    with pytest.raises(ValueError, match="32 bits"):
+        W.mosa_window_forward(q, k, k, 2**32 + 4)
     with pytest.raises(ValueError, match="gamma_q"):
         W.mosa_qk_norm_rope(q, k, torch.zeros(32))
     with pytest.raises(ValueError, match="positions"):
