@@ -170,8 +170,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Pt
     extern __shared__ float sm[];
     float *sQ = sm, *sK = sQ + tile_floats<HD>(), *sV = sK + tile_floats<HD>(),
           *sP = sV + tile_floats<HD>();
-    const int h = blockIdx.y, b = blockIdx.z, hk = h / a.G();
-    const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kT, off = a.Tk - a.Tq;
+    const Place at(blockIdx.x, a.H, a.B);
+    const int h = at.h, b = at.b, hk = h / a.G();
+    const int i0 = ((a.Tq + kT - 1) / kT - 1 - at.tile) * kT, off = a.Tk - a.Tq;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int len = seq_len(p.lens, b, a.Tk);
     const int pf = off + i0, pl = min(off + min(i0 + kT, a.Tq), len) - 1;
@@ -292,8 +293,9 @@ __global__ void __launch_bounds__(kThreads, HD <= 64 ? 2 : 1) window_dq_simt_ker
     float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
           *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sL = sS + kT * kPS,
           *sD = sL + kT;
-    const int h = blockIdx.y, b = blockIdx.z, hk = h / a.G();
-    const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kT, off = a.Tk - a.Tq;
+    const Place at(blockIdx.x, a.H, a.B);
+    const int h = at.h, b = at.b, hk = h / a.G();
+    const int i0 = ((a.Tq + kT - 1) / kT - 1 - at.tile) * kT, off = a.Tk - a.Tq;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int len = seq_len(p.lens, b, a.Tk);
     const int pf = off + i0, pl = min(off + min(i0 + kT, a.Tq), len) - 1;
@@ -340,10 +342,11 @@ __global__ void __launch_bounds__(kThreads, HD <= 64 ? 2 : 1) window_dkv_simt_ke
     float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
           *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sP = sS + kT * kPS,
           *sL = sP + kT * kPS, *sD = sL + kT;
-    const int hk = blockIdx.y, b = blockIdx.z, G = a.G(), off = a.Tk - a.Tq;
+    const Place at(blockIdx.x, a.Hkv, a.B);
+    const int hk = at.h, b = at.b, G = a.G(), off = a.Tk - a.Tq;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int len = seq_len(p.lens, b, a.Tk);
-    const KeyTile<kT> kt(blockIdx.x, a, p.sinks, len);
+    const KeyTile<kT> kt(at.tile, a, p.sinks, len);
     const int k0 = kt.k0;
     float dk[4][HD / 16], dv[4][HD / 16];
 #pragma unroll
@@ -509,7 +512,7 @@ cudaError_t go(Kernel kernel, dim3 grid, int smem, const Attn &a, const Ptrs<T> 
 
 template <class T>
 cudaError_t fwd(const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
-    const dim3 grid((a.Tq + kT - 1) / kT, a.H, a.B);
+    const dim3 grid = grid_of((a.Tq + kT - 1) / kT, a.H, a.B);
     switch (a.hp) {
         case 16: return go(window_fwd_simt_kernel<16, T>, grid, fwd_smem<16>(), a, p, s);
         case 32: return go(window_fwd_simt_kernel<32, T>, grid, fwd_smem<32>(), a, p, s);
@@ -520,7 +523,7 @@ cudaError_t fwd(const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
 
 template <int HD, class T>
 cudaError_t bwd_hd(const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
-    const dim3 gk(p.sinks.ctas(a, kT), a.Hkv, a.B), gq((a.Tq + kT - 1) / kT, a.H, a.B);
+    const dim3 gk = grid_of(p.sinks.ctas(a, kT), a.Hkv, a.B), gq = grid_of((a.Tq + kT - 1) / kT, a.H, a.B);
     cudaError_t e = go(window_dkv_simt_kernel<HD, T>, gk, dkv_smem<HD>(), a, p, s);
     if (e == cudaSuccess) e = go(window_dq_simt_kernel<HD, T>, gq, dq_smem<HD>(), a, p, s);
     return e != cudaSuccess ? e : add_sink_rows(a, p.partial, p.sinks.extra, p.dk, p.dv, s);

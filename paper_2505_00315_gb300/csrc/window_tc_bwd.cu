@@ -121,9 +121,10 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
     constexpr int NB = Sm::NB;
     Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = blockIdx.z, hk = blockIdx.y, off = p.Tk - p.Tq;
+    const Place at(blockIdx.x, p.Hkv, p.a.B);
+    const int b = at.b, hk = at.h, off = p.Tk - p.Tq;
     const int len = seq_len(p.lens, b, p.Tk);
-    const KeyTile<kTile> kt(blockIdx.x, p.a, p.split, len);
+    const KeyTile<kTile> kt(at.tile, p.a, p.split, len);
     const int k0 = kt.k0, first = kt.first, last = kt.last;
     const bool is_extra = kt.part > 0, has_sinks = kt.has_sinks;
     const int blocks = first <= last && k0 < len ? (last - first) / kTile + 1 : 0;
@@ -428,14 +429,14 @@ struct QSm {
 
 constexpr int kQThreads = kWorkers + 64;
 
-// The x-th query tile of all, heaviest of a head first.
+// The x-th query tile of all, the heaviest first.
 struct QueryTile {
     int b, h, i0, pf, pl;
     __device__ __forceinline__ QueryTile(const BwdArgs &p, uint32_t x, int tiles) {
-        const uint32_t rest = x / (uint32_t)tiles;
-        i0 = (tiles - 1 - (int)(x - rest * tiles)) * kTile;
-        b = (int)(rest / (uint32_t)p.H);
-        h = (int)(rest - (uint32_t)(b * p.H));
+        const Place at(x, p.H, p.a.B);
+        i0 = (tiles - 1 - at.tile) * kTile;
+        b = at.b;
+        h = at.h;
         pf = p.Tk - p.Tq + i0;
         pl = min(p.Tk - p.Tq + min(i0 + kTile, p.Tq), seq_len(p.lens, b, p.Tk)) - 1;
     }
@@ -718,7 +719,7 @@ cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     const long long ctas = std::max(std::min(all, 152LL), (all + kMaxTiles - 1) / kMaxTiles);
     e = launch_pdl(window_dq_tc_kernel<HD>, dim3((unsigned)ctas), dim3(kQThreads), qb, s, p, (uint32_t)all, tiles);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(window_dkv_tc_kernel<HD>, dim3(p.split.ctas(p.a, kTile), p.Hkv, B), dim3(kKvThreads), kv, s, p);
+    e = launch_pdl(window_dkv_tc_kernel<HD>, grid_of(p.split.ctas(p.a, kTile), p.Hkv, B), dim3(kKvThreads), kv, s, p);
     if (e != cudaSuccess) return e;
     note_launches(2);
     return add_sink_rows(p.a, p.partial, p.split.extra, p.dK, p.dV, s);

@@ -40,7 +40,7 @@ struct FwdArgs {
     uint32_t *status;
     Str so;
     int keep_rest;               // what O loses by its rounding goes to `rest`
-    int Tq, Tk, H, G, hp, window, sinks;
+    int B, Tq, Tk, H, G, hp, window, sinks;
     float scale_log2;
 };
 
@@ -91,8 +91,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
     Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
-    const int b = blockIdx.z, h = blockIdx.y, hk = h / p.G;
-    const int i0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kQ, off = p.Tk - p.Tq;
+    const Place at(blockIdx.x, p.H, p.B);
+    const int b = at.b, h = at.h, hk = h / p.G;
+    const int i0 = ((p.Tq + kQ - 1) / kQ - 1 - at.tile) * kQ, off = p.Tk - p.Tq;
     const int len = seq_len(p.lens, b, p.Tk);
     const int pf = off + i0, pl = min(off + min(i0 + kQ, p.Tq), len) - 1;
     float *lse = p.lse == nullptr ? nullptr : p.lse + ((long long)b * p.H + h) * p.Tq;
@@ -387,13 +388,14 @@ bool tc_window_fwd(const Attn &a, const void *q, const void *k, const void *v, c
     p.so = a.o;
     p.Tq = a.Tq;
     p.Tk = a.Tk;
+    p.B = a.B;
     p.H = a.H;
     p.G = a.G();
     p.hp = a.hp;
     p.window = a.window;
     p.sinks = a.sinks;
     p.scale_log2 = a.scale * kLog2e;
-    const dim3 grid((a.Tq + kQ - 1) / kQ, a.H, a.B);
+    const dim3 grid = grid_of((a.Tq + kQ - 1) / kQ, a.H, a.B);
     const bool split = a.Tk <= kN;
     *err = a.hp <= 64 ? (split ? launch<64, true>(p, grid, s) : launch<64, false>(p, grid, s))
                       : (split ? launch<128, true>(p, grid, s) : launch<128, false>(p, grid, s));

@@ -52,6 +52,21 @@ struct KeyBlocks {
     }
 };
 
+// A CTA's tile, head and sequence.  Tiles count slowest, so that those with less to do, which are
+// the last of every head, are the last of all: no heavy one is left to start when
+// the others end, and CTAs that run together work on the same part of all the texts.
+struct Place {
+    int tile, h, b;
+    __device__ __forceinline__ Place(uint32_t x, int H, int B) {
+        const uint32_t all = (uint32_t)H * (uint32_t)B, t = x / all, rest = x - t * all;
+        tile = (int)t;
+        b = (int)(rest / (uint32_t)H);
+        h = (int)rest - b * H;
+    }
+};
+
+inline dim3 grid_of(int tiles, int H, int B) { return dim3((unsigned)((long long)tiles * H * B)); }
+
 // dk and dv are summed by one CTA per key tile, over the queries that see it: window + tile of them,
 // but for sinks all later ones, Tk / window times as many.  Those beyond a sink tile's window go
 // to `extra` CTAs of their own, `chunk` tiles of queries each (as many as other tiles have, and more
