@@ -167,6 +167,7 @@ constexpr int tile_floats() { return kT * (HD + 4); }
 
 template <int HD, class T>
 __global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Ptrs<T> p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     extern __shared__ float sm[];
     float *sQ = sm, *sK = sQ + tile_floats<HD>(), *sV = sK + tile_floats<HD>(),
           *sP = sV + tile_floats<HD>();
@@ -289,6 +290,7 @@ __device__ __forceinline__ void load_rows(float *sL, float *sD, const Ptrs<T> &p
 // dq of one 64-query tile.
 template <int HD, class T>
 __global__ void __launch_bounds__(kThreads, HD <= 64 ? 2 : 1) window_dq_simt_kernel(Attn a, Ptrs<T> p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     extern __shared__ float sm[];
     float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
           *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sL = sS + kT * kPS,
@@ -338,6 +340,7 @@ __global__ void __launch_bounds__(kThreads, HD <= 64 ? 2 : 1) window_dq_simt_ker
 // far queries in CTAs of their own (SinkSplit).
 template <int HD, class T>
 __global__ void __launch_bounds__(kThreads, HD <= 64 ? 2 : 1) window_dkv_simt_kernel(Attn a, Ptrs<T> p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     extern __shared__ float sm[];
     float *sQ = sm, *sG = sQ + tile_floats<HD>(), *sK = sG + tile_floats<HD>(),
           *sV = sK + tile_floats<HD>(), *sS = sV + tile_floats<HD>(), *sP = sS + kT * kPS,
@@ -505,9 +508,9 @@ template <class Kernel, class T>
 cudaError_t go(Kernel kernel, dim3 grid, int smem, const Attn &a, const Ptrs<T> &p, cudaStream_t s) {
     cudaError_t e = allow_smem((const void *)kernel, smem);
     if (e != cudaSuccess) return e;
-    kernel<<<grid, kThreads, smem, s>>>(a, p);
+    e = launch_pdl(kernel, grid, dim3(kThreads), smem, s, a, p);
     note_launches(1);
-    return cudaGetLastError();
+    return e;
 }
 
 template <class T>
