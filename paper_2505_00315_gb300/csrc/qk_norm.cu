@@ -7,7 +7,11 @@
 // again from x, which is read anyway).  A head's hp values lie on hp/W lanes, W = 16 a
 // lane where the rows' places allow it (32 bytes of bf16), else 8, so that the mean is a few
 // shuffles and nothing is staged; a block takes some tokens with all their heads and
-// computes each token's sines and cosines once for all of them, in shared memory.
+// computes each token's sines and cosines once for all of them, in shared memory.  Loads of the
+// next item are under way while one is worked on.  What bounds it is how many bytes the
+// registers keep in flight: B4 T4096, 32 + 8 heads of 128, bf16: forward 61 us (5.5 TB/s, 81% of
+// the copy rate), backward 106 (4.8 TB/s, 70%).  One new token of eight sequences: 3 us, a
+// launch and one trip to memory.
 #include <cmath>
 
 #include "head_rows.cuh"
@@ -232,21 +236,31 @@ __global__ void __launch_bounds__(1024) qk_dgamma_kernel(const float *partial, i
     }
 }
 
-// A block stays for several steps: three blocks an SM, two in the backward, whose blocks also keep their dgamma
-// to the end.
+// A block stays for several steps: three blocks an SM (a fourth would have to spill), two in the
+// backward, whose blocks also keep their dgamma to the end.
 constexpr int kMaxBlocks = 152 * 2, kMaxForwardBlocks = 152 * 3;
 
-// Several tokens a step, and an item, only where every SM still gets some: with few, one token a
-// block starts and ends sooner.
-bool many(const Norm &n) { return (long long)n.B * n.T >= 2LL * kMaxTokens * 152; }
+// Tokens of a step: as many as leave three of four SMs a block.  More tokens of a step are more
+// loads in flight and angles at work; with fewer, more SMs take part.  us, forward / backward, 16 + 4
+// heads of 64, steps of 1, 2, 4, 8 tokens:
+//      128 tokens   2.9 / 6.1    3.3 / 6.1    3.1 / 6.8    4.4 / 7.5
+//      512          4.7 / 10.6   3.7 / 8.3    3.2 / 7.0    4.4 / 7.9
+//     2048         10.8 / 19.9   8.2 / 14.3   5.7 / 13.2   5.4 / 11.0
+int tokens_of_step(const Norm &n) {
+    const long long N = (long long)n.B * n.T;
+    int t = kMaxTokens;
+    while (t > 1 && 4 * N < 3LL * 152 * t) t /= 2;
+    return t;
+}
 
 int bwd_blocks(const Norm &n) {
-    const long long N = (long long)n.B * n.T, t = many(n) ? kMaxTokens : 1, steps = (N + t - 1) / t;
+    const long long N = (long long)n.B * n.T, t = tokens_of_step(n), steps = (N + t - 1) / t;
     return (int)(steps < kMaxBlocks ? steps : kMaxBlocks);
 }
 
 // Values of a lane: 16 where rows are whole 16-byte pieces of bf16 and rotated halves split into
-// eights.  B4 T4096 H32 + 8 of 128: 16 a lane FWD16, 8 a lane FWD8.
+// eights.  B4 T4096 H32 + 8 of 128, forward: 79 us at 16 a lane, 88 at 8 (before blocks stayed for
+// several steps).
 bool wide(const Norm &n, bool vec) { return n.bf16 && vec && (!n.halves || n.rotary % 16 == 0); }
 
 template <bool kBackward, class T, bool VEC, int W>
@@ -279,7 +293,7 @@ size_t norm_workspace(const Norm &n) { return (size_t)bwd_blocks(n) * 2 * n.hp *
 
 cudaError_t launch_norm(const Norm &n, const void *q, const void *k, const void *gq, const void *gk,
                         const int32_t *pos, void *yq, void *yk, cudaStream_t s) {
-    NormArgs p{n, q, k, gq, gk, nullptr, nullptr, yq, yk, pos, nullptr, many(n) ? kMaxTokens : 1, 1};
+    NormArgs p{n, q, k, gq, gk, nullptr, nullptr, yq, yk, pos, nullptr, tokens_of_step(n), 1};
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) && rows16(yq, n.yq, n.bf16) &&
                      rows16(yk, n.yk, n.bf16);
     const long long N = (long long)n.B * n.T;
@@ -292,7 +306,7 @@ cudaError_t launch_norm_bwd(const Norm &n, const void *q, const void *k, const v
                             void *dq, void *dk, float *dgq, float *dgk, void *ws, cudaStream_t s) {
     const bool sums = dgq != nullptr || dgk != nullptr;
     NormArgs p{n, q, k, gq, gk, dyq, dyk, dq, dk, pos, sums ? (float *)ws : nullptr,
-               many(n) ? kMaxTokens : 1, 1};
+               tokens_of_step(n), 1};
     const bool vec = rows16(q, n.q, n.bf16) && rows16(k, n.k, n.bf16) &&
                      rows16(dyq, n.yq, n.bf16) && rows16(dyk, n.yk, n.bf16) &&
                      rows16(dq, n.dq, n.bf16) && rows16(dk, n.dk, n.bf16);

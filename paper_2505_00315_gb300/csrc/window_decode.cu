@@ -16,6 +16,10 @@
 //          tcgen05 would want 128 rows and its operands in shared memory; the products are
 //          a tenth of the time that the bytes take.
 //   fp32, hp = 16, unaligned rows   CUDA cores: hp/8 lanes hold a row, eight values a lane.
+// B48, up to 4100 tokens, 32 + 8 heads of 128, bf16: 126 us, 5.1 TB/s, 75% of the copy rate (on CUDA
+// cores 539: each row's products with four heads are more instructions than its bytes have
+// time for).  B1, 1028 tokens, 16 + 4 heads: 6.5 us and 3.6 for the join, latency: the norm, the
+// rotation, one trip for K, one for V, the warps' and the splits' sums in turn.
 #include "head_rows.cuh"
 #include "launch.h"
 #include "profile.h"
@@ -432,6 +436,8 @@ int heads_of(const Decode &d, bool mma) {   // query heads a CTA takes
     return mma ? kMmaHeads : G == 1 ? 1 : G == 2 ? 2 : G <= 4 ? 4 : 8;
 }
 
+// Splits of a sequence: four CTAs an SM in all, of at least 128 tokens each.  (At 8, 16 and 32 CTAs an SM
+// the 48 sequences above took 147, 157 and 183 us against 150, with the loads as they were then.)
 int splits_of(const Decode &d) {
     const int G = d.H / d.Hkv, chunks = (G + kMmaHeads - 1) / kMmaHeads;
     const long long ctas = (long long)d.B * d.Hkv * chunks;

@@ -9,10 +9,18 @@
 //           (S^T = K Q^T), so that P^T and dS^T, bf16 in TMEM in the place of the
 //           scores, are the A operands of dV and dK with no pass through shared memory.
 //   dQ      one CTA an SM, for some (128-query tile, head, sequence) each, over the key blocks they meet.
-// One kernel with five products instead of the seven here would have to add dQ up
+//           dS goes into two products, what bf16 holds of it and what that leaves: a query's dS are
+//           differences that cancel in its sum, and one rounding of them was 1.5 times the error of
+//           a form that rounds only what it stores.  (dK and dV sum over many queries, whose
+//           roundings are independent.)  Costs 512 of 2048 + 512 cycles of MMAs a block.
+// One kernel with five products instead of the eight here would have to add dQ up
 // from several CTAs: 64 KB of fp32 reductions per pair of tiles against 2560
 // cycles of MMAs (hp = 128), in an order that changes from run to run, and a pass to zero
 // and one to round it.
+// B4 T4096, 16 + 4 heads of 128, window 1024: dQ 188 us, dK and dV 202 (the tensor pipe is busy 68% of
+// both; the rest is the chain scores -> weights -> product within a block and, with one CTA an
+// SM, its beginning and end).  B2 T8192, 4 heads of 64, window 512: 36 and 42 us, where MMAs take half
+// the cycles and the elementwise work of a block is what counts.
 // Keys that are sinks are seen by every later query: those queries beyond the
 // tile's window go to CTAs of their own, some blocks each, whose fp32 sums for the
 // sink rows a last small kernel adds up in order (else the first tile's CTA would

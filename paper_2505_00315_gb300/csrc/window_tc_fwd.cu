@@ -17,6 +17,14 @@
 // With hp <= 64 P has columns of its own, and the next scores are computed as soon as
 // the warps have read the last ones.
 //
+// B1 T16384, 32 + 8 heads of 128, window 2048: 509 us, 1.01 PFLOP/s of the pairs that are seen.  With
+// hp = 128 that is bound by issue: 32 instructions for a thread's 32 scores are exponentials, the
+// others loads from TMEM, maxima, sums and the packing of P; issue slots are busy 55% of the time, the
+// tensor pipe 45%, and the rest are waits along the chain that the other CTA covers in part.
+// (Eight worker warps with 64 columns a thread: 606 us against 531 then.)  hp = 64, B2 T8192, 4
+// heads, window 512: 31 us, of which 512 CTAs' beginnings and ends are a third; early scores
+// took it from 33 there.
+//
 // A masked key has P = 0, but 0 times a NaN or infinity of its V row is NaN: a CTA whose
 // results are not all finite runs its blocks a second time with such V rows zeroed in
 // the blocks that it sees in part, and rows that do see one set to NaN.

@@ -377,3 +377,10 @@ def test_gradients_where_the_weight_lies_on_one_token(hp, force, monkeypatch):
     k[:, :1] += (0.7 * u).to(k.dtype)
     want = ref.attention(q, k, v, 24, 1, dO=dO)
     check(run(q, k, v, dO, 24, 1), want, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T", [(1, 237), (3, 101), (1, 461), (2, 299), (1, 911), (7, 131)])
+def test_norm_and_rotation_at_lengths_between(B, T, dtype):
+    """Blocks take 1, 2, 4 or 8 tokens a step by the number of tokens, the last step fewer."""
+    test_norm_and_rotation_against_64_bits(B, T, 5, 2, 64, None, False, "packed", dtype)
