@@ -4,8 +4,8 @@
 //     S = Q K^T,  P = exp(scale S - lse),  dP = dO V^T,  dS = P (dP - D)
 //     dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
 // in two kernels, so that every sum runs in one accumulator in a fixed order:
-//   dK, dV  one CTA per (128-key tile, key / value head, sequence) over the 128-query blocks
-//           of the group's heads that see it.  Scores are taken transposed
+//   dK, dV  one CTA per (128-key tile, key / value head, sequence), or one an SM for some of them, over
+//           the 128-query blocks of the group's heads that see it.  Scores are taken transposed
 //           (S^T = K Q^T), so that P^T and dS^T, bf16 in TMEM in the place of the
 //           scores, are the A operands of dV and dK with no pass through shared memory.
 //   dQ      one CTA an SM, for some (128-query tile, head, sequence) each, over the key blocks they meet.
@@ -19,7 +19,7 @@
 // and one to round it.
 // B4 T4096, 16 + 4 heads of 128, window 1024: dQ 188 us, dK and dV 202 (the tensor pipe is busy 68% of
 // both; the rest is the chain scores -> weights -> product within a block and, with one CTA an
-// SM, its beginning and end).  B2 T8192, 4 heads of 64, window 512: 36 and 42 us, where MMAs take half
+// SM, its beginning and end).  B2 T8192, 4 heads of 64, window 512: 35 and 39 us, where MMAs take half
 // the cycles and the elementwise work of a block is what counts.
 // Keys that are sinks are seen by every later query: those queries beyond the
 // tile's window go to CTAs of their own, some blocks each, whose fp32 sums for the
@@ -52,12 +52,12 @@ constexpr int kWarps = 16, kWorkers = 32 * kWarps;   // the workers'
 constexpr int kCols = 128 / (kWarps / 4);            // score columns of one worker thread
 
 struct BwdArgs {
-    Map q, k, v, go, dk, dv;
+    Map q, k, v, go;
     const int32_t *lens;
     const float *lse, *delta;           // [B, H, Tq]
     bf16 *dQ, *dK, *dV;
     Str sdq, sdk, sdv;
-    int wide_dq;                        // rows of dQ start at a multiple of 32 bytes
+    int wide_dq, wide_dk, wide_dv;      // rows of these start at a multiple of 32 bytes
     float *partial;                     // [B, Hkv, slots, sinks, 2, hp] fp32: dk, dv of the sink rows
     uint32_t *status;
     Attn a;
@@ -65,20 +65,6 @@ struct BwdArgs {
     int Tq, Tk, H, Hkv, G, hp, window, sinks;
     float scale, scale_log2;
 };
-
-// v[0 .. 15] * f of row r (zeros unless `on`) as bf16, into the 16-byte units u0 and u0+1 of its
-// 128 bytes in a staged block.
-__device__ __forceinline__ void stage_bf16_16(uint8_t *blk, int r, int u0, const float (&v)[16], float f,
-                                              bool on) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            w[e] = on ? pack_bf16x2(v[8 * u + 2 * e] * f, v[8 * u + 2 * e + 1] * f) : 0u;
-        *reinterpret_cast<uint4 *>(blk + xoff128(r, u0 + u)) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
 
 // 32 values as bf16 into the 16 TMEM columns at taddr.
 __device__ __forceinline__ void put_weights(uint32_t taddr, const float (&v)[32]) {
@@ -113,7 +99,7 @@ struct KvSm {
     uint8_t k[NB][kBlk], v[NB][kBlk];
     uint8_t q[3][NB][kBlk], go[2][NB][kBlk];
     float lse[2][kTile], delta[2][kTile];      // of a block's queries (lse in log2 units)
-    uint64_t kv_full, q_full[3], q_empty[3], g_full[2], g_empty[2], st_full[2], st_empty[2];
+    uint64_t kv_full, kv_empty, q_full[3], q_empty[3], g_full[2], g_empty[2], st_full[2], st_empty[2];
     uint64_t s_full, dp_full, p_ready, ds_ready, done, drained;
     uint32_t odd[2][4];                        // queries of the block with lse or D not finite
     uint32_t tmem;
@@ -122,40 +108,30 @@ struct KvSm {
 
 constexpr int kKvThreads = kWorkers + 96;
 
+// The x-th key tile of all and the (head of the group, block) pairs that see it, heads outermost.
+struct KeyWork {
+    int b, hk, len, blocks, n;
+    KeyTile<kTile> kt;
+    __device__ __forceinline__ KeyWork(const BwdArgs &p, const Place &at)
+        : b(at.b), hk(at.h), len(seq_len(p.lens, at.b, p.Tk)), kt(at.tile, p.a, p.split, len) {
+        blocks = kt.first <= kt.last && kt.k0 < len ? (kt.last - kt.first) / kTile + 1 : 0;
+        n = blocks * p.G;
+    }
+    __device__ __forceinline__ KeyWork(const BwdArgs &p, uint32_t x) : KeyWork(p, Place(x, p.Hkv, p.a.B)) {}
+};
+
 template <int HD>
-__global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __grid_constant__ BwdArgs p) {
+__global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __grid_constant__ BwdArgs p,
+                                                                      uint32_t all) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using Sm = KvSm<HD>;
     constexpr int NB = Sm::NB;
     Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Place at(blockIdx.x, p.Hkv, p.a.B);
-    const int b = at.b, hk = at.h, off = p.Tk - p.Tq;
-    const int len = seq_len(p.lens, b, p.Tk);
-    const KeyTile<kTile> kt(at.tile, p.a, p.split, len);
-    const int k0 = kt.k0, first = kt.first, last = kt.last;
-    const bool is_extra = kt.part > 0, has_sinks = kt.has_sinks;
-    const int blocks = first <= last && k0 < len ? (last - first) / kTile + 1 : 0;
-    const int n = blocks * p.G;            // (head of the group, block) pairs, heads outermost
-    float *sink_sums = p.partial + kt.partial_at(b, hk, p.a);
-
-    if (n == 0) {   // no query sees the tile: zeros
-        const int units = p.hp / 8;
-        if (has_sinks)
-            for (int e = threadIdx.x; e < min(kTile, p.sinks - k0) * 2 * p.hp; e += kKvThreads)
-                sink_sums[(long long)k0 * 2 * p.hp + e] = 0.f;
-        if (!is_extra)
-            for (int e = threadIdx.x; e < min(kTile, p.Tk - k0) * units; e += kKvThreads) {
-                const int t = k0 + e / units;
-                if (has_sinks && t < p.sinks) continue;
-                *reinterpret_cast<uint4 *>(p.dK + p.sdk.at(b, t, hk) + e % units * 8) = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(p.dV + p.sdv.at(b, t, hk) + e % units * 8) = make_uint4(0, 0, 0, 0);
-            }
-        pdl_wait();
-        return;
-    }
+    const int off = p.Tk - p.Tq;
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&sm.kv_full), 1);
+        mbar_init(smem_u32(&sm.kv_empty), 1);
         for (int s = 0; s < 3; ++s) {
             mbar_init(smem_u32(&sm.q_full[s]), 1);
             mbar_init(smem_u32(&sm.q_empty[s]), 1);
@@ -187,29 +163,39 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
         return wait_or_abort(bar, parity, &sm.abort, p.status);
     };
 
+    // Tiles with something to see and their blocks are numbered on (it, g).
+    int it = 0, g = 0;
+    bool ok = true;
     if (warp == kWarps) {
         if (lane == 0) {
-            const uint32_t kvb = smem_u32(&sm.kv_full);
-            mbar_expect_tx(kvb, 2 * NB * kBlk);
-            for (int c = 0; c < NB; ++c) {
-                load_box(smem_u32(sm.k[c]), p.k, kvb, 64 * c, k0, hk, b);
-                load_box(smem_u32(sm.v[c]), p.v, kvb, 64 * c, k0, hk, b);
-            }
             int nq = 0, ng = 0;
-            for (int i = 0; i < n; ++i) {
-                const int h = hk * p.G + i / blocks, i0 = first - off + kTile * (i % blocks);
-                if (!wait(sm.q_empty[i % 3], ((i / 3) & 1) ^ 1)) break;
-                mbar_expect_tx(smem_u32(&sm.q_full[i % 3]), NB * kBlk);
-                for (int c = 0; c < NB; ++c)
-                    load_box(smem_u32(sm.q[i % 3][c]), p.q, smem_u32(&sm.q_full[i % 3]), 64 * c, i0, h, b);
-                nq = i + 1;
-                if (!wait(sm.g_empty[i & 1], ((i >> 1) & 1) ^ 1)) break;
-                mbar_expect_tx(smem_u32(&sm.g_full[i & 1]), NB * kBlk);
-                for (int c = 0; c < NB; ++c)
-                    load_box(smem_u32(sm.go[i & 1][c]), p.go, smem_u32(&sm.g_full[i & 1]), 64 * c, i0, h, b);
-                ng = i + 1;
+            for (uint32_t x = blockIdx.x; x < all && ok; x += gridDim.x) {
+                const KeyWork w(p, x);
+                if (w.n == 0) continue;
+                if (!(ok = wait(sm.kv_empty, (it & 1) ^ 1))) break;
+                ++it;
+                const uint32_t kvb = smem_u32(&sm.kv_full);
+                mbar_expect_tx(kvb, 2 * NB * kBlk);
+                for (int c = 0; c < NB; ++c) {
+                    load_box(smem_u32(sm.k[c]), p.k, kvb, 64 * c, w.kt.k0, w.hk, w.b);
+                    load_box(smem_u32(sm.v[c]), p.v, kvb, 64 * c, w.kt.k0, w.hk, w.b);
+                }
+                for (int i = 0; i < w.n; ++i, ++g) {
+                    const int h = w.hk * p.G + i / w.blocks, i0 = w.kt.first - off + kTile * (i % w.blocks);
+                    if (!(ok = wait(sm.q_empty[g % 3], ((g / 3) & 1) ^ 1))) break;
+                    mbar_expect_tx(smem_u32(&sm.q_full[g % 3]), NB * kBlk);
+                    for (int c = 0; c < NB; ++c)
+                        load_box(smem_u32(sm.q[g % 3][c]), p.q, smem_u32(&sm.q_full[g % 3]), 64 * c, i0, h, w.b);
+                    nq = g + 1;
+                    if (!(ok = wait(sm.g_empty[g & 1], ((g >> 1) & 1) ^ 1))) break;
+                    mbar_expect_tx(smem_u32(&sm.g_full[g & 1]), NB * kBlk);
+                    for (int c = 0; c < NB; ++c)
+                        load_box(smem_u32(sm.go[g & 1][c]), p.go, smem_u32(&sm.g_full[g & 1]), 64 * c, i0, h, w.b);
+                    ng = g + 1;
+                }
             }
-            drain_phase(kvb, 0);
+            // what was loaded has landed
+            if (it > 0) drain_phase(smem_u32(&sm.kv_full), (it - 1) & 1);
             for (int t = max(0, nq - 3); t < nq; ++t) drain_phase(smem_u32(&sm.q_full[t % 3]), (t / 3) & 1);
             for (int t = max(0, ng - 2); t < ng; ++t) drain_phase(smem_u32(&sm.g_full[t & 1]), (t >> 1) & 1);
         }
@@ -217,196 +203,220 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
         if (elect_one()) {
             constexpr uint32_t idS = idesc_bf16(128, 128, false, false);
             constexpr uint32_t idG = idesc_bf16(128, HD, false, true);
-            bool ok = wait(sm.kv_full, 0);
             const uint64_t dk = k_major(sm.k), dv = k_major(sm.v);
-            auto s_of = [&](int i) {
-                ok = ok && wait(sm.q_full[i % 3], (i / 3) & 1);
+            auto s_of = [&](int g) {
+                ok = ok && wait(sm.q_full[g % 3], (g / 3) & 1);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores<NB>(tS, dk, k_major(sm.q[i % 3]), idS);
+                mma_scores<NB>(tS, dk, k_major(sm.q[g % 3]), idS);
                 mma_commit(smem_u32(&sm.s_full));
             };
-            auto dp_of = [&](int i) {
-                ok = ok && wait(sm.g_full[i & 1], (i >> 1) & 1);
+            // (`free`: the last product of the tile that reads K and V)
+            auto dp_of = [&](int g, bool free) {
+                ok = ok && wait(sm.g_full[g & 1], (g >> 1) & 1);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores<NB>(tG, dv, k_major(sm.go[i & 1]), idS);
+                mma_scores<NB>(tG, dv, k_major(sm.go[g & 1]), idS);
                 mma_commit(smem_u32(&sm.dp_full));
+                if (free) mma_commit(smem_u32(&sm.kv_empty));
             };
-            s_of(0);
-            dp_of(0);
-            for (int i = 0; i < n && ok; ++i) {
-                ok = wait(sm.p_ready, i & 1);
-                if (!ok) break;
-                tc_fence_after();
-                mma_weights<5>(tdV, tS, mn_major(sm.go[i & 1]), idG, i > 0);
-                mma_commit(smem_u32(&sm.g_empty[i & 1]));
-                if (i + 1 < n) s_of(i + 1);
-                ok = ok && wait(sm.ds_ready, i & 1);
-                if (!ok) break;
-                tc_fence_after();
-                mma_weights<5>(tdK, tG, mn_major(sm.q[i % 3]), idG, i > 0);
-                mma_commit(smem_u32(&sm.q_empty[i % 3]));
-                if (i + 1 < n) dp_of(i + 1);
+            auto next_of = [&](uint32_t x, int &n) {   // the next tile with something to see
+                for (n = 0; x < all; x += gridDim.x)
+                    if ((n = KeyWork(p, x).n) > 0) break;
+                return x;
+            };
+            int n, n_next;
+            uint32_t x = next_of(blockIdx.x, n);
+            if (x < all) {
+                ok = wait(sm.kv_full, 0);
+                s_of(0);
+                dp_of(0, n == 1);
             }
-            mma_commit(smem_u32(&sm.done));
+            while (x < all && ok) {
+                const uint32_t x_next = next_of(x + gridDim.x, n_next);
+                for (int i = 0; i < n && ok; ++i, ++g) {
+                    const bool last = i + 1 == n, more = !last || x_next < all;
+                    ok = wait(sm.p_ready, g & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_weights<5>(tdV, tS, mn_major(sm.go[g & 1]), idG, i > 0);
+                    mma_commit(smem_u32(&sm.g_empty[g & 1]));
+                    if (!last) s_of(g + 1);
+                    ok = ok && wait(sm.ds_ready, g & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_weights<5>(tdK, tG, mn_major(sm.q[g % 3]), idG, i > 0);
+                    mma_commit(smem_u32(&sm.q_empty[g % 3]));
+                    if (last) mma_commit(smem_u32(&sm.done));
+                    if (last && more) {
+                        ok = wait(sm.kv_full, (it + 1) & 1);
+                        s_of(g + 1);
+                    }
+                    if (more) dp_of(g + 1, last ? n_next == 1 : i + 2 == n);
+                }
+                ++it;
+                x = x_next;
+                n = n_next;
+            }
             if (!ok) {
+                mma_commit(smem_u32(&sm.done));
                 mma_commit(smem_u32(&sm.s_full));
                 mma_commit(smem_u32(&sm.dp_full));
             }
             drain_mmas(smem_u32(&sm.drained));
         }
     } else if (warp == kWarps + 2) {
-        for (int i = 0; i < n; ++i) {
-            const int u = i & 1;
-            if (!__all_sync(0xffffffffu, wait(sm.st_empty[u], ((i >> 1) & 1) ^ 1))) break;
-            const int pq = first + kTile * (i % blocks);
-            const long long row = ((long long)b * p.H + hk * p.G + i / blocks) * p.Tq + pq - off;
+        for (uint32_t x = blockIdx.x; x < all && ok; x += gridDim.x) {
+            const KeyWork w(p, x);
+            for (int i = 0; i < w.n; ++i, ++g) {
+                const int u = g & 1;
+                if (!(ok = __all_sync(0xffffffffu, wait(sm.st_empty[u], ((g >> 1) & 1) ^ 1)))) break;
+                const int pq = w.kt.first + kTile * (i % w.blocks);
+                const long long row = ((long long)w.b * p.H + w.hk * p.G + i / w.blocks) * p.Tq + pq - off;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int c = 32 * x + lane;
-                const bool on = pq + c < len;   // (len <= Tk)
-                float L = on ? p.lse[row + c] * kLog2e : 0.f, D = on ? p.delta[row + c] : 0.f;
-                const bool odd = !(fabsf(L) < INFINITY) || !(fabsf(D) < INFINITY);
-                if (odd) L = NAN;
-                sm.lse[u][c] = L;
-                sm.delta[u][c] = D;
-                // rows past the length are hidden from every key, whatever they hold (past Tk
-                // they were read as zeros)
-                const uint32_t w = __ballot_sync(0xffffffffu, on ? odd : pq + c < p.Tk);
-                if (lane == 0) sm.odd[u][x] = w;
+                for (int y = 0; y < 4; ++y) {
+                    const int c = 32 * y + lane;
+                    const bool on = pq + c < w.len;   // (len <= Tk)
+                    float L = on ? p.lse[row + c] * kLog2e : 0.f, D = on ? p.delta[row + c] : 0.f;
+                    const bool odd = !(fabsf(L) < INFINITY) || !(fabsf(D) < INFINITY);
+                    if (odd) L = NAN;
+                    sm.lse[u][c] = L;
+                    sm.delta[u][c] = D;
+                    // rows past the length are hidden from every key, whatever they hold (past Tk
+                    // they were read as zeros)
+                    const uint32_t m = __ballot_sync(0xffffffffu, on ? odd : pq + c < p.Tk);
+                    if (lane == 0) sm.odd[u][y] = m;
+                }
+                warp_arrive(sm.st_full[u], lane);
             }
-            warp_arrive(sm.st_full[u], lane);
         }
     } else {
-        const int c0 = kCols * (warp >> 2), r = (warp & 3) * 32 + lane, t = k0 + r;
+        const int c0 = kCols * (warp >> 2), r = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, at = lanes + c0;
+        const int d0 = (warp >> 2) * (HD / 4);   // this thread's quarter of the columns of dK and dV
         const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
-        bool ok = true;
-        for (int i = 0; i < n; ++i) {
-            const int u = i & 1, pq = first + kTile * (i % blocks);
-            const bool whole = pq >= k0 + kTile - 1 && pq + kTile - 1 - k0 < p.window &&
-                               pq + kTile - 1 <= last;
-            uint32_t seen = ~0u;   // which of this thread's queries see its key
-            if (!whole)
-                seen = bits(t - pq - c0, min(last, t < p.sinks ? last : t + p.window - 1) - pq - c0);
-            const float *L = sm.lse[u] + c0, *D = sm.delta[u] + c0;
-            ok = wait(sm.st_full[u], (i >> 1) & 1) && ok;
-            ok = wait(sm.s_full, i & 1) && ok;
-            tc_fence_after();
-            float raw[32];
-            tmem_get32(tS + at, raw);
-            float P[32];
-#pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-                const float4 l4 = *reinterpret_cast<const float4 *>(L + c);
-                const float2 x = fma2(make_float2(raw[c], raw[c + 1]), sl2,
-                                      make_float2(-l4.x, -l4.y));
-                const float2 y = fma2(make_float2(raw[c + 2], raw[c + 3]),
-                                      sl2, make_float2(-l4.z, -l4.w));
-                P[c] = exp2_fast(x.x);
-                P[c + 1] = exp2_fast(x.y);
-                P[c + 2] = exp2_fast(y.x);
-                P[c + 3] = exp2_fast(y.y);
-            }
-            if (!whole) {
-                hide(P, seen, 0.f);
-                if ((sm.odd[u][0] | sm.odd[u][1] | sm.odd[u][2] | sm.odd[u][3]) != 0) {
-                    // zero those queries' rows, once S and dP have been taken from them
-                    ok = wait(sm.dp_full, i & 1) && ok;
-                    const int row = threadIdx.x & 127;
-                    if (threadIdx.x < 256 && ((sm.odd[u][row >> 5] >> (row & 31)) & 1u) != 0) {
-                        uint8_t *x = threadIdx.x < 128 ? sm.q[i % 3][0] : sm.go[i & 1][0];
+        for (uint32_t x = blockIdx.x; x < all && *(volatile int *)&sm.abort == 0; x += gridDim.x) {
+            const KeyWork w(p, x);
+            const int k0 = w.kt.k0, last = w.kt.last, t = k0 + r;
+            int pq = w.kt.first, i_blk = 0;
 #pragma unroll 1
-                        for (int e = 0; e < 8 * NB; ++e)
-                            *reinterpret_cast<uint4 *>(x + (e >> 3) * kBlk + row * 128 + (e & 7) * 16) =
-                                make_uint4(0, 0, 0, 0);
-                    }
-                    fence_proxy_async();
+            for (int i = 0; i < w.n; ++i, ++g) {
+                const int u = g & 1;
+                const bool whole = pq >= k0 + kTile - 1 && pq + kTile - 1 - k0 < p.window &&
+                                   pq + kTile - 1 <= last;
+                uint32_t seen = ~0u;   // which of this thread's queries see its key
+                if (!whole)
+                    seen = bits(t - pq - c0, min(last, t < p.sinks ? last : t + p.window - 1) - pq - c0);
+                const float *L = sm.lse[u] + c0, *D = sm.delta[u] + c0;
+                wait(sm.st_full[u], (g >> 1) & 1);
+                wait(sm.s_full, g & 1);
+                tc_fence_after();
+                float raw[32];
+                tmem_get32(tS + at, raw);
+                float P[32];
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 l4 = *reinterpret_cast<const float4 *>(L + c);
+                    const float2 x = fma2(make_float2(raw[c], raw[c + 1]), sl2,
+                                          make_float2(-l4.x, -l4.y));
+                    const float2 y = fma2(make_float2(raw[c + 2], raw[c + 3]),
+                                          sl2, make_float2(-l4.z, -l4.w));
+                    P[c] = exp2_fast(x.x);
+                    P[c + 1] = exp2_fast(x.y);
+                    P[c + 2] = exp2_fast(y.x);
+                    P[c + 3] = exp2_fast(y.y);
                 }
-            }
-            put_weights(tS + at, P);
-            warp_arrive(sm.p_ready, lane);
+                if (!whole) {
+                    hide(P, seen, 0.f);
+                    if ((sm.odd[u][0] | sm.odd[u][1] | sm.odd[u][2] | sm.odd[u][3]) != 0) {
+                        // zero those queries' rows, once S and dP have been taken from them
+                        wait(sm.dp_full, g & 1);
+                        const int row = threadIdx.x & 127;
+                        if (threadIdx.x < 256 && ((sm.odd[u][row >> 5] >> (row & 31)) & 1u) != 0) {
+                            uint8_t *x = threadIdx.x < 128 ? sm.q[g % 3][0] : sm.go[g & 1][0];
+#pragma unroll 1
+                            for (int e = 0; e < 8 * NB; ++e)
+                                *reinterpret_cast<uint4 *>(x + (e >> 3) * kBlk + row * 128 + (e & 7) * 16) =
+                                    make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async();
+                    }
+                }
+                put_weights(tS + at, P);
+                warp_arrive(sm.p_ready, lane);
 
-            ok = wait(sm.dp_full, i & 1) && ok;
-            tc_fence_after();
-            tmem_get32(tG + at, raw);
+                wait(sm.dp_full, g & 1);
+                tc_fence_after();
+                tmem_get32(tG + at, raw);
 #pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-                const float4 d4 = *reinterpret_cast<const float4 *>(D + c);
-                const float2 x = mul2(make_float2(P[c], P[c + 1]),
-                                      add2(make_float2(raw[c], raw[c + 1]),
-                                           make_float2(-d4.x, -d4.y)));
-                const float2 y = mul2(make_float2(P[c + 2], P[c + 3]),
-                                      add2(make_float2(raw[c + 2], raw[c + 3]),
-                                           make_float2(-d4.z, -d4.w)));
-                P[c] = x.x;
-                P[c + 1] = x.y;
-                P[c + 2] = y.x;
-                P[c + 3] = y.y;
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 d4 = *reinterpret_cast<const float4 *>(D + c);
+                    const float2 x = mul2(make_float2(P[c], P[c + 1]),
+                                          add2(make_float2(raw[c], raw[c + 1]),
+                                               make_float2(-d4.x, -d4.y)));
+                    const float2 y = mul2(make_float2(P[c + 2], P[c + 3]),
+                                          add2(make_float2(raw[c + 2], raw[c + 3]),
+                                               make_float2(-d4.z, -d4.w)));
+                    P[c] = x.x;
+                    P[c + 1] = x.y;
+                    P[c + 2] = y.x;
+                    P[c + 3] = y.y;
+                }
+                if (!whole) {
+                    // (again: dP may be NaN where P is 0; and a query that sees one token only has
+                    // no gradient)
+                    if (p.window == 1 && p.sinks == 0) seen = 0;
+                    if (pq == 0 && c0 == 0) seen &= ~1u;
+                    hide(P, seen, 0.f);
+                }
+                put_weights(tG + at, P);
+                warp_arrive(sm.ds_ready, lane);
+                if (lane == 0) mbar_arrive(smem_u32(&sm.st_empty[u]));
+                pq += kTile;
+                if (++i_blk == w.blocks) i_blk = 0, pq = w.kt.first;
             }
-            if (!whole) {
-                // (again: dP may be NaN where P is 0; and a query that sees one token only has
-                // no gradient)
-                if (p.window == 1 && p.sinks == 0) seen = 0;
-                if (pq == 0 && c0 == 0) seen &= ~1u;
-                hide(P, seen, 0.f);
+            float dv[HD / 64][16], dk[HD / 64][16];
+            if (w.n > 0) {
+                wait(sm.done, it & 1);
+                ++it;
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < HD / 64; ++c) {
+                    tmem_ld16(tdV + lanes + d0 + 16 * c, dv[c]);
+                    tmem_ld16(tdK + lanes + d0 + 16 * c, dk[c]);
+                }
+                tc_fence_before();   // (before the arrival for the next tile's first P)
+            } else {   // no query sees the tile: zeros
+#pragma unroll
+                for (int c = 0; c < HD / 64; ++c)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) dv[c][e] = dk[c][e] = 0.f;
             }
-            put_weights(tG + at, P);
-            warp_arrive(sm.ds_ready, lane);
-            if (lane == 0) mbar_arrive(smem_u32(&sm.st_empty[u]));
-        }
-        ok = wait(sm.done, 0) && ok;
-        tc_fence_after();
-        named_barrier(1, kWorkers);
-        if (*(volatile int *)&sm.abort == 0) {
-            // this thread's quarter of the row's columns, 16 at a time
+            const bool sink = w.kt.has_sinks && t < p.sinks;
+            const bool stores = t < p.Tk && (sink || w.kt.part == 0) && *(volatile int *)&sm.abort == 0;
 #pragma unroll
-            for (int x = 0; x < HD / 64; ++x) {
-                const int c = (warp >> 2) * (HD / 4) + 16 * x;
-                float dv[16], dk[16];
-                tmem_ld16(tdV + lanes + c, dv);
-                tmem_ld16(tdK + lanes + c, dk);
-                if (!has_sinks) {
-                    stage_bf16_16(sm.v[c >> 6], r, (c & 63) >> 3, dv, 1.f, true);
-                    stage_bf16_16(sm.k[c >> 6], r, (c & 63) >> 3, dk, p.scale, true);
-                } else if (t < p.Tk && c < p.hp && (t < p.sinks || !is_extra)) {
-                    if (t < p.sinks) {
-                        float *o = sink_sums + (long long)t * 2 * p.hp + c;
+            for (int c = 0; c < HD / 64; ++c) {
+                const int d = d0 + 16 * c;
+                if (!stores || d >= p.hp) break;
+                if (sink) {
+                    float *o = p.partial + w.kt.partial_at(w.b, w.hk, p.a) + (long long)t * 2 * p.hp + d;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            o[e] = dk[e] * p.scale;
-                            o[p.hp + e] = dv[e];
-                        }
-                    } else {
-#pragma unroll
-                        for (int u = 0; u < 16; u += 8) {
-                            uint32_t wk[4], wv[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                wk[e] = pack_bf16x2(dk[u + 2 * e] * p.scale, dk[u + 2 * e + 1] * p.scale);
-                                wv[e] = pack_bf16x2(dv[u + 2 * e], dv[u + 2 * e + 1]);
-                            }
-                            *reinterpret_cast<uint4 *>(p.dK + p.sdk.at(b, t, hk) + c + u) =
-                                make_uint4(wk[0], wk[1], wk[2], wk[3]);
-                            *reinterpret_cast<uint4 *>(p.dV + p.sdv.at(b, t, hk) + c + u) =
-                                make_uint4(wv[0], wv[1], wv[2], wv[3]);
-                        }
+                    for (int e = 0; e < 16; ++e) {
+                        o[e] = dk[c][e] * p.scale;
+                        o[p.hp + e] = dv[c][e];
                     }
+                } else {
+                    uint32_t wk[8], wv[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        wk[e] = pack_bf16x2(dk[c][2 * e] * p.scale, dk[c][2 * e + 1] * p.scale);
+                        wv[e] = pack_bf16x2(dv[c][2 * e], dv[c][2 * e + 1]);
+                    }
+                    store32(p.dK + p.sdk.at(w.b, t, w.hk) + d, wk, p.wide_dk);
+                    store32(p.dV + p.sdv.at(w.b, t, w.hk) + d, wv, p.wide_dv);
                 }
             }
-            if (!has_sinks) {
-                fence_proxy_async();
-                named_barrier(1, kWorkers);
-                if (threadIdx.x == 0) {
-                    for (int c = 0; c < NB; ++c) {
-                        store_box(p.dv, smem_u32(sm.v[c]), 64 * c, k0, hk, b);
-                        store_box(p.dk, smem_u32(sm.k[c]), 64 * c, k0, hk, b);
-                    }
-                    bulk_commit();
-                    bulk_wait_read0();
-                }
-            }
+            __syncwarp();
         }
     }
     tc_fence_before();
@@ -727,7 +737,16 @@ cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     const long long ctas = std::max(std::min(all, 152LL), (all + kMaxTiles - 1) / kMaxTiles);
     e = launch_pdl(window_dq_tc_kernel<HD>, dim3((unsigned)ctas), dim3(kQThreads), qb, s, p, (uint32_t)all, tiles);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(window_dkv_tc_kernel<HD>, grid_of(p.split.ctas(p.a, kTile), p.Hkv, B), dim3(kKvThreads), kv, s, p);
+    // dK, dV: CTAs that stay where a tile meets few blocks, whose loads and first scores then run beside
+    // the end of the tile before; where it meets many, one tile a CTA, which leaves it to the GPU which SM takes the
+    // next.  Backward, us, staying / not: B2 T8192, 4 heads of 64, window 512 (5 blocks a tile)
+    // 76.7 / 81.7; B4 T4096, 16 heads of 128, window 1024 (9) 438 / 475; 16 + 4 heads of 128 (36) 414 / 412,
+    // of 64 335 / 332.
+    const long long keys = (long long)p.split.ctas(p.a, kTile) * p.Hkv * B;
+    const long long met = (long long)p.G * ((p.window + kTile - 1) / kTile + 1);
+    const long long kv_ctas = met < 24 ? std::min(keys, 152LL) : keys;
+    e = launch_pdl(window_dkv_tc_kernel<HD>, dim3((unsigned)kv_ctas), dim3(kKvThreads), kv, s, p,
+                   (uint32_t)keys);
     if (e != cudaSuccess) return e;
     note_launches(2);
     return add_sink_rows(p.a, p.partial, p.split.extra, p.dK, p.dV, s);
@@ -742,8 +761,7 @@ bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, c
     BwdArgs p;
     if (!make_map(&p.q, q, a.q, a.B, a.Tq, a.H, a.hp) || !make_map(&p.k, k, a.k, a.B, a.Tk, a.Hkv, a.hp) ||
         !make_map(&p.v, v, a.v, a.B, a.Tk, a.Hkv, a.hp) || !make_map(&p.go, dO, a.go, a.B, a.Tq, a.H, a.hp) ||
-        !rows16(dq, a.dq, true) || !make_map(&p.dk, dk, a.dk, a.B, a.Tk, a.Hkv, a.hp) ||
-        !make_map(&p.dv, dv, a.dv, a.B, a.Tk, a.Hkv, a.hp))
+        !rows16(dq, a.dq, true) || !rows16(dk, a.dk, true) || !rows16(dv, a.dv, true))
         return false;
     p.lens = lens;
     p.lse = lse;
@@ -752,7 +770,12 @@ bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, c
     p.dK = (bf16 *)dk;
     p.dV = (bf16 *)dv;
     p.sdq = a.dq;
-    p.wide_dq = (reinterpret_cast<uintptr_t>(dq) & 31) == 0 && ((a.dq.b | a.dq.t | a.dq.h) & 15) == 0;
+    auto wide = [](const void *x, const Str &st) {
+        return (reinterpret_cast<uintptr_t>(x) & 31) == 0 && ((st.b | st.t | st.h) & 15) == 0;
+    };
+    p.wide_dq = wide(dq, a.dq);
+    p.wide_dk = wide(dk, a.dk);
+    p.wide_dv = wide(dv, a.dv);
     p.sdk = a.dk;
     p.sdv = a.dv;
     p.partial = partial;
