@@ -120,7 +120,10 @@ struct KeyWork {
     __device__ __forceinline__ KeyWork(const BwdArgs &p, uint32_t x) : KeyWork(p, Place(x, p.Hkv, p.a.B)) {}
 };
 
-template <int HD>
+// kSplit (Tk <= 128, as in the forward): what P and dS lose by their rounding goes into second
+// products.  A few tokens' sums do not average their roundings (dk of 2 to 91 tokens was up to 1.8 times as
+// far off as the plain form's), and their time is latency.
+template <int HD, bool kSplit>
 __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __grid_constant__ BwdArgs p,
                                                                       uint32_t all) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -240,12 +243,14 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                     if (!ok) break;
                     tc_fence_after();
                     mma_weights<5>(tdV, tS, mn_major(sm.go[g & 1]), idG, i > 0);
+                    if (kSplit) mma_weights<5>(tdV, tS + 16, mn_major(sm.go[g & 1]), idG, true);
                     mma_commit(smem_u32(&sm.g_empty[g & 1]));
                     if (!last) s_of(g + 1);
                     ok = ok && wait(sm.ds_ready, g & 1);
                     if (!ok) break;
                     tc_fence_after();
                     mma_weights<5>(tdK, tG, mn_major(sm.q[g % 3]), idG, i > 0);
+                    if (kSplit) mma_weights<5>(tdK, tG + 16, mn_major(sm.q[g % 3]), idG, true);
                     mma_commit(smem_u32(&sm.q_empty[g % 3]));
                     if (last) mma_commit(smem_u32(&sm.done));
                     if (last && more) {
@@ -342,7 +347,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                         fence_proxy_async();
                     }
                 }
-                put_weights(tS + at, P);
+                kSplit ? put_weights_split(tS + at, P) : put_weights(tS + at, P);
                 warp_arrive(sm.p_ready, lane);
 
                 wait(sm.dp_full, g & 1);
@@ -369,7 +374,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                     if (pq == 0 && c0 == 0) seen &= ~1u;
                     hide(P, seen, 0.f);
                 }
-                put_weights(tG + at, P);
+                kSplit ? put_weights_split(tG + at, P) : put_weights(tG + at, P);
                 warp_arrive(sm.ds_ready, lane);
                 if (lane == 0) mbar_arrive(smem_u32(&sm.st_empty[u]));
                 pq += kTile;
@@ -727,7 +732,8 @@ template <int HD>
 cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     constexpr int kv = (int)sizeof(KvSm<HD>), qb = (int)sizeof(QSm<HD>);
     static_assert(kv <= 227 * 1024 && qb <= 227 * 1024, "shared memory");
-    cudaError_t e = allow_smem((const void *)window_dkv_tc_kernel<HD>, kv);
+    const auto dkv = p.Tk <= kTile ? window_dkv_tc_kernel<HD, true> : window_dkv_tc_kernel<HD, false>;
+    cudaError_t e = allow_smem((const void *)dkv, kv);
     if (e == cudaSuccess) e = allow_smem((const void *)window_dq_tc_kernel<HD>, qb);
     if (e != cudaSuccess) return e;
     // dQ first, whose CTAs all end at about the same time; then dK, dV, whose many CTAs fill the SMs
@@ -745,7 +751,7 @@ cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     const long long keys = (long long)p.split.ctas(p.a, kTile) * p.Hkv * B;
     const long long met = (long long)p.G * ((p.window + kTile - 1) / kTile + 1);
     const long long kv_ctas = met < 24 ? std::min(keys, 152LL) : keys;
-    e = launch_pdl(window_dkv_tc_kernel<HD>, dim3((unsigned)kv_ctas), dim3(kKvThreads), kv, s, p,
+    e = launch_pdl(dkv, dim3((unsigned)kv_ctas), dim3(kKvThreads), kv, s, p,
                    (uint32_t)keys);
     if (e != cudaSuccess) return e;
     note_launches(2);
