@@ -384,3 +384,22 @@ def test_gradients_where_the_weight_lies_on_one_token(hp, force, monkeypatch):
 def test_norm_and_rotation_at_lengths_between(B, T, dtype):
     """Blocks take 1, 2, 4 or 8 tokens a step by the number of tokens, the last step fewer."""
     test_norm_and_rotation_against_64_bits(B, T, 5, 2, 64, None, False, "packed", dtype)
+
+
+@pytest.mark.parametrize("dtype,hp", [("bf16", 64), ("bf16", 128), ("f32", 32)])
+@pytest.mark.parametrize("Hkv,window,sinks", [(8, 100, 2), (4, 300, 0), (8, 1, 130)])
+def test_attention_where_blocks_take_several_tiles(Hkv, window, sinks, dtype, hp):
+    """More tiles than SMs, among them ones with nothing to see, and NaN in all that is hidden."""
+    B, T, H = 8, 900, 8
+    lens = [900, 0, 130, 899, 5, 700, 257, 128]
+    q, k, v, dO = inputs(B, T, T, H, Hkv, hp, dtype, seed=window, layout="plain")
+    dl = torch.tensor(lens, device="cuda", dtype=torch.int32)
+    want = ref.attention(q, k, v, window, sinks, dl, dO=dO)
+    for x in (q, k, v, dO):
+        for b, n in enumerate(lens):
+            x[b, n:] = math.nan
+    got = run(q, k, v, dO, window, sinks, dl)
+    check(got, want, DT[dtype])
+    for b, n in enumerate(lens):
+        for name in ("O", "dq", "dk", "dv"):
+            assert (got[name][b, n:] == 0).all(), name
