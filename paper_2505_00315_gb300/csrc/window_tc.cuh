@@ -51,15 +51,19 @@ __device__ __forceinline__ void store_box(const Map &m, uint32_t src, int c, int
 }
 
 // Waits for a phase; gives up (false) when the CTA is giving up, and after the usual
-// limit, which sets the status.
+// limit, which sets the status.  Looks at the clock on every 16th try only: waiting warps share
+// their issue slots with those that compute.
 __device__ __forceinline__ bool wait_or_abort(uint64_t &bar, uint32_t parity, int *abort,
                                               uint32_t *status) {
     const uint32_t at = smem_u32(&bar);
     if (mbar_try_wait(at, parity)) return true;
-    const unsigned long long t0 = globaltimer();
-    while (!mbar_try_wait(at, parity)) {
+    unsigned long long t0 = 0;
+    for (uint32_t n = 1; !mbar_try_wait(at, parity); ++n) {
+        if ((n & 15) != 0) continue;
         if (*(volatile int *)abort) return false;
-        if (globaltimer() - t0 > kWaitLimitNs) {
+        const unsigned long long now = globaltimer();
+        if (t0 == 0) t0 = now;
+        if (now - t0 > kWaitLimitNs) {
             atomicOr(status, kStatusTimeout);
             *(volatile int *)abort = 1;
             return false;
