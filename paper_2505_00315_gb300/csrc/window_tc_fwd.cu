@@ -17,17 +17,18 @@
 // With hp <= 64 P has columns of its own, and the next scores are computed as soon as
 // the warps have read the last ones.
 //
-// B1 T16384, 32 + 8 heads of 128, window 2048: 509 us, 1.01 PFLOP/s of the pairs that are seen.  With
-// hp = 128 that is bound by issue: 32 instructions for a thread's 32 scores are exponentials, the
-// others loads from TMEM, maxima, sums and the packing of P; issue slots are busy 55% of the time, the
-// tensor pipe 45%, and the rest are waits along the chain that the other CTA covers in part.
-// (Eight worker warps with 64 columns a thread: 606 us against 531 then.)  hp = 64, B2 T8192, 4
-// heads, window 512: 31 us, of which 512 CTAs' beginnings and ends are a third; early scores
-// took it from 33 there.
+// B1 T16384, 32 + 8 heads of 128, window 2048: 482 us, 1.07 PFLOP/s of the pairs that are seen.  With
+// hp = 128 that is bound by issue and by each CTA's chain: a thread's 32 scores take 220 instructions, 96 of
+// which are maxima, scaling, exponentials, sums and packing, the others the waits, fences and exchange of
+// a block; issue slots are busy 50 to 55% of the time, the tensor pipe 45%.  (Eight worker warps with 64
+// columns a thread: 606 us against 531 then.)  hp = 64, B2 T8192, 4 heads, window 512: 30 us, of
+// which 512 CTAs' beginnings and ends are a third; early scores took it from 33 to 31 there.
 //
 // A masked key has P = 0, but 0 times a NaN or infinity of its V row is NaN: a CTA whose
 // results are not all finite runs its blocks a second time with such V rows zeroed in
 // the blocks that it sees in part, and rows that do see one set to NaN.
+#include <type_traits>
+
 #include "launch.h"
 #include "profile.h"
 #include "window_tc.cuh"
@@ -221,88 +222,92 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
             const WholeBlocks wb(kb, pf, pl, p.window);
             float *const part0 = &sm.part[0][0][r];
             float m = -1e38f, l = 0.f;   // (m: below every score, and finite)
+            // (the second pass's loop is one of its own: its code, never run, costs the first one's 5%)
+            auto weigh = [&](auto second) {
+                constexpr bool kSecond = decltype(second)::value;
 #pragma unroll 1
-            for (int j = 0; j < n; ++j, ++phase) {
-                const bool whole = wb.has(j);
-                uint32_t seen = ~0u;
-                if (!whole) seen = seen_bits(kb, j, kb.start(j), 32 * cq, pos, p.window, p.sinks);
-                wait_or_abort(sm.s_full, phase & 1, &sm.abort, p.status);
-                tc_fence_after();
-                float s[32];
-                tmem_get32(tmy, s);
-                if (kEarly) {   // S_{j+1} may be written
-                    tc_fence_before();
-                    warp_arrive(sm.s_free, lane);
-                }
-                if (!whole) hide(s, seen, -INFINITY);
-                float mx[2] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3])};
-#pragma unroll
-                for (int c = 4; c < 32; c += 4) {
-                    mx[0] = max3(mx[0], s[c], s[c + 1]);
-                    mx[1] = max3(mx[1], s[c + 2], s[c + 3]);
-                }
-                // (the buffer of this parity was last read before the last block's barrier)
-                float *const part = part0 + (phase & 1) * (4 * kQ);
-                part[cq * kQ] = fmaxf(mx[0], mx[1]);
-                named_barrier(1 + q, 128);
-                const float mb = fmaxf(max3(part[0], part[kQ], part[2 * kQ]), part[3 * kQ]) * p.scale_log2;
-                const bool grow = mb > m + kRescaleLog2;   // the same in all four threads of the row
-                const float corr = grow ? exp2_fast(m - mb) : 1.f;   // 0 on a row's first block
-                if (grow) m = mb;
-                const float2 neg = make_float2(-m, -m);
-                float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    const float2 x = fma2(make_float2(s[c], s[c + 1]), sl2, neg);
-                    s[c] = exp2_fast(x.x);
-                    s[c + 1] = exp2_fast(x.y);
-                    sum.x += s[c];
-                    sum.y += s[c + 1];
-                }
-                l = l * corr + (sum.x + sum.y);
-                if (!whole && pass == 1) {
-                    // V rows with NaN or infinities: zeroed, and NaN for the rows that see them
-                    const int t = item + v_tile<kEarly>(j, n);
-                    wait_or_abort(sm.kv_full[t % NS], (t / NS) & 1, &sm.abort, p.status);
-                    if (cq == 0) {
-                        const uint32_t odd = __ballot_sync(0xffffffffu, clean_row<NB>(sm.kv[t % NS][0], r));
-                        if (lane == 0) sm.odd[q] = odd;
-                        fence_proxy_async();
-                    }
-                    named_barrier(5, kWorkers);
-                    if ((sm.odd[cq] & seen) != 0) s[0] = NAN;   // times the row of that key, whatever it holds
-                    named_barrier(5, kWorkers);
-                }
-                uint32_t w[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
-                if (kEarly && j > 0) {   // P and O may be written: P_{j-1} V_{j-1} is done
-                    wait_or_abort(sm.pv_done, (phase & 1) ^ 1, &sm.abort, p.status);
+                for (int j = 0; j < n; ++j, ++phase) {
+                    const bool whole = wb.has(j);
+                    uint32_t seen = ~0u;
+                    if (!whole) seen = seen_bits(kb, j, kb.start(j), 32 * cq, pos, p.window, p.sinks);
+                    wait_or_abort(sm.s_full, phase & 1, &sm.abort, p.status);
                     tc_fence_after();
-                }
-                tmem_st16_async(kEarly ? tP + lanes + 16 * cq : tmy, w);
-                if (kSplit) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        w[e] = pack_bf16x2(s[2 * e] - __uint_as_float(w[e] << 16),
-                                           s[2 * e + 1] - __uint_as_float(w[e] & 0xFFFF0000u));
-                    tmem_st16_async(tmy + 16, w);
-                }
-                if (j > 0 && __any_sync(0xffffffffu, grow)) {
-                    // (not early: S_j was issued after P_{j-1} V_{j-1})
-#pragma unroll
-                    for (int c = 0; c < HD / 4; c += 16) {
-                        float o[16];
-                        tmem_ld16(tO + lanes + cq * (HD / 4) + c, o);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * corr);
-                        tmem_st16_async(tO + lanes + cq * (HD / 4) + c, w);
+                    float s[32];
+                    tmem_get32(tmy, s);
+                    if (kEarly) {   // S_{j+1} may be written
+                        tc_fence_before();
+                        warp_arrive(sm.s_free, lane);
                     }
+                    if (!whole) hide(s, seen, -INFINITY);
+                    float mx[2] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3])};
+#pragma unroll
+                    for (int c = 4; c < 32; c += 4) {
+                        mx[0] = max3(mx[0], s[c], s[c + 1]);
+                        mx[1] = max3(mx[1], s[c + 2], s[c + 3]);
+                    }
+                    // (the buffer of this parity was last read before the last block's barrier)
+                    float *const part = part0 + (phase & 1) * (4 * kQ);
+                    part[cq * kQ] = fmaxf(mx[0], mx[1]);
+                    named_barrier(1 + q, 128);
+                    const float mb = fmaxf(max3(part[0], part[kQ], part[2 * kQ]), part[3 * kQ]) * p.scale_log2;
+                    const bool grow = mb > m + kRescaleLog2;   // the same in all four threads of the row
+                    const float corr = grow ? exp2_fast(m - mb) : 1.f;   // 0 on a row's first block
+                    if (grow) m = mb;
+                    const float2 neg = make_float2(-m, -m);
+                    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        const float2 x = fma2(make_float2(s[c], s[c + 1]), sl2, neg);
+                        s[c] = exp2_fast(x.x);
+                        s[c + 1] = exp2_fast(x.y);
+                        sum = add2(sum, make_float2(s[c], s[c + 1]));
+                    }
+                    l = l * corr + (sum.x + sum.y);
+                    if (kSecond && !whole) {
+                        // V rows with NaN or infinities: zeroed, and NaN for the rows that see them
+                        const int t = item + v_tile<kEarly>(j, n);
+                        wait_or_abort(sm.kv_full[t % NS], (t / NS) & 1, &sm.abort, p.status);
+                        if (cq == 0) {
+                            const uint32_t odd = __ballot_sync(0xffffffffu, clean_row<NB>(sm.kv[t % NS][0], r));
+                            if (lane == 0) sm.odd[q] = odd;
+                            fence_proxy_async();
+                        }
+                        named_barrier(5, kWorkers);
+                        if ((sm.odd[cq] & seen) != 0) s[0] = NAN;   // times the row of that key, whatever it holds
+                        named_barrier(5, kWorkers);
+                    }
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
+                    if (kEarly && j > 0) {   // P and O may be written: P_{j-1} V_{j-1} is done
+                        wait_or_abort(sm.pv_done, (phase & 1) ^ 1, &sm.abort, p.status);
+                        tc_fence_after();
+                    }
+                    tmem_st16_async(kEarly ? tP + lanes + 16 * cq : tmy, w);
+                    if (kSplit) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            w[e] = pack_bf16x2(s[2 * e] - __uint_as_float(w[e] << 16),
+                                               s[2 * e + 1] - __uint_as_float(w[e] & 0xFFFF0000u));
+                        tmem_st16_async(tmy + 16, w);
+                    }
+                    if (j > 0 && __any_sync(0xffffffffu, grow)) {
+                        // (not early: S_j was issued after P_{j-1} V_{j-1})
+#pragma unroll
+                        for (int c = 0; c < HD / 4; c += 16) {
+                            float o[16];
+                            tmem_ld16(tO + lanes + cq * (HD / 4) + c, o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * corr);
+                            tmem_st16_async(tO + lanes + cq * (HD / 4) + c, w);
+                        }
+                    }
+                    tmem_stored();
+                    tc_fence_before();
+                    warp_arrive(sm.p_ready, lane);
                 }
-                tmem_stored();
-                tc_fence_before();
-                warp_arrive(sm.p_ready, lane);
-            }
+            };
+            pass == 0 ? weigh(std::false_type()) : weigh(std::true_type());
             item += 2 * n;
             wait_or_abort(sm.o_done, pass, &sm.abort, p.status);
             tc_fence_after();
