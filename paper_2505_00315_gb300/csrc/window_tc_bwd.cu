@@ -17,7 +17,7 @@
 // from several CTAs: 64 KB of fp32 reductions per pair of tiles against 2560
 // cycles of MMAs (hp = 128), in an order that changes from run to run, and a pass to zero
 // and one to round it.
-// B4 T4096, 16 + 4 heads of 128, window 1024: dQ 188 us, dK and dV 202 (the tensor pipe is busy 68% of
+// B4 T4096, 16 + 4 heads of 128, window 1024: dQ 186 us, dK and dV 199 (the tensor pipe is busy 68% of
 // both; the rest is the chain scores -> weights -> product within a block and, with one CTA an
 // SM, its beginning and end).  B2 T8192, 4 heads of 64, window 512: 35 and 39 us, where MMAs take half
 // the cycles and the elementwise work of a block is what counts.
