@@ -403,3 +403,57 @@ def test_attention_where_blocks_take_several_tiles(Hkv, window, sinks, dtype, hp
     for b, n in enumerate(lens):
         for name in ("O", "dq", "dk", "dv"):
             assert (got[name][b, n:] == 0).all(), name
+
+
+@pytest.mark.parametrize("force", ["0", "1"])
+def test_attention_on_tensors_past_32_bits(force, monkeypatch):
+    """Tokens 9 million elements apart, 2.7 * 10^9 from the first to the last: the same bits as packed."""
+    monkeypatch.setenv("MOSA_FORCE_SIMT", force)
+    q, k, v, dO = inputs(1, 300, 300, 2, 2, 64, "bf16", seed=21, layout="plain")
+    want = run(q, k, v, dO, 100, 2)
+    st = 9_000_000
+    far = torch.empty(299 * st + 8 * 128, device="cuda", dtype=torch.bfloat16)
+    at = [far.as_strided(q.shape, (0, st, 64, 1), 128 * n) for n in range(7)]
+    for to, x in zip(at, (q, k, v, dO)):
+        to.copy_(x)
+    O, lse, ws = mosa.mosa_window_forward(*at[:3], 100, 2)
+    g = mosa.mosa_window_backward(*at[:3], O, lse, at[3], ws, 100, 2,
+                                  out={"dq": at[4], "dk": at[5], "dv": at[6]})
+    for name, x in {"O": O, "lse": lse, **g}.items():
+        assert torch.equal(x, want[name]), name
+
+
+def test_the_calls_can_be_captured():
+    """A training step and a decoding step in one graph, replayed on other inputs."""
+    q, k, v, dO = inputs(2, 200, 200, 4, 2, 64, "bf16", seed=22, layout="plain")
+    gq, gk = (torch.rand(64, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).bfloat16()
+              for n in (1, 2))
+    lens = torch.tensor([200, 150], device="cuda", dtype=torch.int32)
+    caches = [torch.zeros(2, 64, 2, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    spaces = {}
+
+    def step():
+        yq, yk = mosa.mosa_qk_norm_rope(q, k, gq, gk)
+        O, lse, spaces["a"] = mosa.mosa_window_forward(yq, yk, v, 70, 4, lens=lens,
+                                                       workspace=spaces.get("a"))
+        g = mosa.mosa_window_backward(yq, yk, v, O, lse, dO, spaces["a"], 70, 4, lens=lens)
+        gn, spaces["n"] = mosa.mosa_qk_norm_rope_backward(q, k, gq, gk, g["dq"], g["dk"],
+                                                          workspace=spaces.get("n"))
+        o, spaces["d"] = mosa.mosa_window_decode(q[:, 0], k[:, 0], v[:, 0], *caches, lens, 60, 4,
+                                                 gamma_q=gq, gamma_k=gk, workspace=spaces.get("d"))
+        return [O, lse, g["dv"], *gn.values(), o]
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for x in (q, k, v, dO):
+        x.copy_(torch.randn(x.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(9)))
+    for c in caches:
+        c.zero_()
+    graph.replay()
+    got = [x.clone() for x in got]
+    for c in caches:
+        c.zero_()
+    for a, b in zip(got, step()):
+        assert torch.equal(a, b)
