@@ -1,0 +1,129 @@
+"""The window heads' binding without a GPU: what reaches the library, call by call.  The library is
+a stand-in that keeps the structs it is given; tensors say that they are on a GPU."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2505_00315_gb300 import _window as W
+
+
+class OnGpu(torch.Tensor):
+    """A tensor of the host that passes for one of the GPU."""
+    is_cuda = True
+
+
+class Library:
+    """Keeps the struct of each call."""
+
+    def __init__(self):
+        self.seen = []
+
+    def __getattr__(self, name):
+        def call(ref, *args):
+            if name.endswith("_bytes"):
+                return 256
+            s = ref._obj
+            self.seen.append((name, {n: getattr(s, n) for n, t in s._fields_
+                                     if t in (ctypes.c_int32, ctypes.c_float)}, args))
+            return 0
+        return call
+
+    def last(self, field):
+        return self.seen[-1][1][field]
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    L = Library()
+    monkeypatch.setattr(W._b, "load", lambda: L)
+    monkeypatch.setattr(W._b, "_stream", lambda stream: 0)
+    monkeypatch.setattr(W, "_plans", {})
+    W._b._torch()
+    return L
+
+
+def t(*shape, dtype=torch.float32):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
+
+
+Q, K = t(2, 8, 4, 64), t(2, 8, 2, 64)
+LSE, SPACE = t(2, 4, 8), t(256, dtype=torch.uint8)
+DG = {"dgamma_q": t(64), "dgamma_k": t(64)}
+
+
+def forward(window=4, sinks=1, scale=0.0):
+    return W.mosa_window_forward(Q, K, K, window, sinks, scale=scale, workspace=SPACE, out={"O": Q, "lse": LSE})
+
+
+def backward(window=4, sinks=1, scale=0.0):
+    return W.mosa_window_backward(Q, K, K, Q, LSE, Q, SPACE, window, sinks, scale=scale)
+
+
+def norm(**kw):
+    return W.mosa_qk_norm_rope(Q, K, **kw)
+
+
+def norm_backward(**kw):
+    return W.mosa_qk_norm_rope_backward(Q, K, None, None, Q, K, workspace=SPACE, out=DG, **kw)
+
+
+def decode(window=4, sinks=1, **kw):
+    return W.mosa_window_decode(Q[:, 0], K[:, 0], K[:, 0], t(2, 8, 2, 64), t(2, 8, 2, 64),
+                                t(2, dtype=torch.int32), window, sinks, workspace=SPACE,
+                                out={"O": t(2, 4, 64)}, **kw)
+
+
+FLOATS = [(forward, "scale"), (backward, "scale"), (decode, "scale")] + [
+    (f, n) for f in (norm, norm_backward, decode) for n in ("theta", "eps")]
+INTS = [(f, n) for f in (forward, backward, decode) for n in ("window", "sinks")] + [
+    (f, "rotary") for f in (norm, norm_backward, decode)]
+
+
+@pytest.mark.parametrize("call,name", FLOATS, ids=lambda x: getattr(x, "__name__", x))
+def test_a_number_that_changes_in_place_counts_at_every_call(call, name, lib):
+    """A learned scale, say: the optimizer writes to the same tensor."""
+    x = torch.tensor(1.5)
+    call(**{name: x})
+    assert lib.last(name) == 1.5
+    x.fill_(2.5)
+    call(**{name: x})
+    assert lib.last(name) == 2.5
+    call(**{name: 3})
+    assert lib.last(name) == 3.0
+
+
+@pytest.mark.parametrize("call,name", INTS, ids=lambda x: getattr(x, "__name__", x))
+def test_an_integer_that_changes_in_place_counts_at_every_call(call, name, lib):
+    x = torch.tensor(2)
+    call(**{name: x})
+    assert lib.last(name) == 2
+    x.fill_(4)
+    call(**{name: x})
+    assert lib.last(name) == 4
+
+
+@pytest.mark.parametrize("call,name", INTS, ids=lambda x: getattr(x, "__name__", x))
+def test_what_is_refused_is_refused_after_an_equal_integer_too(call, name, lib):
+    call(**{name: 4})
+    with pytest.raises(TypeError):
+        call(**{name: 4.0})
+
+
+@pytest.mark.parametrize("call,name", [(norm, "halves"), (norm_backward, "halves"), (decode, "halves"),
+                                       (decode, "norm")], ids=lambda x: getattr(x, "__name__", x))
+def test_a_truth_value_that_changes_in_place_counts_at_every_call(call, name, lib):
+    x = torch.tensor(False)
+    call(**{name: x})
+    assert lib.last(name) == 0
+    x.fill_(True)
+    call(**{name: x})
+    assert lib.last(name) == 1
+
+
+def test_equal_calls_share_a_plan(lib):
+    for _ in range(3):
+        forward(scale=0.25), forward(scale=torch.tensor(0.25)), norm(theta=100), norm(theta=100.0)
+    assert len(W._plans) == 2 and all(math.isclose(s["scale"], 0.25) for n, s, _ in lib.seen
+                                      if n == "mosa_window_forward")
