@@ -152,6 +152,13 @@ def _rotation(rotary, theta, eps, halves):
             eps if type(eps) is float else _float(eps), 1 if halves else 0)
 
 
+def _on(stream):
+    """The context in which a call for ``stream`` runs: with it the current one, so that what the call
+    allocates (and zeroes) is that stream's too."""
+    cuda = _b._torch().cuda
+    return cuda.stream(stream if isinstance(stream, cuda.Stream) else cuda.ExternalStream(stream.cuda_stream))
+
+
 def _space(workspace, need, name, device):
     """The given workspace, or a new one."""
     if workspace is not None:
@@ -200,6 +207,9 @@ def mosa_qk_norm_rope(q, k, gamma_q=None, gamma_k=None, positions=None, rotary=N
     ``rotary`` dimensions (hp/2 by default) by t * theta^(-2p/rotary), neighbours or, with
     ``halves``, (p, p + rotary/2).  Returns (yq, yk); ``out`` may hold "q" and "k" to write
     to, q and k themselves among them."""
+    if stream is not None:
+        with _on(stream):
+            return mosa_qk_norm_rope(q, k, gamma_q, gamma_k, positions, rotary, theta, eps, halves, out)
     torch = _b._torch()
     yq, yk = (out.get("q"), out.get("k")) if out else (None, None)
     rotary, theta, eps, halves = _rotation(rotary, theta, eps, halves)
@@ -224,7 +234,7 @@ def mosa_qk_norm_rope(q, k, gamma_q=None, gamma_k=None, positions=None, rotary=N
         plan[0], q.data_ptr(), k.data_ptr(), None if gamma_q is None else gamma_q.data_ptr(),
         None if gamma_k is None else gamma_k.data_ptr(),
         None if positions is None else positions.data_ptr(), yq.data_ptr(), yk.data_ptr(),
-        _b._stream(stream))
+        _b._stream(None))
     if rc:
         _b._check(rc, "mosa_qk_norm_rope")
     return yq, yk
@@ -236,6 +246,10 @@ def mosa_qk_norm_rope_backward(q, k, gamma_q, gamma_k, dyq, dyk, positions=None,
     """Gradients of mosa_qk_norm_rope from its inputs and the gradients of its outputs.
     Returns ({"dq", "dk", "dgamma_q", "dgamma_k"}, workspace); dgamma_* are fp32 [hp].
     ``out`` may hold any of them ("dq" and "dk" may be dyq and dyk)."""
+    if stream is not None:
+        with _on(stream):
+            return mosa_qk_norm_rope_backward(q, k, gamma_q, gamma_k, dyq, dyk, positions, rotary, theta, eps, halves,
+                                              workspace, out)
     torch = _b._torch()
     dq, dk, dgq, dgk = ((out.get("dq"), out.get("dk"), out.get("dgamma_q"), out.get("dgamma_k"))
                         if out else (None, None, None, None))
@@ -269,7 +283,7 @@ def mosa_qk_norm_rope_backward(q, k, gamma_q, gamma_k, dyq, dyk, positions=None,
         None if gamma_k is None else gamma_k.data_ptr(),
         None if positions is None else positions.data_ptr(), dyq.data_ptr(), dyk.data_ptr(),
         dq.data_ptr(), dk.data_ptr(), dgq.data_ptr(), dgk.data_ptr(), workspace.data_ptr(),
-        workspace.numel(), _b._stream(stream))
+        workspace.numel(), _b._stream(None))
     if rc:
         _b._check(rc, "mosa_qk_norm_rope_backward")
     return {"dq": dq, "dk": dk, "dgamma_q": dgq, "dgamma_k": dgk}, workspace
@@ -305,6 +319,9 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
     first ``sinks``, below its sequence's length (lens [B] int32, Tk by default).
     scale = 0 is 1/sqrt(hp).  Returns (O, lse, workspace): O like q, lse [B,H,Tq] fp32, or
     None without ``want_lse`` (where no backward follows).  ``out`` may hold "O" and "lse"."""
+    if stream is not None:
+        with _on(stream):
+            return mosa_window_forward(q, k, v, window, sinks, lens, scale, workspace, out, None, want_lse)
     torch = _b._torch()
     O, lse = (out.get("O"), out.get("lse")) if out else (None, None)
     window, sinks = _int(window, "window"), _int(sinks, "sinks")
@@ -330,7 +347,7 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
     rc = _b.load().mosa_window_forward(
         plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lens is None else lens.data_ptr(),
         O.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-        workspace.numel(), _b._stream(stream))
+        workspace.numel(), _b._stream(None))
     if rc:
         _b._check(rc, "mosa_window_forward")
     return O, lse, workspace
@@ -341,6 +358,9 @@ def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int
     """Gradients of mosa_window_forward, given its outputs and its workspace: a dict with dq, dk
     and dv like q, k and v, dk and dv summed over the query heads that share them.  ``out`` may
     hold any of them."""
+    if stream is not None:
+        with _on(stream):
+            return mosa_window_backward(q, k, v, O, lse, dO, workspace, window, sinks, lens, scale, out)
     torch = _b._torch()
     dq, dk, dv = (out.get("dq"), out.get("dk"), out.get("dv")) if out else (None, None, None)
     window, sinks = _int(window, "window"), _int(sinks, "sinks")
@@ -371,7 +391,7 @@ def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int
     rc = _b.load().mosa_window_backward(
         plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lens is None else lens.data_ptr(),
         O.data_ptr(), lse.data_ptr(), dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-        workspace.data_ptr(), workspace.numel(), _b._stream(stream))
+        workspace.data_ptr(), workspace.numel(), _b._stream(None))
     if rc:
         _b._check(rc, "mosa_window_backward")
     return {"dq": dq, "dk": dk, "dv": dv}
@@ -424,6 +444,10 @@ def mosa_window_decode(q, k, v, K_cache, V_cache, lens, window: int, sinks: int 
     slots of the ring caches [B,C,Hkv,hp] (token t < sinks in slot t, else sinks +
     (t - sinks) % (C - sinks)), and q attends over the visible tokens.  lens [B] int32 counts
     the new token; 0 skips a sequence.  Returns (O [B,H,hp], workspace)."""
+    if stream is not None:
+        with _on(stream):
+            return mosa_window_decode(q, k, v, K_cache, V_cache, lens, window, sinks, gamma_q, gamma_k, norm, rotary,
+                                      theta, eps, halves, scale, workspace, out)
     torch = _b._torch()
     O = out.get("O") if out else None
     window, sinks, norm = _int(window, "window"), _int(sinks, "sinks"), 1 if norm else 0
@@ -452,7 +476,7 @@ def mosa_window_decode(q, k, v, K_cache, V_cache, lens, window: int, sinks: int 
         plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(),
         None if gamma_q is None else gamma_q.data_ptr(),
         None if gamma_k is None else gamma_k.data_ptr(), lens.data_ptr(), K_cache.data_ptr(),
-        V_cache.data_ptr(), O.data_ptr(), workspace.data_ptr(), workspace.numel(), _b._stream(stream))
+        V_cache.data_ptr(), O.data_ptr(), workspace.data_ptr(), workspace.numel(), _b._stream(None))
     if rc:
         _b._check(rc, "mosa_window_decode")
     return O, workspace

@@ -1,7 +1,9 @@
 """The window heads' binding without a GPU: what reaches the library, call by call.  The library is
 a stand-in that keeps the structs it is given; tensors say that they are on a GPU."""
+import contextlib
 import ctypes
 import math
+import types
 
 import pytest
 import torch
@@ -50,6 +52,7 @@ def t(*shape, dtype=torch.float32):
 
 Q, K = t(2, 8, 4, 64), t(2, 8, 2, 64)
 LSE, SPACE = t(2, 4, 8), t(256, dtype=torch.uint8)
+CACHE, LENS = t(2, 8, 2, 64), t(2, dtype=torch.int32)
 DG = {"dgamma_q": t(64), "dgamma_k": t(64)}
 
 
@@ -70,8 +73,7 @@ def norm_backward(**kw):
 
 
 def decode(window=4, sinks=1, **kw):
-    return W.mosa_window_decode(Q[:, 0], K[:, 0], K[:, 0], t(2, 8, 2, 64), t(2, 8, 2, 64),
-                                t(2, dtype=torch.int32), window, sinks, workspace=SPACE,
+    return W.mosa_window_decode(Q[:, 0], K[:, 0], K[:, 0], CACHE, CACHE, LENS, window, sinks, workspace=SPACE,
                                 out={"O": t(2, 4, 64)}, **kw)
 
 
@@ -127,3 +129,42 @@ def test_equal_calls_share_a_plan(lib):
         forward(scale=0.25), forward(scale=torch.tensor(0.25)), norm(theta=100), norm(theta=100.0)
     assert len(W._plans) == 2 and all(math.isclose(s["scale"], 0.25) for n, s, _ in lib.seen
                                       if n == "mosa_window_forward")
+
+
+ON_A_STREAM = {
+    "norm": lambda S: W.mosa_qk_norm_rope(Q, K, stream=S),
+    "norm_backward": lambda S: W.mosa_qk_norm_rope_backward(Q, K, None, None, Q, K, stream=S),
+    "forward": lambda S: W.mosa_window_forward(Q, K, K, 4, stream=S),
+    "backward": lambda S: W.mosa_window_backward(Q, K, K, Q, LSE, Q, SPACE, 4, stream=S),
+    "decode": lambda S: W.mosa_window_decode(Q[:, 0], K[:, 0], K[:, 0], CACHE, CACHE, LENS, 4, stream=S),
+}
+
+
+@pytest.mark.parametrize("call", ON_A_STREAM.values(), ids=ON_A_STREAM)
+def test_results_and_workspaces_of_a_call_for_a_stream_are_of_that_stream(call, lib, monkeypatch):
+    """Made, and zeroed, on another stream they could still be in use there, or be zeroed after the
+    call's kernels have written them."""
+    current, made = [0], []
+
+    @contextlib.contextmanager
+    def stream(x):
+        current.append(x.cuda_stream)
+        yield
+        current.pop()
+
+    def on(f):
+        def make(*args, **kw):
+            made.append(current[-1])
+            return f(*args, **kw).as_subclass(OnGpu)
+        return make
+
+    S = types.SimpleNamespace(cuda_stream=77)
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda n: types.SimpleNamespace(cuda_stream=n))
+    monkeypatch.setattr(W._b, "_stream", lambda x: current[-1] if x is None else x.cuda_stream)
+    for name in ("empty", "zeros", "empty_like"):
+        monkeypatch.setattr(torch, name, on(getattr(torch, name)))
+    call(S)
+    assert lib.seen[-1][2][-1] == 77          # where the kernels go
+    assert made and set(made) == {77}
+    assert current == [0]
