@@ -3,7 +3,7 @@
 // P is computed again from the forward's lse; with D = sum(dO o O) per query
 //     S = Q K^T,  P = exp(scale S - lse),  dP = dO V^T,  dS = P (dP - D)
 //     dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
-// in two kernels, so that every sum runs in one accumulator in a fixed order:
+// in two parts, so that every sum runs in one accumulator in a fixed order:
 //   dK, dV  one CTA per (128-key tile, key / value head, sequence), or one an SM for some of them, over
 //           the 128-query blocks of the group's heads that see it.  Scores are taken transposed
 //           (S^T = K Q^T), so that P^T and dS^T, bf16 in TMEM in the place of the
@@ -13,7 +13,8 @@
 //           differences that cancel in its sum, and one rounding of them was 1.5 times the error of
 //           a form that rounds only what it stores.  (dK and dV sum over many queries, whose
 //           roundings are independent.)  Costs 512 of 2048 + 512 cycles of MMAs a block.
-// One kernel with five products instead of the eight here would have to add dQ up
+// CTAs of both are one grid, dQ's first (see window_grad_tc_kernel).
+// One part with five products instead of the eight here would have to add dQ up
 // from several CTAs: 64 KB of fp32 reductions per pair of tiles against 2560
 // cycles of MMAs (hp = 128), in an order that changes from run to run, and a pass to zero
 // and one to round it.
@@ -64,7 +65,16 @@ struct BwdArgs {
     SinkSplit split;
     int Tq, Tk, H, Hkv, G, hp, window, sinks;
     float scale, scale_log2;
+    uint32_t q_ctas, q_tiles, kv_tiles;  // CTAs and tiles of dQ, tiles of dK, dV
 };
+
+// Which of a part's CTAs this is: it takes tiles x, x + ctas, x + 2 ctas ..
+struct Share {
+    uint32_t x, ctas;
+};
+
+// Threads of a CTA: the workers, the loader, the issuer and (dK, dV) one warp for lse and D.
+constexpr int kThreads = kWorkers + 96;
 
 // 32 values as bf16 into the 16 TMEM columns at taddr.
 __device__ __forceinline__ void put_weights(uint32_t taddr, const float (&v)[32]) {
@@ -106,8 +116,6 @@ struct KvSm {
     int abort;
 };
 
-constexpr int kKvThreads = kWorkers + 96;
-
 // The x-th key tile of all and the (head of the group, block) pairs that see it, heads outermost.
 struct KeyWork {
     int b, hk, len, blocks, n;
@@ -124,12 +132,11 @@ struct KeyWork {
 // products.  A few tokens' sums do not average their roundings (dk of 2 to 91 tokens was up to 1.8 times as
 // far off as the plain form's), and their time is latency.
 template <int HD, bool kSplit>
-__global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __grid_constant__ BwdArgs p,
-                                                                      uint32_t all) {
-    extern __shared__ __align__(1024) uint8_t smem_raw[];
+__device__ __forceinline__ void key_grads(const BwdArgs &p, uint8_t *smem, const Share cta) {
     using Sm = KvSm<HD>;
     constexpr int NB = Sm::NB;
-    Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
+    Sm &sm = *reinterpret_cast<Sm *>(smem);
+    const uint32_t all = p.kv_tiles;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int off = p.Tk - p.Tq;
     if (threadIdx.x == 0) {
@@ -172,7 +179,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
     if (warp == kWarps) {
         if (lane == 0) {
             int nq = 0, ng = 0;
-            for (uint32_t x = blockIdx.x; x < all && ok; x += gridDim.x) {
+            for (uint32_t x = cta.x; x < all && ok; x += cta.ctas) {
                 const KeyWork w(p, x);
                 if (w.n == 0) continue;
                 if (!(ok = wait(sm.kv_empty, (it & 1) ^ 1))) break;
@@ -224,19 +231,19 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
                 if (free) mma_commit(smem_u32(&sm.kv_empty));
             };
             auto next_of = [&](uint32_t x, int &n) {   // the next tile with something to see
-                for (n = 0; x < all; x += gridDim.x)
+                for (n = 0; x < all; x += cta.ctas)
                     if ((n = KeyWork(p, x).n) > 0) break;
                 return x;
             };
             int n, n_next;
-            uint32_t x = next_of(blockIdx.x, n);
+            uint32_t x = next_of(cta.x, n);
             if (x < all) {
                 ok = wait(sm.kv_full, 0);
                 s_of(0);
                 dp_of(0, n == 1);
             }
             while (x < all && ok) {
-                const uint32_t x_next = next_of(x + gridDim.x, n_next);
+                const uint32_t x_next = next_of(x + cta.ctas, n_next);
                 for (int i = 0; i < n && ok; ++i, ++g) {
                     const bool last = i + 1 == n, more = !last || x_next < all;
                     ok = wait(sm.p_ready, g & 1);
@@ -271,7 +278,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
             drain_mmas(smem_u32(&sm.drained));
         }
     } else if (warp == kWarps + 2) {
-        for (uint32_t x = blockIdx.x; x < all && ok; x += gridDim.x) {
+        for (uint32_t x = cta.x; x < all && ok; x += cta.ctas) {
             const KeyWork w(p, x);
             for (int i = 0; i < w.n; ++i, ++g) {
                 const int u = g & 1;
@@ -300,7 +307,7 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, at = lanes + c0;
         const int d0 = (warp >> 2) * (HD / 4);   // this thread's quarter of the columns of dK and dV
         const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
-        for (uint32_t x = blockIdx.x; x < all && *(volatile int *)&sm.abort == 0; x += gridDim.x) {
+        for (uint32_t x = cta.x; x < all && *(volatile int *)&sm.abort == 0; x += cta.ctas) {
             const KeyWork w(p, x);
             const int k0 = w.kt.k0, last = w.kt.last, t = k0 + r;
             int pq = w.kt.first, i_blk = 0;
@@ -428,7 +435,6 @@ __global__ void __launch_bounds__(kKvThreads, 1) window_dkv_tc_kernel(const __gr
     __syncthreads();
     tc_fence_after();
     if (warp == kWarps) tmem_dealloc(sm.tmem, 512);
-    pdl_wait();   // this kernel ends after the dQ kernel that it started beside
 }
 
 // ---------------------------------------------------------------------- dQ
@@ -450,8 +456,6 @@ struct QSm {
     uint8_t again[kMaxTiles];   // tiles whose results are not all finite
 };
 
-constexpr int kQThreads = kWorkers + 64;
-
 // The x-th query tile of all, the heaviest first.
 struct QueryTile {
     int b, h, i0, pf, pl;
@@ -467,15 +471,12 @@ struct QueryTile {
 };
 
 template <int HD>
-__global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid_constant__ BwdArgs p,
-                                                                    uint32_t all, int tiles) {
-    extern __shared__ __align__(1024) uint8_t smem_raw[];
+__device__ __forceinline__ void query_grads(const BwdArgs &p, uint8_t *smem, const Share cta) {
     using Sm = QSm<HD>;
     constexpr int NB = Sm::NB;
-    Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    pdl_wait();      // D, and all that came before it
-    pdl_trigger();   // the dK, dV kernel may take the SMs that this one leaves
+    Sm &sm = *reinterpret_cast<Sm *>(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tiles = (p.Tq + kTile - 1) / kTile;
+    const uint32_t all = p.q_tiles;
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&sm.q_full), 1);
         mbar_init(smem_u32(&sm.q_empty), 1);
@@ -517,7 +518,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
             if (lane == 0) {
                 int nq = it, nk = g, nv = g;
                 for (int t = 0; ok; ++t) {
-                    const uint32_t x = blockIdx.x + (uint32_t)t * gridDim.x;
+                    const uint32_t x = cta.x + (uint32_t)t * cta.ctas;
                     if (x >= all) break;
                     if (pass == 1 && sm.again[t] == 0) continue;
                     const QueryTile w(p, x, tiles);
@@ -573,7 +574,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                     if (last) mma_commit(smem_u32(&sm.q_empty));   // (the last scores came before)
                 };
                 for (int t = 0; ok; ++t) {
-                    const uint32_t x = blockIdx.x + (uint32_t)t * gridDim.x;
+                    const uint32_t x = cta.x + (uint32_t)t * cta.ctas;
                     if (x >= all) break;
                     if (pass == 1 && sm.again[t] == 0) continue;
                     const QueryTile w(p, x, tiles);
@@ -607,7 +608,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 }
             }
             __syncwarp();
-        } else {
+        } else if (warp < kWarps) {
             const int c0 = kCols * (warp >> 2), r = (warp & 3) * 32 + lane;
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
             const int d0 = (warp >> 2) * (HD / 4);   // this thread's quarter of the columns of dQ
@@ -630,11 +631,11 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 return y;
             };
             auto next_of = [&](int t) {   // the next tile of this pass from t on
-                while (pass == 1 && blockIdx.x + (uint32_t)t * gridDim.x < all && sm.again[t] == 0) ++t;
+                while (pass == 1 && cta.x + (uint32_t)t * cta.ctas < all && sm.again[t] == 0) ++t;
                 return t;
             };
             int t = next_of(0);
-            uint32_t x = blockIdx.x + (uint32_t)t * gridDim.x;
+            uint32_t x = cta.x + (uint32_t)t * cta.ctas;
             Row row = row_of(min(x, all - 1));
             while (x < all && *(volatile int *)&sm.abort == 0) {
                 const QueryTile w = row.w;
@@ -643,7 +644,7 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
                 const float2 nL = make_float2(-row.L, -row.L), nD = make_float2(-row.D, -row.D);
                 bf16 *out = p.dQ + p.sdq.at(w.b, w.i0 + r, w.h) + d0;
                 t = next_of(t + 1);
-                x = blockIdx.x + (uint32_t)t * gridDim.x;
+                x = cta.x + (uint32_t)t * cta.ctas;
                 if (w.empty()) {
                     if (w.i0 + r < p.Tq)
 #pragma unroll
@@ -728,21 +729,28 @@ __global__ void __launch_bounds__(kQThreads, 1) window_dq_tc_kernel(const __grid
     if (warp == kWarps) tmem_dealloc(sm.tmem, 512);
 }
 
+// Both parts in one grid: dQ's CTAs first, which all end at about the same time; then dK's and dV's, which fill
+// the SMs as they come free.  All of them wait for D, which the kernel before computes.
+template <int HD, bool kSplit>
+__global__ void __launch_bounds__(kThreads, 1) window_grad_tc_kernel(const __grid_constant__ BwdArgs p) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    pdl_wait();
+    if (blockIdx.x < p.q_ctas)
+        query_grads<HD>(p, smem_raw, Share{blockIdx.x, p.q_ctas});
+    else
+        key_grads<HD, kSplit>(p, smem_raw, Share{blockIdx.x - p.q_ctas, gridDim.x - p.q_ctas});
+}
+
 template <int HD>
-cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
-    constexpr int kv = (int)sizeof(KvSm<HD>), qb = (int)sizeof(QSm<HD>);
-    static_assert(kv <= 227 * 1024 && qb <= 227 * 1024, "shared memory");
-    const auto dkv = p.Tk <= kTile ? window_dkv_tc_kernel<HD, true> : window_dkv_tc_kernel<HD, false>;
-    cudaError_t e = allow_smem((const void *)dkv, kv);
-    if (e == cudaSuccess) e = allow_smem((const void *)window_dq_tc_kernel<HD>, qb);
+cudaError_t launch(BwdArgs p, int B, cudaStream_t s) {
+    constexpr int smem = (int)std::max(sizeof(KvSm<HD>), sizeof(QSm<HD>));
+    static_assert(smem <= 227 * 1024, "shared memory");
+    const auto kernel = p.Tk <= kTile ? window_grad_tc_kernel<HD, true> : window_grad_tc_kernel<HD, false>;
+    cudaError_t e = allow_smem((const void *)kernel, smem);
     if (e != cudaSuccess) return e;
-    // dQ first, whose CTAs all end at about the same time; then dK, dV, whose many CTAs fill the SMs
-    // as they come free (it waits for D through the dQ kernel, and for that one's end at its own).
-    const int tiles = (p.Tq + kTile - 1) / kTile;
-    const long long all = (long long)tiles * p.H * B;
-    const long long ctas = std::max(std::min(all, 152LL), (all + kMaxTiles - 1) / kMaxTiles);
-    e = launch_pdl(window_dq_tc_kernel<HD>, dim3((unsigned)ctas), dim3(kQThreads), qb, s, p, (uint32_t)all, tiles);
-    if (e != cudaSuccess) return e;
+    const long long all = (long long)((p.Tq + kTile - 1) / kTile) * p.H * B;
+    p.q_ctas = (uint32_t)std::max(std::min(all, 152LL), (all + kMaxTiles - 1) / kMaxTiles);
+    p.q_tiles = (uint32_t)all;
     // dK, dV: CTAs that stay where a tile meets few blocks, whose loads and first scores then run beside
     // the end of the tile before; where it meets many, one tile a CTA, which leaves it to the GPU which SM takes the
     // next.  Backward, us, staying / not: B2 T8192, 4 heads of 64, window 512 (5 blocks a tile)
@@ -751,10 +759,10 @@ cudaError_t launch(const BwdArgs &p, int B, cudaStream_t s) {
     const long long keys = (long long)p.split.ctas(p.a, kTile) * p.Hkv * B;
     const long long met = (long long)p.G * ((p.window + kTile - 1) / kTile + 1);
     const long long kv_ctas = met < 24 ? std::min(keys, 152LL) : keys;
-    e = launch_pdl(dkv, dim3((unsigned)kv_ctas), dim3(kKvThreads), kv, s, p,
-                   (uint32_t)keys);
+    p.kv_tiles = (uint32_t)keys;
+    e = launch_pdl(kernel, dim3((unsigned)(p.q_ctas + kv_ctas)), dim3(kThreads), smem, s, p);
+    note_launches(1);
     if (e != cudaSuccess) return e;
-    note_launches(2);
     return add_sink_rows(p.a, p.partial, p.split.extra, p.dK, p.dV, s);
 }
 
