@@ -132,7 +132,6 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
             const float4 g4 = *reinterpret_cast<const float4 *>(&gamma[w.key][at.at(e)]);
             gm[e] = g4.x; gm[e + 1] = g4.y; gm[e + 2] = g4.z; gm[e + 3] = g4.w;
         }
-        const float isq = w.key ? 0.f : 1.f, isk = w.key ? 1.f : 0.f;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             if (u >= p.batch) break;
@@ -155,9 +154,10 @@ __global__ void __launch_bounds__(kThreads, kBackward ? 2 : 3) qk_norm_rope_kern
 #pragma unroll
                 for (int e = 0; e < W; ++e) {
                     v[e] *= r;
+                    // (chosen, not multiplied by 0 or 1: a NaN of a key reaches no query's sum)
                     const float d = on ? g[e] * v[e] : 0.f;
-                    acc[0][e] = fmaf(d, isq, acc[0][e]);
-                    acc[1][e] = fmaf(d, isk, acc[1][e]);
+                    acc[0][e] += w.key ? 0.f : d;
+                    acc[1][e] += w.key ? d : 0.f;
                     g[e] *= gm[e];
                     dot = fmaf(g[e], v[e], dot);
                 }
