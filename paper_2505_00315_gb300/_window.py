@@ -257,7 +257,7 @@ def mosa_qk_norm_rope_backward(q, k, gamma_q, gamma_k, dyq, dyk, positions=None,
     try:
         key = (2, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, rotary, theta, eps, halves,
                _sig(gamma_q), _sig(gamma_k), _sig(positions), dyq.shape, dyq.stride(), dyq.dtype,
-               dyk.shape, dyk.stride(), dyk.dtype, out and (_sig(dq), _sig(dk), _sig(dgq), _sig(dgk)))
+               dyk.shape, dyk.stride(), dyk.dtype, (_sig(dq), _sig(dk), _sig(dgq), _sig(dgk)) if out else None)
     except AttributeError:
         _bad(("q", q), ("k", k), ("gamma_q", gamma_q), ("gamma_k", gamma_k), ("dyq", dyq), ("dyk", dyk),
              ("positions", positions), ("dq", dq), ("dk", dk), ("dgamma_q", dgq), ("dgamma_k", dgk))
@@ -329,7 +329,7 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
     try:
         qs = q.shape
         key = (3, qs, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
-               window, sinks, scale, _sig(lens), out and (_sig(O), _sig(lse)))
+               window, sinks, scale, _sig(lens), (_sig(O), _sig(lse)) if out else None)
     except AttributeError:
         _bad(("q", q), ("k", k), ("v", v), ("lens", lens), ("O", O), ("lse", lse))
     plan = _plans.get(key) or _keep(key, _window_plan(q, k, v, O, lse, lens, window, sinks, scale))
@@ -368,7 +368,7 @@ def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int
     try:
         key = (4, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
                O.shape, O.stride(), O.dtype, lse.shape, lse.stride(), lse.dtype, dO.shape, dO.stride(),
-               dO.dtype, window, sinks, scale, _sig(lens), out and (_sig(dq), _sig(dk), _sig(dv)))
+               dO.dtype, window, sinks, scale, _sig(lens), (_sig(dq), _sig(dk), _sig(dv)) if out else None)
     except AttributeError:
         _bad(("q", q), ("k", k), ("v", v), ("O", O), ("lse", lse), ("dO", dO), ("lens", lens), ("dq", dq),
              ("dk", dk), ("dv", dv))

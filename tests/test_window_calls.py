@@ -168,3 +168,28 @@ def test_results_and_workspaces_of_a_call_for_a_stream_are_of_that_stream(call, 
     assert lib.seen[-1][2][-1] == 77          # where the kernels go
     assert made and set(made) == {77}
     assert current == [0]
+
+
+ALL = {
+    "norm": lambda **kw: W.mosa_qk_norm_rope(Q, K, **kw),
+    "norm_backward": lambda **kw: W.mosa_qk_norm_rope_backward(Q, K, None, None, Q, K, workspace=SPACE, **kw),
+    "forward": lambda **kw: W.mosa_window_forward(Q, K, K, 4, workspace=SPACE, **kw),
+    "backward": lambda **kw: W.mosa_window_backward(Q, K, K, Q, LSE, Q, SPACE, 4, **kw),
+    "decode": lambda **kw: W.mosa_window_decode(Q[:, 0], K[:, 0], K[:, 0], CACHE, CACHE, LENS, 4, workspace=SPACE,
+                                                **kw),
+}
+
+
+@pytest.fixture
+def on_gpu(monkeypatch):
+    """New tensors pass for ones of the GPU too."""
+    for name in ("empty", "zeros", "empty_like"):
+        f = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, _f=f, **kw: _f(*a, **kw).as_subclass(OnGpu))
+
+
+@pytest.mark.parametrize("call", ALL.values(), ids=ALL)
+def test_out_may_hold_nothing(call, lib, on_gpu):
+    for out in ({}, None, {"unused": 1}):
+        call(out=out)
+    assert len(lib.seen) == 3
