@@ -159,14 +159,12 @@ def _on(stream):
     return cuda.stream(stream if isinstance(stream, cuda.Stream) else cuda.ExternalStream(stream.cuda_stream))
 
 
-def _space(workspace, need, name, device):
-    """The given workspace, or a new one."""
+def _space(workspace, need, device):
+    """The given workspace, or a new one (empty where the library refuses the sizes, as it will say)."""
     if workspace is not None:
         if not (workspace.is_cuda and workspace.dtype is _b._torch_mod.uint8 and workspace.is_contiguous()):
             _b._dev(workspace, "workspace", _b._torch_mod.uint8)   # says what is wrong
         return workspace
-    if need == 0:
-        raise _b.MosaError(_b.MOSA_ERR_INVALID_ARG, name)
     # zeroed: the status word of a window call's workspace is read before any call clears it
     return _b._torch_mod.zeros(need, dtype=_b._torch_mod.uint8, device=device)
 
@@ -277,7 +275,7 @@ def mosa_qk_norm_rope_backward(q, k, gamma_q, gamma_k, dyq, dyk, positions=None,
             and (gamma_k is None or gamma_k.is_cuda) and (positions is None or positions.is_cuda)):
         _bad(("q", q), ("k", k), ("gamma_q", gamma_q), ("gamma_k", gamma_k), ("dyq", dyq), ("dyk", dyk),
              ("positions", positions), ("dq", dq), ("dk", dk), ("dgamma_q", dgq), ("dgamma_k", dgk))
-    workspace = _space(workspace, plan[1], "mosa_qk_norm_rope_backward", dev)
+    workspace = _space(workspace, plan[1], dev)
     rc = _b.load().mosa_qk_norm_rope_backward(
         plan[0], q.data_ptr(), k.data_ptr(), None if gamma_q is None else gamma_q.data_ptr(),
         None if gamma_k is None else gamma_k.data_ptr(),
@@ -343,7 +341,7 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
     if not (q.is_cuda and k.is_cuda and v.is_cuda and O.is_cuda and (lse is None or lse.is_cuda)
             and (lens is None or lens.is_cuda)):
         _bad(("q", q), ("k", k), ("v", v), ("lens", lens), ("O", O), ("lse", lse))
-    workspace = _space(workspace, plan[1], "mosa_window_forward", dev)
+    workspace = _space(workspace, plan[1], dev)
     rc = _b.load().mosa_window_forward(
         plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lens is None else lens.data_ptr(),
         O.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
@@ -387,7 +385,7 @@ def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int
              ("dk", dk), ("dv", dv))
     if workspace is None:
         raise TypeError("workspace must be the forward's")
-    _space(workspace, 0, "mosa_window_backward", dev)
+    _space(workspace, 0, dev)
     rc = _b.load().mosa_window_backward(
         plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lens is None else lens.data_ptr(),
         O.data_ptr(), lse.data_ptr(), dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
@@ -471,7 +469,7 @@ def mosa_window_decode(q, k, v, K_cache, V_cache, lens, window: int, sinks: int 
             and (gamma_k is None or gamma_k.is_cuda)):
         _bad(("q", q), ("k", k), ("v", v), ("K_cache", K_cache), ("V_cache", V_cache), ("lens", lens),
              ("O", O), ("gamma_q", gamma_q), ("gamma_k", gamma_k))
-    workspace = _space(workspace, plan[1], "mosa_window_decode", q.device)
+    workspace = _space(workspace, plan[1], q.device)
     rc = _b.load().mosa_window_decode(
         plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(),
         None if gamma_q is None else gamma_q.data_ptr(),

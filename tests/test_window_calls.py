@@ -193,3 +193,26 @@ def test_out_may_hold_nothing(call, lib, on_gpu):
     for out in ({}, None, {"unused": 1}):
         call(out=out)
     assert len(lib.seen) == 3
+
+
+def test_the_librarys_own_refusal_is_what_a_call_raises(monkeypatch, on_gpu):
+    """A head size that it does not support, and a rotation that is no even number, with and without a
+    workspace."""
+    monkeypatch.setattr(W._b, "_stream", lambda stream: 0)
+    q, k, lse, kc = t(2, 8, 4, 48), t(2, 8, 2, 48), t(2, 4, 8), t(2, 8, 2, 48)
+    for ws in (None, SPACE):
+        for call in (lambda: W.mosa_qk_norm_rope(q, k),
+                     lambda: W.mosa_qk_norm_rope_backward(q, k, None, None, q, k, workspace=ws),
+                     lambda: W.mosa_window_forward(q, k, k, 4, workspace=ws),
+                     lambda: W.mosa_window_backward(q, k, k, q, lse, q, SPACE, 4),
+                     lambda: W.mosa_window_decode(q[:, 0], k[:, 0], k[:, 0], kc, kc, LENS, 4, workspace=ws)):
+            with pytest.raises(W._b.MosaError) as e:
+                call()
+            assert e.value.code == W._b.MOSA_ERR_UNSUPPORTED
+        for call in (lambda: W.mosa_qk_norm_rope(Q, K, rotary=7),
+                     lambda: W.mosa_qk_norm_rope_backward(Q, K, None, None, Q, K, rotary=7, workspace=ws),
+                     lambda: W.mosa_window_forward(Q, K, K, -4, workspace=ws),
+                     lambda: W.mosa_window_decode(Q[:, 0], K[:, 0], K[:, 0], CACHE, CACHE, LENS, -4, workspace=ws)):
+            with pytest.raises(W._b.MosaError) as e:
+                call()
+            assert e.value.code == W._b.MOSA_ERR_INVALID_ARG
