@@ -362,7 +362,8 @@ typedef struct {
 /* Workspace of a forward or backward (256-byte aligned); 0 if the shape is invalid or
  * unsupported.  It carries the status word in its first 4 bytes (zero those once,
  * before the workspace's first call) and, from a bf16 forward with lse to the backward
- * that follows, what the rounding of O cut off: pass the same buffer to both. */
+ * that follows, what the rounding of O cut off: pass the same buffer to both.  A forward
+ * without lse needs its first 256 bytes only.  Beyond the status word it may hold anything. */
 size_t mosa_window_workspace_bytes(const mosa_window_shape *shape);
 
 /* Forward: q [B,Tq,H,hp], k and v [B,Tk,Hkv,hp], lens [B] int32 or NULL (all

@@ -11,6 +11,9 @@ from . import _binding as _b
 
 _i32, _i64, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
+#: The workspace of a forward that no backward follows: the status word, at its alignment.
+STATUS_BYTES = 256
+
 
 class MosaStrides(ctypes.Structure):
     """mosa_strides: elements between sequences, tokens and heads."""
@@ -159,14 +162,18 @@ def _on(stream):
     return cuda.stream(stream if isinstance(stream, cuda.Stream) else cuda.ExternalStream(stream.cuda_stream))
 
 
-def _space(workspace, need, device):
-    """The given workspace, or a new one (empty where the library refuses the sizes, as it will say)."""
+def _space(workspace, need, device, status=False):
+    """The given workspace, or a new one (empty where the library refuses the sizes, as it will say).  With
+    ``status`` its first word is zeroed, which is read before any call clears it; the rest may hold anything
+    (zeroing all of it was 68 MB a call at B4 T4096, 16 heads of 128)."""
     if workspace is not None:
         if not (workspace.is_cuda and workspace.dtype is _b._torch_mod.uint8 and workspace.is_contiguous()):
             _b._dev(workspace, "workspace", _b._torch_mod.uint8)   # says what is wrong
         return workspace
-    # zeroed: the status word of a window call's workspace is read before any call clears it
-    return _b._torch_mod.zeros(need, dtype=_b._torch_mod.uint8, device=device)
+    workspace = _b._torch_mod.empty(need, dtype=_b._torch_mod.uint8, device=device)
+    if status:
+        workspace[:4].zero_()
+    return workspace
 
 
 # ------------------------------------------------------ norm and rotation
@@ -341,7 +348,7 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
     if not (q.is_cuda and k.is_cuda and v.is_cuda and O.is_cuda and (lse is None or lse.is_cuda)
             and (lens is None or lens.is_cuda)):
         _bad(("q", q), ("k", k), ("v", v), ("lens", lens), ("O", O), ("lse", lse))
-    workspace = _space(workspace, plan[1], dev)
+    workspace = _space(workspace, plan[1] if want_lse else min(plan[1], STATUS_BYTES), dev, True)
     rc = _b.load().mosa_window_forward(
         plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lens is None else lens.data_ptr(),
         O.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),

@@ -147,8 +147,9 @@ bool tensor_cores() { return use_split(); }
 
 // The status word, then the backward's D [B,H,Tq], what the forward's O lost by its rounding
 // (bf16 storage) and the backward's partial sums of sink rows.
+constexpr size_t kStatusBytes = 256;
 size_t rest_at(const Attn &a) {
-    return 256 + ((size_t)a.B * a.H * a.Tq * sizeof(float) + 255) / 256 * 256;
+    return kStatusBytes + ((size_t)a.B * a.H * a.Tq * sizeof(float) + 255) / 256 * 256;
 }
 size_t partial_at(const Attn &a) {
     return rest_at(a) + (a.bf16 ? ((size_t)a.B * a.H * a.Tq * a.hp * 2 + 255) / 256 * 256 : 0);
@@ -214,7 +215,8 @@ mosa_status mosa_window_forward(const mosa_window_shape *shape, const void *q, c
     if (st != MOSA_OK) return st;
     if ((st = check_ptrs(shape->dtype, {q, k, v, O})) != MOSA_OK) return st;
     if (!aligned(lens, MOSA_F32) || !aligned(lse, MOSA_F32)) return MOSA_ERR_INVALID_ARG;
-    if ((st = check_space(workspace, workspace_bytes, window_bytes(a))) != MOSA_OK) return st;
+    const size_t need = lse != nullptr ? window_bytes(a) : kStatusBytes;
+    if ((st = check_space(workspace, workspace_bytes, need)) != MOSA_OK) return st;
     cudaStream_t cs = (cudaStream_t)stream;
     cudaError_t e = cudaSuccess;
     bf16 *rest = lse != nullptr && a.bf16 ? (bf16 *)((char *)workspace + rest_at(a)) : nullptr;
@@ -234,7 +236,7 @@ mosa_status mosa_window_backward(const mosa_window_shape *shape, const void *q, 
     if ((st = check_ptrs(MOSA_F32, {lse})) != MOSA_OK) return st;
     if (!aligned(lens, MOSA_F32)) return MOSA_ERR_INVALID_ARG;
     if ((st = check_space(workspace, workspace_bytes, window_bytes(a))) != MOSA_OK) return st;
-    float *delta = reinterpret_cast<float *>(static_cast<char *>(workspace) + 256);
+    float *delta = reinterpret_cast<float *>(static_cast<char *>(workspace) + kStatusBytes);
     cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e = window_delta(a, O, a.bf16 ? (const bf16 *)((const char *)workspace + rest_at(a)) : nullptr, dO,
                                  delta, s);

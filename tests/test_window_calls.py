@@ -18,6 +18,7 @@ class OnGpu(torch.Tensor):
 
 class Library:
     """Keeps the struct of each call."""
+    bytes = 256
 
     def __init__(self):
         self.seen = []
@@ -25,7 +26,7 @@ class Library:
     def __getattr__(self, name):
         def call(ref, *args):
             if name.endswith("_bytes"):
-                return 256
+                return self.bytes
             s = ref._obj
             self.seen.append((name, {n: getattr(s, n) for n, t in s._fields_
                                      if t in (ctypes.c_int32, ctypes.c_float)}, args))
@@ -216,3 +217,22 @@ def test_the_librarys_own_refusal_is_what_a_call_raises(monkeypatch, on_gpu):
             with pytest.raises(W._b.MosaError) as e:
                 call()
             assert e.value.code == W._b.MOSA_ERR_INVALID_ARG
+
+
+def test_a_new_workspace_is_as_large_as_its_call_needs(lib, on_gpu, monkeypatch):
+    """... and only its status word is zeroed: the rest may be large."""
+    zeroed = []
+    zero_ = torch.Tensor.zero_
+    monkeypatch.setattr(torch.Tensor, "zero_", lambda x: (zeroed.append(x.numel()), zero_(x))[1])
+    monkeypatch.setattr(torch, "zeros", lambda n, *a, **kw: zeroed.append(n) or torch.full((n,), 0, **kw))
+    monkeypatch.setattr(Library, "bytes", 4096)
+    O, lse, ws = W.mosa_window_forward(Q, K, K, 4)
+    assert ws.numel() == 4096 and set(zeroed) == {4} and (ws[:4] == 0).all()
+    O, lse, ws = W.mosa_window_forward(Q, K, K, 4, want_lse=False)
+    assert lse is None and ws.numel() == 256 and set(zeroed) == {4}
+    assert lib.seen[-1][2][-2] == 256
+    zeroed.clear()
+    _, ws = W.mosa_qk_norm_rope_backward(Q, K, None, None, Q, K)
+    assert ws.numel() == 4096
+    _, ws = W.mosa_window_decode(Q[:, 0], K[:, 0], K[:, 0], CACHE, CACHE, LENS, 4)
+    assert ws.numel() == 4096 and not zeroed
