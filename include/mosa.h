@@ -347,8 +347,10 @@ mosa_status mosa_qk_norm_rope_backward(const mosa_qk_shape *shape, const void *q
  *     S = scale q k^T,  P = softmax over the visible tokens,  O = P v
  * scale = 0 stands for 1/sqrt(hp).  A query that sees nothing (p >= lens[b])
  * gets O = 0, lse = -inf and no gradient.  What a masked place holds, NaN and
- * infinities among them, reaches no output that does not see it; a visible
- * NaN or infinity makes the results that it reaches NaN or infinite.
+ * infinities among them, reaches no output that does not see it.  A visible NaN or
+ * infinity makes the results that depend on it NaN or infinite (except where it only
+ * takes a token's weight away, by a score of -infinity), and may make NaN of all
+ * results of the queries that see it and of the gradients of the tokens that those see.
  * 0 <= window; 0 <= sinks; 1 <= Tq <= Tk; B*H*Tq < 2^31. */
 typedef struct {
     int32_t B, Tq, Tk, H, Hkv, hp;

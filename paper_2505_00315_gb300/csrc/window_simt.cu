@@ -105,8 +105,13 @@ __device__ __forceinline__ int col_of(int tx, int c) {
     return CW <= 4 ? tx * CW + c : (c >> 2) * 64 + tx * 4 + (c & 3);
 }
 
-// acc[i][c] += sum_j W[ty*4+i][j] X[j][col_of(c)].  With `skip` a weight of zero adds
-// nothing whatever X holds (masked places may hold NaN).
+// A hidden place's weight in a tile of scores.  What a query sees has +0 where it underflows, times
+// whose row a NaN or an infinity is NaN.
+constexpr float kHidden = -0.f;
+__device__ __forceinline__ bool hidden(float w) { return __float_as_uint(w) == 0x80000000u; }
+
+// acc[i][c] += sum_j W[ty*4+i][j] X[j][col_of(c)].  With `skip` a hidden place adds
+// nothing whatever X holds (it may hold NaN).
 template <int HD, bool kRowsFirst>
 __device__ __forceinline__ void add_weighted(const float *W, const float *X, int ty, int tx,
                                              bool skip, float (&acc)[4][HD / 16]) {
@@ -142,7 +147,7 @@ __device__ __forceinline__ void add_weighted(const float *W, const float *X, int
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (!skip || w[i][u] != 0.f) {
+                if (!skip || !hidden(w[i][u])) {
 #pragma unroll
                     for (int c = 0; c < CW; ++c) acc[i][c] = fmaf(w[i][u], x[c], acc[i][c]);
                 }
@@ -207,12 +212,11 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Pt
             for (int i = 0; i < 4; ++i) {
                 const int pos = pf + ty * 4 + i;
                 float mb = -INFINITY;
+                bool on[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    if (!whole && !(pos <= pl && kb.sees(j, ks, tx + 16 * c, pos, a.window, a.sinks)))
-                        s[i][c] = -INFINITY;
-                    else
-                        s[i][c] *= sl2;
+                    on[c] = whole || (pos <= pl && kb.sees(j, ks, tx + 16 * c, pos, a.window, a.sinks));
+                    s[i][c] = on[c] ? s[i][c] * sl2 : -INFINITY;
                     mb = fmaxf(mb, s[i][c]);
                 }
                 // (fmax drops a NaN; the exponentials keep it)
@@ -224,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Pt
                 for (int c = 0; c < 4; ++c) {
                     const float e = exp2f(s[i][c] - base);
                     sum += e;
-                    sP[(ty * 4 + i) * kPS + tx + 16 * c] = e;
+                    sP[(ty * 4 + i) * kPS + tx + 16 * c] = on[c] ? e : kHidden;
                 }
                 l[i] = l[i] * corr + sum16(sum);
                 m[i] = mn;
@@ -256,7 +260,8 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Pt
 }
 
 // P (into sP, [query][key]) and dS (into sS) of one pair of tiles: queries at
-// positions pq .. pq+63 (rows past `last` see nothing), keys ks .. ks+63.
+// positions pq .. pq+63 (rows past `last` see nothing), keys ks .. ks+63.  What is seen never is
+// kHidden: P is not negative, and dS has +0 added.
 template <int HD, class Sees>
 __device__ __forceinline__ void grad_scores(const float *sQ, const float *sG, const float *sK,
                                             const float *sV, const float *sL, const float *sD,
@@ -273,9 +278,9 @@ __device__ __forceinline__ void grad_scores(const float *sQ, const float *sG, co
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const bool on = whole || sees(r, tx + 16 * c);
-            const float e = on ? exp2f(fmaf(s[i][c], sl2, -lse2)) : 0.f;
+            const float e = on ? exp2f(fmaf(s[i][c], sl2, -lse2)) : kHidden;
             if (sP != nullptr) sP[r * kPS + tx + 16 * c] = e;
-            sS[r * kPS + tx + 16 * c] = on && !one ? e * (dp[i][c] - D) : 0.f;
+            sS[r * kPS + tx + 16 * c] = on && !one ? e * (dp[i][c] - D) + 0.f : kHidden;
         }
     }
 }

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2505_00315_gb300 as mosa
-from test_gpu_window import norm_inputs
+from test_gpu_window import inputs, norm_inputs, run
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,29 @@ def test_the_norms_gradients_of_queries_and_keys_stay_apart(where, bad, dtype, l
         keep = torch.ones(got["d" + mine].shape[:3], dtype=torch.bool, device="cuda")
         keep[B - 1, T // 2, 1] = False
         assert torch.equal(got["d" + mine][keep], clean["d" + mine][keep])
+
+
+KERNELS = [("bf16", "0"), ("bf16", "1"), ("f32", "0")]   # tensor cores, CUDA cores with either storage
+
+
+@pytest.mark.parametrize("dtype,force", KERNELS)
+@pytest.mark.parametrize("hp", [64, 128])
+def test_a_visible_nan_counts_where_its_weight_underflows(hp, dtype, force, monkeypatch):
+    """A token with a score so low that its weight is 0 (2^-900), and a NaN in its value: the queries
+    that see it have NaN there, and it has NaN gradients, in tiles seen whole or in part."""
+    monkeypatch.setenv("MOSA_FORCE_SIMT", force)
+    T, j, w = 400, 150, 130
+    q, k, v, dO = inputs(1, T, T, 2, 1, hp, dtype, seed=41, layout="plain")
+    q.fill_(2.0)
+    k[0, j] = -640.0 * hp ** -0.5 / 2
+    clean = run(q, k, v, dO, w, 0)
+    assert torch.isfinite(clean["O"]).all()
+    v[0, j, 0, 3] = math.nan
+    got = run(q, k, v, dO, w, 0)
+    sees = torch.zeros(T, dtype=torch.bool, device="cuda")
+    sees[j:j + w] = True
+    assert torch.isnan(got["O"][0, sees][..., 3]).all()
+    assert not torch.isfinite(got["dq"][0, sees].float()).any()
+    assert not torch.isfinite(got["dk"][0, j].float()).any()
+    for n in ("O", "dq"):
+        assert torch.equal(got[n][0, ~sees], clean[n][0, ~sees]), n
