@@ -261,7 +261,8 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Pt
 
 // P (into sP, [query][key]) and dS (into sS) of one pair of tiles: queries at
 // positions pq .. pq+63 (rows past `last` see nothing), keys ks .. ks+63.  What is seen never is
-// kHidden: P is not negative, and dS has +0 added.
+// kHidden: P is not negative, and dS has +0 added (a query that sees one token: 0 times dS, which
+// stays NaN where that is).
 template <int HD, class Sees>
 __device__ __forceinline__ void grad_scores(const float *sQ, const float *sG, const float *sK,
                                             const float *sV, const float *sL, const float *sD,
@@ -280,7 +281,7 @@ __device__ __forceinline__ void grad_scores(const float *sQ, const float *sG, co
             const bool on = whole || sees(r, tx + 16 * c);
             const float e = on ? exp2f(fmaf(s[i][c], sl2, -lse2)) : kHidden;
             if (sP != nullptr) sP[r * kPS + tx + 16 * c] = e;
-            sS[r * kPS + tx + 16 * c] = on && !one ? e * (dp[i][c] - D) + 0.f : kHidden;
+            sS[r * kPS + tx + 16 * c] = on ? fmaf(e * (dp[i][c] - D), one ? 0.f : 1.f, 0.f) : kHidden;
         }
     }
 }

@@ -376,9 +376,11 @@ __device__ __forceinline__ void key_grads(const BwdArgs &p, uint8_t *smem, const
                 }
                 if (!whole) {
                     // (again: dP may be NaN where P is 0; and a query that sees one token only has
-                    // no gradient)
-                    if (p.window == 1 && p.sinks == 0) seen = 0;
-                    if (pq == 0 && c0 == 0) seen &= ~1u;
+                    // no gradient, but NaN where it meets one)
+                    if (p.window == 1 && p.sinks == 0)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) P[c] *= 0.f;
+                    if (pq == 0 && c0 == 0) P[0] *= 0.f;
                     hide(P, seen, 0.f);
                 }
                 kSplit ? put_weights_split(tG + at, P) : put_weights(tG + at, P);

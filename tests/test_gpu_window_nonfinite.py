@@ -55,3 +55,26 @@ def test_a_visible_nan_counts_where_its_weight_underflows(hp, dtype, force, monk
     assert not torch.isfinite(got["dk"][0, j].float()).any()
     for n in ("O", "dq"):
         assert torch.equal(got[n][0, ~sees], clean[n][0, ~sees]), n
+
+
+@pytest.mark.parametrize("dtype,force", KERNELS)
+@pytest.mark.parametrize("T,window", [(1, 0), (3, 1), (200, 1)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("where", ["q", "k", "v", "dO"])
+def test_a_query_that_sees_one_token_passes_a_nan_on(where, bad, T, window, dtype, force, monkeypatch):
+    """Its scores have no gradient (P = 1), unless what it meets is no number."""
+    monkeypatch.setenv("MOSA_FORCE_SIMT", force)
+    q, k, v, dO = inputs(1, T, T, 1, 1, 64, dtype, seed=42, layout="plain")
+    clean = run(q, k, v, dO, window, 0)
+    for n in ("dq", "dk"):
+        assert (clean[n] == 0).all()
+    j = T // 2
+    {"q": q, "k": k, "v": v, "dO": dO}[where][0, j] = bad
+    got = run(q, k, v, dO, window, 0)
+    reached = {"q": ("O", "dq", "dk", "dv"), "k": ("O", "dq", "dk", "dv"), "v": ("O", "dq", "dk"),
+               "dO": ("dq", "dk", "dv")}[where]
+    for n in reached:
+        assert not torch.isfinite(got[n][0, j].float()).any(), n
+    keep = torch.arange(T, device="cuda") != j
+    for n in ("O", "dq", "dk", "dv"):
+        assert torch.equal(got[n][0, keep], clean[n][0, keep]), n
