@@ -243,7 +243,9 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Pt
     for (int i = 0; i < 4; ++i) {
         const int r = i0 + ty * 4 + i;
         if (r >= a.Tq) continue;
-        const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+        // (l = 0 where all that a query sees has a score of -inf: 0 / 0 there)
+        const bool seen = off + r <= pl;
+        const float inv = seen ? 1.f / l[i] : 0.f;
         store_row<HD>(p.o + a.o.at(b, r, h), tx, acc[i], inv);
         if (p.rest != nullptr) {
 #pragma unroll
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_simt_kernel(Attn a, Pt
         }
         if (p.lse != nullptr && tx == 0)
             p.lse[((long long)b * a.H + h) * a.Tq + r] =
-                l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
+                seen ? (m[i] + log2f(l[i])) * kLn2 : -INFINITY;
     }
 }
 

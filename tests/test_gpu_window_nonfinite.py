@@ -78,3 +78,19 @@ def test_a_query_that_sees_one_token_passes_a_nan_on(where, bad, T, window, dtyp
     keep = torch.arange(T, device="cuda") != j
     for n in ("O", "dq", "dk", "dv"):
         assert torch.equal(got[n][0, keep], clean[n][0, keep]), n
+
+
+@pytest.mark.parametrize("dtype,force", KERNELS)
+def test_scores_of_minus_infinity_are_no_empty_row(dtype, force, monkeypatch):
+    """A query all of whose scores are -inf sees tokens: O is NaN (0 / 0), not the zeros of a query
+    past its sequence's end; beside others such a token has no weight."""
+    monkeypatch.setenv("MOSA_FORCE_SIMT", force)
+    q, k, v, dO = inputs(1, 200, 200, 2, 1, 64, dtype, seed=43, layout="plain")
+    q[0, 90].fill_(-math.inf)
+    k.abs_().add_(0.1)
+    lens = torch.tensor([150], device="cuda", dtype=torch.int32)
+    O, lse, _ = mosa.mosa_window_forward(q, k, v, 40, 2, lens=lens)
+    assert torch.isnan(O[0, 90].float()).all() and not torch.isfinite(lse[0, :, 90]).any()
+    keep = torch.arange(200, device="cuda") != 90
+    assert torch.isfinite(O[0, keep].float()).all()
+    assert (O[0, 150:] == 0).all() and (lse[0, :, 150:] == -math.inf).all()
