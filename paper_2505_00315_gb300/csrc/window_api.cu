@@ -1,6 +1,7 @@
 // C ABI of the window heads (declared in include/mosa.h): argument checks,
 // workspace and dispatch of the norm and rotation of queries and keys, the sliding-window
 // attention and the decoding step.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -32,10 +33,35 @@ bool strides(const mosa_strides &s, int B, int T, int H, Str *out) {
     return out->b <= lim / B && out->t <= lim / T && out->h <= lim / H;
 }
 
-// An output may not meet itself: no two elements of it share a place.  Checked for
-// what a stride shorter than a head's row shows.
+// An output may not meet itself: no two of its elements share a place.  Where each stride passes
+// what the smaller ones reach, as in every layout that is some order of the dimensions, that is
+// plain; else two rows less than hp apart are looked for, by the differences of their sequences
+// and heads (2^20 of those at most: what has more is refused).
 bool output(const Str &s, int B, int T, int H, int hp) {
-    return (B <= 1 || s.b >= hp) && (T <= 1 || s.t >= hp) && (H <= 1 || s.h >= hp);
+    struct Dim {
+        long long stride, n;
+    } d[3] = {{s.b, B}, {s.t, T}, {s.h, H}};
+    std::sort(d, d + 3, [](const Dim &x, const Dim &y) { return x.stride < y.stride; });
+    long long reach = hp;
+    bool nested = true;
+    for (const Dim &x : d) {
+        if (x.n <= 1) continue;
+        if (x.stride < hp) return false;
+        nested = nested && x.stride >= reach;
+        reach += (x.n - 1) * x.stride;
+    }
+    if (nested) return true;
+    if ((long long)B * H > 1 << 20) return false;
+    for (long long b = 0; b < B; ++b)
+        for (long long h = b == 0 ? 0 : 1 - H; h < H; ++h) {
+            const long long x = b * s.b + h * s.h;
+            const long long t = T <= 1 ? 0 : std::min((x < 0 ? -x : x) / s.t, T - 1LL);   // tokens that lead back
+            for (long long dt = t; dt <= t + 1 && dt < T; ++dt) {
+                const long long apart = (x < 0 ? -x : x) - dt * s.t;
+                if ((b != 0 || h != 0 || dt != 0) && apart < hp && -apart < hp) return false;
+            }
+        }
+    return true;
 }
 
 bool aligned(const void *p, int dtype) {
