@@ -72,6 +72,16 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t &bar, uint32_t parity, in
     return true;
 }
 
+// Whether a query sees few tokens (by the shape: lengths are on the device): P and dS are then taken in two
+// parts, what bf16 holds of them and what that leaves, in every product.  Where few weights add up,
+// some of them are large, and their rounding shows in O, in the backward's D and, where dP - D
+// cancels, in dq and dk.  Errors of dq / dk over those of a form that rounds only what it stores, T 1000, scores
+// of standard deviation 3: window 2 and 1 sink 2.0 / 2.2 in one part, 1.0 / 1.0 in two; 16 and 4 1.5 / 1.8,
+// 1.0 / 1.0; 64 and 4 1.3 / 1.6, 1.0 / 1.0; in one part 256 and 4 1.2 / 1.6 still, no window 1.2 / 1.5.  Times in
+// one part / two, window 64: B2 T8192, 4 heads of 64, forward 20.5 / 24.8 us, backward 58 / 63; B4 T4096, 16 + 4
+// heads of 128 88 / 107, 217 / 236.
+inline bool few_terms(const Attn &a) { return std::min((long long)a.Tk, (long long)a.window + a.sinks) <= 128; }
+
 // Products of whole tiles, issued by one thread.  Operand tiles are NB 64-column blocks of 128
 // rows, kBlk bytes apart; their descriptors differ by constants from the first, so that a
 // product costs the issuing thread a few instructions and not the dozen of a descriptor made

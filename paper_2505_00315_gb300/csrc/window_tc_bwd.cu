@@ -12,7 +12,7 @@
 //           dS goes into two products, what bf16 holds of it and what that leaves: a query's dS are
 //           differences that cancel in its sum, and one rounding of them was 1.5 times the error of
 //           a form that rounds only what it stores.  (dK and dV sum over many queries, whose
-//           roundings are independent.)  Costs 512 of 2048 + 512 cycles of MMAs a block.
+//           roundings are independent: 1.4 times; in two parts where few tokens are seen.)  Costs 512 of 2048 + 512 cycles of MMAs a block.
 // CTAs of both are one grid, dQ's first (see window_grad_tc_kernel).
 // One part with five products instead of the eight here would have to add dQ up
 // from several CTAs: 64 KB of fp32 reductions per pair of tiles against 2560
@@ -128,9 +128,8 @@ struct KeyWork {
     __device__ __forceinline__ KeyWork(const BwdArgs &p, uint32_t x) : KeyWork(p, Place(x, p.Hkv, p.a.B)) {}
 };
 
-// kSplit (Tk <= 128, as in the forward): what P and dS lose by their rounding goes into second
-// products.  A few tokens' sums do not average their roundings (dk of 2 to 91 tokens was up to 1.8 times as
-// far off as the plain form's), and their time is latency.
+// kSplit (few_terms, as in the forward): what P and dS lose by their rounding goes into second
+// products.
 template <int HD, bool kSplit>
 __device__ __forceinline__ void key_grads(const BwdArgs &p, uint8_t *smem, const Share cta) {
     using Sm = KvSm<HD>;
@@ -747,7 +746,7 @@ template <int HD>
 cudaError_t launch(BwdArgs p, int B, cudaStream_t s) {
     constexpr int smem = (int)std::max(sizeof(KvSm<HD>), sizeof(QSm<HD>));
     static_assert(smem <= 227 * 1024, "shared memory");
-    const auto kernel = p.Tk <= kTile ? window_grad_tc_kernel<HD, true> : window_grad_tc_kernel<HD, false>;
+    const auto kernel = few_terms(p.a) ? window_grad_tc_kernel<HD, true> : window_grad_tc_kernel<HD, false>;
     cudaError_t e = allow_smem((const void *)kernel, smem);
     if (e != cudaSuccess) return e;
     const long long all = (long long)((p.Tq + kTile - 1) / kTile) * p.H * B;

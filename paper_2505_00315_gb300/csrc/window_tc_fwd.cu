@@ -8,14 +8,14 @@
 // and O / l, lse = (m + log2 l) ln 2 at the end.  m rises only when a block's maximum
 // exceeds it by more than 2^8 (O and l are then rescaled); P stays within the bf16
 // range at the same relative precision.  P is rounded to bf16, the type of the V it
-// meets (8 bits, as the output has); l sums the unrounded values.
+// meets (8 bits, as the output has), in two parts where few tokens are seen; l sums the unrounded values.
 //
 // Sixteen warps compute (four per TMEM lane quadrant, each a quarter of the keys: four threads a
 // row), one loads by TMA, one issues the MMAs.  Two CTAs share an SM (256 of 512 TMEM columns, half
 // the shared memory each): while one's softmax runs the other's MMAs do.  With hp = 128, S and
 // O fill a CTA's columns and P takes the place of S, so its chain is S -> P -> O -> S.
 // With hp <= 64 P has columns of its own, and the next scores are computed as soon as
-// the warps have read the last ones.
+// the warps have read the last ones (unless P is taken in two parts).
 //
 // B1 T16384, 32 + 8 heads of 128, window 2048: 482 us, 1.07 PFLOP/s of the pairs that are seen.  With
 // hp = 128 that is bound by issue and by each CTA's chain: a thread's 32 scores take 220 instructions, 96 of
@@ -87,16 +87,15 @@ __device__ __forceinline__ int v_tile(int j, int n) {
     return !kEarly || j == n - 1 ? 2 * j + 1 : 2 * j + 2;
 }
 
-// kSplit (Tk <= 128: every tile meets one block): P's rounding is given back by a second product with
-// what it left, in columns of S that nothing uses any more.  Short texts have few and large
-// weights, whose rounding would show in the backward's D; their time is latency, and
-// stays the same.  (In the kernel for longer ones the branch alone, never taken, cost a fifth.)
+// kSplit (few_terms): P's rounding is given back by a second product with what it left, in columns of S
+// that nothing uses any more, so that no scores come early.  (In the kernel for many terms the
+// branch alone, never taken, cost a fifth.)
 template <int HD, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid_constant__ FwdArgs p) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using Sm = FwdSm<HD>;
     constexpr int NB = Sm::NB, NS = Sm::NS;
-    constexpr bool kEarly = HD == 64;
+    constexpr bool kEarly = HD == 64 && !kSplit;
     Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
@@ -409,7 +408,7 @@ bool tc_window_fwd(const Attn &a, const void *q, const void *k, const void *v, c
     p.sinks = a.sinks;
     p.scale_log2 = a.scale * kLog2e;
     const dim3 grid = grid_of((a.Tq + kQ - 1) / kQ, a.H, a.B);
-    const bool split = a.Tk <= kN;
+    const bool split = few_terms(a);
     *err = a.hp <= 64 ? (split ? launch<64, true>(p, grid, s) : launch<64, false>(p, grid, s))
                       : (split ? launch<128, true>(p, grid, s) : launch<128, false>(p, grid, s));
     return true;
