@@ -755,8 +755,10 @@ cudaError_t launch(BwdArgs p, int B, cudaStream_t s) {
     // dK, dV: CTAs that stay where a tile meets few blocks, whose loads and first scores then run beside
     // the end of the tile before; where it meets many, one tile a CTA, which leaves it to the GPU which SM takes the
     // next.  Backward, us, staying / not: B2 T8192, 4 heads of 64, window 512 (5 blocks a tile)
-    // 76.7 / 81.7; B4 T4096, 16 heads of 128, window 1024 (9) 438 / 475; 16 + 4 heads of 128 (36) 414 / 412,
-    // of 64 335 / 332.
+    // 76.7 / 81.7; B4 T4096, 16 heads of 128, window 1024 (9) 438 / 475, 1408 (12) 505 / 536, 16 + 8 heads (18) 447 /
+    // 450; B2 T8192, 8 + 4 heads of 64, window 1024 (18) 183 / 196; B4 T4096, 16 + 4 heads of 128, window 1024 (36)
+    // 414 / 412, of 64 335 / 332.  (Also where sink tiles that meet many more are not split: 970 / 1078, B8
+    // T4096, 32 heads of 64, window 512, 4 sinks.)
     const long long keys = (long long)p.split.ctas(p.a, kTile) * p.Hkv * B;
     const long long met = (long long)p.G * ((p.window + kTile - 1) / kTile + 1);
     const long long kv_ctas = met < 24 ? std::min(keys, 152LL) : keys;

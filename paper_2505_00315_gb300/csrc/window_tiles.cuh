@@ -70,25 +70,31 @@ inline dim3 grid_of(int tiles, int H, int B) { return dim3((unsigned)((long long
 // dk and dv are summed by one CTA per key tile, over the queries that see it: window + tile of them,
 // but for sinks all later ones, Tk / window times as many.  Those beyond a sink tile's window go
 // to `extra` CTAs of their own, `chunk` tiles of queries each (as many as other tiles have, and more
-// where that would take over kMostExtra CTAs), which leave fp32 sums of the sink rows;
-// add_sink_rows adds them up in order.  With over kMostSinks sinks their tiles are many and
-// fill the GPU by themselves: nothing is split, so that the sums' room stays small.
+// where that would take over kMostExtra CTAs, or over kMostBytes for their sums), which leave fp32 sums of the
+// sink rows; add_sink_rows adds them up in order.  Where the sink tiles of all heads and sequences are as
+// many as SMs they fill the GPU by themselves and nothing is split (so kMostBytes has room for three sums
+// at least).  Backward, us, split / not: B1 T16384, 8 heads on 1 of 64, window 512, 513 sinks (5 tiles) 202 / 1437;
+// B8 T4096, 8 heads of 64, window 256, 512 sinks (256 tiles) 400 / 279; B8 T4096, 32 heads of 64,
+// window 512, 4 sinks (256 tiles) 1011 / 970; B16 T4096, 16 heads of 64, window 256, 1 sink (256 tiles) 842 / 870.
 struct SinkSplit {
-    static constexpr int kMostExtra = 64, kMostSinks = 512;
+    static constexpr int kMostExtra = 64;
+    static constexpr long long kMostBytes = 64 << 20;
     int extra = 0, chunk = 1;
     SinkSplit() = default;
     SinkSplit(const Attn &a, int tile) {
         const long long beyond = ((long long)a.Tk - (tile - 1 + (long long)a.window) + tile - 1) / tile;   // tiles
-        if (a.sinks <= 0 || a.sinks > kMostSinks || beyond <= 0) return;
-        chunk = std::max((a.window + tile - 2) / tile + 1, (int)((beyond + kMostExtra - 1) / kMostExtra));
+        const long long tiles = (long long)((a.sinks + tile - 1) / tile) * a.Hkv * a.B;
+        if (tiles == 0 || tiles >= 152 || beyond <= 0) return;
+        const long long most = std::min<long long>(kMostExtra, kMostBytes / sum_bytes(a) - 1);
+        chunk = std::max((a.window + tile - 2) / tile + 1, (int)((beyond + most - 1) / most));
         extra = (int)((beyond + chunk - 1) / chunk);
     }
     __host__ __device__ int extras(const Attn &a, int tile) const { return (a.sinks + tile - 1) / tile * extra; }
     // CTAs of one key head of one sequence: the extra ones first.
     int ctas(const Attn &a, int tile) const { return extras(a, tile) + (a.Tk + tile - 1) / tile; }
-    size_t bytes(const Attn &a) const {
-        return extra == 0 ? 0 : (size_t)a.B * a.Hkv * (extra + 1) * a.sinks * 2 * a.hp * sizeof(float);
-    }
+    // Of one sum of all sink rows' dk and dv, and of all of them.
+    static long long sum_bytes(const Attn &a) { return (long long)a.B * a.Hkv * a.sinks * 2 * a.hp * (long long)sizeof(float); }
+    size_t bytes(const Attn &a) const { return extra == 0 ? 0 : (size_t)(extra + 1) * sum_bytes(a); }
 };
 
 // One of those CTAs: its key tile from k0 on and its query positions first .. last.
@@ -96,7 +102,7 @@ template <int N>
 struct KeyTile {
     int k0, part, first, last, extra;
     bool has_sinks;   // rows below the number of sinks go to the partial sums
-    __device__ __forceinline__ KeyTile(int x, const Attn &a, const SinkSplit &sp, int len) {
+    __host__ __device__ __forceinline__ KeyTile(int x, const Attn &a, const SinkSplit &sp, int len) {
         const int extras = sp.extras(a, N), off = a.Tk - a.Tq;
         extra = sp.extra;
         part = x < extras ? 1 + x % extra : 0;
