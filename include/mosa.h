@@ -294,7 +294,10 @@ mosa_status mosa_route_noalloc(const mosa_shape *shape, const void *X, const voi
  *     (else MOSA_ERR_INVALID_ARG); the norm takes any H and Hkv.
  *   - Nothing is captured into graphs by these calls, so they can be captured by
  *     the caller (after one call outside the capture, which loads the kernels).
- *   - MOSA_FORCE_SIMT=1 runs the CUDA-core kernels only, as for the layer. */
+ *   - MOSA_FORCE_SIMT=1 runs the CUDA-core kernels only, as for the layer.
+ *   - For tests of the give-up path only: MOSA_TEST_WINDOW_WAIT_NS=n limits each wait of
+ *     the tensor-core kernels to n nanoseconds instead of 2 s (read at the launch); a wait
+ *     that runs out makes mosa_window_check_status return MOSA_ERR_DEVICE_TIMEOUT. */
 typedef struct {
     int64_t b, t, h;
 } mosa_strides;

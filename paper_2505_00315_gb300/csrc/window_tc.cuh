@@ -3,6 +3,8 @@
 // waits, TMEM loads whose values cannot be used early, bf16 packing).
 #pragma once
 
+#include <cstdlib>
+
 #include "tc_common.cuh"
 #include "tc_tiles.cuh"
 #include "tmap.h"
@@ -50,20 +52,30 @@ __device__ __forceinline__ void store_box(const Map &m, uint32_t src, int c, int
         : "memory");
 }
 
-// Waits for a phase; gives up (false) when the CTA is giving up, and after the usual
-// limit, which sets the status.  Looks at the clock on every 16th try only: waiting warps share
-// their issue slots with those that compute.
-__device__ __forceinline__ bool wait_or_abort(uint64_t &bar, uint32_t parity, int *abort,
-                                              uint32_t *status) {
+// The longest that a wait of the kernels lasts, in ns: kWaitLimitNs, or for tests of giving up the value of
+// MOSA_TEST_WINDOW_WAIT_NS (> 0 and less than that).
+static_assert(kWaitLimitNs < 1ull << 32, "32 bits");
+inline uint32_t wait_limit() {
+    const char *v = std::getenv("MOSA_TEST_WINDOW_WAIT_NS");
+    const unsigned long long ns = v == nullptr ? 0 : std::strtoull(v, nullptr, 10);
+    return (uint32_t)(ns > 0 && ns < kWaitLimitNs ? ns : kWaitLimitNs);
+}
+
+// Waits for a phase; gives up (false) when the CTA is giving up, and after the limit,
+// which sets the status.  Looks at the clock on every 16th try (a shorter limit: every one), as waiting
+// warps share their issue slots with those that compute: one by one the prompt of 16384 tokens took 2%
+// longer.
+__device__ __forceinline__ bool wait_or_abort(uint64_t &bar, uint32_t parity, int *abort, uint32_t *status,
+                                              uint32_t limit_ns) {
     const uint32_t at = smem_u32(&bar);
     if (mbar_try_wait(at, parity)) return true;
     unsigned long long t0 = 0;
     for (uint32_t n = 1; !mbar_try_wait(at, parity); ++n) {
-        if ((n & 15) != 0) continue;
+        if ((n & 15) != 0 && limit_ns == kWaitLimitNs) continue;
         if (*(volatile int *)abort) return false;
         const unsigned long long now = globaltimer();
         if (t0 == 0) t0 = now;
-        if (now - t0 > kWaitLimitNs) {
+        if (now - t0 > limit_ns) {
             atomicOr(status, kStatusTimeout);
             *(volatile int *)abort = 1;
             return false;
@@ -81,6 +93,26 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t &bar, uint32_t parity, in
 // one part / two, window 64: B2 T8192, 4 heads of 64, forward 20.5 / 24.8 us, backward 58 / 63; B4 T4096, 16 + 4
 // heads of 128 88 / 107, 217 / 236.
 inline bool few_terms(const Attn &a) { return std::min((long long)a.Tk, (long long)a.window + a.sinks) <= 128; }
+
+// Whether the CTA is giving up, the same answer for all lanes of a warp: some may have read the word before it
+// was set, and what follows is for whole warps.
+__device__ __forceinline__ bool giving_up(const int *abort) {
+    return __any_sync(0xffffffffu, *(const volatile int *)abort != 0);
+}
+
+// The same for the `threads` that meet at named barrier id.
+__device__ __forceinline__ bool giving_up_at(int id, int threads, const int *abort) {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.s32 q, %3, 0;\n\t"
+        "barrier.cta.red.or.pred p, %1, %2, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(any)
+        : "r"(id), "r"(threads), "r"(*(const volatile int *)abort)
+        : "memory");
+    return any != 0;
+}
 
 // Products of whole tiles, issued by one thread.  Operand tiles are NB 64-column blocks of 128
 // rows, kBlk bytes apart; their descriptors differ by constants from the first, so that a

@@ -61,6 +61,7 @@ struct BwdArgs {
     int wide_dq, wide_dk, wide_dv;      // rows of these start at a multiple of 32 bytes
     float *partial;                     // [B, Hkv, slots, sinks, 2, hp] fp32: dk, dv of the sink rows
     uint32_t *status;
+    uint32_t wait_ns;
     Attn a;
     SinkSplit split;
     int Tq, Tk, H, Hkv, G, hp, window, sinks;
@@ -169,7 +170,7 @@ __device__ __forceinline__ void key_grads(const BwdArgs &p, uint8_t *smem, const
     tc_fence_after();
     const uint32_t tS = sm.tmem, tG = tS + 128, tdV = tS + 256, tdK = tS + 384;
     auto wait = [&](uint64_t &bar, uint32_t parity) {
-        return wait_or_abort(bar, parity, &sm.abort, p.status);
+        return wait_or_abort(bar, parity, &sm.abort, p.status, p.wait_ns);
     };
 
     // Tiles with something to see and their blocks are numbered on (it, g).
@@ -306,7 +307,7 @@ __device__ __forceinline__ void key_grads(const BwdArgs &p, uint8_t *smem, const
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, at = lanes + c0;
         const int d0 = (warp >> 2) * (HD / 4);   // this thread's quarter of the columns of dK and dV
         const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
-        for (uint32_t x = cta.x; x < all && *(volatile int *)&sm.abort == 0; x += cta.ctas) {
+        for (uint32_t x = cta.x; x < all && !giving_up(&sm.abort); x += cta.ctas) {
             const KeyWork w(p, x);
             const int k0 = w.kt.k0, last = w.kt.last, t = k0 + r;
             int pq = w.kt.first, i_blk = 0;
@@ -508,7 +509,7 @@ __device__ __forceinline__ void query_grads(const BwdArgs &p, uint8_t *smem, con
     tc_fence_after();
     const uint32_t tS = sm.tmem, tG = tS + 256, tdQ = tS + 384;   // S buffers at tS, tS + 128
     auto wait = [&](uint64_t &bar, uint32_t parity) {
-        return wait_or_abort(bar, parity, &sm.abort, p.status);
+        return wait_or_abort(bar, parity, &sm.abort, p.status, p.wait_ns);
     };
     // Tiles and key blocks of both passes are numbered on (it, g); the S of block g lies in buffer
     // g & 1.  The second pass takes the tiles marked in `again`.
@@ -638,7 +639,7 @@ __device__ __forceinline__ void query_grads(const BwdArgs &p, uint8_t *smem, con
             int t = next_of(0);
             uint32_t x = cta.x + (uint32_t)t * cta.ctas;
             Row row = row_of(min(x, all - 1));
-            while (x < all && *(volatile int *)&sm.abort == 0) {
+            while (x < all && !giving_up(&sm.abort)) {
                 const QueryTile w = row.w;
                 const int pos = w.pf + r, tile_no = t;
                 const bool valid = pos <= w.pl;
@@ -797,6 +798,7 @@ bool tc_window_bwd(const Attn &a, const void *q, const void *k, const void *v, c
     p.sdv = a.dv;
     p.partial = partial;
     p.status = status;
+    p.wait_ns = wait_limit();
     p.Tq = a.Tq;
     p.Tk = a.Tk;
     p.H = a.H;

@@ -47,6 +47,7 @@ struct FwdArgs {
     bf16 *O;
     float *lse;
     uint32_t *status;
+    uint32_t wait_ns;
     Str so;
     int keep_rest;               // what O loses by its rounding goes to `rest`
     int B, Tq, Tk, H, G, hp, window, sinks;
@@ -155,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     int j;
                     const bool is_v = kv_tile<kEarly>(x, n, j);
                     const int s = item % NS;
-                    ok = wait_or_abort(sm.kv_empty[s], ((item / NS) & 1) ^ 1, &sm.abort, p.status);
+                    ok = wait_or_abort(sm.kv_empty[s], ((item / NS) & 1) ^ 1, &sm.abort, p.status, p.wait_ns);
                     if (!ok) break;
                     const uint32_t bar = smem_u32(&sm.kv_full[s]);
                     mbar_expect_tx(bar, NB * kBlk);
@@ -174,10 +175,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                 constexpr uint32_t idS = idesc_bf16(128, kN, false, false);
                 constexpr uint32_t idO = idesc_bf16(128, HD, false, true);
                 const uint64_t dq = k_major(sm.q);
-                ok = ok && wait_or_abort(sm.q_full, 0, &sm.abort, p.status);
+                ok = ok && wait_or_abort(sm.q_full, 0, &sm.abort, p.status, p.wait_ns);
                 auto next = [&]() -> int {   // slot of the next tile, or -1
                     const int s = item % NS;
-                    ok = ok && wait_or_abort(sm.kv_full[s], (item / NS) & 1, &sm.abort, p.status);
+                    ok = ok && wait_or_abort(sm.kv_full[s], (item / NS) & 1, &sm.abort, p.status, p.wait_ns);
                     ++item;
                     tc_fence_after();
                     return ok ? s : -1;
@@ -193,10 +194,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                 scores();
                 for (int j = 0; j < n && ok; ++j, ++phase) {
                     if (kEarly && j + 1 < n) {
-                        ok = wait_or_abort(sm.s_free, phase & 1, &sm.abort, p.status);
+                        ok = wait_or_abort(sm.s_free, phase & 1, &sm.abort, p.status, p.wait_ns);
                         scores();
                     }
-                    ok = ok && wait_or_abort(sm.p_ready, phase & 1, &sm.abort, p.status);
+                    ok = ok && wait_or_abort(sm.p_ready, phase & 1, &sm.abort, p.status, p.wait_ns);
                     const int s = next();
                     if (s < 0) break;
                     const uint64_t dv = mn_major(sm.kv[s]);
@@ -229,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     const bool whole = wb.has(j);
                     uint32_t seen = ~0u;
                     if (!whole) seen = seen_bits(kb, j, kb.start(j), 32 * cq, pos, p.window, p.sinks);
-                    wait_or_abort(sm.s_full, phase & 1, &sm.abort, p.status);
+                    wait_or_abort(sm.s_full, phase & 1, &sm.abort, p.status, p.wait_ns);
                     tc_fence_after();
                     float s[32];
                     tmem_get32(tmy, s);
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
                     if (kSecond && !whole) {
                         // V rows with NaN or infinities: zeroed, and NaN for the rows that see them
                         const int t = item + v_tile<kEarly>(j, n);
-                        wait_or_abort(sm.kv_full[t % NS], (t / NS) & 1, &sm.abort, p.status);
+                        wait_or_abort(sm.kv_full[t % NS], (t / NS) & 1, &sm.abort, p.status, p.wait_ns);
                         if (cq == 0) {
                             const uint32_t odd = __ballot_sync(0xffffffffu, clean_row<NB>(sm.kv[t % NS][0], r));
                             if (lane == 0) sm.odd[q] = odd;
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
 #pragma unroll
                     for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
                     if (kEarly && j > 0) {   // P and O may be written: P_{j-1} V_{j-1} is done
-                        wait_or_abort(sm.pv_done, (phase & 1) ^ 1, &sm.abort, p.status);
+                        wait_or_abort(sm.pv_done, (phase & 1) ^ 1, &sm.abort, p.status, p.wait_ns);
                         tc_fence_after();
                     }
                     tmem_st16_async(kEarly ? tP + lanes + 16 * cq : tmy, w);
@@ -308,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
             };
             pass == 0 ? weigh(std::false_type()) : weigh(std::true_type());
             item += 2 * n;
-            wait_or_abort(sm.o_done, pass, &sm.abort, p.status);
+            wait_or_abort(sm.o_done, pass, &sm.abort, p.status, p.wait_ns);
             tc_fence_after();
             float o[HD / 64][16];   // this thread's quarter of the columns
             float odd = 0.f;
@@ -322,9 +323,8 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_tc_kernel(const __grid
             if (pass == 0 && valid && !(odd == 0.f)) sm.redo = 1;
             float (*part)[kQ] = sm.part[phase & 1];
             part[cq][r] = l;
-            named_barrier(5, kWorkers);
+            const bool live = !giving_up_at(5, kWorkers, &sm.abort);
             l = (part[0][r] + part[1][r]) + (part[2][r] + part[3][r]);
-            const bool live = *(volatile int *)&sm.abort == 0;
             if (live && (pass == 1 || *(volatile int *)&sm.redo == 0)) {
                 const float inv = valid ? 1.f / l : 0.f;
 #pragma unroll
@@ -397,6 +397,7 @@ bool tc_window_fwd(const Attn &a, const void *q, const void *k, const void *v, c
     p.O = (bf16 *)O;
     p.lse = lse;
     p.status = status;
+    p.wait_ns = wait_limit();
     p.so = a.o;
     p.Tq = a.Tq;
     p.Tk = a.Tk;
