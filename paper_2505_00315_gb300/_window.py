@@ -79,6 +79,11 @@ def _sig(t):
     return None if t is None else (t.shape, t.stride(), t.dtype)
 
 
+def _half(rotary, hp):
+    """The rotated dimensions: half a head by default."""
+    return hp // 2 if rotary is None else _int(rotary, "rotary")
+
+
 def _bad(*named):
     """Says which argument is not a tensor on the GPU."""
     for name, t in named:
@@ -133,8 +138,8 @@ def _rank(t, name, n):
         raise ValueError(f"{name} must have {n} dimensions, got {tuple(t.shape)}")
 
 
-# What goes into a key is a number of its own, taken from the argument at each call: an object that
-# stands for one (a tensor, say) may hold another the next time.
+# What goes into a key is a plain number, taken from the argument at each call where that is none: an
+# object that stands for one (a tensor, say) may hold another the next time.
 
 def _int(x, name):
     """A Python or NumPy integer, or a tensor of one, that the library's 32-bit field holds."""
@@ -145,14 +150,13 @@ def _int(x, name):
 
 
 def _float(x):
-    """The value of a number that is no Python float, as the library's 32-bit field holds it."""
-    return _f32(x).value
+    """The value of a number, as the library's 32-bit field holds it if it is no Python float."""
+    return x if type(x) is float else _f32(x).value
 
 
 def _rotation(rotary, theta, eps, halves):
     """The rotation's and the norm's arguments as plain numbers (rotary None: half a head)."""
-    return (None if rotary is None else _int(rotary, "rotary"), theta if type(theta) is float else _float(theta),
-            eps if type(eps) is float else _float(eps), 1 if halves else 0)
+    return (None if rotary is None else _int(rotary, "rotary"), _float(theta), _float(eps), bool(halves))
 
 
 def _on(stream):
@@ -194,8 +198,8 @@ def _qk_plan(q, k, gamma_q, gamma_k, positions, rotary, theta, eps, halves, yq, 
     _vector(dgamma_q, "dgamma_q", (hp,), torch.float32)
     _vector(dgamma_k, "dgamma_k", (hp,), torch.float32)
     y = ("dyq", "dyk") if backward else ("out q", "out k")
-    s = MosaQkShape(B, T, H, Hkv, hp, _b._dtype_code(q), hp // 2 if rotary is None else rotary, halves, theta,
-                    eps, _heads(q, "q"), _heads(k, "k", None, dt), _out(yq, y[0], q.shape, dt),
+    s = MosaQkShape(B, T, H, Hkv, hp, _b._dtype_code(q), _half(rotary, hp), 1 if halves else 0,
+                    theta, eps, _heads(q, "q"), _heads(k, "k", None, dt), _out(yq, y[0], q.shape, dt),
                     _out(yk, y[1], k.shape, dt))
     need = 0
     if backward:
@@ -217,7 +221,8 @@ def mosa_qk_norm_rope(q, k, gamma_q=None, gamma_k=None, positions=None, rotary=N
             return mosa_qk_norm_rope(q, k, gamma_q, gamma_k, positions, rotary, theta, eps, halves, out)
     torch = _b._torch()
     yq, yk = (out.get("q"), out.get("k")) if out else (None, None)
-    rotary, theta, eps, halves = _rotation(rotary, theta, eps, halves)
+    if not (type(theta) is type(eps) is float and type(halves) is bool and (rotary is None or type(rotary) is int)):
+        rotary, theta, eps, halves = _rotation(rotary, theta, eps, halves)
     try:
         key = (1, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, rotary, theta, eps, halves,
                _sig(gamma_q), _sig(gamma_k), _sig(positions), _sig(yq), _sig(yk))
@@ -258,7 +263,8 @@ def mosa_qk_norm_rope_backward(q, k, gamma_q, gamma_k, dyq, dyk, positions=None,
     torch = _b._torch()
     dq, dk, dgq, dgk = ((out.get("dq"), out.get("dk"), out.get("dgamma_q"), out.get("dgamma_k"))
                         if out else (None, None, None, None))
-    rotary, theta, eps, halves = _rotation(rotary, theta, eps, halves)
+    if not (type(theta) is type(eps) is float and type(halves) is bool and (rotary is None or type(rotary) is int)):
+        rotary, theta, eps, halves = _rotation(rotary, theta, eps, halves)
     try:
         key = (2, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, rotary, theta, eps, halves,
                _sig(gamma_q), _sig(gamma_k), _sig(positions), dyq.shape, dyq.stride(), dyq.dtype,
@@ -307,9 +313,9 @@ def _window_plan(q, k, v, O, lse, lens, window, sinks, scale, dO=None, dq=None, 
     dt = q.dtype
     _vector(lens, "lens", (B,), torch.int32)
     _vector(lse, "lse", (B, H, Tq), torch.float32)
-    s = MosaWindowShape(B, Tq, Tk, H, Hkv, hp, _b._dtype_code(q), window, sinks, scale,
-                        _heads(q, "q"), _heads(k, "k", None, dt), _heads(v, "v", k.shape, dt),
-                        _out(O, "O", q.shape, dt))
+    s = MosaWindowShape(B, Tq, Tk, H, Hkv, hp, _b._dtype_code(q), _int(window, "window"),
+                        _int(sinks, "sinks"), scale, _heads(q, "q"), _heads(k, "k", None, dt),
+                        _heads(v, "v", k.shape, dt), _out(O, "O", q.shape, dt))
     if dO is not None:
         s.go = _heads(dO, "dO", q.shape, dt)
         s.dq, s.dk, s.dv = (_out(dq, "dq", q.shape, dt), _out(dk, "dk", k.shape, dt),
@@ -329,8 +335,8 @@ def mosa_window_forward(q, k, v, window: int, sinks: int = 0, lens=None, scale: 
             return mosa_window_forward(q, k, v, window, sinks, lens, scale, workspace, out, None, want_lse)
     torch = _b._torch()
     O, lse = (out.get("O"), out.get("lse")) if out else (None, None)
-    window, sinks = _int(window, "window"), _int(sinks, "sinks")
-    scale = scale if type(scale) is float else _float(scale)
+    if not (type(window) is type(sinks) is int and type(scale) is float):
+        window, sinks, scale = _int(window, "window"), _int(sinks, "sinks"), _float(scale)
     try:
         qs = q.shape
         key = (3, qs, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
@@ -368,8 +374,8 @@ def mosa_window_backward(q, k, v, O, lse, dO, workspace, window: int, sinks: int
             return mosa_window_backward(q, k, v, O, lse, dO, workspace, window, sinks, lens, scale, out)
     torch = _b._torch()
     dq, dk, dv = (out.get("dq"), out.get("dk"), out.get("dv")) if out else (None, None, None)
-    window, sinks = _int(window, "window"), _int(sinks, "sinks")
-    scale = scale if type(scale) is float else _float(scale)
+    if not (type(window) is type(sinks) is int and type(scale) is float):
+        window, sinks, scale = _int(window, "window"), _int(sinks, "sinks"), _float(scale)
     try:
         key = (4, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
                O.shape, O.stride(), O.dtype, lse.shape, lse.stride(), lse.dtype, dO.shape, dO.stride(),
@@ -435,8 +441,8 @@ def _decode_plan(q, k, v, Kc, Vc, lens, O, gamma_q, gamma_k, window, sinks, norm
                _bh(O, "O", q.shape, dt), _heads(Kc, "K_cache", cache, dt),
                _heads(Vc, "V_cache", cache, dt))
     _vector(lens, "lens", (B,), _b._torch_mod.int32)
-    s = MosaDecodeShape(B, C, H, Hkv, hp, _b._dtype_code(q), window, sinks, norm,
-                        hp // 2 if rotary is None else rotary, halves, scale, theta, eps, *strides)
+    s = MosaDecodeShape(B, C, H, Hkv, hp, _b._dtype_code(q), _int(window, "window"), _int(sinks, "sinks"),
+                        1 if norm else 0, _half(rotary, hp), 1 if halves else 0, scale, theta, eps, *strides)
     return ctypes.byref(s), int(_b.load().mosa_window_decode_workspace_bytes(ctypes.byref(s))), s
 
 
@@ -455,9 +461,10 @@ def mosa_window_decode(q, k, v, K_cache, V_cache, lens, window: int, sinks: int 
                                       theta, eps, halves, scale, workspace, out)
     torch = _b._torch()
     O = out.get("O") if out else None
-    window, sinks, norm = _int(window, "window"), _int(sinks, "sinks"), 1 if norm else 0
-    scale = scale if type(scale) is float else _float(scale)
-    rotary, theta, eps, halves = _rotation(rotary, theta, eps, halves)
+    if not (type(window) is type(sinks) is int and type(scale) is float and type(norm) is bool):
+        window, sinks, scale, norm = _int(window, "window"), _int(sinks, "sinks"), _float(scale), bool(norm)
+    if not (type(theta) is type(eps) is float and type(halves) is bool and (rotary is None or type(rotary) is int)):
+        rotary, theta, eps, halves = _rotation(rotary, theta, eps, halves)
     try:
         key = (5, q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
                K_cache.shape, K_cache.stride(), K_cache.dtype, V_cache.shape, V_cache.stride(),
