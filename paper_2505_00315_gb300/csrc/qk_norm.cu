@@ -10,7 +10,7 @@
 // computes each token's sines and cosines once for all of them, in shared memory.  Loads of the
 // next item are under way while one is worked on.  What bounds it is how many bytes the
 // registers keep in flight: B4 T4096, 32 + 8 heads of 128, bf16: forward 61 us (5.5 TB/s, 81% of
-// the copy rate), backward 106 (4.8 TB/s, 70%).  One new token of eight sequences: 3 us, a
+// the copy rate), backward 107 (4.7 TB/s, 69%); fp32 113 (6.0 TB/s, 88%) and 180 (5.6 TB/s, 82%).  One new token of eight sequences: 3 us, a
 // launch and one trip to memory.
 #include <cmath>
 

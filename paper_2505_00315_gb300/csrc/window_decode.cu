@@ -16,9 +16,9 @@
 //          tcgen05 would want 128 rows and its operands in shared memory; the products are
 //          a tenth of the time that the bytes take.
 //   fp32, hp = 16, unaligned rows   CUDA cores: hp/8 lanes hold a row, eight values a lane.
-// B48, up to 4100 tokens, 32 + 8 heads of 128, bf16: 126 us, 5.1 TB/s, 75% of the copy rate (on CUDA
+// B48, up to 4100 tokens, 32 + 8 heads of 128, bf16: 122 us, 5.3 TB/s, 78% of the copy rate (on CUDA
 // cores 539: each row's products with four heads are more instructions than its bytes have
-// time for).  B1, 1028 tokens, 16 + 4 heads: 6.5 us and 3.6 for the join, latency: the norm, the
+// time for); fp32, all of them whole, 362 us, 4.4 TB/s, 66%.  B1, 1028 tokens, 16 + 4 heads: 6.4 us and 3.3 for the join, latency: the norm, the
 // rotation, one trip for K, one for V, the warps' and the splits' sums in turn.
 #include "head_rows.cuh"
 #include "launch.h"

@@ -10,8 +10,8 @@
 // thread, operands as fp32 in shared memory, the softmax's running maximum and
 // sum in registers.  The backward takes one kernel by key tiles (dk, dv) and one by
 // query tiles (dq), so that every sum runs in one thread in a fixed order.
-// B2 T1000, 12 heads of 64, window 125, fp32: forward 45 us, dk and dv 85, dq 56; the FMA pipe is
-// busy 35 to 42% of the time, shared memory 52 to 65%, the issue slots 55 to 62%.  What bounds them:
+// B2 T1000, 12 heads of 64, window 125, fp32: ragged lengths: forward 43 us, dk and dv 85, dq 57; the
+// FMA pipe is busy 36 to 42% of the time, shared memory 54 to 65%, the issue slots 55 to 61%.  What bounds them:
 // operands from shared memory (a 16-byte load for every eight FMAs of a thread), 16 warps an
 // SM whose tiles are loaded between barriers, and 384 CTAs for 304 places.  Packed FMAs changed nothing, three CTAs an SM at
 // 80 registers took a third longer.

@@ -18,9 +18,9 @@
 // from several CTAs: 64 KB of fp32 reductions per pair of tiles against 2560
 // cycles of MMAs (hp = 128), in an order that changes from run to run, and a pass to zero
 // and one to round it.
-// B4 T4096, 16 + 4 heads of 128, window 1024: dQ 186 us, dK and dV 199 (the tensor pipe is busy 68% of
-// both; the rest is the chain scores -> weights -> product within a block and, with one CTA an
-// SM, its beginning and end).  B2 T8192, 4 heads of 64, window 512: 35 and 39 us, where MMAs take half
+// B4 T4096, 16 + 4 heads of 128, window 1024: 373 us, of which dQ about a half (the tensor pipe is busy 67% of
+// them; the rest is the chain scores -> weights -> product within a block and, with one CTA an
+// SM, its beginning and end).  B2 T8192, 4 heads of 64, window 512: 66 us, where MMAs take a third of
 // the cycles and the elementwise work of a block is what counts.
 // Keys that are sinks are seen by every later query: those queries beyond the
 // tile's window go to CTAs of their own, some blocks each, whose fp32 sums for the

@@ -17,11 +17,11 @@
 // With hp <= 64 P has columns of its own, and the next scores are computed as soon as
 // the warps have read the last ones (unless P is taken in two parts).
 //
-// B1 T16384, 32 + 8 heads of 128, window 2048: 482 us, 1.07 PFLOP/s of the pairs that are seen.  With
-// hp = 128 that is bound by issue and by each CTA's chain: a thread's 32 scores take 220 instructions, 96 of
+// B1 T16384, 32 + 8 heads of 128, window 2048: 482 us back to back (502 with the call around it and nothing of it in
+// L2), 1.07 PFLOP/s of the pairs that are seen.  With hp = 128 that is bound by issue and by each CTA's chain: a thread's 32 scores take 220 instructions, 96 of
 // which are maxima, scaling, exponentials, sums and packing, the others the waits, fences and exchange of
 // a block; issue slots are busy 50 to 55% of the time, the tensor pipe 45%.  (Eight worker warps with 64
-// columns a thread: 606 us against 531 then.)  hp = 64, B2 T8192, 4 heads, window 512: 30 us, of
+// columns a thread: 606 us against 531 then.)  hp = 64, B2 T8192, 4 heads, window 512: 29 us, of
 // which 512 CTAs' beginnings and ends are a third; early scores took it from 33 to 31 there.
 //
 // A masked key has P = 0, but 0 times a NaN or infinity of its V row is NaN: a CTA whose
