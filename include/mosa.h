@@ -420,6 +420,142 @@ mosa_status mosa_window_decode(const mosa_decode_shape *shape, const void *q, co
                                const int32_t *lens, void *K_cache, void *V_cache, void *O,
                                void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Block operators: what a language model has around its heads ----------
+ * The residual step between two blocks (norm of a block's output, gate, dropout, scaled sum with
+ * the stream, norm before the next block), dropout alone, and log probabilities of given tokens
+ * with entropy and top alternatives.
+ *
+ * Conventions shared by these calls (where they differ from the layer's):
+ *   - A tensor [B,T,n] is a device pointer and the strides, in elements, of its sequences (b) and
+ *     tokens (t) (h is ignored); the n values of a token are contiguous.  Strides are >= 0; where a
+ *     size is 1 its stride is ignored.  Inputs may overlap (stride 0 repeats a row); outputs may not,
+ *     neither within themselves nor with inputs but where a call says so.
+ *   - Sums, norms and softmax statistics are held in fp32; outputs are rounded once.  Sums
+ *     over tokens run in a fixed order: the same bits every time.
+ *   - Tensors start at a multiple of their element size.  Where pointers are multiples of 16
+ *     bytes and strides of 16 bytes' worth of elements, rows move in 16-byte pieces.
+ *   - B*T < 2^31 (else MOSA_ERR_UNSUPPORTED).
+ *   - Nothing is captured into graphs by these calls, so they can be captured by the caller (after
+ *     one call outside the capture, which loads the kernels).  Two calls under way at the same
+ *     time need workspaces of their own.
+ *
+ * Random numbers: the 32-bit word of column j of token (b, t) is word j % 4 of Philox 4x32 with seven
+ * rounds (Salmon et al., 2011) of the counter (j / 4, b*T + t, o mod 2^32, o / 2^32) under the key
+ * (s mod 2^32, s / 2^32), where s = rng[0] and o = rng[1] + site mod 2^64: rng [2] int64 lies on the
+ * device and is read when the call runs, so that a replayed graph sees what it holds then;
+ * sites tell the places of one model apart that share it.  A value is kept where its word is at
+ * least round(p 2^32), and then scaled by 1/(1-p); a dropped one is 0 whatever it was.  No mask is
+ * stored: a backward with the same rng, site and p draws the same words. */
+
+/* Residual step: for each token, with y the block's output and x the stream,
+ *     n = r_y y gamma_post,  r_y = 1/sqrt(mean(y^2) + eps)   (post_norm = 0: n = y)
+ *     u = keep/(1-p) g n,    g = 1, gate [d] or gate [B,T,d]  (sigmoid = 1: of sigmoid(gate))
+ *     x_out = x + scale u
+ *     h = r_x x_out gamma_pre, r_x = 1/sqrt(mean(x_out^2) + eps)  (pre_norm = 0: none; of x_out
+ *                                                               before its rounding)
+ * Sizes: 1 <= d <= 8192 (else MOSA_ERR_UNSUPPORTED); eps >= 0; 0 <= dropout <= 1. */
+typedef enum { MOSA_GATE_NONE = 0, MOSA_GATE_CHANNEL = 1, MOSA_GATE_TOKEN = 2 } mosa_gate;
+
+typedef struct {
+    int32_t B, T, d;
+    int32_t dtype;       /* storage: gamma_post, gamma_pre, gate, h; in the backward dy and the
+                          * gradient of a gate per token */
+    int32_t x_dtype;     /* the stream: x, x_out, dx_out, dx */
+    int32_t y_dtype;     /* the block's output y (the layer's Y is fp32) */
+    int32_t dh_dtype;    /* dh (the layer's dX is fp32) */
+    int32_t post_norm, pre_norm;   /* 0 or 1 */
+    int32_t gate;        /* mosa_gate */
+    int32_t sigmoid;     /* 0 or 1 */
+    int32_t site;        /* see random numbers */
+    float scale, eps;
+    double dropout;      /* p */
+    mosa_strides x, y, g, xo, h;          /* forward; g of a gate per token */
+    mosa_strides dxo, dh, dx, dy, dg;     /* backward only */
+} mosa_residual_shape;
+
+/* Forward.  gamma_post, gamma_pre [d] or NULL for ones; gate as the shape says (NULL with
+ * MOSA_GATE_NONE); rng NULL where dropout = 0; outputs x_out (which may be x itself: same pointer and
+ * strides, where no backward follows, since that needs x), h [B,T,d] (not written with pre_norm = 0)
+ * and stats [2,B,T] fp32, r_y and r_x for the backward (NULL where none follows).  Needs no
+ * workspace. */
+mosa_status mosa_residual_forward(const mosa_residual_shape *shape, const void *x, const void *y,
+                                  const void *gate, const void *gamma_post, const void *gamma_pre,
+                                  const int64_t *rng, void *x_out, void *h, float *stats,
+                                  void *stream);
+
+/* Workspace of the backward (256-byte aligned; it may hold anything); 0 if the shape is invalid. */
+size_t mosa_residual_workspace_bytes(const mosa_residual_shape *shape);
+
+/* Backward: from the forward's inputs and stats and the gradients dx_out (x_dtype) and dh
+ * (dh_dtype; NULL with pre_norm = 0) of its outputs (either NULL: none), the gradients dx (which may be dx_out
+ * itself), dy (storage dtype), of gate: dgate [d] fp32 or [B,T,d] in the storage dtype, and dgamma_post,
+ * dgamma_pre [d] fp32.  Each of the last three may be NULL. */
+mosa_status mosa_residual_backward(const mosa_residual_shape *shape, const void *x, const void *y,
+                                   const void *gate, const void *gamma_post,
+                                   const void *gamma_pre, const int64_t *rng, const float *stats,
+                                   const void *dx_out, const void *dh, void *dx, void *dy,
+                                   void *dgate, float *dgamma_post, float *dgamma_pre,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/* Dropout: y = keep/(1-p) x for x [B,T,d], y in the same dtype, which may be x itself.  The same
+ * call on dy is its backward. */
+typedef struct {
+    int32_t B, T, d;
+    int32_t dtype;
+    int32_t site;
+    double dropout;
+    mosa_strides x, y;
+} mosa_dropout_shape;
+
+mosa_status mosa_dropout(const mosa_dropout_shape *shape, const void *x, const int64_t *rng, void *y,
+                         void *stream);
+
+/* Log probabilities: for each row z of logits [B,T,V], a = scale z (scale: 1 / temperature),
+ *     lse = log sum_j exp(a_j),  p_j = exp(a_j - lse)
+ *     logp = a_t - lse of the target t,  entropy = -sum_j p_j (a_j - lse)
+ * and the `top` largest entries, in falling order, ties by the lower index, with their a_j - lse.
+ * Entries of -2^90 or less (-infinity and the lowest value of a type among them) are ruled out:
+ * weight 0, log probability -infinity, no gradient.  A row with nothing else has lse and
+ * logp = -infinity, entropy 0 and no gradients.  A NaN or an entry above 2^90 makes its row's results
+ * and gradients NaN; the top indices of such a row are some of 0 .. V-1.  A target below 0 is none: logp 0 and no gradient through
+ * it; one of V or more makes logp NaN, and passes no gradient on.
+ * Sizes: 1 <= V < 2^31 - 2^16; 0 <= top <= 32 and top <= V; 2^-20 <= scale <= 2^20
+ * (else MOSA_ERR_UNSUPPORTED). */
+typedef struct {
+    int32_t B, T, V;
+    int32_t dtype;       /* logits and their gradient */
+    int32_t target64;    /* targets are int32 (0) or int64 (1) */
+    int32_t top;
+    float scale;
+    mosa_strides z, dz;  /* logits; their gradient (backward only) */
+} mosa_logprob_shape;
+
+/* Workspace of the forward (256-byte aligned; it may hold anything); 0 if the shape is invalid or
+ * unsupported. */
+size_t mosa_token_logprobs_workspace_bytes(const mosa_logprob_shape *shape);
+
+/* Forward.  targets [B,T] (NULL: none); logp, entropy, lse [B,T] fp32, each may be NULL (logp is
+ * where targets is); top_index [B,T,top] int32 and top_logp [B,T,top] fp32 (NULL where top = 0). */
+mosa_status mosa_token_logprobs(const mosa_logprob_shape *shape, const void *logits,
+                                const void *targets, float *logp, float *entropy, float *lse,
+                                int32_t *top_index, float *top_logp, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* Backward: dlogits (which may be logits itself: same pointer and strides) from the forward's
+ * lse and entropy and the gradients dlogp, dentropy, dlse [B,T] and dtop_logp [B,T,top] fp32 of its
+ * results, each NULL where there is none (entropy is read with dentropy only; top = 0 where dtop_logp is
+ * NULL).  With G = dlogp + sum dtop_logp
+ *     dz_j = scale (dlogp [j = t] + sum_i dtop_logp_i [j = top_i] - G p_j + dlse p_j
+ *                   - dentropy p_j (log p_j + entropy)).
+ * A row whose gradients are all 0 gets zeros.  top_index must hold what the forward returned (an index
+ * outside 0 .. V-1 is skipped). */
+mosa_status mosa_token_logprobs_backward(const mosa_logprob_shape *shape, const void *logits,
+                                         const void *targets, const float *lse,
+                                         const float *entropy, const int32_t *top_index,
+                                         const float *dlogp, const float *dentropy,
+                                         const float *dlse, const float *dtop_logp, void *dlogits,
+                                         void *stream);
+
 /* ---- Measurement support (not part of the layer) ----------------------
  * Stages: 0 router, 1 select, 2 qkv, 3 attn_fwd, 4 out, 5 out_bwd,
  * 6 attn_bwd, 7 in_bwd, 8 w_bwd, 9 dwo (dW_o), 10 fwd_unit (F3-F5 fused,

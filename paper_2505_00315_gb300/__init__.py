@@ -20,13 +20,17 @@ __all__ = ["mosa_forward", "mosa_forward_with_indices", "mosa_backward", "mosa_t
 #: The window heads' calls (``_window``).
 _WINDOW = ["mosa_qk_norm_rope", "mosa_qk_norm_rope_backward", "mosa_window_forward",
            "mosa_window_backward", "mosa_window_check_status", "mosa_window_decode"]
-__all__ += _WINDOW
+#: The block operators' calls (``_block``).
+_BLOCK = ["mosa_residual_forward", "mosa_residual_backward", "mosa_dropout", "mosa_token_logprobs",
+          "mosa_token_logprobs_backward"]
+__all__ += _WINDOW + _BLOCK
 
 
 def __getattr__(name):
     if name in __all__:
-        from . import _binding, _window
-        value = getattr(_window if name in _WINDOW else _binding, name)
+        from . import _binding, _block, _window
+        home = _window if name in _WINDOW else _block if name in _BLOCK else _binding
+        value = getattr(home, name)
         globals()[name] = value   # found at once the next time
         return value
     raise AttributeError(name)

@@ -34,7 +34,10 @@ EXPORTED = ("mosa_status_string", "mosa_workspace_bytes", "mosa_forward",
             "mosa_profile_spans_copy", "mosa_qk_norm_rope", "mosa_qk_norm_rope_workspace_bytes",
             "mosa_qk_norm_rope_backward", "mosa_window_workspace_bytes", "mosa_window_forward",
             "mosa_window_backward", "mosa_window_check_status",
-            "mosa_window_decode_workspace_bytes", "mosa_window_decode")
+            "mosa_window_decode_workspace_bytes", "mosa_window_decode", "mosa_residual_forward",
+            "mosa_residual_workspace_bytes", "mosa_residual_backward", "mosa_dropout",
+            "mosa_token_logprobs_workspace_bytes", "mosa_token_logprobs",
+            "mosa_token_logprobs_backward")
 
 
 class MosaShape(ctypes.Structure):
@@ -131,8 +134,9 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         L.mosa_hybrid_forward.restype = ctypes.c_int
         L.mosa_hybrid_backward.argtypes = [hp_] + [vp] * 10 + [vp, vp, vp] + [vp] * 10 + [vp, sz, vp]
         L.mosa_hybrid_backward.restype = ctypes.c_int
-        from . import _window
+        from . import _block, _window
         _window.declare(L)
+        _block.declare(L)
         _lib = L
         return L
 

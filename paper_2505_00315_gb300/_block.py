@@ -1,0 +1,460 @@
+"""ctypes binding of the block operators (include/mosa.h): the residual step between two blocks,
+dropout, and log probabilities of given tokens.  Argument marshalling only, as in
+``_binding``; tensors are [B, T, n] with any strides whose last is 1."""
+from __future__ import annotations
+
+import ctypes
+
+from . import _binding as _b
+from ._window import MosaStrides, _bad, _float, _int, _keep, _new, _on, _plans, _rank, _sig, _space, _vector
+
+_i32, _f32, _f64 = ctypes.c_int32, ctypes.c_float, ctypes.c_double
+
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN = 0, 1, 2
+
+
+class MosaResidualShape(ctypes.Structure):
+    """mosa_residual_shape: sizes, types, options and strides of mosa_residual_forward and its backward."""
+    _fields_ = ([(n, _i32) for n in ("B", "T", "d", "dtype", "x_dtype", "y_dtype", "dh_dtype", "post_norm",
+                                     "pre_norm", "gate", "sigmoid", "site")]
+                + [("scale", _f32), ("eps", _f32), ("dropout", _f64)]
+                + [(n, MosaStrides) for n in ("x", "y", "g", "xo", "h", "dxo", "dh", "dx", "dy", "dg")])
+
+
+class MosaDropoutShape(ctypes.Structure):
+    """mosa_dropout_shape: sizes and strides of mosa_dropout."""
+    _fields_ = ([(n, _i32) for n in ("B", "T", "d", "dtype", "site")]
+                + [("dropout", _f64), ("x", MosaStrides), ("y", MosaStrides)])
+
+
+class MosaLogprobShape(ctypes.Structure):
+    """mosa_logprob_shape: sizes and strides of mosa_token_logprobs and its backward."""
+    _fields_ = ([(n, _i32) for n in ("B", "T", "V", "dtype", "target64", "top")]
+                + [("scale", _f32), ("z", MosaStrides), ("dz", MosaStrides)])
+
+
+def declare(L) -> None:
+    """Signatures of the block operators' functions."""
+    vp, sz, st = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
+    res, drop, lp = (ctypes.POINTER(c) for c in (MosaResidualShape, MosaDropoutShape, MosaLogprobShape))
+    for name, args, ret in (
+            ("mosa_residual_forward", [res] + [vp] * 10, st),
+            ("mosa_residual_workspace_bytes", [res], sz),
+            ("mosa_residual_backward", [res] + [vp] * 14 + [vp, sz, vp], st),
+            ("mosa_dropout", [drop] + [vp] * 4, st),
+            ("mosa_token_logprobs_workspace_bytes", [lp], sz),
+            ("mosa_token_logprobs", [lp] + [vp] * 7 + [vp, sz, vp], st),
+            ("mosa_token_logprobs_backward", [lp] + [vp] * 11, st)):
+        f = getattr(L, name)
+        f.argtypes, f.restype = args, ret
+
+
+# Calls make and look for everything on the current device and its current stream; one whose tensors lie on
+# another device, or that names a stream, is made again in that one's place.
+
+def _away(t, stream):
+    """Whether the call has to be made again elsewhere: for a stream, or on t's device."""
+    return stream is not None or (t.is_cuda and t.get_device() != _b._torch()._C._cuda_getDevice())
+
+
+def _there(t, stream, call, *args):
+    """The call on ``stream``, or on the current stream of t's device."""
+    cuda = _b._torch().cuda
+    if stream is None:
+        with cuda.device(t.get_device()):
+            return call(*args)
+    if not t.is_cuda:
+        return call(*args)   # refuses it
+    with _on(stream):
+        if cuda.current_device() != t.get_device():
+            raise ValueError("the stream must be one of the tensors' device")
+        return call(*args)
+
+
+def _one_device(dev, *named):
+    """Every tensor lies on device ``dev`` (a number; -1 stands for the CPU)."""
+    for name, t in named:
+        if t is not None and t.get_device() != dev:
+            _bad((name, t)) if not t.is_cuda else None
+            raise ValueError(f"{name} must be on the device of the other tensors")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rows(t, name, like=None, dtype=None):
+    """Strides of a tensor [B, T, n], its shape ``like`` and type checked."""
+    if like is not None and t.shape != like:
+        raise ValueError(f"{name} must have shape {tuple(like)}, got {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    s = t.stride()
+    if s[2] != 1 and t.shape[2] != 1:
+        raise ValueError(f"{name}: the values of a token must be contiguous")
+    return MosaStrides(s[0], s[1], 0)
+
+
+def _result(t, name, like, dtype):
+    """Strides of a result: a given tensor's, or those of the one to be made."""
+    return MosaStrides(like[1] * like[2], like[2], 0) if t is None else _rows(t, name, like, dtype)
+
+
+def _made(t, like, dtype, device):
+    return _b._torch_mod.empty(like, dtype=dtype, device=device) if t is None else t
+
+
+def _check_rng(rng, dropout):
+    if rng is None:
+        if dropout > 0:
+            raise ValueError("dropout needs rng, an int64 tensor of two numbers on the GPU")
+        return
+    if rng.shape != (2,) or rng.dtype != _b._torch_mod.int64 or not rng.is_contiguous():
+        raise ValueError("rng must be a contiguous int64 tensor of two numbers")
+
+
+# ------------------------------------------------------------ residual step
+
+def _storage(dtype, gate, gamma_post, gamma_pre, x):
+    """The storage type: given, or that of the first of gamma_pre, gamma_post, gate and x that is there."""
+    if dtype is not None:
+        return dtype
+    for t in (gamma_pre, gamma_post, gate, x):
+        if t is not None:
+            return t.dtype
+
+
+def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmoid, scale, eps, dropout, rng,
+                   site, dtype, xo, h, stats, back=None):
+    """Checks, and the library's struct.  back: dx_out, dh and the results dx, dy, dgate, dgamma_post,
+    dgamma_pre of a backward."""
+    torch = _b._torch_mod
+    for name, t in (("x", x), ("y", y)):
+        _rank(t, name, 3)
+    B, T, d = x.shape
+    code = {torch.float32: _b.MOSA_F32, torch.bfloat16: _b.MOSA_BF16}
+    if dtype not in code:
+        raise TypeError(f"unsupported storage dtype {dtype} (float32 or bfloat16)")
+    kind = GATE_NONE
+    if gate is not None:
+        kind = GATE_TOKEN if len(gate.shape) == 3 else GATE_CHANNEL
+    s = MosaResidualShape(B, T, d, code[dtype], _b._dtype_code(x), _b._dtype_code(y), code[dtype],
+                          1 if post_norm else 0, 1 if pre_norm else 0, kind, 1 if sigmoid else 0, site, scale,
+                          eps, dropout, _rows(x, "x"), _rows(y, "y", x.shape))
+    _vector(gamma_post, "gamma_post", (d,), dtype)
+    _vector(gamma_pre, "gamma_pre", (d,), dtype)
+    if kind == GATE_TOKEN:
+        s.g = _rows(gate, "gate", x.shape, dtype)
+    else:
+        _vector(gate, "gate", (d,), dtype)
+    _check_rng(rng, dropout)
+    _vector(stats, "stats", (2, B, T), torch.float32)
+    need = 0
+    if back is None:
+        s.xo = _result(xo, "out x", x.shape, x.dtype)
+        s.h = _result(h, "out h", x.shape, dtype)
+    else:
+        dxo, dh, dx, dy, dg, dgpost, dgpre = back
+        if dxo is not None:
+            s.dxo = _rows(dxo, "dx_out", x.shape, x.dtype)
+        if dh is not None:
+            s.dh_dtype = _b._dtype_code(dh)
+            s.dh = _rows(dh, "dh", x.shape)
+        s.dx, s.dy = _result(dx, "dx", x.shape, x.dtype), _result(dy, "dy", x.shape, dtype)
+        if kind == GATE_TOKEN:
+            s.dg = _result(dg, "dgate", x.shape, dtype)
+        else:
+            _vector(dg, "dgate", (d,), torch.float32)
+        _vector(dgpost, "dgamma_post", (d,), torch.float32)
+        _vector(dgpre, "dgamma_pre", (d,), torch.float32)
+        need = int(_b.load().mosa_residual_workspace_bytes(ctypes.byref(s)))
+    return ctypes.byref(s), need, s
+
+
+def _options(post_norm, pre_norm, sigmoid, scale, eps, dropout, site):
+    """Flags and numbers as plain ones."""
+    return (bool(post_norm), bool(pre_norm), bool(sigmoid), _float(scale), _float(eps), float(dropout),
+            _int(site, "site"))
+
+
+def mosa_residual_forward(x, y, gate=None, gamma_post=None, gamma_pre=None, post_norm: bool = True,
+                          pre_norm: bool = True, sigmoid: bool = False, scale: float = 1.0, eps: float = 1e-6,
+                          dropout: float = 0.0, rng=None, site: int = 0, dtype=None, out=None, stream=None):
+    """The step between two blocks, for the stream x and a block's output y, both [B,T,d]:
+    n = RMS norm of y with gamma_post [d] (y itself without ``post_norm``); u = dropout of gate * n (gate: None,
+    [d] or [B,T,d], through a sigmoid with ``sigmoid``); x_out = x + scale * u; h = RMS norm of x_out with
+    gamma_pre (None without ``pre_norm``), the next block's input.  Returns (x_out, h, stats): x_out like
+    x, h in the storage type (``dtype``, by default that of gamma_pre, gamma_post, gate or x), stats
+    [2,B,T] fp32 for the backward.  x and y may each be fp32 or bf16; gammas and gate have the storage
+    type.  ``rng`` [2] int64 on the GPU holds seed and offset, read when the call runs; ``site`` tells
+    calls that share it apart.  ``out`` may hold "x" (x itself where no backward follows), "h" and "stats"."""
+    try:
+        if _away(x, stream):
+            return _there(x, stream, mosa_residual_forward, x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
+                          sigmoid, scale, eps, dropout, rng, site, dtype, out)
+        torch = _b._torch()
+        xo, h, stats = (out.get("x"), out.get("h"), out.get("stats")) if out else (None, None, None)
+        post_norm, pre_norm, sigmoid, scale, eps, dropout, site = _options(post_norm, pre_norm, sigmoid, scale, eps,
+                                                                           dropout, site)
+        dt = _storage(dtype, gate, gamma_post, gamma_pre, x)
+        key = (6, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype, _sig(gate), _sig(gamma_post),
+               _sig(gamma_pre), post_norm, pre_norm, sigmoid, scale, eps, dropout, site, dt, _sig(rng),
+               (_sig(xo), _sig(h), _sig(stats)) if out else None)
+    except AttributeError:
+        _bad(("x", x), ("y", y), ("gate", gate), ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng))
+    plan = _plans.get(key) or _keep(key, _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
+                                                        sigmoid, scale, eps, dropout, rng, site, dt, xo, h, stats))
+    dev = x.get_device()
+    if dev < 0:
+        _bad(("x", x))
+    _one_device(dev, ("y", y), ("gate", gate), ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng),
+                ("out x", xo), ("out h", h), ("stats", stats))
+    if xo is None:
+        xo = _new(x)
+    if not pre_norm:
+        h = None
+    elif h is None:
+        h = torch.empty(x.shape, dtype=dt, device=x.device)
+    if stats is None:
+        stats = torch.empty((2, x.shape[0], x.shape[1]), dtype=torch.float32, device=x.device)
+    rc = _b.load().mosa_residual_forward(
+        plan[0], x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(gamma_post), _ptr(gamma_pre), _ptr(rng),
+        xo.data_ptr(), _ptr(h), stats.data_ptr(), _b._stream(None))
+    if rc:
+        _b._check(rc, "mosa_residual_forward")
+    return xo, h, stats
+
+
+def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, gamma_pre=None,
+                           post_norm: bool = True, pre_norm: bool = True, sigmoid: bool = False,
+                           scale: float = 1.0, eps: float = 1e-6, dropout: float = 0.0, rng=None, site: int = 0,
+                           dtype=None, workspace=None, out=None, stream=None):
+    """Gradients of mosa_residual_forward from its inputs and stats and the gradients dx_out (like x) and
+    dh (fp32 or bf16) of its results, either of which may be None.  Returns ({"dx", "dy", "dgate",
+    "dgamma_post", "dgamma_pre"}, workspace): dx like x, dy in the storage type, dgate [d] fp32 or [B,T,d]
+    in the storage type, dgamma_* [d] fp32; without the ones that the call has no input for (a norm
+    without gamma has a gamma of ones).  ``rng`` must hold what it held in the forward.  ``out`` may hold any of
+    them ("dx" may be dx_out)."""
+    try:
+        if _away(x, stream):
+            return _there(x, stream, mosa_residual_backward, x, y, stats, dx_out, dh, gate, gamma_post, gamma_pre,
+                          post_norm, pre_norm, sigmoid, scale, eps, dropout, rng, site, dtype, workspace, out)
+        torch = _b._torch()
+        f32 = torch.float32
+        dx, dy, dg, dgpost, dgpre = ((out.get("dx"), out.get("dy"), out.get("dgate"), out.get("dgamma_post"),
+                                      out.get("dgamma_pre")) if out else (None,) * 5)
+        post_norm, pre_norm, sigmoid, scale, eps, dropout, site = _options(post_norm, pre_norm, sigmoid, scale, eps,
+                                                                           dropout, site)
+        if not pre_norm:
+            dh = None
+        dt = _storage(dtype, gate, gamma_post, gamma_pre, x)
+        key = (7, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype, _sig(gate), _sig(gamma_post),
+               _sig(gamma_pre), post_norm, pre_norm, sigmoid, scale, eps, dropout, site, dt, _sig(rng),
+               stats.shape, stats.stride(), stats.dtype, _sig(dx_out), _sig(dh),
+               (_sig(dx), _sig(dy), _sig(dg), _sig(dgpost), _sig(dgpre)) if out else None)
+    except AttributeError:
+        _bad(("x", x), ("y", y), ("stats", stats), ("dx_out", dx_out), ("dh", dh), ("gate", gate),
+             ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng))
+    plan = _plans.get(key) or _keep(key, _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
+                                                        sigmoid, scale, eps, dropout, rng, site, dt, None, None, stats,
+                                                        (dx_out, dh, dx, dy, dg, dgpost, dgpre)))
+    dev = x.get_device()
+    if dev < 0:
+        _bad(("x", x))
+    _one_device(dev, ("y", y), ("stats", stats), ("dx_out", dx_out), ("dh", dh), ("gate", gate),
+                ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng), ("dx", dx), ("dy", dy),
+                ("dgate", dg), ("dgamma_post", dgpost), ("dgamma_pre", dgpre), ("workspace", workspace))
+    device, d = x.device, x.shape[2]
+    if dx is None:
+        dx = _new(x)
+    if dy is None:
+        dy = torch.empty(x.shape, dtype=dt, device=device)
+    g = {"dx": dx, "dy": dy}
+    if gate is None:
+        dg = None
+    else:
+        if dg is None:
+            dg = torch.empty(gate.shape, dtype=dt if len(gate.shape) == 3 else f32, device=device)
+        g["dgate"] = dg
+    if not post_norm:
+        dgpost = None
+    else:
+        if dgpost is None:
+            dgpost = torch.empty(d, dtype=f32, device=device)
+        g["dgamma_post"] = dgpost
+    if not pre_norm:
+        dgpre = None
+    else:
+        if dgpre is None:
+            dgpre = torch.empty(d, dtype=f32, device=device)
+        g["dgamma_pre"] = dgpre
+    workspace = _space(workspace, plan[1], device)
+    rc = _b.load().mosa_residual_backward(
+        plan[0], x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(gamma_post), _ptr(gamma_pre), _ptr(rng),
+        stats.data_ptr(), _ptr(dx_out), _ptr(dh), dx.data_ptr(), dy.data_ptr(), _ptr(dg), _ptr(dgpost), _ptr(dgpre),
+        workspace.data_ptr(), workspace.numel(), _b._stream(None))
+    if rc:
+        _b._check(rc, "mosa_residual_backward")
+    return g, workspace
+
+
+# ------------------------------------------------------------------ dropout
+
+def _dropout_plan(x, p, rng, site, y):
+    _rank(x, "x", 3)
+    _check_rng(rng, p)
+    s = MosaDropoutShape(*x.shape, _b._dtype_code(x), site, p, _rows(x, "x"), _result(y, "out y", x.shape, x.dtype))
+    return ctypes.byref(s), 0, s
+
+
+def mosa_dropout(x, p: float, rng, site: int = 0, out=None, stream=None):
+    """x [B,T,d] with each value dropped (0) with probability p, the others times 1/(1-p).  ``rng`` [2]
+    int64 on the GPU holds seed and offset, read when the call runs; ``site`` tells calls that share
+    it apart.  The same call on the gradient is the backward.  ``out`` may hold "y", x itself among them."""
+    try:
+        if _away(x, stream):
+            return _there(x, stream, mosa_dropout, x, p, rng, site, out)
+        _b._torch()
+        y = out.get("y") if out else None
+        p, site = float(p), _int(site, "site")
+        key = (8, x.shape, x.stride(), x.dtype, p, site, _sig(rng), _sig(y))
+    except AttributeError:
+        _bad(("x", x), ("rng", rng), ("out y", y))
+    plan = _plans.get(key) or _keep(key, _dropout_plan(x, p, rng, site, y))
+    dev = x.get_device()
+    if dev < 0:
+        _bad(("x", x))
+    _one_device(dev, ("rng", rng), ("out y", y))
+    if y is None:
+        y = _new(x)
+    rc = _b.load().mosa_dropout(plan[0], x.data_ptr(), _ptr(rng), y.data_ptr(), _b._stream(None))
+    if rc:
+        _b._check(rc, "mosa_dropout")
+    return y
+
+
+# -------------------------------------------------------- log probabilities
+
+def _logprob_plan(logits, targets, top, scale, results, back=None):
+    """results: (name, tensor, columns or 0, type) of [B,T] or [B,T,columns] tensors to be checked."""
+    torch = _b._torch_mod
+    _rank(logits, "logits", 3)
+    B, T, V = logits.shape
+    if targets is not None:
+        _b._want("targets", targets, (B, T))
+        if targets.dtype not in (torch.int32, torch.int64):
+            raise TypeError(f"targets must be int32 or int64, got {targets.dtype}")
+        if not targets.is_contiguous():
+            raise ValueError("targets must be contiguous")
+    for name, t, n, dtype in results:
+        _vector(t, name, (B, T, n) if n else (B, T), dtype)
+    s = MosaLogprobShape(B, T, V, _b._dtype_code(logits), 1 if targets is not None and targets.dtype == torch.int64 else 0,
+                         top, scale, _rows(logits, "logits"))
+    if back is not None:
+        s.dz = _result(back[0], "dlogits", logits.shape, logits.dtype)
+        return ctypes.byref(s), 0, s
+    return ctypes.byref(s), int(_b.load().mosa_token_logprobs_workspace_bytes(ctypes.byref(s))), s
+
+
+def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, workspace=None, out=None,
+                        stream=None):
+    """Log probabilities under softmax(scale * logits), logits [B,T,V] (scale: 1 / temperature).  Returns
+    ({"logp", "entropy", "lse", "top", "top_logp"}, workspace): logp [B,T] of the targets [B,T] (int32 or int64;
+    below 0: none, logp 0), entropy and lse [B,T], and with ``top`` > 0 (up to 32) the indices [B,T,top] int32
+    of the largest entries in falling order, ties by the lower index, and their log probabilities;
+    all fp32 but the indices.  Entries of -inf (or -2^90 and less) are ruled out.  ``out`` may hold any of
+    them."""
+    try:
+        if _away(logits, stream):
+            return _there(logits, stream, mosa_token_logprobs, logits, targets, top, scale, workspace, out)
+        torch = _b._torch()
+        f32 = torch.float32
+        logp, ent, lse, idx, tlp = ((out.get("logp"), out.get("entropy"), out.get("lse"), out.get("top"),
+                                     out.get("top_logp")) if out else (None,) * 5)
+        top, scale = _int(top, "top"), _float(scale)
+        key = (9, logits.shape, logits.stride(), logits.dtype, _sig(targets), top, scale,
+               (_sig(logp), _sig(ent), _sig(lse), _sig(idx), _sig(tlp)) if out else None)
+    except AttributeError:
+        _bad(("logits", logits), ("targets", targets))
+    plan = _plans.get(key) or _keep(key, _logprob_plan(
+        logits, targets, top, scale, [("logp", logp, 0, f32), ("entropy", ent, 0, f32), ("lse", lse, 0, f32),
+                                      ("top", idx, top, torch.int32), ("top_logp", tlp, top, f32)]))
+    dev = logits.get_device()
+    if dev < 0:
+        _bad(("logits", logits))
+    _one_device(dev, ("targets", targets), ("logp", logp), ("entropy", ent), ("lse", lse), ("top", idx),
+                ("top_logp", tlp), ("workspace", workspace))
+    device, lead = logits.device, logits.shape[:2]
+    r = {}
+    if targets is None:
+        logp = None
+    else:
+        r["logp"] = logp = _made(logp, lead, f32, device)
+    r["entropy"] = ent = _made(ent, lead, f32, device)
+    r["lse"] = lse = _made(lse, lead, f32, device)
+    if top > 0:
+        r["top"] = idx = _made(idx, (*lead, top), torch.int32, device)
+        r["top_logp"] = tlp = _made(tlp, (*lead, top), f32, device)
+    else:
+        idx = tlp = None
+    workspace = _space(workspace, plan[1], device)
+    rc = _b.load().mosa_token_logprobs(
+        plan[0], logits.data_ptr(), _ptr(targets), _ptr(logp), ent.data_ptr(), lse.data_ptr(), _ptr(idx), _ptr(tlp),
+        workspace.data_ptr(), workspace.numel(), _b._stream(None))
+    if rc:
+        _b._check(rc, "mosa_token_logprobs")
+    return r, workspace
+
+
+def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None, dentropy=None, dlse=None, top=None,
+                                 dtop_logp=None, scale: float = 1.0, out=None, stream=None):
+    """Gradient of the logits (like them) from mosa_token_logprobs' lse and entropy and the gradients dlogp,
+    dentropy, dlse [B,T] and dtop_logp [B,T,top] fp32 of its results, each None where there is none; ``top``:
+    the indices that it returned, read with dtop_logp.  ``out`` may hold "dlogits", logits itself among
+    them."""
+    try:
+        if _away(logits, stream):
+            return _there(logits, stream, mosa_token_logprobs_backward, logits, targets, lse, entropy, dlogp, dentropy,
+                          dlse, top, dtop_logp, scale, out)
+        torch = _b._torch()
+        f32 = torch.float32
+        dz = out.get("dlogits") if out else None
+        if dtop_logp is None:
+            top = None
+        scale = _float(scale)
+        key = (10, logits.shape, logits.stride(), logits.dtype, _sig(targets), lse.shape, lse.stride(), lse.dtype,
+               _sig(entropy), _sig(dlogp), _sig(dentropy), _sig(dlse), _sig(top), _sig(dtop_logp), scale, _sig(dz))
+    except AttributeError:
+        _bad(("logits", logits), ("lse", lse), ("targets", targets), ("entropy", entropy), ("dlogp", dlogp),
+             ("dentropy", dentropy), ("dlse", dlse), ("top", top), ("dtop_logp", dtop_logp), ("dlogits", dz))
+    plan = _plans.get(key)
+    if plan is None:
+        n = 0
+        if dtop_logp is not None:
+            if top is None:
+                raise TypeError("dtop_logp needs top, the indices of the forward")
+            _rank(top, "top", 3)
+            n = top.shape[2]
+            if n == 0:
+                raise ValueError("top must hold at least one index of each row")
+        if dlogp is not None and targets is None:
+            raise TypeError("dlogp needs targets")
+        if dentropy is not None and entropy is None:
+            raise TypeError("dentropy needs entropy, the forward's")
+        plan = _keep(key, _logprob_plan(
+            logits, targets, n, scale,
+            [("lse", lse, 0, f32), ("entropy", entropy, 0, f32), ("dlogp", dlogp, 0, f32), ("dentropy", dentropy, 0, f32),
+             ("dlse", dlse, 0, f32), ("top", top, n, torch.int32), ("dtop_logp", dtop_logp, n, f32)], (dz,)))
+    dev = logits.get_device()
+    if dev < 0:
+        _bad(("logits", logits))
+    _one_device(dev, ("targets", targets), ("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy),
+                ("dlse", dlse), ("top", top), ("dtop_logp", dtop_logp), ("dlogits", dz))
+    if dz is None:
+        dz = _new(logits)
+    rc = _b.load().mosa_token_logprobs_backward(
+        plan[0], logits.data_ptr(), _ptr(targets), lse.data_ptr(), _ptr(entropy), _ptr(top), _ptr(dlogp), _ptr(dentropy),
+        _ptr(dlse), _ptr(dtop_logp), dz.data_ptr(), _b._stream(None))
+    if rc:
+        _b._check(rc, "mosa_token_logprobs_backward")
+    return dz

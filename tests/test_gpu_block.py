@@ -1,0 +1,559 @@
+"""The block operators on the GPU against their definitions in 64 bits (bounds: _block_ref.py)."""
+import pytest
+import torch
+
+import paper_2505_00315_gb300 as mosa
+from _block_ref import keep_mask, logprobs, near, residual
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+NAN, INF = float("nan"), float("inf")
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def state(seed=5):
+    return torch.tensor([seed * 0x123456789ABCDE + 3, 2**40 + seed], dtype=torch.int64, device="cuda")
+
+
+def inputs(B, T, d, dt=BF, xt=None, yt=None, ht=None, gate="none", seed=0):
+    g = gen(seed)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")   # noqa: E731
+    xt, yt, ht = xt or dt, yt or dt, ht or dt
+    s = {"x": (2 * r(B, T, d)).to(xt), "y": (0.5 * r(B, T, d)).to(yt), "gamma_post": (1 + 0.3 * r(d)).to(dt),
+         "gamma_pre": (1 + 0.3 * r(d)).to(dt), "gate": None}
+    if gate != "none":
+        s["gate"] = r(d).to(dt) if gate == "channel" else r(B, T, d).to(dt)
+    return s, r(B, T, d).to(xt), r(B, T, d).to(ht)
+
+
+def check(s, dx_out, dh, bounds=residual, **kw):
+    x, h, stats = mosa.mosa_residual_forward(**s, **kw)
+    g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, **s, **kw)
+    torch.cuda.synchronize()
+    kw.pop("dtype", None)
+    want = bounds(**s, dx_out=dx_out, dh=dh, backward=True, **kw)
+    got = {"x": x, "h": h, **g}
+    assert {n for n, t in got.items() if t is not None} == set(want)
+    for n, (ref, bound) in want.items():
+        near(n, got[n], ref, bound)
+    return got
+
+
+SIZES = [(1, 1, 8), (2, 3, 1), (1, 5, 7), (3, 50, 64), (2, 77, 256), (2, 33, 264), (1, 40, 1001), (2, 64, 1024),
+         (1, 9, 2048), (2, 5, 4104), (1, 3, 8192), (1, 700, 96), (1, 2, 8191), (5, 400, 520)]
+
+
+@pytest.mark.parametrize("gate,sigmoid,p", [("none", False, 0.0), ("channel", False, 0.1), ("token", True, 0.3)])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B,T,d", SIZES)
+def test_residual_step(B, T, d, dt, gate, sigmoid, p):
+    s, dx_out, dh = inputs(B, T, d, dt, gate=gate, seed=d)
+    check(s, dx_out, dh, sigmoid=sigmoid, scale=0.7, dropout=p, rng=state(), site=2)
+
+
+@pytest.mark.parametrize("xt", [BF, F32])
+@pytest.mark.parametrize("yt", [BF, F32])
+@pytest.mark.parametrize("ht", [BF, F32])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_types_of_each_tensor(dt, xt, yt, ht):
+    s, dx_out, dh = inputs(2, 31, 520, dt, xt, yt, ht, gate="token", seed=1)
+    got = check(s, dx_out, dh, scale=-0.5, dropout=0.25, rng=state(), eps=1e-5)
+    assert got["x"].dtype == xt and got["dx"].dtype == xt and got["h"].dtype == dt and got["dy"].dtype == dt
+
+
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("pre", [True, False])
+@pytest.mark.parametrize("gate,sigmoid", [("none", True), ("channel", True), ("token", False)])
+def test_norms_and_gates_left_out(post, pre, gate, sigmoid):
+    for d in (200, 6000):
+        s, dx_out, dh = inputs(2, 30, d, gate=gate, seed=2)
+        check(s, dx_out, dh if pre else None, post_norm=post, pre_norm=pre, sigmoid=sigmoid, dropout=0.1, rng=state())
+
+
+def test_without_gammas_and_with_one_gradient():
+    s, dx_out, dh = inputs(2, 30, 320, seed=3)
+    s["gamma_post"] = s["gamma_pre"] = None
+    check(s, dx_out, dh)
+    check(s, None, dh)
+    check(s, dx_out, None)
+    got = check(s, None, None)
+    assert not any(t.any() for n, t in got.items() if n.startswith("d"))
+
+
+def test_strides_and_places():
+    """Rows out of wider tensors, sequences and tokens swapped, a repeated gate, tensors that start at any element;
+    results into places of the caller's, with what lies around them as it was."""
+    B, T, d = 3, 20, 136
+    s, dx_out, dh = inputs(B, T, d, gate="token", seed=4)
+    wide = torch.randn(B, T, 3 * d + 5, generator=gen(9), device="cuda").to(BF)
+    s["x"] = wide[..., 1:1 + d]
+    s["y"] = wide.flatten()[d:d + T * B * 2 * d].view(T, B, 2 * d).transpose(0, 1)[..., :d]
+    s["gate"] = s["gate"][:, :1].expand(B, T, d)
+    kw = dict(scale=0.5, dropout=0.2, rng=state(), site=-1)
+    want = residual(**s, dx_out=dx_out, dh=dh, backward=True, **kw)
+    room = {n: torch.full((B, T, d + 9), 7.0, device="cuda", dtype=BF) for n in ("x", "h", "dx", "dy", "dgate")}
+    out = {n: t[..., 3:3 + d] for n, t in room.items()}
+    x, h, stats = mosa.mosa_residual_forward(**s, out=out, **kw)
+    g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, out=out, **s, **kw)
+    assert x.data_ptr() == out["x"].data_ptr() and g["dgate"].data_ptr() == out["dgate"].data_ptr()
+    for n, (ref, bound) in want.items():
+        near(n, {"x": x, "h": h, **g}[n], ref, bound)
+    for n, t in room.items():
+        assert (t[..., :3] == 7).all() and (t[..., 3 + d:] == 7).all(), n
+
+
+def test_in_place():
+    s, dx_out, dh = inputs(4, 100, 1024, gate="channel", seed=5)
+    kw = dict(dropout=0.1, rng=state())
+    x, h, stats = mosa.mosa_residual_forward(**s, **kw)
+    g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, **s, **kw)
+    dxo = dx_out.clone()
+    g2, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dxo, dh=dh, out={"dx": dxo}, **s, **kw)
+    assert g2["dx"] is dxo and all(torch.equal(g[n], g2[n]) for n in g)
+    x2 = s["x"].clone()
+    got, h2, _ = mosa.mosa_residual_forward(**{**s, "x": x2}, out={"x": x2}, **kw)
+    assert got is x2 and torch.equal(x2, x) and torch.equal(h2, h)
+
+
+def test_the_same_bits_every_time_whatever_the_workspace_holds():
+    s, dx_out, dh = inputs(3, 777, 768, gate="channel", seed=6)
+    stats = mosa.mosa_residual_forward(**s)[2]
+    g, ws = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, **s)
+    first = {n: t.clone() for n, t in g.items()}
+    ws.fill_(0xFF)
+    for _ in range(3):
+        g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, workspace=ws, **s)
+        assert all(torch.equal(first[n], g[n]) for n in g)
+
+
+def test_dropped_values_do_not_count():
+    """Without a norm of y, a dropped NaN or infinity reaches nothing; a kept one only its row."""
+    B, T, d, p = 2, 6, 512, 0.5
+    s, dx_out, dh = inputs(B, T, d, F32, gate="token", seed=7)
+    rng = state(8)
+    keep = keep_mask(rng, 0, (B, T, d), p, "cuda")
+    clean = residual(**s, post_norm=False, dropout=p, rng=rng, dx_out=dx_out, dh=dh, backward=True)
+    s["y"] = torch.where(keep, s["y"], NAN)
+    s["gate"] = torch.where(keep, s["gate"], INF)
+    got = mosa.mosa_residual_forward(**s, post_norm=False, dropout=p, rng=rng)
+    g, _ = mosa.mosa_residual_backward(stats=got[2], dx_out=dx_out, dh=dh, **s, post_norm=False, dropout=p, rng=rng)
+    for n, t in {"x": got[0], "h": got[1], **g}.items():
+        near(n, t, *clean[n])
+    s["y"][1, 2, int(keep[1, 2].nonzero()[0])] = NAN
+    x, h, _ = mosa.mosa_residual_forward(**s, post_norm=False, dropout=p, rng=rng)
+    rows = torch.isnan(h).all(-1)
+    assert rows[1, 2] and int(rows.sum()) == 1 and int(torch.isnan(h).any(-1).sum()) == 1
+    assert int(torch.isnan(x).sum()) == 1
+
+
+def test_everything_and_nothing_dropped():
+    s, dx_out, dh = inputs(2, 20, 264, gate="channel", seed=8)
+    check(s, dx_out, dh, dropout=1.0, rng=state())
+    got = mosa.mosa_residual_forward(**s, dropout=1.0, rng=state())
+    assert torch.equal(got[0], s["x"])
+    a = mosa.mosa_residual_forward(**s, dropout=0.0, rng=state())
+    b = mosa.mosa_residual_forward(**s)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_zero_rows_and_large_values():
+    """A row of zeros (its norm is 0 / sqrt(eps)), rows whose squares are near the ends of fp32."""
+    s, dx_out, dh = inputs(1, 5, 300, F32, seed=9)
+    s["y"][0, 0] = 0
+    s["x"][0, 0] = 0
+    s["y"][0, 1] *= 1e15
+    s["x"][0, 2] *= 1e15
+    s["x"][0, 3] = -s["y"][0, 3]
+    check(s, dx_out, dh, post_norm=True)
+    check(s, dx_out, dh, post_norm=False)   # x + y of row 3: all zeros
+
+
+def test_gradients_against_differences():
+    """(f(v + t w) - f(v - t w)) / 2 t for every input in a random direction w.  f = sum of outputs times
+    upstream over n values, each off by u = 2^-24 or so of values around 2: 2^-23 sqrt(n) / t with t = 2^-7,
+    n = 4000, is 1e-3 of results around sqrt(n) = 60, beside the differences' own t^2 / 6 of some third
+    derivatives (about 1e-4 of them): within 2 % of the gradients' norm in that direction."""
+    B, T, d, t = 2, 8, 250, 2.0 ** -7
+    s, dx_out, dh = inputs(B, T, d, F32, gate="token", seed=10)
+    kw = dict(sigmoid=True, scale=0.6, dropout=0.2, rng=state())
+
+    def f(v):
+        x, h, _ = mosa.mosa_residual_forward(**v, **kw)
+        return float((x.double() * dx_out.double()).sum() + (h.double() * dh.double()).sum())
+
+    stats = mosa.mosa_residual_forward(**s, **kw)[2]
+    g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, **s, **kw)
+    for i, n in enumerate(("x", "y", "gate", "gamma_post", "gamma_pre")):
+        w = torch.randn(s[n].shape, generator=gen(100 + i), device="cuda")
+        want = float((g["d" + n].double() * w.double()).sum())
+        got = (f({**s, n: s[n] + t * w}) - f({**s, n: s[n] - t * w})) / (2 * t)
+        assert abs(got - want) <= 0.02 * float(g["d" + n].double().norm()), n
+
+
+# ------------------------------------------------------------------ dropout
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B,T,d", [(1, 1, 1), (2, 3, 7), (3, 100, 8), (2, 50, 40), (1, 33, 256), (2, 9, 1001),
+                                   (1, 4, 5000), (4, 300, 512), (1, 1, 70001)])
+def test_dropout(B, T, d, dt):
+    x, rng = inputs(B, T, d, dt, seed=11)[0]["x"], state()
+    for p, site in ((0.1, 0), (0.75, 2**31 - 1)):
+        y = mosa.mosa_dropout(x, p, rng, site=site)
+        keep = keep_mask(rng, site, x.shape, p, "cuda")
+        want = torch.where(keep, x.double() / (1 - p), 0.0)
+        assert y.dtype == dt and torch.equal(y == 0, want == 0)
+        near("y", y, want, 2.0 ** -23 * want.abs())   # 1/(1-p) in fp32, one product
+
+
+def test_dropout_ends_places_and_uses():
+    x, rng = inputs(2, 30, 136, seed=12)[0]["x"], state()
+    assert torch.equal(mosa.mosa_dropout(x, 0.0, rng), x) and torch.equal(mosa.mosa_dropout(x, 0.0, None), x)
+    assert not mosa.mosa_dropout(torch.full_like(x, NAN), 1.0, rng).any()
+    y = mosa.mosa_dropout(x, 0.3, rng, site=4)
+    assert not torch.equal(y, mosa.mosa_dropout(x, 0.3, rng, site=5))
+    # rows by other strides have the same words; in place
+    room = torch.full((30, 2, 140), 7.0, device="cuda", dtype=BF)
+    z = room.transpose(0, 1)[..., 1:137]
+    z.copy_(x)
+    got = mosa.mosa_dropout(z, 0.3, rng, site=4, out={"y": z})
+    assert got is z and torch.equal(z, y) and (room[..., 0] == 7).all() and (room[..., 137:] == 7).all()
+    # the residual step's own dropout is the same one
+    a = mosa.mosa_residual_forward(torch.zeros_like(x), x, post_norm=False, pre_norm=False, dropout=0.3, rng=rng, site=4)[0]
+    assert torch.equal(a, y)
+
+
+def test_replayed_graphs_see_new_words():
+    """A captured step reads the state when it runs."""
+    x, rng = inputs(2, 30, 512, seed=13)[0]["x"], state()
+    y = torch.empty_like(x)
+    mosa.mosa_dropout(x, 0.5, rng, out={"y": y})
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mosa.mosa_dropout(x, 0.5, rng, site=1, out={"y": y})
+        rng[1:] += 2
+    for i in range(3):
+        graph.replay()
+        now = torch.tensor([int(rng[0]), int(rng[1]) - 2], device="cuda")
+        assert torch.equal(y, mosa.mosa_dropout(x, 0.5, now, site=1)), i
+        assert torch.equal(y != 0, keep_mask(now, 1, x.shape, 0.5, "cuda") & (x != 0))
+
+
+# -------------------------------------------------------- log probabilities
+
+def logits_of(B, T, V, dt=BF, seed=0, spread=3.0):
+    return (spread * torch.randn(B, T, V, generator=gen(seed), device="cuda")).to(dt)
+
+
+def check_logprobs(z, targets=None, top=0, scale=1.0, up=("logp", "entropy", "lse", "top"), seed=0, **kw):
+    B, T, V = z.shape
+    r, _ = mosa.mosa_token_logprobs(z, targets, top=top, scale=scale, **kw)
+    g = {}
+    for i, n in enumerate(up):
+        if n == "top" and not top or n == "logp" and targets is None:
+            continue
+        shape = (B, T, top) if n == "top" else (B, T)
+        g["dtop" if n == "top" else "d" + n] = torch.randn(shape, generator=gen(50 + i), device="cuda")
+    want = logprobs(z, targets, top, scale, **g)
+    if g:
+        names = {"dtop_logp" if n == "dtop" else n: t for n, t in g.items()}
+        r["dlogits"] = mosa.mosa_token_logprobs_backward(z, targets, r["lse"], r["entropy"], top=r.get("top"), scale=scale,
+                                                         **names)
+    assert set(r) == set(want)
+    for n, (ref, bound) in want.items():
+        if n == "top":
+            bad = torch.isnan(r["lse"])[..., None]   # (unspecified, but in range)
+            assert torch.equal(torch.where(bad, 0, r[n]), torch.where(bad, 0, ref)), n
+            assert ((r[n] >= 0) & (r[n] < V)).all()
+        else:
+            near(n, r[n], ref, bound)
+    return r
+
+
+def targets_of(B, T, V, seed=0, dtype=torch.int64):
+    t = torch.randint(0, V, (B, T), generator=gen(seed), device="cuda")
+    t.view(-1)[::5] = -1
+    return t.to(dtype)
+
+
+LENGTHS = [1, 2, 7, 8, 9, 31, 100, 255, 257, 1000, 1024, 1025, 2048, 4095, 5001, 9000]
+
+
+@pytest.mark.parametrize("top", [0, 1, 5, 32])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("V", LENGTHS)
+def test_logprobs(V, dt, top):
+    z = logits_of(2, 13, V, dt, seed=V)
+    check_logprobs(z, targets_of(2, 13, V, dtype=torch.int32 if V % 2 else torch.int64), min(top, V), 0.8)
+
+
+@pytest.mark.parametrize("B,T,V,top", [(1, 1, 131072, 20), (8, 1, 131071, 32), (1, 3, 200003, 7), (3, 100, 20000, 9),
+                                       (2, 1500, 3000, 4), (1, 2500, 4099, 20), (1, 9000, 300, 3)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_rows_taken_by_warps_blocks_and_segments(B, T, V, top, dt):
+    z = logits_of(B, T, V, dt, seed=V)
+    check_logprobs(z, targets_of(B, T, V), top, 1.3)
+    check_logprobs(z, targets_of(B, T, V), 0, 1.0)
+
+
+@pytest.mark.parametrize("V", [50, 1500, 9000, 70000])
+def test_ties_rising_and_falling_rows(V):
+    """Equal values (the lowest index first), zeros of both signs, rows that rise (every value is a new best) and
+    fall, for one row, and for so many that each is a warp's."""
+    i = torch.arange(V, device="cuda").float()
+    rows = torch.stack([torch.zeros_like(i), torch.where(i % 2 == 0, 0.0, -0.0), i % 3, i * (8.0 / V), -i * (8.0 / V),
+                        torch.where(i == V - 1, 5.0, 1.0), torch.floor(i * (40.0 / V)) / 8])
+    for dt in (BF, F32):
+        for z in (rows[None].to(dt), rows.to(dt).repeat(400, 1)[None] if V < 9000 else rows[None, :1].to(dt)):
+            check_logprobs(z.contiguous(), targets_of(1, z.shape[1], V), 32)
+            check_logprobs(z.contiguous(), None, 1, up=())
+
+
+@pytest.mark.parametrize("V", [40, 3001, 40000])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_masks(V, dt):
+    """Rows with one entry, few or none left, by infinities and by the type's lowest value; targets ruled out."""
+    z = logits_of(1, 8, V, dt, seed=3)
+    low = torch.finfo(dt).min
+    z[0, 0] = -INF
+    z[0, 1] = low
+    z[0, 2, 1:] = -INF
+    z[0, 3, :-1] = low
+    z[0, 4, ::2] = -INF
+    z[0, 5, 5:] = low
+    z[0, 6, : V // 2] = -INF
+    z[0, 7, 1] = -INF
+    z[0, 7, 0] = low
+    t = torch.tensor([[3, 3, 0, 0, 1, 2, V - 1, 1]], device="cuda")
+    for top in (0, 7):
+        check_logprobs(z, t, top, 0.5)
+    r = mosa.mosa_token_logprobs(z, t, top=4)[0]
+    assert r["top"][0, 0].tolist() == [0, 1, 2, 3] and r["logp"][0, 0] == -INF and r["entropy"][0, 0] == 0
+    assert r["top"][0, 2].tolist() == [0, 1, 2, 3] and r["top_logp"][0, 2].tolist() == [0.0, -INF, -INF, -INF]
+
+
+@pytest.mark.parametrize("V", [40, 3001, 40000])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_not_numbers_stay_in_their_rows(V, dt):
+    z = logits_of(2, 8, V, dt, seed=4)
+    z[0, 1, V // 2] = NAN
+    z[0, 2, 3] = INF
+    z[0, 3] = NAN
+    z[0, 4, V - 1] = 1e30
+    z[0, 5, 0] = -NAN
+    z[0, 6] = INF
+    r = check_logprobs(z, targets_of(2, 8, V), 6)
+    assert torch.isfinite(r["dlogits"][1]).all() and torch.isfinite(r["logp"][1]).all()
+
+
+def test_targets_out_of_range():
+    z = logits_of(1, 6, 1000, seed=5)
+    for dtype in (torch.int32, torch.int64):
+        t = torch.tensor([[0, 999, 1000, -1, -100, 2**31 - 1]], device="cuda").to(dtype)
+        r = check_logprobs(z, t, 3)
+        assert torch.isnan(r["logp"][0, [2, 5]]).all() and (r["logp"][0, 3:5] == 0).all()
+    t = torch.tensor([[2**40, -2**40, 2**32 + 5, 5, 2**63 - 1, -2**63]], device="cuda")
+    r = check_logprobs(z, t, 0)
+    assert torch.isnan(r["logp"][0, [0, 2, 4]]).all() and (r["logp"][0, [1, 5]] == 0).all()
+
+
+def test_rows_without_gradients_and_single_gradients():
+    z = logits_of(2, 10, 3000, seed=6)
+    z[0, 4, 7] = NAN
+    t = targets_of(2, 10, 3000)
+    r, _ = mosa.mosa_token_logprobs(z, t, top=3)
+    up = torch.randn(2, 10, device="cuda")
+    up[0, 4] = up[1, 3] = 0
+    dz = mosa.mosa_token_logprobs_backward(z, t, r["lse"], dlogp=up)
+    assert not dz[0, 4].any() and not dz[1, 3].any() and not dz[t < 0].any() and dz[1, 4].any()
+    for n in ("logp", "entropy", "lse", "top"):
+        check_logprobs(logits_of(2, 10, 3000, seed=7), t, 3, up=(n,))
+    dz = mosa.mosa_token_logprobs_backward(z, None, r["lse"])
+    assert not dz.any()
+
+
+def test_the_same_alternative_twice():
+    z = logits_of(1, 2, 2000, F32, seed=8)
+    r, _ = mosa.mosa_token_logprobs(z, top=4)
+    idx = torch.tensor([[[7, 9, 7, 7], [3, -1, 2000, 3]]], dtype=torch.int32, device="cuda")
+    g = torch.randn(1, 2, 4, device="cuda")
+    t = torch.tensor([[9, 3]], device="cuda")
+    up = torch.tensor([[0.5, -1.5]], device="cuda")
+    dz = mosa.mosa_token_logprobs_backward(z, t, r["lse"], dlogp=up, top=idx, dtop_logp=g)
+    p = torch.softmax(z.double(), -1)
+    own = torch.zeros_like(p)
+    own.scatter_add_(-1, t[..., None], up.double()[..., None])
+    ok = (idx >= 0) & (idx < 2000)
+    own.scatter_add_(-1, torch.where(ok, idx, 0).long(), torch.where(ok, g, 0.0).double())
+    G = own.sum(-1, keepdim=True)
+    # p within 2^-17 (2000 / 32 additions, values below 16), sums of five terms
+    near("dlogits", dz, own - p * G, 2.0 ** -16 * (own.abs() + p * (g.abs().sum(-1, keepdim=True) + 1.5)))
+
+
+def test_logprobs_in_place_places_and_streams():
+    B, T, V = 2, 9, 2001
+    room = torch.full((T, B, V + 11), 7.0, device="cuda", dtype=BF)
+    z = room.transpose(0, 1)[..., 5:5 + V]
+    z.copy_(logits_of(B, T, V, seed=9))
+    t = targets_of(B, T, V)
+    a = check_logprobs(z, t, 5)
+    b = check_logprobs(z.contiguous(), t, 5)
+    assert all(torch.equal(a[n], b[n]) for n in ("top", "dlogits"))
+    up = torch.randn(B, T, device="cuda")
+    want = mosa.mosa_token_logprobs_backward(z, t, a["lse"], dlogp=up)
+    got = mosa.mosa_token_logprobs_backward(z, t, a["lse"], dlogp=up, out={"dlogits": z})
+    assert got is z and torch.equal(z, want)
+    assert (room[..., :5] == 7).all() and (room[..., 5 + V:] == 7).all()
+
+
+def test_logprobs_for_temperatures_and_large_logits():
+    z = logits_of(1, 20, 3000, F32, seed=10)
+    for scale in (2.0 ** -20, 0.01, 30.0):
+        check_logprobs(z, targets_of(1, 20, 3000), 4, scale)
+    check_logprobs(z * 1e3 + 1e4, targets_of(1, 20, 3000), 4)
+    check_logprobs(z * 1e20, targets_of(1, 20, 3000), 4)
+
+
+def test_logits_past_32_bits():
+    """More than 2^32 elements: the last rows."""
+    B, T, V = 1, 33000, 131072
+    z = torch.empty(B, T, V, device="cuda", dtype=BF)
+    z[0, -40:] = logits_of(1, 40, V, seed=11)[0]
+    z[0, :-40] = 0
+    t = torch.full((B, T), V - 1, device="cuda")
+    r, _ = mosa.mosa_token_logprobs(z, t, top=3)
+    up = torch.zeros(B, T, device="cuda")
+    up[0, -40:] = 1.0
+    dz = mosa.mosa_token_logprobs_backward(z, t, r["lse"], dlogp=up)
+    want = logprobs(z[:, -40:], t[:, -40:], 3, dlogp=up[:, -40:])
+    assert torch.equal(r["top"][:, -40:], want["top"][0]) and torch.equal(r["top"][0, 0].cpu(), torch.arange(3).int())
+    for n, v in (("logp", r["logp"][:, -40:]), ("dlogits", dz[:, -40:])):
+        near(n, v, *want[n])
+    assert not dz[0, :-40].any()
+
+
+def test_rows_past_32_bits():
+    """A stream whose rows lie further than 2^32 elements apart."""
+    room = torch.zeros(2**32 + 4096, device="cuda", dtype=BF)
+    s, dx_out, dh = inputs(1, 3, 1024, seed=14)
+    x = room.as_strided((1, 3, 1024), (0, 2**31 + 512, 1))
+    x.copy_(s["x"])
+    a = mosa.mosa_residual_forward(**s, dropout=0.1, rng=state())
+    b = mosa.mosa_residual_forward(**{**s, "x": x}, dropout=0.1, rng=state(), out={"x": x})
+    assert torch.equal(a[1], b[1]) and torch.equal(a[0], x)
+    assert torch.equal(mosa.mosa_dropout(x, 0.4, state()), mosa.mosa_dropout(a[0], 0.4, state()))
+
+
+# ------------------------------------------------------------------ together
+
+def block_step(m, tokens, rng, stream=None):
+    """A layer of MoSA heads between two residual steps, then the loss: all results of one training step.
+    With m["still"], (Y, dX), those take the place of the layer, which adds up in an order that changes and captures
+    graphs of its own, and the head is a product by values, not by a matrix: the same bits every time."""
+    kw = dict(dropout=0.1, rng=rng, stream=stream)
+    still = m.get("still")
+    x0, W, k = m["x"], m["W"], m["k"]
+    o = {}
+    x1, h1, s1 = mosa.mosa_residual_forward(x0, m["y0"], gamma_post=m["a"], gamma_pre=m["b"], site=0, **kw)
+    if still:
+        Y = still[0]
+    else:
+        Y, I, r, _, ws = mosa.mosa_forward(h1, *W, k, stream=stream)
+    x2, h2, s2 = mosa.mosa_residual_forward(x1, Y, gate=m["gate"], gamma_post=m["a"], gamma_pre=m["b"], site=1, **kw)
+    logits = h2 * m["e"] if still else h2 @ m["E"]
+    o, _ = mosa.mosa_token_logprobs(logits, tokens, top=3, stream=stream)
+    up = torch.full(tokens.shape, -1.0 / tokens.numel(), device="cuda")
+    dz = mosa.mosa_token_logprobs_backward(logits, tokens, o["lse"], dlogp=up, stream=stream)
+    dh2 = dz * m["e"] if still else dz @ m["E"].T
+    g2, _ = mosa.mosa_residual_backward(x1, Y, s2, None, dh2, gate=m["gate"], gamma_post=m["a"], gamma_pre=m["b"], site=1,
+                                        **kw)
+    dX = still[1] if still else mosa.mosa_backward(h1, *W, I, r, g2["dy"], ws, stream=stream)["dX"]
+    g1, _ = mosa.mosa_residual_backward(x0, m["y0"], s1, g2["dx"], dX, gamma_post=m["a"], gamma_pre=m["b"], site=0,
+                                        **kw)
+    return {**o, **{"2" + n: t for n, t in g2.items()}, **{"1" + n: t for n, t in g1.items()}, "x2": x2,
+            "dz": dz}
+
+
+def model(B=2, T=128, d=256, V=500, seed=20):
+    r = lambda *s: torch.randn(s, generator=gen(seed + len(s)), device="cuda")   # noqa: E731
+    H, hp = 4, 64
+    W = [(r(*s) * d ** -0.5).to(BF) for s in ((d, H), (H, d, hp), (H, d, hp), (H, d, hp), (H, hp, d))]
+    return {"x": r(B, T, d).to(BF), "y0": r(B, T, d).to(BF), "W": W, "k": 32, "a": (1 + 0.1 * r(d)).to(BF),
+            "b": (1 + 0.2 * r(d)).to(BF), "gate": r(d).to(BF), "E": (r(d, V) * d ** -0.5).to(BF)}
+
+
+def test_a_layer_between_two_steps():
+    """Around the MoSA heads, against the same in 64 bits by autograd (heads taken as they came: the layer is
+    tested elsewhere): outputs in bf16 go through four more roundings (2^-8 each at most) and a layer within
+    2e-2; the loss's gradients stay within 5 % of their norm."""
+    m, rng = model(), state(3)
+    tokens = torch.randint(0, 500, (2, 128), generator=gen(1), device="cuda")
+    got = block_step(m, tokens, rng)
+    torch.cuda.synchronize()
+    one = residual(m["x"], m["y0"], gamma_post=m["a"], gamma_pre=m["b"], dropout=0.1, rng=rng, site=0)
+    h1 = one["h"][0].to(BF)
+    Y = mosa.mosa_forward(h1, *m["W"], m["k"])[0]
+    x1, Yd, gate = one["x"][0], Y.double().requires_grad_(), m["gate"].double().requires_grad_()
+    keep = keep_mask(rng, 1, Y.shape, 0.1, "cuda").double() / 0.9
+    n = Yd / torch.sqrt((Yd * Yd).mean(-1, keepdim=True) + 1e-6) * m["a"].double()
+    x2 = x1 + keep * gate * n
+    h2 = x2 / torch.sqrt((x2 * x2).mean(-1, keepdim=True) + 1e-6) * m["b"].double()
+    lp = torch.log_softmax(h2 @ m["E"].double(), -1).gather(-1, tokens[..., None])[..., 0]
+    dY, dgate = torch.autograd.grad(-lp.mean(), (Yd, gate))
+    far = lambda a, b: float((a.double() - b).norm() / b.norm())   # noqa: E731
+    assert far(got["logp"], lp.detach()) < 0.05 and far(got["x2"], x2.detach()) < 0.05
+    assert far(got["2dy"], dY) < 0.05 and far(got["2dgate"], dgate) < 0.05
+
+
+def test_streams_and_graphs():
+    """The whole step for another stream, while the current one is busy, and captured and replayed."""
+    m, rng = model(seed=30), state(4)
+    r = lambda *n: torch.randn(n, generator=gen(31 + len(n)), device="cuda")   # noqa: E731
+    m["still"], m["e"] = (r(2, 128, 256), r(2, 128, 256)), r(256).to(BF)
+    tokens = torch.randint(0, 256, (2, 128), generator=gen(1), device="cuda")
+    keep = {n: t.clone() for n, t in block_step(m, tokens, rng).items()}
+
+    def same(got):
+        for n, t in keep.items():
+            assert torch.equal(got[n], t), n
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        same(block_step(m, tokens, rng))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            got = block_step(m, tokens, rng)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        same(got)
+
+
+def test_a_call_for_a_stream_is_not_held_up():
+    s, dx_out, dh = inputs(2, 100, 512, seed=15)
+    z, t = logits_of(1, 2, 100000, seed=16), targets_of(1, 2, 100000)
+
+    def calls(stream):
+        x, h, stats = mosa.mosa_residual_forward(**s, stream=stream)
+        g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, stream=stream, **s)
+        y = mosa.mosa_dropout(x, 0.1, rng, stream=stream)
+        r, _ = mosa.mosa_token_logprobs(z, t, top=3, stream=stream)
+        dz = mosa.mosa_token_logprobs_backward(z, t, r["lse"], dlogp=up, stream=stream)
+        return [x, h, y, *g.values(), *r.values(), dz]
+
+    up, rng = z[..., 0].float().contiguous(), state()
+    want = calls(None)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    got = calls(other)
+    other.synchronize()
+    assert not torch.cuda.current_stream().query()     # (0.1 s: still asleep)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
