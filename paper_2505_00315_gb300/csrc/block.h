@@ -39,6 +39,7 @@ struct Vec {
 struct Residual {
     int B, T, d;
     int post, pre, gate, sigmoid;
+    int storage_wide;      // gammas, gate, h, dy and a gate's gradient are fp32
     float scale, eps;
     Drop drop;
     Rows x, y, g;          // inputs; g: a gate per token

@@ -50,6 +50,7 @@ mosa_status check_residual(const mosa_residual_shape *s, bool backward, Residual
     r->pre = s->pre_norm;
     r->gate = s->gate;
     r->sigmoid = s->sigmoid;
+    r->storage_wide = s->dtype == MOSA_F32;
     r->scale = s->scale;
     r->eps = s->eps;
     const bool token = s->gate == MOSA_GATE_TOKEN;

@@ -21,6 +21,7 @@
 
 #include "block.h"
 #include "launch.h"
+#include "pairs.cuh"
 #include "profile.h"
 
 namespace mosa {
@@ -49,39 +50,6 @@ struct Args {
     int units;          // backward: warps of a row
 };
 
-struct F2 {
-    float x, y;
-};
-__device__ __forceinline__ unsigned long long two(float x, float y) {
-    unsigned long long r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ F2 of_two(unsigned long long v) {
-    F2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
-    unsigned long long r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
-    unsigned long long r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ float pow2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // The larger one; a NaN stays.
 __device__ __forceinline__ float max_nan(float a, float b) {
     float y;
@@ -98,9 +66,6 @@ __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
     return y;
 }
-__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
 // 16 bytes of a row: eight bf16 or four fp32 values.
 struct Piece {
     uint32_t w[4];
@@ -304,9 +269,9 @@ __global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const __grid_const
     const int from = (int)((long long)steps * share / shares), to = (int)((long long)steps * (share + 1) / shares);
 
     float m = kLeast;
-    unsigned long long s = 0, sum_t = 0;   // pairs of sums
+    Pair s = 0, sum_t = 0;   // pairs of sums
     Best best;
-    const unsigned long long c2 = two(p.c, p.c);
+    const Pair c2 = both(p.c);
     Piece cur[kVecs];
 #pragma unroll
     for (int u = 0; u < kVecs; ++u)
@@ -356,15 +321,15 @@ __global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const __grid_const
         if (here > m) {   // (false for a NaN)
             const float by = fmaxf((m - here) * p.c, -1000.f), f = pow2(by);
             m = here;
-            sum_t = mul2(two(f, f), fma2(s, two(by, by), sum_t));
-            s = mul2(two(f, f), s);
+            sum_t = mul2(both(f), fma2(s, both(by), sum_t));
+            s = mul2(both(f), s);
         }
-        const unsigned long long minus = two(-m, -m);
+        const Pair minus = both(-m);
 #pragma unroll
         for (int u = 0; u < kVecs; ++u) {
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
-                unsigned long long a;
+                Pair a;
                 if (kWide) {
                     a = two(max_nan(__uint_as_float(cur[u].w[e]), kLeast), max_nan(__uint_as_float(cur[u].w[e + 1]), kLeast));
                 } else {
@@ -373,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const __grid_const
                 }
                 a = mul2(add2(a, minus), c2);
                 const F2 x = of_two(a);
-                const unsigned long long ex = two(pow2(x.x), pow2(x.y));
+                const Pair ex = two(pow2(x.x), pow2(x.y));
                 s = add2(s, ex);
                 sum_t = fma2(ex, a, sum_t);
             }
@@ -421,12 +386,6 @@ __global__ void __launch_bounds__(kThreads) logprob_join_kernel(const __grid_con
 }
 
 // ------------------------------------------------------------------ backward
-
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    uint32_t w;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
-    return w;
-}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -495,8 +454,8 @@ __global__ void __launch_bounds__(kThreads) logprob_bwd_kernel(const __grid_cons
             return pow2(b) * fmaf(B, b, A);
         };
         const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(z.p)) & 15) == 0;
-        const unsigned long long scale2 = two(l.scale, l.scale), minus = two(-ref, -ref), to2 = two(kLog2e, kLog2e);
-        const unsigned long long A2 = two(A, A), B2 = two(B, B);
+        const Pair scale2 = both(l.scale), minus = both(-ref), to2 = both(kLog2e);
+        const Pair A2 = both(A), B2 = both(B);
         Piece cur[kVecs];
 #pragma unroll
         for (int u = 0; u < kVecs; ++u)
@@ -512,7 +471,7 @@ __global__ void __launch_bounds__(kThreads) logprob_bwd_kernel(const __grid_cons
                 if (!zero) {
 #pragma unroll
                     for (int e = 0; e < E; e += 2) {
-                        unsigned long long a;
+                        Pair a;
                         if (kWide) {
                             a = two(max_nan(__uint_as_float(cur[u].w[e]), leastw), max_nan(__uint_as_float(cur[u].w[e + 1]), leastw));
                         } else {
