@@ -498,7 +498,8 @@ mosa_status mosa_residual_backward(const mosa_residual_shape *shape, const void 
                                    void *workspace, size_t workspace_bytes, void *stream);
 
 /* Dropout: y = keep/(1-p) x for x [B,T,d], y in the same dtype, which may be x itself.  The same
- * call on dy is its backward. */
+ * call on dy is its backward.  Sizes: d < 2^31 - 2^16 and B*T*(d/256 + 1) < 2^31 (else
+ * MOSA_ERR_UNSUPPORTED). */
 typedef struct {
     int32_t B, T, d;
     int32_t dtype;

@@ -52,11 +52,6 @@ def declare(L) -> None:
 # Calls make and look for everything on the current device and its current stream; one whose tensors lie on
 # another device, or that names a stream, is made again in that one's place.
 
-def _away(t, stream):
-    """Whether the call has to be made again elsewhere: for a stream, or on t's device."""
-    return stream is not None or (t.is_cuda and t.get_device() != _b._torch()._C._cuda_getDevice())
-
-
 def _there(t, stream, call, *args):
     """The call on ``stream``, or on the current stream of t's device."""
     cuda = _b._torch().cuda
@@ -71,11 +66,17 @@ def _there(t, stream, call, *args):
         return call(*args)
 
 
-def _one_device(dev, *named):
-    """Every tensor lies on device ``dev`` (a number; -1 stands for the CPU)."""
+def _all_on(dev, *ts):
+    return all(t is None or t.get_device() == dev for t in ts)
+
+
+def _elsewhere(dev, *named):
+    """Says which tensor does not lie on device ``dev`` (a number; below 0: the CPU)."""
+    for name, t in named:
+        if t is not None and not t.is_cuda:
+            _bad((name, t))
     for name, t in named:
         if t is not None and t.get_device() != dev:
-            _bad((name, t)) if not t.is_cuda else None
             raise ValueError(f"{name} must be on the device of the other tensors")
 
 
@@ -132,6 +133,7 @@ def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmo
     for name, t in (("x", x), ("y", y)):
         _rank(t, name, 3)
     B, T, d = x.shape
+    dtype = _storage(dtype, gate, gamma_post, gamma_pre, x)
     code = {torch.float32: _b.MOSA_F32, torch.bfloat16: _b.MOSA_BF16}
     if dtype not in code:
         raise TypeError(f"unsupported storage dtype {dtype} (float32 or bfloat16)")
@@ -139,7 +141,7 @@ def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmo
     if gate is not None:
         kind = GATE_TOKEN if len(gate.shape) == 3 else GATE_CHANNEL
     s = MosaResidualShape(B, T, d, code[dtype], _b._dtype_code(x), _b._dtype_code(y), code[dtype],
-                          1 if post_norm else 0, 1 if pre_norm else 0, kind, 1 if sigmoid else 0, site, scale,
+                          1 if post_norm else 0, 1 if pre_norm else 0, kind, 1 if sigmoid else 0, _int(site, "site"), scale,
                           eps, dropout, _rows(x, "x"), _rows(y, "y", x.shape))
     _vector(gamma_post, "gamma_post", (d,), dtype)
     _vector(gamma_pre, "gamma_pre", (d,), dtype)
@@ -168,7 +170,7 @@ def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmo
         _vector(dgpost, "dgamma_post", (d,), torch.float32)
         _vector(dgpre, "dgamma_pre", (d,), torch.float32)
         need = int(_b.load().mosa_residual_workspace_bytes(ctypes.byref(s)))
-    return ctypes.byref(s), need, s
+    return ctypes.byref(s), need, s, dtype
 
 
 def _options(post_norm, pre_norm, sigmoid, scale, eps, dropout, site):
@@ -189,37 +191,43 @@ def mosa_residual_forward(x, y, gate=None, gamma_post=None, gamma_pre=None, post
     type.  ``rng`` [2] int64 on the GPU holds seed and offset, read when the call runs; ``site`` tells
     calls that share it apart.  ``out`` may hold "x" (x itself where no backward follows), "h" and "stats"."""
     try:
-        if _away(x, stream):
+        dev = x.get_device()
+        if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):
             return _there(x, stream, mosa_residual_forward, x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
                           sigmoid, scale, eps, dropout, rng, site, dtype, out)
         torch = _b._torch()
         xo, h, stats = (out.get("x"), out.get("h"), out.get("stats")) if out else (None, None, None)
-        post_norm, pre_norm, sigmoid, scale, eps, dropout, site = _options(post_norm, pre_norm, sigmoid, scale, eps,
-                                                                           dropout, site)
-        dt = _storage(dtype, gate, gamma_post, gamma_pre, x)
+        if not (type(scale) is type(eps) is type(dropout) is float and type(site) is int
+                and type(post_norm) is type(pre_norm) is type(sigmoid) is bool):
+            post_norm, pre_norm, sigmoid, scale, eps, dropout, site = _options(post_norm, pre_norm, sigmoid, scale, eps,
+                                                                               dropout, site)
         key = (6, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype, _sig(gate), _sig(gamma_post),
-               _sig(gamma_pre), post_norm, pre_norm, sigmoid, scale, eps, dropout, site, dt, _sig(rng),
+               _sig(gamma_pre), post_norm, pre_norm, sigmoid, scale, eps, dropout, site, dtype, _sig(rng),
                (_sig(xo), _sig(h), _sig(stats)) if out else None)
     except AttributeError:
         _bad(("x", x), ("y", y), ("gate", gate), ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng))
     plan = _plans.get(key) or _keep(key, _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
-                                                        sigmoid, scale, eps, dropout, rng, site, dt, xo, h, stats))
-    dev = x.get_device()
-    if dev < 0:
-        _bad(("x", x))
-    _one_device(dev, ("y", y), ("gate", gate), ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng),
-                ("out x", xo), ("out h", h), ("stats", stats))
+                                                        sigmoid, scale, eps, dropout, rng, site, dtype, xo, h, stats))
+    if not (dev >= 0 and y.get_device() == dev and (gate is None or gate.get_device() == dev)
+            and (gamma_post is None or gamma_post.get_device() == dev)
+            and (gamma_pre is None or gamma_pre.get_device() == dev) and (rng is None or rng.get_device() == dev)
+            and (out is None or _all_on(dev, xo, h, stats))):
+        _elsewhere(dev, ("x", x), ("y", y), ("gate", gate), ("gamma_post", gamma_post), ("gamma_pre", gamma_pre),
+                   ("rng", rng), ("out x", xo), ("out h", h), ("stats", stats))
+    dt = plan[3]
     if xo is None:
         xo = _new(x)
     if not pre_norm:
         h = None
     elif h is None:
-        h = torch.empty(x.shape, dtype=dt, device=x.device)
+        h = _new(x) if dt is x.dtype else torch.empty(x.shape, dtype=dt, device=x.device)
     if stats is None:
-        stats = torch.empty((2, x.shape[0], x.shape[1]), dtype=torch.float32, device=x.device)
+        stats = torch.empty((2, *x.shape[:2]), dtype=torch.float32, device=x.device)
     rc = _b.load().mosa_residual_forward(
-        plan[0], x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(gamma_post), _ptr(gamma_pre), _ptr(rng),
-        xo.data_ptr(), _ptr(h), stats.data_ptr(), _b._stream(None))
+        plan[0], x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
+        None if gamma_post is None else gamma_post.data_ptr(), None if gamma_pre is None else gamma_pre.data_ptr(),
+        None if rng is None else rng.data_ptr(), xo.data_ptr(), None if h is None else h.data_ptr(),
+        stats.data_ptr(), _b._stream(None))
     if rc:
         _b._check(rc, "mosa_residual_forward")
     return xo, h, stats
@@ -236,39 +244,44 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
     without gamma has a gamma of ones).  ``rng`` must hold what it held in the forward.  ``out`` may hold any of
     them ("dx" may be dx_out)."""
     try:
-        if _away(x, stream):
+        dev = x.get_device()
+        if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):
             return _there(x, stream, mosa_residual_backward, x, y, stats, dx_out, dh, gate, gamma_post, gamma_pre,
                           post_norm, pre_norm, sigmoid, scale, eps, dropout, rng, site, dtype, workspace, out)
         torch = _b._torch()
         f32 = torch.float32
         dx, dy, dg, dgpost, dgpre = ((out.get("dx"), out.get("dy"), out.get("dgate"), out.get("dgamma_post"),
                                       out.get("dgamma_pre")) if out else (None,) * 5)
-        post_norm, pre_norm, sigmoid, scale, eps, dropout, site = _options(post_norm, pre_norm, sigmoid, scale, eps,
-                                                                           dropout, site)
+        if not (type(scale) is type(eps) is type(dropout) is float and type(site) is int
+                and type(post_norm) is type(pre_norm) is type(sigmoid) is bool):
+            post_norm, pre_norm, sigmoid, scale, eps, dropout, site = _options(post_norm, pre_norm, sigmoid, scale, eps,
+                                                                               dropout, site)
         if not pre_norm:
             dh = None
-        dt = _storage(dtype, gate, gamma_post, gamma_pre, x)
         key = (7, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype, _sig(gate), _sig(gamma_post),
-               _sig(gamma_pre), post_norm, pre_norm, sigmoid, scale, eps, dropout, site, dt, _sig(rng),
+               _sig(gamma_pre), post_norm, pre_norm, sigmoid, scale, eps, dropout, site, dtype, _sig(rng),
                stats.shape, stats.stride(), stats.dtype, _sig(dx_out), _sig(dh),
                (_sig(dx), _sig(dy), _sig(dg), _sig(dgpost), _sig(dgpre)) if out else None)
     except AttributeError:
         _bad(("x", x), ("y", y), ("stats", stats), ("dx_out", dx_out), ("dh", dh), ("gate", gate),
              ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng))
     plan = _plans.get(key) or _keep(key, _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
-                                                        sigmoid, scale, eps, dropout, rng, site, dt, None, None, stats,
+                                                        sigmoid, scale, eps, dropout, rng, site, dtype, None, None, stats,
                                                         (dx_out, dh, dx, dy, dg, dgpost, dgpre)))
-    dev = x.get_device()
-    if dev < 0:
-        _bad(("x", x))
-    _one_device(dev, ("y", y), ("stats", stats), ("dx_out", dx_out), ("dh", dh), ("gate", gate),
-                ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng), ("dx", dx), ("dy", dy),
-                ("dgate", dg), ("dgamma_post", dgpost), ("dgamma_pre", dgpre), ("workspace", workspace))
-    device, d = x.device, x.shape[2]
+    if not (dev >= 0 and y.get_device() == dev and stats.get_device() == dev
+            and (dx_out is None or dx_out.get_device() == dev) and (dh is None or dh.get_device() == dev)
+            and (gate is None or gate.get_device() == dev) and (gamma_post is None or gamma_post.get_device() == dev)
+            and (gamma_pre is None or gamma_pre.get_device() == dev) and (rng is None or rng.get_device() == dev)
+            and (workspace is None or workspace.get_device() == dev)
+            and (out is None or _all_on(dev, dx, dy, dg, dgpost, dgpre))):
+        _elsewhere(dev, ("x", x), ("y", y), ("stats", stats), ("dx_out", dx_out), ("dh", dh), ("gate", gate),
+                   ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng), ("workspace", workspace),
+                   ("dx", dx), ("dy", dy), ("dgate", dg), ("dgamma_post", dgpost), ("dgamma_pre", dgpre))
+    device, shape, dt = x.device, x.shape, plan[3]
     if dx is None:
         dx = _new(x)
     if dy is None:
-        dy = torch.empty(x.shape, dtype=dt, device=device)
+        dy = _new(x) if dt is x.dtype else torch.empty(shape, dtype=dt, device=device)
     g = {"dx": dx, "dy": dy}
     if gate is None:
         dg = None
@@ -279,19 +292,18 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
     if not post_norm:
         dgpost = None
     else:
-        if dgpost is None:
-            dgpost = torch.empty(d, dtype=f32, device=device)
-        g["dgamma_post"] = dgpost
+        g["dgamma_post"] = dgpost = torch.empty(shape[2], dtype=f32, device=device) if dgpost is None else dgpost
     if not pre_norm:
         dgpre = None
     else:
-        if dgpre is None:
-            dgpre = torch.empty(d, dtype=f32, device=device)
-        g["dgamma_pre"] = dgpre
+        g["dgamma_pre"] = dgpre = torch.empty(shape[2], dtype=f32, device=device) if dgpre is None else dgpre
     workspace = _space(workspace, plan[1], device)
     rc = _b.load().mosa_residual_backward(
-        plan[0], x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(gamma_post), _ptr(gamma_pre), _ptr(rng),
-        stats.data_ptr(), _ptr(dx_out), _ptr(dh), dx.data_ptr(), dy.data_ptr(), _ptr(dg), _ptr(dgpost), _ptr(dgpre),
+        plan[0], x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
+        None if gamma_post is None else gamma_post.data_ptr(), None if gamma_pre is None else gamma_pre.data_ptr(),
+        None if rng is None else rng.data_ptr(), stats.data_ptr(), None if dx_out is None else dx_out.data_ptr(),
+        None if dh is None else dh.data_ptr(), dx.data_ptr(), dy.data_ptr(), None if dg is None else dg.data_ptr(),
+        None if dgpost is None else dgpost.data_ptr(), None if dgpre is None else dgpre.data_ptr(),
         workspace.data_ptr(), workspace.numel(), _b._stream(None))
     if rc:
         _b._check(rc, "mosa_residual_backward")
@@ -303,7 +315,7 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
 def _dropout_plan(x, p, rng, site, y):
     _rank(x, "x", 3)
     _check_rng(rng, p)
-    s = MosaDropoutShape(*x.shape, _b._dtype_code(x), site, p, _rows(x, "x"), _result(y, "out y", x.shape, x.dtype))
+    s = MosaDropoutShape(*x.shape, _b._dtype_code(x), _int(site, "site"), p, _rows(x, "x"), _result(y, "out y", x.shape, x.dtype))
     return ctypes.byref(s), 0, s
 
 
@@ -312,22 +324,23 @@ def mosa_dropout(x, p: float, rng, site: int = 0, out=None, stream=None):
     int64 on the GPU holds seed and offset, read when the call runs; ``site`` tells calls that share
     it apart.  The same call on the gradient is the backward.  ``out`` may hold "y", x itself among them."""
     try:
-        if _away(x, stream):
+        dev = x.get_device()
+        if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):
             return _there(x, stream, mosa_dropout, x, p, rng, site, out)
         _b._torch()
         y = out.get("y") if out else None
-        p, site = float(p), _int(site, "site")
+        if not (type(p) is float and type(site) is int):
+            p, site = float(p), _int(site, "site")
         key = (8, x.shape, x.stride(), x.dtype, p, site, _sig(rng), _sig(y))
     except AttributeError:
         _bad(("x", x), ("rng", rng), ("out y", y))
     plan = _plans.get(key) or _keep(key, _dropout_plan(x, p, rng, site, y))
-    dev = x.get_device()
-    if dev < 0:
-        _bad(("x", x))
-    _one_device(dev, ("rng", rng), ("out y", y))
+    if not (dev >= 0 and (rng is None or rng.get_device() == dev) and (y is None or y.get_device() == dev)):
+        _elsewhere(dev, ("x", x), ("rng", rng), ("out y", y))
     if y is None:
         y = _new(x)
-    rc = _b.load().mosa_dropout(plan[0], x.data_ptr(), _ptr(rng), y.data_ptr(), _b._stream(None))
+    rc = _b.load().mosa_dropout(plan[0], x.data_ptr(), None if rng is None else rng.data_ptr(), y.data_ptr(),
+                                _b._stream(None))
     if rc:
         _b._check(rc, "mosa_dropout")
     return y
@@ -349,7 +362,7 @@ def _logprob_plan(logits, targets, top, scale, results, back=None):
     for name, t, n, dtype in results:
         _vector(t, name, (B, T, n) if n else (B, T), dtype)
     s = MosaLogprobShape(B, T, V, _b._dtype_code(logits), 1 if targets is not None and targets.dtype == torch.int64 else 0,
-                         top, scale, _rows(logits, "logits"))
+                         _int(top, "top"), scale, _rows(logits, "logits"))
     if back is not None:
         s.dz = _result(back[0], "dlogits", logits.shape, logits.dtype)
         return ctypes.byref(s), 0, s
@@ -365,13 +378,15 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
     all fp32 but the indices.  Entries of -inf (or -2^90 and less) are ruled out.  ``out`` may hold any of
     them."""
     try:
-        if _away(logits, stream):
+        dev = logits.get_device()
+        if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):
             return _there(logits, stream, mosa_token_logprobs, logits, targets, top, scale, workspace, out)
         torch = _b._torch()
         f32 = torch.float32
         logp, ent, lse, idx, tlp = ((out.get("logp"), out.get("entropy"), out.get("lse"), out.get("top"),
                                      out.get("top_logp")) if out else (None,) * 5)
-        top, scale = _int(top, "top"), _float(scale)
+        if not (type(top) is int and type(scale) is float):
+            top, scale = _int(top, "top"), _float(scale)
         key = (9, logits.shape, logits.stride(), logits.dtype, _sig(targets), top, scale,
                (_sig(logp), _sig(ent), _sig(lse), _sig(idx), _sig(tlp)) if out else None)
     except AttributeError:
@@ -379,11 +394,11 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
     plan = _plans.get(key) or _keep(key, _logprob_plan(
         logits, targets, top, scale, [("logp", logp, 0, f32), ("entropy", ent, 0, f32), ("lse", lse, 0, f32),
                                       ("top", idx, top, torch.int32), ("top_logp", tlp, top, f32)]))
-    dev = logits.get_device()
-    if dev < 0:
-        _bad(("logits", logits))
-    _one_device(dev, ("targets", targets), ("logp", logp), ("entropy", ent), ("lse", lse), ("top", idx),
-                ("top_logp", tlp), ("workspace", workspace))
+    if not (dev >= 0 and (targets is None or targets.get_device() == dev)
+            and (workspace is None or workspace.get_device() == dev)
+            and (out is None or _all_on(dev, logp, ent, lse, idx, tlp))):
+        _elsewhere(dev, ("logits", logits), ("targets", targets), ("workspace", workspace), ("logp", logp),
+                   ("entropy", ent), ("lse", lse), ("top", idx), ("top_logp", tlp))
     device, lead = logits.device, logits.shape[:2]
     r = {}
     if targets is None:
@@ -399,7 +414,8 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
         idx = tlp = None
     workspace = _space(workspace, plan[1], device)
     rc = _b.load().mosa_token_logprobs(
-        plan[0], logits.data_ptr(), _ptr(targets), _ptr(logp), ent.data_ptr(), lse.data_ptr(), _ptr(idx), _ptr(tlp),
+        plan[0], logits.data_ptr(), None if targets is None else targets.data_ptr(),
+        None if logp is None else logp.data_ptr(), ent.data_ptr(), lse.data_ptr(), _ptr(idx), _ptr(tlp),
         workspace.data_ptr(), workspace.numel(), _b._stream(None))
     if rc:
         _b._check(rc, "mosa_token_logprobs")
@@ -413,7 +429,8 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
     the indices that it returned, read with dtop_logp.  ``out`` may hold "dlogits", logits itself among
     them."""
     try:
-        if _away(logits, stream):
+        dev = logits.get_device()
+        if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):
             return _there(logits, stream, mosa_token_logprobs_backward, logits, targets, lse, entropy, dlogp, dentropy,
                           dlse, top, dtop_logp, scale, out)
         torch = _b._torch()
@@ -421,7 +438,8 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
         dz = out.get("dlogits") if out else None
         if dtop_logp is None:
             top = None
-        scale = _float(scale)
+        if type(scale) is not float:
+            scale = _float(scale)
         key = (10, logits.shape, logits.stride(), logits.dtype, _sig(targets), lse.shape, lse.stride(), lse.dtype,
                _sig(entropy), _sig(dlogp), _sig(dentropy), _sig(dlse), _sig(top), _sig(dtop_logp), scale, _sig(dz))
     except AttributeError:
@@ -445,11 +463,9 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
             logits, targets, n, scale,
             [("lse", lse, 0, f32), ("entropy", entropy, 0, f32), ("dlogp", dlogp, 0, f32), ("dentropy", dentropy, 0, f32),
              ("dlse", dlse, 0, f32), ("top", top, n, torch.int32), ("dtop_logp", dtop_logp, n, f32)], (dz,)))
-    dev = logits.get_device()
-    if dev < 0:
-        _bad(("logits", logits))
-    _one_device(dev, ("targets", targets), ("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy),
-                ("dlse", dlse), ("top", top), ("dtop_logp", dtop_logp), ("dlogits", dz))
+    if not (dev >= 0 and lse.get_device() == dev and _all_on(dev, targets, entropy, dlogp, dentropy, dlse, top, dtop_logp, dz)):
+        _elsewhere(dev, ("logits", logits), ("targets", targets), ("lse", lse), ("entropy", entropy), ("dlogp", dlogp),
+                   ("dentropy", dentropy), ("dlse", dlse), ("top", top), ("dtop_logp", dtop_logp), ("dlogits", dz))
     if dz is None:
         dz = _new(logits)
     rc = _b.load().mosa_token_logprobs_backward(

@@ -194,6 +194,9 @@ mosa_status mosa_dropout(const mosa_dropout_shape *shape, const void *x, const i
     mosa_status st = check_rows(shape->B, shape->T, shape->d);
     if (st != MOSA_OK) return st;
     if (!dtype_ok(shape->dtype)) return MOSA_ERR_INVALID_ARG;
+    // (runs of 256 columns are counted in 31 bits: a tensor that needs more has a terabyte)
+    if ((long long)shape->B * shape->T * (shape->d / 256LL + 1) >= 1LL << 31 || shape->d >= 2147483647 - 65536)
+        return MOSA_ERR_UNSUPPORTED;
     Drop d;
     if ((st = check_drop(shape->dropout, shape->site, rng, &d)) != MOSA_OK) return st;
     Str xs, ys;

@@ -8,14 +8,16 @@
 //               A = scale (dlse - G - dentropy entropy), B = -scale ln 2 dentropy; then the few places
 //               with a gradient of their own (the target and the alternatives) once more.  (scale z
 //               is rounded as in lse, so that b of a row's only large entry is 0 however large it is.)
-// A warp takes a row, or the warps of a block share one where rows are few, or some blocks, whose
+// A warp takes a row, or 2, 4 or 8 of a block share one where rows are fewer, or some blocks, whose
 // results a second kernel joins.  Rows move in 16-byte pieces wherever they start: a row is cut at the
 // addresses' multiples of 16, its first and last pieces are read value by value.
 //
-// Alternatives: a warp keeps its 32 best entries, one a lane, as 64-bit keys in falling order (the
-// value's bits in an order of integers, then the index, low ones first).  Values above the last
-// one wanted are rare after the first pieces; they gather in shared memory and are sorted and merged 32
-// at a time.  The first piece's bar is the top-th largest of its lanes' maxima.
+// Alternatives: the pass over the row only notes, for each lane, the largest values of its three best steps (32 bf16
+// or 16 fp32 values a step) and that of the fourth.  A value T that the largest of `top` steps of lanes reach is
+// one that `top` entries reach at least, so that the wanted ones lie in the few steps of lanes whose largest reaches it:
+// those are read once more.  (Where a lane's fourth best reaches T as well, as with equal values, its warp
+// looks through its part of the row again.)  The best 32 entries are kept one a lane, in falling order, as 64-bit keys:
+// the value's bits in an order of integers, then the index, low ones first.
 #include <algorithm>
 #include <cmath>
 
@@ -44,7 +46,8 @@ struct Part {
 struct Args {
     LogProb l;
     float c;            // scale log2 e
-    int segments;       // forward: blocks of a row
+    int share;          // forward: warps of a row in a block (1, 2, 4, 8)
+    int segments;       // forward: blocks of a row (share = 8)
     Part *parts;        // [rows][segments]
     unsigned long long *tops;   // [rows][segments][32]
     int units;          // backward: warps of a row
@@ -92,7 +95,10 @@ struct Row {
             return;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; ++i) v.w[i] = kWide ? 0xFF800000u : 0xFF80FF80u;
+        if (col + E <= 0 || col >= V) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {   // (the first or the last piece of the row)
             if (kWide) {
                 v.w[i] = col + i >= 0 && col + i < V ? reinterpret_cast<const uint32_t *>(p)[col + i] : 0xFF800000u;
             } else {
@@ -102,6 +108,21 @@ struct Row {
                          (a + 1 >= 0 && a + 1 < V ? (uint32_t)q[a + 1] : 0xFF80u) << 16;
             }
         }
+    }
+    // A step's pieces of this lane.
+    __device__ __forceinline__ void load_step(int step, int lane, Piece (&v)[kVecs]) const {
+        const int col = first + step * step_columns<kWide>();
+        if (col >= 0 && col + step_columns<kWide>() <= V) {   // (most steps: no piece is cut)
+            const uint4 *q = reinterpret_cast<const uint4 *>(p + (long long)col * (kWide ? 4 : 2)) + lane;
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) {
+                const uint4 x = q[32 * u];
+                v[u].w[0] = x.x; v[u].w[1] = x.y; v[u].w[2] = x.z; v[u].w[3] = x.w;
+            }
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) load(column(step, u, lane), v[u]);
     }
     __device__ __forceinline__ float value(int col) const {
         return kWide ? reinterpret_cast<const float *>(p)[col] : to_f32(reinterpret_cast<const bf16 *>(p)[col]);
@@ -116,11 +137,24 @@ __device__ __forceinline__ float value_of(const Piece &v, int e) {
 // Largest value of a piece (a NaN gives way).
 template <bool kWide>
 __device__ __forceinline__ float largest(const Piece &v) {
-    if (kWide)
+    if constexpr (kWide)
         return fmaxf(fmaxf(__uint_as_float(v.w[0]), __uint_as_float(v.w[1])),
                      fmaxf(__uint_as_float(v.w[2]), __uint_as_float(v.w[3])));
     const uint32_t m = max2(max2(v.w[0], v.w[1]), max2(v.w[2], v.w[3]));
     return fmaxf(low(m), high(m));
+}
+
+template <bool kWide>
+__device__ __forceinline__ float largest(const Piece (&v)[kVecs]) {
+    if constexpr (kWide) {
+        return fmaxf(fmaxf(largest<true>(v[0]), largest<true>(v[1])), fmaxf(largest<true>(v[2]), largest<true>(v[3])));
+    } else {
+        uint32_t m[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = max2(max2(v[0].w[i], v[1].w[i]), max2(v[2].w[i], v[3].w[i]));
+        m[0] = max2(max2(m[0], m[1]), max2(m[2], m[3]));
+        return fmaxf(low(m[0]), high(m[0]));
+    }
 }
 
 __device__ __forceinline__ int row_split(const LogProb &l, long long row, int *t) {
@@ -141,10 +175,12 @@ __device__ __forceinline__ float of_order(uint32_t o) {
     return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
 
-__device__ __forceinline__ Key pick(Key a, Key b, bool larger) { return (a > b) == larger ? a : b; }
+template <class K>
+__device__ __forceinline__ K pick(K a, K b, bool larger) { return (a > b) == larger ? a : b; }
 
 // Falling order over the lanes.
-__device__ __forceinline__ Key sorted(Key k, int lane) {
+template <class K>
+__device__ __forceinline__ K sorted(K k, int lane) {
 #pragma unroll
     for (int n = 2; n <= 32; n *= 2)
 #pragma unroll
@@ -153,43 +189,142 @@ __device__ __forceinline__ Key sorted(Key k, int lane) {
     return k;
 }
 // The 32 largest of two lists in falling order.
-__device__ __forceinline__ Key merged(Key a, Key b, int lane) {
-    Key k = pick(a, __shfl_sync(0xffffffffu, b, 31 - lane), true);
+template <class K>
+__device__ __forceinline__ K merged(K a, K b, int lane) {
+    K k = pick(a, __shfl_sync(0xffffffffu, b, 31 - lane), true);
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) k = pick(k, __shfl_xor_sync(0xffffffffu, k, o), (lane & o) == 0);
     return k;
 }
 
-struct Best {
-    Key list = 0;          // this lane's entry (0: none)
-    float bar = 0.f;       // the last entry wanted
-    bool all = true;       // there is no bar yet
-    int waiting = 0;       // candidates in shared memory
-};
+// Puts lanes' keys (0: none; `who` has one) into the list: one at a time, or sorted and merged where they are many.
+__device__ __forceinline__ Key put_in(Key list, Key k, uint32_t who, int lane) {
+    if (__popc(who) > 8) return merged(list, sorted(k, lane), lane);
+#pragma unroll 1
+    for (; who != 0; who &= who - 1) {
+        const Key one = __shfl_sync(0xffffffffu, k, __ffs(who) - 1);
+        const int before = __popc(__ballot_sync(0xffffffffu, list > one));
+        const Key up = __shfl_up_sync(0xffffffffu, list, 1);
+        list = lane < before ? list : lane == before ? one : up;
+    }
+    return list;
+}
+__device__ __forceinline__ Key key_of(float v, int col) { return (Key)order_of(v) << 32 | (0xFFFFFFFFu - (uint32_t)col); }
 
-// Merges the first 32 candidates (those there are).
-__device__ __forceinline__ void take_in(Best &b, Key *wait, int top, int lane) {
-    __syncwarp();
-    Key k = lane < b.waiting ? wait[lane] : 0;
-    const Key rest = 32 + lane < b.waiting ? wait[32 + lane] : 0;
-    __syncwarp();
-    wait[lane] = rest;
-    b.waiting = max(b.waiting - 32, 0);
-    b.list = merged(b.list, sorted(k, lane), lane);
-    const uint32_t last = (uint32_t)(__shfl_sync(0xffffffffu, b.list, top - 1) >> 32);
-    b.all = last == 0;
-    b.bar = of_order(last);
-    __syncwarp();
+// The best of a warp's part of a row, looked through once more: what reaches `bar` (low: whatever there is).
+template <bool kWide>
+__device__ __noinline__ Key look_again(const Row<kWide> &z, int from, int to, float bar, bool low, int top) {
+    constexpr int E = kWide ? 4 : 8;
+    const int lane = threadIdx.x & 31;
+    Key list = 0;
+    bool full = false;   // the list holds `top` entries: what comes later has to be above the last of them
+    Piece v[kVecs], next[kVecs];
+    z.load_step(from, lane, v);
+#pragma unroll 1
+    for (int i = from; i < to; ++i) {
+        if (i + 1 < to) z.load_step(i + 1, lane, next);
+        const float here = largest<kWide>(v);
+        if (__any_sync(0xffffffffu, low || (full ? here > bar : here >= bar))) {
+#pragma unroll 1
+            for (int u = 0; u < kVecs; ++u) {
+                const Piece x = v[0];
+#pragma unroll
+                for (int j = 0; j + 1 < kVecs; ++j) v[j] = v[j + 1];
+                const int col = z.column(i, u, lane);
+                uint32_t on = 0;   // a bit for each value (the bar stays within a piece: lanes' values do not come by index)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float y = value_of<kWide>(x, e);
+                    const bool in = col + e >= 0 && col + e < z.V;
+                    on |= in && (low || (full ? y > bar : y >= bar)) ? 1u << e : 0u;
+                }
+#pragma unroll 1
+                for (uint32_t who; (who = __ballot_sync(0xffffffffu, on != 0)) != 0;) {
+                    const int e = __ffs(on) - 1;
+                    float y = value_of<kWide>(x, 0);
+#pragma unroll
+                    for (int j = 1; j < E; ++j) y = e == j ? value_of<kWide>(x, j) : y;
+                    list = put_in(list, on != 0 ? key_of(y, col + e) : 0, who, lane);
+                    on &= on - 1;
+                }
+                const uint32_t last = (uint32_t)(__shfl_sync(0xffffffffu, list, top - 1) >> 32);
+                if (last != 0) {
+                    full = true;
+                    low = false;
+                    bar = of_order(last);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) v[u] = next[u];
+    }
+    return list;
 }
 
-// The 32 best of all warps' lists, in warp 0.
-__device__ __forceinline__ Key best_of_block(Key list, Key (*room)[32], int warp, int lane) {
+// What a lane has seen: the largest values of its three best steps, which ones, and that of the fourth.
+struct Peaks {
+    float a, b, c, d;
+    int step_a, step_b, step_c;   // -1: none
+};
+
+// The 32 best of the lists of `share` warps side by side, in the first of them (all threads of the block).
+template <class K>
+__device__ __noinline__ K best_of(K list, Key (*room)[32], int share) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i = warp & (share - 1);
+#pragma unroll 1
+    for (int o = share / 2; o > 0; o /= 2) {
+        __syncthreads();
+        if (i >= o && i < 2 * o) room[warp][lane] = list;
+        __syncthreads();
+        if (i < o) list = merged(list, (K)room[warp + o][lane], lane);
+    }
+    return list;
+}
+
+// The 32 best of a warp's part of a row, those that reach T at least (all threads of the block call it).
+template <bool kWide>
+__device__ __noinline__ Key alternatives(const Row<kWide> &z, const Peaks &q, int from, int to, int share, int top,
+                                         Key (*room)[32]) {
+    constexpr int E = kWide ? 4 : 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t best = sorted(order_of(q.a), lane);
+    // (few lanes for many entries: the others of a lane's steps count, which makes T larger)
+    if (top > 8 * share) best = merged(merged(best, sorted(order_of(q.b), lane), lane), sorted(order_of(q.c), lane), lane);
+    best = best_of(best, room, share);
+    uint32_t order = __shfl_sync(0xffffffffu, best, top - 1);
+    if (share > 1) {
+        __syncthreads();
+        if ((warp & (share - 1)) == 0 && lane == 0) room[warp][0] = order;
+        __syncthreads();
+        order = (uint32_t)room[warp & ~(share - 1)][0];
+        __syncthreads();
+    }
+    const float T = of_order(order);
+    const bool low = !(T > __int_as_float(0xFF800000));
+    if (from >= to) return 0;
+    if (__any_sync(0xffffffffu, low || q.d >= T)) return look_again(z, from, to, T, low, top);
+    Key list = 0;
+#pragma unroll 1
+    for (int round = 0; round < 3; ++round) {
+        const int step = round == 0 ? q.step_a : round == 1 ? q.step_b : q.step_c;
+        uint32_t who = __ballot_sync(0xffffffffu, (round == 0 ? q.a : round == 1 ? q.b : q.c) >= T && step >= 0);
+        while (who != 0) {
+            // (four steps' values at once: a lane reads one of each, as many as a lane's step has)
+            Key k[4];
 #pragma unroll
-    for (int o = kWarps / 2; o > 0; o /= 2) {
-        __syncthreads();
-        if (warp >= o && warp < 2 * o) room[warp - o][lane] = list;
-        __syncthreads();
-        if (warp < o) list = merged(list, room[warp][lane], lane);
+            for (int j = 0; j < 4; ++j) {
+                const int src = __ffs(who) - 1;
+                who &= who - 1;
+                const int col = z.column(__shfl_sync(0xffffffffu, step, max(src, 0)), lane / E, src) + lane % E;
+                k[j] = 0;
+                if (src >= 0 && lane < kVecs * E && col >= 0 && col < z.V) {
+                    const float v = z.value(col);
+                    if (v >= T) k[j] = key_of(v, col);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) list = put_in(list, k[j], __ballot_sync(0xffffffffu, k[j] != 0), lane);
+        }
     }
     return list;
 }
@@ -214,9 +349,27 @@ __device__ __forceinline__ Part join(Part a, float c) {
     return a;
 }
 
+// A row's target and what the row holds there.
+struct Target {
+    long long at;
+    float z;
+};
+template <bool kWide>
+__device__ __forceinline__ Target target_of(const LogProb &l, long long row) {
+    Target t{-1, 0.f};
+    if (l.logp == nullptr) return t;
+    t.at = l.target64 ? static_cast<const int64_t *>(l.targets)[row] : (long long)static_cast<const int32_t *>(l.targets)[row];
+    if (t.at >= 0 && t.at < l.V) {
+        int it;
+        const int ib = row_split(l, row, &it);
+        t.z = Row<kWide>(l.z.at(ib, it), l.V).value((int)t.at);
+    }
+    return t;
+}
+
 // One warp writes a row's results.
-template <bool kWide, bool kTop>
-__device__ __forceinline__ void finish(const Args &p, long long row, const Part &a, Key list, int lane) {
+template <bool kTop>
+__device__ __forceinline__ void finish(const Args &p, long long row, const Part &a, const Target &t, Key list, int lane) {
     const LogProb &l = p.l;
     const bool none = a.m <= kLeast, bad = a.m > -kLeast;
     const float lg = logf(a.s), inf = __int_as_float(0x7F800000), nan = __int_as_float(0x7FC00000);
@@ -225,20 +378,8 @@ __device__ __forceinline__ void finish(const Args &p, long long row, const Part 
         if (l.lse != nullptr) l.lse[row] = lse;
         if (l.entropy != nullptr)
             l.entropy[row] = bad ? nan : none && a.s == a.s ? 0.f : fmaf(-kLn2, a.t / a.s, lg);
-        if (l.logp != nullptr) {
-            const long long t = l.target64 ? static_cast<const int64_t *>(l.targets)[row]
-                                           : (long long)static_cast<const int32_t *>(l.targets)[row];
-            float lp = 0.f;
-            if (t >= l.V) {
-                lp = nan;
-            } else if (t >= 0) {
-                int it;
-                const int ib = row_split(l, row, &it);
-                const float z = Row<kWide>(l.z.at(ib, it), l.V).value((int)t);
-                lp = lse != lse ? nan : z <= kLeast ? -inf : fmaf(z - a.m, l.scale, -lg);
-            }
-            l.logp[row] = lp;
-        }
+        if (l.logp != nullptr)
+            l.logp[row] = t.at < 0 ? 0.f : t.at >= l.V || lse != lse ? nan : t.z <= kLeast ? -inf : fmaf(t.z - a.m, l.scale, -lg);
     }
     if (kTop && lane < l.top) {
         const float v = of_order((uint32_t)(list >> 32));
@@ -247,76 +388,47 @@ __device__ __forceinline__ void finish(const Args &p, long long row, const Part 
     }
 }
 
-// kShared: the warps of a block share a row (segment blockIdx.x % segments of it); else a row each.
-template <bool kWide, bool kTop, bool kShared>
-__global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const __grid_constant__ Args p) {
+// `share` warps of a block take a row together, or all of them a segment of one.
+template <bool kWide, bool kTop>
+__global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int E = kWide ? 4 : 8;
-    __shared__ Key waiting[kTop ? kWarps : 1][64];
-    __shared__ Key room[kTop && kShared ? kWarps / 2 : 1][32];
-    __shared__ Part part[kShared ? kWarps : 1];
+    __shared__ Key room[kTop ? kWarps : 1][32];
+    __shared__ Part part[kWarps];
     const LogProb &l = p.l;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, mine = warp & (p.share - 1);
     const long long rows = (long long)l.B * l.T;
-    long long row = kShared ? blockIdx.x / p.segments : (long long)blockIdx.x * kWarps + warp;
-    const int segment = kShared ? (int)(blockIdx.x - row * p.segments) : 0;
-    if (row >= rows) return;   // (kShared: no block)
+    const long long row = p.segments > 1 ? blockIdx.x / p.segments : (long long)blockIdx.x * (kWarps / p.share) + warp / p.share;
+    const int segment = p.segments > 1 ? (int)(blockIdx.x - row * p.segments) : 0;
+    if (p.share == 1 && row >= rows) return;   // (else to the block's barriers, with nothing)
     int t;
-    const int b = row_split(l, row, &t);
+    const int b = row_split(l, row < rows ? row : 0, &t);
     const Row<kWide> z(l.z.at(b, t), l.V);
-    const int steps = z.steps();
-    const int share = kShared ? segment * kWarps + warp : 0, shares = kShared ? p.segments * kWarps : 1;
-    const int from = (int)((long long)steps * share / shares), to = (int)((long long)steps * (share + 1) / shares);
+    const int steps = row < rows ? z.steps() : 0, at = segment * p.share + mine, shares = p.segments * p.share;
+    const int from = (int)((long long)steps * at / shares), to = (int)((long long)steps * (at + 1) / shares);
+    Target target{-1, 0.f};
+    if (mine == 0 && p.segments == 1 && row < rows) target = target_of<kWide>(l, row);
 
     float m = kLeast;
     Pair s = 0, sum_t = 0;   // pairs of sums
-    Best best;
+    const float none_yet = __int_as_float(0xFF800000);
+    Peaks q{none_yet, none_yet, none_yet, none_yet, -1, -1, -1};
     const Pair c2 = both(p.c);
     Piece cur[kVecs];
-#pragma unroll
-    for (int u = 0; u < kVecs; ++u)
-        if (from < to) z.load(z.column(from, u, lane), cur[u]);
+    if (from < to) z.load_step(from, lane, cur);
     for (int i = from; i < to; ++i) {
         Piece next[kVecs];
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u)
-            if (i + 1 < to) z.load(z.column(i + 1, u, lane), next[u]);
-        float most[kVecs], here;
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) most[u] = largest<kWide>(cur[u]);
-        here = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-        if (kTop && __any_sync(0xffffffffu, best.all || here > best.bar)) {
-            float bar = best.bar;
-            bool all = best.all;
-            const bool first = i == from;
-            if (first) {
-                // as many lanes as entries are wanted hold one of at least this value
-                const Key k = sorted((Key)order_of(here) << 32, lane);
-                bar = of_order((uint32_t)(__shfl_sync(0xffffffffu, k, l.top - 1) >> 32));
-                all = false;
-            }
-#pragma unroll
-            for (int u = 0; u < kVecs; ++u) {
-                if (!__any_sync(0xffffffffu, all || most[u] > bar || (first && most[u] == bar))) continue;
-                const int col = z.column(i, u, lane);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float v = value_of<kWide>(cur[u], e);
-                    const bool on = (all || v > bar || (first && v == bar)) && col + e >= 0 && col + e < l.V;
-                    const uint32_t who = __ballot_sync(0xffffffffu, on);
-                    if (who == 0) continue;
-                    if (on)
-                        waiting[warp][best.waiting + __popc(who & ((1u << lane) - 1))] =
-                            (Key)order_of(v) << 32 | (0xFFFFFFFFu - (uint32_t)(col + e));
-                    best.waiting += __popc(who);
-                    if (best.waiting >= 32) take_in(best, waiting[warp], l.top, lane);
-                }
-            }
-            // Those of the first step are at least `top`: what comes later has to be above their bar.
-            if (first && best.all) {
-                best.bar = bar;
-                best.all = bar != bar;
-            }
+        if (i + 1 < to) z.load_step(i + 1, lane, next);
+        const float here = largest<kWide>(cur);
+        if (kTop) {   // (chosen, not branched; a NaN is above nothing)
+            const bool first = here > q.a, second = here > q.b, third = here > q.c;
+            q.d = third ? q.c : fmaxf(q.d, here);
+            q.c = second ? q.b : third ? here : q.c;
+            q.step_c = second ? q.step_b : third ? i : q.step_c;
+            q.b = first ? q.a : second ? here : q.b;
+            q.step_b = first ? q.step_a : second ? i : q.step_b;
+            q.a = first ? here : q.a;
+            q.step_a = first ? i : q.step_a;
         }
         if (here > m) {   // (false for a NaN)
             const float by = fmaxf((m - here) * p.c, -1000.f), f = pow2(by);
@@ -346,43 +458,44 @@ __global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const __grid_const
 #pragma unroll
         for (int u = 0; u < kVecs; ++u) cur[u] = next[u];
     }
-    if (kTop)
-        while (best.waiting > 0) take_in(best, waiting[warp], l.top, lane);
     const F2 s2 = of_two(s), t2 = of_two(sum_t);
     Part a = join(Part{m, s2.x + s2.y, t2.x + t2.y, 0.f}, p.c);
-    if (!kShared) {
-        finish<kWide, kTop>(p, row, a, best.list, lane);
-        return;
+    Key list = 0;
+    if (kTop) list = alternatives<kWide>(z, q, from, to, p.share, l.top, room);
+    if (p.share > 1) {
+        if (lane == 0) part[warp] = a;
+        if (kTop) list = best_of(list, room, p.share);
+        __syncthreads();
+        if (mine != 0 || row >= rows) return;
+        a = join(lane < p.share ? part[warp + lane] : Part{kLeast, 0.f, 0.f, 0.f}, p.c);
+        if (p.segments > 1) {
+            if (lane == 0) p.parts[blockIdx.x] = a;
+            if (kTop) p.tops[(long long)blockIdx.x * 32 + lane] = list;
+            return;
+        }
     }
-    if (lane == 0) part[warp] = a;
-    if (kTop) best.list = best_of_block(best.list, room, warp, lane);
-    __syncthreads();
-    if (warp != 0) return;
-    a = join(lane < kWarps ? part[lane] : Part{kLeast, 0.f, 0.f, 0.f}, p.c);
-    if (p.segments == 1) {
-        finish<kWide, kTop>(p, row, a, best.list, lane);
-        return;
-    }
-    if (lane == 0) p.parts[blockIdx.x] = a;
-    if (kTop) p.tops[(long long)blockIdx.x * 32 + lane] = best.list;
+    finish<kTop>(p, row, a, target, list, lane);
 }
 
 // The segments of a row together: a block a row.
 template <bool kWide, bool kTop>
 __global__ void __launch_bounds__(kThreads) logprob_join_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    __shared__ Key room[kTop ? kWarps / 2 : 1][32];
+    __shared__ Key room[kTop ? kWarps : 1][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long row = blockIdx.x, at = row * p.segments;
+    Target target{-1, 0.f};
+    if (warp == 0) target = target_of<kWide>(p.l, row);
     Key list = 0;
     if (kTop) {
-        for (int i = warp; i < p.segments; i += kWarps) list = merged(list, p.tops[(at + i) * 32 + lane], lane);
-        list = best_of_block(list, room, warp, lane);
+#pragma unroll 1
+        for (int i = warp; i < p.segments; i += kWarps) list = merged(list, (Key)p.tops[(at + i) * 32 + lane], lane);
+        list = best_of(list, room, kWarps);
     }
     if (warp != 0) return;
     const Part none{kLeast, 0.f, 0.f, 0.f};
     const Part a = join(lane < p.segments ? p.parts[at + lane] : none, p.c);
-    finish<kWide, kTop>(p, row, a, list, lane);
+    finish<kTop>(p, row, a, target, list, lane);
 }
 
 // ------------------------------------------------------------------ backward
@@ -457,14 +570,10 @@ __global__ void __launch_bounds__(kThreads) logprob_bwd_kernel(const __grid_cons
         const Pair scale2 = both(l.scale), minus = both(-ref), to2 = both(kLog2e);
         const Pair A2 = both(A), B2 = both(B);
         Piece cur[kVecs];
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u)
-            if (from < to && !zero) z.load(z.column(from, u, lane), cur[u]);
+        if (from < to && !zero) z.load_step(from, lane, cur);
         for (int i = from; i < to; ++i) {
             Piece next[kVecs];
-#pragma unroll
-            for (int u = 0; u < kVecs; ++u)
-                if (i + 1 < to && !zero) z.load(z.column(i + 1, u, lane), next[u]);
+            if (i + 1 < to && !zero) z.load_step(i + 1, lane, next);
 #pragma unroll
             for (int u = 0; u < kVecs; ++u) {
                 uint32_t w[4] = {0u, 0u, 0u, 0u};
@@ -532,27 +641,29 @@ int steps_of(const LogProb &l) {   // (as if a row started at a multiple of 16 b
     return (int)(((long long)l.V + K - 1) / K);
 }
 
-// Forward: a row is a warp's where rows are many or short; else a block's, or that of as many
-// blocks as let two SMs of three have two.
-int segments_of(const LogProb &l) {   // 0: a warp a row
-    const long long rows = (long long)l.B * l.T;
-    // (the same for both types, so that the workspace's size does not hang on a pointer)
-    const int steps = (int)(((long long)l.V + 1023) / 1024);
-    if (rows >= 2432 || steps < 4) return 0;
-    const long long most = std::max(1, steps / kWarps);
-    return (int)std::min<long long>(std::min<long long>(most, 32), std::max(1LL, 2 * kSms / rows));
+// Forward: how many warps of a block share a row, and how many blocks.  As few as make two rounds of
+// all SMs' warps, so that the last one, which leaves SMs idle, is short; as many as have some steps each.  us
+// with 1, 2, 4, 8 warps a row (bf16, no alternatives / 5): 4096 rows of 50001 entries 82, 74, 74, 76 / 145, 119, 103,
+// 118 (before the steps' largest were noted three deep), 1000 of 32003 -, -, -, 18 / -, -, -, 28.
+// More blocks than one cost a second kernel: 300 rows of 32003 take 5.9 us with one, 7.2 with two; 100 rows of
+// 131072 8.2 with six.
+void split(const LogProb &l, int *share, int *segments) {
+    const long long rows = (long long)l.B * l.T, all = 32LL * kSms;
+    // (counted alike for both types and places, so that the workspace's size does not hang on a pointer)
+    const long long steps = ((long long)l.V + 1023) / 1024;
+    *share = *segments = 1;
+    while (*share < kWarps && rows * *share < 2 * all && steps >= 4 * *share) *share *= 2;
+    if (*share < kWarps) return;
+    const long long n = std::min(std::min(32LL, steps / kWarps), all / (rows * kWarps));
+    if (n >= 3) *segments = (int)n;
 }
 
 template <bool kWide, bool kTop>
 cudaError_t launch(const Args &p, cudaStream_t s) {
-    const long long rows = (long long)p.l.B * p.l.T;
-    cudaError_t e;
+    const long long rows = (long long)p.l.B * p.l.T, per = kWarps / p.share;
+    const unsigned blocks = (unsigned)(p.segments > 1 ? rows * p.segments : (rows + per - 1) / per);
     note_launches(1);
-    if (p.segments == 0) {
-        const long long blocks = (rows + kWarps - 1) / kWarps;
-        return launch_pdl(logprob_kernel<kWide, kTop, false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p);
-    }
-    e = launch_pdl(logprob_kernel<kWide, kTop, true>, dim3((unsigned)(rows * p.segments)), dim3(kThreads), 0, s, p);
+    cudaError_t e = launch_pdl(logprob_kernel<kWide, kTop>, dim3(blocks), dim3(kThreads), 0, s, p);
     if (e != cudaSuccess || p.segments == 1) return e;
     note_launches(1);
     return launch_pdl(logprob_join_kernel<kWide, kTop>, dim3((unsigned)rows), dim3(kThreads), 0, s, p);
@@ -568,13 +679,15 @@ Args args_of(const LogProb &l) {
 }  // namespace
 
 size_t logprob_workspace(const LogProb &l) {
-    const size_t n = (size_t)l.B * l.T * std::max(segments_of(l), 0);
+    int share, segments;
+    split(l, &share, &segments);
+    const size_t n = segments > 1 ? (size_t)l.B * l.T * segments : 0;
     return 256 + (n + 15) / 16 * 256 + (l.top > 0 ? n * 32 * sizeof(Key) : 0);
 }
 
 cudaError_t launch_logprob(const LogProb &l, void *ws, cudaStream_t s) {
     Args p = args_of(l);
-    p.segments = segments_of(l);
+    split(l, &p.share, &p.segments);
     const size_t n = (size_t)l.B * l.T * p.segments;
     p.parts = reinterpret_cast<Part *>(static_cast<char *>(ws) + 256);
     p.tops = reinterpret_cast<Key *>(static_cast<char *>(ws) + 256 + (n + 15) / 16 * 256);

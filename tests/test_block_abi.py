@@ -96,7 +96,8 @@ def test_residual_refuses_pointers_and_workspaces():
 
 @pytest.mark.parametrize("kw,code", [
     (dict(B=0), INV), (dict(T=-1), INV), (dict(d=0), INV), (dict(dtype=2), INV), (dict(dropout=1.5), INV),
-    (dict(dropout=NAN), INV), (dict(B=1 << 16, T=1 << 15), UNS), (dict(x=S(-1, 64, 0)), INV), (dict(y=S(0, 64, 0)), INV),
+    (dict(dropout=NAN), INV), (dict(B=1 << 16, T=1 << 15), UNS), (dict(d=2**31 - 1), UNS), (dict(T=1 << 20, d=1 << 20), UNS),
+    (dict(x=S(-1, 64, 0)), INV), (dict(y=S(0, 64, 0)), INV),
     (dict(y=S(640, 63, 0)), INV),
 ])
 def test_dropout_refuses(kw, code):
