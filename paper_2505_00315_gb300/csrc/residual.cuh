@@ -27,6 +27,7 @@ struct Args {
     Residual r;
     float *partial;     // backward: [blocks][3][d] sums over tokens, of gamma_post, gamma_pre, gate
     int warps, groups;  // W, G
+    int most;           // warps of a block at most: 16, or 8 where each has 256 registers a thread
     int stages, stage_bytes;
     int off[kIn];       // of each tensor within a warp's stage
     int flat;           // every tensor's rows lie one stride apart, sequences too
@@ -418,11 +419,24 @@ __device__ __forceinline__ Oct vector_at(const Args &p, const Place &l, int whic
 #undef MOSA_OCT
 
 // Eights of columns of a thread: as many as registers hold, since what a row costs beside its values is
-// shared by them (the backward keeps three sums of each column and what its second round needs; a
-// gate per token takes room), but enough warps for all SMs first.
-inline int times_of(const Residual &r, bool backward) {
+// shared by them, but enough warps for all SMs first.  The forward takes four (two with a gate per
+// token); the backward, which keeps two sums of each column and what its second round needs, two in blocks
+// of 8 warps (256 registers a thread) where a group has some rows, else one in blocks of 16.  us of the backward with
+// one / two: B4 T4096 d1024 55.5 / 53.7, B2 T8192 d4096 267 / 251, fp32 B4 T1000 d768 21.2 / 22.5 (two in blocks of
+// 16, which spill: 74, 537 and 29).
+inline int times_of(const Residual &r, bool backward, int *most) {
     const long long rows = (long long)r.B * r.T;
-    int times = backward ? 1 : r.gate == MOSA_GATE_TOKEN ? 2 : 4;
+    *most = kWarps;
+    if (backward) {
+        int W = 1;
+        while (W * 512 < r.d) W *= 2;
+        if (W <= kWarps / 2 && r.d > 256 && rows * W >= kSms * 8 * 16) {
+            *most = kWarps / 2;
+            return 2;
+        }
+        return 256 * kWarps < r.d ? 2 : 1;
+    }
+    int times = r.gate == MOSA_GATE_TOKEN ? 2 : 4;
     while (times > 1 && rows * ((r.d + 256 * times - 1) / (256 * times)) < kSms * kWarps) times /= 2;
     while (256 * times * kWarps < r.d) times *= 2;
     return times;
@@ -444,8 +458,8 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
     if (r.T == 1 && !p.flat)
         for (Rows *m : all) m->t = 0;
     p.warps = 1;
-    const int most = times_of(r, backward);
-    while (p.warps * 256 * most < r.d) p.warps *= 2;
+    const int each = times_of(r, backward, &p.most);
+    while (p.warps * 256 * each < r.d) p.warps *= 2;
     *times = (r.d + p.warps * 256 - 1) / (p.warps * 256);
     if (*times == 3) *times = 4;
     const Rows *in[kIn] = {&r.x, &r.y, &r.dxo, &r.dh, &r.g};
@@ -458,7 +472,7 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
     }
     // As many rows as the block has warps for, but blocks for all SMs first, and two stages at least.
     const int vectors = (backward ? 3 : 2) * *times * p.warps * 1024;
-    p.groups = (int)std::min<long long>(kWarps / p.warps, std::max(1LL, rows / kSms));
+    p.groups = (int)std::min<long long>(p.most / p.warps, std::max(1LL, rows / kSms));
     for (;; --p.groups) {
         const int nwarps = p.warps * p.groups, fixed = nwarps * (kScratch + 2 * 16);
         p.held = fixed + nwarps * p.stage_bytes + vectors <= kSmem;

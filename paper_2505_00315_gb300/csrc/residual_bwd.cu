@@ -1,214 +1,9 @@
-// The residual step's backward, one pass over its tensors.  With yh = r_y y, xh = r_x x', e = dh gamma_pre and
-// c = scale keep/(1-p),
-//     t = dx' + r_x (e - xh mean(e xh)),  dx = t,  dgamma_pre = sum dh xh
-//     w = c g gamma_post t,  dy = r_y (w - yh mean(w yh)),  dgamma_post = sum c g t yh,  dg = c t n.
-// x' is computed again from x and y (the bytes are those of x' itself, and no rounding of x' comes in),
-// the mask from its counters.  Both means are known from one round of sums: with u = c g gamma_post yh and
-// b = dx' + r_x e, mean(w yh) = mean(u b) - r_x mean(e xh) mean(u xh).  Sums over tokens stay in
-// registers and leave once a block; a second kernel adds the blocks' up in order.
-#include "residual.cuh"
+// The residual step's backward in blocks of 16 warps, its sums over tokens and its launch; the kernel: residual_bwd.cuh.
+#include "residual_bwd.cuh"
 
 namespace mosa {
 namespace blk {
 namespace {
-
-template <int C, class Ty>
-__global__ void __launch_bounds__(kThreads, 1) residual_bwd_kernel(const __grid_constant__ Args p) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    constexpr bool kFast = Ty::kFast;
-    extern __shared__ __align__(16) char smem[];
-    const Residual &r = p.r;
-    const Place l(p, smem, C);
-    const DropKey key = drop_key(r.drop);
-    const bool drops = r.drop.rng != nullptr, token = r.gate == MOSA_GATE_TOKEN;
-    const bool has_dxo = r.dxo.p != nullptr, has_dh = r.dh.p != nullptr;
-    const float unit = r.scale * (drops ? r.drop.scale : 1.f), inv_d = 1.f / l.d;   // unit: c of a kept value
-    if (l.d < 256 * C * l.W || !has_dxo || !has_dh) clear_ring(l);
-    uint32_t row = blockIdx.x * p.groups + l.group;   // (row + kMaxStages step fits 32 bits)
-    Arrival<C, kFast, Ty::x> x_in, dxo_in;
-    Arrival<C, kFast, Ty::y> y_in;
-    Arrival<C, kFast, Ty::dh> dh_in;
-    Arrival<C, kFast, Ty::storage> g_in;
-    x_in.init(p, l, r.x, row);
-    y_in.init(p, l, r.y, row);
-    dxo_in.init(p, l, r.dxo, row);
-    dh_in.init(p, l, r.dh, row);
-    g_in.init(p, l, r.g, row);
-    Departure<C, kFast, Ty::x> dx_out;
-    Departure<C, kFast, Ty::storage> dy_out, dg_out;
-    dx_out.init(p, l, r.dx, row);
-    dy_out.init(p, l, r.dy, row);
-    dg_out.init(p, l, r.dg, row);
-    // Where the tensors' columns lie in a stage.
-    const int y_off = kFast ? bytes_of(Ty::x, C) : p.off[1], dxo_off = kFast ? y_off + bytes_of(Ty::y, C) : p.off[2];
-    const int dh_off = kFast ? dxo_off + bytes_of(Ty::x, C) : p.off[3];
-    const int g_off = kFast ? dh_off + bytes_of(Ty::dh, C) : p.off[4];
-    auto fill = [&](uint32_t at, int slot) {
-        const uint32_t to = l.ring32 + slot * p.stage_bytes;
-        x_in.issue(p, l, r.x, at, to);
-        y_in.issue(p, l, r.y, at, to + y_off);
-        if (has_dxo) dxo_in.issue(p, l, r.dxo, at, to + dxo_off);
-        if (has_dh) dh_in.issue(p, l, r.dh, at, to + dh_off);
-        if (token) g_in.issue(p, l, r.g, at, to + g_off);
-    };
-    const int ahead = p.stages - 1;
-    for (int i = 0; i < ahead; ++i) {
-        if (row + i * l.step < l.rows) fill(row + i * l.step, i);
-        copies_end();
-    }
-    if (kFast || p.held) hold<C, false>(p, l, unit);
-
-    int slot = 0, turn = 0;
-    // Sums over tokens: 0 of gamma_post over c g, which the gate of a channel shares (each has a factor of
-    // the column's own), with a gate per token of gamma_post itself; 1 of gamma_pre.
-    Oct acc[2][C];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int c = 0; c < C; ++c) acc[i][c] = zeros();
-    float next_ry = 1.f, next_rx = 1.f;
-    if (row < l.rows) {
-        next_ry = r.stats[row];
-        next_rx = r.stats[(uint64_t)l.rows + row];
-    }
-    for (; row < l.rows; row += l.step) {
-        __syncwarp();   // (the slot that is filled next has been read by all lanes)
-        if (row + ahead * l.step < l.rows) fill(row + ahead * l.step, slot == 0 ? ahead : slot - 1);
-        copies_end();
-        const float ry = r.post ? next_ry : 1.f, rx = next_rx;
-        if (row + l.step < l.rows) {
-            next_ry = r.stats[row + l.step];
-            next_rx = r.stats[(uint64_t)l.rows + row + l.step];
-        }
-        uint32_t bits[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c) bits[c] = 0xFFu;
-        if (drops) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) bits[c] = kept8(r.drop, key, row, (uint32_t)l.column(c) >> 3);
-        }
-        copies_wait(ahead);
-        __syncwarp();
-        const char *in = l.ring + slot * p.stage_bytes;
-        slot = slot == ahead ? 0 : slot + 1;
-        const int xw = wide_of(Ty::x, r.x), yw = wide_of(Ty::y, r.y), hw = wide_of(Ty::dh, r.dh);
-        const int gw = wide_of(Ty::storage, r.g);
-        auto token_gate = [&](int c) {
-            const Oct g = take(in + g_off + bytes_of(gw, c), gw, l.lane);
-            return r.sigmoid ? logistic(g) : g;
-        };
-        // What both rounds need, from what the ring holds.
-        struct Values {
-            Oct yh, xh, cg, base;   // cg: c g (0 where dropped); base: dx' + r_x e
-        };
-        auto values = [&](int c, Oct &u, Oct &dh, Oct &e) {
-            Values v;
-            const Oct y = take(in + y_off + bytes_of(yw, c), yw, l.lane);
-            const Oct x = take(in + bytes_of(xw, c), xw, l.lane);
-            const Oct dxo = take(in + dxo_off + bytes_of(xw, c), xw, l.lane);
-            dh = take(in + dh_off + bytes_of(hw, c), hw, l.lane);
-            v.cg = token ? times(token_gate(c), unit) : vector_at<C, false, kFast>(p, l, 2, c, unit);
-            v.yh = times(y, ry);
-            if (drops) {
-                v.cg = chosen(v.cg, bits[c]);
-                // (with a norm, what is not finite is so in its whole row)
-                if (!r.post) v.yh = chosen(v.yh, bits[c]);
-            }
-            u = times(times(v.yh, vector_at<C, false, kFast>(p, l, 0, c, unit)), v.cg);
-            v.xh = times(plus(x, u), rx);
-            e = times(dh, vector_at<C, false, kFast>(p, l, 1, c, unit));
-            v.base = fused(e, rx, dxo);
-            return v;
-        };
-        // (with eight columns a thread they stay in registers from one round to the other)
-        constexpr bool kStay = C == 1;
-        Values stay;
-        Pair s0 = 0, s1 = 0, s2 = 0;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            Oct u, dh, e;
-            const Values v = values(c, u, dh, e);
-            if (kStay) stay = v;
-            acc[1][c] = fused(dh, v.xh, acc[1][c]);
-            add_products(s0, e, v.xh);
-            add_products(s1, u, v.base);
-            add_products(s2, u, v.xh);
-        }
-        const float4 s = row_sums(sum_of(s0), sum_of(s1), sum_of(s2), l.red + turn * l.W, l.W, l.w, l.lane, l.group);
-        turn ^= 1;
-        const float m1 = rx * s.x * inv_d;                      // r_x mean(e xh)
-        const float m2 = r.post ? (s.y - m1 * s.z) * inv_d : 0.f;   // mean(w yh)
-        dx_out.begin(p, r.dx, row);
-        dy_out.begin(p, r.dy, row);
-        if (r.dg.p != nullptr) dg_out.begin(p, r.dg, row);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            Oct u, dh, e;
-            Values v = stay;
-            if (!kStay) v = values(c, u, dh, e);
-            const Oct gamma = vector_at<C, false, kFast>(p, l, 0, c, unit);
-            const Oct t = fused(v.xh, -m1, v.base), f = times(t, v.cg);
-            dx_out.put_row(l, r.dx, c, t);
-            if (token) {
-                acc[0][c] = fused(f, v.yh, acc[0][c]);
-                if (r.dg.p != nullptr) {
-                    Oct g = times(times(t, unit), times(v.yh, gamma));
-                    if (drops) g = chosen(g, bits[c]);
-                    if (r.sigmoid) {
-                        const Oct k = token_gate(c);
-                        g = times(g, fused(times(k, -1.f), k, k));
-                    }
-                    dg_out.put_row(l, r.dg, c, g);
-                }
-            } else {
-                acc[0][c] = fused(drops ? chosen(t, bits[c]) : t, v.yh, acc[0][c]);
-            }
-            dy_out.put_row(l, r.dy, c, times(fused(v.yh, -m2, times(f, gamma)), ry));
-        }
-        dx_out.end(l, r.dx);
-        dy_out.end(l, r.dy);
-        dg_out.end(l, r.dg);
-    }
-    if (p.partial != nullptr) {
-        copies_wait(0);
-        __syncthreads();
-        float *sums = p.groups > 1 ? reinterpret_cast<float *>(smem) : p.partial + (long long)blockIdx.x * 3 * l.d;
-        const int width = p.groups > 1 ? 256 * C * l.W : l.d;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            Oct of[3] = {acc[0][c], acc[1][c], zeros()};   // of gamma_post, gamma_pre, gate
-            if (!token) {
-                const Oct own = acc[0][c];
-                of[0] = times(own, vector_of<false>(r, 2, l.column(c), unit));
-                if (r.gate == MOSA_GATE_CHANNEL) {
-                    of[2] = times(times(own, unit), vector_of<false>(r, 0, l.column(c), unit));
-                    if (r.sigmoid) {
-                        const Oct k = logistic(vector8(r.gch, l.column(c), l.d));
-                        of[2] = times(of[2], fused(times(k, -1.f), k, k));
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 3; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int col = l.column(c) + 2 * e;
-                    const F2 f = of_two(of[i].v[e]);
-                    if (col < l.d) sums[(l.group * 3 + i) * width + col] = f.x;
-                    if (col + 1 < l.d) sums[(l.group * 3 + i) * width + col + 1] = f.y;
-                }
-        }
-        if (p.groups > 1) {
-            __syncthreads();
-            for (int o = threadIdx.x; o < 3 * l.d; o += blockDim.x) {
-                const int i = o / l.d, col = o - i * l.d;
-                float sum = 0.f;
-                for (int g = 0; g < p.groups; ++g) sum += sums[(g * 3 + i) * width + col];
-                p.partial[(long long)blockIdx.x * 3 * l.d + o] = sum;
-            }
-        }
-    }
-}
 
 // The sums over tokens from the blocks': 32 columns a block, 32 runs of blocks each, in a fixed order.
 __global__ void __launch_bounds__(1024) residual_sums_kernel(const float *partial, int blocks, int d,
@@ -230,15 +25,6 @@ __global__ void __launch_bounds__(1024) residual_sums_kernel(const float *partia
     }
 }
 
-template <class Ty>
-cudaError_t go(const Args &p, int blocks, int times, int bytes, cudaStream_t s) {
-    const auto kernel = times == 1 ? residual_bwd_kernel<1, Ty> : residual_bwd_kernel<2, Ty>;
-    cudaError_t e = allow_smem((const void *)kernel, kSmem);
-    if (e != cudaSuccess) return e;
-    note_launches(1);
-    return launch_pdl(kernel, dim3(blocks), dim3(p.warps * p.groups * 32), bytes, s, p);
-}
-
 }  // namespace
 
 size_t residual_workspace(const Residual &r) {
@@ -252,14 +38,8 @@ cudaError_t launch_residual_bwd(const Residual &r, float *partial, cudaStream_t 
     p.partial = sums ? partial : nullptr;
     int blocks, times, bytes;
     shape(p, true, &blocks, &times, &bytes);
-    const int x = r.x.wide, y = r.y.wide, dh = r.dh.p != nullptr && r.dh.wide, st = r.storage_wide;
-    cudaError_t e;
-    if (!fast(p) || (st && !(x && y && dh))) e = go<Types<-1, -1, -1, -1>>(p, blocks, times, bytes, s);
-    else if (st) e = go<Types<1, 1, 1, 1>>(p, blocks, times, bytes, s);
-    else if (x) e = y ? dh ? go<Types<1, 1, 1, 0>>(p, blocks, times, bytes, s) : go<Types<1, 1, 0, 0>>(p, blocks, times, bytes, s)
-                      : dh ? go<Types<1, 0, 1, 0>>(p, blocks, times, bytes, s) : go<Types<1, 0, 0, 0>>(p, blocks, times, bytes, s);
-    else e = y ? dh ? go<Types<0, 1, 1, 0>>(p, blocks, times, bytes, s) : go<Types<0, 1, 0, 0>>(p, blocks, times, bytes, s)
-               : dh ? go<Types<0, 0, 1, 0>>(p, blocks, times, bytes, s) : go<Types<0, 0, 0, 0>>(p, blocks, times, bytes, s);
+    cudaError_t e = p.most < kWarps ? residual_bwd8(p, blocks, bytes, s)
+                    : times == 1 ? go_by_types<1, kWarps>(p, blocks, bytes, s) : go_by_types<2, kWarps>(p, blocks, bytes, s);
     if (e != cudaSuccess || !sums) return e;
     note_launches(1);
     return launch_pdl(residual_sums_kernel, dim3((3 * r.d + 31) / 32), dim3(1024), 0, s, (const float *)partial,

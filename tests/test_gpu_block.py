@@ -64,6 +64,24 @@ def test_types_of_each_tensor(dt, xt, yt, ht):
     assert got["x"].dtype == xt and got["dx"].dtype == xt and got["h"].dtype == dt and got["dy"].dtype == dt
 
 
+@pytest.mark.parametrize("xt", [BF, F32])
+@pytest.mark.parametrize("yt", [BF, F32])
+@pytest.mark.parametrize("ht", [BF, F32])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_many_rows_of_each_type(dt, xt, yt, ht):
+    """Enough rows for several columns a thread, in both directions."""
+    s, dx_out, dh = inputs(3, 3500, 520, dt, xt, yt, ht, gate="channel", seed=16)
+    check(s, dx_out, dh, sigmoid=True, scale=0.5, dropout=0.1, rng=state())
+
+
+@pytest.mark.parametrize("gate", ["none", "token"])
+@pytest.mark.parametrize("B,T,d", [(2, 5000, 1023), (1, 20000, 300), (2, 9000, 776), (1, 2500, 4096), (1, 2600, 3000)])
+def test_many_rows(B, T, d, gate):
+    s, dx_out, dh = inputs(B, T, d, gate=gate, seed=17)
+    check(s, dx_out, dh, sigmoid=True, dropout=0.1, rng=state())
+    check(s, dx_out, dh, post_norm=False)
+
+
 @pytest.mark.parametrize("post", [True, False])
 @pytest.mark.parametrize("pre", [True, False])
 @pytest.mark.parametrize("gate,sigmoid", [("none", True), ("channel", True), ("token", False)])
