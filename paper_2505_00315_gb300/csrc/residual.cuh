@@ -239,19 +239,18 @@ __device__ __forceinline__ Oct vector8(const Vec &m, int at, int d) {
 __device__ __forceinline__ void row_barrier(int W, int group) {
     asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(W * 32) : "memory");
 }
-// Sums over the threads of a row's W warps (1, 2, 4, 8 or 16), in every thread and in an order that is
-// always the same.  `red` holds the warps' sums: each lane reads one of them, the W of them as often as
-// there are lanes for, and what comes out too often is divided by that power of two, exactly.
+// Sums over the threads of a row's W warps (16 at most), in every thread and in an order that is always the
+// same.  `red` holds the warps' sums; each lane reads one of them.
 __device__ __forceinline__ float row_sum(float v, float4 *red, int W, int w, int lane, int group) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     if (W == 1) return v;
     if (lane == 0) red[w].x = v;
     row_barrier(W, group);
-    v = red[lane & (W - 1)].x;
+    v = (lane & 15) < W ? red[lane & 15].x : 0.f;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v * (W * 0.0625f);
+    return v;
 }
 // Of three values: lanes first share out which of them they add up (a quarter of the warp each).
 __device__ __forceinline__ float4 row_sums(float a, float b, float c, float4 *red, int W, int w, int lane, int group) {
@@ -265,11 +264,10 @@ __device__ __forceinline__ float4 row_sums(float a, float b, float c, float4 *re
         const int which = lane >> 3, from = lane & 7;
         if (from == 0) reinterpret_cast<float *>(red + w)[which] = u;
         row_barrier(W, group);
-        u = reinterpret_cast<const float *>(red + (from & (W - 1)))[which];
-        if (W == 16) u += reinterpret_cast<const float *>(red + from + 8)[which];
+        u = from < W ? reinterpret_cast<const float *>(red + from)[which] : 0.f;
+        if (from + 8 < W) u += reinterpret_cast<const float *>(red + from + 8)[which];
 #pragma unroll
         for (int o = 4; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
-        u *= min(W, 8) * 0.125f;
     }
     return make_float4(__shfl_sync(0xffffffffu, u, 0), __shfl_sync(0xffffffffu, u, 8), __shfl_sync(0xffffffffu, u, 16), 0.f);
 }
@@ -426,19 +424,23 @@ __device__ __forceinline__ Oct vector_at(const Args &p, const Place &l, int whic
 // 16, which spill: 74, 537 and 29).
 inline int times_of(const Residual &r, bool backward, int *most) {
     const long long rows = (long long)r.B * r.T;
+    auto warps = [&](int times) { return (r.d + 256 * times - 1) / (256 * times); };
     *most = kWarps;
     if (backward) {
-        int W = 1;
-        while (W * 512 < r.d) W *= 2;
-        if (W <= kWarps / 2 && r.d > 256 && rows * W >= kSms * 8 * 16) {
+        // (how much of a block's threads and of their columns a row's width leaves at work)
+        auto used = [&](int times, int of) {
+            const int W = warps(times), G = of / W;
+            return G == 0 ? 0.0 : (double)r.d / (256 * times * W) * (G * W) / of;
+        };
+        if (r.d > 256 && warps(2) <= kWarps / 2 && rows * warps(2) >= kSms * 8 * 16 && used(2, kWarps / 2) >= 0.95 * used(1, kWarps)) {
             *most = kWarps / 2;
             return 2;
         }
-        return 256 * kWarps < r.d ? 2 : 1;
+        return warps(1) > kWarps ? 2 : 1;
     }
     int times = r.gate == MOSA_GATE_TOKEN ? 2 : 4;
-    while (times > 1 && rows * ((r.d + 256 * times - 1) / (256 * times)) < kSms * kWarps) times /= 2;
-    while (256 * times * kWarps < r.d) times *= 2;
+    while (times > 1 && rows * warps(times) < kSms * kWarps) times /= 2;
+    while (warps(times) > kWarps) times *= 2;
     return times;
 }
 
@@ -457,11 +459,9 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
     }
     if (r.T == 1 && !p.flat)
         for (Rows *m : all) m->t = 0;
-    p.warps = 1;
     const int each = times_of(r, backward, &p.most);
-    while (p.warps * 256 * each < r.d) p.warps *= 2;
-    *times = (r.d + p.warps * 256 - 1) / (p.warps * 256);
-    if (*times == 3) *times = 4;
+    p.warps = (r.d + 256 * each - 1) / (256 * each);
+    *times = (r.d + 256 * p.warps - 1) / (256 * p.warps);   // (no more than the width asks for)
     const Rows *in[kIn] = {&r.x, &r.y, &r.dxo, &r.dh, &r.g};
     p.stage_bytes = 0;
     for (int i = 0; i < kIn; ++i) {

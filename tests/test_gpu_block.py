@@ -75,7 +75,8 @@ def test_many_rows_of_each_type(dt, xt, yt, ht):
 
 
 @pytest.mark.parametrize("gate", ["none", "token"])
-@pytest.mark.parametrize("B,T,d", [(2, 5000, 1023), (1, 20000, 300), (2, 9000, 776), (1, 2500, 4096), (1, 2600, 3000)])
+@pytest.mark.parametrize("B,T,d", [(2, 5000, 1023), (1, 20000, 300), (2, 9000, 776), (1, 2500, 4096), (1, 2600, 3000),
+                                   (1, 1300, 8192), (1, 2100, 5120), (2, 9000, 1536)])
 def test_many_rows(B, T, d, gate):
     s, dx_out, dh = inputs(B, T, d, gate=gate, seed=17)
     check(s, dx_out, dh, sigmoid=True, dropout=0.1, rng=state())
