@@ -1,11 +1,12 @@
 """A small language model whose attention layers run on this library: window heads (norm and
 rotation of queries and keys, sliding-window attention with sinks), beside them MoSA heads
-if asked for, trained on a made-up language and then continued token by token through
-the decoding step's ring caches.
+if asked for, the residual steps between layers (norms, gate, dropout, sum) and the loss, trained on a
+made-up language and then continued token by token through the decoding step's ring caches.
 
     python examples/window_lm.py                # window heads: trains, then generates
     python examples/window_lm.py --mosa 4       # 4 MoSA heads beside them (trains only: expert
                                                 # choice looks at whole sequences)
+    python examples/window_lm.py --dropout 0.1  # with dropout in the residual steps
 
 The language: a sentence repeats its own first ``period`` random tokens, so that each later token
 is found ``period`` tokens back, inside the window.
@@ -71,13 +72,58 @@ class MosaHeads(torch.autograd.Function):
         return (g["dX"].to(X.dtype), g["dW_r"], g["dW_q"], g["dW_k"], g["dW_v"], g["dW_o"], None)
 
 
-class Layer(torch.nn.Module):
-    """Pre-norm attention layer: H window heads on Hkv key / value heads, and n_mosa MoSA heads."""
+class ResidualStep(torch.autograd.Function):
+    """x, y -> x + gate * dropout(norm(y)) and its norm, the next layer's input in bf16; ``norm_y`` False: y as
+    it is.  ``drop``: probability, random state and site of the dropout."""
 
-    def __init__(self, d, H, Hkv, hp, window, sinks, n_mosa=0, k=16):
+    @staticmethod
+    def forward(ctx, x, y, gate, gamma_post, gamma_pre, norm_y, drop):
+        p, rng, site = drop
+        ctx.kw = dict(post_norm=norm_y, dropout=p, site=site)
+        state = rng.clone() if p > 0 else None   # (what it holds now: the backward's words are the same)
+        x_out, h, stats = mosa.mosa_residual_forward(x, y, gate, gamma_post, gamma_pre, rng=state, **ctx.kw)
+        ctx.save_for_backward(x, y, gate, gamma_post, gamma_pre, stats, state)
+        return x_out, h
+
+    @staticmethod
+    def backward(ctx, dx_out, dh):
+        x, y, gate, gamma_post, gamma_pre, stats, state = ctx.saved_tensors
+        g, _ = mosa.mosa_residual_backward(x, y, stats, dx_out.contiguous(), dh.contiguous(), gate, gamma_post,
+                                           gamma_pre, rng=state, **ctx.kw)
+
+        def like(name, t):
+            return None if t is None else g[name].to(t.dtype)
+
+        return (g["dx"], g["dy"].to(y.dtype), like("dgate", gate), like("dgamma_post", gamma_post if ctx.kw["post_norm"] else None),
+                like("dgamma_pre", gamma_pre), None, None)
+
+
+class TokenLoss(torch.autograd.Function):
+    """Mean of -log p of the targets (below 0: none)."""
+
+    @staticmethod
+    def forward(ctx, logits, targets):
+        r, _ = mosa.mosa_token_logprobs(logits, targets)
+        n = (targets >= 0).sum().clamp(min=1)
+        ctx.save_for_backward(logits, targets, r["lse"], n)
+        return -r["logp"].sum() / n
+
+    @staticmethod
+    def backward(ctx, g):
+        logits, targets, lse, n = ctx.saved_tensors
+        dlogp = (-g / n).expand(targets.shape).contiguous()
+        return mosa.mosa_token_logprobs_backward(logits, targets, lse, dlogp=dlogp), None
+
+
+class Layer(torch.nn.Module):
+    """Attention layer: H window heads on Hkv key / value heads, and n_mosa MoSA heads, then the residual step to
+    the next layer."""
+
+    def __init__(self, d, H, Hkv, hp, window, sinks, n_mosa=0, k=16, site=0):
         super().__init__()
         self.H, self.Hkv, self.hp, self.window, self.sinks, self.k = H, Hkv, hp, window, sinks, k
-        self.norm = torch.nn.LayerNorm(d)
+        self.site = site
+        self.gate, self.gamma_post, self.gamma_next = (torch.nn.Parameter(torch.ones(d)) for _ in range(3))
         self.qkv = torch.nn.Linear(d, (H + 2 * Hkv) * hp, bias=False)
         self.out = torch.nn.Linear(H * hp, d, bias=False)
         self.gamma_q, self.gamma_k = (torch.nn.Parameter(torch.ones(hp)) for _ in range(2))
@@ -91,43 +137,59 @@ class Layer(torch.nn.Module):
         x = self.qkv(h).unflatten(-1, (self.H + 2 * self.Hkv, self.hp))
         return x.split((self.H, self.Hkv, self.Hkv), dim=-2)
 
-    def forward(self, x):
-        h = self.norm(x).to(torch.bfloat16)
+    def join(self, x, y, drop):
+        """The stream with the layer's output, and the next layer's input."""
+        gate, post, pre = (t.to(torch.bfloat16) for t in (self.gate, self.gamma_post, self.gamma_next))
+        return ResidualStep.apply(x, y, gate, post, pre, True, (*drop, self.site))
+
+    def forward(self, x, h, drop):
         q, k, v = self.split(h)
         q, k = NormRope.apply(q, k, self.gamma_q.to(h.dtype), self.gamma_k.to(h.dtype))
         y = self.out(WindowAttention.apply(q, k, v, self.window, self.sinks).flatten(-2))
         if self.mosa is not None:
             y = y + MosaHeads.apply(h, *self.mosa, self.k)
-        return x + y
+        return self.join(x, y, drop)
 
     def caches(self, B, device):
         """Ring caches of the sinks and the window's tokens."""
         shape = (B, self.Hkv, self.sinks + self.window, self.hp)
         return [torch.empty(shape, device=device, dtype=torch.bfloat16).transpose(1, 2) for _ in range(2)]
 
-    def step(self, x, cache, lens, state):
-        """One new token of each sequence, x [B, d]; lens counts it."""
-        h = self.norm(x).to(torch.bfloat16)
-        q, k, v = self.split(h)
+    def step(self, x, h, cache, lens, state):
+        """One new token of each sequence, x and h [B, 1, d]; lens counts it."""
+        q, k, v = self.split(h[:, 0])
         O, state["ws"] = mosa.mosa_window_decode(
             q, k, v, *cache, lens, self.window, self.sinks, gamma_q=self.gamma_q.to(h.dtype),
             gamma_k=self.gamma_k.to(h.dtype), workspace=state.get("ws"))
-        return x + self.out(O.flatten(-2))
+        return self.join(x, self.out(O.flatten(-2))[:, None], (0.0, None))
 
 
 class Model(torch.nn.Module):
-    def __init__(self, vocab, d=256, layers=2, H=4, Hkv=2, hp=64, window=48, sinks=2, n_mosa=0):
+    def __init__(self, vocab, d=256, layers=2, H=4, Hkv=2, hp=64, window=48, sinks=2, n_mosa=0, dropout=0.0, seed=0):
         super().__init__()
         self.emb = torch.nn.Embedding(vocab, d)
-        self.layers = torch.nn.ModuleList(Layer(d, H, Hkv, hp, window, sinks, n_mosa)
-                                          for _ in range(layers))
+        self.gamma_first = torch.nn.Parameter(torch.ones(d))
+        self.layers = torch.nn.ModuleList(Layer(d, H, Hkv, hp, window, sinks, n_mosa, site=i)
+                                          for i in range(layers))
         self.head = torch.nn.Linear(d, vocab, bias=False)
+        # seed and offset of the dropout: each step takes as many offsets as there are layers
+        self.dropout = dropout
+        self.register_buffer("rng", torch.tensor([seed, 0]))
+
+    def first(self, tokens):
+        """The stream's beginning and the first layer's input: a step from nothing, without a norm of its own."""
+        x = self.emb(tokens)
+        nothing = x.new_zeros(x.shape[-1]).expand(x.shape)
+        return ResidualStep.apply(nothing, x, None, None, self.gamma_first.to(torch.bfloat16), False, (0.0, None, 0))
 
     def forward(self, tokens):
-        x = self.emb(tokens)
+        drop = (self.dropout if self.training else 0.0, self.rng)
+        x, h = self.first(tokens)
         for layer in self.layers:
-            x = layer(x)
-        return self.head(x)
+            x, h = layer(x, h, drop)
+        if drop[0] > 0:
+            self.rng[1] += len(self.layers)
+        return self.head(h)
 
     @torch.no_grad()
     def generate(self, prompt, n):
@@ -139,13 +201,18 @@ class Model(torch.nn.Module):
         out, token = [prompt], prompt[:, 0]
         for t in range(P + n - 1):
             lens += 1
-            x = self.emb(token)
-            for layer, cache, state in zip(self.layers, caches, states):
-                x = layer.step(x, cache, lens, state)
-            token = prompt[:, t + 1] if t + 1 < P else self.head(x).argmax(-1)
+            logits = self.next_logits(token, caches, lens, states)
+            token = prompt[:, t + 1] if t + 1 < P else logits.argmax(-1)
             if t + 1 >= P:
                 out.append(token[:, None])
         return torch.cat(out, 1)
+
+    def next_logits(self, token, caches, lens, states):
+        """Logits [B, vocab] after one new token [B] of each sequence."""
+        x, h = self.first(token[:, None])
+        for layer, cache, state in zip(self.layers, caches, states):
+            x, h = layer.step(x, h, cache, lens, state)
+        return self.head(h[:, 0])
 
 
 def sentences(B, T, period, vocab, gen):
@@ -153,20 +220,19 @@ def sentences(B, T, period, vocab, gen):
     return x.repeat(1, T // period + 1)[:, :T]
 
 
-def main(steps=150, n_mosa=0, seed=0, T=160, period=24, vocab=64, quiet=False):
+def main(steps=150, n_mosa=0, seed=0, T=160, period=24, vocab=64, quiet=False, dropout=0.0):
     """Trains; returns the first and the last loss, and where there are no MoSA heads the share of
     generated tokens that are right and the model's largest difference between its two ways of running."""
     torch.manual_seed(seed)
     gen = torch.Generator(device="cuda").manual_seed(seed)
-    model = Model(vocab, n_mosa=n_mosa).cuda()
+    model = Model(vocab, n_mosa=n_mosa, dropout=dropout, seed=seed).cuda()
     opt = torch.optim.Adam(model.parameters(), lr=2e-3)
     losses = []
     for i in range(steps):
         x = sentences(32, T + 1, period, vocab, gen)
         with torch.autocast("cuda", dtype=torch.bfloat16):
             logits = model(x[:, :-1])
-        loss = torch.nn.functional.cross_entropy(logits[:, period:].float().flatten(0, 1),
-                                                 x[:, period + 1:].flatten())
+        loss = TokenLoss.apply(logits[:, period:], x[:, period + 1:].contiguous())
         opt.zero_grad()
         loss.backward()
         opt.step()
@@ -175,6 +241,7 @@ def main(steps=150, n_mosa=0, seed=0, T=160, period=24, vocab=64, quiet=False):
             print(f"step {i:4d}  loss {losses[-1]:.4f}")
     if n_mosa:
         return losses[0], losses[-1], None, None
+    model.eval()
     x = sentences(8, T, period, vocab, gen)
     with torch.autocast("cuda", dtype=torch.bfloat16):
         got = model.generate(x[:, :2 * period], T - 2 * period)
@@ -186,10 +253,8 @@ def main(steps=150, n_mosa=0, seed=0, T=160, period=24, vocab=64, quiet=False):
             whole = model(x).float()
             for t in range(T):
                 lens += 1
-                h = model.emb(x[:, t])
-                for layer, cache, state in zip(model.layers, caches, states):
-                    h = layer.step(h, cache, lens, state)
-                far = max(far, float((model.head(h).float() - whole[:, t]).norm() / whole[:, t].norm()))
+                one = model.next_logits(x[:, t], caches, lens, states).float()
+                far = max(far, float((one - whole[:, t]).norm() / whole[:, t].norm()))
     if not quiet:
         print(f"generated tokens that are right: {right:.3f}; whole text against token by token: {far:.4f}")
     return losses[0], losses[-1], right, far
@@ -199,5 +264,6 @@ if __name__ == "__main__":
     a = argparse.ArgumentParser()
     a.add_argument("--steps", type=int, default=150)
     a.add_argument("--mosa", type=int, default=0)
+    a.add_argument("--dropout", type=float, default=0.0)
     a = a.parse_args()
-    main(a.steps, a.mosa)
+    main(a.steps, a.mosa, dropout=a.dropout)
