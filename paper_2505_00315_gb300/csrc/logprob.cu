@@ -31,6 +31,7 @@ namespace blk {
 namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32, kSms = 152;
+constexpr int kFewWarps = 4;                    // of a block where rows are many, and of the backward's
 constexpr int kVecs = 4;                        // 16-byte pieces that a lane has under way
 constexpr float kLeast = -0x1p90f;              // this and less is ruled out
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
@@ -389,16 +390,17 @@ __device__ __forceinline__ void finish(const Args &p, long long row, const Part 
 }
 
 // `share` warps of a block take a row together, or all of them a segment of one.
-template <bool kWide, bool kTop>
-__global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_constant__ Args p) {
+// (kOf: warps of a block)
+template <bool kWide, bool kTop, int kOf>
+__global__ void __launch_bounds__(kOf * 32, 32 / kOf) logprob_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int E = kWide ? 4 : 8;
-    __shared__ Key room[kTop ? kWarps : 1][32];
-    __shared__ Part part[kWarps];
+    __shared__ Key room[kTop ? kOf : 1][32];
+    __shared__ Part part[kOf];
     const LogProb &l = p.l;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, mine = warp & (p.share - 1);
     const long long rows = (long long)l.B * l.T;
-    const long long row = p.segments > 1 ? blockIdx.x / p.segments : (long long)blockIdx.x * (kWarps / p.share) + warp / p.share;
+    const long long row = p.segments > 1 ? blockIdx.x / p.segments : (long long)blockIdx.x * (kOf / p.share) + warp / p.share;
     const int segment = p.segments > 1 ? (int)(blockIdx.x - row * p.segments) : 0;
     if (p.share == 1 && row >= rows) return;   // (else to the block's barriers, with nothing)
     int t;
@@ -508,13 +510,13 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 // A warp takes one of the `units` shares of a row.
 template <bool kWide>
-__global__ void __launch_bounds__(kThreads) logprob_bwd_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__(kFewWarps * 32) logprob_bwd_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int E = kWide ? 4 : 8;
     const LogProb &l = p.l;
     const int lane = threadIdx.x & 31;
-    const long long all = (long long)l.B * l.T * p.units, warps = (long long)gridDim.x * kWarps;
-    for (long long unit = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); unit < all; unit += warps) {
+    const long long all = (long long)l.B * l.T * p.units, warps = (long long)gridDim.x * kFewWarps;
+    for (long long unit = (long long)blockIdx.x * kFewWarps + (threadIdx.x >> 5); unit < all; unit += warps) {
         const long long row = unit / p.units;
         const int share = (int)(unit - row * p.units);
         int it;
@@ -525,6 +527,9 @@ __global__ void __launch_bounds__(kThreads) logprob_bwd_kernel(const __grid_cons
         const int from = (int)((long long)steps * share / p.units), to = (int)((long long)steps * (share + 1) / p.units);
         const int col0 = max(z.first + from * step_columns<kWide>(), 0);
         const int col1 = min(z.first + to * step_columns<kWide>(), l.V);
+
+        Piece cur[kVecs];   // (under way while the row's gradients arrive)
+        if (from < to) z.load_step(from, lane, cur);
 
         // The row's gradients.
         long long target = -1;
@@ -569,8 +574,6 @@ __global__ void __launch_bounds__(kThreads) logprob_bwd_kernel(const __grid_cons
         const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(z.p)) & 15) == 0;
         const Pair scale2 = both(l.scale), minus = both(-ref), to2 = both(kLog2e);
         const Pair A2 = both(A), B2 = both(B);
-        Piece cur[kVecs];
-        if (from < to && !zero) z.load_step(from, lane, cur);
         for (int i = from; i < to; ++i) {
             Piece next[kVecs];
             if (i + 1 < to && !zero) z.load_step(i + 1, lane, next);
@@ -641,29 +644,38 @@ int steps_of(const LogProb &l) {   // (as if a row started at a multiple of 16 b
     return (int)(((long long)l.V + K - 1) / K);
 }
 
-// Forward: how many warps of a block share a row, and how many blocks.  As few as make two rounds of
-// all SMs' warps, so that the last one, which leaves SMs idle, is short; as many as have some steps each.  us
-// with 1, 2, 4, 8 warps a row (bf16, no alternatives / 5): 4096 rows of 50001 entries 82, 74, 74, 76 / 145, 119, 103,
-// 118 (before the steps' largest were noted three deep), 1000 of 32003 -, -, -, 18 / -, -, -, 28.
-// More blocks than one cost a second kernel: 300 rows of 32003 take 5.9 us with one, 7.2 with two; 100 rows of
-// 131072 8.2 with six.
-void split(const LogProb &l, int *share, int *segments) {
+// Forward: warps of a block, how many of them share a row, and how many blocks do.  As few warps a row as make
+// two rounds of all SMs' warps, so that the last one, which leaves SMs idle, is short; as many as have some
+// steps each.  Small blocks wait for fewer of their warps, large ones share a row between more.  us in blocks of 4 / 8
+// (bf16, no alternatives; 5; 20):
+//     4096 rows of 50001   72 / 73    103 / 108   130 / 130
+//     1024 of 131072       48 / 51     60 / 67     83 / 70
+//     1000 of 32003        16 / 18     22 / 28     39 / 31
+//     300 of 32003          7 / 6      14 / 10     17 / 12
+// More blocks a row than one cost a second kernel: 300 rows of 32003 took 7.2 us with two, 5.9 with one.
+struct Split {
+    int of, share, segments;
+};
+Split split(const LogProb &l) {
     const long long rows = (long long)l.B * l.T, all = 32LL * kSms;
     // (counted alike for both types and places, so that the workspace's size does not hang on a pointer)
     const long long steps = ((long long)l.V + 1023) / 1024;
-    *share = *segments = 1;
-    while (*share < kWarps && rows * *share < 2 * all && steps >= 4 * *share) *share *= 2;
-    if (*share < kWarps) return;
+    Split p{rows * kFewWarps * 4 >= 3 * all ? kFewWarps : kWarps, 1, 1};
+    while (p.share < p.of && rows * p.share < 2 * all && steps >= 4 * p.share) p.share *= 2;
+    if (p.share < kWarps) return p;
     const long long n = std::min(std::min(32LL, steps / kWarps), all / (rows * kWarps));
-    if (n >= 3) *segments = (int)n;
+    if (n >= 3) p.segments = (int)n;
+    return p;
 }
 
 template <bool kWide, bool kTop>
-cudaError_t launch(const Args &p, cudaStream_t s) {
-    const long long rows = (long long)p.l.B * p.l.T, per = kWarps / p.share;
+cudaError_t launch(const Args &p, int of, cudaStream_t s) {
+    const long long rows = (long long)p.l.B * p.l.T, per = of / p.share;
     const unsigned blocks = (unsigned)(p.segments > 1 ? rows * p.segments : (rows + per - 1) / per);
     note_launches(1);
-    cudaError_t e = launch_pdl(logprob_kernel<kWide, kTop>, dim3(blocks), dim3(kThreads), 0, s, p);
+    cudaError_t e = of == kWarps
+                        ? launch_pdl(logprob_kernel<kWide, kTop, kWarps>, dim3(blocks), dim3(kThreads), 0, s, p)
+                        : launch_pdl(logprob_kernel<kWide, kTop, kFewWarps>, dim3(blocks), dim3(kFewWarps * 32), 0, s, p);
     if (e != cudaSuccess || p.segments == 1) return e;
     note_launches(1);
     return launch_pdl(logprob_join_kernel<kWide, kTop>, dim3((unsigned)rows), dim3(kThreads), 0, s, p);
@@ -679,31 +691,33 @@ Args args_of(const LogProb &l) {
 }  // namespace
 
 size_t logprob_workspace(const LogProb &l) {
-    int share, segments;
-    split(l, &share, &segments);
+    const int segments = split(l).segments;
     const size_t n = segments > 1 ? (size_t)l.B * l.T * segments : 0;
     return 256 + (n + 15) / 16 * 256 + (l.top > 0 ? n * 32 * sizeof(Key) : 0);
 }
 
 cudaError_t launch_logprob(const LogProb &l, void *ws, cudaStream_t s) {
     Args p = args_of(l);
-    split(l, &p.share, &p.segments);
+    const Split by = split(l);
+    p.share = by.share;
+    p.segments = by.segments;
     const size_t n = (size_t)l.B * l.T * p.segments;
     p.parts = reinterpret_cast<Part *>(static_cast<char *>(ws) + 256);
     p.tops = reinterpret_cast<Key *>(static_cast<char *>(ws) + 256 + (n + 15) / 16 * 256);
-    if (l.z.wide) return l.top > 0 ? launch<true, true>(p, s) : launch<true, false>(p, s);
-    return l.top > 0 ? launch<false, true>(p, s) : launch<false, false>(p, s);
+    if (l.z.wide) return l.top > 0 ? launch<true, true>(p, by.of, s) : launch<true, false>(p, by.of, s);
+    return l.top > 0 ? launch<false, true>(p, by.of, s) : launch<false, false>(p, by.of, s);
 }
 
 cudaError_t launch_logprob_bwd(const LogProb &l, cudaStream_t s) {
     Args p = args_of(l);
-    p.units = std::max(1, steps_of(l) / 4);
+    // (eight steps a warp, as far as they go: 313 us for 16384 rows of 32768 bf16, 322 with four, 329 with four in
+    // blocks of 8 warps)
+    p.units = std::max(1, steps_of(l) / 8);
     const long long units = (long long)l.B * l.T * p.units;
-    const long long blocks = std::min<long long>((units + kWarps - 1) / kWarps, 1 << 20);
+    const unsigned blocks = (unsigned)std::min<long long>((units + kFewWarps - 1) / kFewWarps, 1 << 20);
     note_launches(1);
-    if (l.z.wide)
-        return launch_pdl(logprob_bwd_kernel<true>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p);
-    return launch_pdl(logprob_bwd_kernel<false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p);
+    return l.z.wide ? launch_pdl(logprob_bwd_kernel<true>, dim3(blocks), dim3(kFewWarps * 32), 0, s, p)
+                    : launch_pdl(logprob_bwd_kernel<false>, dim3(blocks), dim3(kFewWarps * 32), 0, s, p);
 }
 
 }  // namespace blk
