@@ -20,7 +20,7 @@ namespace blk {
 constexpr int kWarps = 16, kThreads = kWarps * 32, kSms = 152;
 constexpr int kIn = 5;              // tensors that may arrive: x, y, dx_out, dh, a gate per token
 constexpr int kMaxStages = 4;
-constexpr int kSmem = 220 * 1024;
+constexpr int kSmem = 227 * 1024;   // what a block may have
 constexpr int kScratch = 1024;      // bytes of a warp: 256 columns on their way out
 
 struct Args {
@@ -35,9 +35,9 @@ struct Args {
 };
 
 // Which of the tensors are fp32: 0 or 1, or -1 where that is only known at run time.  Such kernels
-// also take rows of any place, stride and number of columns; those of known types take rows of whole
-// 16-byte pieces, one stride apart, and have gammas and gate in shared memory: no branch stands
-// between their loads.
+// also take rows of any place, stride and number of columns (16-byte pieces arrive as they lie in memory,
+// and what is read from them is shifted); those of known types take rows of whole pieces, one stride
+// apart, and have gammas and gate in shared memory: no branch stands between their loads.
 template <int kX, int kY, int kDh, int kStorage>
 struct Types {
     static constexpr bool kFast = kX >= 0;
@@ -53,6 +53,10 @@ __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+// `bytes` of them from src, the others 0.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // All but the last n rounds of copies have arrived.
 __device__ __forceinline__ void copies_wait(int n) {
@@ -65,32 +69,6 @@ __device__ __forceinline__ void copies_wait(int n) {
 // 256 columns of a warp in shared memory: 16-byte pieces in order, those of fp32 with every second run
 // of eight swapped in pairs, so that lanes that read two neighbouring pieces each meet no bank twice.
 __device__ __forceinline__ int piece_at(int j) { return 16 * (j ^ ((j >> 3) & 1)); }
-
-// The columns [col, col + 256) of a row, as far as there are any, value by value (the others are 0).
-__device__ __forceinline__ void fetch_values(int wide, const char *row, int col, int d, char *to, int lane) {
-    if (wide) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int at = col + 32 * i + lane;
-            v[i] = at < d ? reinterpret_cast<const float *>(row)[at] : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = 32 * i + lane;
-            *reinterpret_cast<float *>(to + piece_at(e >> 2) + 4 * (e & 3)) = v[i];
-        }
-    } else {
-        unsigned short v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int at = col + 32 * i + lane;
-            v[i] = at < d ? reinterpret_cast<const unsigned short *>(row)[at] : (unsigned short)0;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) *reinterpret_cast<unsigned short *>(to + 2 * (32 * i + lane)) = v[i];
-    }
-}
 
 // Eight values in pairs.
 struct Oct {
@@ -135,6 +113,11 @@ __device__ __forceinline__ Oct zeros() {
     MOSA_OCT r.v[e] = 0;
     return r;
 }
+__device__ __forceinline__ Oct all_of(float v) {
+    Oct r;
+    MOSA_OCT r.v[e] = both(v);
+    return r;
+}
 // The values whose bit is set; 0 for the others, whatever they are.
 __device__ __forceinline__ Oct chosen(const Oct &a, uint32_t bits) {
     Oct r;
@@ -162,6 +145,36 @@ __device__ __forceinline__ Oct take(const char *from, int wide, int lane) {
     const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(from + at);
     const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(from + (at ^ 16));
     r.v[0] = a.x; r.v[1] = a.y; r.v[2] = b.x; r.v[3] = b.y;
+    return r;
+}
+// The same, c times 256 columns on, of a row whose columns begin `shift` bytes into the first piece.
+__device__ __forceinline__ Oct take_shifted(const char *from, int wide, int lane, int c, int shift) {
+    uint32_t w[12];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        if (i == 2 && !wide) break;
+        const int j = wide ? 64 * c + 2 * lane + i : 32 * c + lane + i;
+        const uint4 a = *reinterpret_cast<const uint4 *>(from + (wide ? piece_at(j) : 16 * j));
+        w[4 * i] = a.x; w[4 * i + 1] = a.y; w[4 * i + 2] = a.z; w[4 * i + 3] = a.w;
+    }
+    const int n = wide ? 12 : 8;
+    if (shift & 4) {
+#pragma unroll
+        for (int i = 0; i < 11; ++i) w[i] = i + 1 < n ? w[i + 1] : 0u;
+    }
+    if (shift & 8) {
+#pragma unroll
+        for (int i = 0; i < 10; ++i) w[i] = i + 2 < n ? w[i + 2] : 0u;
+    }
+    if (!wide) {
+        if (shift & 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+        return unpacked(make_uint4(w[0], w[1], w[2], w[3]));
+    }
+    Oct r;
+    MOSA_OCT r.v[e] = two(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
     return r;
 }
 __device__ __forceinline__ void keep(char *to, int lane, const Oct &v) {   // as fp32
@@ -346,20 +359,29 @@ struct Arrival {
             next += (uint64_t)l.step * (uint32_t)m.t;
             return;
         }
-        const char *src = row_at(p, m, row);
-        if (!m.vec) {
+        // The 16-byte pieces in which the columns lie (device memory is allocated in larger ones, so the bytes
+        // before the first column are there to be read), up to the row's end; the others hold 0.
+        const char *src = row_at(p, m, row), *end = src + (m.wide ? 4 : 2) * l.d;
+        src += (m.wide ? 4 : 2) * l.col0;
+        src -= reinterpret_cast<uintptr_t>(src) & 15;
+        const int pieces = (m.wide ? 64 : 32) * C + (m.vec ? 0 : 1);
 #pragma unroll 1
-            for (int c = 0; c < C; ++c) fetch_values(m.wide, src, l.col0 + 256 * c, l.d, l.ring + (to - l.ring32) + bytes_of(m.wide, c), l.lane);
-            return;
-        }
-#pragma unroll 1
-        for (int i = 0; i < (m.wide ? 2 * C : C); ++i) {
-            const int col = l.col0 + (m.wide ? 128 * i + 4 * l.lane : 256 * i + 8 * l.lane);
-            if (col < l.d)
-                copy16(to + 512 * i + (m.wide ? piece_at(l.lane) : 16 * l.lane), src + (m.wide ? 4 : 2) * col);
+        for (int j = l.lane; j < pieces; j += 32) {
+            const long long left = end - (src + 16 * j);
+            copy16(to + (m.wide ? piece_at(j) : 16 * j), left > 0 ? src + 16 * j : src, (int)max(0LL, min(left, 16LL)));
         }
     }
+    // How far into the first piece the warp's columns of a row begin (-1: pieces are whole).
+    __device__ __forceinline__ int shift(const Args &p, const Place &l, const Rows &m, uint32_t row) const {
+        if (kFast || m.vec) return -1;
+        return (int)(reinterpret_cast<uintptr_t>(row_at(p, m, row) + (m.wide ? 4 : 2) * l.col0) & 15);
+    }
 };
+// The lane's eight columns, c times 256 on, of what has arrived at `from`.
+template <bool kFast>
+__device__ __forceinline__ Oct arrived(const char *from, int wide, const Place &l, int c, int shift) {
+    return kFast || shift < 0 ? take(from + bytes_of(wide, c), wide, l.lane) : take_shifted(from, wide, l.lane, c, shift);
+}
 
 // Rows of one tensor that leave.
 template <int C, bool kFast, int kWide>
@@ -386,7 +408,7 @@ __device__ __forceinline__ void clear_ring(const Place &l) {
 }
 
 // Eight columns of one of the vectors: 0 gamma_post, 1 gamma_pre, 2 the channels' gate times c (1 times c where there
-// is none); the forward's 0 is the product of 0 and 2.
+// is none, which is not kept); the forward's 0 is the product of 0 and 2.
 template <bool kForward>
 __device__ __forceinline__ Oct vector_of(const Residual &r, int which, int col, float unit) {
     Oct v = vector8(which == 0 ? r.gpost : which == 1 ? r.gpre : r.gch, col, r.d);
@@ -398,11 +420,16 @@ __device__ __forceinline__ Oct vector_of(const Residual &r, int which, int col, 
     return which == 0 ? times(v, k) : k;
 }
 
+// How many vectors a block keeps.
+__host__ __device__ __forceinline__ int vectors_of(const Residual &r, bool backward) {
+    return backward && r.gate == MOSA_GATE_CHANNEL ? 3 : 2;
+}
+
 // All vectors to shared memory, the warps sharing the work.
 template <int C, bool kForward>
 __device__ __forceinline__ void hold(const Args &p, const Place &l, float unit) {
     const int n = C * l.W;   // 256 columns each
-    for (int i = l.warp; i < (kForward ? 2 : 3) * n; i += l.nwarps) {
+    for (int i = l.warp; i < vectors_of(p.r, !kForward) * n; i += l.nwarps) {
         const int which = i / n, k = i - which * n;
         keep(l.held + i * 1024, l.lane, vector_of<kForward>(p.r, which, k * 256 + 8 * l.lane, unit));
     }
@@ -462,16 +489,20 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
     const int each = times_of(r, backward, &p.most);
     p.warps = (r.d + 256 * each - 1) / (256 * each);
     *times = (r.d + 256 * p.warps - 1) / (256 * p.warps);   // (no more than the width asks for)
+    // (a piece more where one may be cut by a row's beginning)
+    bool vec = true;
+    for (const Rows *m : all) vec = vec && (m->p == nullptr || m->vec);
+    const int slack = vec ? 0 : 16;
     const Rows *in[kIn] = {&r.x, &r.y, &r.dxo, &r.dh, &r.g};
     p.stage_bytes = 0;
     for (int i = 0; i < kIn; ++i) {
         // (in the backward, zeros stand for a gradient that is not there: dx_out's like x)
         const int wide = i == 2 ? r.x.wide : in[i]->wide;
         p.off[i] = p.stage_bytes;
-        if (in[i]->p != nullptr || (backward && (i == 2 || i == 3))) p.stage_bytes += *times * (wide ? 1024 : 512);
+        if (in[i]->p != nullptr || (backward && (i == 2 || i == 3))) p.stage_bytes += bytes_of(wide, *times) + slack;
     }
     // As many rows as the block has warps for, but blocks for all SMs first, and two stages at least.
-    const int vectors = (backward ? 3 : 2) * *times * p.warps * 1024;
+    const int vectors = vectors_of(r, backward) * *times * p.warps * 1024;
     p.groups = (int)std::min<long long>(p.most / p.warps, std::max(1LL, rows / kSms));
     for (;; --p.groups) {
         const int nwarps = p.warps * p.groups, fixed = nwarps * (kScratch + 2 * 16);

@@ -95,8 +95,10 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         slot = slot == ahead ? 0 : slot + 1;
         const int xw = wide_of(Ty::x, r.x), yw = wide_of(Ty::y, r.y), hw = wide_of(Ty::dh, r.dh);
         const int gw = wide_of(Ty::storage, r.g);
+        const int xs = x_in.shift(p, l, r.x, row), ys = y_in.shift(p, l, r.y, row), gs = token ? g_in.shift(p, l, r.g, row) : -1;
+        const int dxos = has_dxo ? dxo_in.shift(p, l, r.dxo, row) : -1, dhs = has_dh ? dh_in.shift(p, l, r.dh, row) : -1;
         auto token_gate = [&](int c) {
-            const Oct g = take(in + g_off + bytes_of(gw, c), gw, l.lane);
+            const Oct g = arrived<kFast>(in + g_off, gw, l, c, gs);
             return r.sigmoid ? logistic(g) : g;
         };
         // What both rounds need, from what the ring holds.
@@ -105,11 +107,12 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         };
         auto values = [&](int c, Oct &u, Oct &dh, Oct &e) {
             Values v;
-            const Oct y = take(in + y_off + bytes_of(yw, c), yw, l.lane);
-            const Oct x = take(in + bytes_of(xw, c), xw, l.lane);
-            const Oct dxo = take(in + dxo_off + bytes_of(xw, c), xw, l.lane);
-            dh = take(in + dh_off + bytes_of(hw, c), hw, l.lane);
-            v.cg = token ? times(token_gate(c), unit) : vector_at<C, false, kFast>(p, l, 2, c, unit);
+            const Oct y = arrived<kFast>(in + y_off, yw, l, c, ys);
+            const Oct x = arrived<kFast>(in, xw, l, c, xs);
+            const Oct dxo = arrived<kFast>(in + dxo_off, xw, l, c, dxos);
+            dh = arrived<kFast>(in + dh_off, hw, l, c, dhs);
+            v.cg = token ? times(token_gate(c), unit)
+                   : r.gate == MOSA_GATE_NONE ? all_of(unit) : vector_at<C, false, kFast>(p, l, 2, c, unit);
             v.yh = times(y, ry);
             if (drops) {
                 v.cg = chosen(v.cg, bits[c]);

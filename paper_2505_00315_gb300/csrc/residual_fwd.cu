@@ -61,7 +61,8 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
         const char *in = l.ring + slot * p.stage_bytes;
         slot = slot == ahead ? 0 : slot + 1;
         const int xw = wide_of(Ty::x, r.x), yw = wide_of(Ty::y, r.y);
-        auto y_at = [&](int c) { return take(in + y_off + bytes_of(yw, c), yw, l.lane); };
+        const int xs = x_in.shift(p, l, r.x, row), ys = y_in.shift(p, l, r.y, row), gs = token ? g_in.shift(p, l, r.g, row) : -1;
+        auto y_at = [&](int c) { return arrived<kFast>(in + y_off, yw, l, c, ys); };
         float ry = 1.f, rx = 1.f;
         if (r.post) {
             Pair s = 0;
@@ -81,17 +82,17 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
                 Oct u = times(y_at(c), times(vector_at<C, true, kFast>(p, l, 0, c, unit), ry));
                 if (token) {
                     const int gw = wide_of(Ty::storage, r.g);
-                    const Oct g = take(in + g_off + bytes_of(gw, c), gw, l.lane);
+                    const Oct g = arrived<kFast>(in + g_off, gw, l, c, gs);
                     u = times(u, r.sigmoid ? logistic(g) : g);
                 }
-                x[c] = plus(take(in + bytes_of(xw, c), xw, l.lane), chosen(u, bits[c]));
+                x[c] = plus(arrived<kFast>(in, xw, l, c, xs), chosen(u, bits[c]));
                 add_products(s, x[c], x[c]);
             }
         } else {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 x[c] = fused(y_at(c), times(vector_at<C, true, kFast>(p, l, 0, c, unit), ry),
-                             take(in + bytes_of(xw, c), xw, l.lane));
+                             arrived<kFast>(in, xw, l, c, xs));
                 add_products(s, x[c], x[c]);
             }
         }
