@@ -94,7 +94,7 @@ class ResidualStep(torch.autograd.Function):
         def like(name, t):
             return None if t is None else g[name].to(t.dtype)
 
-        return (g["dx"], g["dy"].to(y.dtype), like("dgate", gate), like("dgamma_post", gamma_post if ctx.kw["post_norm"] else None),
+        return (g["dx"], g["dy"].to(y.dtype), like("dgate", gate), like("dgamma_post", gamma_post),
                 like("dgamma_pre", gamma_pre), None, None)
 
 

@@ -49,6 +49,7 @@ def declare(L) -> None:
         f.argtypes, f.restype = args, ret
 
 
+# What depends on shapes, strides, types and numbers alone is done once and kept as a plan, as for the window heads.
 # Calls make and look for everything on the current device and its current stream; one whose tensors lie on
 # another device, or that names a stream, is made again in that one's place.
 
@@ -99,10 +100,6 @@ def _rows(t, name, like=None, dtype=None):
 def _result(t, name, like, dtype):
     """Strides of a result: a given tensor's, or those of the one to be made."""
     return MosaStrides(like[1] * like[2], like[2], 0) if t is None else _rows(t, name, like, dtype)
-
-
-def _made(t, like, dtype, device):
-    return _b._torch_mod.empty(like, dtype=dtype, device=device) if t is None else t
 
 
 def _check_rng(rng, dropout):
@@ -170,7 +167,7 @@ def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmo
         _vector(dgpost, "dgamma_post", (d,), torch.float32)
         _vector(dgpre, "dgamma_pre", (d,), torch.float32)
         need = int(_b.load().mosa_residual_workspace_bytes(ctypes.byref(s)))
-    return ctypes.byref(s), need, s, dtype
+    return ctypes.byref(s), need, s, (dtype, x.device, x.shape, (2, B, T))
 
 
 def _options(post_norm, pre_norm, sigmoid, scale, eps, dropout, site):
@@ -201,9 +198,12 @@ def mosa_residual_forward(x, y, gate=None, gamma_post=None, gamma_pre=None, post
                 and type(post_norm) is type(pre_norm) is type(sigmoid) is bool):
             post_norm, pre_norm, sigmoid, scale, eps, dropout, site = _options(post_norm, pre_norm, sigmoid, scale, eps,
                                                                                dropout, site)
-        key = (6, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype, _sig(gate), _sig(gamma_post),
-               _sig(gamma_pre), post_norm, pre_norm, sigmoid, scale, eps, dropout, site, dtype, _sig(rng),
-               (_sig(xo), _sig(h), _sig(stats)) if out else None)
+        key = (6, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype,
+               None if gate is None else (gate.shape, gate.stride(), gate.dtype),
+               None if gamma_post is None else (gamma_post.shape, gamma_post.stride(), gamma_post.dtype),
+               None if gamma_pre is None else (gamma_pre.shape, gamma_pre.stride(), gamma_pre.dtype),
+               None if rng is None else (rng.shape, rng.stride(), rng.dtype), post_norm, pre_norm, sigmoid, scale, eps,
+               dropout, site, dtype, dev, (_sig(xo), _sig(h), _sig(stats)) if out else None)
     except AttributeError:
         _bad(("x", x), ("y", y), ("gate", gate), ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng))
     plan = _plans.get(key) or _keep(key, _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
@@ -214,20 +214,20 @@ def mosa_residual_forward(x, y, gate=None, gamma_post=None, gamma_pre=None, post
             and (out is None or _all_on(dev, xo, h, stats))):
         _elsewhere(dev, ("x", x), ("y", y), ("gate", gate), ("gamma_post", gamma_post), ("gamma_pre", gamma_pre),
                    ("rng", rng), ("out x", xo), ("out h", h), ("stats", stats))
-    dt = plan[3]
+    dt, device, shape, short = plan[3]
     if xo is None:
-        xo = _new(x)
+        xo = torch.empty_like(x) if x.is_contiguous() else torch.empty(shape, dtype=x.dtype, device=device)
     if not pre_norm:
         h = None
     elif h is None:
-        h = _new(x) if dt is x.dtype else torch.empty(x.shape, dtype=dt, device=x.device)
+        h = torch.empty_like(xo) if dt is x.dtype and out is None else torch.empty(shape, dtype=dt, device=device)
     if stats is None:
-        stats = torch.empty((2, *x.shape[:2]), dtype=torch.float32, device=x.device)
-    rc = _b.load().mosa_residual_forward(
+        stats = torch.empty(short, dtype=torch.float32, device=device)
+    rc = (_b._lib or _b.load()).mosa_residual_forward(
         plan[0], x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
         None if gamma_post is None else gamma_post.data_ptr(), None if gamma_pre is None else gamma_pre.data_ptr(),
         None if rng is None else rng.data_ptr(), xo.data_ptr(), None if h is None else h.data_ptr(),
-        stats.data_ptr(), _b._stream(None))
+        stats.data_ptr(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _b._check(rc, "mosa_residual_forward")
     return xo, h, stats
@@ -258,9 +258,14 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
                                                                                dropout, site)
         if not pre_norm:
             dh = None
-        key = (7, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype, _sig(gate), _sig(gamma_post),
-               _sig(gamma_pre), post_norm, pre_norm, sigmoid, scale, eps, dropout, site, dtype, _sig(rng),
-               stats.shape, stats.stride(), stats.dtype, _sig(dx_out), _sig(dh),
+        key = (7, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype,
+               None if gate is None else (gate.shape, gate.stride(), gate.dtype),
+               None if gamma_post is None else (gamma_post.shape, gamma_post.stride(), gamma_post.dtype),
+               None if gamma_pre is None else (gamma_pre.shape, gamma_pre.stride(), gamma_pre.dtype),
+               None if rng is None else (rng.shape, rng.stride(), rng.dtype), post_norm, pre_norm, sigmoid, scale, eps,
+               dropout, site, dtype, dev, stats.shape, stats.stride(), stats.dtype,
+               None if dx_out is None else (dx_out.shape, dx_out.stride(), dx_out.dtype),
+               None if dh is None else (dh.shape, dh.stride(), dh.dtype),
                (_sig(dx), _sig(dy), _sig(dg), _sig(dgpost), _sig(dgpre)) if out else None)
     except AttributeError:
         _bad(("x", x), ("y", y), ("stats", stats), ("dx_out", dx_out), ("dh", dh), ("gate", gate),
@@ -277,12 +282,13 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
         _elsewhere(dev, ("x", x), ("y", y), ("stats", stats), ("dx_out", dx_out), ("dh", dh), ("gate", gate),
                    ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng), ("workspace", workspace),
                    ("dx", dx), ("dy", dy), ("dgate", dg), ("dgamma_post", dgpost), ("dgamma_pre", dgpre))
-    device, shape, dt = x.device, x.shape, plan[3]
+    dt, device, shape, _ = plan[3]
     if dx is None:
-        dx = _new(x)
+        dx = torch.empty_like(x) if x.is_contiguous() else torch.empty(shape, dtype=x.dtype, device=device)
     if dy is None:
-        dy = _new(x) if dt is x.dtype else torch.empty(shape, dtype=dt, device=device)
+        dy = torch.empty(shape, dtype=dt, device=device)
     g = {"dx": dx, "dy": dy}
+    width = shape[2]
     if gate is None:
         dg = None
     else:
@@ -292,19 +298,19 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
     if not post_norm:
         dgpost = None
     else:
-        g["dgamma_post"] = dgpost = torch.empty(shape[2], dtype=f32, device=device) if dgpost is None else dgpost
+        g["dgamma_post"] = dgpost = torch.empty(width, dtype=f32, device=device) if dgpost is None else dgpost
     if not pre_norm:
         dgpre = None
     else:
-        g["dgamma_pre"] = dgpre = torch.empty(shape[2], dtype=f32, device=device) if dgpre is None else dgpre
+        g["dgamma_pre"] = dgpre = torch.empty(width, dtype=f32, device=device) if dgpre is None else dgpre
     workspace = _space(workspace, plan[1], device)
-    rc = _b.load().mosa_residual_backward(
+    rc = (_b._lib or _b.load()).mosa_residual_backward(
         plan[0], x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
         None if gamma_post is None else gamma_post.data_ptr(), None if gamma_pre is None else gamma_pre.data_ptr(),
         None if rng is None else rng.data_ptr(), stats.data_ptr(), None if dx_out is None else dx_out.data_ptr(),
         None if dh is None else dh.data_ptr(), dx.data_ptr(), dy.data_ptr(), None if dg is None else dg.data_ptr(),
         None if dgpost is None else dgpost.data_ptr(), None if dgpre is None else dgpre.data_ptr(),
-        workspace.data_ptr(), workspace.numel(), _b._stream(None))
+        workspace.data_ptr(), workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _b._check(rc, "mosa_residual_backward")
     return g, workspace
@@ -315,7 +321,8 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
 def _dropout_plan(x, p, rng, site, y):
     _rank(x, "x", 3)
     _check_rng(rng, p)
-    s = MosaDropoutShape(*x.shape, _b._dtype_code(x), _int(site, "site"), p, _rows(x, "x"), _result(y, "out y", x.shape, x.dtype))
+    s = MosaDropoutShape(*x.shape, _b._dtype_code(x), _int(site, "site"), p, _rows(x, "x"),
+                         _result(y, "out y", x.shape, x.dtype))
     return ctypes.byref(s), 0, s
 
 
@@ -327,20 +334,21 @@ def mosa_dropout(x, p: float, rng, site: int = 0, out=None, stream=None):
         dev = x.get_device()
         if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):
             return _there(x, stream, mosa_dropout, x, p, rng, site, out)
-        _b._torch()
+        torch = _b._torch()
         y = out.get("y") if out else None
         if not (type(p) is float and type(site) is int):
             p, site = float(p), _int(site, "site")
-        key = (8, x.shape, x.stride(), x.dtype, p, site, _sig(rng), _sig(y))
+        key = (8, x.shape, x.stride(), x.dtype, p, site, None if rng is None else (rng.shape, rng.stride(), rng.dtype),
+               None if y is None else _sig(y))
     except AttributeError:
         _bad(("x", x), ("rng", rng), ("out y", y))
     plan = _plans.get(key) or _keep(key, _dropout_plan(x, p, rng, site, y))
     if not (dev >= 0 and (rng is None or rng.get_device() == dev) and (y is None or y.get_device() == dev)):
         _elsewhere(dev, ("x", x), ("rng", rng), ("out y", y))
     if y is None:
-        y = _new(x)
-    rc = _b.load().mosa_dropout(plan[0], x.data_ptr(), None if rng is None else rng.data_ptr(), y.data_ptr(),
-                                _b._stream(None))
+        y = torch.empty_like(x) if x.is_contiguous() else _new(x)
+    rc = (_b._lib or _b.load()).mosa_dropout(plan[0], x.data_ptr(), None if rng is None else rng.data_ptr(), y.data_ptr(),
+                                             torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _b._check(rc, "mosa_dropout")
     return y
@@ -361,12 +369,14 @@ def _logprob_plan(logits, targets, top, scale, results, back=None):
             raise ValueError("targets must be contiguous")
     for name, t, n, dtype in results:
         _vector(t, name, (B, T, n) if n else (B, T), dtype)
-    s = MosaLogprobShape(B, T, V, _b._dtype_code(logits), 1 if targets is not None and targets.dtype == torch.int64 else 0,
+    s = MosaLogprobShape(B, T, V, _b._dtype_code(logits),
+                         1 if targets is not None and targets.dtype == torch.int64 else 0,
                          _int(top, "top"), scale, _rows(logits, "logits"))
     if back is not None:
         s.dz = _result(back[0], "dlogits", logits.shape, logits.dtype)
         return ctypes.byref(s), 0, s
-    return ctypes.byref(s), int(_b.load().mosa_token_logprobs_workspace_bytes(ctypes.byref(s))), s
+    return (ctypes.byref(s), int(_b.load().mosa_token_logprobs_workspace_bytes(ctypes.byref(s))), s,
+            (logits.device, (B, T), (B, T, top)))
 
 
 def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, workspace=None, out=None,
@@ -387,7 +397,10 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
                                      out.get("top_logp")) if out else (None,) * 5)
         if not (type(top) is int and type(scale) is float):
             top, scale = _int(top, "top"), _float(scale)
-        key = (9, logits.shape, logits.stride(), logits.dtype, _sig(targets), top, scale,
+        if top == 0:
+            idx = tlp = None
+        key = (9, logits.shape, logits.stride(), logits.dtype,
+               None if targets is None else (targets.shape, targets.stride(), targets.dtype), top, scale, dev,
                (_sig(logp), _sig(ent), _sig(lse), _sig(idx), _sig(tlp)) if out else None)
     except AttributeError:
         _bad(("logits", logits), ("targets", targets))
@@ -399,24 +412,22 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
             and (out is None or _all_on(dev, logp, ent, lse, idx, tlp))):
         _elsewhere(dev, ("logits", logits), ("targets", targets), ("workspace", workspace), ("logp", logp),
                    ("entropy", ent), ("lse", lse), ("top", idx), ("top_logp", tlp))
-    device, lead = logits.device, logits.shape[:2]
+    device, lead, tops = plan[3]
     r = {}
     if targets is None:
         logp = None
     else:
-        r["logp"] = logp = _made(logp, lead, f32, device)
-    r["entropy"] = ent = _made(ent, lead, f32, device)
-    r["lse"] = lse = _made(lse, lead, f32, device)
+        r["logp"] = logp = torch.empty(lead, dtype=f32, device=device) if logp is None else logp
+    r["entropy"] = ent = torch.empty(lead, dtype=f32, device=device) if ent is None else ent
+    r["lse"] = lse = torch.empty(lead, dtype=f32, device=device) if lse is None else lse
     if top > 0:
-        r["top"] = idx = _made(idx, (*lead, top), torch.int32, device)
-        r["top_logp"] = tlp = _made(tlp, (*lead, top), f32, device)
-    else:
-        idx = tlp = None
+        r["top"] = idx = torch.empty(tops, dtype=torch.int32, device=device) if idx is None else idx
+        r["top_logp"] = tlp = torch.empty(tops, dtype=f32, device=device) if tlp is None else tlp
     workspace = _space(workspace, plan[1], device)
-    rc = _b.load().mosa_token_logprobs(
+    rc = (_b._lib or _b.load()).mosa_token_logprobs(
         plan[0], logits.data_ptr(), None if targets is None else targets.data_ptr(),
         None if logp is None else logp.data_ptr(), ent.data_ptr(), lse.data_ptr(), _ptr(idx), _ptr(tlp),
-        workspace.data_ptr(), workspace.numel(), _b._stream(None))
+        workspace.data_ptr(), workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _b._check(rc, "mosa_token_logprobs")
     return r, workspace
@@ -463,14 +474,15 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
             logits, targets, n, scale,
             [("lse", lse, 0, f32), ("entropy", entropy, 0, f32), ("dlogp", dlogp, 0, f32), ("dentropy", dentropy, 0, f32),
              ("dlse", dlse, 0, f32), ("top", top, n, torch.int32), ("dtop_logp", dtop_logp, n, f32)], (dz,)))
-    if not (dev >= 0 and lse.get_device() == dev and _all_on(dev, targets, entropy, dlogp, dentropy, dlse, top, dtop_logp, dz)):
+    if not (dev >= 0 and lse.get_device() == dev
+            and _all_on(dev, targets, entropy, dlogp, dentropy, dlse, top, dtop_logp, dz)):
         _elsewhere(dev, ("logits", logits), ("targets", targets), ("lse", lse), ("entropy", entropy), ("dlogp", dlogp),
                    ("dentropy", dentropy), ("dlse", dlse), ("top", top), ("dtop_logp", dtop_logp), ("dlogits", dz))
     if dz is None:
         dz = _new(logits)
-    rc = _b.load().mosa_token_logprobs_backward(
+    rc = (_b._lib or _b.load()).mosa_token_logprobs_backward(
         plan[0], logits.data_ptr(), _ptr(targets), lse.data_ptr(), _ptr(entropy), _ptr(top), _ptr(dlogp), _ptr(dentropy),
-        _ptr(dlse), _ptr(dtop_logp), dz.data_ptr(), _b._stream(None))
+        _ptr(dlse), _ptr(dtop_logp), dz.data_ptr(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _b._check(rc, "mosa_token_logprobs_backward")
     return dz

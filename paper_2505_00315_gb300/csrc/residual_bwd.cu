@@ -11,9 +11,14 @@ __global__ void __launch_bounds__(1024) residual_sums_kernel(const float *partia
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ float red[32][33];
     const int cc = threadIdx.x & 31, run = threadIdx.x >> 5, col = blockIdx.x * 32 + cc;
-    float sum = 0.f;
-    if (col < 3 * d)
-        for (int b = run; b < blocks; b += 32) sum += partial[(long long)b * 3 * d + col];
+    float sum = 0.f, v[kSms / 32 + 1];   // (all loads first)
+#pragma unroll
+    for (int i = 0; i < kSms / 32 + 1; ++i) {
+        const int b = run + 32 * i;
+        v[i] = b < blocks && col < 3 * d ? partial[(long long)b * 3 * d + col] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kSms / 32 + 1; ++i) sum += v[i];
     red[run][cc] = sum;
     __syncthreads();
     if (run == 0 && col < 3 * d) {

@@ -466,6 +466,50 @@ def test_rows_past_32_bits():
     assert torch.equal(mosa.mosa_dropout(x, 0.4, state()), mosa.mosa_dropout(a[0], 0.4, state()))
 
 
+def test_tensors_of_another_device_are_refused():
+    s, dx_out, dh = inputs(1, 4, 64, seed=18)
+    for n in ("x", "y", "gamma_post"):
+        with pytest.raises(ValueError, match="CUDA tensor"):
+            mosa.mosa_residual_forward(**{**s, n: s[n].cpu()})
+    stats = mosa.mosa_residual_forward(**s)[2]
+    with pytest.raises(ValueError, match="dh must be a CUDA"):
+        mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh.cpu(), **s)
+    with pytest.raises(ValueError, match="out x must be a CUDA"):
+        mosa.mosa_residual_forward(**s, out={"x": dx_out.cpu()})
+    with pytest.raises(ValueError, match="rng must be a CUDA"):
+        mosa.mosa_dropout(s["x"], 0.1, state().cpu())
+    z, t = logits_of(1, 3, 50), targets_of(1, 3, 50)
+    with pytest.raises(ValueError, match="targets must be a CUDA"):
+        mosa.mosa_token_logprobs(z, t.cpu())
+    r, ws = mosa.mosa_token_logprobs(z, t, top=2)
+    with pytest.raises(ValueError, match="dlogp must be a CUDA"):
+        mosa.mosa_token_logprobs_backward(z, t, r["lse"], dlogp=r["logp"].cpu())
+    # results of a call with alternatives serve one without
+    again, _ = mosa.mosa_token_logprobs(z, t, out=r, workspace=ws)
+    assert set(again) == {"logp", "entropy", "lse"} and again["lse"] is r["lse"]
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with results and a workspace of its own, give what they give alone."""
+    s, dx_out, dh = inputs(3, 700, 1024, gate="channel", seed=19)
+    z, t = logits_of(2, 300, 40000, seed=20), targets_of(2, 300, 40000)
+    kw = dict(dropout=0.1, rng=state())
+
+    def calls(stream):
+        x, h, stats = mosa.mosa_residual_forward(**s, **kw, stream=stream)
+        g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, **s, **kw, stream=stream)
+        r, _ = mosa.mosa_token_logprobs(z, t, top=9, stream=stream)
+        return [x, h, *g.values(), *r.values()]
+
+    want = calls(None)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [calls(st) for _ in range(4) for st in streams]
+    torch.cuda.synchronize()
+    for one in got:
+        assert all(torch.equal(a, b) for a, b in zip(one, want))
+
+
 # ------------------------------------------------------------------ together
 
 def block_step(m, tokens, rng, stream=None):
