@@ -459,11 +459,15 @@ inline int times_of(const Residual &r, bool backward, int *most) {
             const int W = warps(times), G = of / W;
             return G == 0 ? 0.0 : (double)r.d / (256 * times * W) * (G * W) / of;
         };
+        if (warps(1) > kWarps) {
+            *most = kWarps / 2;
+            return 4;
+        }
         if (r.d > 256 && warps(2) <= kWarps / 2 && rows * warps(2) >= kSms * 8 * 16 && used(2, kWarps / 2) >= 0.95 * used(1, kWarps)) {
             *most = kWarps / 2;
             return 2;
         }
-        return warps(1) > kWarps ? 2 : 1;
+        return 1;
     }
     int times = r.gate == MOSA_GATE_TOKEN ? 2 : 4;
     while (times > 1 && rows * warps(times) < kSms * kWarps) times /= 2;
@@ -489,6 +493,7 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
     const int each = times_of(r, backward, &p.most);
     p.warps = (r.d + 256 * each - 1) / (256 * each);
     *times = (r.d + 256 * p.warps - 1) / (256 * p.warps);   // (no more than the width asks for)
+    if (backward && *times == 3) *times = 4;
     // (a piece more where one may be cut by a row's beginning)
     bool vec = true;
     for (const Rows *m : all) vec = vec && (m->p == nullptr || m->vec);

@@ -43,8 +43,8 @@ cudaError_t launch_residual_bwd(const Residual &r, float *partial, cudaStream_t 
     p.partial = sums ? partial : nullptr;
     int blocks, times, bytes;
     shape(p, true, &blocks, &times, &bytes);
-    cudaError_t e = p.most < kWarps ? residual_bwd8(p, blocks, bytes, s)
-                    : times == 1 ? go_by_types<1, kWarps>(p, blocks, bytes, s) : go_by_types<2, kWarps>(p, blocks, bytes, s);
+    cudaError_t e = times == 1 ? go_by_types<1, kWarps>(p, blocks, bytes, s)
+                    : times == 2 ? residual_bwd_16(p, blocks, bytes, s) : residual_bwd_32(p, blocks, bytes, s);
     if (e != cudaSuccess || !sums) return e;
     note_launches(1);
     return launch_pdl(residual_sums_kernel, dim3((3 * r.d + 31) / 32), dim3(1024), 0, s, (const float *)partial,

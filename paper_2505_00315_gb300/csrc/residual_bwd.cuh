@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             return v;
         };
         // (they stay in registers from one round to the other where those suffice)
-        constexpr bool kStay = C * kMost <= kWarps;
+        constexpr bool kStay = C <= 2;
         Values stay[C];
         Pair s0 = 0, s1 = 0, s2 = 0;
 #pragma unroll
@@ -242,8 +242,9 @@ cudaError_t go_by_types(const Args &p, int blocks, int bytes, cudaStream_t s) {
     }
 }
 
-// Blocks of 8 warps, 16 columns a thread (residual_bwd8.cu; a file of its own for the compiler's time).
-cudaError_t residual_bwd8(const Args &p, int blocks, int bytes, cudaStream_t s);
+// Blocks of 8 warps, 16 or 32 columns a thread (files of their own for the compiler's time).
+cudaError_t residual_bwd_16(const Args &p, int blocks, int bytes, cudaStream_t s);
+cudaError_t residual_bwd_32(const Args &p, int blocks, int bytes, cudaStream_t s);
 
 }  // namespace blk
 }  // namespace mosa

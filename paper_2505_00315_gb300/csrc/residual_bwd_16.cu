@@ -1,0 +1,12 @@
+// The residual step's backward in blocks of 8 warps, 16 columns a thread; the kernel: residual_bwd.cuh.
+#include "residual_bwd.cuh"
+
+namespace mosa {
+namespace blk {
+
+cudaError_t residual_bwd_16(const Args &p, int blocks, int bytes, cudaStream_t s) {
+    return go_by_types<2, kWarps / 2>(p, blocks, bytes, s);
+}
+
+}  // namespace blk
+}  // namespace mosa
