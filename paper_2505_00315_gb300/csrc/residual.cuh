@@ -38,9 +38,11 @@ struct Args {
 // also take rows of any place, stride and number of columns (16-byte pieces arrive as they lie in memory,
 // and what is read from them is shifted); those of known types take rows of whole pieces, one stride
 // apart, and have gammas and gate in shared memory: no branch stands between their loads.
-template <int kX, int kY, int kDh, int kStorage>
+// (kHeld 0: gammas and gate are not there, and are read where they lie.)
+template <int kX, int kY, int kDh, int kStorage, int kHeld_ = 1>
 struct Types {
-    static constexpr bool kFast = kX >= 0;
+    static constexpr bool kFast = kX >= 0, kHeld = kFast && kHeld_;   // kHeld: known to be held
+    static constexpr bool kLies = kFast && !kHeld_;                   // known not to be
     static constexpr int x = kX, y = kY, dh = kDh, storage = kStorage;
 };
 __device__ __forceinline__ int wide_of(int known, const Rows &m) { return known < 0 ? m.wide : known; }
@@ -196,8 +198,10 @@ __device__ __forceinline__ void put_values(int wide, char *row, int col, int d, 
 }
 
 // The warp's 256 columns from `col` on to a row, through its scratch where lanes' own eight columns
-// are not the pieces that leave together.
-template <bool kVec, int kWide>
+// are not the pieces that leave together.  kDirect: fp32 columns without it, 32 bytes a lane, which pays where they are
+// one of several outputs (the backward beside a bf16 dy, B2 T8192 d4096: 251 -> 239 us), not where all are fp32 (16384
+// rows of 2048: 127 -> 142).
+template <bool kVec, int kWide, bool kDirect = false>
 __device__ __forceinline__ void put(const Rows &m, char *row, int col, int d, char *scratch, int lane, const Oct &v) {
     if (!wide_of(kWide, m)) {
         const F2 a = of_two(v.v[0]), b = of_two(v.v[1]), c = of_two(v.v[2]), e = of_two(v.v[3]);
@@ -209,6 +213,14 @@ __device__ __forceinline__ void put(const Rows &m, char *row, int col, int d, ch
         __syncwarp();
         *reinterpret_cast<uint4 *>(scratch + 16 * lane) = w;
     } else {
+        if (kDirect && (kVec || m.vec)) {
+            if (col + 8 * lane < d) {
+                ulonglong2 *q = reinterpret_cast<ulonglong2 *>(row + 4 * (col + 8 * lane));
+                q[0] = make_ulonglong2(v.v[0], v.v[1]);
+                q[1] = make_ulonglong2(v.v[2], v.v[3]);
+            }
+            return;
+        }
         __syncwarp();
         keep(scratch, lane, v);
         if (kVec || m.vec) {
@@ -384,7 +396,7 @@ __device__ __forceinline__ Oct arrived(const char *from, int wide, const Place &
 }
 
 // Rows of one tensor that leave.
-template <int C, bool kFast, int kWide>
+template <int C, bool kFast, int kWide, bool kDirect = false>
 struct Departure {
     char *at;   // the row's columns of the warp
     __device__ __forceinline__ void init(const Args &p, const Place &l, const Rows &m, uint32_t row) {
@@ -394,7 +406,7 @@ struct Departure {
         if (!kFast) at = row_at(p, m, row);
     }
     __device__ __forceinline__ void put_row(const Place &l, const Rows &m, int c, const Oct &v) {
-        put<kFast, kWide>(m, at, l.col0 + 256 * c, l.d, l.scratch, l.lane, v);
+        put<kFast, kWide, kDirect>(m, at, l.col0 + 256 * c, l.d, l.scratch, l.lane, v);
     }
     __device__ __forceinline__ void end(const Place &l, const Rows &m) {
         if (kFast) at += (uint64_t)l.step * (uint32_t)m.t;
@@ -435,9 +447,9 @@ __device__ __forceinline__ void hold(const Args &p, const Place &l, float unit) 
     }
     __syncthreads();
 }
-template <int C, bool kForward, bool kFast>
+template <int C, bool kForward, class Ty>
 __device__ __forceinline__ Oct vector_at(const Args &p, const Place &l, int which, int c, float unit) {
-    if (kFast || p.held) return take(l.held + (which * l.W + l.w) * C * 1024 + c * 1024, 1, l.lane);
+    if (Ty::kHeld || (!Ty::kLies && p.held)) return take(l.held + (which * l.W + l.w) * C * 1024 + c * 1024, 1, l.lane);
     return vector_of<kForward>(p.r, which, l.column(c), unit);
 }
 
@@ -521,10 +533,10 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
     *blocks = (int)std::min<long long>((rows + p.groups - 1) / p.groups, kSms);
 }
 
-// Whether a kernel of known types takes the call.
+// Whether a kernel of known types takes the call's places and strides.
 inline bool fast(const Args &p) {
     const Residual &r = p.r;
-    bool vec = p.flat && p.held;
+    bool vec = p.flat;
     for (const Rows *m : {&r.x, &r.y, &r.g, &r.xo, &r.h, &r.dxo, &r.dh, &r.dx, &r.dy, &r.dg})
         vec = vec && (m->p == nullptr || m->vec);
     return vec;

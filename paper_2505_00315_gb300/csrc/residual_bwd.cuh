@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
     dxo_in.init(p, l, r.dxo, row);
     dh_in.init(p, l, r.dh, row);
     g_in.init(p, l, r.g, row);
-    Departure<C, kFast, Ty::x> dx_out;
+    Departure<C, kFast, Ty::x, Ty::storage == 0> dx_out;
     Departure<C, kFast, Ty::storage> dy_out, dg_out;
     dx_out.init(p, l, r.dx, row);
     dy_out.init(p, l, r.dy, row);
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         if (row + i * l.step < l.rows) fill(row + i * l.step, i);
         copies_end();
     }
-    if (kFast || p.held) hold<C, false>(p, l, unit);
+    if (Ty::kHeld || (!Ty::kLies && p.held)) hold<C, false>(p, l, unit);
 
     int slot = 0, turn = 0;
     // Sums over tokens: 0 of gamma_post over c g, which the gate of a channel shares (each has a factor of
@@ -112,16 +112,16 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             const Oct dxo = arrived<kFast>(in + dxo_off, xw, l, c, dxos);
             dh = arrived<kFast>(in + dh_off, hw, l, c, dhs);
             v.cg = token ? times(token_gate(c), unit)
-                   : r.gate == MOSA_GATE_NONE ? all_of(unit) : vector_at<C, false, kFast>(p, l, 2, c, unit);
+                   : r.gate == MOSA_GATE_NONE ? all_of(unit) : vector_at<C, false, Ty>(p, l, 2, c, unit);
             v.yh = times(y, ry);
             if (drops) {
                 v.cg = chosen(v.cg, bits[c]);
                 // (with a norm, what is not finite is so in its whole row)
                 if (!r.post) v.yh = chosen(v.yh, bits[c]);
             }
-            u = times(times(v.yh, vector_at<C, false, kFast>(p, l, 0, c, unit)), v.cg);
+            u = times(times(v.yh, vector_at<C, false, Ty>(p, l, 0, c, unit)), v.cg);
             v.xh = times(plus(x, u), rx);
-            e = times(dh, vector_at<C, false, kFast>(p, l, 1, c, unit));
+            e = times(dh, vector_at<C, false, Ty>(p, l, 1, c, unit));
             v.base = fused(e, rx, dxo);
             return v;
         };
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             Oct u, dh, e;
             Values v = stay[c];
             if (!kStay) v = values(c, u, dh, e);
-            const Oct gamma = vector_at<C, false, kFast>(p, l, 0, c, unit);
+            const Oct gamma = vector_at<C, false, Ty>(p, l, 0, c, unit);
             const Oct t = fused(v.xh, -m1, v.base), f = times(t, v.cg);
             dx_out.put_row(l, r.dx, c, t);
             if (token) {
@@ -228,7 +228,10 @@ template <int C, int kMost>
 cudaError_t go_by_types(const Args &p, int blocks, int bytes, cudaStream_t s) {
     const Residual &r = p.r;
     const int x = r.x.wide, y = r.y.wide, dh = r.dh.p != nullptr && r.dh.wide, st = r.storage_wide;
-    if (!fast(p) || (st && !(x && y && dh))) return go<C, kMost, Types<-1, -1, -1, -1>>(p, blocks, bytes, s);
+    if (!fast(p) || (st && !(x && y && dh)) || (!p.held && !(C == 4 && st)))
+        return go<C, kMost, Types<-1, -1, -1, -1>>(p, blocks, bytes, s);
+    if constexpr (C == 4)
+        if (!p.held) return go<C, kMost, Types<1, 1, 1, 1, 0>>(p, blocks, bytes, s);
     if (st) return go<C, kMost, Types<1, 1, 1, 1>>(p, blocks, bytes, s);
     switch (4 * x + 2 * y + dh) {
         case 0: return go<C, kMost, Types<0, 0, 0, 0>>(p, blocks, bytes, s);

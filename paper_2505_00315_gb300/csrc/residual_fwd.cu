@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
         if (row + i * l.step < l.rows) fill(row + i * l.step, i);
         copies_end();
     }
-    if (kFast || p.held) hold<C, true>(p, l, unit);
+    if (Ty::kHeld || (!Ty::kLies && p.held)) hold<C, true>(p, l, unit);
 
     int slot = 0, turn = 0;
     for (; row < l.rows; row += l.step) {
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
         if (token || drops) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                Oct u = times(y_at(c), times(vector_at<C, true, kFast>(p, l, 0, c, unit), ry));
+                Oct u = times(y_at(c), times(vector_at<C, true, Ty>(p, l, 0, c, unit), ry));
                 if (token) {
                     const int gw = wide_of(Ty::storage, r.g);
                     const Oct g = arrived<kFast>(in + g_off, gw, l, c, gs);
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
         } else {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                x[c] = fused(y_at(c), times(vector_at<C, true, kFast>(p, l, 0, c, unit), ry),
+                x[c] = fused(y_at(c), times(vector_at<C, true, Ty>(p, l, 0, c, unit), ry),
                              arrived<kFast>(in, xw, l, c, xs));
                 add_products(s, x[c], x[c]);
             }
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
             h_out.begin(p, r.h, row);
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                h_out.put_row(l, r.h, c, times(x[c], times(vector_at<C, true, kFast>(p, l, 1, c, unit), rx)));
+                h_out.put_row(l, r.h, c, times(x[c], times(vector_at<C, true, Ty>(p, l, 1, c, unit), rx)));
             h_out.end(l, r.h);
         }
         if (r.stats != nullptr && l.w == 0 && l.lane == 0) {
@@ -133,7 +133,7 @@ cudaError_t launch_residual(const Residual &r, cudaStream_t s) {
     p.r = r;
     int blocks, times, bytes;
     shape(p, false, &blocks, &times, &bytes);
-    if (fast(p)) {
+    if (fast(p) && p.held) {
         const int x = r.x.wide, y = r.y.wide, st = r.storage_wide;
         if (!st && !x && !y) return go<Types<0, 0, 0, 0>>(p, blocks, times, bytes, s);
         if (!st && !x && y) return go<Types<0, 1, 0, 0>>(p, blocks, times, bytes, s);
