@@ -1,7 +1,8 @@
 // Dropout without a stored mask: y = keep/(1-p) x, the words of a token's columns from their counters
 // (philox.cuh).  Memory bound: x and y move once; two counters for eight columns are some ten
 // instructions a value.  A warp takes a few runs of 256 columns (or of some whole rows, where those are
-// short), one after another in memory, all loads first.
+// short), one after another in memory, all loads first.  fp32 B4 T4096 d1024 22.3 us (6.0 TB/s, 89% of the copy rate;
+// runs of whole units of 1024 columns a warp 29.7); B8 T1024 d512 bf16 6.8 (10.8), one wave.
 #include <algorithm>
 
 #include "block.h"

@@ -11,6 +11,9 @@
 // A warp takes a row, or 2, 4 or 8 of a block share one where rows are fewer, or some blocks, whose
 // results a second kernel joins.  Rows move in 16-byte pieces wherever they start: a row is cut at the
 // addresses' multiples of 16, its first and last pieces are read value by value.
+// us and share of the copy rate, bf16: 16384 rows of 32768 forward 170 (93%), backward 312 (all of it); 4096 rows of 50001 forward
+// 72 (84%), with 5 alternatives 103 (59%: 9.6 instructions a value, and each warp's end a chain); fp32, 1000 rows of 32003
+// with 8: 38 and 44 (49%, 86%); 8 rows of 131072 with 20: 10, two launches.
 //
 // Alternatives: the pass over the row only notes, for each lane, the largest values of its three best steps (32 bf16
 // or 16 fp32 values a step) and that of the fourth.  A value T that the largest of `top` steps of lanes reach is
