@@ -163,11 +163,11 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
                 acc[0][c] = fused(f, v.yh, acc[0][c]);
                 if (r.dg.p != nullptr) {
                     Oct g = times(times(t, unit), times(v.yh, gamma));
-                    if (drops) g = chosen(g, bits[c]);
                     if (r.sigmoid) {
                         const Oct k = token_gate(c);
                         g = times(g, fused(times(k, -1.f), k, k));
                     }
+                    if (drops) g = chosen(g, bits[c]);
                     dg_out.put_row(l, r.dg, c, g);
                 }
             } else {

@@ -161,6 +161,16 @@ def test_dropped_values_do_not_count():
     g, _ = mosa.mosa_residual_backward(stats=got[2], dx_out=dx_out, dh=dh, **s, post_norm=False, dropout=p, rng=rng)
     for n, t in {"x": got[0], "h": got[1], **g}.items():
         near(n, t, *clean[n])
+    # through a sigmoid, and a gate that is no number where it is dropped
+    gate = torch.where(keep, s["gate"], 0.5)
+    clean = residual(**{**s, "y": torch.where(keep, s["y"], 0.0), "gate": gate}, post_norm=False, dropout=p, rng=rng,
+                     sigmoid=True, dx_out=dx_out, dh=dh, backward=True)
+    bad = {**s, "gate": torch.where(keep, s["gate"], NAN)}
+    got = mosa.mosa_residual_forward(**bad, post_norm=False, dropout=p, rng=rng, sigmoid=True)
+    g, _ = mosa.mosa_residual_backward(stats=got[2], dx_out=dx_out, dh=dh, **bad, post_norm=False, dropout=p, rng=rng,
+                                       sigmoid=True)
+    for n, t in {"x": got[0], "h": got[1], **g}.items():
+        near(n, t, *clean[n])
     s["y"][1, 2, int(keep[1, 2].nonzero()[0])] = NAN
     x, h, _ = mosa.mosa_residual_forward(**s, post_norm=False, dropout=p, rng=rng)
     rows = torch.isnan(h).all(-1)
