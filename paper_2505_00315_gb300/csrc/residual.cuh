@@ -458,9 +458,10 @@ __device__ __forceinline__ Oct vector_at(const Args &p, const Place &l, int whic
 // Eights of columns of a thread: as many as registers hold, since what a row costs beside its values is
 // shared by them, but enough warps for all SMs first.  The forward takes four (two with a gate per
 // token); the backward, which keeps two sums of each column and what its second round needs, two in blocks
-// of 8 warps (256 registers a thread) where a group has some rows, else one in blocks of 16.  us of the backward with
-// one / two: B4 T4096 d1024 55.5 / 53.7, B2 T8192 d4096 267 / 251, fp32 B4 T1000 d768 21.2 / 22.5 (two in blocks of
-// 16, which spill: 74, 537 and 29).
+// of 8 warps (256 registers a thread) where a group has some rows, four (what the second round needs computed again) where a row
+// is too wide for 16 warps of one, else one in blocks of 16.  us of the backward with one / two: B4 T4096 d1024 55.5 / 53.7,
+// B2 T8192 d4096 267 / 251, fp32 B4 T1000 d768 21.2 / 22.5 (two in blocks of 16, which spill: 74, 537 and 29);
+// 8192 rows of 8192 with two in blocks of 16 / four in blocks of 8: 211 / 168.
 inline int times_of(const Residual &r, bool backward, int *most) {
     const long long rows = (long long)r.B * r.T;
     auto warps = [&](int times) { return (r.d + 256 * times - 1) / (256 * times); };
@@ -492,6 +493,7 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
     Residual &r = p.r;
     const long long rows = (long long)r.B * r.T;
     Rows *all[] = {&r.x, &r.y, &r.g, &r.xo, &r.h, &r.dxo, &r.dh, &r.dx, &r.dy, &r.dg};
+    if (r.dh.p == nullptr) r.dh.wide = r.storage_wide;   // (zeros stand for it, of the type that most kernels know)
     p.flat = 1;
     for (Rows *m : all) {
         if (r.d % 8 != 0) m->vec = 0;   // (a piece would reach into the next row)
@@ -541,8 +543,6 @@ inline bool fast(const Args &p) {
         vec = vec && (m->p == nullptr || m->vec);
     return vec;
 }
-
-
 
 }  // namespace blk
 }  // namespace mosa

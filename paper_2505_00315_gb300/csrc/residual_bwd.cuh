@@ -232,7 +232,7 @@ cudaError_t go(const Args &p, int blocks, int bytes, cudaStream_t s) {
 template <int C, int kMost>
 cudaError_t go_by_types(const Args &p, int blocks, int bytes, cudaStream_t s) {
     const Residual &r = p.r;
-    const int x = r.x.wide, y = r.y.wide, dh = r.dh.p != nullptr && r.dh.wide, st = r.storage_wide;
+    const int x = r.x.wide, y = r.y.wide, dh = r.dh.wide, st = r.storage_wide;
     if (!fast(p) || (st && !(x && y && dh)) || (!p.held && !(C == 4 && st)))
         return go<C, kMost, Types<-1, -1, -1, -1>>(p, blocks, bytes, s);
     if constexpr (C == 4)

@@ -100,6 +100,11 @@ def test_without_gammas_and_with_one_gradient():
     check(s, dx_out, None)
     got = check(s, None, None)
     assert not any(t.any() for n, t in got.items() if n.startswith("d"))
+    for d in (320, 1500):
+        s, dx_out, dh = inputs(2, 30, d, F32, gate="channel", seed=4)
+        check(s, dx_out, None)
+        check(s, None, dh, post_norm=False)
+        check(s, dx_out, None, pre_norm=False)
 
 
 def test_strides_and_places():
