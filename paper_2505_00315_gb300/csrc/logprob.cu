@@ -558,9 +558,9 @@ __global__ void __launch_bounds__(kFewWarps * 32) logprob_bwd_kernel(const __gri
         float B = -l.scale * kLn2 * dH;
         if (zero) A = B = 0.f;
         const float ref = zero ? 0.f : lse;
-        // Values that are clamped to this have weight 0, and no infinity meets it.  (Rounded down, so
-        // that no larger one is met.)
-        const float least = fmaxf((ref - 208.f) / l.scale, kLeast);
+        // Values that are clamped to this have weight 0, and no infinity meets it.  (Far enough below a large lse that
+        // no rounding brings it back there.)
+        const float least = fmaxf((ref - 208.f - fabsf(ref) * 0x1p-6f) / l.scale, kLeast);
         const uint32_t least2 = 0x10001u * (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rd(least));
         const float leastw = __bfloat162float(__float2bfloat16_rd(least));
 

@@ -451,6 +451,16 @@ def test_logprobs_for_temperatures_and_large_logits():
     check_logprobs(z * 1e20, targets_of(1, 20, 3000), 4)
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("size", [2.0 ** 31, 2.0 ** 33, -2.0 ** 34, 1e20, -1e20])
+def test_logits_so_large_that_lse_is_the_largest(size, dt):
+    # (values of bf16 in both types: lse is one of them)
+    z = (size * (1 + torch.rand(1, 20, 3000, generator=gen(12), device="cuda"))).to(BF).to(dt)
+    z[..., 7] = 8 * size if size > 0 else size / 8   # (the only one of its size)
+    for scale in (1.0, 0.5):
+        check_logprobs(z, targets_of(1, 20, 3000), 4, scale)
+
+
 def test_logits_past_32_bits():
     """More than 2^32 elements: the last rows."""
     B, T, V = 1, 33000, 131072
