@@ -330,6 +330,7 @@ def mosa_dropout(x, p: float, rng, site: int = 0, out=None, stream=None):
     """x [B,T,d] with each value dropped (0) with probability p, the others times 1/(1-p).  ``rng`` [2]
     int64 on the GPU holds seed and offset, read when the call runs; ``site`` tells calls that share
     it apart.  The same call on the gradient is the backward.  ``out`` may hold "y", x itself among them."""
+    y = None
     try:
         dev = x.get_device()
         if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):
@@ -439,6 +440,7 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
     dentropy, dlse [B,T] and dtop_logp [B,T,top] fp32 of its results, each None where there is none; ``top``:
     the indices that it returned, read with dtop_logp.  ``out`` may hold "dlogits", logits itself among
     them."""
+    dz = None
     try:
         dev = logits.get_device()
         if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):

@@ -221,6 +221,17 @@ def test_binding_refuses():
         K.mosa_token_logprobs_backward(x, None, x[..., 0].contiguous(), dentropy=x[..., 0].contiguous())
 
 
+@pytest.mark.parametrize("bad", [None, [1.0], 3])
+def test_binding_names_what_is_no_tensor(bad):
+    x, rng = torch.zeros(2, 8, 64), torch.zeros(2, dtype=torch.int64)
+    row = x[..., 0].contiguous()
+    for call in (lambda: K.mosa_residual_forward(bad, x), lambda: K.mosa_residual_backward(bad, x, x, x, x),
+                 lambda: K.mosa_dropout(bad, 0.5, rng), lambda: K.mosa_token_logprobs(bad),
+                 lambda: K.mosa_token_logprobs_backward(bad, None, row)):
+        with pytest.raises((TypeError, ValueError), match="must be a|missing"):
+            call()
+
+
 def test_random_words_are_the_published_ones():
     """Philox 4x32 with seven rounds: the known answers that its authors publish with their library."""
     for counter, key, words in (
