@@ -487,8 +487,8 @@ mosa_status mosa_residual_forward(const mosa_residual_shape *shape, const void *
 size_t mosa_residual_workspace_bytes(const mosa_residual_shape *shape);
 
 /* Backward: from the forward's inputs and stats and the gradients dx_out (x_dtype) and dh
- * (dh_dtype; NULL with pre_norm = 0) of its outputs (either NULL: none), the gradients dx (which may be dx_out
- * itself), dy (storage dtype), of gate: dgate [d] fp32 or [B,T,d] in the storage dtype, and dgamma_post,
+ * (dh_dtype; NULL with pre_norm = 0) of its outputs (either NULL: none; x is not read with pre_norm = 0), the
+ * gradients dx (which may be dx_out itself), dy (storage dtype), of gate: dgate [d] fp32 or [B,T,d] in the storage dtype, and dgamma_post,
  * dgamma_pre [d] fp32.  Each of the last three may be NULL. */
 mosa_status mosa_residual_backward(const mosa_residual_shape *shape, const void *x, const void *y,
                                    const void *gate, const void *gamma_post,

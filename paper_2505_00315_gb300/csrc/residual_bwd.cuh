@@ -30,7 +30,8 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
     const bool drops = r.drop.rng != nullptr, token = r.gate == MOSA_GATE_TOKEN;
     const bool has_dxo = r.dxo.p != nullptr, has_dh = r.dh.p != nullptr;
     const float unit = r.scale * (drops ? r.drop.scale : 1.f), inv_d = 1.f / l.d;   // unit: c of a kept value
-    if (l.d < 256 * C * l.W || !has_dxo || !has_dh) clear_ring(l);
+    // (x is not read without the second norm, whose xh alone needs it: zeros do, and no infinity of x counts)
+    if (l.d < 256 * C * l.W || !has_dxo || !has_dh || !r.pre) clear_ring(l);
     uint32_t row = blockIdx.x * p.groups + l.group;   // (row + kMaxStages step fits 32 bits)
     Arrival<C, kFast, Ty::x> x_in, dxo_in;
     Arrival<C, kFast, Ty::y> y_in;
@@ -52,7 +53,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
     const int g_off = kFast ? dh_off + bytes_of(Ty::dh, C) : p.off[4];
     auto fill = [&](uint32_t at, int slot) {
         const uint32_t to = l.ring32 + slot * p.stage_bytes;
-        x_in.issue(p, l, r.x, at, to);
+        if (r.pre) x_in.issue(p, l, r.x, at, to);
         y_in.issue(p, l, r.y, at, to + y_off);
         if (has_dxo) dxo_in.issue(p, l, r.dxo, at, to + dxo_off);
         if (has_dh) dh_in.issue(p, l, r.dh, at, to + dh_off);

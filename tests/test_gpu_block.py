@@ -183,6 +183,18 @@ def test_dropped_values_do_not_count():
     assert int(torch.isnan(x).sum()) == 1
 
 
+@pytest.mark.parametrize("xt,d", [(F32, 320), (BF, 1500), (BF, 1001)])
+def test_without_the_second_norm_the_stream_does_not_count(xt, d):
+    """dx = dx_out and all others are the same, whatever x holds: padded tokens may hold anything."""
+    s, dx_out, _ = inputs(2, 30, d, BF, xt=xt, gate="channel", seed=12)
+    stats = mosa.mosa_residual_forward(**s, pre_norm=False)[2]
+    clean, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=None, **s, pre_norm=False)
+    s["x"][0, 3], s["x"][1, 4, 5], s["x"][1, 29] = NAN, INF, 1e38
+    got, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=None, **s, pre_norm=False)
+    assert torch.equal(got["dx"], dx_out)
+    assert set(got) == set(clean) and all(torch.equal(got[n], clean[n]) for n in got)
+
+
 def test_everything_and_nothing_dropped():
     s, dx_out, dh = inputs(2, 20, 264, gate="channel", seed=8)
     check(s, dx_out, dh, dropout=1.0, rng=state())
