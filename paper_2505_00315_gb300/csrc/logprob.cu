@@ -217,7 +217,7 @@ __device__ __forceinline__ Key key_of(float v, int col) { return (Key)order_of(v
 
 // The best of a warp's part of a row, looked through once more: what reaches `bar` (low: whatever there is).
 template <bool kWide>
-__device__ __noinline__ Key look_again(const Row<kWide> &z, int from, int to, float bar, bool low, int top) {
+__device__ __noinline__ Key look_again(const Row<kWide> z, int from, int to, float bar, bool low, int top) {
     constexpr int E = kWide ? 4 : 8;
     const int lane = threadIdx.x & 31;
     Key list = 0;
@@ -265,11 +265,20 @@ __device__ __noinline__ Key look_again(const Row<kWide> &z, int from, int to, fl
     return list;
 }
 
-// What a lane has seen: the largest values of its three best steps, which ones, and that of the fourth.
+// What a lane has seen: the largest values of its three best steps, and that of the fourth.  The lower 16 bits of each
+// say which step it was, so that one minimum and maximum move both.
+constexpr float kLowest = -0x1p127f;   // (less counts as this: with a step's bits no infinity becomes a NaN)
 struct Peaks {
     float a, b, c, d;
-    int step_a, step_b, step_c;   // -1: none
 };
+__device__ __forceinline__ float peak_of(float v, int step) {   // (the sum: -0 counts as 0)
+    return __uint_as_float((__float_as_uint(fmaxf(v, kLowest) + 0.f) & 0xFFFF0000u) | (step & 0xFFFF));
+}
+// The least value whose peak has the same upper half.
+__device__ __forceinline__ float floor_of(float peak) {
+    const uint32_t b = __float_as_uint(peak);
+    return __uint_as_float((b & 0xFFFF0000u) | (b >> 31 ? 0xFFFFu : 0u));
+}
 
 // The 32 best of the lists of `share` warps side by side, in the first of them (all threads of the block).
 template <class K>
@@ -287,7 +296,7 @@ __device__ __noinline__ K best_of(K list, Key (*room)[32], int share) {
 
 // The 32 best of a warp's part of a row, those that reach T at least (all threads of the block call it).
 template <bool kWide>
-__device__ __noinline__ Key alternatives(const Row<kWide> &z, const Peaks &q, int from, int to, int share, int top,
+__device__ __noinline__ Key alternatives(const Row<kWide> z, const Peaks q, int from, int to, int share, int top,
                                          Key (*room)[32]) {
     constexpr int E = kWide ? 4 : 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -303,15 +312,17 @@ __device__ __noinline__ Key alternatives(const Row<kWide> &z, const Peaks &q, in
         order = (uint32_t)room[warp & ~(share - 1)][0];
         __syncthreads();
     }
-    const float T = of_order(order);
-    const bool low = !(T > __int_as_float(0xFF800000));
+    const float T = floor_of(of_order(order));
+    const bool low = !(T > kLowest);
     if (from >= to) return 0;
-    if (__any_sync(0xffffffffu, low || q.d >= T)) return look_again(z, from, to, T, low, top);
+    // (steps that 16 bits do not count are looked through as well)
+    if (__any_sync(0xffffffffu, low || floor_of(q.d) >= T || to - from > 65536)) return look_again(z, from, to, T, low, top);
     Key list = 0;
 #pragma unroll 1
     for (int round = 0; round < 3; ++round) {
-        const int step = round == 0 ? q.step_a : round == 1 ? q.step_b : q.step_c;
-        uint32_t who = __ballot_sync(0xffffffffu, (round == 0 ? q.a : round == 1 ? q.b : q.c) >= T && step >= 0);
+        const float peak = round == 0 ? q.a : round == 1 ? q.b : q.c;
+        const int step = from + (int)(__float_as_uint(peak) & 0xFFFF);
+        uint32_t who = __ballot_sync(0xffffffffu, floor_of(peak) >= T);
         while (who != 0) {
             // (four steps' values at once: a lane reads one of each, as many as a lane's step has)
             Key k[4];
@@ -416,8 +427,7 @@ __global__ void __launch_bounds__(kOf * 32, 32 / kOf) logprob_kernel(const __gri
 
     float m = kLeast;
     Pair s = 0, sum_t = 0;   // pairs of sums
-    const float none_yet = __int_as_float(0xFF800000);
-    Peaks q{none_yet, none_yet, none_yet, none_yet, -1, -1, -1};
+    Peaks q{kLowest, kLowest, kLowest, kLowest};
     const Pair c2 = both(p.c);
     Piece cur[kVecs];
     if (from < to) z.load_step(from, lane, cur);
@@ -425,15 +435,15 @@ __global__ void __launch_bounds__(kOf * 32, 32 / kOf) logprob_kernel(const __gri
         Piece next[kVecs];
         if (i + 1 < to) z.load_step(i + 1, lane, next);
         const float here = largest<kWide>(cur);
-        if (kTop) {   // (chosen, not branched; a NaN is above nothing)
-            const bool first = here > q.a, second = here > q.b, third = here > q.c;
-            q.d = third ? q.c : fmaxf(q.d, here);
-            q.c = second ? q.b : third ? here : q.c;
-            q.step_c = second ? q.step_b : third ? i : q.step_c;
-            q.b = first ? q.a : second ? here : q.b;
-            q.step_b = first ? q.step_a : second ? i : q.step_b;
-            q.a = first ? here : q.a;
-            q.step_a = first ? i : q.step_a;
+        if (kTop) {
+            float k = peak_of(here, i - from), less;
+            less = fminf(q.a, k);
+            q.a = fmaxf(q.a, k);
+            k = fminf(q.b, less);
+            q.b = fmaxf(q.b, less);
+            less = fminf(q.c, k);
+            q.c = fmaxf(q.c, k);
+            q.d = fmaxf(q.d, less);
         }
         if (here > m) {   // (false for a NaN)
             const float by = fmaxf((m - here) * p.c, -1000.f), f = pow2(by);
