@@ -294,9 +294,13 @@ __device__ __noinline__ K best_of(K list, Key (*room)[32], int share) {
     return list;
 }
 
+// Lanes whose steps are all read again, rather than every lane's (16384 rows of 32768, 20 alternatives: 302 us when that was
+// done for any, 232; a tenth of the rows has some).
+constexpr int kAgain = 8;
+
 // The 32 best of a warp's part of a row, those that reach T at least (all threads of the block call it).
 template <bool kWide>
-__device__ __noinline__ Key alternatives(const Row<kWide> z, const Peaks q, int from, int to, int share, int top,
+__device__ __forceinline__ Key alternatives(const Row<kWide> z, const Peaks q, int from, int to, int share, int top,
                                          Key (*room)[32]) {
     constexpr int E = kWide ? 4 : 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -315,14 +319,42 @@ __device__ __noinline__ Key alternatives(const Row<kWide> z, const Peaks q, int 
     const float T = floor_of(of_order(order));
     const bool low = !(T > kLowest);
     if (from >= to) return 0;
+    uint32_t again = __ballot_sync(0xffffffffu, floor_of(q.d) >= T);
     // (steps that 16 bits do not count are looked through as well)
-    if (__any_sync(0xffffffffu, low || floor_of(q.d) >= T || to - from > 65536)) return look_again(z, from, to, T, low, top);
+    if (low || __popc(again) > kAgain || to - from > 65536) return look_again(z, from, to, T, low, top);
     Key list = 0;
+    int round = 0, at = from;
 #pragma unroll 1
-    for (int round = 0; round < 3; ++round) {
-        const float peak = round == 0 ? q.a : round == 1 ? q.b : q.c;
-        const int step = from + (int)(__float_as_uint(peak) & 0xFFFF);
-        uint32_t who = __ballot_sync(0xffffffffu, floor_of(peak) >= T);
+    for (;;) {
+        int step, of = -1;   // this lane's step, if it reaches T; of: the lane whose step it was (-1: this one)
+        bool in;
+        if (round < 3) {
+            const float peak = round == 0 ? q.a : round == 1 ? q.b : q.c;
+            step = from + (int)(__float_as_uint(peak) & 0xFFFF);
+            in = floor_of(peak) >= T && !(again >> lane & 1);
+            ++round;
+        } else if (again != 0) {   // all steps of a lane that had more than three, 32 at a time
+            of = __ffs(again) - 1;
+            step = at + lane;
+            float here = __int_as_float(0xFF800000);
+            if (step < to) {
+#pragma unroll
+                for (int u = 0; u < kVecs; ++u) {
+                    Piece v;
+                    z.load(z.column(step, u, of), v);
+                    here = fmaxf(here, largest<kWide>(v));
+                }
+            }
+            in = here >= T;
+            at += 32;
+            if (at >= to) {
+                at = from;
+                again &= again - 1;
+            }
+        } else {
+            break;
+        }
+        uint32_t who = __ballot_sync(0xffffffffu, in);
         while (who != 0) {
             // (four steps' values at once: a lane reads one of each, as many as a lane's step has)
             Key k[4];
@@ -330,7 +362,7 @@ __device__ __noinline__ Key alternatives(const Row<kWide> z, const Peaks q, int 
             for (int j = 0; j < 4; ++j) {
                 const int src = __ffs(who) - 1;
                 who &= who - 1;
-                const int col = z.column(__shfl_sync(0xffffffffu, step, max(src, 0)), lane / E, src) + lane % E;
+                const int col = z.column(__shfl_sync(0xffffffffu, step, max(src, 0)), lane / E, of < 0 ? src : of) + lane % E;
                 k[j] = 0;
                 if (src >= 0 && lane < kVecs * E && col >= 0 && col < z.V) {
                     const float v = z.value(col);
@@ -411,6 +443,7 @@ __global__ void __launch_bounds__(kOf * 32, 32 / kOf) logprob_kernel(const __gri
     constexpr int E = kWide ? 4 : 8;
     __shared__ Key room[kTop ? kOf : 1][32];
     __shared__ Part part[kOf];
+    __shared__ Target targets[kTop ? kOf : 1];
     const LogProb &l = p.l;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, mine = warp & (p.share - 1);
     const long long rows = (long long)l.B * l.T;
@@ -476,9 +509,15 @@ __global__ void __launch_bounds__(kOf * 32, 32 / kOf) logprob_kernel(const __gri
     const F2 s2 = of_two(s), t2 = of_two(sum_t);
     Part a = join(Part{m, s2.x + s2.y, t2.x + t2.y, 0.f}, p.c);
     Key list = 0;
-    if (kTop) list = alternatives<kWide>(z, q, from, to, p.share, l.top, room);
+    if (lane == 0) part[warp] = a;
+    if (kTop) {   // (what is wanted after it lies in shared memory: registers that a call saves are memory traffic)
+        if (lane == 0) targets[warp] = target;
+        list = alternatives<kWide>(z, q, from, to, p.share, l.top, room);
+        __syncwarp();
+        a = part[warp];
+        target = targets[warp];
+    }
     if (p.share > 1) {
-        if (lane == 0) part[warp] = a;
         if (kTop) list = best_of(list, room, p.share);
         __syncthreads();
         if (mine != 0 || row >= rows) return;

@@ -358,6 +358,22 @@ def test_ties_rising_and_falling_rows(V):
             check_logprobs(z.contiguous(), None, 1, up=())
 
 
+@pytest.mark.parametrize("rows,V", [(6, 9003), (3, 40000), (10000, 4103)])
+@pytest.mark.parametrize("lanes,many", [(1, 4), (1, 9), (2, 7), (7, 5), (9, 4), (12, 30)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_alternatives_of_few_lanes(rows, V, lanes, many, dt):
+    """The largest entries `many` on each of some lanes, in columns a step of 1024 (bf16) or 512 apart: of the same size
+    and of different ones."""
+    z = logits_of(1, rows, V, dt, seed=14)
+    step, wide = (1024, 8) if dt is BF else (512, 4)
+    for j in range(many):
+        for n in range(lanes):
+            col = (j * step + (3 + 2 * n) * wide + j % wide) % V
+            z[0, :, col] = 20.0 + ((j * 7 + n) % 5 if rows % 2 == 0 else 0)
+    for top in (1, 4, 10, 32):
+        check_logprobs(z, None, top, up=())
+
+
 @pytest.mark.parametrize("V", [40, 3001, 40000])
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_masks(V, dt):
