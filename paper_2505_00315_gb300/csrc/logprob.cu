@@ -297,6 +297,7 @@ __device__ __noinline__ K best_of(K list, Key (*room)[32], int share) {
 // Lanes whose steps are all read again, rather than every lane's (16384 rows of 32768, 20 alternatives: 302 us when that was
 // done for any, 232; a tenth of the rows has some).
 constexpr int kAgain = 8;
+constexpr int kBatch = 4;   // steps read again at once (8: 88.5 us for 86.8, 4096 rows of 50001, 5 alternatives; 16: 92)
 
 // The 32 best of a warp's part of a row, those that reach T at least (all threads of the block call it).
 template <bool kWide>
@@ -323,54 +324,64 @@ __device__ __forceinline__ Key alternatives(const Row<kWide> z, const Peaks q, i
     // (steps that 16 bits do not count are looked through as well)
     if (low || __popc(again) > kAgain || to - from > 65536) return look_again(z, from, to, T, low, top);
     Key list = 0;
-    int round = 0, at = from;
+    // The steps to be read: of each lane's three, then all those of a lane that had more, 32 at a time.
+    const uint32_t once = ~again;
+    uint32_t m0 = __ballot_sync(0xffffffffu, floor_of(q.a) >= T) & once, m1 = __ballot_sync(0xffffffffu, floor_of(q.b) >= T) & once;
+    uint32_t m2 = __ballot_sync(0xffffffffu, floor_of(q.c) >= T) & once;
+    int step0 = from + (int)(__float_as_uint(q.a) & 0xFFFF), of = -1, at = from;   // of: the lane of all steps; -1: each its own
+    const int step1 = from + (int)(__float_as_uint(q.b) & 0xFFFF), step2 = from + (int)(__float_as_uint(q.c) & 0xFFFF);
 #pragma unroll 1
     for (;;) {
-        int step, of = -1;   // this lane's step, if it reaches T; of: the lane whose step it was (-1: this one)
-        bool in;
-        if (round < 3) {
-            const float peak = round == 0 ? q.a : round == 1 ? q.b : q.c;
-            step = from + (int)(__float_as_uint(peak) & 0xFFFF);
-            in = floor_of(peak) >= T && !(again >> lane & 1);
-            ++round;
-        } else if (again != 0) {   // all steps of a lane that had more than three, 32 at a time
+        if ((m0 | m1 | m2) == 0) {
+            if (again == 0) break;
             of = __ffs(again) - 1;
-            step = at + lane;
+            step0 = at + lane;
             float here = __int_as_float(0xFF800000);
-            if (step < to) {
+            if (step0 < to) {
 #pragma unroll
                 for (int u = 0; u < kVecs; ++u) {
                     Piece v;
-                    z.load(z.column(step, u, of), v);
+                    z.load(z.column(step0, u, of), v);
                     here = fmaxf(here, largest<kWide>(v));
                 }
             }
-            in = here >= T;
+            m0 = __ballot_sync(0xffffffffu, here >= T);
             at += 32;
             if (at >= to) {
                 at = from;
                 again &= again - 1;
             }
-        } else {
-            break;
         }
-        uint32_t who = __ballot_sync(0xffffffffu, in);
-        while (who != 0) {
-            // (four steps' values at once: a lane reads one of each, as many as a lane's step has)
-            Key k[4];
+        // (some steps' values at once: a lane reads one of each, as many as a lane's step has)
+        float v[kBatch];
+        int col[kBatch];
+        uint32_t hits = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int src = __ffs(who) - 1;
-                who &= who - 1;
-                const int col = z.column(__shfl_sync(0xffffffffu, step, max(src, 0)), lane / E, of < 0 ? src : of) + lane % E;
-                k[j] = 0;
-                if (src >= 0 && lane < kVecs * E && col >= 0 && col < z.V) {
-                    const float v = z.value(col);
-                    if (v >= T) k[j] = key_of(v, col);
-                }
+        for (int j = 0; j < kBatch; ++j) {
+            const uint32_t m = m0 != 0 ? m0 : m1 != 0 ? m1 : m2;
+            const int src = __ffs(m) - 1;
+            const int step = __shfl_sync(0xffffffffu, m0 != 0 ? step0 : m1 != 0 ? step1 : step2, max(src, 0));
+            if (m0 != 0) m0 &= m0 - 1;
+            else if (m1 != 0) m1 &= m1 - 1;
+            else m2 &= m2 - 1;
+            col[j] = z.column(step, lane / E, of < 0 ? src : of) + lane % E;
+            v[j] = __int_as_float(0xFF800000);
+            if (src >= 0 && lane < kVecs * E && col[j] >= 0 && col[j] < z.V) v[j] = z.value(col[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) hits |= v[j] >= T ? 1u << j : 0u;
+#pragma unroll 1
+        for (uint32_t who; (who = __ballot_sync(0xffffffffu, hits != 0)) != 0;) {
+            const int j = __ffs(hits) - 1;
+            float y = v[0];
+            int at_col = col[0];
+#pragma unroll
+            for (int i = 1; i < kBatch; ++i) {
+                y = j == i ? v[i] : y;
+                at_col = j == i ? col[i] : at_col;
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) list = put_in(list, k[j], __ballot_sync(0xffffffffu, k[j] != 0), lane);
+            list = put_in(list, hits != 0 ? key_of(y, at_col) : 0, who, lane);
+            hits &= hits - 1;
         }
     }
     return list;
