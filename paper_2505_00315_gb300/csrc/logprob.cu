@@ -280,18 +280,16 @@ __device__ __forceinline__ float floor_of(float peak) {
     return __uint_as_float((b & 0xFFFF0000u) | (b >> 31 ? 0xFFFFu : 0u));
 }
 
-// The 32 best of the lists of `share` warps side by side, in the first of them (all threads of the block).
+// The 32 best of the lists that `share` warps (2, 4 or 8) left in shared memory.
 template <class K>
-__device__ __noinline__ K best_of(K list, Key (*room)[32], int share) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i = warp & (share - 1);
+__device__ __noinline__ K best_of(const K (*room)[32], int share, int lane) {
+    K a = room[0][lane], b = room[1][lane];
 #pragma unroll 1
-    for (int o = share / 2; o > 0; o /= 2) {
-        __syncthreads();
-        if (i >= o && i < 2 * o) room[warp][lane] = list;
-        __syncthreads();
-        if (i < o) list = merged(list, (K)room[warp + o][lane], lane);
+    for (int i = 2; i < share; i += 2) {   // (two chains side by side)
+        a = merged(a, room[i][lane], lane);
+        b = merged(b, room[i + 1][lane], lane);
     }
-    return list;
+    return merged(a, b, lane);
 }
 
 // Lanes whose steps are all read again, rather than every lane's (16384 rows of 32768, 20 alternatives: 302 us when that was
@@ -302,21 +300,18 @@ constexpr int kBatch = 4;   // steps read again at once (8: 88.5 us for 86.8, 40
 // The 32 best of a warp's part of a row, those that reach T at least (all threads of the block call it).
 template <bool kWide>
 __device__ __forceinline__ Key alternatives(const Row<kWide> z, const Peaks q, int from, int to, int share, int top,
-                                         Key (*room)[32]) {
+                                         uint32_t (*room)[32]) {
     constexpr int E = kWide ? 4 : 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t best = sorted(order_of(q.a), lane);
     // (few lanes for many entries: the others of a lane's steps count, which makes T larger)
     if (top > 8 * share) best = merged(merged(best, sorted(order_of(q.b), lane), lane), sorted(order_of(q.c), lane), lane);
-    best = best_of(best, room, share);
-    uint32_t order = __shfl_sync(0xffffffffu, best, top - 1);
     if (share > 1) {
+        room[warp][lane] = best;
         __syncthreads();
-        if ((warp & (share - 1)) == 0 && lane == 0) room[warp][0] = order;
-        __syncthreads();
-        order = (uint32_t)room[warp & ~(share - 1)][0];
-        __syncthreads();
+        best = best_of(room + (warp & ~(share - 1)), share, lane);
     }
+    const uint32_t order = __shfl_sync(0xffffffffu, best, top - 1);
     const float T = floor_of(of_order(order));
     const bool low = !(T > kLowest);
     if (from >= to) return 0;
@@ -452,6 +447,7 @@ template <bool kWide, bool kTop, int kOf>
 __global__ void __launch_bounds__(kOf * 32, 32 / kOf) logprob_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int E = kWide ? 4 : 8;
+    __shared__ uint32_t bars[kTop ? kOf : 1][32];
     __shared__ Key room[kTop ? kOf : 1][32];
     __shared__ Part part[kOf];
     __shared__ Target targets[kTop ? kOf : 1];
@@ -523,15 +519,16 @@ __global__ void __launch_bounds__(kOf * 32, 32 / kOf) logprob_kernel(const __gri
     if (lane == 0) part[warp] = a;
     if (kTop) {   // (what is wanted after it lies in shared memory: registers that a call saves are memory traffic)
         if (lane == 0) targets[warp] = target;
-        list = alternatives<kWide>(z, q, from, to, p.share, l.top, room);
+        list = alternatives<kWide>(z, q, from, to, p.share, l.top, bars);
         __syncwarp();
         a = part[warp];
         target = targets[warp];
     }
     if (p.share > 1) {
-        if (kTop) list = best_of(list, room, p.share);
+        if (kTop) room[warp][lane] = list;
         __syncthreads();
         if (mine != 0 || row >= rows) return;
+        if (kTop) list = best_of(room + warp, p.share, lane);
         a = join(lane < p.share ? part[warp + lane] : Part{kLeast, 0.f, 0.f, 0.f}, p.c);
         if (p.segments > 1) {
             if (lane == 0) p.parts[blockIdx.x] = a;
@@ -555,9 +552,11 @@ __global__ void __launch_bounds__(kThreads) logprob_join_kernel(const __grid_con
     if (kTop) {
 #pragma unroll 1
         for (int i = warp; i < p.segments; i += kWarps) list = merged(list, (Key)p.tops[(at + i) * 32 + lane], lane);
-        list = best_of(list, room, kWarps);
+        room[warp][lane] = list;
+        __syncthreads();
     }
     if (warp != 0) return;
+    if (kTop) list = best_of(room, kWarps, lane);
     const Part none{kLeast, 0.f, 0.f, 0.f};
     const Part a = join(lane < p.segments ? p.parts[at + lane] : none, p.c);
     finish<kTop>(p, row, a, target, list, lane);
