@@ -105,6 +105,7 @@ mosa_status check_logprob(const mosa_logprob_shape *s, bool backward, LogProb *l
     l->T = s->T;
     l->V = s->V;
     l->target64 = s->target64;
+    l->z.wide = l->dz.wide = s->dtype == MOSA_F32;
     l->top = s->top;
     l->scale = s->scale;
     const mosa_strides a = {s->z.b, s->z.t, 0}, b = {s->dz.b, s->dz.t, 0};

@@ -706,27 +706,37 @@ int steps_of(const LogProb &l) {   // (as if a row started at a multiple of 16 b
     return (int)(((long long)l.V + K - 1) / K);
 }
 
-// Forward: warps of a block, how many of them share a row, and how many blocks do.  As few warps a row as make
-// two rounds of all SMs' warps, so that the last one, which leaves SMs idle, is short; as many as have some
-// steps each.  Small blocks wait for fewer of their warps, large ones share a row between more.  us in blocks of 4 / 8
-// (bf16, no alternatives; 5; 20):
-//     4096 rows of 50001   72 / 73    103 / 108   130 / 130
-//     1024 of 131072       48 / 51     60 / 67     83 / 70
-//     1000 of 32003        16 / 18     22 / 28     39 / 31
-//     300 of 32003          7 / 6      14 / 10     17 / 12
-// More blocks a row than one cost a second kernel: 300 rows of 32003 took 7.2 us with two, 5.9 with one.
+// Forward: warps of a block, how many of them share a row, and how many blocks do.  What a choice costs is counted in steps of a
+// warp while all SMs' warps are at work (1.6 us): a round of all of them takes a row's steps, one of a share x of them 0.41 + 0.59 x
+// of that (fewer warps wait less for memory, which they leave idle), and each round its beginning and its end.
+// us with 1 / 2 / 4 / 8 / 16 warps of a row (bf16; 16: two blocks and the second kernel), the choice in brackets:
+//     4096 rows of 32003   [48] / 50 / 51 / 57        5 alternatives   [54] / 57 / 61 / 76
+//     1000 of 32003        29 / 19 / [15] / 18 / 19                    32 / 22 / [18] / 23 / 31
+//     300 of 32003         27 / 16 / 10 / [8] / 9                      30 / 18 / 12 / [11] / 14
+//     300 of 131072        94 / 49 / 28 / 19 / [18]                    99 / 53 / 31 / 22 / [23]
 struct Split {
     int of, share, segments;
 };
 Split split(const LogProb &l) {
-    const long long rows = (long long)l.B * l.T, all = 32LL * kSms;
-    // (counted alike for both types and places, so that the workspace's size does not hang on a pointer)
-    const long long steps = ((long long)l.V + 1023) / 1024;
-    Split p{rows * kFewWarps * 4 >= 3 * all ? kFewWarps : kWarps, 1, 1};
-    while (p.share < p.of && rows * p.share < 2 * all && steps >= 4 * p.share) p.share *= 2;
-    if (p.share < kWarps) return p;
-    const long long n = std::min(std::min(32LL, steps / kWarps), all / (rows * kWarps));
-    if (n >= 3) p.segments = (int)n;
+    const long long rows = (long long)l.B * l.T, all = 32LL * kSms, steps = steps_of(l);
+    const double end = l.top > 0 ? 3.2 + 0.17 * l.top : 1.6, join = l.top > 0 ? 2.8 : 1.3;
+    auto cost = [&](long long warps) {   // of a row
+        const long long w = rows * warps, full = w / all;
+        const double x = (double)(w % all) / all, part = x > 0 ? 1 : 0;
+        return (double)((steps + warps - 1) / warps) * (full + part * (0.41 + 0.59 * x)) + (full + part) * end;
+    };
+    Split p{kFewWarps, 1, 1};
+    double best = cost(1);
+    for (int share = 2; share <= kWarps && share <= steps; share *= 2)
+        if (const double c = cost(share); c < best) {
+            best = c;
+            p = Split{share == kWarps ? kWarps : kFewWarps, share, 1};
+        }
+    for (int n = 2; n <= 32 && n * kWarps <= steps; ++n)
+        if (const double c = cost(n * kWarps) + join; c < best) {
+            best = c;
+            p = Split{kWarps, kWarps, n};
+        }
     return p;
 }
 
