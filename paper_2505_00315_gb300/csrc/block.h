@@ -20,13 +20,14 @@ struct Rows {
     long long b, t;        // strides in bytes
     int wide;
     int vec;               // every row starts at a multiple of 16 bytes
+    int jump;              // residual step: bytes from a sequence's end to the next one's beginning
     __host__ __device__ char *at(int ib, int it) const { return p + ib * b + it * t; }
 };
 
 inline Rows rows_of(const void *p, const Str &s, int dtype) {
     const int wide = dtype == MOSA_F32, e = wide ? 4 : 2;
     return Rows{(char *)p, s.b * e, s.t * e, wide,
-                ((uintptr_t)p % 16 == 0) && s.b * e % 16 == 0 && s.t * e % 16 == 0};
+                ((uintptr_t)p % 16 == 0) && s.b * e % 16 == 0 && s.t * e % 16 == 0, 0};
 }
 
 // A vector [d]; null: not there.

@@ -31,13 +31,14 @@ struct Args {
     int stages, stage_bytes;
     int off[kIn];       // of each tensor within a warp's stage
     int flat;           // every tensor's rows lie one stride apart, sequences too
+    int near;           // strides and jumps fit 32 bits
     int held;           // gammas and gate are in shared memory (all but the widest fp32 rows' backward)
 };
 
 // Which of the tensors are fp32: 0 or 1, or -1 where that is only known at run time.  Such kernels
 // also take rows of any place, stride and number of columns (16-byte pieces arrive as they lie in memory,
-// and what is read from them is shifted); those of known types take rows of whole pieces, one stride
-// apart, and have gammas and gate in shared memory: no branch stands between their loads.
+// and what is read from them is shifted); those of known types take rows of whole pieces and near
+// strides, and have gammas and gate in shared memory: no branch stands between their loads.
 // (kHeld 0: gammas and gate are not there, and are read where they lie.)
 template <int kX, int kY, int kDh, int kStorage, int kHeld_ = 1>
 struct Types {
@@ -354,21 +355,33 @@ __device__ __forceinline__ char *row_at(const Args &p, const Rows &m, uint32_t r
     return m.at((int)b, (int)(row - b * (uint32_t)p.r.T));
 }
 
-// One tensor's rows on their way to the ring.  Of known types: from pointers that move on from row to row.
-template <int C, bool kFast, int kWide>
+// With near strides: a row's start, and how many sequences end between a group's row and its next.
+__device__ __forceinline__ char *near_at(const Args &p, const Rows &m, uint32_t row) {
+    return m.p + (uint64_t)row * (uint32_t)m.t + (p.flat ? 0LL : (long long)(row / (uint32_t)p.r.T) * m.jump);
+}
+__device__ __forceinline__ int ends_between(const Args &p, const Place &l, uint32_t row) {
+    return (int)((row + l.step) / (uint32_t)p.r.T - row / (uint32_t)p.r.T);
+}
+
+// One tensor's rows on their way to the ring.  Of known types: from pointers that move on from row to row, or (kCounts)
+// counted from the row, which takes instructions (3% of the backward's time) but no registers: the forward with 24 or
+// 32 columns a thread, which spills else (4096 fp32 rows of 8192: 112 -> 88 us).
+template <int C, bool kFast, int kWide, bool kCounts = false>
 struct Arrival {
-    const char *next;   // kFast: this lane's place in the next row
+    const char *next;   // this lane's place in the next row
     __device__ __forceinline__ void init(const Args &p, const Place &l, const Rows &m, uint32_t row) {
-        if (kFast) next = m.p + (uint64_t)row * (uint32_t)m.t + (kWide ? 4 * l.col0 : 2 * l.col0) + 16 * l.lane;
+        if (kFast && !kCounts) next = near_at(p, m, row) + (kWide ? 4 * l.col0 : 2 * l.col0) + 16 * l.lane;
     }
+    __device__ __forceinline__ void jump(const Rows &m, int ends) { next += (long long)ends * m.jump; }
     // To the shared address `to`.
     __device__ __forceinline__ void issue(const Args &p, const Place &l, const Rows &m, uint32_t row, uint32_t to) {
         if (kFast) {
+            if (kCounts) next = near_at(p, m, row) + ((kWide ? 4 * l.col0 : 2 * l.col0) + 16 * l.lane);
             const uint32_t dst = to + (kWide ? piece_at(l.lane) : 16 * l.lane);
 #pragma unroll
             for (int i = 0; i < (kWide ? 2 * C : C); ++i)
                 if (l.col0 + (kWide ? 128 * i + 4 * l.lane : 256 * i + 8 * l.lane) < l.d) copy16(dst + 512 * i, next + 512 * i);
-            next += (uint64_t)l.step * (uint32_t)m.t;
+            if (!kCounts) next += (uint64_t)l.step * (uint32_t)m.t;
             return;
         }
         // The 16-byte pieces in which the columns lie (device memory is allocated in larger ones, so the bytes
@@ -396,20 +409,22 @@ __device__ __forceinline__ Oct arrived(const char *from, int wide, const Place &
 }
 
 // Rows of one tensor that leave.
-template <int C, bool kFast, int kWide, bool kDirect = false>
+template <int C, bool kFast, int kWide, bool kDirect = false, bool kCounts = false>
 struct Departure {
-    char *at;   // the row's columns of the warp
+    char *at;   // the row
     __device__ __forceinline__ void init(const Args &p, const Place &l, const Rows &m, uint32_t row) {
-        if (kFast) at = m.p + (uint64_t)row * (uint32_t)m.t;
+        if (kFast && !kCounts) at = near_at(p, m, row);
     }
+    __device__ __forceinline__ void jump(const Rows &m, int ends) { at += (long long)ends * m.jump; }
     __device__ __forceinline__ void begin(const Args &p, const Rows &m, uint32_t row) {
         if (!kFast) at = row_at(p, m, row);
+        else if (kCounts) at = near_at(p, m, row);
     }
     __device__ __forceinline__ void put_row(const Place &l, const Rows &m, int c, const Oct &v) {
         put<kFast, kWide, kDirect>(m, at, l.col0 + 256 * c, l.d, l.scratch, l.lane, v);
     }
     __device__ __forceinline__ void end(const Place &l, const Rows &m) {
-        if (kFast) at += (uint64_t)l.step * (uint32_t)m.t;
+        if (kFast && !kCounts) at += (uint64_t)l.step * (uint32_t)m.t;
     }
 };
 
@@ -502,6 +517,16 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
         else if (r.B > 1 && m->b != m->t * r.T) p.flat = 0;
         if (m->t >= 1LL << 32) p.flat = 0;
     }
+    p.near = p.flat;
+    if (!p.flat && r.B > 1 && r.T > 1) {
+        p.near = 1;
+        for (Rows *m : all) {
+            if (m->p == nullptr) continue;
+            const long long jump = m->b - m->t * r.T;
+            if (m->t >= 1LL << 32 || jump >= 1LL << 31 || jump < -(1LL << 31)) p.near = 0;
+            else m->jump = (int)jump;
+        }
+    }
     if (r.T == 1 && !p.flat)
         for (Rows *m : all) m->t = 0;
     const int each = times_of(r, backward, &p.most);
@@ -538,7 +563,7 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
 // Whether a kernel of known types takes the call's places and strides.
 inline bool fast(const Args &p) {
     const Residual &r = p.r;
-    bool vec = p.flat;
+    bool vec = p.near;
     for (const Rows *m : {&r.x, &r.y, &r.g, &r.xo, &r.h, &r.dxo, &r.dh, &r.dx, &r.dy, &r.dg})
         vec = vec && (m->p == nullptr || m->vec);
     return vec;

@@ -59,9 +59,18 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         if (has_dh) dh_in.issue(p, l, r.dh, at, to + dh_off);
         if (token) g_in.issue(p, l, r.g, at, to + g_off);
     };
+    auto jump = [&](uint32_t at) {   // (after fill)
+        const int ends = ends_between(p, l, at);
+        x_in.jump(r.x, ends);
+        y_in.jump(r.y, ends);
+        dxo_in.jump(r.dxo, ends);
+        dh_in.jump(r.dh, ends);
+        g_in.jump(r.g, ends);
+    };
     const int ahead = p.stages - 1;
     for (int i = 0; i < ahead; ++i) {
         if (row + i * l.step < l.rows) fill(row + i * l.step, i);
+        if (kFast && !p.flat) jump(row + i * l.step);
         copies_end();
     }
     if (Ty::kHeld || (!Ty::kLies && p.held)) hold<C, false>(p, l, unit);
@@ -179,6 +188,13 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         dx_out.end(l, r.dx);
         dy_out.end(l, r.dy);
         dg_out.end(l, r.dg);
+        if (kFast && !p.flat) {
+            jump(row + ahead * l.step);
+            const int ends = ends_between(p, l, row);
+            dx_out.jump(r.dx, ends);
+            dy_out.jump(r.dy, ends);
+            dg_out.jump(r.dg, ends);
+        }
     }
     if (p.partial != nullptr) {
         copies_wait(0);

@@ -14,7 +14,7 @@ namespace {
 template <int C, class Ty>
 __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    constexpr bool kFast = Ty::kFast;
+    constexpr bool kFast = Ty::kFast, kCounts = kFast && C > 2;
     extern __shared__ __align__(16) char smem[];
     const Residual &r = p.r;
     const Place l(p, smem, C);
@@ -23,14 +23,14 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
     const float unit = r.scale * (drops ? r.drop.scale : 1.f), inv_d = 1.f / l.d;
     if (l.d < 256 * C * l.W) clear_ring(l);
     uint32_t row = blockIdx.x * p.groups + l.group;   // (row + kMaxStages step fits 32 bits)
-    Arrival<C, kFast, Ty::x> x_in;
-    Arrival<C, kFast, Ty::y> y_in;
-    Arrival<C, kFast, Ty::storage> g_in;
+    Arrival<C, kFast, Ty::x, kCounts> x_in;
+    Arrival<C, kFast, Ty::y, kCounts> y_in;
+    Arrival<C, kFast, Ty::storage, kCounts> g_in;
     x_in.init(p, l, r.x, row);
     y_in.init(p, l, r.y, row);
     g_in.init(p, l, r.g, row);
-    Departure<C, kFast, Ty::x> x_out;
-    Departure<C, kFast, Ty::storage> h_out;
+    Departure<C, kFast, Ty::x, false, kCounts> x_out;
+    Departure<C, kFast, Ty::storage, false, kCounts> h_out;
     x_out.init(p, l, r.xo, row);
     h_out.init(p, l, r.h, row);
     // Where the tensors' columns lie in a stage.
@@ -41,9 +41,16 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
         y_in.issue(p, l, r.y, at, to + y_off);
         if (token) g_in.issue(p, l, r.g, at, to + g_off);
     };
+    auto jump = [&](uint32_t at) {   // (after fill)
+        const int ends = ends_between(p, l, at);
+        x_in.jump(r.x, ends);
+        y_in.jump(r.y, ends);
+        g_in.jump(r.g, ends);
+    };
     const int ahead = p.stages - 1;
     for (int i = 0; i < ahead; ++i) {
         if (row + i * l.step < l.rows) fill(row + i * l.step, i);
+        if (kFast && !kCounts && !p.flat) jump(row + i * l.step);
         copies_end();
     }
     if (Ty::kHeld || (!Ty::kLies && p.held)) hold<C, true>(p, l, unit);
@@ -116,6 +123,12 @@ __global__ void __launch_bounds__(kThreads, 1) residual_kernel(const __grid_cons
         if (r.stats != nullptr && l.w == 0 && l.lane == 0) {
             r.stats[row] = ry;
             r.stats[(uint64_t)l.rows + row] = rx;
+        }
+        if (kFast && !kCounts && !p.flat) {
+            jump(row + ahead * l.step);
+            const int ends = ends_between(p, l, row);
+            x_out.jump(r.xo, ends);
+            h_out.jump(r.h, ends);
         }
     }
 }

@@ -129,6 +129,32 @@ def test_strides_and_places():
         assert (t[..., :3] == 7).all() and (t[..., 3 + d:] == 7).all(), n
 
 
+@pytest.mark.parametrize("dt,xt,yt,d", [(BF, BF, BF, 1024), (BF, F32, F32, 520), (BF, BF, F32, 3000), (F32, F32, F32, 256)])
+@pytest.mark.parametrize("gate", ["channel", "token"])
+def test_some_tokens_of_longer_sequences(dt, xt, yt, d, gate):
+    """Tokens 2 to T + 1 of T + 5, in and out, alone and beside whole tensors; sequences that follow each other
+    backwards through memory's order (the batch inside the tokens)."""
+    B, T = 3, 90
+    s, dx_out, dh = inputs(B, T + 5, d, dt, xt, yt, yt, gate, seed=21)
+    cut = lambda t: t[:, 2:2 + T]   # noqa: E731
+    swap = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)   # noqa: E731
+    whole = {n: cut(t) if t is not None and t.dim() == 3 else t for n, t in s.items()}
+    kw = dict(scale=0.5, dropout=0.2, rng=state(), sigmoid=gate == "token")
+    want = residual(**whole, dx_out=cut(dx_out), dh=cut(dh), backward=True, **kw)
+    types = {"x": xt, "h": dt, "dx": xt, "dy": dt, "dgate": dt}
+    for mine, theirs in ((lambda t: t, lambda t: t), (lambda t: t, lambda t: t.contiguous()), (swap, lambda t: t)):
+        room = {n: torch.full((B, T + 5, d), 7.0, device="cuda", dtype=types[n]) for n in types
+                if n != "dgate" or gate == "token"}
+        out = {n: cut(t) for n, t in room.items()}
+        given = {**whole, "x": mine(whole["x"]), "y": theirs(whole["y"])}
+        x, h, stats = mosa.mosa_residual_forward(**given, out=out, **kw)
+        g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=theirs(cut(dx_out)), dh=mine(cut(dh)), out=out, **given, **kw)
+        for n, (ref, bound) in want.items():
+            near(n, {"x": x, "h": h, **g}[n], ref, bound)
+        for n, t in room.items():
+            assert (t[:, :2] == 7).all() and (t[:, 2 + T:] == 7).all(), n
+
+
 def test_in_place():
     s, dx_out, dh = inputs(4, 100, 1024, gate="channel", seed=5)
     kw = dict(dropout=0.1, rng=state())
