@@ -18,8 +18,9 @@
 namespace mosa {
 namespace blk {
 
-// kMost: warps of a block at most.
-template <int C, int kMost, class Ty>
+// kMost: warps of a block at most.  kCut: sequences lie apart; kernels of their own, since the jumps between them cost
+// registers (B2 T8192 d4096: 248 us in one kernel with the others, 242).
+template <int C, int kMost, class Ty, bool kCut>
 __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr bool kFast = Ty::kFast;
@@ -70,7 +71,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
     const int ahead = p.stages - 1;
     for (int i = 0; i < ahead; ++i) {
         if (row + i * l.step < l.rows) fill(row + i * l.step, i);
-        if (kFast && !p.flat) jump(row + i * l.step);
+        if (kCut) jump(row + i * l.step);
         copies_end();
     }
     if (Ty::kHeld || (!Ty::kLies && p.held)) hold<C, false>(p, l, unit);
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         dx_out.end(l, r.dx);
         dy_out.end(l, r.dy);
         dg_out.end(l, r.dg);
-        if (kFast && !p.flat) {
+        if (kCut) {
             jump(row + ahead * l.step);
             const int ends = ends_between(p, l, row);
             dx_out.jump(r.dx, ends);
@@ -238,38 +239,49 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
 }
 
 // The kernel for a call's types.
-template <int C, int kMost, class Ty>
+template <int C, int kMost, class Ty, bool kCut>
 cudaError_t go(const Args &p, int blocks, int bytes, cudaStream_t s) {
-    const auto kernel = residual_bwd_kernel<C, kMost, Ty>;
+    const auto kernel = residual_bwd_kernel<C, kMost, Ty, kCut>;
     cudaError_t e = allow_smem((const void *)kernel, kSmem);
     if (e != cudaSuccess) return e;
     note_launches(1);
     return launch_pdl(kernel, dim3(blocks), dim3(p.warps * p.groups * 32), bytes, s, p);
 }
-template <int C, int kMost>
+template <int C, int kMost, bool kCut>
 cudaError_t go_by_types(const Args &p, int blocks, int bytes, cudaStream_t s) {
     const Residual &r = p.r;
     const int x = r.x.wide, y = r.y.wide, dh = r.dh.wide, st = r.storage_wide;
-    if (!fast(p) || (st && !(x && y && dh)) || (!p.held && !(C == 4 && st)))
-        return go<C, kMost, Types<-1, -1, -1, -1>>(p, blocks, bytes, s);
     if constexpr (C == 4)
-        if (!p.held) return go<C, kMost, Types<1, 1, 1, 1, 0>>(p, blocks, bytes, s);
-    if (st) return go<C, kMost, Types<1, 1, 1, 1>>(p, blocks, bytes, s);
+        if (!p.held) return go<C, kMost, Types<1, 1, 1, 1, 0>, kCut>(p, blocks, bytes, s);
+    if (st) return go<C, kMost, Types<1, 1, 1, 1>, kCut>(p, blocks, bytes, s);
     switch (4 * x + 2 * y + dh) {
-        case 0: return go<C, kMost, Types<0, 0, 0, 0>>(p, blocks, bytes, s);
-        case 1: return go<C, kMost, Types<0, 0, 1, 0>>(p, blocks, bytes, s);
-        case 2: return go<C, kMost, Types<0, 1, 0, 0>>(p, blocks, bytes, s);
-        case 3: return go<C, kMost, Types<0, 1, 1, 0>>(p, blocks, bytes, s);
-        case 4: return go<C, kMost, Types<1, 0, 0, 0>>(p, blocks, bytes, s);
-        case 5: return go<C, kMost, Types<1, 0, 1, 0>>(p, blocks, bytes, s);
-        case 6: return go<C, kMost, Types<1, 1, 0, 0>>(p, blocks, bytes, s);
-        default: return go<C, kMost, Types<1, 1, 1, 0>>(p, blocks, bytes, s);
+        case 0: return go<C, kMost, Types<0, 0, 0, 0>, kCut>(p, blocks, bytes, s);
+        case 1: return go<C, kMost, Types<0, 0, 1, 0>, kCut>(p, blocks, bytes, s);
+        case 2: return go<C, kMost, Types<0, 1, 0, 0>, kCut>(p, blocks, bytes, s);
+        case 3: return go<C, kMost, Types<0, 1, 1, 0>, kCut>(p, blocks, bytes, s);
+        case 4: return go<C, kMost, Types<1, 0, 0, 0>, kCut>(p, blocks, bytes, s);
+        case 5: return go<C, kMost, Types<1, 0, 1, 0>, kCut>(p, blocks, bytes, s);
+        case 6: return go<C, kMost, Types<1, 1, 0, 0>, kCut>(p, blocks, bytes, s);
+        default: return go<C, kMost, Types<1, 1, 1, 0>, kCut>(p, blocks, bytes, s);
     }
 }
 
-// Blocks of 8 warps, 16 or 32 columns a thread (files of their own for the compiler's time).
+// Sequences that lie apart, `times` eights of columns a thread; blocks of 8 warps with two and with four (files of
+// their own for the compiler's time).
+cudaError_t residual_bwd_cut(const Args &p, int times, int blocks, int bytes, cudaStream_t s);
+cudaError_t residual_bwd_16_cut(const Args &p, int blocks, int bytes, cudaStream_t s);
 cudaError_t residual_bwd_16(const Args &p, int blocks, int bytes, cudaStream_t s);
 cudaError_t residual_bwd_32(const Args &p, int blocks, int bytes, cudaStream_t s);
+
+// The kernel for a call: of its types, where its places, strides and types have one.
+template <int C, int kMost>
+cudaError_t go_by_places(const Args &p, int blocks, int bytes, cudaStream_t s) {
+    const Residual &r = p.r;
+    const int st = r.storage_wide;
+    if (!fast(p) || (st && !(r.x.wide && r.y.wide && r.dh.wide)) || (!p.held && !(C == 4 && st)))
+        return go<C, kMost, Types<-1, -1, -1, -1>, false>(p, blocks, bytes, s);
+    return p.flat ? go_by_types<C, kMost, false>(p, blocks, bytes, s) : residual_bwd_cut(p, C, blocks, bytes, s);
+}
 
 }  // namespace blk
 }  // namespace mosa
