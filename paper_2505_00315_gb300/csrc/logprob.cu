@@ -11,15 +11,15 @@
 // A warp takes a row, or 2, 4 or 8 of a block share one where rows are fewer, or some blocks, whose
 // results a second kernel joins.  Rows move in 16-byte pieces wherever they start: a row is cut at the
 // addresses' multiples of 16, its first and last pieces are read value by value.
-// us and share of the copy rate, bf16: 16384 rows of 32768 forward 170 (93%), backward 312 (all of it); 4096 rows of 50001 forward
-// 72 (84%), with 5 alternatives 103 (59%: 9.6 instructions a value, and each warp's end a chain); fp32, 1000 rows of 32003
-// with 8: 38 and 44 (49%, 86%); 8 rows of 131072 with 20: 10, two launches.
+// us and share of the copy rate, bf16: 16384 rows of 32768 forward 170 (93%), backward 312 (all of it); 4096 rows of 50001
+// forward 70 (86%), with 5 alternatives 76.5 (79%: 7.7 instructions a value, and each warp's end a chain); fp32, 1000 rows
+// of 32003 with 8: 27.5 and 44 (68%, 86%); 8 rows of 131072 with 20: 8.6, two launches.
 //
 // Alternatives: the pass over the row only notes, for each lane, the largest values of its three best steps (32 bf16
 // or 16 fp32 values a step) and that of the fourth.  A value T that the largest of `top` steps of lanes reach is
 // one that `top` entries reach at least, so that the wanted ones lie in the few steps of lanes whose largest reaches it:
-// those are read once more.  (Where a lane's fourth best reaches T as well, as with equal values, its warp
-// looks through its part of the row again.)  The best 32 entries are kept one a lane, in falling order, as 64-bit keys:
+// those are read once more.  (Where a lane's fourth best reaches T as well, all steps of that lane are; where that is
+// so for many lanes, as with equal values, the warp looks through its part of the row again.)  The best 32 entries are kept one a lane, in falling order, as 64-bit keys:
 // the value's bits in an order of integers, then the index, low ones first.
 #include <algorithm>
 #include <cmath>

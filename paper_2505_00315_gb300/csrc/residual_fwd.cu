@@ -2,9 +2,9 @@
 //     n = r_y y gamma_post,  u = keep/(1-p) g n,  x' = x + scale u,  h = r_x x' gamma_pre
 // with r = 1/sqrt(mean of squares + eps).  Layout and tools: residual.cuh.
 // Memory bound: x, y (and a gate per token) come in, x' and h go out, once; a row's squares are summed twice, of y and of
-// x', which is the chain of a row.  us and share of the copy rate: B4 T4096 d1024 with fp32 y 29.5 (84%), with dropout 33
-// (75%: the random words are 14 of its 27 instructions a value); B2 T8192 d4096, fp32 stream, gate per token, dropout 150
-// (92%); eight tokens of 1024: 2.8.
+// x', which is the chain of a row.  us and share of the copy rate: B4 T4096 d1024 with fp32 y 28.7 (86%), with dropout 30
+// (82%: the random words are 14 of its 29 instructions a value); B2 T8192 d4096, fp32 stream, gate per token, dropout 151
+// (91%); eight tokens of 1024: 2.9.
 #include "residual.cuh"
 
 namespace mosa {
