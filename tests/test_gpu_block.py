@@ -129,12 +129,15 @@ def test_strides_and_places():
         assert (t[..., :3] == 7).all() and (t[..., 3 + d:] == 7).all(), n
 
 
-@pytest.mark.parametrize("dt,xt,yt,d", [(BF, BF, BF, 1024), (BF, F32, F32, 520), (BF, BF, F32, 3000), (F32, F32, F32, 256)])
+@pytest.mark.parametrize("dt,xt,yt,T,d", [(BF, BF, BF, 90, 1024), (BF, F32, F32, 90, 520), (BF, BF, F32, 90, 3000),
+                                          (F32, F32, F32, 90, 256), (BF, F32, BF, 40, 5000), (F32, F32, F32, 40, 8192),
+                                          (BF, BF, BF, 40, 8192), (BF, BF, F32, 3300, 1024), (BF, F32, F32, 3300, 1024),
+                                          (F32, F32, F32, 3300, 1024)])
 @pytest.mark.parametrize("gate", ["channel", "token"])
-def test_some_tokens_of_longer_sequences(dt, xt, yt, d, gate):
+def test_some_tokens_of_longer_sequences(dt, xt, yt, T, d, gate):
     """Tokens 2 to T + 1 of T + 5, in and out, alone and beside whole tensors; sequences that follow each other
     backwards through memory's order (the batch inside the tokens)."""
-    B, T = 3, 90
+    B = 3
     s, dx_out, dh = inputs(B, T + 5, d, dt, xt, yt, yt, gate, seed=21)
     cut = lambda t: t[:, 2:2 + T]   # noqa: E731
     swap = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)   # noqa: E731
