@@ -487,9 +487,10 @@ mosa_status mosa_residual_forward(const mosa_residual_shape *shape, const void *
 size_t mosa_residual_workspace_bytes(const mosa_residual_shape *shape);
 
 /* Backward: from the forward's inputs and stats and the gradients dx_out (x_dtype) and dh
- * (dh_dtype; NULL with pre_norm = 0) of its outputs (either NULL: none; x is not read with pre_norm = 0), the
- * gradients dx (which may be dx_out itself), dy (storage dtype), of gate: dgate [d] fp32 or [B,T,d] in the storage dtype, and dgamma_post,
- * dgamma_pre [d] fp32.  Each of the last three may be NULL. */
+ * (dh_dtype; NULL with pre_norm = 0) of its outputs (either NULL: none; without dh x is not read, and dx is
+ * dx_out whatever x and y hold), the gradients dx (which may be dx_out itself), dy (storage dtype), of gate:
+ * dgate [d] fp32 or [B,T,d] in the storage dtype, and dgamma_post, dgamma_pre [d] fp32.  Each of the last
+ * three may be NULL. */
 mosa_status mosa_residual_backward(const mosa_residual_shape *shape, const void *x, const void *y,
                                    const void *gate, const void *gamma_post,
                                    const void *gamma_pre, const int64_t *rng, const float *stats,

@@ -43,7 +43,8 @@ cudaError_t launch_residual_bwd(const Residual &r, float *partial, cudaStream_t 
     p.partial = sums ? partial : nullptr;
     int blocks, times, bytes;
     shape(p, true, &blocks, &times, &bytes);
-    cudaError_t e = times == 1 ? go_by_places<1, kWarps>(p, blocks, bytes, s)
+    cudaError_t e = r.dh.p == nullptr ? residual_bwd_alone(p, times, blocks, bytes, s)
+                    : times == 1 ? go_by_places<1, kWarps, true>(p, blocks, bytes, s)
                     : times == 2 ? residual_bwd_16(p, blocks, bytes, s) : residual_bwd_32(p, blocks, bytes, s);
     if (e != cudaSuccess || !sums) return e;
     note_launches(1);

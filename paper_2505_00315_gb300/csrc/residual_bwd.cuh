@@ -19,8 +19,10 @@ namespace mosa {
 namespace blk {
 
 // kMost: warps of a block at most.  kCut: sequences lie apart; kernels of their own, since the jumps between them cost
-// registers (B2 T8192 d4096: 248 us in one kernel with the others, 242).
-template <int C, int kMost, class Ty, bool kCut>
+// registers (B2 T8192 d4096: 248 us in one kernel with the others, 242).  kSecond: the second norm has a gradient (dh).
+// Without one, dx is dx_out whatever x and y hold, so nothing of xh is computed, since 0 times an infinity of it would
+// count; kernels of their own for it, since a choice in each row moves registers (8192 rows of 8192: 170 -> 178 us).
+template <int C, int kMost, class Ty, bool kCut, bool kSecond>
 __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr bool kFast = Ty::kFast;
@@ -29,10 +31,9 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
     const Place l(p, smem, C);
     const DropKey key = drop_key(r.drop);
     const bool drops = r.drop.rng != nullptr, token = r.gate == MOSA_GATE_TOKEN;
-    const bool has_dxo = r.dxo.p != nullptr, has_dh = r.dh.p != nullptr;
+    const bool has_dxo = r.dxo.p != nullptr;
     const float unit = r.scale * (drops ? r.drop.scale : 1.f), inv_d = 1.f / l.d;   // unit: c of a kept value
-    // (x is not read without the second norm, whose xh alone needs it: zeros do, and no infinity of x counts)
-    if (l.d < 256 * C * l.W || !has_dxo || !has_dh || !r.pre) clear_ring(l);
+    if (l.d < 256 * C * l.W || !has_dxo) clear_ring(l);
     uint32_t row = blockIdx.x * p.groups + l.group;   // (row + kMaxStages step fits 32 bits)
     Arrival<C, kFast, Ty::x> x_in, dxo_in;
     Arrival<C, kFast, Ty::y> y_in;
@@ -54,18 +55,18 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
     const int g_off = kFast ? dh_off + bytes_of(Ty::dh, C) : p.off[4];
     auto fill = [&](uint32_t at, int slot) {
         const uint32_t to = l.ring32 + slot * p.stage_bytes;
-        if (r.pre) x_in.issue(p, l, r.x, at, to);
+        if (kSecond) x_in.issue(p, l, r.x, at, to);
         y_in.issue(p, l, r.y, at, to + y_off);
         if (has_dxo) dxo_in.issue(p, l, r.dxo, at, to + dxo_off);
-        if (has_dh) dh_in.issue(p, l, r.dh, at, to + dh_off);
+        if (kSecond) dh_in.issue(p, l, r.dh, at, to + dh_off);
         if (token) g_in.issue(p, l, r.g, at, to + g_off);
     };
     auto jump = [&](uint32_t at) {   // (after fill)
         const int ends = ends_between(p, l, at);
-        x_in.jump(r.x, ends);
+        if (kSecond) x_in.jump(r.x, ends);
         y_in.jump(r.y, ends);
         dxo_in.jump(r.dxo, ends);
-        dh_in.jump(r.dh, ends);
+        if (kSecond) dh_in.jump(r.dh, ends);
         g_in.jump(r.g, ends);
     };
     const int ahead = p.stages - 1;
@@ -87,7 +88,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
     float next_ry = 1.f, next_rx = 1.f;
     if (row < l.rows) {
         next_ry = r.stats[row];
-        next_rx = r.stats[(uint64_t)l.rows + row];
+        if (kSecond) next_rx = r.stats[(uint64_t)l.rows + row];
     }
     for (; row < l.rows; row += l.step) {
         __syncwarp();   // (the slot that is filled next has been read by all lanes)
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         const float ry = r.post ? next_ry : 1.f, rx = next_rx;
         if (row + l.step < l.rows) {
             next_ry = r.stats[row + l.step];
-            next_rx = r.stats[(uint64_t)l.rows + row + l.step];
+            if (kSecond) next_rx = r.stats[(uint64_t)l.rows + row + l.step];
         }
         uint32_t bits[C];
 #pragma unroll
@@ -112,7 +113,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         const int xw = wide_of(Ty::x, r.x), yw = wide_of(Ty::y, r.y), hw = wide_of(Ty::dh, r.dh);
         const int gw = wide_of(Ty::storage, r.g);
         const int xs = x_in.shift(p, l, r.x, row), ys = y_in.shift(p, l, r.y, row), gs = token ? g_in.shift(p, l, r.g, row) : -1;
-        const int dxos = has_dxo ? dxo_in.shift(p, l, r.dxo, row) : -1, dhs = has_dh ? dh_in.shift(p, l, r.dh, row) : -1;
+        const int dxos = has_dxo ? dxo_in.shift(p, l, r.dxo, row) : -1, dhs = kSecond ? dh_in.shift(p, l, r.dh, row) : -1;
         auto token_gate = [&](int c) {
             const Oct g = arrived<kFast>(in + g_off, gw, l, c, gs);
             return r.sigmoid ? logistic(g) : g;
@@ -124,9 +125,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         auto values = [&](int c, Oct &u, Oct &dh, Oct &e) {
             Values v;
             const Oct y = arrived<kFast>(in + y_off, yw, l, c, ys);
-            const Oct x = arrived<kFast>(in, xw, l, c, xs);
             const Oct dxo = arrived<kFast>(in + dxo_off, xw, l, c, dxos);
-            dh = arrived<kFast>(in + dh_off, hw, l, c, dhs);
             v.cg = token ? times(token_gate(c), unit)
                    : r.gate == MOSA_GATE_NONE ? all_of(unit) : vector_at<C, false, Ty>(p, l, 2, c, unit);
             v.yh = times(y, ry);
@@ -136,9 +135,15 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
                 if (!r.post) v.yh = chosen(v.yh, bits[c]);
             }
             u = times(times(v.yh, vector_at<C, false, Ty>(p, l, 0, c, unit)), v.cg);
-            v.xh = times(plus(x, u), rx);
-            e = times(dh, vector_at<C, false, Ty>(p, l, 1, c, unit));
-            v.base = fused(e, rx, dxo);
+            if (kSecond) {
+                const Oct x = arrived<kFast>(in, xw, l, c, xs);
+                dh = arrived<kFast>(in + dh_off, hw, l, c, dhs);
+                v.xh = times(plus(x, u), rx);
+                e = times(dh, vector_at<C, false, Ty>(p, l, 1, c, unit));
+                v.base = fused(e, rx, dxo);
+            } else {
+                v.base = dxo;
+            }
             return v;
         };
         // (they stay in registers from one round to the other where those suffice)
@@ -150,10 +155,12 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             Oct u, dh, e;
             const Values v = values(c, u, dh, e);
             if (kStay) stay[c] = v;
-            acc[1][c] = fused(dh, v.xh, acc[1][c]);
-            add_products(s0, e, v.xh);
             add_products(s1, u, v.base);
-            add_products(s2, u, v.xh);
+            if (kSecond) {
+                acc[1][c] = fused(dh, v.xh, acc[1][c]);
+                add_products(s0, e, v.xh);
+                add_products(s2, u, v.xh);
+            }
         }
         const float4 s = row_sums(sum_of(s0), sum_of(s1), sum_of(s2), l.red + turn * l.W, l.W, l.w, l.lane, l.group);
         turn ^= 1;
@@ -168,7 +175,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             Values v = stay[c];
             if (!kStay) v = values(c, u, dh, e);
             const Oct gamma = vector_at<C, false, Ty>(p, l, 0, c, unit);
-            const Oct t = fused(v.xh, -m1, v.base), f = times(t, v.cg);
+            const Oct t = kSecond ? fused(v.xh, -m1, v.base) : v.base, f = times(t, v.cg);
             dx_out.put_row(l, r.dx, c, t);
             if (token) {
                 acc[0][c] = fused(f, v.yh, acc[0][c]);
@@ -239,48 +246,54 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
 }
 
 // The kernel for a call's types.
-template <int C, int kMost, class Ty, bool kCut>
+template <int C, int kMost, class Ty, bool kCut, bool kSecond>
 cudaError_t go(const Args &p, int blocks, int bytes, cudaStream_t s) {
-    const auto kernel = residual_bwd_kernel<C, kMost, Ty, kCut>;
+    const auto kernel = residual_bwd_kernel<C, kMost, Ty, kCut, kSecond>;
     cudaError_t e = allow_smem((const void *)kernel, kSmem);
     if (e != cudaSuccess) return e;
     note_launches(1);
     return launch_pdl(kernel, dim3(blocks), dim3(p.warps * p.groups * 32), bytes, s, p);
 }
-template <int C, int kMost, bool kCut>
+template <int C, int kMost, bool kCut, bool kSecond>
 cudaError_t go_by_types(const Args &p, int blocks, int bytes, cudaStream_t s) {
     const Residual &r = p.r;
     const int x = r.x.wide, y = r.y.wide, dh = r.dh.wide, st = r.storage_wide;
     if constexpr (C == 4)
-        if (!p.held) return go<C, kMost, Types<1, 1, 1, 1, 0>, kCut>(p, blocks, bytes, s);
-    if (st) return go<C, kMost, Types<1, 1, 1, 1>, kCut>(p, blocks, bytes, s);
-    switch (4 * x + 2 * y + dh) {
-        case 0: return go<C, kMost, Types<0, 0, 0, 0>, kCut>(p, blocks, bytes, s);
-        case 1: return go<C, kMost, Types<0, 0, 1, 0>, kCut>(p, blocks, bytes, s);
-        case 2: return go<C, kMost, Types<0, 1, 0, 0>, kCut>(p, blocks, bytes, s);
-        case 3: return go<C, kMost, Types<0, 1, 1, 0>, kCut>(p, blocks, bytes, s);
-        case 4: return go<C, kMost, Types<1, 0, 0, 0>, kCut>(p, blocks, bytes, s);
-        case 5: return go<C, kMost, Types<1, 0, 1, 0>, kCut>(p, blocks, bytes, s);
-        case 6: return go<C, kMost, Types<1, 1, 0, 0>, kCut>(p, blocks, bytes, s);
-        default: return go<C, kMost, Types<1, 1, 1, 0>, kCut>(p, blocks, bytes, s);
+        if (!p.held) return go<C, kMost, Types<1, 1, 1, 1, 0>, kCut, kSecond>(p, blocks, bytes, s);
+    if (st) return go<C, kMost, Types<1, 1, 1, 1>, kCut, kSecond>(p, blocks, bytes, s);
+    if constexpr (kSecond)   // (else dh counts as of the storage type)
+        if (dh) switch (2 * x + y) {
+            case 0: return go<C, kMost, Types<0, 0, 1, 0>, kCut, true>(p, blocks, bytes, s);
+            case 1: return go<C, kMost, Types<0, 1, 1, 0>, kCut, true>(p, blocks, bytes, s);
+            case 2: return go<C, kMost, Types<1, 0, 1, 0>, kCut, true>(p, blocks, bytes, s);
+            default: return go<C, kMost, Types<1, 1, 1, 0>, kCut, true>(p, blocks, bytes, s);
+        }
+    switch (2 * x + y) {
+        case 0: return go<C, kMost, Types<0, 0, 0, 0>, kCut, kSecond>(p, blocks, bytes, s);
+        case 1: return go<C, kMost, Types<0, 1, 0, 0>, kCut, kSecond>(p, blocks, bytes, s);
+        case 2: return go<C, kMost, Types<1, 0, 0, 0>, kCut, kSecond>(p, blocks, bytes, s);
+        default: return go<C, kMost, Types<1, 1, 0, 0>, kCut, kSecond>(p, blocks, bytes, s);
     }
 }
 
-// Sequences that lie apart, `times` eights of columns a thread; blocks of 8 warps with two and with four (files of
-// their own for the compiler's time).
+// Sequences that lie apart, `times` eights of columns a thread; blocks of 8 warps with two and with four; calls without dh
+// (files of their own for the compiler's time).
 cudaError_t residual_bwd_cut(const Args &p, int times, int blocks, int bytes, cudaStream_t s);
 cudaError_t residual_bwd_16_cut(const Args &p, int blocks, int bytes, cudaStream_t s);
 cudaError_t residual_bwd_16(const Args &p, int blocks, int bytes, cudaStream_t s);
 cudaError_t residual_bwd_32(const Args &p, int blocks, int bytes, cudaStream_t s);
+cudaError_t residual_bwd_alone(const Args &p, int times, int blocks, int bytes, cudaStream_t s);
+cudaError_t residual_bwd_alone_cut(const Args &p, int times, int blocks, int bytes, cudaStream_t s);
 
 // The kernel for a call: of its types, where its places, strides and types have one.
-template <int C, int kMost>
+template <int C, int kMost, bool kSecond>
 cudaError_t go_by_places(const Args &p, int blocks, int bytes, cudaStream_t s) {
     const Residual &r = p.r;
     const int st = r.storage_wide;
     if (!fast(p) || (st && !(r.x.wide && r.y.wide && r.dh.wide)) || (!p.held && !(C == 4 && st)))
-        return go<C, kMost, Types<-1, -1, -1, -1>, false>(p, blocks, bytes, s);
-    return p.flat ? go_by_types<C, kMost, false>(p, blocks, bytes, s) : residual_bwd_cut(p, C, blocks, bytes, s);
+        return go<C, kMost, Types<-1, -1, -1, -1>, false, kSecond>(p, blocks, bytes, s);
+    if (p.flat) return go_by_types<C, kMost, false, kSecond>(p, blocks, bytes, s);
+    return kSecond ? residual_bwd_cut(p, C, blocks, bytes, s) : residual_bwd_alone_cut(p, C, blocks, bytes, s);
 }
 
 }  // namespace blk

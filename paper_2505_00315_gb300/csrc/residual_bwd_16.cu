@@ -5,7 +5,7 @@ namespace mosa {
 namespace blk {
 
 cudaError_t residual_bwd_16(const Args &p, int blocks, int bytes, cudaStream_t s) {
-    return go_by_places<2, kWarps / 2>(p, blocks, bytes, s);
+    return go_by_places<2, kWarps / 2, true>(p, blocks, bytes, s);
 }
 
 }  // namespace blk

@@ -1,0 +1,41 @@
+"""The block operators where inputs, gradients or places are not the usual ones, against their definitions in 64 bits."""
+import pytest
+import torch
+
+import paper_2505_00315_gb300 as mosa
+from test_gpu_block import BF, F32, INF, NAN, inputs
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------ residual step
+
+# Kernels of 8, 16 and 32 columns a thread, in both types, and those of rows that are not whole pieces.
+WIDTHS = [(BF, BF, 30, 320), (BF, F32, 30, 1500), (F32, F32, 30, 768), (BF, F32, 4000, 1024), (F32, F32, 30, 6000),
+          (F32, F32, 30, 8192), (BF, BF, 30, 1001)]
+
+
+@pytest.mark.parametrize("dt,xt,T,d", WIDTHS)
+@pytest.mark.parametrize("pre", [True, False])
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("gate", ["none", "token"])
+def test_without_a_gradient_of_h_dx_is_dx_out_whatever_the_inputs_hold(dt, xt, T, d, pre, post, gate):
+    s, dx_out, _ = inputs(2, T, d, dt, xt=xt, gate=gate, seed=31)
+    kw = dict(post_norm=post, pre_norm=pre, scale=0.5)
+
+    def backward(v):
+        stats = mosa.mosa_residual_forward(**v, **kw)[2]
+        return mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=None, **v, **kw)[0]
+
+    clean = backward(s)
+    y, x = s["y"].clone(), s["x"].clone()
+    y[0, 3], y[1, 4, 5], y[1, 29, d - 1] = NAN, INF, -INF
+    x[0, 7], x[1, 9, 2] = NAN, INF
+    got = backward({**s, "x": x, "y": y, "gamma_pre": torch.full_like(s["gamma_pre"], NAN)})
+    assert torch.equal(got["dx"], dx_out) and torch.equal(clean["dx"], dx_out)
+    others = torch.ones(2, T, dtype=torch.bool, device="cuda")
+    others[0, 3] = others[1, 4] = others[1, 29] = False
+    for n in ("dy", "dgate"):
+        assert n not in got or torch.equal(got[n][others], clean[n][others]), n
+    if pre:
+        assert not got["dgamma_pre"].any()
