@@ -191,7 +191,10 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             } else {
                 acc[0][c] = fused(drops ? chosen(t, bits[c]) : t, v.yh, acc[0][c]);
             }
-            dy_out.put_row(l, r.dy, c, times(fused(v.yh, -m2, times(f, gamma)), ry));
+            // (without a norm of y dy does not see it, and an infinity may not meet m2 = 0; with the second norm its
+            // row is lost anyhow)
+            const Oct w = times(f, gamma);
+            dy_out.put_row(l, r.dy, c, kSecond || r.post ? times(fused(v.yh, -m2, w), ry) : w);
         }
         dx_out.end(l, r.dx);
         dy_out.end(l, r.dy);

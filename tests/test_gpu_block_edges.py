@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2505_00315_gb300 as mosa
+from _block_ref import near
 from test_gpu_block import BF, F32, INF, NAN, inputs
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,24 @@ def test_without_a_gradient_of_h_dx_is_dx_out_whatever_the_inputs_hold(dt, xt, T
         assert n not in got or torch.equal(got[n][others], clean[n][others]), n
     if pre:
         assert not got["dgamma_pre"].any()
+
+
+@pytest.mark.parametrize("dt,xt,T,d", WIDTHS)
+@pytest.mark.parametrize("gate", ["none", "channel", "token"])
+def test_without_a_norm_dy_does_not_see_y(dt, xt, T, d, gate):
+    """dy = scale g dx_out, also where y is infinite or no number."""
+    s, dx_out, _ = inputs(2, T, d, dt, xt=xt, gate=gate, seed=32)
+    kw = dict(post_norm=False, pre_norm=False, scale=0.5)
+
+    def backward(v):
+        stats = mosa.mosa_residual_forward(**v, **kw)[2]
+        return mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=None, **v, **kw)[0]
+
+    clean = backward(s)
+    y = s["y"].clone()
+    y[0, 3], y[1, 4, 5], y[1, 29, d - 1] = NAN, INF, -INF
+    got = backward({**s, "y": y})
+    assert torch.equal(got["dy"], clean["dy"])
+    g = 1.0 if gate == "none" else s["gate"].double()
+    want = 0.5 * g * dx_out.double()
+    near("dy", got["dy"], want, 2.0 ** -22 * want.abs())   # three products
