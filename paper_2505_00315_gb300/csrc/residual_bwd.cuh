@@ -131,8 +131,8 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             v.yh = times(y, ry);
             if (drops) {
                 v.cg = chosen(v.cg, bits[c]);
-                // (with a norm, what is not finite is so in its whole row)
-                if (!r.post) v.yh = chosen(v.yh, bits[c]);
+                // (with a norm, a NaN is one in its whole row; an infinity makes r_y 0, and counts only where it is kept)
+                if (!r.post || ry == 0.f) v.yh = chosen(v.yh, bits[c]);
             }
             u = times(times(v.yh, vector_at<C, false, Ty>(p, l, 0, c, unit)), v.cg);
             if (kSecond) {

@@ -3,8 +3,8 @@ import pytest
 import torch
 
 import paper_2505_00315_gb300 as mosa
-from _block_ref import near
-from test_gpu_block import BF, F32, INF, NAN, inputs
+from _block_ref import keep_mask, near, residual
+from test_gpu_block import BF, F32, INF, NAN, inputs, state
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,28 @@ def test_without_a_norm_dy_does_not_see_y(dt, xt, T, d, gate):
     g = 1.0 if gate == "none" else s["gate"].double()
     want = 0.5 * g * dx_out.double()
     near("dy", got["dy"], want, 2.0 ** -22 * want.abs())   # three products
+
+
+@pytest.mark.parametrize("dt,xt,T,d", WIDTHS)
+@pytest.mark.parametrize("gate", ["none", "channel", "token"])
+def test_a_dropped_infinity_of_a_normed_row_does_not_count(dt, xt, T, d, gate):
+    """1 / sqrt(mean(y^2)) is 0 there, and the row that of a block that gave zeros, but for dy, which is 0 with r_y."""
+    p, rng = 0.5, state(9)
+    s, dx_out, dh = inputs(2, T, d, dt, xt=xt, gate=gate, seed=33)
+    keep = keep_mask(rng, 0, s["x"].shape, p, "cuda")
+    y, zero = s["y"].clone(), s["y"].clone()
+    rows = ((0, 3), (1, 4), (1, 29))
+    for i, (b, t) in enumerate(rows):
+        gone = (~keep[b, t]).nonzero()[:, 0]
+        y[b, t, gone[:1 + 3 * i]] = -INF if i == 1 else INF
+        zero[b, t] = 0
+    y[1, 29, (~keep[1, 29]).nonzero()[-1, 0]] = -INF
+    s["y"] = y
+    kw = dict(dropout=p, rng=rng, scale=0.5)
+    x, h, stats = mosa.mosa_residual_forward(**s, **kw)
+    g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, **s, **kw)
+    want = residual(**{**s, "y": zero}, dx_out=dx_out, dh=dh, backward=True, **kw)
+    for b, t in rows:
+        want["dy"][0][b, t] = want["dy"][1][b, t] = 0
+    for n, t in {"x": x, "h": h, **g}.items():
+        near(n, t, *want[n])
