@@ -681,7 +681,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) logprob_bwd_kernel(const __gri
         if (zero || !(here || __any_sync(0xffffffffu, mine))) continue;
         __syncwarp();
         auto place = [&](int col, float v, float g) {
-            const float x = v <= kLeast ? 0.f : fmaf(l.scale, g, weight(v));
+            const float x = v <= kLeast && ref == ref ? 0.f : fmaf(l.scale, g, weight(v));   // (a row with a NaN is one)
             if (kWide) reinterpret_cast<float *>(out)[col] = x;
             else reinterpret_cast<bf16 *>(out)[col] = from_f32<bf16>(x);
         };

@@ -4,7 +4,7 @@ import torch
 
 import paper_2505_00315_gb300 as mosa
 from _block_ref import keep_mask, near, residual
-from test_gpu_block import BF, F32, INF, NAN, inputs, state
+from test_gpu_block import BF, F32, INF, NAN, check_logprobs, inputs, logits_of, state
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,24 @@ def test_a_dropped_infinity_of_a_normed_row_does_not_count(dt, xt, T, d, gate):
         want["dy"][0][b, t] = want["dy"][1][b, t] = 0
     for n, t in {"x": x, "h": h, **g}.items():
         near(n, t, *want[n])
+
+
+# -------------------------------------------------------- log probabilities
+
+@pytest.mark.parametrize("V", [40, 3001, 40000])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_rows_that_are_no_numbers_are_so_where_entries_are_ruled_out(V, dt):
+    """A NaN or an entry above 2^90 beside ruled-out ones, which are targets and alternatives."""
+    z = logits_of(1, 6, V, dt, seed=34)
+    z[0, :, V // 2:] = -INF
+    z[0, 0], z[0, 0, 1] = -INF, NAN
+    z[0, 1, 3] = INF
+    z[0, 2], z[0, 2, V - 1] = torch.finfo(dt).min, 1e30
+    z[0, 3, 0] = NAN
+    t = torch.tensor([[V - 1, V - 1, 0, V // 2, V - 1, 2]], device="cuda")
+    r = check_logprobs(z, t, 5)
+    assert torch.isnan(r["dlogits"][0, :4]).all() and torch.isfinite(r["dlogits"][0, 4:]).all()
+    idx = torch.tensor([[[V - 1, 7, V - 2]]], dtype=torch.int32, device="cuda").expand(1, 6, 3).contiguous()
+    up = torch.ones(1, 6, 3, device="cuda")
+    dz = mosa.mosa_token_logprobs_backward(z, t, r["lse"], top=idx, dtop_logp=up)
+    assert torch.isnan(dz[0, :4]).all() and torch.isfinite(dz[0, 4:]).all()
