@@ -114,9 +114,9 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
         const int gw = wide_of(Ty::storage, r.g);
         const int xs = x_in.shift(p, l, r.x, row), ys = y_in.shift(p, l, r.y, row), gs = token ? g_in.shift(p, l, r.g, row) : -1;
         const int dxos = has_dxo ? dxo_in.shift(p, l, r.dxo, row) : -1, dhs = kSecond ? dh_in.shift(p, l, r.dh, row) : -1;
-        auto token_gate = [&](int c) {
+        auto token_gate = [&](int c, bool slope) {
             const Oct g = arrived<kFast>(in + g_off, gw, l, c, gs);
-            return r.sigmoid ? logistic(g) : g;
+            return !r.sigmoid ? g : slope ? logistic_slope(g) : logistic(g);
         };
         // What both rounds need, from what the ring holds.
         struct Values {
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             Values v;
             const Oct y = arrived<kFast>(in + y_off, yw, l, c, ys);
             const Oct dxo = arrived<kFast>(in + dxo_off, xw, l, c, dxos);
-            v.cg = token ? times(token_gate(c), unit)
+            v.cg = token ? times(token_gate(c, false), unit)
                    : r.gate == MOSA_GATE_NONE ? all_of(unit) : vector_at<C, false, Ty>(p, l, 2, c, unit);
             v.yh = times(y, ry);
             if (drops) {
@@ -181,10 +181,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
                 acc[0][c] = fused(f, v.yh, acc[0][c]);
                 if (r.dg.p != nullptr) {
                     Oct g = times(times(t, unit), times(v.yh, gamma));
-                    if (r.sigmoid) {
-                        const Oct k = token_gate(c);
-                        g = times(g, fused(times(k, -1.f), k, k));
-                    }
+                    if (r.sigmoid) g = times(g, token_gate(c, true));
                     if (drops) g = chosen(g, bits[c]);
                     dg_out.put_row(l, r.dg, c, g);
                 }
@@ -220,10 +217,7 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
                 of[0] = times(own, vector_of<false>(r, 2, l.column(c), unit));
                 if (r.gate == MOSA_GATE_CHANNEL) {
                     of[2] = times(times(own, unit), vector_of<false>(r, 0, l.column(c), unit));
-                    if (r.sigmoid) {
-                        const Oct k = logistic(vector8(r.gch, l.column(c), l.d));
-                        of[2] = times(of[2], fused(times(k, -1.f), k, k));
-                    }
+                    if (r.sigmoid) of[2] = times(of[2], logistic_slope(vector8(r.gch, l.column(c), l.d)));
                 }
             }
 #pragma unroll

@@ -4,7 +4,7 @@ import torch
 
 import paper_2505_00315_gb300 as mosa
 from _block_ref import keep_mask, near, residual
-from test_gpu_block import BF, F32, INF, NAN, check_logprobs, inputs, logits_of, state
+from test_gpu_block import BF, F32, INF, NAN, check_logprobs, gen, inputs, logits_of, state
 
 pytestmark = pytest.mark.gpu
 
@@ -84,6 +84,28 @@ def test_a_dropped_infinity_of_a_normed_row_does_not_count(dt, xt, T, d, gate):
     want = residual(**{**s, "y": zero}, dx_out=dx_out, dh=dh, backward=True, **kw)
     for b, t in rows:
         want["dy"][0][b, t] = want["dy"][1][b, t] = 0
+    for n, t in {"x": x, "h": h, **g}.items():
+        near(n, t, *want[n])
+
+
+@pytest.mark.parametrize("dt,xt,T,d", WIDTHS)
+@pytest.mark.parametrize("gate", ["channel", "token"])
+def test_gradient_of_a_saturated_gate(dt, xt, T, d, gate):
+    """Through a sigmoid s of gates far from 0, where 1 - s is not what fp32 keeps of s.  The gradient is that of the
+    gate s itself times s (1 - s), and its bound that one's, with u = 2^-24: s (1 - s) = e r^2 of e = e^-|x| (off by 1.3 u |x|
+    from the exponent, 4 u from the power), 1 + e (u), r (2 u) twice and two products is off by (4 + 2 (1 + 2) + 2 + 1.3 |x|) u
+    = (12 + 1.3 |x|) u relative, a share of (12 + 1.3 |x|) / 256 of the bound's 2^-16."""
+    s, dx_out, dh = inputs(2, T, d, dt, xt=xt, gate=gate, seed=35)
+    some = torch.tensor([0.0, 1.0, -1.0, 8.0, -8.0, 12.0, -12.0, 16.0, -16.0, 30.0, -30.0, -60.0], device="cuda")
+    s["gate"] = some[torch.randint(0, 12, s["gate"].shape, generator=gen(36), device="cuda")].to(dt)
+    kw = dict(scale=0.5, dropout=0.1, rng=state())
+    x, h, stats = mosa.mosa_residual_forward(**s, sigmoid=True, **kw)
+    g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, **s, sigmoid=True, **kw)
+    z = s["gate"].double()
+    want = residual(**{**s, "gate": torch.sigmoid(z)}, dx_out=dx_out, dh=dh, backward=True, **kw)
+    slope = torch.sigmoid(z) * torch.sigmoid(-z)
+    ref, bound = want["dgate"]
+    want["dgate"] = ref * slope, bound * slope * (1 + (12 + 1.3 * z.abs()) / 256)
     for n, t in {"x": x, "h": h, **g}.items():
         near(n, t, *want[n])
 
