@@ -103,16 +103,16 @@ class TokenLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, targets):
-        r, _ = mosa.mosa_token_logprobs(logits, targets)
+        r, _ = mosa.mosa_token_logprobs(logits, targets, stats=True)
         n = (targets >= 0).sum().clamp(min=1)
-        ctx.save_for_backward(logits, targets, r["lse"], n)
+        ctx.save_for_backward(logits, targets, r["stats"], n)
         return -r["logp"].sum() / n
 
     @staticmethod
     def backward(ctx, g):
-        logits, targets, lse, n = ctx.saved_tensors
+        logits, targets, stats, n = ctx.saved_tensors
         dlogp = (-g / n).expand(targets.shape).contiguous()
-        return mosa.mosa_token_logprobs_backward(logits, targets, lse, dlogp=dlogp), None
+        return mosa.mosa_token_logprobs_backward(logits, targets, stats, dlogp=dlogp), None
 
 
 class Layer(torch.nn.Module):

@@ -529,6 +529,7 @@ typedef struct {
     int32_t target64;    /* targets are int32 (0) or int64 (1) */
     int32_t top;
     float scale;
+    int32_t stats;       /* lse is [B,T] (0), or [3,B,T] (1): lse, the row's largest entry m, sum_j exp(scale (z_j - m)) */
     mosa_strides z, dz;  /* logits; their gradient (backward only) */
 } mosa_logprob_shape;
 
@@ -537,7 +538,7 @@ typedef struct {
 size_t mosa_token_logprobs_workspace_bytes(const mosa_logprob_shape *shape);
 
 /* Forward.  targets [B,T] (NULL: none); logp, entropy, lse [B,T] fp32, each may be NULL (logp is
- * where targets is); top_index [B,T,top] int32 and top_logp [B,T,top] fp32 (NULL where top = 0). */
+ * where targets is; lse [3,B,T] with stats = 1); top_index [B,T,top] int32 and top_logp [B,T,top] fp32 (NULL where top = 0). */
 mosa_status mosa_token_logprobs(const mosa_logprob_shape *shape, const void *logits,
                                 const void *targets, float *logp, float *entropy, float *lse,
                                 int32_t *top_index, float *top_logp, void *workspace,
@@ -549,6 +550,9 @@ mosa_status mosa_token_logprobs(const mosa_logprob_shape *shape, const void *log
  * NULL).  With G = dlogp + sum dtop_logp
  *     dz_j = scale (dlogp [j = t] + sum_i dtop_logp_i [j = top_i] - G p_j + dlse p_j
  *                   - dentropy p_j (log p_j + entropy)).
+ * lse alone is one fp32 number, whose rounding makes the row's p_j off by |lse| 2^-24 relative; with stats = 1
+ * (lse as the forward left it then, [3,B,T]) p_j comes from m and the sum, and its error does not grow with
+ * the logits' size.
  * A row whose gradients are all 0 gets zeros.  top_index must hold what the forward returned (an index
  * outside 0 .. V-1 is skipped). */
 mosa_status mosa_token_logprobs_backward(const mosa_logprob_shape *shape, const void *logits,

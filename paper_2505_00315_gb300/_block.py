@@ -30,7 +30,7 @@ class MosaDropoutShape(ctypes.Structure):
 class MosaLogprobShape(ctypes.Structure):
     """mosa_logprob_shape: sizes and strides of mosa_token_logprobs and its backward."""
     _fields_ = ([(n, _i32) for n in ("B", "T", "V", "dtype", "target64", "top")]
-                + [("scale", _f32), ("z", MosaStrides), ("dz", MosaStrides)])
+                + [("scale", _f32), ("stats", _i32), ("z", MosaStrides), ("dz", MosaStrides)])
 
 
 def declare(L) -> None:
@@ -357,8 +357,9 @@ def mosa_dropout(x, p: float, rng, site: int = 0, out=None, stream=None):
 
 # -------------------------------------------------------- log probabilities
 
-def _logprob_plan(logits, targets, top, scale, results, back=None):
-    """results: (name, tensor, columns or 0, type) of [B,T] or [B,T,columns] tensors to be checked."""
+def _logprob_plan(logits, targets, top, scale, results, stats=None, keeps=False, back=None):
+    """results: (name, tensor, columns or 0, type) of [B,T] or [B,T,columns] tensors to be checked; stats [3,B,T],
+    which the call ``keeps`` or reads."""
     torch = _b._torch_mod
     _rank(logits, "logits", 3)
     B, T, V = logits.shape
@@ -370,28 +371,30 @@ def _logprob_plan(logits, targets, top, scale, results, back=None):
             raise ValueError("targets must be contiguous")
     for name, t, n, dtype in results:
         _vector(t, name, (B, T, n) if n else (B, T), dtype)
+    _vector(stats, "stats", (3, B, T), torch.float32)
     s = MosaLogprobShape(B, T, V, _b._dtype_code(logits),
                          1 if targets is not None and targets.dtype == torch.int64 else 0,
-                         _int(top, "top"), scale, _rows(logits, "logits"))
+                         _int(top, "top"), scale, 1 if keeps else 0, _rows(logits, "logits"))
     if back is not None:
         s.dz = _result(back[0], "dlogits", logits.shape, logits.dtype)
         return ctypes.byref(s), 0, s
     return (ctypes.byref(s), int(_b.load().mosa_token_logprobs_workspace_bytes(ctypes.byref(s))), s,
-            (logits.device, (B, T), (B, T, top)))
+            (logits.device, (B, T), (B, T, top), (3, B, T)))
 
 
 def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, workspace=None, out=None,
-                        stream=None):
+                        stream=None, stats: bool = False):
     """Log probabilities under softmax(scale * logits), logits [B,T,V] (scale: 1 / temperature).  Returns
     ({"logp", "entropy", "lse", "top", "top_logp"}, workspace): logp [B,T] of the targets [B,T] (int32 or int64;
     below 0: none, logp 0), entropy and lse [B,T], and with ``top`` > 0 (up to 32) the indices [B,T,top] int32
     of the largest entries in falling order, ties by the lower index, and their log probabilities;
-    all fp32 but the indices.  Entries of -inf (or -2^90 and less) are ruled out.  ``out`` may hold any of
-    them."""
+    all fp32 but the indices.  Entries of -inf (or -2^90 and less) are ruled out.  With ``stats``, also "stats" [3,B,T]
+    for the backward: lse (r["lse"] is that plane), the largest entry and the sum of powers relative to it, whose gradient does
+    not lose digits where logits are large.  ``out`` may hold any of them."""
     try:
         dev = logits.get_device()
         if stream is not None or (dev >= 0 and dev != _b._torch()._C._cuda_getDevice()):
-            return _there(logits, stream, mosa_token_logprobs, logits, targets, top, scale, workspace, out)
+            return _there(logits, stream, mosa_token_logprobs, logits, targets, top, scale, workspace, out, None, stats)
         torch = _b._torch()
         f32 = torch.float32
         logp, ent, lse, idx, tlp = ((out.get("logp"), out.get("entropy"), out.get("lse"), out.get("top"),
@@ -400,26 +403,35 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
             top, scale = _int(top, "top"), _float(scale)
         if top == 0:
             idx = tlp = None
+        sums = None
+        if stats:
+            stats = True
+            sums = out.get("stats") if out else None
+            if lse is not None and (sums is None or lse.data_ptr() != sums.data_ptr()):
+                raise ValueError("with stats, lse is the first of its planes: out may hold stats alone")
         key = (9, logits.shape, logits.stride(), logits.dtype,
                None if targets is None else (targets.shape, targets.stride(), targets.dtype), top, scale, dev,
-               (_sig(logp), _sig(ent), _sig(lse), _sig(idx), _sig(tlp)) if out else None)
+               (_sig(logp), _sig(ent), _sig(lse), _sig(idx), _sig(tlp), _sig(sums)) if out else None, True if stats else False)
     except AttributeError:
         _bad(("logits", logits), ("targets", targets))
     plan = _plans.get(key) or _keep(key, _logprob_plan(
         logits, targets, top, scale, [("logp", logp, 0, f32), ("entropy", ent, 0, f32), ("lse", lse, 0, f32),
-                                      ("top", idx, top, torch.int32), ("top_logp", tlp, top, f32)]))
+                                      ("top", idx, top, torch.int32), ("top_logp", tlp, top, f32)], sums, stats))
     if not (dev >= 0 and (targets is None or targets.get_device() == dev)
             and (workspace is None or workspace.get_device() == dev)
-            and (out is None or _all_on(dev, logp, ent, lse, idx, tlp))):
+            and (out is None or _all_on(dev, logp, ent, lse, idx, tlp, sums))):
         _elsewhere(dev, ("logits", logits), ("targets", targets), ("workspace", workspace), ("logp", logp),
-                   ("entropy", ent), ("lse", lse), ("top", idx), ("top_logp", tlp))
-    device, lead, tops = plan[3]
+                   ("entropy", ent), ("lse", lse), ("top", idx), ("top_logp", tlp), ("stats", sums))
+    device, lead, tops, planes = plan[3]
     r = {}
     if targets is None:
         logp = None
     else:
         r["logp"] = logp = torch.empty(lead, dtype=f32, device=device) if logp is None else logp
     r["entropy"] = ent = torch.empty(lead, dtype=f32, device=device) if ent is None else ent
+    if stats:
+        r["stats"] = sums = torch.empty(planes, dtype=f32, device=device) if sums is None else sums
+        lse = sums[0] if lse is None else lse
     r["lse"] = lse = torch.empty(lead, dtype=f32, device=device) if lse is None else lse
     if top > 0:
         r["top"] = idx = torch.empty(tops, dtype=torch.int32, device=device) if idx is None else idx
@@ -436,10 +448,11 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
 
 def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None, dentropy=None, dlse=None, top=None,
                                  dtop_logp=None, scale: float = 1.0, out=None, stream=None):
-    """Gradient of the logits (like them) from mosa_token_logprobs' lse and entropy and the gradients dlogp,
-    dentropy, dlse [B,T] and dtop_logp [B,T,top] fp32 of its results, each None where there is none; ``top``:
-    the indices that it returned, read with dtop_logp.  ``out`` may hold "dlogits", logits itself among
-    them."""
+    """Gradient of the logits (like them) from mosa_token_logprobs' lse [B,T] or stats [3,B,T] and entropy and the gradients
+    dlogp, dentropy, dlse [B,T] and dtop_logp [B,T,top] fp32 of its results, each None where there is none; ``top``:
+    the indices that it returned, read with dtop_logp.  From lse alone the row's probabilities are off by |lse| 2^-24
+    relative (its rounding), from stats by an amount that does not grow with the logits.  ``out`` may hold "dlogits", logits
+    itself among them."""
     dz = None
     try:
         dev = logits.get_device()
@@ -472,10 +485,13 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
             raise TypeError("dlogp needs targets")
         if dentropy is not None and entropy is None:
             raise TypeError("dentropy needs entropy, the forward's")
+        kept = len(lse.shape) == 3
         plan = _keep(key, _logprob_plan(
             logits, targets, n, scale,
-            [("lse", lse, 0, f32), ("entropy", entropy, 0, f32), ("dlogp", dlogp, 0, f32), ("dentropy", dentropy, 0, f32),
-             ("dlse", dlse, 0, f32), ("top", top, n, torch.int32), ("dtop_logp", dtop_logp, n, f32)], (dz,)))
+            [("lse", None if kept else lse, 0, f32), ("entropy", entropy, 0, f32), ("dlogp", dlogp, 0, f32),
+             ("dentropy", dentropy, 0, f32), ("dlse", dlse, 0, f32), ("top", top, n, torch.int32),
+             ("dtop_logp", dtop_logp, n, f32)],
+            lse if kept else None, kept, (dz,)))
     if not (dev >= 0 and lse.get_device() == dev
             and _all_on(dev, targets, entropy, dlogp, dentropy, dlse, top, dtop_logp, dz)):
         _elsewhere(dev, ("logits", logits), ("targets", targets), ("lse", lse), ("entropy", entropy), ("dlogp", dlogp),

@@ -61,11 +61,12 @@ cudaError_t launch_dropout(int B, int T, int d, const Rows &x, const Rows &y, co
 
 struct LogProb {
     int B, T, V;
-    int target64, top;
+    int target64, top, stats;
     float scale;
     Rows z, dz;
     const void *targets;
-    float *logp, *entropy, *lse;             // forward's outputs; backward: entropy and lse are read
+    float *logp, *entropy, *lse;             // forward's outputs; backward: entropy and lse are read.  stats: lse is [3][rows],
+                                             // with the largest entry and the sum of powers relative to it
     int32_t *top_index;
     float *top_logp;
     const float *dlogp, *dentropy, *dlse, *dtop;   // backward

@@ -95,7 +95,7 @@ mosa_status check_logprob(const mosa_logprob_shape *s, bool backward, LogProb *l
     if (s == nullptr) return MOSA_ERR_INVALID_ARG;
     mosa_status st = check_rows(s->B, s->T, s->V);
     if (st != MOSA_OK) return st;
-    if (!dtype_ok(s->dtype) || !flag_ok(s->target64)) return MOSA_ERR_INVALID_ARG;
+    if (!dtype_ok(s->dtype) || !flag_ok(s->target64) || !flag_ok(s->stats)) return MOSA_ERR_INVALID_ARG;
     if (s->top < 0 || s->top > s->V) return MOSA_ERR_INVALID_ARG;
     if (!(s->scale > 0.f) || std::isinf(s->scale)) return MOSA_ERR_INVALID_ARG;
     if (s->top > 32 || s->scale < 1.f / 1048576 || s->scale > 1048576.f) return MOSA_ERR_UNSUPPORTED;
@@ -107,6 +107,7 @@ mosa_status check_logprob(const mosa_logprob_shape *s, bool backward, LogProb *l
     l->target64 = s->target64;
     l->z.wide = l->dz.wide = s->dtype == MOSA_F32;
     l->top = s->top;
+    l->stats = s->stats;
     l->scale = s->scale;
     const mosa_strides a = {s->z.b, s->z.t, 0}, b = {s->dz.b, s->dz.t, 0};
     if (!strides(a, s->B, s->T, 1, z)) return MOSA_ERR_INVALID_ARG;

@@ -8,6 +8,8 @@
 //               A = scale (dlse - G - dentropy entropy), B = -scale ln 2 dentropy; then the few places
 //               with a gradient of their own (the target and the alternatives) once more.  (scale z
 //               is rounded as in lse, so that b of a row's only large entry is 0 however large it is.)
+//               Where the caller keeps m and s, b = c (z - m), with 1/s and ln s in A and B: p's error does not
+//               grow with |lse| then, as it does through lse, one rounded number (|lse| 2^-24).
 // A warp takes a row, or 2, 4 or 8 of a block share one where rows are fewer, or some blocks, whose
 // results a second kernel joins.  Rows move in 16-byte pieces wherever they start: a row is cut at the
 // addresses' multiples of 16, its first and last pieces are read value by value.
@@ -428,7 +430,14 @@ __device__ __forceinline__ void finish(const Args &p, long long row, const Part 
     const float lg = logf(a.s), inf = __int_as_float(0x7F800000), nan = __int_as_float(0x7FC00000);
     const float lse = bad ? nan : none && a.s == a.s ? -inf : __fadd_rn(__fmul_rn(a.m, l.scale), lg);
     if (lane == 0) {
-        if (l.lse != nullptr) l.lse[row] = lse;
+        if (l.lse != nullptr) {
+            l.lse[row] = lse;
+            if (l.stats) {
+                const long long rows = (long long)l.B * l.T;
+                l.lse[rows + row] = a.m;
+                l.lse[2 * rows + row] = a.s;
+            }
+        }
         if (l.entropy != nullptr)
             l.entropy[row] = bad ? nan : none && a.s == a.s ? 0.f : fmaf(-kLn2, a.t / a.s, lg);
         if (l.logp != nullptr)
@@ -570,8 +579,8 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// A warp takes one of the `units` shares of a row.
-template <bool kWide>
+// A warp takes one of the `units` shares of a row.  kStats: the caller has kept m and s.
+template <bool kWide, bool kStats>
 __global__ void __launch_bounds__(kFewWarps * 32) logprob_bwd_kernel(const __grid_constant__ Args p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int E = kWide ? 4 : 8;
@@ -616,7 +625,15 @@ __global__ void __launch_bounds__(kFewWarps * 32) logprob_bwd_kernel(const __gri
         if (dH != 0.f) A -= l.scale * (dH * l.entropy[row]);
         float B = -l.scale * kLn2 * dH;
         if (zero) A = B = 0.f;
-        const float ref = zero ? 0.f : lse;
+        float ref = zero ? 0.f : lse, off = ref;   // scale z where weights are near 1; what is taken off (stats: of z, else of scale z)
+        if (kStats && !zero) {
+            const long long rows = (long long)l.B * l.T;
+            const float s = l.lse[2 * rows + row], by = 1.f / s;
+            off = l.lse[rows + row];
+            ref = off * l.scale;
+            A = lse == lse ? fmaf(l.scale * dH, logf(s), A) * by : lse;   // (a row that is no number stays so)
+            B *= by;
+        }
         // Values that are clamped to this have weight 0, and no infinity meets it.  (Far enough below a large lse that
         // no rounding brings it back there.)
         const float least = fmaxf((ref - 208.f - fabsf(ref) * 0x1p-6f) / l.scale, kLeast);
@@ -630,11 +647,11 @@ __global__ void __launch_bounds__(kFewWarps * 32) logprob_bwd_kernel(const __gri
 
         auto weight = [&](float v) {   // 2^b and its gradient without the place's own
             v = max_nan(v, leastw);
-            const float b = __fsub_rn(__fmul_rn(v, l.scale), ref) * kLog2e;
+            const float b = kStats ? (v - off) * p.c : __fsub_rn(__fmul_rn(v, l.scale), off) * kLog2e;
             return pow2(b) * fmaf(B, b, A);
         };
         const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(z.p)) & 15) == 0;
-        const Pair scale2 = both(l.scale), minus = both(-ref), to2 = both(kLog2e);
+        const Pair scale2 = both(l.scale), minus = both(-off), to2 = both(kStats ? p.c : kLog2e);
         const Pair A2 = both(A), B2 = both(B);
         for (int i = from; i < to; ++i) {
             Piece next[kVecs];
@@ -652,7 +669,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) logprob_bwd_kernel(const __gri
                             const uint32_t v = max2_nan(cur[u].w[e / 2], least2);
                             a = two(low(v), high(v));
                         }
-                        a = mul2(add2(mul2(a, scale2), minus), to2);
+                        a = mul2(add2(kStats ? a : mul2(a, scale2), minus), to2);
                         const F2 x = of_two(a);
                         const F2 g = of_two(mul2(two(pow2(x.x), pow2(x.y)), fma2(B2, a, A2)));
                         if (kWide) {
@@ -681,7 +698,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) logprob_bwd_kernel(const __gri
         if (zero || !(here || __any_sync(0xffffffffu, mine))) continue;
         __syncwarp();
         auto place = [&](int col, float v, float g) {
-            const float x = v <= kLeast && ref == ref ? 0.f : fmaf(l.scale, g, weight(v));   // (a row with a NaN is one)
+            const float x = v <= kLeast && lse == lse ? 0.f : fmaf(l.scale, g, weight(v));   // (a row with a NaN is one)
             if (kWide) reinterpret_cast<float *>(out)[col] = x;
             else reinterpret_cast<bf16 *>(out)[col] = from_f32<bf16>(x);
         };
@@ -788,8 +805,9 @@ cudaError_t launch_logprob_bwd(const LogProb &l, cudaStream_t s) {
     const long long units = (long long)l.B * l.T * p.units;
     const unsigned blocks = (unsigned)std::min<long long>((units + kFewWarps - 1) / kFewWarps, 1 << 20);
     note_launches(1);
-    return l.z.wide ? launch_pdl(logprob_bwd_kernel<true>, dim3(blocks), dim3(kFewWarps * 32), 0, s, p)
-                    : launch_pdl(logprob_bwd_kernel<false>, dim3(blocks), dim3(kFewWarps * 32), 0, s, p);
+    const auto kernel = l.z.wide ? l.stats ? logprob_bwd_kernel<true, true> : logprob_bwd_kernel<true, false>
+                                 : l.stats ? logprob_bwd_kernel<false, true> : logprob_bwd_kernel<false, false>;
+    return launch_pdl(kernel, dim3(blocks), dim3(kFewWarps * 32), 0, s, p);
 }
 
 }  // namespace blk

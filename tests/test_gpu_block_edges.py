@@ -3,8 +3,8 @@ import pytest
 import torch
 
 import paper_2505_00315_gb300 as mosa
-from _block_ref import keep_mask, near, residual
-from test_gpu_block import BF, F32, INF, NAN, check_logprobs, gen, inputs, logits_of, state
+from _block_ref import keep_mask, logprobs, near, residual
+from test_gpu_block import BF, F32, INF, NAN, check_logprobs, gen, inputs, logits_of, state, targets_of
 
 pytestmark = pytest.mark.gpu
 
@@ -129,3 +129,87 @@ def test_rows_that_are_no_numbers_are_so_where_entries_are_ruled_out(V, dt):
     up = torch.ones(1, 6, 3, device="cuda")
     dz = mosa.mosa_token_logprobs_backward(z, t, r["lse"], top=idx, dtop_logp=up)
     assert torch.isnan(dz[0, :4]).all() and torch.isfinite(dz[0, 4:]).all()
+
+
+def gradients(z, t, top, scale, seed=0, stats=True):
+    """The forward's results, upstream gradients of all of them, and the logits' gradient."""
+    B, T, V = z.shape
+    r, _ = mosa.mosa_token_logprobs(z, t, top=top, scale=scale, stats=stats)
+    up = {n: torch.randn((B, T) + (top,) * (n == "dtop_logp"), generator=gen(seed + i), device="cuda")
+          for i, n in enumerate(("dlogp", "dentropy", "dlse", "dtop_logp")) if top or n != "dtop_logp"}
+    dz = mosa.mosa_token_logprobs_backward(z, t, r["stats" if stats else "lse"], r["entropy"], top=r.get("top"), scale=scale,
+                                           **up)
+    return r, up, dz
+
+
+@pytest.mark.parametrize("B,T,V,top", [(2, 13, 2000, 3), (1, 9, 1001, 0), (1, 2, 131072, 20), (1, 5, 40001, 4),
+                                       (1, 3000, 1500, 2)])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("scale", [1.0, 0.8])
+@pytest.mark.parametrize("far", [0.0, 30.0, -1000.0, 1e5])
+def test_gradient_of_logits_far_from_zero(far, scale, dt, B, T, V, top):
+    """From stats, within a bound that knows how far a logit lies from its row's largest, not from 0.  With u = 2^-24 and
+    k = (a_max - a_j): the exponent c (z - m) is off by 3 u of itself (difference, c, product) and its power by 4 u, so a term
+    by (3 k + 4) u; a sum adds up V / 64 of them one after another at most, and 16 in a tree; its inverse and two products are
+    6 u more: e_j = (V / 64 + 32 + 3 k) u relative for p_j, beside the terms' own errors in the sum, on average
+    (3 E[k] + 4) u with E[k] <= H.  ln s and t / s, of which H and log p + H are made, carry the same relative errors: of
+    quantities of at most 2 + H and 2 + H + k."""
+    u = 2.0 ** -24
+    z = (logits_of(B, T, V, F32, seed=37) + far).to(dt)
+    t = targets_of(B, T, V)
+    r, up, dz = gradients(z, t, top, scale, seed=60)
+    a = z.double() * float(torch.tensor(scale))
+    logp = torch.log_softmax(a, -1)
+    p = logp.exp()
+    H = -(p * logp).sum(-1, keepdim=True)
+    k = a.amax(-1, keepdim=True) - a
+    row = (V / 64 + 36 + 3 * H) * u
+    e = row + (V / 64 + 32 + 3 * k) * u
+    gl = torch.where(t < 0, 0.0, up["dlogp"].double())[..., None]
+    own = torch.zeros_like(p).scatter_add_(-1, t.clamp(min=0)[..., None], gl)
+    G, Ga = gl, gl.abs()
+    if top:
+        g = up["dtop_logp"].double()
+        own.scatter_add_(-1, r["top"].long(), g)
+        G, Ga = G + g.sum(-1, keepdim=True), Ga + g.abs().sum(-1, keepdim=True)
+    dH, dL = up["dentropy"].double()[..., None], up["dlse"].double()[..., None]
+    s = float(torch.tensor(scale))
+    want = s * (own + p * (dL - G - dH * (logp + H)))
+    # (the factor of p is a sum of some terms, each off by some u: 24 for up to 20 alternatives and the rest)
+    size = p * (dL.abs() + Ga + dH.abs() * (logp.abs() + H))
+    bound = s * (own.abs() * 24 * u + (e + 24 * u) * size + p * dH.abs() * (e + row) * (4 + 2 * H + k))
+    near("dlogits", dz, want, bound + 2.0 ** -126 * s * (dL.abs() + Ga + dH.abs() * 210 + 1))
+    if dt is F32:   # p of a row sums to 1
+        one = torch.ones(B, T, device="cuda")
+        p1 = mosa.mosa_token_logprobs_backward(z, None, r["stats"], dlse=one, scale=scale).double() / s
+        assert ((p1.sum(-1, keepdim=True) - 1).abs() <= (p * e).sum(-1, keepdim=True) + 2 * u).all()
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_stats_are_for_all_rows(dt):
+    """Masked rows, rows that are no numbers, large and few entries: results as without stats, and gradients within the
+    bounds of those."""
+    V = 3001
+    z = logits_of(2, 8, V, dt, seed=38)
+    low = torch.finfo(dt).min
+    z[0, 0], z[0, 1], z[0, 2, 1:], z[0, 3, :-1], z[0, 4, ::2] = -INF, low, -INF, low, -INF
+    z[0, 5, 5], z[0, 6, 7], z[1, 0, 3], z[1, 1] = NAN, INF, 1e30, NAN
+    z[1, 2], z[1, 3] = z[1, 2] * 1e20, z[1, 3] - 1e20
+    z[1, 4, :-3] = -INF
+    t = targets_of(2, 8, V)
+    t[1, 5], t[1, 6] = V, 2**40
+    for top in (0, 7):
+        for scale in (1.0, 0.5, 2.0 ** -20):
+            plain = mosa.mosa_token_logprobs(z, t, top=top, scale=scale)[0]
+            r, up, dz = gradients(z, t, top, scale, seed=70)
+            assert set(r) == set(plain) | {"stats"} and r["lse"].data_ptr() == r["stats"].data_ptr()
+            for n in plain:
+                assert torch.equal(torch.nan_to_num(r[n].double(), 7e77), torch.nan_to_num(plain[n].double(), 7e77)), n
+            up["dtop"] = up.pop("dtop_logp", None)
+            near("dlogits", dz, *logprobs(z, t, top, scale, **up)["dlogits"])
+            again = mosa.mosa_token_logprobs(z, t, top=top, scale=scale, stats=True, out=r)[0]
+            assert all(again[n] is r[n] for n in r)
+    with pytest.raises(ValueError, match="planes"):
+        mosa.mosa_token_logprobs(z, t, stats=True, out={"lse": plain["lse"]})
+    with pytest.raises(ValueError, match="stats"):
+        mosa.mosa_token_logprobs_backward(z, t, r["stats"][:2].contiguous(), dlse=plain["lse"])
