@@ -49,9 +49,32 @@ def declare(L) -> None:
         f.argtypes, f.restype = args, ret
 
 
-# What depends on shapes, strides, types and numbers alone is done once and kept as a plan, as for the window heads.
+# What depends on shapes, strides and types alone is done once and kept as a plan, as for the window heads.  Numbers in
+# which a model's layers and steps differ (scale, eps, dropout, site) make no plans of their own: a plan keeps a struct for
+# each set of them, which is written once and then only read.
 # Calls make and look for everything on the current device and its current stream; one whose tensors lie on
 # another device, or that names a stream, is made again in that one's place.
+
+_structs = 0   # that plans keep, since they were last let go
+
+
+def _numbered(plan, rng, **numbers):
+    """A reference to the plan's struct with a call's numbers, kept under them."""
+    global _structs
+    if numbers.get("dropout", 0) > 0 and rng is None:
+        raise ValueError("dropout needs rng, an int64 tensor of two numbers on the GPU")
+    s = type(plan[2]).from_buffer_copy(plan[2])
+    for name, value in numbers.items():
+        setattr(s, name, _int(value, name) if name == "site" else value)
+    if _structs >= 8192:   # (some megabytes: a site that counts steps, say)
+        for p in list(_plans.values()):
+            if type(p[0]) is dict:
+                p[0].clear()
+        _structs = 0
+    _structs += 1
+    plan[0][tuple(numbers.values())] = ref = ctypes.byref(s)
+    return ref
+
 
 def _there(t, stream, call, *args):
     """The call on ``stream``, or on the current stream of t's device."""
@@ -102,10 +125,8 @@ def _result(t, name, like, dtype):
     return MosaStrides(like[1] * like[2], like[2], 0) if t is None else _rows(t, name, like, dtype)
 
 
-def _check_rng(rng, dropout):
+def _check_rng(rng):
     if rng is None:
-        if dropout > 0:
-            raise ValueError("dropout needs rng, an int64 tensor of two numbers on the GPU")
         return
     if rng.shape != (2,) or rng.dtype != _b._torch_mod.int64 or not rng.is_contiguous():
         raise ValueError("rng must be a contiguous int64 tensor of two numbers")
@@ -122,10 +143,9 @@ def _storage(dtype, gate, gamma_post, gamma_pre, x):
             return t.dtype
 
 
-def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmoid, scale, eps, dropout, rng,
-                   site, dtype, xo, h, stats, back=None):
-    """Checks, and the library's struct.  back: dx_out, dh and the results dx, dy, dgate, dgamma_post,
-    dgamma_pre of a backward."""
+def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmoid, rng, dtype, xo, h, stats, back=None):
+    """Checks, and the library's struct without a call's numbers.  back: dx_out, dh and the results dx, dy, dgate,
+    dgamma_post, dgamma_pre of a backward."""
     torch = _b._torch_mod
     for name, t in (("x", x), ("y", y)):
         _rank(t, name, 3)
@@ -138,15 +158,15 @@ def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmo
     if gate is not None:
         kind = GATE_TOKEN if len(gate.shape) == 3 else GATE_CHANNEL
     s = MosaResidualShape(B, T, d, code[dtype], _b._dtype_code(x), _b._dtype_code(y), code[dtype],
-                          1 if post_norm else 0, 1 if pre_norm else 0, kind, 1 if sigmoid else 0, _int(site, "site"), scale,
-                          eps, dropout, _rows(x, "x"), _rows(y, "y", x.shape))
+                          1 if post_norm else 0, 1 if pre_norm else 0, kind, 1 if sigmoid else 0, 0, 1.0, 0.0, 0.0,
+                          _rows(x, "x"), _rows(y, "y", x.shape))
     _vector(gamma_post, "gamma_post", (d,), dtype)
     _vector(gamma_pre, "gamma_pre", (d,), dtype)
     if kind == GATE_TOKEN:
         s.g = _rows(gate, "gate", x.shape, dtype)
     else:
         _vector(gate, "gate", (d,), dtype)
-    _check_rng(rng, dropout)
+    _check_rng(rng)
     _vector(stats, "stats", (2, B, T), torch.float32)
     need = 0
     if back is None:
@@ -167,7 +187,7 @@ def _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm, sigmo
         _vector(dgpost, "dgamma_post", (d,), torch.float32)
         _vector(dgpre, "dgamma_pre", (d,), torch.float32)
         need = int(_b.load().mosa_residual_workspace_bytes(ctypes.byref(s)))
-    return ctypes.byref(s), need, s, (dtype, x.device, x.shape, (2, B, T))
+    return {}, need, s, (dtype, x.device, x.shape, (2, B, T))
 
 
 def _options(post_norm, pre_norm, sigmoid, scale, eps, dropout, site):
@@ -202,12 +222,14 @@ def mosa_residual_forward(x, y, gate=None, gamma_post=None, gamma_pre=None, post
                None if gate is None else (gate.shape, gate.stride(), gate.dtype),
                None if gamma_post is None else (gamma_post.shape, gamma_post.stride(), gamma_post.dtype),
                None if gamma_pre is None else (gamma_pre.shape, gamma_pre.stride(), gamma_pre.dtype),
-               None if rng is None else (rng.shape, rng.stride(), rng.dtype), post_norm, pre_norm, sigmoid, scale, eps,
-               dropout, site, dtype, dev, (_sig(xo), _sig(h), _sig(stats)) if out else None)
+               None if rng is None else (rng.shape, rng.stride(), rng.dtype), post_norm, pre_norm, sigmoid, dtype, dev,
+               (_sig(xo), _sig(h), _sig(stats)) if out else None)
     except AttributeError:
         _bad(("x", x), ("y", y), ("gate", gate), ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng))
     plan = _plans.get(key) or _keep(key, _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
-                                                        sigmoid, scale, eps, dropout, rng, site, dtype, xo, h, stats))
+                                                        sigmoid, rng, dtype, xo, h, stats))
+    ref = plan[0].get((scale, eps, dropout, site)) or _numbered(plan, rng, scale=scale, eps=eps, dropout=dropout,
+                                                                site=site)
     if not (dev >= 0 and y.get_device() == dev and (gate is None or gate.get_device() == dev)
             and (gamma_post is None or gamma_post.get_device() == dev)
             and (gamma_pre is None or gamma_pre.get_device() == dev) and (rng is None or rng.get_device() == dev)
@@ -224,7 +246,7 @@ def mosa_residual_forward(x, y, gate=None, gamma_post=None, gamma_pre=None, post
     if stats is None:
         stats = torch.empty(short, dtype=torch.float32, device=device)
     rc = (_b._lib or _b.load()).mosa_residual_forward(
-        plan[0], x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
+        ref, x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
         None if gamma_post is None else gamma_post.data_ptr(), None if gamma_pre is None else gamma_pre.data_ptr(),
         None if rng is None else rng.data_ptr(), xo.data_ptr(), None if h is None else h.data_ptr(),
         stats.data_ptr(), torch._C._cuda_getCurrentRawStream(dev))
@@ -262,8 +284,8 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
                None if gate is None else (gate.shape, gate.stride(), gate.dtype),
                None if gamma_post is None else (gamma_post.shape, gamma_post.stride(), gamma_post.dtype),
                None if gamma_pre is None else (gamma_pre.shape, gamma_pre.stride(), gamma_pre.dtype),
-               None if rng is None else (rng.shape, rng.stride(), rng.dtype), post_norm, pre_norm, sigmoid, scale, eps,
-               dropout, site, dtype, dev, stats.shape, stats.stride(), stats.dtype,
+               None if rng is None else (rng.shape, rng.stride(), rng.dtype), post_norm, pre_norm, sigmoid, dtype, dev,
+               stats.shape, stats.stride(), stats.dtype,
                None if dx_out is None else (dx_out.shape, dx_out.stride(), dx_out.dtype),
                None if dh is None else (dh.shape, dh.stride(), dh.dtype),
                (_sig(dx), _sig(dy), _sig(dg), _sig(dgpost), _sig(dgpre)) if out else None)
@@ -271,8 +293,10 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
         _bad(("x", x), ("y", y), ("stats", stats), ("dx_out", dx_out), ("dh", dh), ("gate", gate),
              ("gamma_post", gamma_post), ("gamma_pre", gamma_pre), ("rng", rng))
     plan = _plans.get(key) or _keep(key, _residual_plan(x, y, gate, gamma_post, gamma_pre, post_norm, pre_norm,
-                                                        sigmoid, scale, eps, dropout, rng, site, dtype, None, None, stats,
+                                                        sigmoid, rng, dtype, None, None, stats,
                                                         (dx_out, dh, dx, dy, dg, dgpost, dgpre)))
+    ref = plan[0].get((scale, eps, dropout, site)) or _numbered(plan, rng, scale=scale, eps=eps, dropout=dropout,
+                                                                site=site)
     if not (dev >= 0 and y.get_device() == dev and stats.get_device() == dev
             and (dx_out is None or dx_out.get_device() == dev) and (dh is None or dh.get_device() == dev)
             and (gate is None or gate.get_device() == dev) and (gamma_post is None or gamma_post.get_device() == dev)
@@ -305,7 +329,7 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
         g["dgamma_pre"] = dgpre = torch.empty(width, dtype=f32, device=device) if dgpre is None else dgpre
     workspace = _space(workspace, plan[1], device)
     rc = (_b._lib or _b.load()).mosa_residual_backward(
-        plan[0], x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
+        ref, x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
         None if gamma_post is None else gamma_post.data_ptr(), None if gamma_pre is None else gamma_pre.data_ptr(),
         None if rng is None else rng.data_ptr(), stats.data_ptr(), None if dx_out is None else dx_out.data_ptr(),
         None if dh is None else dh.data_ptr(), dx.data_ptr(), dy.data_ptr(), None if dg is None else dg.data_ptr(),
@@ -318,12 +342,11 @@ def mosa_residual_backward(x, y, stats, dx_out, dh, gate=None, gamma_post=None, 
 
 # ------------------------------------------------------------------ dropout
 
-def _dropout_plan(x, p, rng, site, y):
+def _dropout_plan(x, rng, y):
     _rank(x, "x", 3)
-    _check_rng(rng, p)
-    s = MosaDropoutShape(*x.shape, _b._dtype_code(x), _int(site, "site"), p, _rows(x, "x"),
-                         _result(y, "out y", x.shape, x.dtype))
-    return ctypes.byref(s), 0, s
+    _check_rng(rng)
+    s = MosaDropoutShape(*x.shape, _b._dtype_code(x), 0, 0.0, _rows(x, "x"), _result(y, "out y", x.shape, x.dtype))
+    return {}, 0, s
 
 
 def mosa_dropout(x, p: float, rng, site: int = 0, out=None, stream=None):
@@ -339,16 +362,17 @@ def mosa_dropout(x, p: float, rng, site: int = 0, out=None, stream=None):
         y = out.get("y") if out else None
         if not (type(p) is float and type(site) is int):
             p, site = float(p), _int(site, "site")
-        key = (8, x.shape, x.stride(), x.dtype, p, site, None if rng is None else (rng.shape, rng.stride(), rng.dtype),
+        key = (8, x.shape, x.stride(), x.dtype, None if rng is None else (rng.shape, rng.stride(), rng.dtype),
                None if y is None else _sig(y))
     except AttributeError:
         _bad(("x", x), ("rng", rng), ("out y", y))
-    plan = _plans.get(key) or _keep(key, _dropout_plan(x, p, rng, site, y))
+    plan = _plans.get(key) or _keep(key, _dropout_plan(x, rng, y))
+    ref = plan[0].get((p, site)) or _numbered(plan, rng, dropout=p, site=site)
     if not (dev >= 0 and (rng is None or rng.get_device() == dev) and (y is None or y.get_device() == dev)):
         _elsewhere(dev, ("x", x), ("rng", rng), ("out y", y))
     if y is None:
         y = torch.empty_like(x) if x.is_contiguous() else _new(x)
-    rc = (_b._lib or _b.load()).mosa_dropout(plan[0], x.data_ptr(), None if rng is None else rng.data_ptr(), y.data_ptr(),
+    rc = (_b._lib or _b.load()).mosa_dropout(ref, x.data_ptr(), None if rng is None else rng.data_ptr(), y.data_ptr(),
                                              torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _b._check(rc, "mosa_dropout")
@@ -357,7 +381,7 @@ def mosa_dropout(x, p: float, rng, site: int = 0, out=None, stream=None):
 
 # -------------------------------------------------------- log probabilities
 
-def _logprob_plan(logits, targets, top, scale, results, stats=None, keeps=False, back=None):
+def _logprob_plan(logits, targets, top, results, stats=None, keeps=False, back=None):
     """results: (name, tensor, columns or 0, type) of [B,T] or [B,T,columns] tensors to be checked; stats [3,B,T],
     which the call ``keeps`` or reads."""
     torch = _b._torch_mod
@@ -374,11 +398,11 @@ def _logprob_plan(logits, targets, top, scale, results, stats=None, keeps=False,
     _vector(stats, "stats", (3, B, T), torch.float32)
     s = MosaLogprobShape(B, T, V, _b._dtype_code(logits),
                          1 if targets is not None and targets.dtype == torch.int64 else 0,
-                         _int(top, "top"), scale, 1 if keeps else 0, _rows(logits, "logits"))
+                         _int(top, "top"), 1.0, 1 if keeps else 0, _rows(logits, "logits"))
     if back is not None:
         s.dz = _result(back[0], "dlogits", logits.shape, logits.dtype)
-        return ctypes.byref(s), 0, s
-    return (ctypes.byref(s), int(_b.load().mosa_token_logprobs_workspace_bytes(ctypes.byref(s))), s,
+        return {}, 0, s
+    return ({}, int(_b.load().mosa_token_logprobs_workspace_bytes(ctypes.byref(s))), s,
             (logits.device, (B, T), (B, T, top), (3, B, T)))
 
 
@@ -410,13 +434,15 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
             if lse is not None and (sums is None or lse.data_ptr() != sums.data_ptr()):
                 raise ValueError("with stats, lse is the first of its planes: out may hold stats alone")
         key = (9, logits.shape, logits.stride(), logits.dtype,
-               None if targets is None else (targets.shape, targets.stride(), targets.dtype), top, scale, dev,
-               (_sig(logp), _sig(ent), _sig(lse), _sig(idx), _sig(tlp), _sig(sums)) if out else None, True if stats else False)
+               None if targets is None else (targets.shape, targets.stride(), targets.dtype), top, dev,
+               (_sig(logp), _sig(ent), _sig(lse), _sig(idx), _sig(tlp), _sig(sums)) if out else None,
+               True if stats else False)
     except AttributeError:
         _bad(("logits", logits), ("targets", targets))
     plan = _plans.get(key) or _keep(key, _logprob_plan(
-        logits, targets, top, scale, [("logp", logp, 0, f32), ("entropy", ent, 0, f32), ("lse", lse, 0, f32),
-                                      ("top", idx, top, torch.int32), ("top_logp", tlp, top, f32)], sums, stats))
+        logits, targets, top, [("logp", logp, 0, f32), ("entropy", ent, 0, f32), ("lse", lse, 0, f32),
+                               ("top", idx, top, torch.int32), ("top_logp", tlp, top, f32)], sums, stats))
+    ref = plan[0].get((scale,)) or _numbered(plan, None, scale=scale)
     if not (dev >= 0 and (targets is None or targets.get_device() == dev)
             and (workspace is None or workspace.get_device() == dev)
             and (out is None or _all_on(dev, logp, ent, lse, idx, tlp, sums))):
@@ -438,7 +464,7 @@ def mosa_token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, 
         r["top_logp"] = tlp = torch.empty(tops, dtype=f32, device=device) if tlp is None else tlp
     workspace = _space(workspace, plan[1], device)
     rc = (_b._lib or _b.load()).mosa_token_logprobs(
-        plan[0], logits.data_ptr(), None if targets is None else targets.data_ptr(),
+        ref, logits.data_ptr(), None if targets is None else targets.data_ptr(),
         None if logp is None else logp.data_ptr(), ent.data_ptr(), lse.data_ptr(), _ptr(idx), _ptr(tlp),
         workspace.data_ptr(), workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
@@ -467,7 +493,7 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
         if type(scale) is not float:
             scale = _float(scale)
         key = (10, logits.shape, logits.stride(), logits.dtype, _sig(targets), lse.shape, lse.stride(), lse.dtype,
-               _sig(entropy), _sig(dlogp), _sig(dentropy), _sig(dlse), _sig(top), _sig(dtop_logp), scale, _sig(dz))
+               _sig(entropy), _sig(dlogp), _sig(dentropy), _sig(dlse), _sig(top), _sig(dtop_logp), _sig(dz))
     except AttributeError:
         _bad(("logits", logits), ("lse", lse), ("targets", targets), ("entropy", entropy), ("dlogp", dlogp),
              ("dentropy", dentropy), ("dlse", dlse), ("top", top), ("dtop_logp", dtop_logp), ("dlogits", dz))
@@ -487,11 +513,12 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
             raise TypeError("dentropy needs entropy, the forward's")
         kept = len(lse.shape) == 3
         plan = _keep(key, _logprob_plan(
-            logits, targets, n, scale,
+            logits, targets, n,
             [("lse", None if kept else lse, 0, f32), ("entropy", entropy, 0, f32), ("dlogp", dlogp, 0, f32),
              ("dentropy", dentropy, 0, f32), ("dlse", dlse, 0, f32), ("top", top, n, torch.int32),
              ("dtop_logp", dtop_logp, n, f32)],
             lse if kept else None, kept, (dz,)))
+    ref = plan[0].get((scale,)) or _numbered(plan, None, scale=scale)
     if not (dev >= 0 and lse.get_device() == dev
             and _all_on(dev, targets, entropy, dlogp, dentropy, dlse, top, dtop_logp, dz)):
         _elsewhere(dev, ("logits", logits), ("targets", targets), ("lse", lse), ("entropy", entropy), ("dlogp", dlogp),
@@ -499,7 +526,7 @@ def mosa_token_logprobs_backward(logits, targets, lse, entropy=None, dlogp=None,
     if dz is None:
         dz = _new(logits)
     rc = (_b._lib or _b.load()).mosa_token_logprobs_backward(
-        plan[0], logits.data_ptr(), _ptr(targets), lse.data_ptr(), _ptr(entropy), _ptr(top), _ptr(dlogp), _ptr(dentropy),
+        ref, logits.data_ptr(), _ptr(targets), lse.data_ptr(), _ptr(entropy), _ptr(top), _ptr(dlogp), _ptr(dentropy),
         _ptr(dlse), _ptr(dtop_logp), dz.data_ptr(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _b._check(rc, "mosa_token_logprobs_backward")
