@@ -110,6 +110,47 @@ def test_gradient_of_a_saturated_gate(dt, xt, T, d, gate):
         near(n, t, *want[n])
 
 
+@pytest.mark.parametrize("dt,xt,T,d", [*WIDTHS, (BF, F32, 40, 5000), (F32, F32, 3300, 1024), (BF, F32, 3300, 2048)])
+@pytest.mark.parametrize("gate", ["channel", "token"])
+def test_cut_sequences_without_a_gradient_of_h(dt, xt, T, d, gate):
+    """Tokens 2 to T + 1 of T + 5, in and out, and what lies around them as it was; without dx_out too."""
+    B = 3
+    s, dx_out, _ = inputs(B, T + 5, d, dt, xt, xt, gate=gate, seed=39)
+    cut = lambda t: t[:, 2:2 + T]   # noqa: E731
+    s = {n: cut(v) if v is not None and v.dim() == 3 else v for n, v in s.items()}
+    kw = dict(scale=0.5, dropout=0.2, rng=state(), sigmoid=gate == "token")
+    types = {"dx": xt, "dy": dt, **({"dgate": dt} if gate == "token" else {})}
+    for up in (cut(dx_out), None):
+        room = {n: torch.full((B, T + 5, d), 7.0, device="cuda", dtype=v) for n, v in types.items()}
+        stats = mosa.mosa_residual_forward(**s, **kw)[2]
+        g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=up, dh=None, out={n: cut(v) for n, v in room.items()}, **s, **kw)
+        want = residual(**s, dx_out=up, dh=None, backward=True, **kw)
+        for n in g:
+            near(n, g[n], *want[n])
+        for n, v in room.items():
+            assert (v[:, :2] == 7).all() and (v[:, 2 + T:] == 7).all(), n
+
+
+@pytest.mark.parametrize("B,T", [(1, 3), (3, 1), (2, 2)])
+@pytest.mark.parametrize("with_dh", [True, False])
+def test_backward_of_rows_past_32_bits(B, T, with_dh):
+    """A stream and its gradient whose rows, or sequences, lie further than 2^32 bytes apart; dx takes dx_out's place."""
+    d, far = 1024, 2**31 + 512
+    room = torch.zeros(2 * far + 8192, device="cuda", dtype=BF)
+    s, dx_out, dh = inputs(B, T, d, gate="channel", seed=40)
+    stride = (far, 4096, 1) if T == 2 else (far, far, 1)
+    x, up = (room.as_strided((B, T, d), stride, i * 2048) for i in range(2))
+    x.copy_(s["x"]), up.copy_(dx_out)
+    dh = dh if with_dh else None
+    kw = dict(dropout=0.1, rng=state(), scale=0.5)
+    want = residual(**s, dx_out=dx_out, dh=dh, backward=True, **kw)
+    stats = mosa.mosa_residual_forward(**{**s, "x": x}, **kw)[2]
+    g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=up, dh=dh, out={"dx": up}, **{**s, "x": x}, **kw)
+    assert g["dx"] is up and torch.equal(x, s["x"])
+    for n in g:
+        near(n, g[n], *want[n])
+
+
 # -------------------------------------------------------- log probabilities
 
 @pytest.mark.parametrize("V", [40, 3001, 40000])
@@ -213,3 +254,32 @@ def test_stats_are_for_all_rows(dt):
         mosa.mosa_token_logprobs(z, t, stats=True, out={"lse": plain["lse"]})
     with pytest.raises(ValueError, match="stats"):
         mosa.mosa_token_logprobs_backward(z, t, r["stats"][:2].contiguous(), dlse=plain["lse"])
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("stats", [False, True])
+def test_gradient_in_place_where_warps_share_a_row(dt, stats):
+    """Each warp reads the target and the alternatives in its own columns before it writes any: rows of 40001 entries, with
+    alternatives on both sides of every step's border (1024 columns of bf16, 512 of fp32) and the target at it.  Bit for bit
+    what the call gives elsewhere, and that within the bounds."""
+    V, K = 40001, 1024 if dt is BF else 512
+    T = V // K
+    z = logits_of(1, T, V, dt, seed=41)
+    border = torch.arange(1, T + 1, device="cuda") * K
+    t = border[None].contiguous()
+    idx = (border[:, None] + torch.arange(-16, 16, device="cuda")).clamp(max=V - 1).int()[None].contiguous()
+    r, _ = mosa.mosa_token_logprobs(z, t, scale=0.7, stats=stats)
+    up, up_top = torch.randn(1, T, generator=gen(42), device="cuda"), torch.randn(1, T, 32, generator=gen(43), device="cuda")
+    kw = dict(entropy=r["entropy"], dlogp=up, dentropy=up, top=idx, dtop_logp=up_top, scale=0.7)
+    lse = r["stats" if stats else "lse"]
+    want = mosa.mosa_token_logprobs_backward(z, t, lse, **kw)
+    p = torch.softmax(z.double() * float(torch.tensor(0.7)), -1)
+    own = torch.zeros_like(p).scatter_add_(-1, t[..., None], up.double()[..., None])
+    own.scatter_add_(-1, idx.long(), up_top.double())
+    G, H = own.sum(-1, keepdim=True), -(p * p.log()).sum(-1, keepdim=True)
+    dz = 0.7 * (own - p * (G + up.double()[..., None] * (p.log() + H)))
+    # (logits below 20, so that lse's rounding is 2^-19; sums of V / 64 = 626 terms 2^-14; some 40 additions of upstream values)
+    size = own.abs() + p * (own.abs().sum(-1, keepdim=True) + up.abs().double()[..., None] * (p.log().abs() + H))
+    near("dlogits", want, dz, 2.0 ** -13 * size)
+    got = mosa.mosa_token_logprobs_backward(z, t, lse, out={"dlogits": z}, **kw)
+    assert got is z and torch.equal(got, want)
