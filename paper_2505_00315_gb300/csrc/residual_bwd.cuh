@@ -118,14 +118,20 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             const Oct g = arrived<kFast>(in + g_off, gw, l, c, gs);
             return !r.sigmoid ? g : slope ? logistic_slope(g) : logistic(g);
         };
-        // What both rounds need, from what the ring holds.
+        // What both rounds need, from what the ring holds.  kEarly: all of it is fetched first (us, first / when needed: B2 T8192
+        // d4096 243.7 / 246.3, 4096 rows of 8192 with a gate per channel and dropout 140 / 144; with 8 columns a thread, which
+        // spills sooner, 16384 rows of 768 in fp32 71.6 / 70.4).
+        constexpr bool kEarly = C > 1;
         struct Values {
             Oct yh, xh, cg, base;   // cg: c g (0 where dropped); base: dx' + r_x e
         };
         auto values = [&](int c, Oct &u, Oct &dh, Oct &e) {
             Values v;
             const Oct y = arrived<kFast>(in + y_off, yw, l, c, ys);
+            Oct x = zeros();
+            if (kSecond && kEarly) x = arrived<kFast>(in, xw, l, c, xs);
             const Oct dxo = arrived<kFast>(in + dxo_off, xw, l, c, dxos);
+            if (kSecond && kEarly) dh = arrived<kFast>(in + dh_off, hw, l, c, dhs);
             v.cg = token ? times(token_gate(c, false), unit)
                    : r.gate == MOSA_GATE_NONE ? all_of(unit) : vector_at<C, false, Ty>(p, l, 2, c, unit);
             v.yh = times(y, ry);
@@ -136,8 +142,10 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             }
             u = times(times(v.yh, vector_at<C, false, Ty>(p, l, 0, c, unit)), v.cg);
             if (kSecond) {
-                const Oct x = arrived<kFast>(in, xw, l, c, xs);
-                dh = arrived<kFast>(in + dh_off, hw, l, c, dhs);
+                if (!kEarly) {
+                    x = arrived<kFast>(in, xw, l, c, xs);
+                    dh = arrived<kFast>(in + dh_off, hw, l, c, dhs);
+                }
                 v.xh = times(plus(x, u), rx);
                 e = times(dh, vector_at<C, false, Ty>(p, l, 1, c, unit));
                 v.base = fused(e, rx, dxo);
@@ -155,12 +163,12 @@ __global__ void __launch_bounds__(kMost * 32, 1) residual_bwd_kernel(const __gri
             Oct u, dh, e;
             const Values v = values(c, u, dh, e);
             if (kStay) stay[c] = v;
-            add_products(s1, u, v.base);
             if (kSecond) {
                 acc[1][c] = fused(dh, v.xh, acc[1][c]);
                 add_products(s0, e, v.xh);
-                add_products(s2, u, v.xh);
             }
+            add_products(s1, u, v.base);
+            if (kSecond) add_products(s2, u, v.xh);
         }
         const float4 s = row_sums(sum_of(s0), sum_of(s1), sum_of(s2), l.red + turn * l.W, l.W, l.w, l.lane, l.group);
         turn ^= 1;
