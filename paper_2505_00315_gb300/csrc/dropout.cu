@@ -1,8 +1,10 @@
 // Dropout without a stored mask: y = keep/(1-p) x, the words of a token's columns from their counters
-// (philox.cuh).  Memory bound: x and y move once; two counters for eight columns are some ten
-// instructions a value.  A warp takes a few runs of 256 columns (or of some whole rows, where those are
+// (philox.cuh).  Memory bound in fp32: x and y move once; two counters for eight columns are some ten
+// instructions of 25 a value (bf16 23).  A warp takes a few runs of 256 columns (or of some whole rows, where those are
 // short), one after another in memory, all loads first.  fp32 B4 T4096 d1024 22.3 us (6.0 TB/s, 89% of the copy rate;
 // runs of whole units of 1024 columns a warp 29.7); B8 T1024 d512 bf16 6.8 (10.8), one wave.
+// bf16 B4 T4096 d1024 18.0, 55% of the copy rate: as many instructions for half the bytes, with 59% of the issue slots busy.
+// Rows that are not whole pieces go value by value: 16384 of 1001 fp32 49, bf16 43.
 #include <algorithm>
 
 #include "block.h"

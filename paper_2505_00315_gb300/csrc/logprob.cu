@@ -13,7 +13,7 @@
 // A warp takes a row, or 2, 4 or 8 of a block share one where rows are fewer, or some blocks, whose
 // results a second kernel joins.  Rows move in 16-byte pieces wherever they start: a row is cut at the
 // addresses' multiples of 16, its first and last pieces are read value by value.
-// us and share of the copy rate, bf16: 16384 rows of 32768 forward 170 (93%), backward 312 (all of it); 4096 rows of 50001
+// us and share of the copy rate, bf16: 16384 rows of 32768 forward 170 (93%), backward 312 (all of it; from m and s 318); 4096 rows of 50001
 // forward 70 (86%), with 5 alternatives 76.5 (79%: 7.7 instructions a value, and each warp's end a chain); fp32, 1000 rows
 // of 32003 with 8: 27.5 and 44 (68%, 86%); 8 rows of 131072 with 20: 8.6, two launches.
 //

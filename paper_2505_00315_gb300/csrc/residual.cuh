@@ -547,7 +547,6 @@ inline void shape(Args &p, bool backward, int *blocks, int *times, int *bytes) {
     const int each = times_of(r, backward, &p.most);
     p.warps = (r.d + 256 * each - 1) / (256 * each);
     *times = (r.d + 256 * p.warps - 1) / (256 * p.warps);   // (no more than the width asks for)
-    if (backward && *times == 3) *times = 4;
     // (a piece more where one may be cut by a row's beginning)
     bool vec = true;
     for (const Rows *m : all) vec = vec && (m->p == nullptr || m->vec);

@@ -9,8 +9,9 @@
 // x, y, dx', dh (and a gate per token) come in, dx, dy (and the gate's gradient) go out, once.  What bounds it at bf16 is the chain of
 // a row (arrival, sums over the warps, second round: 2 us) on the few warps that 250 registers a thread leave; at fp32 and
 // at wide rows the bytes.  us and share of the copy rate, the second kernel's 5 us among them: B4 T4096 d1024, fp32 y and dh, gate
-// per channel, dropout 54 (74%); B2 T8192 d4096, fp32 stream, gate per token, dropout 242 (90%); fp32, 16384 rows of
-// 2048, 127 (93%).  A spill of a few registers costs a third (see times_of).
+// per channel, dropout 54 (74%); B2 T8192 d4096, fp32 stream, gate per token, dropout 244 (89%); fp32, 16384 rows of
+// 2048, 128 (92%).  A spill of two registers cost a fifth (16384 rows of 768, fp32 stream, y and dh: 66 us, 56 without); the kernels of
+// 16 warps that still have some (4 to 24 bytes) were not seen to gain from less.
 #pragma once
 
 #include "residual.cuh"

@@ -3,7 +3,7 @@
 // with r = 1/sqrt(mean of squares + eps).  Layout and tools: residual.cuh.
 // Memory bound: x, y (and a gate per token) come in, x' and h go out, once; a row's squares are summed twice, of y and of
 // x', which is the chain of a row.  us and share of the copy rate: B4 T4096 d1024 with fp32 y 28.7 (86%), with dropout 30
-// (82%: the random words are 14 of its 29 instructions a value); B2 T8192 d4096, fp32 stream, gate per token, dropout 151
+// (83%: the random words are 11 of its 29 instructions a value); B2 T8192 d4096, fp32 stream, gate per token, dropout 151
 // (91%); eight tokens of 1024: 2.9.
 #include "residual.cuh"
 
