@@ -179,6 +179,10 @@ mosa_status mosa_residual_backward(const mosa_residual_shape *shape, const void 
         return MOSA_ERR_INVALID_ARG;
     if ((st = check_space(workspace, workspace_bytes, residual_workspace(r))) != MOSA_OK) return st;
     r.stats = const_cast<float *>(stats);
+    if (shape->dropout >= 1.0) {   // nothing of y counts, nor of its norm, whatever they are
+        r.post = 0;
+        r.gpost = vec_of(nullptr, shape->dtype);
+    }
     if (dx_out != nullptr) r.dxo = rows_of(dx_out, str[5], shape->x_dtype);
     if (shape->pre_norm && dh != nullptr) r.dh = rows_of(dh, str[6], shape->dh_dtype);
     r.dx = rows_of(dx, str[7], shape->x_dtype);

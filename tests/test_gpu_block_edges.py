@@ -89,6 +89,20 @@ def test_a_dropped_infinity_of_a_normed_row_does_not_count(dt, xt, T, d, gate):
 
 
 @pytest.mark.parametrize("dt,xt,T,d", WIDTHS)
+@pytest.mark.parametrize("gate", ["none", "channel", "token"])
+def test_a_block_that_is_dropped_whole_does_not_count(dt, xt, T, d, gate):
+    """Rows of NaN, of infinities, and of zeros whose norm has no eps: gradients know nothing of them."""
+    s, dx_out, dh = inputs(2, T, d, dt, xt=xt, gate=gate, seed=44)
+    kw = dict(dropout=1.0, rng=state(10), scale=0.5, eps=0.0)
+    want = residual(**s, dx_out=dx_out, dh=dh, backward=True, **kw)
+    s["y"][0, ::3], s["y"][0, 1::3], s["y"][1, ::2, 0] = 0.0, NAN, INF
+    x, h, stats = mosa.mosa_residual_forward(**s, **kw)
+    g, _ = mosa.mosa_residual_backward(stats=stats, dx_out=dx_out, dh=dh, **s, **kw)
+    for n, t in {"x": x, "h": h, **g}.items():
+        near(n, t, *want[n])
+
+
+@pytest.mark.parametrize("dt,xt,T,d", WIDTHS)
 @pytest.mark.parametrize("gate", ["channel", "token"])
 def test_gradient_of_a_saturated_gate(dt, xt, T, d, gate):
     """Through a sigmoid s of gates far from 0, where 1 - s is not what fp32 keeps of s.  The gradient is that of the
